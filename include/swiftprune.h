@@ -392,6 +392,151 @@ sp_status sp_select_24_compressed(sp_ctx *ctx, const void *W, sp_dtype dtype, in
 sp_status sp_apply_mask(const void *W, sp_dtype dtype, int64_t n_rows, int64_t n_cols, int64_t ldw,
                         const uint32_t *mask, void *W_out, int64_t ldo, sp_stream stream);
 
+/* ------------------------------------------------------------------ microscaled 4-bit weights */
+
+/*
+ * A pruned matrix held in 4 bits per weight plus a scale byte for every 32 (17/32 byte per
+ * weight), and its product with activations.  The format is microscaled 4-bit floating point: in
+ * every block of 32 consecutive columns of a row (the last block of a row may be short)
+ *     value = code * 2^(byte - 127),   code in {0, .5, 1, 1.5, 2, 3, 4, 6} with a sign,
+ *     byte  = floor(log2 max|w|) - 2 + 127, at least 0;
+ * codes are nearest to w / 2^(byte - 127), ties to the even code, magnitudes above 6 become 6.  A
+ * weight of 0 keeps the value 0, so pruning survives.  A block that holds a NaN or an infinity
+ * gets byte 255 and all its values are NaN.  Layout (the library's own):
+ *   codes   [n_rows, ldc bytes]: two codes per byte, the even column in the low half (bit 3 of a
+ *           code: sign, bits 2..0: index into the list above); block b of a row takes the bytes
+ *           16b .. 16b+15; columns past n_cols hold code 0.  16-byte aligned, ldc a multiple of
+ *           16 and >= 16 * ceil(n_cols / 32);
+ *   scales  sp_mx4_scale_bytes(n_rows, n_cols) bytes, 16-byte aligned: tiles of 512 bytes for 128
+ *           rows x 4 blocks (n_cols / 128 tiles, rounded up, for the first 128 rows, and so on);
+ *           byte (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4 of a tile belongs to row r, block b; the
+ *           bytes of rows and blocks that do not exist are 0.
+ * These calls need no context and work on the CURRENT device.
+ */
+
+/* Size of the scale array of an n_rows x n_cols matrix; 0 for an empty one or negative sizes. */
+int64_t sp_mx4_scale_bytes(int64_t n_rows, int64_t n_cols);
+
+/*
+ * Quantises W [n_rows, n_cols] (leading dimension ldw).  mask (nullable, the layout of the
+ * selection calls) prunes on the way: weights whose keep bit is 0 count as 0.
+ */
+sp_status sp_mx4_quantize(const void *W, sp_dtype dtype, int64_t n_rows, int64_t n_cols,
+                          int64_t ldw, const uint32_t *mask, uint8_t *codes, int64_t ldc,
+                          uint8_t *scales, sp_stream stream);
+
+/* The way back: W_out [n_rows, n_cols] = the values, rounded to dtype (exact where the codes
+ * came from a matrix of that dtype). */
+sp_status sp_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales,
+                            int64_t n_rows, int64_t n_cols, sp_dtype dtype, void *W_out,
+                            int64_t ldo, sp_stream stream);
+
+/*
+ * Y [n_tokens, n_rows] = X [n_tokens, n_cols] V^T, V the values of (codes, scales), sums in
+ * binary32, rounded once to dtype (that of X and Y).  mode:
+ *   SP_MX4_A16   X as it is (what decoding steps use);
+ *   SP_MX4_A4    X quantised like the weights first, 32 channels at a time (what long prompts
+ *                use: both operands then go to the 4-bit tensor cores as they are).
+ * workspace: sp_mx4_linear_workspace bytes of device memory, 16-byte aligned, contents arbitrary
+ * before and after (NULL where that is 0).  n_cols >= 1.  Y must not overlap X or the workspace.
+ */
+typedef enum { SP_MX4_A16 = 0, SP_MX4_A4 = 1 } sp_mx4_mode;
+sp_status sp_mx4_linear_workspace(int64_t n_tokens, int64_t n_rows, int64_t n_cols, int mode,
+                                  int64_t *bytes /* host */);
+sp_status sp_mx4_linear(const void *X, sp_dtype dtype, int64_t n_tokens, int64_t ldx,
+                        const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t n_rows,
+                        int64_t n_cols, int mode, void *Y, int64_t ldy, void *workspace,
+                        int64_t workspace_bytes, sp_stream stream);
+
+/* ------------------------------------------------------------------ 8-bit key/value cache */
+
+/*
+ * Keys and values held as 8-bit floats (e4m3: sign, 4 exponent bits, 3 mantissa bits, no
+ * infinities) with one power-of-two scale for each block of tokens and head, K and V apart:
+ *     value = code * scale,  scale = 2^e,  e the least whole number >= -126 with
+ *     max|v| <= 448 * 2^e over the block's finite values (a floating code loses no precision to
+ *     a power-of-two scale); codes are nearest to v / scale, ties to even; a NaN or an infinity
+ *     is stored as NaN.
+ * A block holds block_tokens consecutive tokens of one sequence for every head; token j of
+ * sequence b lies in block table[b, j / block_tokens] at place j % block_tokens.  A table entry
+ * outside [0, n_blocks) names no block: its tokens are not written and take no part.
+ * All pointers are device pointers; k and v 16-byte aligned.  Requirements: head_dim 64 or 128,
+ * block_tokens 16, 32 or 64 (else SP_ERR_SHAPE).  The calls work on the CURRENT device.
+ */
+typedef struct {
+    void *k, *v;               /* codes [n_blocks, n_kv_heads, block_tokens, head_dim] */
+    float *k_scale, *v_scale;  /* [n_blocks, n_kv_heads] */
+    const int32_t *table;      /* [n_seqs, ld_table]; the first table_cols of a row are used */
+    int64_t n_blocks, n_seqs, table_cols, ld_table;
+    int n_kv_heads, head_dim, block_tokens;
+} sp_cache;
+
+/* Strides in elements of a [sequence, token, head, head_dim] tensor of 16-bit floats; a head's
+ * values are consecutive. */
+typedef struct {
+    int64_t seq, token, head;
+} sp_strides;
+
+/*
+ * Writes the tokens K, V [n_seqs, n_new, n_kv_heads, head_dim] at the places start[b] ..
+ * start[b] + count[b] - 1 of every sequence (start, count: device int32; count nullable: n_new
+ * everywhere; larger counts and places past the table are cut off, negative ones write nothing).
+ * A block that already holds tokens before start[b] keeps its scale, or, where the new tokens
+ * need a larger one, has its codes brought to that; a block whose first token is new starts
+ * afresh.  Places after the written ones are left as they are.
+ */
+sp_status sp_cache_append(const sp_cache *cache /* host struct */, const void *K,
+                          const sp_strides *k_strides, const void *V, const sp_strides *v_strides,
+                          sp_dtype dtype, int64_t n_new, const int32_t *start,
+                          const int32_t *count, sp_stream stream);
+
+/*
+ * Attention of n_q query tokens per sequence over the cache:
+ *     O[b, i, h] = sum_j p[j] v[j],  p = softmax over j of scale * q[b, i, h] . k[j]
+ * with lens[b] (device int32) tokens in the cache, the call's own n_q included: query i sits at
+ * place lens[b] - n_q + i and sees the tokens up to it.  n_heads is a multiple of n_kv_heads;
+ * consecutive heads share a kv head.  A query that sees no token gives 0 and lse -inf.  What lies
+ * in the cache past a query's place takes no part, whatever it is.  max_len >= every lens[b]
+ * (tokens past it are ignored).  lse (nullable): [n_seqs, n_q, n_heads], log of the sum of
+ * exp(scale * q . k).
+ * acc_out (nullable) [n_seqs, n_kv_heads, ld_acc], ld_acc >= max_len, accumulates the attention
+ * that every token received, for sp_cache_evict:
+ *     acc_out[b, g, j] = acc_in[b, g, j] + sum of p[j] over the queries and the heads of group g
+ * for j < lens[b], 0 up to max_len; acc_in (nullable: zeros; may be acc_out) counts as 0 for the
+ * call's own n_q tokens.  workspace as in sp_mx4_linear.
+ */
+sp_status sp_cache_attention_workspace(const sp_cache *cache, int64_t n_q, int n_heads,
+                                       int64_t max_len, int want_acc, int64_t *bytes /* host */);
+sp_status sp_cache_attention(const sp_cache *cache, const void *Q, const sp_strides *q_strides,
+                             sp_dtype dtype, int64_t n_q, int n_heads, const int32_t *lens,
+                             int64_t max_len, float scale, void *O, const sp_strides *o_strides,
+                             float *lse, const float *acc_in, float *acc_out, int64_t ld_acc,
+                             void *workspace, int64_t workspace_bytes, sp_stream stream);
+
+/*
+ * Keeps, for every sequence and kv head on its own, m = min(lens[b], budget) of the tokens: the
+ * last min(recent, m), and of those before them the ones with the largest acc[b, g, j]
+ * (accumulated attention; NaN above every number, among equals the lower j first, -0 equal to 0).
+ * They are laid, in their order, into the first ceil(budget / block_tokens) blocks of dst's
+ * table, with new scales; slots past m hold zeros.  dst has the head count, head size and block
+ * size of src (else SP_ERR_SHAPE) and none of src's blocks (the pools may be the same).
+ *   kept_out  [n_seqs, n_kv_heads, budget]: the kept places j, ascending, -1 past m;
+ *   acc_out   nullable [n_seqs, n_kv_heads, ld_acc_out], ld_acc_out >= budget: acc of the kept
+ *             tokens, 0 past m; must not overlap acc;
+ *   lens_out  nullable [n_seqs]: m; must not overlap lens.
+ */
+sp_status sp_cache_evict(const sp_cache *src, const int32_t *lens, int64_t max_len,
+                         const float *acc, int64_t ld_acc, int64_t budget, int64_t recent,
+                         const sp_cache *dst, int32_t *kept_out, float *acc_out,
+                         int64_t ld_acc_out, int32_t *lens_out, sp_stream stream);
+
+/*
+ * Waits of the kernels above on their own copies and tensor-core work are bounded; *expired
+ * receives how many ran out on the current device since the last clear (0 unless the device or
+ * the library is at fault; results of such a call are wrong).  Synchronises the device.
+ */
+sp_status sp_wait_status(int *expired /* host */, int clear);
+
 /* ------------------------------------------------------------------ host-buffer variants */
 
 /*

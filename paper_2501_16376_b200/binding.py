@@ -23,6 +23,7 @@ SP_F16, SP_BF16 = 0, 1
 SP_S_GATED, SP_S_LITERAL_W2, SP_S_FROZEN, SP_S_READING_X2, SP_S_LITERAL_SCAN = 0, 1, 2, 3, 4
 SP_COUNTER_KEPT, SP_COUNTER_S_HAZARD, SP_NUM_COUNTERS = 0, 1, 2
 SP_CALIB_X_COMPLETE = 1
+SP_MX4_A16, SP_MX4_A4 = 0, 1
 
 #: every symbol include/swiftprune.h declares
 EXPORTS = (
@@ -32,7 +33,10 @@ EXPORTS = (
     "sp_select_unstructured_ex", "sp_search_la", "sp_ewma_trace", "sp_select_nm", "sp_select_24_compressed", "sp_apply_mask", "sp_calib_accumulate_host",
     "sp_select_nm_host", "sp_select_unstructured_host", "sp_select_unstructured_group",
     "sp_select_unstructured_group_ex", "sp_select_nm_group", "sp_select_unstructured_multi",
-    "sp_select_unstructured_multi_ex", "sp_select_nm_multi", "sp_debug_status", "sp_status_string",
+    "sp_select_unstructured_multi_ex", "sp_select_nm_multi", "sp_mx4_scale_bytes", "sp_mx4_quantize",
+    "sp_mx4_dequantize", "sp_mx4_linear_workspace", "sp_mx4_linear", "sp_cache_append",
+    "sp_cache_attention_workspace", "sp_cache_attention", "sp_cache_evict", "sp_wait_status",
+    "sp_debug_status", "sp_status_string",
     "sp_last_cuda_error", "sp_launch_count",
 )
 
@@ -57,6 +61,21 @@ class Matrix(ctypes.Structure):
 class Batch(ctypes.Structure):
     """sp_batch: one batch of calibration activations of a multi-input call."""
     _fields_ = [("X", ctypes.c_void_p), ("n_tokens", ctypes.c_int64), ("ldx", ctypes.c_int64)]
+
+
+class CacheStruct(ctypes.Structure):
+    """sp_cache: an 8-bit key/value cache."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_blocks", ctypes.c_int64), ("n_seqs", ctypes.c_int64),
+                ("table_cols", ctypes.c_int64), ("ld_table", ctypes.c_int64),
+                ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("block_tokens", ctypes.c_int)]
+
+
+class Strides(ctypes.Structure):
+    """sp_strides: strides in elements of a [sequence, token, head, head_dim] tensor."""
+    _fields_ = [("seq", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 SP_MAX_GROUP = 8
@@ -105,6 +124,19 @@ def _load() -> ctypes.CDLL:
     lib.sp_finalize_multi.argtypes = [ctypes.POINTER(vp), ci, vp]
     lib.sp_select_nm_multi.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(Matrix), ci, ci, ci, ci,
                                        vp]
+    pc, ps, pi64 = ctypes.POINTER(CacheStruct), ctypes.POINTER(Strides), ctypes.POINTER(i64)
+    lib.sp_mx4_scale_bytes.argtypes = [i64, i64]
+    lib.sp_mx4_scale_bytes.restype = i64
+    lib.sp_mx4_quantize.argtypes = [vp, ci, i64, i64, i64, vp, vp, i64, vp, vp]
+    lib.sp_mx4_dequantize.argtypes = [vp, i64, vp, i64, i64, ci, vp, i64, vp]
+    lib.sp_mx4_linear_workspace.argtypes = [i64, i64, i64, ci, pi64]
+    lib.sp_mx4_linear.argtypes = [vp, ci, i64, i64, vp, i64, vp, i64, i64, ci, vp, i64, vp, i64, vp]
+    lib.sp_cache_append.argtypes = [pc, vp, ps, vp, ps, ci, i64, vp, vp, vp]
+    lib.sp_cache_attention_workspace.argtypes = [pc, i64, ci, i64, ci, pi64]
+    lib.sp_cache_attention.argtypes = [pc, vp, ps, ci, i64, ci, vp, i64, f32, vp, ps, vp, vp, vp,
+                                       i64, vp, i64, vp]
+    lib.sp_cache_evict.argtypes = [pc, vp, i64, vp, i64, i64, i64, pc, vp, vp, i64, vp, vp]
+    lib.sp_wait_status.argtypes = [ctypes.POINTER(ci), ci]
     lib.sp_debug_status.argtypes = [ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(i64),
                                     ctypes.POINTER(i64), ci]
     lib.sp_status_string.argtypes = [ci]
@@ -500,6 +532,271 @@ def sp_calib_stats_noalloc(X: torch.Tensor, colsq_out: torch.Tensor | None = Non
     with torch.cuda.device(X.device):
         _check(lib.sp_calib_stats_noalloc(ptr, _dtype_of(X), T, n, ld, _ptr(colsq_out),
                                           _ptr(factor_out), _ptr(S_out), _stream(stream)))
+
+
+# ---------------------------------------------------------------- microscaled 4-bit weights
+
+def _on_current_device(t: torch.Tensor, what: str):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise SpError(SP_ERR_INVALID_ARG, "%s must be a CUDA tensor of the current device" % what)
+
+
+def _codes(codes: torch.Tensor, scales: torch.Tensor, n_cols: int):
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise SpError(SP_ERR_DTYPE, "codes and scales are uint8 tensors")
+    _on_current_device(codes, "codes")
+    _on_current_device(scales, "scales")
+    ptr, R, width, ldc = _matrix(codes, "codes")
+    if width < (n_cols + 31) // 32 * 16:
+        raise SpError(SP_ERR_SHAPE, "codes have %d bytes a row, %d columns need %d"
+                      % (width, n_cols, (n_cols + 31) // 32 * 16))
+    if scales.numel() < lib.sp_mx4_scale_bytes(R, n_cols) or not scales.is_contiguous():
+        raise SpError(SP_ERR_SHAPE, "scales must be contiguous with sp_mx4_scale_bytes entries")
+    return ptr, R, ldc, scales.data_ptr()
+
+
+def sp_mx4_scale_bytes(n_rows: int, n_cols: int) -> int:
+    return int(lib.sp_mx4_scale_bytes(int(n_rows), int(n_cols)))
+
+
+def sp_mx4_quantize(W: torch.Tensor, mask: torch.Tensor | None = None, codes=None, scales=None,
+                    stream=None):
+    """Microscaled 4-bit form of W (with the keep mask of a selection applied on the way).
+    Returns (codes uint8 [rows, 16 * ceil(cols / 32)], scales uint8 in tiles; layout in the C
+    header)."""
+    _on_current_device(W, "W")
+    ptr, R, n, ld = _matrix(W, "W")
+    if mask is not None:
+        _on_current_device(mask, "mask")
+        if (mask.dtype != torch.int32 or tuple(mask.shape) != (R, (n + 31) // 32)
+                or not mask.is_contiguous()):
+            raise SpError(SP_ERR_SHAPE, "mask must be contiguous int32 [rows, ceil(cols/32)]")
+    if codes is None:
+        codes = torch.empty(R, (n + 31) // 32 * 16, dtype=torch.uint8, device=W.device)
+    if scales is None:
+        scales = torch.empty(lib.sp_mx4_scale_bytes(R, n), dtype=torch.uint8, device=W.device)
+    cptr, rows, ldc, sptr = _codes(codes, scales, n)
+    if rows != R:
+        raise SpError(SP_ERR_SHAPE, "codes have %d rows, W has %d" % (rows, R))
+    _check(lib.sp_mx4_quantize(ptr, _dtype_of(W), R, n, ld, _ptr(mask), cptr, ldc, sptr,
+                               _stream(stream)))
+    return codes, scales
+
+
+def sp_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, dtype=None,
+                      W_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The values of a 4-bit matrix as a 16-bit one [rows, n_cols] (of W_out's type, or dtype)."""
+    cptr, R, ldc, sptr = _codes(codes, scales, n_cols)
+    if W_out is None:
+        W_out = torch.empty(R, n_cols, dtype=dtype or torch.bfloat16, device=codes.device)
+    _on_current_device(W_out, "W_out")
+    optr, rows, n, ldo = _matrix(W_out, "W_out")
+    if (rows, n) != (R, n_cols):
+        raise SpError(SP_ERR_SHAPE, "W_out must be [%d, %d]" % (R, n_cols))
+    _check(lib.sp_mx4_dequantize(cptr, ldc, sptr, R, n_cols, _dtype_of(W_out), optr, ldo,
+                                 _stream(stream)))
+    return W_out
+
+
+def _workspace(need: int, workspace, device):
+    """(pointer, bytes, tensor that keeps it alive) of a call's scratch memory."""
+    if need == 0:
+        return None, 0, None
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
+        raise SpError(SP_ERR_INVALID_ARG, "the workspace needs %d contiguous bytes" % need)
+    return workspace.data_ptr(), need, workspace
+
+
+def _hold(keep, workspace, stream):
+    """Scratch memory made here is not reused before the work on another stream is done."""
+    if keep is not None and workspace is None and stream is not None:
+        keep.record_stream(stream if hasattr(stream, "cuda_stream")
+                           else torch.cuda.ExternalStream(int(stream)))
+
+
+def sp_mx4_linear_workspace(n_tokens: int, n_rows: int, n_cols: int, mode: int = SP_MX4_A16) -> int:
+    need = ctypes.c_int64()
+    _check(lib.sp_mx4_linear_workspace(int(n_tokens), int(n_rows), int(n_cols), int(mode),
+                                       ctypes.byref(need)))
+    return need.value
+
+
+def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                  mode: int = SP_MX4_A16, Y: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Y [tokens, rows] = X [tokens, cols] times the transposed 4-bit matrix.  SP_MX4_A16 takes
+    X as it is, SP_MX4_A4 quantises it like the weights first."""
+    _on_current_device(X, "X")
+    ptr, T, n, ldx = _matrix(X, "X")
+    cptr, R, ldc, sptr = _codes(codes, scales, n)
+    if Y is None:
+        Y = torch.empty(T, R, dtype=X.dtype, device=X.device)
+    _on_current_device(Y, "Y")
+    yptr, rows, cols, ldy = _matrix(Y, "Y")
+    if (rows, cols) != (T, R):
+        raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
+    if Y.dtype != X.dtype:
+        raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
+    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X.device)
+    _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, int(mode), yptr,
+                             ldy, wptr, wbytes, _stream(stream)))
+    _hold(keep, workspace, stream)
+    return Y
+
+
+# ---------------------------------------------------------------- 8-bit key/value cache
+
+def _heads(t: torch.Tensor, what: str, n_seqs: int, head_dim: int) -> Strides:
+    if t.dim() != 4 or t.shape[0] != n_seqs or t.shape[3] != head_dim or t.stride(3) != 1:
+        raise SpError(SP_ERR_SHAPE, "%s must be [%d, tokens, heads, %d] with consecutive values"
+                      % (what, n_seqs, head_dim))
+    _on_current_device(t, what)
+    s = t.stride()
+    return Strides(s[0], s[1], s[2])
+
+
+def _int32(t, what, shape):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous int32 %s" % (what, list(shape)))
+    _on_current_device(t, what)
+    return t.data_ptr()
+
+
+def _acc(t, what, n_seqs, n_heads, length):
+    """Pointer and leading dimension of a float [n_seqs, kv heads, >= length] tensor."""
+    if (t.dtype != torch.float32 or t.dim() != 3 or t.shape[0] != n_seqs or t.shape[1] != n_heads
+            or t.shape[2] < length or not t.is_contiguous()):
+        raise SpError(SP_ERR_SHAPE, "%s must be contiguous float32 [%d, %d, >= %d]"
+                      % (what, n_seqs, n_heads, length))
+    _on_current_device(t, what)
+    return t.data_ptr(), t.shape[2]
+
+
+class KvCache:
+    """An 8-bit key/value cache over tensors that the caller owns (``sp_cache``): codes uint8
+    [n_blocks, kv heads, block tokens, head size] and float32 scales [n_blocks, kv heads] for K
+    and V, and an int32 table [n_seqs, blocks of a sequence]."""
+
+    def __init__(self, k, v, k_scale, v_scale, table):
+        for t, what in ((k, "k"), (v, "v")):
+            if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous():
+                raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous uint8 [n_blocks, heads, "
+                                                  "block tokens, head size]" % what)
+            _on_current_device(t, what)
+        if k.shape != v.shape:
+            raise SpError(SP_ERR_SHAPE, "k and v must have the same shape")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32 or t.shape != k.shape[:2] or not t.is_contiguous():
+                raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous float32 [n_blocks, heads]" % what)
+            _on_current_device(t, what)
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise SpError(SP_ERR_INVALID_ARG, "table must be int32 [n_seqs, blocks]")
+        _on_current_device(table, "table")
+        self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
+        self.n_seqs, (_, self.n_kv_heads, self.block_tokens, self.head_dim) = table.shape[0], k.shape
+        ld = table.stride(0) if self.n_seqs > 1 else max(table.stride(0), table.shape[1])
+        self._c = CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                              table.data_ptr(), k.shape[0], self.n_seqs, table.shape[1], ld,
+                              self.n_kv_heads, self.head_dim, self.block_tokens)
+
+    @classmethod
+    def empty(cls, n_seqs: int, max_tokens: int, n_kv_heads: int, head_dim: int,
+              block_tokens: int = 32, device=None) -> "KvCache":
+        """A cache with its own blocks for max_tokens tokens of each sequence."""
+        device = device or torch.device("cuda", torch.cuda.current_device())
+        per = (max_tokens + block_tokens - 1) // block_tokens
+        shape = (n_seqs * per, n_kv_heads, block_tokens, head_dim)
+        k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        ks, vs = (torch.ones(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
+        table = torch.arange(n_seqs * per, dtype=torch.int32, device=device).view(n_seqs, per)
+        return cls(k, v, ks, vs, table)
+
+    def sp_cache_append(self, K, V, start, count=None, stream=None):
+        """Writes K, V [n_seqs, new, kv heads, head size] at the places start[b] and following
+        (start, count: int32 [n_seqs]; count defaults to all the new tokens)."""
+        ks, vs = (_heads(t, w, self.n_seqs, self.head_dim) for t, w in ((K, "K"), (V, "V")))
+        if K.shape != V.shape or K.shape[2] != self.n_kv_heads:
+            raise SpError(SP_ERR_SHAPE, "K and V must have the same shape and %d heads" % self.n_kv_heads)
+        if K.dtype != V.dtype:
+            raise SpError(SP_ERR_DTYPE, "K and V must have the same dtype")
+        shape = (self.n_seqs,)
+        _check(lib.sp_cache_append(self._c, K.data_ptr(), ks, V.data_ptr(), vs, _dtype_of(K),
+                                   K.shape[1], _int32(start, "start", shape),
+                                   _int32(count, "count", shape), _stream(stream)))
+
+    def sp_cache_attention_workspace(self, n_q: int, n_heads: int, max_len: int, want_acc: bool) -> int:
+        need = ctypes.c_int64()
+        _check(lib.sp_cache_attention_workspace(self._c, n_q, n_heads, max_len, int(want_acc),
+                                                ctypes.byref(need)))
+        return need.value
+
+    def sp_cache_attention(self, Q, lens, max_len: int, scale: float | None = None, O=None,
+                           lse=None, acc_in=None, acc_out=None, workspace=None, stream=None):
+        """Attention of Q [n_seqs, n_q, heads, head size] over the cache, whose lens (int32
+        [n_seqs]) count the call's own n_q tokens; max_len bounds them.  scale defaults to
+        1 / sqrt(head size).  acc_out (float32 [n_seqs, kv heads, >= max_len]) accumulates the
+        attention every token received on top of acc_in.  Returns O."""
+        qs = _heads(Q, "Q", self.n_seqs, self.head_dim)
+        if O is None:
+            O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        os_ = _heads(O, "O", self.n_seqs, self.head_dim)
+        if O.shape != Q.shape:
+            raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
+        if O.dtype != Q.dtype:
+            raise SpError(SP_ERR_DTYPE, "Q and O must have the same dtype")
+        n_q, n_heads = Q.shape[1], Q.shape[2]
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                                or tuple(lse.shape) != tuple(Q.shape[:3])):
+            raise SpError(SP_ERR_SHAPE, "lse must be contiguous float32 [n_seqs, n_q, heads]")
+        ai = ao = None
+        ld = max_len
+        if acc_out is not None:
+            ao, ld = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, max_len)
+            if acc_in is not None:
+                ai, ld_in = _acc(acc_in, "acc_in", self.n_seqs, self.n_kv_heads, max_len)
+                if ld_in != ld:
+                    raise SpError(SP_ERR_SHAPE, "acc_in and acc_out must have the same shape")
+        need = self.sp_cache_attention_workspace(n_q, n_heads, max_len, ao is not None)
+        wptr, wbytes, keep = _workspace(need, workspace, Q.device)
+        _check(lib.sp_cache_attention(self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads,
+                                      _int32(lens, "lens", (self.n_seqs,)), max_len,
+                                      self.head_dim ** -0.5 if scale is None else scale,
+                                      O.data_ptr(), os_, _ptr(lse), ai, ao, ld, wptr, wbytes,
+                                      _stream(stream)))
+        _hold(keep, workspace, stream)
+        return O
+
+    def sp_cache_evict(self, lens, max_len: int, acc, budget: int, recent: int, dst: "KvCache",
+                       acc_out=None, kept_out=None, lens_out=None, stream=None):
+        """Keeps budget tokens of every (sequence, kv head): the last `recent` and those with the
+        largest acc; lays them into dst's blocks.  Returns (kept_out, acc_out, lens_out)."""
+        a, ld = _acc(acc, "acc", self.n_seqs, self.n_kv_heads, max_len)
+        if dst.n_seqs != self.n_seqs:
+            raise SpError(SP_ERR_SHAPE, "dst must have the same sequences")
+        shape = (self.n_seqs, self.n_kv_heads, budget)
+        if kept_out is None:
+            kept_out = torch.empty(shape, dtype=torch.int32, device=acc.device)
+        if acc_out is None:
+            acc_out = torch.empty(shape, dtype=torch.float32, device=acc.device)
+        if lens_out is None:
+            lens_out = torch.empty(self.n_seqs, dtype=torch.int32, device=acc.device)
+        ao, ld_out = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, budget)
+        _check(lib.sp_cache_evict(self._c, _int32(lens, "lens", (self.n_seqs,)), max_len, a, ld,
+                                  budget, recent, dst._c, _int32(kept_out, "kept_out", shape), ao,
+                                  ld_out, _int32(lens_out, "lens_out", (self.n_seqs,)),
+                                  _stream(stream)))
+        return kept_out, acc_out, lens_out
+
+
+def sp_wait_status(clear: bool = False) -> int:
+    """How many bounded waits of the serving kernels ran out (0 unless something is broken)."""
+    n = ctypes.c_int()
+    _check(lib.sp_wait_status(ctypes.byref(n), 1 if clear else 0))
+    return n.value
 
 
 def new_counters(device=None) -> torch.Tensor:

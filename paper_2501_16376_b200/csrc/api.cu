@@ -8,19 +8,17 @@
 #include <new>
 #include <vector>
 
-#include <nvtx3/nvToolsExt.h>
-
-#include "sp_internal.h"
+#include "sp_api.h"
 
 namespace sp {
 
 static thread_local char g_cuda_error[256] = "";
 // readers of the per-translation-unit index-check records (debug build only; see sp_debug.cuh)
-static DebugReader g_debug_readers[16];
+static DebugReader g_debug_readers[32];
 static int g_debug_reader_count = 0;
 
 void register_debug_reader(DebugReader reader) {
-    if (g_debug_reader_count < 16) g_debug_readers[g_debug_reader_count++] = reader;
+    if (g_debug_reader_count < 32) g_debug_readers[g_debug_reader_count++] = reader;
 }
 
 static std::atomic<uint64_t> g_launches{0};
@@ -53,19 +51,6 @@ class DeviceGuard {
     bool switched_ = false;
     cudaError_t err_ = cudaSuccess;
 };
-
-// NVTX range around one entry point: shows up in a timeline profile under the call's name;
-// costs a function-pointer test when no profiler is attached.
-class CallRange {
-   public:
-    explicit CallRange(const char *name) { nvtxRangePushA(name); }
-    ~CallRange() { nvtxRangePop(); }
-    CallRange(const CallRange &) = delete;
-    CallRange &operator=(const CallRange &) = delete;
-};
-#define SP_CALL_RANGE() CallRange sp_call_range__(__func__)
-
-static bool valid_dtype(sp_dtype d) { return d == SP_F16 || d == SP_BF16; }
 
 static bool ewma_params_valid(const sp_ewma_params *params) {
     if (params == nullptr) return false;

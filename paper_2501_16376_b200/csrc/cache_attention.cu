@@ -1,0 +1,507 @@
+// Attention of a few query tokens over the 8-bit cache.
+//
+// Mathematics: s_j = scale * q . k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) with the
+// running maximum m of an online softmax, in one pass over the cache; the splits of a long cache
+// are joined afterwards by the same rule.  Accumulated weights need the final maximum and sum, so
+// the pass leaves the scores (4 bytes a row and token, against 2 * head_dim of cache) and the
+// joining kernel turns them into weights.
+//
+// Bound by memory: 2 * head_dim bytes per token and kv head.  The heads of a group and the query
+// tokens form the rows that share a pass, 8 (or 16) at a time.  Tokens are the long side of both
+// tensor-core products (m16n8k16 on binary16, to which e4m3 converts exactly), so that 8 rows
+// cost no padding to 16 and no operand passes through shared memory:
+//   S^T [16 tokens x 8 rows] = K [16 x D] Q^T: a lane loads D/4 consecutive bytes of two tokens'
+//     keys - the order of the inner dimension is free as long as Q agrees - and uses them as they lie;
+//   O^T [D x 8 rows] += V^T [D x 16] P^T: a lane loads D/8 consecutive bytes of four tokens'
+//     values and interleaves pairs of tokens bytewise before converting; P^T is S^T transposed
+//     8x8 by movmatrix.
+// The block scale of K goes onto the scores and that of V onto the 16-token partial product, in
+// binary32.  P is rounded to binary16 for the product; for binary16 outputs the remainder follows
+// as a second operand (2^-22 in all), since one rounding of P alone would be as large as that of
+// the output.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
+// the reductions of nearly all steps and leaves P at most 256.
+#include <algorithm>
+
+#include "cache_common.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int kAttnWarps = 4;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kRaise = 8.0f;  // how far (in powers of two) a score may exceed the running maximum
+
+struct AttnArgs {
+    sp_cache cache;
+    const uint16_t *Q;
+    sp_strides q, o;
+    int64_t n_q, max_len;
+    int n_heads, group, rows;  // rows = n_q * group
+    int row_tiles, splits;
+    const int32_t *lens;
+    float scale_log2;
+    uint16_t *O;
+    float *lse;
+    float *part_o;   // [seq, kv head, split, row, D] unnormalised, relative to part_m
+    float2 *part_ml; // [seq, kv head, split, row] maximum (log2) and sum
+    float *scores;   // [seq, kv head, max_len, rows], log2; nullable
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t u) { return unpack2<false>(u); }
+
+// N consecutive words of read-once cache data
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
+    if constexpr (N == 2) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(p));
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(p + i * 4));
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    }
+}
+
+// Place of a row's query token in its sequence, at most the last cached token; < 0: sees nothing.
+__device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row, int64_t len) {
+    if (row >= a.rows) return -1;
+    return static_cast<int>(min(int64_t(a.lens[seq]) - a.n_q + row / a.group, len - 1));
+}
+
+}  // namespace
+
+// NT: tiles of 8 rows
+template <bool BF16, int D, int NT>
+__global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const AttnArgs a) {
+    constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
+    constexpr int VW = D / 32;  // words of values a lane holds of one token
+    constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
+    __shared__ float sh_o[kAttnWarps][NT * 8][D];
+    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
+    __shared__ int nan_from[D];  // first token among the call's own whose value is NaN, by column
+    const sp_cache &c = a.cache;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t seq = blockIdx.z;
+    const int head = blockIdx.y / a.row_tiles, row0 = blockIdx.y % a.row_tiles * NT * 8;
+    const int H = c.n_kv_heads, T = c.block_tokens;
+    pdl_launch_dependents();
+    for (int d = threadIdx.x; d < D; d += kAttnWarps * 32) nan_from[d] = 0x7fffffff;
+    pdl_wait();
+    const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols * T)));
+    const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
+    const int steps = (len + 15) / 16;
+    const int first = static_cast<int>(int64_t(steps) * blockIdx.x / a.splits);
+    const int last = static_cast<int>(int64_t(steps) * (blockIdx.x + 1) / a.splits);
+
+    // queries: operand registers, and the factor that undoes their scaling
+    uint32_t qf[NT][KW][2];
+    float qscale[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
+    int limit[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + n * 8 + g;
+        float undo = a.scale_log2;
+        if (row < a.rows) {
+            const uint16_t *q = a.Q + seq * a.q.seq + (row / a.group) * a.q.token +
+                                (head * a.group + row % a.group) * a.q.head + t * (D / 4);
+            uint32_t raw[KW][2];
+#pragma unroll
+            for (int s = 0; s < KW; ++s) {
+                raw[s][0] = q[4 * s] | (uint32_t(q[4 * s + 1]) << 16);
+                raw[s][1] = q[4 * s + 2] | (uint32_t(q[4 * s + 3]) << 16);
+            }
+            if constexpr (BF16) {
+                // binary16 holds a row scaled by a power of two: its largest magnitude comes to
+                // [2^14, 2^15), and what is lost lies 2^39 below that
+                uint32_t top = 0;
+#pragma unroll
+                for (int s = 0; s < KW; ++s)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t lo = (raw[s][i] << 16) & 0x7fffffffu, hi = raw[s][i] & 0x7fff0000u;
+                        if (lo < 0x7f800000u) top = max(top, lo);
+                        if (hi < 0x7f800000u) top = max(top, hi);
+                    }
+                const unsigned quad = 0xfu << (lane & 28);
+                top = max(top, __shfl_xor_sync(quad, top, 1));
+                top = max(top, __shfl_xor_sync(quad, top, 2));
+                const int up = min(141 - max(static_cast<int>(top >> 23), 1), 126);
+                const float f = pow2(up);
+                undo *= pow2(-up);
+#pragma unroll
+                for (int s = 0; s < KW; ++s)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float2 v = unpack2<true>(raw[s][i]);
+                        raw[s][i] = pack_f16(v.x * f, v.y * f);
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < KW; ++s) {
+                qf[n][s][0] = raw[s][0];
+                qf[n][s][1] = raw[s][1];
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KW; ++s) qf[n][s][0] = qf[n][s][1] = 0u;
+        }
+        // the scores' columns are rows 2t and 2t + 1
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            qscale[n][i] = __shfl_sync(kFullWarp, undo, (2 * t + i) * 4);
+            limit[n][i] = row_limit(a, seq, row0 + n * 8 + 2 * t + i, len);
+            m[n][i] = -INFINITY;
+            l[n][i] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < MT; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][k][i] = 0.0f;
+    }
+    __syncthreads();
+
+    for (int step = first + warp; step < last; step += kAttnWarps) {
+        const int j0 = step * 16;
+        const int64_t block = cache_block(c, seq, j0 / T);
+        if (block < 0) {
+            if (a.scores != nullptr)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + g + (i >> 1) * 8, row = row0 + n * 8 + 2 * t + (i & 1);
+                        if (j < len && row < a.rows)
+                            a.scores[((seq * H + head) * a.max_len + j) * a.rows + row] = -INFINITY;
+                    }
+            continue;
+        }
+        const int64_t at = ((block * H + head) * T + j0 % T) * D;
+        const uint8_t *kp = static_cast<const uint8_t *>(c.k) + at, *vp = static_cast<const uint8_t *>(c.v) + at;
+        uint32_t kw[2][KW], vw[4][VW];
+        load_words(kp + g * D + t * (D / 4), kw[0]);
+        load_words(kp + (g + 8) * D + t * (D / 4), kw[1]);
+        load_words(vp + (2 * t) * D + g * (D / 8), vw[0]);
+        load_words(vp + (2 * t + 1) * D + g * (D / 8), vw[1]);
+        load_words(vp + (2 * t + 8) * D + g * (D / 8), vw[2]);
+        load_words(vp + (2 * t + 9) * D + g * (D / 8), vw[3]);
+        const float k_scale = c.k_scale[block * H + head], v_scale = c.v_scale[block * H + head];
+
+        // scores
+        float s[NT][4];
+        {
+            float s2[NT][2][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s2[n][0][i] = s2[n][1][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                uint32_t f[4];
+                e4m3_to_f16(kw[0][k], f[0], f[2]);
+                e4m3_to_f16(kw[1][k], f[1], f[3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_f16(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
+            }
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + g + (i >> 1) * 8;
+                    const float x = (s2[n][0][i] + s2[n][1][i]) * (k_scale * qscale[n][i & 1]);
+                    s[n][i] = j <= limit[n][i & 1] ? x : -INFINITY;
+                    raise |= s[n][i] > m[n][i & 1] + kRaise;
+                }
+            if (a.scores != nullptr) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + g + (i >> 1) * 8, row = row0 + n * 8 + 2 * t + (i & 1);
+                        if (j < len && row < a.rows)
+                            a.scores[((seq * H + head) * a.max_len + j) * a.rows + row] = s[n][i];
+                    }
+            }
+            if (__any_sync(kFullWarp, raise)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float top = fmaxf(s[n][i], s[n][i + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 16));
+                        top = fmaxf(top, m[n][i]);
+                        const float f = top == m[n][i] ? 1.0f : exp2f(m[n][i] - top);
+                        m[n][i] = top;
+                        l[n][i] *= f;
+#pragma unroll
+                        for (int k = 0; k < MT; ++k) {
+                            o[n][k][i] *= f;
+                            o[n][k][i + 2] *= f;
+                        }
+                    }
+            }
+        }
+        // weights, as the operand of the output product
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + g + (i >> 1) * 8;
+                p[i] = j <= limit[n][i & 1] ? exp2f(s[n][i] - m[n][i & 1]) : 0.0f;
+                l[n][i & 1] += p[i];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t hi = pack_f16(p[2 * h], p[2 * h + 1]);
+                ph[n][h] = transpose8x8(hi);
+                if constexpr (!BF16) {
+                    const float2 r = unpack_f16(hi);
+                    pl[n][h] = transpose8x8(pack_f16(p[2 * h] - r.x, p[2 * h + 1] - r.y));
+                }
+            }
+        }
+        // values past the end, and NaN of the call's own tokens, which some rows do not see
+        if (j0 + 16 > own_from) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + 2 * t + (i & 1) + (i >> 1) * 8;
+#pragma unroll
+                for (int w = 0; w < VW; ++w) {
+                    if (j >= len) vw[i][w] = 0u;
+                    else if (j >= own_from) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (((vw[i][w] >> (8 * k)) & 0x7fu) == 0x7fu) {
+                                atomicMin(&nan_from[g * (D / 8) + w * 4 + k], j);
+                                vw[i][w] &= ~(0xffu << (8 * k));
+                            }
+                    }
+                }
+            }
+            __syncwarp();
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                // two columns of four tokens: (column, token pair)
+                const uint32_t sel = half == 0 ? 0x5140u : 0x7362u;
+                uint32_t f[4];
+                e4m3_to_f16(prmt(vw[0][w], vw[1][w], sel), f[0], f[1]);
+                e4m3_to_f16(prmt(vw[2][w], vw[3][w], sel), f[2], f[3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    mma_f16(x, f, ph[n][0], ph[n][1]);
+                    if constexpr (!BF16) mma_f16(x, f, pl[n][0], pl[n][1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[n][2 * w + half][i] = fmaf(v_scale, x[i], o[n][2 * w + half][i]);
+                }
+            }
+        }
+    }
+
+    // the warps' parts meet in shared memory
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = n * 8 + 2 * t + i;
+            float sum = l[n][i];
+            sum += __shfl_xor_sync(kFullWarp, sum, 4);
+            sum += __shfl_xor_sync(kFullWarp, sum, 8);
+            sum += __shfl_xor_sync(kFullWarp, sum, 16);
+            if (g == 0) {
+                sh_m[warp][row] = m[n][i];
+                sh_l[warp][row] = sum;
+            }
+#pragma unroll
+            for (int k = 0; k < MT; ++k) {
+                sh_o[warp][row][g * (D / 8) + 2 * k] = o[n][k][i];
+                sh_o[warp][row][g * (D / 8) + 2 * k + 1] = o[n][k][i + 2];
+            }
+        }
+    __syncthreads();
+    for (int at = threadIdx.x; at < NT * 8 * D; at += kAttnWarps * 32) {
+        const int r = at / D, d = at % D, row = row0 + r;
+        if (row >= a.rows) break;
+        float top = sh_m[0][r];
+#pragma unroll
+        for (int w = 1; w < kAttnWarps; ++w) top = fmaxf(top, sh_m[w][r]);
+        float sum = 0.0f, out = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kAttnWarps; ++w) {
+            const float f = sh_m[w][r] == top ? 1.0f : exp2f(sh_m[w][r] - top);
+            sum = fmaf(f, sh_l[w][r], sum);
+            out = fmaf(f, sh_o[w][r][d], out);
+        }
+        if (nan_from[d] <= row_limit(a, seq, row, len)) out = __uint_as_float(0x7fc00000u);
+        if (a.part_o != nullptr) {
+            const int64_t p = ((seq * H + head) * a.splits + blockIdx.x) * a.rows + row;
+            a.part_o[p * D + d] = out;
+            if (d == 0) a.part_ml[p] = make_float2(top, sum);
+        } else {
+            const int i = row / a.group, hq = head * a.group + row % a.group;
+            const float y = top == -INFINITY && sum == 0.0f ? 0.0f : out / sum;
+            uint16_t bits;
+            if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+            else bits = __half_as_ushort(__float2half_rn(y));
+            a.O[seq * a.o.seq + i * a.o.token + hq * a.o.head + d] = bits;
+            if (d == 0 && a.lse != nullptr)
+                a.lse[(seq * a.n_q + i) * a.n_heads + hq] = (top + log2f(sum)) * 0.6931471805599453f;
+        }
+    }
+}
+
+// Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)
+// takes the rows x, x + gridDim.x, ... of the output and the x-th stretch of the tokens.
+template <bool BF16>
+__global__ void __launch_bounds__(256)
+cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t ld_acc, int64_t stretch) {
+    extern __shared__ float row_lse[];  // log2 of the sum of 2^s, +inf where a row sees nothing
+    const sp_cache &c = a.cache;
+    const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y;
+    const int64_t seq = blockIdx.z, pair = seq * H + head;
+    pdl_launch_dependents();
+    pdl_wait();
+    const float2 *ml = a.part_ml + pair * a.splits * a.rows;
+    const float *part = a.part_o + pair * a.splits * a.rows * D;
+    if (acc_out != nullptr) {
+        for (int row = threadIdx.x; row < a.rows; row += blockDim.x) {
+            float top = -INFINITY, sum = 0.0f;
+            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * a.rows + row].x);
+            for (int s = 0; s < a.splits; ++s) {
+                const float2 v = ml[s * a.rows + row];
+                sum = fmaf(v.x == top ? 1.0f : exp2f(v.x - top), v.y, sum);
+            }
+            row_lse[row] = top == -INFINITY && sum == 0.0f ? INFINITY : top + log2f(sum);
+        }
+        __syncthreads();
+        const int64_t len = max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols * c.block_tokens));
+        const int64_t own = a.lens[seq] - a.n_q;
+        const int64_t end = min((blockIdx.x + 1) * stretch, a.max_len);
+        for (int64_t j = blockIdx.x * stretch + threadIdx.x; j < end; j += blockDim.x) {
+            float sum = 0.0f;
+            if (j < len) {
+                const float *s = a.scores + (pair * a.max_len + j) * a.rows;
+                for (int row = 0; row < a.rows; ++row) {
+                    const float x = s[row], z = row_lse[row];
+                    sum += x == -INFINITY ? 0.0f : exp2f(x - z);
+                }
+                if (acc_in != nullptr && j < own) sum += acc_in[pair * ld_acc + j];
+            }
+            acc_out[pair * ld_acc + j] = sum;
+        }
+    }
+    for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int i = row / a.group, hq = head * a.group + row % a.group;
+        float top = -INFINITY;
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * a.rows + row].x);
+        for (int d = threadIdx.x; d < D; d += blockDim.x) {
+            float sum = 0.0f, out = 0.0f;
+            for (int s = 0; s < a.splits; ++s) {
+                const float2 v = ml[s * a.rows + row];
+                const float f = v.x == top ? 1.0f : exp2f(v.x - top);
+                sum = fmaf(f, v.y, sum);
+                out = fmaf(f, part[(s * a.rows + row) * int64_t(D) + d], out);
+            }
+            const float y = top == -INFINITY && sum == 0.0f ? 0.0f : out / sum;
+            uint16_t bits;
+            if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+            else bits = __half_as_ushort(__float2half_rn(y));
+            a.O[seq * a.o.seq + i * a.o.token + hq * a.o.head + d] = bits;
+            if (d == 0 && a.lse != nullptr)
+                a.lse[(seq * a.n_q + i) * a.n_heads + hq] = (top + log2f(sum)) * 0.6931471805599453f;
+        }
+    }
+}
+
+// How many blocks share a (sequence, kv head, row tile): enough for about 8 blocks an SM, none
+// with less than 64 tokens.
+static int attention_splits(const sp_cache &c, int row_tiles, int64_t max_len, bool want_acc) {
+    const int64_t units = c.n_seqs * c.n_kv_heads * row_tiles;
+    const int64_t most = std::max(int64_t(1), (max_len + 63) / 64);
+    return static_cast<int>(std::max(int64_t(1), std::min(std::min(most, int64_t(256)), 148 * 8 / units)));
+}
+static int attention_row_tiles(int64_t rows) { return static_cast<int>(rows <= 8 ? 1 : (rows + 15) / 16); }
+
+int64_t cache_attention_workspace(const sp_cache &c, int64_t n_q, int n_heads, int64_t max_len, bool want_acc) {
+    const int64_t rows = n_q * (n_heads / c.n_kv_heads), pairs = c.n_seqs * c.n_kv_heads;
+    const int splits = attention_splits(c, attention_row_tiles(rows), max_len, want_acc);
+    if (pairs == 0 || rows == 0 || (splits == 1 && !want_acc)) return 0;
+    int64_t bytes = pairs * splits * rows * (c.head_dim * 4 + 8);
+    if (want_acc) bytes += pairs * max_len * rows * 4;
+    return bytes;
+}
+
+sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_strides &q, sp_dtype dtype, int64_t n_q,
+                                 int n_heads, const int32_t *lens, int64_t max_len, float scale, void *O,
+                                 const sp_strides &o, float *lse, const float *acc_in, float *acc_out, int64_t ld_acc,
+                                 void *workspace, cudaStream_t stream) {
+    AttnArgs a = {};
+    a.cache = c;
+    a.Q = static_cast<const uint16_t *>(Q);
+    a.q = q;
+    a.o = o;
+    a.n_q = n_q;
+    a.max_len = max_len;
+    a.n_heads = n_heads;
+    a.group = n_heads / c.n_kv_heads;
+    a.rows = static_cast<int>(n_q * a.group);
+    a.row_tiles = attention_row_tiles(a.rows);
+    a.splits = attention_splits(c, a.row_tiles, max_len, acc_out != nullptr);
+    a.lens = lens;
+    a.scale_log2 = scale * kLog2e;
+    a.O = static_cast<uint16_t *>(O);
+    a.lse = lse;
+    const int64_t pairs = c.n_seqs * c.n_kv_heads;
+    const bool join = a.splits > 1 || acc_out != nullptr;
+    if (join) {
+        a.part_ml = static_cast<float2 *>(workspace);
+        a.part_o = reinterpret_cast<float *>(a.part_ml + pairs * a.splits * a.rows);
+        if (acc_out != nullptr) a.scores = a.part_o + pairs * a.splits * a.rows * c.head_dim;
+    }
+    PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
+    cudaError_t e;
+#define SP_LAUNCH(B, DD, N) e = cudaLaunchKernelEx(&pdl.cfg, cache_attention_kernel<B, DD, N>, a)
+#define SP_PICK(B)                                                                                     \
+    if (c.head_dim == 64) { if (a.rows <= 8) SP_LAUNCH(B, 64, 1); else SP_LAUNCH(B, 64, 2); }          \
+    else { if (a.rows <= 8) SP_LAUNCH(B, 128, 1); else SP_LAUNCH(B, 128, 2); }
+    if (dtype == SP_BF16) { SP_PICK(true) } else { SP_PICK(false) }
+#undef SP_PICK
+#undef SP_LAUNCH
+    if (e != cudaSuccess) return cuda_fail(e);
+    sp_status st = check_launch();
+    if (st != SP_OK || !join) return st;
+    const int64_t stretch = 1024;
+    const int64_t blocks = std::max(acc_out != nullptr ? (max_len + stretch - 1) / stretch : 1, std::min(int64_t(a.rows), int64_t(8)));
+    PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(256), stream);
+    second.cfg.dynamicSmemBytes = a.rows * sizeof(float);
+    if (dtype == SP_BF16) e = cudaLaunchKernelEx(&second.cfg, cache_join_kernel<true>, a, acc_in, acc_out, ld_acc, stretch);
+    else e = cudaLaunchKernelEx(&second.cfg, cache_join_kernel<false>, a, acc_in, acc_out, ld_acc, stretch);
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+}  // namespace sp

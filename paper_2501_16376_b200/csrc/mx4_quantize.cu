@@ -1,0 +1,147 @@
+// Microscaled 4-bit quantisation of a 16-bit matrix and the way back.
+//
+// Mathematics: in every block of 32 columns  e = floor(log2 max|w|) - 2,  code = nearest 4-bit
+// float to w / 2^e.  One pass over the matrix; bound by memory: 2 bytes read and 17/32 written
+// per weight (the reverse for the way back).  A warp takes four rows that lie 32 apart and 256
+// columns of each: a quad of lanes holds a block (16 bytes a lane, four loads in flight), the
+// largest magnitude costs two shuffles, and the scale bytes of the four rows are 16 consecutive
+// bytes of a tile, so they leave in one store.
+#include "mx4_common.cuh"
+
+namespace sp {
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(256)
+mx4_quantize_kernel(const uint16_t *__restrict__ W, int64_t n_rows, int64_t n_cols, int64_t ldw,
+                    const uint32_t *__restrict__ mask, uint8_t *__restrict__ codes, int64_t ldc,
+                    uint8_t *__restrict__ scales, int64_t chunks, int64_t n_tasks) {
+    const int64_t task = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    if (task >= n_tasks) return;
+    const int64_t chunk = task % chunks, rows32 = task / chunks;
+    const int64_t row0 = (rows32 >> 5) * kMx4TileRows + (rows32 & 31);
+    const int64_t col = chunk * 256 + lane * 8;
+    const int64_t nb = mx4_blocks(n_cols), words = (n_cols + 31) / 32;
+    pdl_wait();
+    uint32_t p[4][4], keep[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + 32 * i;
+        keep[i] = 0xffu;
+        if (r < n_rows) {
+            load8<VEC, true>(W + r * ldw, col, n_cols, p[i]);
+            if (mask != nullptr && col < n_cols)
+                keep[i] = (mask[r * words + (col >> 5)] >> (col & 31)) & 0xffu;
+        } else {
+            p[i][0] = p[i][1] = p[i][2] = p[i][3] = 0u;
+        }
+    }
+    uint32_t tile[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (mask != nullptr) zero_pruned(p[i], keep[i]);
+        uint32_t word;
+        const uint32_t byte = mx4_quantize_quad<BF16>(p[i], word);
+        const int64_t r = row0 + 32 * i;
+        if (r < n_rows && col < nb * 32)
+            *reinterpret_cast<uint32_t *>(codes + r * ldc + (col >> 1)) = word;
+        uint32_t t = byte << (8 * ((lane >> 2) & 3));
+        t |= __shfl_xor_sync(kFullWarp, t, 4);
+        t |= __shfl_xor_sync(kFullWarp, t, 8);
+        tile[i] = t;
+    }
+    const int64_t kt = mx4_tile_cols(n_cols), at = chunk * 2 + (lane >> 4);
+    if ((lane & 15) == 0 && at < kt)
+        *reinterpret_cast<uint4 *>(scales + ((rows32 >> 5) * kt + at) * kMx4TileBytes +
+                                   (rows32 & 31) * 16) = make_uint4(tile[0], tile[1], tile[2], tile[3]);
+}
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(256)
+mx4_dequantize_kernel(const uint8_t *__restrict__ codes, int64_t ldc,
+                      const uint8_t *__restrict__ scales, int64_t n_rows, int64_t n_cols,
+                      uint16_t *__restrict__ W, int64_t ldw, int64_t chunks, int64_t n_tasks) {
+    const int64_t task = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    if (task >= n_tasks) return;
+    const int64_t chunk = task % chunks, rows32 = task / chunks;
+    const int64_t row0 = (rows32 >> 5) * kMx4TileRows + (rows32 & 31);
+    const int64_t col = chunk * 256 + lane * 8;
+    if (col >= n_cols) return;
+    const int64_t kt = mx4_tile_cols(n_cols);
+    pdl_wait();
+    const uint4 tile = *reinterpret_cast<const uint4 *>(
+        scales + ((rows32 >> 5) * kt + chunk * 2 + (lane >> 4)) * kMx4TileBytes + (rows32 & 31) * 16);
+    const uint32_t words[4] = {tile.x, tile.y, tile.z, tile.w};
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + 32 * i;
+        w[i] = r < n_rows ? __ldcs(reinterpret_cast<const uint32_t *>(codes + r * ldc + (col >> 1))) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + 32 * i;
+        if (r >= n_rows) break;
+        const uint32_t byte = (words[i] >> (8 * ((lane >> 2) & 3))) & 0xffu;
+        const float s = byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte);
+        uint32_t h[4], out[4];
+        mx4_unpack8(w[i], h);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack2<false>(h[k]);
+            if constexpr (BF16) {
+                __nv_bfloat162 v = __floats2bfloat162_rn(f.x * s, f.y * s);
+                out[k] = *reinterpret_cast<uint32_t *>(&v);
+            } else {
+                __half2 v = __floats2half2_rn(f.x * s, f.y * s);
+                out[k] = *reinterpret_cast<uint32_t *>(&v);
+            }
+        }
+        store8<VEC>(W + r * ldw, col, n_cols, out);
+    }
+}
+
+sp_status launch_mx4_quantize(const void *W, sp_dtype dtype, int64_t n_rows, int64_t n_cols,
+                              int64_t ldw, const uint32_t *mask, uint8_t *codes, int64_t ldc,
+                              uint8_t *scales, cudaStream_t stream) {
+    const uint16_t *Wp = static_cast<const uint16_t *>(W);
+    const int64_t chunks = (n_cols + 255) / 256;
+    const int64_t n_tasks = mx4_tile_rows(n_rows) * 32 * chunks;
+    if ((n_tasks + 7) / 8 > 0x7fffffff) return SP_ERR_SHAPE;
+    const bool vec = aligned16(W) && ldw % 8 == 0 && n_cols % 8 == 0;
+    PdlConfig pdl(dim3(static_cast<unsigned>((n_tasks + 7) / 8)), dim3(256), stream);
+    cudaError_t e;
+#define SP_LAUNCH(B, V)                                                                       \
+    e = cudaLaunchKernelEx(&pdl.cfg, mx4_quantize_kernel<B, V>, Wp, n_rows, n_cols, ldw, mask, \
+                           codes, ldc, scales, chunks, n_tasks)
+    if (dtype == SP_BF16) { if (vec) SP_LAUNCH(true, true); else SP_LAUNCH(true, false); }
+    else { if (vec) SP_LAUNCH(false, true); else SP_LAUNCH(false, false); }
+#undef SP_LAUNCH
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+sp_status launch_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales,
+                                int64_t n_rows, int64_t n_cols, sp_dtype dtype, void *W,
+                                int64_t ldw, cudaStream_t stream) {
+    uint16_t *Wp = static_cast<uint16_t *>(W);
+    const int64_t chunks = (n_cols + 255) / 256;
+    const int64_t n_tasks = mx4_tile_rows(n_rows) * 32 * chunks;
+    if ((n_tasks + 7) / 8 > 0x7fffffff) return SP_ERR_SHAPE;
+    const bool vec = aligned16(W) && ldw % 8 == 0 && n_cols % 8 == 0;
+    PdlConfig pdl(dim3(static_cast<unsigned>((n_tasks + 7) / 8)), dim3(256), stream);
+    cudaError_t e;
+#define SP_LAUNCH(B, V)                                                                          \
+    e = cudaLaunchKernelEx(&pdl.cfg, mx4_dequantize_kernel<B, V>, codes, ldc, scales, n_rows,     \
+                           n_cols, Wp, ldw, chunks, n_tasks)
+    if (dtype == SP_BF16) { if (vec) SP_LAUNCH(true, true); else SP_LAUNCH(true, false); }
+    else { if (vec) SP_LAUNCH(false, true); else SP_LAUNCH(false, false); }
+#undef SP_LAUNCH
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+}  // namespace sp

@@ -1,0 +1,383 @@
+// Product of a few tokens with a microscaled 4-bit matrix (a decoding step): the weights stream
+// by once, everything else hides behind them.
+//
+// Mathematics: y[t, r] = sum over blocks b of  2^(byte - 127)[r, b] * sum_{k in b} code[r, k] x[t, k].
+// The codes are exact in binary16, so a block's inner sum is two m16n8k16 tensor-core products on
+// the bare codes, accumulated in binary32, and the scale - a power of two - is applied to that
+// sum by one multiply-add per output instead of to every weight.
+//
+// Bound by memory: 17/32 byte per weight.  A block of threads owns 128 rows and a slice of the
+// columns; a producer thread keeps kStages x (128 rows x 256 columns) in flight by TMA; eight
+// warps (4 groups of 32 rows x 2 halves of the columns of a stage) convert and multiply.  The
+// column order inside a 32-column block is free as long as weights and activations agree on it:
+// a lane takes 8 consecutive columns, so a weight operand is one 4-byte word of codes (four
+// conversions) and an activation operand is one 16-byte load.  With few rows the columns are cut
+// over a cluster of up to 8 blocks whose partial sums meet through distributed shared memory, in
+// rank order (results do not depend on scheduling).
+//
+// bf16 activations become binary16 here: every (token, 256 columns) is scaled by a power of two
+// so that its largest magnitude lies in [2^14, 2^15).  What binary16 cannot hold - an element
+// more than 2^30 times smaller than the largest of its 256 - goes into a second pass over the
+// weights, with the remainders scaled by 2^40; a block takes that pass only if it has one.
+#include "mx4_common.cuh"
+#include "sp_tma.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int kStages = 4;
+constexpr int kCodeBytes = kMx4TileRows * 128;  // codes of a stage: 128 rows x 256 columns
+constexpr int kPartPitch = 132;                 // floats between columns of a block's partial sums
+constexpr int kWarps = 8;
+
+struct StreamArgs {
+    const uint16_t *X;
+    int64_t ldx, n_tokens, n_cols, n_rows;
+    const uint8_t *scales;
+    uint16_t *Y;
+    int64_t ldy;
+    int tile_cols;     // scale tiles along a row
+    int stages;        // 256-column stages of a row
+    int chunk_stages;  // stages whose activations are in shared memory at a time
+    int quantize_x;
+    int vec_x;
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// One (token, 256 columns) of the activations -> binary16 in shared memory and its scale;
+// returns whether a remainder is left (bf16).  pass 1 stores the remainders.
+template <bool BF16>
+__device__ __forceinline__ bool convert_x(const StreamArgs &a, int64_t token, int64_t col, int lane,
+                                          int pass, __half *dst, float *scale_out) {
+    uint32_t p[4] = {0u, 0u, 0u, 0u};
+    if (token < a.n_tokens) {
+        if (a.vec_x) load8<true, false>(a.X + token * a.ldx, col, a.n_cols, p);
+        else load8<false, false>(a.X + token * a.ldx, col, a.n_cols, p);
+    }
+    float v[8];
+    if (a.quantize_x) {
+        uint32_t word, h[4];
+        const uint32_t byte = mx4_quantize_quad<BF16>(p, word);
+        const float s = byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte);
+        mx4_unpack8(word, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<false>(h[i]);
+            v[2 * i] = f.x * s;
+            v[2 * i + 1] = f.y * s;
+        }
+    } else {
+        unpack8<BF16>(p, v);
+    }
+    float inverse = 1.0f;
+    bool rest = false;
+    if constexpr (BF16) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
+            if (bits < 0x7f800000u) m = max(m, bits);
+        }
+        m = __reduce_max_sync(kFullWarp, m);
+        const int e = static_cast<int>(m >> 23);               // exponent of the largest + 127
+        const int up = min(141 - max(e, 1), 126);
+        const float f = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
+        inverse = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = v[i] * f;
+            const float hi = __half2float(__float2half_rn(x));
+            const float r = fabsf(x) <= 65504.0f ? x - hi : 0.0f;  // 0 for what is not finite
+            rest |= r != 0.0f;
+            v[i] = pass == 0 ? x : r * 1099511627776.0f;           // 2^40
+        }
+        if (pass != 0) inverse *= 9.094947017729282e-13f;          // 2^-40
+    }
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        out[i] = *reinterpret_cast<uint32_t *>(&h);
+    }
+    *reinterpret_cast<uint4 *>(dst + lane * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+    if (lane == 0) *scale_out = inverse;
+    return rest;
+}
+
+}  // namespace
+
+template <bool BF16, int NT>
+__global__ void __launch_bounds__(kWarps * 32 + 32)
+mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ uint64_t full[kStages], empty[kStages];
+    __shared__ uint32_t failed, has_rest;
+    constexpr int kTokens = NT * 8;
+    uint8_t *const code_smem = smem;
+    uint8_t *const scale_smem = smem + kStages * kCodeBytes;
+    const int x_pitch = a.chunk_stages * 512 + 64;              // bytes; 64 mod 128: no conflicts
+    uint8_t *const x_smem = scale_smem + kStages * 2 * kMx4TileBytes;
+    float *const xs_smem = reinterpret_cast<float *>(x_smem + kTokens * x_pitch);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int slices = gridDim.y, slice = blockIdx.y;
+    const int64_t row0 = int64_t(blockIdx.x) * kMx4TileRows;
+    const int first = static_cast<int>(int64_t(a.stages) * slice / slices);
+    const int last = static_cast<int>(int64_t(a.stages) * (slice + 1) / slices);
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&codes_map);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_addr(&full[s]), 1);
+            mbar_init(smem_addr(&empty[s]), kWarps);
+        }
+        failed = has_rest = 0u;
+        mbar_fence_init();
+    }
+    __syncthreads();
+    pdl_launch_dependents();
+    pdl_wait();
+
+    float acc[2][NT][4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+
+    const int g = lane >> 2, t = lane & 3;
+    const int wr = warp & 3, wk = warp >> 2;
+    int step = 0;  // stages issued (producer) or taken (consumers), over both passes
+    for (int pass = 0; pass < 2; ++pass) {
+        if (warp == kWarps) {
+            if (lane == 0) {
+                for (int s = first; s < last; ++s, ++step) {
+                    const int slot = step % kStages;
+                    if (step >= kStages && !mbar_wait_or_fail(smem_addr(&empty[slot]), ((step / kStages) - 1) & 1, &failed)) break;
+                    const int tiles = min(2, a.tile_cols - 2 * s);
+                    const uint32_t bar = smem_addr(&full[slot]);
+                    mbar_expect_tx(bar, kCodeBytes + tiles * kMx4TileBytes);
+                    tma_load_2d(smem_addr(code_smem + slot * kCodeBytes), &codes_map, s * 128,
+                                static_cast<int>(row0), bar);
+                    bulk_load(smem_addr(scale_smem + slot * 2 * kMx4TileBytes),
+                              a.scales + (int64_t(blockIdx.x) * a.tile_cols + 2 * s) * kMx4TileBytes,
+                              tiles * kMx4TileBytes, bar);
+                }
+            }
+            __syncwarp();
+        } else {
+            for (int c0 = first; c0 < last; c0 += a.chunk_stages) {
+                const int c1 = min(c0 + a.chunk_stages, last);
+                if (c0 != first || pass != 0) consumer_sync();  // everyone is done with the last chunk
+                bool rest = false;
+                for (int u = warp; u < (c1 - c0) * kTokens; u += kWarps) {
+                    const int s = u / kTokens, token = u % kTokens;
+                    rest |= convert_x<BF16>(a, token, int64_t(c0 + s) * 256 + lane * 8, lane, pass,
+                                            reinterpret_cast<__half *>(x_smem + token * x_pitch + s * 512),
+                                            xs_smem + u);
+                }
+                if (rest) has_rest = 1u;
+                consumer_sync();
+                for (int s = c0; s < c1; ++s, ++step) {
+                    const int slot = step % kStages;
+                    mbar_wait_or_fail(smem_addr(&full[slot]), (step / kStages) & 1, &failed);
+                    if (2 * s + wk < a.tile_cols) {
+                        const uint32_t codes = smem_addr(code_smem + slot * kCodeBytes) + (wr * 32 + g) * 128 + t * 4;
+                        const uint32_t sc = smem_addr(scale_smem + (slot * 2 + wk) * kMx4TileBytes) + g * 16 + wr * 4;
+                        const uint32_t xa = smem_addr(x_smem) + g * x_pitch + (s - c0) * 512 + wk * 256 + t * 16;
+                        uint32_t scale_word[4];  // rows g, g+8, g+16, g+24 of the warp's 32
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) scale_word[j] = lds32(sc + j * 128);
+                        float st[2][NT][4];
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            uint4 x[NT];
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) x[n] = lds128(xa + n * 8 * x_pitch + b * 64);
+                            // chunk of row r in the swizzled stage: block ^ (r & 7); all rows here have r & 7 == g
+                            const uint32_t at = codes + (((wk * 4 + b) ^ g) << 4);
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                uint32_t lo[4], hi[4];
+                                mx4_unpack8(lds32(at + m * 2048), lo);
+                                mx4_unpack8(lds32(at + m * 2048 + 1024), hi);
+                                const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]};
+                                const uint32_t a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+                                const float s0 = mx4_scale((scale_word[2 * m] >> (8 * b)) & 0xffu);
+                                const float s1 = mx4_scale((scale_word[2 * m + 1] >> (8 * b)) & 0xffu);
+#pragma unroll
+                                for (int n = 0; n < NT; ++n) {
+                                    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                    mma_f16(c, a0, x[n].x, x[n].y);
+                                    mma_f16(c, a1, x[n].z, x[n].w);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const float sc_i = i < 2 ? s0 : s1;
+                                        st[m][n][i] = b == 0 ? sc_i * c[i] : fmaf(sc_i, c[i], st[m][n][i]);
+                                    }
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const float2 xs = *reinterpret_cast<const float2 *>(xs_smem + (s - c0) * kTokens + n * 8 + 2 * t);
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                acc[m][n][0] = fmaf(xs.x, st[m][n][0], acc[m][n][0]);
+                                acc[m][n][1] = fmaf(xs.y, st[m][n][1], acc[m][n][1]);
+                                acc[m][n][2] = fmaf(xs.x, st[m][n][2], acc[m][n][2]);
+                                acc[m][n][3] = fmaf(xs.y, st[m][n][3], acc[m][n][3]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
+                }
+            }
+        }
+        __syncthreads();
+        if (!BF16 || has_rest == 0u || failed != 0u) break;
+    }
+    if (failed != 0u) {
+        if (warp == kWarps && lane == 0)
+            for (int s = max(0, step - kStages); s < step; ++s) mbar_wait(smem_addr(&full[s % kStages]), (s / kStages) & 1);
+    }
+
+    // the two column halves meet in shared memory (the stages are free: all copies have arrived)
+    float *const part = reinterpret_cast<float *>(smem);
+    float *const mine = part + (2 * t) * kPartPitch + wr * 32 + g;
+    if (failed != 0u) __syncthreads();
+    if (warp < kWarps && wk == 1) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mine[(n * 8 + (i & 1)) * kPartPitch + m * 16 + (i >> 1) * 8] = acc[m][n][i];
+    }
+    __syncthreads();
+    if (warp < kWarps && wk == 0) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mine[(n * 8 + (i & 1)) * kPartPitch + m * 16 + (i >> 1) * 8] += acc[m][n][i];
+    }
+    if (slices > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+    // (token, row) pairs over the threads of the cluster's blocks; ranks are summed in order
+    const int row = threadIdx.x & 127;
+    if (warp < kWarps && row0 + row < a.n_rows) {
+        for (int token = slice * 2 + (threadIdx.x >> 7); token < min(int64_t(kTokens), a.n_tokens); token += 2 * slices) {
+            const uint32_t at = smem_addr(part + token * kPartPitch + row);
+            float sum = 0.0f;
+            for (int r = 0; r < slices; ++r) {
+                float v;
+                if (slices > 1) {
+                    uint32_t remote;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(r));
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
+                } else {
+                    v = part[token * kPartPitch + row];
+                }
+                sum += v;
+            }
+            uint16_t bits;
+            if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(sum));
+            else bits = __half_as_ushort(__float2half_rn(sum));
+            a.Y[token * a.ldy + row0 + row] = bits;
+        }
+    }
+    if (slices > 1)
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <bool BF16, int NT>
+static sp_status launch_tile(const CUtensorMap &map, StreamArgs a, cudaStream_t stream) {
+    const int row_tiles = static_cast<int>(mx4_tile_rows(a.n_rows));
+    // enough blocks for every SM; a slice has two stages at least
+    int slices = 1;
+    while (slices < 8 && row_tiles * slices < 128 && a.stages >= 4 * slices) slices *= 2;
+    const int per_slice = (a.stages + slices - 1) / slices;
+    a.chunk_stages = min(per_slice, 16 / NT);
+    const size_t smem = kStages * (kCodeBytes + 2 * kMx4TileBytes) +
+                        NT * 8 * (a.chunk_stages * 512 + 64 + a.chunk_stages * 4);
+    auto *kernel = mx4_stream_kernel<BF16, NT>;
+    static DynamicSmem limit;
+    cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
+    if (e != cudaSuccess) return cuda_fail(e);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1;
+    attr[1].val.clusterDim.y = slices;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(row_tiles, slices);
+    cfg.blockDim = dim3(kWarps * 32 + 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = slices > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, map, a);
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
+    CUtensorMap map;
+    cudaError_t e = encode_byte_tiles(&map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
+    if (e != cudaSuccess) return cuda_fail(e);
+    StreamArgs a = {};
+    a.ldx = p.ldx;
+    a.n_cols = p.n_cols;
+    a.n_rows = p.n_rows;
+    a.scales = p.scales;
+    a.ldy = p.ldy;
+    a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
+    a.stages = (a.tile_cols + 1) / 2;
+    a.quantize_x = p.quantize_x;
+    a.vec_x = aligned16(p.X) && p.ldx % 8 == 0 && p.n_cols % 8 == 0;
+    for (int64_t t0 = 0; t0 < p.n_tokens; t0 += 32) {
+        a.X = static_cast<const uint16_t *>(p.X) + t0 * p.ldx;
+        a.Y = static_cast<uint16_t *>(p.Y) + t0 * p.ldy;
+        a.n_tokens = min(int64_t(32), p.n_tokens - t0);
+        sp_status st;
+        if (p.dtype == SP_BF16)
+            st = a.n_tokens <= 8 ? launch_tile<true, 1>(map, a, stream)
+                                 : a.n_tokens <= 16 ? launch_tile<true, 2>(map, a, stream)
+                                                    : launch_tile<true, 4>(map, a, stream);
+        else
+            st = a.n_tokens <= 8 ? launch_tile<false, 1>(map, a, stream)
+                                 : a.n_tokens <= 16 ? launch_tile<false, 2>(map, a, stream)
+                                                    : launch_tile<false, 4>(map, a, stream);
+        if (st != SP_OK) return st;
+    }
+    return SP_OK;
+}
+
+}  // namespace sp

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "sp_debug.cuh"
 #include "swiftprune.h"
 
@@ -78,6 +80,11 @@ inline sp_status check_launch() {
     count_launch();
     return SP_OK;
 }
+
+// Readers of the bounded waits that ran out, one for each translation unit that has such waits
+// (sp_tma.cuh); sp_wait_status collects them.
+typedef cudaError_t (*WaitReader)(unsigned int *out, bool clear);
+void register_wait_reader(WaitReader reader);  // api_serve.cu
 
 // calib.cu
 int calib_query_blocks_per_sm();
@@ -188,9 +195,69 @@ struct PdlConfig {
     }
 };
 
+// Allows a kernel all the dynamic shared memory of an SM, once for each device.
+class DynamicSmem {
+   public:
+    cudaError_t allow(const void *kernel) {
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = uint64_t(1) << (device & 63);
+        if (done_.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        cudaFuncAttributes attr;
+        e = cudaFuncGetAttributes(&attr, kernel);
+        if (e != cudaSuccess) return e;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kMaxBlockSmem - static_cast<int>(attr.sharedSizeBytes));
+        if (e == cudaSuccess) done_.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+    static constexpr int kMaxBlockSmem = 227 * 1024;
+
+   private:
+    std::atomic<uint64_t> done_{0};
+};
+
 sp_status launch_ewma_trace(const sp_ctx *ctx, const void *W, sp_dtype dtype, int64_t n_rows,
                             int64_t ldw, const sp_ewma_params &p, float *est_out, float *dev_out,
                             float *score_out, cudaStream_t stream);
+
+// mx4_quantize.cu
+sp_status launch_mx4_quantize(const void *W, sp_dtype dtype, int64_t n_rows, int64_t n_cols,
+                              int64_t ldw, const uint32_t *mask, uint8_t *codes, int64_t ldc,
+                              uint8_t *scales, cudaStream_t stream);
+sp_status launch_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales,
+                                int64_t n_rows, int64_t n_cols, sp_dtype dtype, void *W,
+                                int64_t ldw, cudaStream_t stream);
+
+// A product with a microscaled 4-bit matrix: Y [n_tokens, n_rows] = X [n_tokens, n_cols] W^T.
+struct Mx4Product {
+    const void *X;
+    int64_t n_tokens, ldx;
+    const uint8_t *codes;
+    int64_t ldc;
+    const uint8_t *scales;
+    int64_t n_rows, n_cols;
+    void *Y;
+    int64_t ldy;
+    sp_dtype dtype;
+    bool quantize_x;  // SP_MX4_A4
+};
+// mx4_stream.cu: few tokens, the weights stream by once for every 32
+sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream);
+
+// cache_append.cu, cache_attention.cu, cache_evict.cu: the 8-bit key/value cache
+sp_status launch_cache_append(const sp_cache &cache, const void *K, const sp_strides &ks, const void *V,
+                              const sp_strides &vs, sp_dtype dtype, int64_t n_new, const int32_t *start,
+                              const int32_t *count, cudaStream_t stream);
+int64_t cache_attention_workspace(const sp_cache &c, int64_t n_q, int n_heads, int64_t max_len, bool want_acc);
+sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_strides &q, sp_dtype dtype, int64_t n_q,
+                                 int n_heads, const int32_t *lens, int64_t max_len, float scale, void *O,
+                                 const sp_strides &o, float *lse, const float *acc_in, float *acc_out, int64_t ld_acc,
+                                 void *workspace, cudaStream_t stream);
+sp_status launch_cache_evict(const sp_cache &src, const int32_t *lens, int64_t max_len, const float *acc, int64_t ld_acc,
+                             int64_t budget, int64_t recent, const sp_cache &dst, int32_t *kept, float *acc_out,
+                             int64_t ld_acc_out, int32_t *lens_out, cudaStream_t stream);
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -1,0 +1,77 @@
+// Asynchronous copies into shared memory (TMA) and the barriers they complete on.
+//
+// Every wait is bounded: a wait that runs out marks the block as failed, after which its other
+// waits give up at once, the block drains the copies it has in flight and returns; the host
+// reads the mark with sp_wait_status.  Nothing traps or spins for ever.
+#pragma once
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sp_device.cuh"
+#include "sp_internal.h"
+
+namespace sp {
+
+constexpr uint32_t kWaitLimit = 1u << 22;  // tries of one wait: seconds, against microseconds
+
+static __device__ unsigned int g_expired_waits;
+
+static cudaError_t read_expired_waits(unsigned int *out, bool clear) {
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_expired_waits, sizeof(unsigned int));
+    if (e == cudaSuccess && clear) {
+        const unsigned int zero = 0;
+        e = cudaMemcpyToSymbol(g_expired_waits, &zero, sizeof zero);
+    }
+    return e;
+}
+namespace {
+struct WaitRegistration {
+    WaitRegistration() { register_wait_reader(read_expired_waits); }
+};
+const WaitRegistration g_wait_registration;
+}  // namespace
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0u;
+}
+// True once the phase of the given parity has completed; false if the wait ran out or another
+// thread of the block has given up.
+__device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
+    if (mbar_try(bar, parity)) return true;
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if (*failed != 0u) return false;
+    }
+    *failed = 1u;
+    atomicAdd(&g_expired_waits, 1u);
+    return false;
+}
+
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+// Box of a 2-D tensor at (x, y) -> shared memory.  x * element size is a multiple of 16 bytes.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// Describes a row-major matrix of `rows` rows of `row_bytes` bytes (pitch a multiple of 16) as
+// boxes of 128 bytes x `box_rows`, laid into shared memory with the 128-byte swizzle (the
+// 16-byte chunk c of row r lands at chunk c ^ (r & 7)); what lies outside reads as zero.
+// Elements are bytes.  api_serve.cu holds the driver entry point.
+cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t row_bytes,
+                              int64_t pitch, int box_rows);
+
+}  // namespace sp
