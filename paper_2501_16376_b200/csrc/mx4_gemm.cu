@@ -1,0 +1,271 @@
+// Product of two microscaled 4-bit matrices on the 4-bit tensor cores (long prompts): the
+// activations are quantised first (mx4_quantize.cu, into the workspace), then
+//     Y [tokens, rows] = Xq Wq^T,   both operands as they are stored, scales included.
+//
+// Bound by the tensor cores at many tokens, by the weights' bytes at few.  A tile is 128 tokens x
+// N rows of the weights (N = 64 .. 256, see tile_rows), summed over the columns 256 at a time:
+// one thread keeps kStages of both operands and their scale tiles in flight by TMA, one issues
+// the products (64 columns each; scale tiles go to tensor memory by a copy just before), four
+// warps empty the accumulators.  Two accumulators alternate so that emptying one overlaps
+// filling the other; 2 x 256 columns and the scales do not fit 512, so the two share 64 columns,
+// which are emptied first.
+#include <algorithm>
+
+#include "mx4_common.cuh"
+#include "sp_tcgen05.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int kTileTokens = 128;
+constexpr int kStageBytesA = kTileTokens * 128;
+constexpr int kTmemColumns = 512;
+constexpr int kScaleColumns = 448;  // two buffers of 24 columns: A 2 tiles x 4, B 2 x 8
+
+struct GemmArgs {
+    const uint8_t *scale_x, *scale_w;
+    uint16_t *Y;
+    int64_t n_tokens, n_rows, ldy;
+    int tile_cols;  // scale tiles along the columns
+    int steps;      // 256-column stages
+    int token_tiles, tiles;
+    int vec_y;
+};
+
+}  // namespace
+
+template <bool BF16, int N, int STAGES>
+__global__ void __launch_bounds__(256, 1)
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const GemmArgs a) {
+    constexpr int kStageBytesB = N * 128;
+    constexpr int kOperandBytes = kStageBytesA + kStageBytesB;
+    constexpr int kScaleTilesB = N > 128 ? 2 : 1;           // row tiles of scales under a tile of N rows
+    constexpr int kScaleBytes = 2 * kMx4TileBytes * (1 + kScaleTilesB);
+    constexpr int kSecond = N == 256 ? 192 : N;             // column of the second accumulator
+    constexpr int kShared = N == 256 ? 2 : 0;               // its first 32-column pieces that the first one shares
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free, drained;
+    __shared__ uint32_t tmem_base, failed;
+    uint8_t *const operands = smem, *const scales = smem + STAGES * kOperandBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&x_map);
+        tma_prefetch_map(&w_map);
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(smem_addr(&full[s]), 1);
+            mbar_init(smem_addr(&empty[s]), 1);
+        }
+        mbar_init(smem_addr(&acc_full[0]), 1);
+        mbar_init(smem_addr(&acc_full[1]), 1);
+        mbar_init(smem_addr(&acc_free), 128);
+        mbar_init(smem_addr(&drained), 1);
+        failed = 0u;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(&tmem_base, kTmemColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base;
+    pdl_launch_dependents();
+    pdl_wait();
+
+    if (warp == 0 && lane == 0) {
+        int step = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
+            const int m = tile % a.token_tiles, n = tile / a.token_tiles;
+            const int64_t wt = int64_t(n) * N / kMx4TileRows;
+            const int w_tiles = static_cast<int>(min(int64_t(kScaleTilesB), mx4_tile_rows(a.n_rows) - wt));
+            for (int k = 0; k < a.steps; ++k, ++step) {
+                const int slot = step % STAGES;
+                if (step >= STAGES && !mbar_wait_or_fail(smem_addr(&empty[slot]), (step / STAGES - 1) & 1, &failed)) { ok = false; break; }
+                const uint32_t bar = smem_addr(&full[slot]);
+                const int cols = min(2, a.tile_cols - 2 * k);
+                const uint32_t to = smem_addr(operands + slot * kOperandBytes), sc = smem_addr(scales + slot * kScaleBytes);
+                mbar_expect_tx(bar, kOperandBytes + cols * kMx4TileBytes * (1 + w_tiles));
+                tma_load_2d(to, &x_map, k * 128, m * kTileTokens, bar);
+                tma_load_2d(to + kStageBytesA, &w_map, k * 128, n * N, bar);
+                bulk_load(sc, a.scale_x + (int64_t(m) * a.tile_cols + 2 * k) * kMx4TileBytes, cols * kMx4TileBytes, bar);
+                for (int i = 0; i < w_tiles; ++i)
+                    bulk_load(sc + (1 + i) * 2 * kMx4TileBytes, a.scale_w + ((wt + i) * a.tile_cols + 2 * k) * kMx4TileBytes,
+                              cols * kMx4TileBytes, bar);
+            }
+        }
+        if (failed != 0u)
+            for (int s = max(0, step - STAGES); s < step; ++s) mbar_wait(smem_addr(&full[s % STAGES]), (s / STAGES) & 1);
+    } else if (warp == 1 && lane == 0) {
+        int step = 0, count = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+            const int n = tile / a.token_tiles;
+            if (count > 0 && !mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed)) break;
+            tcgen05_fence_after();
+            const uint32_t acc = tmem + (count & 1) * kSecond;
+            // a tile of 64 or 192 rows may begin in the middle of a tile of scales
+            const uint32_t skip = (n * N % kMx4TileRows) / 32;
+            for (int k = 0; k < a.steps; ++k, ++step) {
+                const int slot = step % STAGES;
+                if (!mbar_wait_or_fail(smem_addr(&full[slot]), (step / STAGES) & 1, &failed)) { ok = false; break; }
+                // the scale columns written now were last read two stages ago
+                if (step >= 2 && !mbar_wait_or_fail(smem_addr(&empty[(step - 2) % STAGES]), ((step - 2) / STAGES) & 1, &failed)) { ok = false; break; }
+                tcgen05_fence_after();
+                const uint32_t sc = smem_addr(scales + slot * kScaleBytes);
+                const uint32_t sfa = tmem + kScaleColumns + (step & 1) * 24, sfb = sfa + 8;
+                const uint64_t da = desc_rows128(smem_addr(operands + slot * kOperandBytes));
+                const uint64_t db = desc_rows128(smem_addr(operands + slot * kOperandBytes + kStageBytesA));
+                const int products = min(4, (a.tile_cols - 2 * k) * 2);
+                for (int c = 0; c < products / 2; ++c) {
+                    tmem_copy_scales(sfa + c * 4, desc_scales(sc + c * kMx4TileBytes));
+                    for (int i = 0; i < kScaleTilesB; ++i)
+                        tmem_copy_scales(sfb + c * 8 + i * 4, desc_scales(sc + ((1 + i) * 2 + c) * kMx4TileBytes));
+                }
+                for (int p = 0; p < products; ++p)
+                    mma_mxf4(acc, da + p * 2, db + p * 2, mxf4_instruction(N, p & 1), sfa + (p >> 1) * 4,
+                             sfb + (p >> 1) * 8 + skip, k > 0 || p > 0);
+                tcgen05_commit(smem_addr(&empty[slot]));
+            }
+            if (ok) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+        }
+        if (failed != 0u) {
+            tcgen05_commit(smem_addr(&drained));
+            mbar_wait(smem_addr(&drained), 0);
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3;
+        int count = 0;
+        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++count) {
+            const int m = tile % a.token_tiles, n = tile / a.token_tiles;
+            const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
+            tcgen05_fence_after();
+            const uint32_t acc = tmem + (count & 1) * kSecond + (static_cast<uint32_t>(quarter * 32) << 16);
+            const int64_t token = int64_t(m) * kTileTokens + quarter * 32 + lane;
+            if (kShared == 0) {
+                tcgen05_fence_before();
+                mbar_arrive(smem_addr(&acc_free));
+            }
+#pragma unroll 1
+            for (int i = 0; i < N / 32; ++i) {
+                // shared columns first: the last pieces of the first accumulator, the first of the second
+                const int piece = kShared != 0 && (count & 1) == 0 ? (i + N / 32 - kShared) % (N / 32) : i;
+                uint32_t v[32];
+                tmem_load32(acc + piece * 32, v);
+                tmem_load_wait();
+                if (kShared != 0 && i == kShared - 1) {
+                    tcgen05_fence_before();
+                    mbar_arrive(smem_addr(&acc_free));
+                }
+                const int64_t row = int64_t(n) * N + piece * 32;
+                if (token < a.n_tokens && row < a.n_rows) {
+                    uint16_t *y = a.Y + token * a.ldy + row;
+                    uint32_t h[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float lo = __uint_as_float(v[2 * j]), hi = __uint_as_float(v[2 * j + 1]);
+                        if constexpr (BF16) {
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+                            h[j] = *reinterpret_cast<const uint32_t *>(&b);
+                        } else {
+                            const __half2 b = __floats2half2_rn(lo, hi);
+                            h[j] = *reinterpret_cast<const uint32_t *>(&b);
+                        }
+                    }
+                    if (a.vec_y && row + 32 <= a.n_rows) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            reinterpret_cast<uint4 *>(y)[j] = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (row + j < a.n_rows) y[j] = static_cast<uint16_t>(j & 1 ? h[j >> 1] >> 16 : h[j >> 1]);
+                    }
+                }
+            }
+        }
+        tcgen05_fence_before();
+    }
+    __syncthreads();
+    if (warp == 2) {
+        tcgen05_fence_after();
+        tmem_free(tmem, kTmemColumns);
+    }
+}
+
+// Rows of the weights in a tile: the size that needs the least time in whole rounds over the SMs
+// (a round costs N and something like 32 for filling and emptying).
+static int tile_rows(int64_t token_tiles, int64_t n_rows, int sms) {
+    int best = 256;
+    int64_t least = INT64_MAX;
+    for (int n = 256; n >= 64; n -= 64) {
+        const int64_t tiles = token_tiles * ((n_rows + n - 1) / n);
+        const int64_t cost = (tiles + sms - 1) / sms * (n + 32);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
+}
+
+template <bool BF16, int N, int STAGES>
+static sp_status launch_gemm(const CUtensorMap &x_map, const CUtensorMap &w_map, GemmArgs a, int sms, cudaStream_t stream) {
+    auto *kernel = mx4_gemm_kernel<BF16, N, STAGES>;
+    static DynamicSmem limit;
+    cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
+    if (e != cudaSuccess) return cuda_fail(e);
+    PdlConfig pdl(dim3(static_cast<unsigned>(std::min(a.tiles, sms))), dim3(256), stream);
+    pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2));
+    e = cudaLaunchKernelEx(&pdl.cfg, kernel, x_map, w_map, a);
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+int64_t mx4_gemm_workspace(int64_t n_tokens, int64_t n_cols) {
+    return (n_tokens * mx4_blocks(n_cols) * 16 + 127) / 128 * 128 + mx4_tile_rows(n_tokens) * mx4_tile_cols(n_cols) * kMx4TileBytes;
+}
+
+sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t stream) {
+    const int64_t pitch = mx4_blocks(p.n_cols) * 16;
+    uint8_t *codes = static_cast<uint8_t *>(workspace);
+    uint8_t *scales = codes + (p.n_tokens * pitch + 127) / 128 * 128;
+    sp_status st = launch_mx4_quantize(p.X, p.dtype, p.n_tokens, p.n_cols, p.ldx, nullptr, codes, pitch, scales, stream);
+    if (st != SP_OK) return st;
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_fail(e);
+    GemmArgs a = {};
+    a.scale_x = scales;
+    a.scale_w = p.scales;
+    a.Y = static_cast<uint16_t *>(p.Y);
+    a.n_tokens = p.n_tokens;
+    a.n_rows = p.n_rows;
+    a.ldy = p.ldy;
+    a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
+    a.steps = (a.tile_cols + 1) / 2;
+    a.vec_y = aligned16(p.Y) && p.ldy % 8 == 0;
+    const int64_t token_tiles = (p.n_tokens + kTileTokens - 1) / kTileTokens;
+    const int n = tile_rows(token_tiles, p.n_rows, sms);
+    const int64_t tiles = token_tiles * ((p.n_rows + n - 1) / n);
+    if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
+    a.token_tiles = static_cast<int>(token_tiles);
+    a.tiles = static_cast<int>(tiles);
+    CUtensorMap x_map, w_map;
+    e = encode_byte_tiles(&x_map, codes, p.n_tokens, pitch, pitch, kTileTokens);
+    if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, pitch, p.ldc, n);
+    if (e != cudaSuccess) return cuda_fail(e);
+#define SP_LAUNCH(NN, S)                                                                        \
+    return p.dtype == SP_BF16 ? launch_gemm<true, NN, S>(x_map, w_map, a, sms, stream)          \
+                              : launch_gemm<false, NN, S>(x_map, w_map, a, sms, stream)
+    switch (n) {
+        case 64: SP_LAUNCH(64, 8);
+        case 128: SP_LAUNCH(128, 6);
+        case 192: SP_LAUNCH(192, 5);
+        default: SP_LAUNCH(256, 4);
+    }
+#undef SP_LAUNCH
+}
+
+}  // namespace sp
