@@ -48,9 +48,9 @@ cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 
 constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens of a 4-bit product
 
-// Whether a product takes the 4-bit tensor cores: from 33 tokens on, where streaming the weights
-// past registers would take a second pass.
-static bool takes_gemm4(int64_t n_tokens, int mode) { return mode == SP_MX4_A4 && n_tokens > 32; }
+// Whether a product takes the kernels that tile over tokens: from 33 tokens on, where streaming
+// the weights past registers would take a second pass.
+static bool takes_tiles(int64_t n_tokens) { return n_tokens > 32; }
 
 static sp_status check_codes(const void *codes, int64_t ldc, const void *scales, int64_t n_cols) {
     if (codes == nullptr || scales == nullptr) return SP_ERR_INVALID_ARG;
@@ -116,7 +116,9 @@ sp_status sp_mx4_linear_workspace(int64_t n_tokens, int64_t n_rows, int64_t n_co
     if (bytes == nullptr || n_tokens < 0 || n_rows < 0 || n_cols < 0) return SP_ERR_INVALID_ARG;
     if (mode != SP_MX4_A16 && mode != SP_MX4_A4) return SP_ERR_INVALID_ARG;
     if (n_tokens > kMaxMx4Side || n_rows > kMaxMx4Side || n_cols > kMaxMx4Side) return SP_ERR_SHAPE;
-    *bytes = n_rows > 0 && n_cols > 0 && takes_gemm4(n_tokens, mode) ? mx4_gemm_workspace(n_tokens, n_cols) : 0;
+    *bytes = 0;
+    if (n_rows > 0 && n_cols > 0 && takes_tiles(n_tokens))
+        *bytes = mode == SP_MX4_A4 ? mx4_gemm_workspace(n_tokens, n_cols) : mx4_gemm16_workspace(n_tokens, n_cols);
     return SP_OK;
 }
 
@@ -135,7 +137,9 @@ sp_status sp_mx4_linear(const void *X, sp_dtype dtype, int64_t n_tokens, int64_t
     if (st != SP_OK) return st;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
     const Mx4Product p{X, n_tokens, ldx, codes, ldc, scales, n_rows, n_cols, Y, ldy, dtype, mode == SP_MX4_A4};
-    if (takes_gemm4(n_tokens, mode)) return launch_mx4_gemm(p, workspace, static_cast<cudaStream_t>(stream));
+    if (takes_tiles(n_tokens))
+        return p.quantize_x ? launch_mx4_gemm(p, workspace, static_cast<cudaStream_t>(stream))
+                            : launch_mx4_gemm16(p, workspace, static_cast<cudaStream_t>(stream));
     return launch_mx4_stream(p, static_cast<cudaStream_t>(stream));
 }
 

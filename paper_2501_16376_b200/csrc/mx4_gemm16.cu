@@ -1,0 +1,346 @@
+// Product of 16-bit activations with a microscaled 4-bit matrix on the 16-bit tensor cores (more
+// tokens than the streaming kernel takes in a pass).
+//
+// Mathematics: Y^T [rows, tokens] = V X^T, V = code * 2^(byte - 127) brought to the activations'
+// type in shared memory on the way to the tensor cores.  In bf16 that is exact (4-bit codes and
+// powers of two fit at every scale).  binary16 has not the range, so a row of V is kept relative
+// to its largest scale R: V = code * 2^(byte - R + 13), 49152 at most, and the sums are multiplied
+// by 2^(R - 140) when they leave; blocks whose scale lies more than 2^36 below the row's largest
+// lose bits that are as far below the row's largest products.
+//
+// Bound by the tensor cores.  The weights are the 128 rows of a tile because that side is the one
+// that has to be converted: every weight once for up to 256 tokens, 16 weights a cycle, which
+// eight warps do beside the products.  One thread streams the activations by TMA, one the codes,
+// one issues the products, four warps empty the accumulators (two, alternating: 2 x 256 columns).
+#include <algorithm>
+
+#include "mx4_common.cuh"
+#include "sp_tcgen05.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int kSlots = 3;                        // stages of 64 columns: converted weights and activations
+constexpr int kCodeSlots = 3;                    // stages of 256 columns: codes and scales as stored
+constexpr int kWeightBytes = kMx4TileRows * 128; // 128 rows x 64 columns of 16 bits
+constexpr int kMostTokens = 256;
+constexpr int kSlotBytes = kWeightBytes + kMostTokens * 128;
+constexpr int kCodeSlotBytes = kMx4TileRows * 128 + 2 * kMx4TileBytes;
+constexpr int kTmemColumns = 512;
+constexpr int kThreads = 512;  // 4 warps of single threads' roles, 4 that empty, 8 that convert
+
+struct Gemm16Args {
+    const uint8_t *scales;
+    uint16_t *Y;
+    int64_t n_tokens, n_rows, ldy;
+    int tile_cols;    // scale tiles along the columns
+    int steps;        // 64-column stages
+    int tile_tokens;  // tokens of a tile, a multiple of 16
+    int row_tiles, tiles;
+};
+
+// 2^e as binary16 bits, 0 below its range.
+__device__ __forceinline__ uint32_t half_pow2(int e) {
+    return e >= -14 ? static_cast<uint32_t>(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u;
+}
+
+// Eight codes -> eight values in the activations' type; `factor` holds the scale in both halves.
+template <bool BF16>
+__device__ __forceinline__ uint4 convert8(uint32_t w, uint32_t factor) {
+    uint32_t h[4];
+    if constexpr (BF16) {
+        // bytes of the bf16 magnitudes by table, signs from bit 3 of the codes
+        const uint32_t sel = w & 0x77777777u, up = w << 4;
+        const uint32_t hi_a = prmt(0x3f3f3f00u, 0x40404040u, sel) | (prmt(up, w, 0x5140u) & 0x80808080u);
+        const uint32_t hi_b = prmt(0x3f3f3f00u, 0x40404040u, sel >> 16) | (prmt(up, w, 0x7362u) & 0x80808080u);
+        const uint32_t lo_a = prmt(0xc0800000u, 0xc0804000u, sel), lo_b = prmt(0xc0800000u, 0xc0804000u, sel >> 16);
+        h[0] = prmt(lo_a, hi_a, 0x5140u);
+        h[1] = prmt(lo_a, hi_a, 0x7362u);
+        h[2] = prmt(lo_b, hi_b, 0x5140u);
+        h[3] = prmt(lo_b, hi_b, 0x7362u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("mul.bf16x2 %0, %0, %1;" : "+r"(h[i]) : "r"(factor));
+    } else {
+        mx4_unpack8(w, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("mul.f16x2 %0, %0, %1;" : "+r"(h[i]) : "r"(factor));
+    }
+    return make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+}  // namespace
+
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads, 1)
+mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Gemm16Args a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots], acc_full[2], acc_free, drained;
+    __shared__ uint32_t tmem_base, failed;
+    __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
+    uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&x_map);
+        tma_prefetch_map(&w_map);
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(smem_addr(&full[s]), 9);  // the activations' copy and eight converting warps
+            mbar_init(smem_addr(&empty[s]), 1);
+        }
+        for (int s = 0; s < kCodeSlots; ++s) {
+            mbar_init(smem_addr(&code_full[s]), 1);
+            mbar_init(smem_addr(&code_empty[s]), 8);
+        }
+        mbar_init(smem_addr(&acc_full[0]), 1);
+        mbar_init(smem_addr(&acc_full[1]), 1);
+        mbar_init(smem_addr(&acc_free), 128);
+        mbar_init(smem_addr(&drained), 1);
+        failed = 0u;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(&tmem_base, kTmemColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int code_steps = (a.steps + 3) / 4;
+
+    if (warp == 0 && lane == 0) {
+        int step = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
+            const int n = tile / a.row_tiles;
+            for (int k = 0; k < a.steps; ++k, ++step) {
+                const int slot = step % kSlots;
+                if (step >= kSlots && !mbar_wait_or_fail(smem_addr(&empty[slot]), (step / kSlots - 1) & 1, &failed)) { ok = false; break; }
+                const uint32_t bar = smem_addr(&full[slot]);
+                mbar_expect_tx(bar, a.tile_tokens * 128);
+                tma_load_2d(smem_addr(slots + slot * kSlotBytes + kWeightBytes), &x_map, k * 128, n * a.tile_tokens, bar);
+            }
+        }
+        // a barrier that the converting warps no longer complete says nothing of the copy: the
+        // block ends only after its slots' copies had the time of a bounded wait
+        if (failed != 0u)
+            for (int s = max(0, step - kSlots); s < step; ++s) mbar_wait(smem_addr(&full[s % kSlots]), (s / kSlots) & 1);
+    } else if (warp == 3 && lane == 0) {
+        int step = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
+            const int m = tile % a.row_tiles;
+            for (int k = 0; k < code_steps; ++k, ++step) {
+                const int slot = step % kCodeSlots;
+                if (step >= kCodeSlots && !mbar_wait_or_fail(smem_addr(&code_empty[slot]), (step / kCodeSlots - 1) & 1, &failed)) { ok = false; break; }
+                const uint32_t bar = smem_addr(&code_full[slot]), to = smem_addr(codes + slot * kCodeSlotBytes);
+                const int cols = min(2, a.tile_cols - 2 * k);
+                mbar_expect_tx(bar, kMx4TileRows * 128 + cols * kMx4TileBytes);
+                tma_load_2d(to, &w_map, k * 128, m * kMx4TileRows, bar);
+                bulk_load(to + kMx4TileRows * 128, a.scales + (int64_t(m) * a.tile_cols + 2 * k) * kMx4TileBytes,
+                          cols * kMx4TileBytes, bar);
+            }
+        }
+        if (failed != 0u)
+            for (int s = max(0, step - kCodeSlots); s < step; ++s) mbar_wait(smem_addr(&code_full[s % kCodeSlots]), (s / kCodeSlots) & 1);
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t instruction = f16_instruction(a.tile_tokens, BF16);
+        int step = 0, count = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+            if (count > 0 && !mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed)) break;
+            tcgen05_fence_after();
+            const uint32_t acc = tmem + (count & 1) * 256;
+            for (int k = 0; k < a.steps; ++k, ++step) {
+                const int slot = step % kSlots;
+                if (!mbar_wait_or_fail(smem_addr(&full[slot]), (step / kSlots) & 1, &failed)) { ok = false; break; }
+                tcgen05_fence_after();
+                const uint64_t da = desc_rows128(smem_addr(slots + slot * kSlotBytes));
+                const uint64_t db = desc_rows128(smem_addr(slots + slot * kSlotBytes + kWeightBytes));
+#pragma unroll
+                for (int p = 0; p < 4; ++p) mma_16bit(acc, da + p * 2, db + p * 2, instruction, k > 0 || p > 0);
+                tcgen05_commit(smem_addr(&empty[slot]));
+            }
+            if (ok) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+        }
+        if (failed != 0u) {
+            tcgen05_commit(smem_addr(&drained));
+            mbar_wait(smem_addr(&drained), 0);
+        }
+    } else if (warp >= 8) {
+        // a thread converts one block of 32 columns of a stage: row and half
+        const int row = (threadIdx.x - 256) >> 1, half = threadIdx.x & 1, swap = row & 7;
+        const uint32_t scale_at = (row & 31) * 16 + (row >> 5) * 4;
+        int step = 0, code_step = 0, count = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+            int top = 0;
+            if constexpr (!BF16) {
+                const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + scale_at;
+                uint32_t most = 0;
+#pragma unroll 4
+                for (int c = half; c < a.tile_cols; c += 2) {
+                    uint32_t w = *reinterpret_cast<const uint32_t *>(s + int64_t(c) * kMx4TileBytes);
+                    w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
+                    most = __vmaxu4(most, w);
+                }
+                most = __vmaxu4(most, most >> 16);
+                most = max(most & 0xffu, (most >> 8) & 0xffu);
+                top = static_cast<int>(max(most, __shfl_xor_sync(kFullWarp, most, 1)));
+                if (half == 0) row_top[count & 3][row] = top;
+            }
+            for (int k = 0; ok && k < a.steps; ++k, ++step) {
+                const int slot = step % kSlots, code_slot = code_step % kCodeSlots, sub = k & 3;
+                if (sub == 0) ok = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed));
+                if (ok && step >= kSlots)
+                    ok = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&empty[slot]), (step / kSlots - 1) & 1, &failed));
+                if (!ok) break;
+                const uint8_t *in = codes + code_slot * kCodeSlotBytes;
+                const uint32_t byte = in[kMx4TileRows * 128 + (sub >> 1) * kMx4TileBytes + scale_at + (sub & 1) * 2 + half];
+                uint32_t factor;
+                if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
+                else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
+                factor |= factor << 16;
+                const uint4 w = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
+                uint8_t *out = slots + slot * kSlotBytes + row * 128;
+                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<uint4 *>(out + (((half * 4 + i) ^ swap) << 4)) = convert8<BF16>(words[i], factor);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_addr(&full[slot]));
+                    if (sub == 3 || k == a.steps - 1) mbar_arrive(smem_addr(&code_empty[code_slot]));
+                }
+                if (sub == 3 || k == a.steps - 1) ++code_step;
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3;
+        int count = 0;
+        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++count) {
+            const int m = tile % a.row_tiles, n = tile / a.row_tiles;
+            const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
+            tcgen05_fence_after();
+            tcgen05_fence_before();
+            mbar_arrive(smem_addr(&acc_free));  // the other accumulator was emptied before
+            const uint32_t acc = tmem + (count & 1) * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
+            const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
+            float f0 = 1.0f, f1 = 1.0f;
+            if constexpr (!BF16) {
+                const int e = row_top[count & 3][quarter * 32 + lane] - 140;
+                f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
+                f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
+            }
+            const int64_t token0 = int64_t(n) * a.tile_tokens;
+            const int tokens = static_cast<int>(min(int64_t(a.tile_tokens), a.n_tokens - token0));
+#pragma unroll 1
+            for (int c = 0; c < tokens; c += 32) {
+                uint32_t v[32];
+                tmem_load32(acc + c, v);
+                tmem_load_wait();
+                if (row < a.n_rows) {
+                    uint16_t *y = a.Y + (token0 + c) * a.ldy + row;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (c + j < tokens) {
+                            const float x = __uint_as_float(v[j]) * f0 * f1;
+                            if constexpr (BF16) y[j * a.ldy] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+                            else y[j * a.ldy] = __half_as_ushort(__float2half_rn(x));
+                        }
+                }
+                __syncwarp();
+            }
+        }
+        tcgen05_fence_before();
+    }
+    __syncthreads();
+    if (warp == 2) {
+        tcgen05_fence_after();
+        tmem_free(tmem, kTmemColumns);
+    }
+}
+
+// Activations that TMA cannot read (rows not on 16-byte boundaries) are copied to rows that are.
+__global__ void __launch_bounds__(256)
+mx4_align_rows_kernel(const uint16_t *__restrict__ X, int64_t ldx, int64_t n_cols, uint16_t *__restrict__ out, int64_t pitch) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t row = blockIdx.x;
+    for (int64_t c = threadIdx.x; c < n_cols; c += blockDim.x) out[row * pitch + c] = X[row * ldx + c];
+}
+
+// Tokens of a tile: as few rounds over the SMs as possible, each as short as possible (a round
+// of less than 112 tokens is bound by the conversion).
+static int tile_tokens(int64_t n_tokens, int64_t row_tiles, int sms) {
+    int best = 16;
+    int64_t least = INT64_MAX;
+    const int64_t first = (n_tokens + kMostTokens - 1) / kMostTokens;
+    for (int64_t parts = first; parts <= first + 8; ++parts) {
+        const int64_t n = ((n_tokens + parts - 1) / parts + 15) / 16 * 16;
+        const int64_t tiles = row_tiles * ((n_tokens + n - 1) / n);
+        const int64_t cost = (tiles + sms - 1) / sms * std::max(n, int64_t(112));
+        if (cost < least) {
+            least = cost;
+            best = static_cast<int>(n);
+        }
+    }
+    return best;
+}
+
+int64_t mx4_gemm16_workspace(int64_t n_tokens, int64_t n_cols) { return n_tokens * ((n_cols + 7) / 8 * 8) * 2; }
+
+sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t stream) {
+    const void *X = p.X;
+    int64_t ldx = p.ldx;
+    cudaError_t e;
+    if (!aligned16(X) || ldx % 8 != 0) {
+        ldx = (p.n_cols + 7) / 8 * 8;
+        if (p.n_tokens > 0x7fffffff) return SP_ERR_SHAPE;
+        PdlConfig copy(dim3(static_cast<unsigned>(p.n_tokens)), dim3(256), stream);
+        e = cudaLaunchKernelEx(&copy.cfg, mx4_align_rows_kernel, static_cast<const uint16_t *>(X), p.ldx, p.n_cols,
+                               static_cast<uint16_t *>(workspace), ldx);
+        if (e != cudaSuccess) return cuda_fail(e);
+        sp_status st = check_launch();
+        if (st != SP_OK) return st;
+        X = workspace;
+    }
+    int device = 0, sms = 0;
+    e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_fail(e);
+    Gemm16Args a = {};
+    a.scales = p.scales;
+    a.Y = static_cast<uint16_t *>(p.Y);
+    a.n_tokens = p.n_tokens;
+    a.n_rows = p.n_rows;
+    a.ldy = p.ldy;
+    a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
+    a.steps = static_cast<int>((p.n_cols + 63) / 64);
+    const int64_t row_tiles = mx4_tile_rows(p.n_rows);
+    a.tile_tokens = tile_tokens(p.n_tokens, row_tiles, sms);
+    const int64_t tiles = row_tiles * ((p.n_tokens + a.tile_tokens - 1) / a.tile_tokens);
+    if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
+    a.row_tiles = static_cast<int>(row_tiles);
+    a.tiles = static_cast<int>(tiles);
+    CUtensorMap x_map, w_map;
+    e = encode_byte_tiles(&x_map, X, p.n_tokens, p.n_cols * 2, ldx * 2, a.tile_tokens);
+    if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
+    if (e != cudaSuccess) return cuda_fail(e);
+    PdlConfig pdl(dim3(static_cast<unsigned>(std::min(a.tiles, sms))), dim3(kThreads), stream);
+    pdl.cfg.dynamicSmemBytes = kSlots * kSlotBytes + kCodeSlots * kCodeSlotBytes;
+    if (p.dtype == SP_BF16) {
+        static DynamicSmem limit;
+        e = limit.allow(reinterpret_cast<const void *>(mx4_gemm16_kernel<true>));
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, mx4_gemm16_kernel<true>, x_map, w_map, a);
+    } else {
+        static DynamicSmem limit;
+        e = limit.allow(reinterpret_cast<const void *>(mx4_gemm16_kernel<false>));
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, mx4_gemm16_kernel<false>, x_map, w_map, a);
+    }
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+}  // namespace sp

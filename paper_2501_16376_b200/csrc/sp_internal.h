@@ -248,6 +248,9 @@ sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream);
 // mx4_gemm.cu: both operands in 4 bits (quantises X into the workspace first)
 int64_t mx4_gemm_workspace(int64_t n_tokens, int64_t n_cols);
 sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t stream);
+// mx4_gemm16.cu: 16-bit activations (the workspace takes rows that TMA cannot read)
+int64_t mx4_gemm16_workspace(int64_t n_tokens, int64_t n_cols);
+sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t stream);
 
 // cache_append.cu, cache_attention.cu, cache_evict.cu: the 8-bit key/value cache
 sp_status launch_cache_append(const sp_cache &cache, const void *K, const sp_strides &ks, const void *V,

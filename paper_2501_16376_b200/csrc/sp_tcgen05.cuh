@@ -57,6 +57,18 @@ __device__ __forceinline__ void tmem_copy_scales(uint32_t dst, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
 }
 
+// D [128 x n] (+)= A [128 x 16] B [n x 16]^T of 16-bit floats, binary32 sums.
+__device__ __forceinline__ uint32_t f16_instruction(int n, bool bf16) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void mma_16bit(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(accumulate ? 1u : 0u) : "memory");
+}
+// Shared memory written by ordinary stores becomes visible to the tensor cores' reads.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // D [128 x n] (+)= A [128 x 64] B [n x 64]^T of 4-bit floats with a scale for every 32.
 // `half`: which two of a tile's four blocks the 64 columns are.
 __device__ __forceinline__ uint32_t mxf4_instruction(int n, int half) {
