@@ -48,7 +48,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free, drained;
     __shared__ uint32_t tmem_base, failed;
     uint8_t *const operands = smem, *const scales = smem + STAGES * kOperandBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
         tma_prefetch_map(&w_map);
@@ -71,66 +71,84 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     pdl_launch_dependents();
     pdl_wait();
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        RingPlace<STAGES> at;
         int step = 0;
         bool ok = true;
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
             const int m = tile % a.token_tiles, n = tile / a.token_tiles;
             const int64_t wt = int64_t(n) * N / kMx4TileRows;
             const int w_tiles = static_cast<int>(min(int64_t(kScaleTilesB), mx4_tile_rows(a.n_rows) - wt));
-            for (int k = 0; k < a.steps; ++k, ++step) {
-                const int slot = step % STAGES;
-                if (step >= STAGES && !mbar_wait_or_fail(smem_addr(&empty[slot]), (step / STAGES - 1) & 1, &failed)) { ok = false; break; }
-                const uint32_t bar = smem_addr(&full[slot]);
-                const int cols = min(2, a.tile_cols - 2 * k);
-                const uint32_t to = smem_addr(operands + slot * kOperandBytes), sc = smem_addr(scales + slot * kScaleBytes);
-                mbar_expect_tx(bar, kOperandBytes + cols * kMx4TileBytes * (1 + w_tiles));
-                tma_load_2d(to, &x_map, k * 128, m * kTileTokens, bar);
-                tma_load_2d(to + kStageBytesA, &w_map, k * 128, n * N, bar);
-                bulk_load(sc, a.scale_x + (int64_t(m) * a.tile_cols + 2 * k) * kMx4TileBytes, cols * kMx4TileBytes, bar);
-                for (int i = 0; i < w_tiles; ++i)
-                    bulk_load(sc + (1 + i) * 2 * kMx4TileBytes, a.scale_w + ((wt + i) * a.tile_cols + 2 * k) * kMx4TileBytes,
-                              cols * kMx4TileBytes, bar);
+            const uint8_t *sx = a.scale_x + int64_t(m) * a.tile_cols * kMx4TileBytes;
+            const uint8_t *sw = a.scale_w + wt * a.tile_cols * kMx4TileBytes;
+            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+                if (step >= STAGES) ok = mbar_wait_or_fail(smem_addr(&empty[at.slot]), at.parity ^ 1u, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                if (elect_one()) {
+                    const uint32_t bar = smem_addr(&full[at.slot]);
+                    const int bytes = min(2, a.tile_cols - 2 * k) * kMx4TileBytes;
+                    const uint32_t to = smem_addr(operands + at.slot * kOperandBytes), sc = smem_addr(scales + at.slot * kScaleBytes);
+                    mbar_expect_tx(bar, kOperandBytes + bytes * (1 + w_tiles));
+                    tma_load_2d(to, &x_map, k * 128, m * kTileTokens, bar);
+                    tma_load_2d(to + kStageBytesA, &w_map, k * 128, n * N, bar);
+                    bulk_load(sc, sx + k * (2 * kMx4TileBytes), bytes, bar);
+                    for (int i = 0; i < w_tiles; ++i)
+                        bulk_load(sc + (1 + i) * 2 * kMx4TileBytes, sw + (int64_t(i) * a.tile_cols + 2 * k) * kMx4TileBytes, bytes, bar);
+                }
+                __syncwarp();
             }
         }
-        if (failed != 0u)
+        if (failed != 0u && lane == 0)
             for (int s = max(0, step - STAGES); s < step; ++s) mbar_wait(smem_addr(&full[s % STAGES]), (s / STAGES) & 1);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
+        RingPlace<STAGES> at, before;  // `before` follows two stages behind
         int step = 0, count = 0;
         bool ok = true;
+        const uint64_t desc0 = desc_rows128(smem_addr(operands)), scale0 = desc_scales(smem_addr(scales));
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
             const int n = tile / a.token_tiles;
-            if (count > 0 && !mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed)) break;
-            tcgen05_fence_after();
+            if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
             const uint32_t acc = tmem + (count & 1) * kSecond;
             // a tile of 64 or 192 rows may begin in the middle of a tile of scales
             const uint32_t skip = (n * N % kMx4TileRows) / 32;
-            for (int k = 0; k < a.steps; ++k, ++step) {
-                const int slot = step % STAGES;
-                if (!mbar_wait_or_fail(smem_addr(&full[slot]), (step / STAGES) & 1, &failed)) { ok = false; break; }
+            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+                ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
                 // the scale columns written now were last read two stages ago
-                if (step >= 2 && !mbar_wait_or_fail(smem_addr(&empty[(step - 2) % STAGES]), ((step - 2) / STAGES) & 1, &failed)) { ok = false; break; }
-                tcgen05_fence_after();
-                const uint32_t sc = smem_addr(scales + slot * kScaleBytes);
-                const uint32_t sfa = tmem + kScaleColumns + (step & 1) * 24, sfb = sfa + 8;
-                const uint64_t da = desc_rows128(smem_addr(operands + slot * kOperandBytes));
-                const uint64_t db = desc_rows128(smem_addr(operands + slot * kOperandBytes + kStageBytesA));
-                const int products = min(4, (a.tile_cols - 2 * k) * 2);
-                for (int c = 0; c < products / 2; ++c) {
-                    tmem_copy_scales(sfa + c * 4, desc_scales(sc + c * kMx4TileBytes));
-                    for (int i = 0; i < kScaleTilesB; ++i)
-                        tmem_copy_scales(sfb + c * 8 + i * 4, desc_scales(sc + ((1 + i) * 2 + c) * kMx4TileBytes));
+                if (step >= 2) {
+                    ok = ok && mbar_wait_or_fail(smem_addr(&empty[before.slot]), before.parity, &failed);
+                    before.next();
                 }
-                for (int p = 0; p < products; ++p)
-                    mma_mxf4(acc, da + p * 2, db + p * 2, mxf4_instruction(N, p & 1), sfa + (p >> 1) * 4,
-                             sfb + (p >> 1) * 8 + skip, k > 0 || p > 0);
-                tcgen05_commit(smem_addr(&empty[slot]));
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    const uint32_t sfa = tmem + kScaleColumns + (step & 1) * 24, sfb = sfa + 8;
+                    const uint64_t da = desc0 + static_cast<uint32_t>(at.slot * (kOperandBytes / 16)), db = da + kStageBytesA / 16;
+                    const uint64_t sc = scale0 + static_cast<uint32_t>(at.slot * (kScaleBytes / 16));
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (2 * k + c >= a.tile_cols) break;
+                        tmem_copy_scales(sfa + c * 4, sc + c * (kMx4TileBytes / 16));
+#pragma unroll
+                        for (int i = 0; i < kScaleTilesB; ++i)
+                            tmem_copy_scales(sfb + c * 8 + i * 4, sc + ((1 + i) * 2 + c) * (kMx4TileBytes / 16));
+                    }
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        if (2 * k + (p >> 1) >= a.tile_cols) break;
+                        mma_mxf4(acc, da + p * 2, db + p * 2, mxf4_instruction(N, p & 1), sfa + (p >> 1) * 4,
+                                 sfb + (p >> 1) * 8 + skip, k > 0 || p > 0);
+                    }
+                    tcgen05_commit(smem_addr(&empty[at.slot]));
+                    if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+                }
+                __syncwarp();
             }
-            if (ok) tcgen05_commit(smem_addr(&acc_full[count & 1]));
         }
         if (failed != 0u) {
-            tcgen05_commit(smem_addr(&drained));
-            mbar_wait(smem_addr(&drained), 0);
+            if (elect_one()) tcgen05_commit(smem_addr(&drained));
+            __syncwarp();
+            if (lane == 0) mbar_wait(smem_addr(&drained), 0);
         }
     } else if (warp >= 4) {
         const int quarter = warp & 3;

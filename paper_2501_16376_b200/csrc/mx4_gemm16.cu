@@ -79,7 +79,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     __shared__ uint32_t tmem_base, failed;
     __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
         tma_prefetch_map(&w_map);
@@ -107,64 +107,77 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     pdl_wait();
     const int code_steps = (a.steps + 3) / 4;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        RingPlace<kSlots> at;
         int step = 0;
         bool ok = true;
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
             const int n = tile / a.row_tiles;
-            for (int k = 0; k < a.steps; ++k, ++step) {
-                const int slot = step % kSlots;
-                if (step >= kSlots && !mbar_wait_or_fail(smem_addr(&empty[slot]), (step / kSlots - 1) & 1, &failed)) { ok = false; break; }
-                const uint32_t bar = smem_addr(&full[slot]);
-                mbar_expect_tx(bar, a.tile_tokens * 128);
-                tma_load_2d(smem_addr(slots + slot * kSlotBytes + kWeightBytes), &x_map, k * 128, n * a.tile_tokens, bar);
+            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+                if (step >= kSlots) ok = mbar_wait_or_fail(smem_addr(&empty[at.slot]), at.parity ^ 1u, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                if (elect_one()) {
+                    const uint32_t bar = smem_addr(&full[at.slot]);
+                    mbar_expect_tx(bar, a.tile_tokens * 128);
+                    tma_load_2d(smem_addr(slots + at.slot * kSlotBytes + kWeightBytes), &x_map, k * 128, n * a.tile_tokens, bar);
+                }
+                __syncwarp();
             }
         }
         // a barrier that the converting warps no longer complete says nothing of the copy: the
         // block ends only after its slots' copies had the time of a bounded wait
-        if (failed != 0u)
+        if (failed != 0u && lane == 0)
             for (int s = max(0, step - kSlots); s < step; ++s) mbar_wait(smem_addr(&full[s % kSlots]), (s / kSlots) & 1);
-    } else if (warp == 3 && lane == 0) {
+    } else if (warp == 3) {
+        RingPlace<kCodeSlots> at;
         int step = 0;
         bool ok = true;
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
             const int m = tile % a.row_tiles;
-            for (int k = 0; k < code_steps; ++k, ++step) {
-                const int slot = step % kCodeSlots;
-                if (step >= kCodeSlots && !mbar_wait_or_fail(smem_addr(&code_empty[slot]), (step / kCodeSlots - 1) & 1, &failed)) { ok = false; break; }
-                const uint32_t bar = smem_addr(&code_full[slot]), to = smem_addr(codes + slot * kCodeSlotBytes);
-                const int cols = min(2, a.tile_cols - 2 * k);
-                mbar_expect_tx(bar, kMx4TileRows * 128 + cols * kMx4TileBytes);
-                tma_load_2d(to, &w_map, k * 128, m * kMx4TileRows, bar);
-                bulk_load(to + kMx4TileRows * 128, a.scales + (int64_t(m) * a.tile_cols + 2 * k) * kMx4TileBytes,
-                          cols * kMx4TileBytes, bar);
+            const uint8_t *sw = a.scales + int64_t(m) * a.tile_cols * kMx4TileBytes;
+            for (int k = 0; k < code_steps; ++k, ++step, at.next()) {
+                if (step >= kCodeSlots) ok = mbar_wait_or_fail(smem_addr(&code_empty[at.slot]), at.parity ^ 1u, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                if (elect_one()) {
+                    const uint32_t bar = smem_addr(&code_full[at.slot]), to = smem_addr(codes + at.slot * kCodeSlotBytes);
+                    const int bytes = min(2, a.tile_cols - 2 * k) * kMx4TileBytes;
+                    mbar_expect_tx(bar, kMx4TileRows * 128 + bytes);
+                    tma_load_2d(to, &w_map, k * 128, m * kMx4TileRows, bar);
+                    bulk_load(to + kMx4TileRows * 128, sw + k * (2 * kMx4TileBytes), bytes, bar);
+                }
+                __syncwarp();
             }
         }
-        if (failed != 0u)
+        if (failed != 0u && lane == 0)
             for (int s = max(0, step - kCodeSlots); s < step; ++s) mbar_wait(smem_addr(&code_full[s % kCodeSlots]), (s / kCodeSlots) & 1);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         const uint32_t instruction = f16_instruction(a.tile_tokens, BF16);
-        int step = 0, count = 0;
+        const uint64_t desc0 = desc_rows128(smem_addr(slots));
+        RingPlace<kSlots> at;
+        int count = 0;
         bool ok = true;
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
-            if (count > 0 && !mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed)) break;
-            tcgen05_fence_after();
+            if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
             const uint32_t acc = tmem + (count & 1) * 256;
-            for (int k = 0; k < a.steps; ++k, ++step) {
-                const int slot = step % kSlots;
-                if (!mbar_wait_or_fail(smem_addr(&full[slot]), (step / kSlots) & 1, &failed)) { ok = false; break; }
+            for (int k = 0; k < a.steps; ++k, at.next()) {
+                ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 tcgen05_fence_after();
-                const uint64_t da = desc_rows128(smem_addr(slots + slot * kSlotBytes));
-                const uint64_t db = desc_rows128(smem_addr(slots + slot * kSlotBytes + kWeightBytes));
+                if (elect_one()) {
+                    const uint64_t da = desc0 + static_cast<uint32_t>(at.slot * (kSlotBytes / 16)), db = da + kWeightBytes / 16;
 #pragma unroll
-                for (int p = 0; p < 4; ++p) mma_16bit(acc, da + p * 2, db + p * 2, instruction, k > 0 || p > 0);
-                tcgen05_commit(smem_addr(&empty[slot]));
+                    for (int p = 0; p < 4; ++p) mma_16bit(acc, da + p * 2, db + p * 2, instruction, k > 0 || p > 0);
+                    tcgen05_commit(smem_addr(&empty[at.slot]));
+                    if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+                }
+                __syncwarp();
             }
-            if (ok) tcgen05_commit(smem_addr(&acc_full[count & 1]));
         }
         if (failed != 0u) {
-            tcgen05_commit(smem_addr(&drained));
-            mbar_wait(smem_addr(&drained), 0);
+            if (elect_one()) tcgen05_commit(smem_addr(&drained));
+            __syncwarp();
+            if (lane == 0) mbar_wait(smem_addr(&drained), 0);
         }
     } else if (warp >= 8) {
         // a thread converts one block of 32 columns of a stage: row and half
