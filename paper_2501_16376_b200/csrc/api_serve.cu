@@ -46,6 +46,10 @@ cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, 
     return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, row_bytes, pitch, box_rows);
 }
 
+cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, rows, cols, ld * 2, box_rows);
+}
+
 constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens of a 4-bit product
 
 // Whether a product takes the kernels that tile over tokens: from 33 tokens on, where streaming

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kTileTokens = 128;
 constexpr int kStageBytesA = kTileTokens * 128;
+constexpr int kOutBytes = 32 * 128;   // a warp's piece of the output, 32 tokens x 64 rows, on its way out
 constexpr int kTmemColumns = 512;
 constexpr int kScaleColumns = 448;  // two buffers of 24 columns: A 2 tiles x 4, B 2 x 8
 
@@ -30,24 +31,25 @@ struct GemmArgs {
     int tile_cols;  // scale tiles along the columns
     int steps;      // 256-column stages
     int token_tiles, tiles;
-    int vec_y;
+    int tma_y;
 };
 
 }  // namespace
 
 template <bool BF16, int N, int STAGES>
 __global__ void __launch_bounds__(256, 1)
-mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const GemmArgs a) {
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
+                const __grid_constant__ CUtensorMap y_map, const GemmArgs a) {
     constexpr int kStageBytesB = N * 128;
     constexpr int kOperandBytes = kStageBytesA + kStageBytesB;
     constexpr int kScaleTilesB = N > 128 ? 2 : 1;           // row tiles of scales under a tile of N rows
     constexpr int kScaleBytes = 2 * kMx4TileBytes * (1 + kScaleTilesB);
     constexpr int kSecond = N == 256 ? 192 : N;             // column of the second accumulator
-    constexpr int kShared = N == 256 ? 2 : 0;               // its first 32-column pieces that the first one shares
+    constexpr int kShared = N == 256 ? 64 : 0;              // its first columns that the first one shares
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free, drained;
     __shared__ uint32_t tmem_base, failed;
-    uint8_t *const operands = smem, *const scales = smem + STAGES * kOperandBytes;
+    uint8_t *const operands = smem, *const out_stage = smem + STAGES * kOperandBytes, *const scales = out_stage + 4 * kOutBytes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
@@ -159,49 +161,57 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
             const uint32_t acc = tmem + (count & 1) * kSecond + (static_cast<uint32_t>(quarter * 32) << 16);
-            const int64_t token = int64_t(m) * kTileTokens + quarter * 32 + lane;
+            const int64_t token0 = int64_t(m) * kTileTokens + quarter * 32, token = token0 + lane;
             if (kShared == 0) {
                 tcgen05_fence_before();
                 mbar_arrive(smem_addr(&acc_free));
             }
 #pragma unroll 1
-            for (int i = 0; i < N / 32; ++i) {
-                // shared columns first: the last pieces of the first accumulator, the first of the second
-                const int piece = kShared != 0 && (count & 1) == 0 ? (i + N / 32 - kShared) % (N / 32) : i;
-                uint32_t v[32];
-                tmem_load32(acc + piece * 32, v);
+            for (int i = 0; i < N / 64; ++i) {
+                // the shared columns first: the last piece of the first accumulator, the first of the second
+                const int piece = kShared != 0 && (count & 1) == 0 ? (i + N / 64 - 1) % (N / 64) : i;
+                uint32_t v[64];
+                tmem_load32(acc + piece * 64, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
+                tmem_load32(acc + piece * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
                 tmem_load_wait();
-                if (kShared != 0 && i == kShared - 1) {
+                if (kShared != 0 && i == 0) {
                     tcgen05_fence_before();
                     mbar_arrive(smem_addr(&acc_free));
                 }
-                const int64_t row = int64_t(n) * N + piece * 32;
-                if (token < a.n_tokens && row < a.n_rows) {
-                    uint16_t *y = a.Y + token * a.ldy + row;
-                    uint32_t h[16];
+                const int64_t row = int64_t(n) * N + piece * 64;
+                uint32_t h[32];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float lo = __uint_as_float(v[2 * j]), hi = __uint_as_float(v[2 * j + 1]);
-                        if constexpr (BF16) {
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-                            h[j] = *reinterpret_cast<const uint32_t *>(&b);
-                        } else {
-                            const __half2 b = __floats2half2_rn(lo, hi);
-                            h[j] = *reinterpret_cast<const uint32_t *>(&b);
-                        }
-                    }
-                    if (a.vec_y && row + 32 <= a.n_rows) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            reinterpret_cast<uint4 *>(y)[j] = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                for (int j = 0; j < 32; ++j) {
+                    const float lo = __uint_as_float(v[2 * j]), hi = __uint_as_float(v[2 * j + 1]);
+                    if constexpr (BF16) {
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+                        h[j] = *reinterpret_cast<const uint32_t *>(&b);
                     } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (row + j < a.n_rows) y[j] = static_cast<uint16_t>(j & 1 ? h[j >> 1] >> 16 : h[j >> 1]);
+                        const __half2 b = __floats2half2_rn(lo, hi);
+                        h[j] = *reinterpret_cast<const uint32_t *>(&b);
                     }
+                }
+                if (a.tma_y) {
+                    uint8_t *const stage = out_stage + quarter * kOutBytes;
+                    if (lane == 0) tma_store_wait_read();
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                            make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && token0 < a.n_tokens && row < a.n_rows)
+                        tma_store_2d(&y_map, smem_addr(stage), static_cast<int>(row), static_cast<int>(token0));
+                } else if (token < a.n_tokens) {
+                    uint16_t *y = a.Y + token * a.ldy + row;
+#pragma unroll
+                    for (int j = 0; j < 64; ++j)
+                        if (row + j < a.n_rows) y[j] = static_cast<uint16_t>(j & 1 ? h[j >> 1] >> 16 : h[j >> 1]);
                 }
             }
         }
+        if (lane == 0) tma_store_wait();
         tcgen05_fence_before();
     }
     __syncthreads();
@@ -228,14 +238,14 @@ static int tile_rows(int64_t token_tiles, int64_t n_rows, int sms) {
 }
 
 template <bool BF16, int N, int STAGES>
-static sp_status launch_gemm(const CUtensorMap &x_map, const CUtensorMap &w_map, GemmArgs a, int sms, cudaStream_t stream) {
+static sp_status launch_gemm(const CUtensorMap &x_map, const CUtensorMap &w_map, const CUtensorMap &y_map, GemmArgs a, int sms, cudaStream_t stream) {
     auto *kernel = mx4_gemm_kernel<BF16, N, STAGES>;
     static DynamicSmem limit;
     cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
     if (e != cudaSuccess) return cuda_fail(e);
     PdlConfig pdl(dim3(static_cast<unsigned>(std::min(a.tiles, sms))), dim3(256), stream);
-    pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2));
-    e = cudaLaunchKernelEx(&pdl.cfg, kernel, x_map, w_map, a);
+    pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2)) + 4 * kOutBytes;
+    e = cudaLaunchKernelEx(&pdl.cfg, kernel, x_map, w_map, y_map, a);
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }
@@ -263,24 +273,25 @@ sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t str
     a.ldy = p.ldy;
     a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
     a.steps = (a.tile_cols + 1) / 2;
-    a.vec_y = aligned16(p.Y) && p.ldy % 8 == 0;
+    a.tma_y = aligned16(p.Y) && p.ldy % 8 == 0;
     const int64_t token_tiles = (p.n_tokens + kTileTokens - 1) / kTileTokens;
     const int n = tile_rows(token_tiles, p.n_rows, sms);
     const int64_t tiles = token_tiles * ((p.n_rows + n - 1) / n);
     if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
     a.token_tiles = static_cast<int>(token_tiles);
     a.tiles = static_cast<int>(tiles);
-    CUtensorMap x_map, w_map;
+    CUtensorMap x_map, w_map, y_map = {};
     e = encode_byte_tiles(&x_map, codes, p.n_tokens, pitch, pitch, kTileTokens);
     if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, pitch, p.ldc, n);
+    if (e == cudaSuccess && a.tma_y) e = encode_half_tiles(&y_map, p.Y, p.n_tokens, p.n_rows, p.ldy, 32);
     if (e != cudaSuccess) return cuda_fail(e);
 #define SP_LAUNCH(NN, S)                                                                        \
-    return p.dtype == SP_BF16 ? launch_gemm<true, NN, S>(x_map, w_map, a, sms, stream)          \
-                              : launch_gemm<false, NN, S>(x_map, w_map, a, sms, stream)
+    return p.dtype == SP_BF16 ? launch_gemm<true, NN, S>(x_map, w_map, y_map, a, sms, stream)          \
+                              : launch_gemm<false, NN, S>(x_map, w_map, y_map, a, sms, stream)
     switch (n) {
         case 64: SP_LAUNCH(64, 8);
         case 128: SP_LAUNCH(128, 6);
-        case 192: SP_LAUNCH(192, 5);
+        case 192: SP_LAUNCH(192, 4);
         default: SP_LAUNCH(256, 4);
     }
 #undef SP_LAUNCH

@@ -67,11 +67,25 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                  "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
+// Shared memory -> box of a 2-D tensor at (x, y), both inside it; what lies outside is not written.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
+                 "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// Until the stores this thread issued have read their shared memory / have completed.
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // Describes a row-major matrix of `rows` rows of `row_bytes` bytes (pitch a multiple of 16) as
 // boxes of 128 bytes x `box_rows`, laid into shared memory with the 128-byte swizzle (the
 // 16-byte chunk c of row r lands at chunk c ^ (r & 7)); what lies outside reads as zero.
 // Elements are bytes.  api_serve.cu holds the driver entry point.
 cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t row_bytes,
                               int64_t pitch, int box_rows);
+// The same for 16-bit elements (an inner extent that is not a multiple of 16 bytes is clipped
+// exactly): boxes of 64 elements x box_rows.
+cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld,
+                              int box_rows);
 
 }  // namespace sp
