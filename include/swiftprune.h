@@ -461,7 +461,8 @@ sp_status sp_mx4_linear(const void *X, sp_dtype dtype, int64_t n_tokens, int64_t
  * sequence b lies in block table[b, j / block_tokens] at place j % block_tokens.  A table entry
  * outside [0, n_blocks) names no block: its tokens are not written and take no part.
  * All pointers are device pointers; k and v 16-byte aligned.  Requirements: head_dim 64 or 128,
- * block_tokens 16, 32 or 64 (else SP_ERR_SHAPE).  The calls work on the CURRENT device.
+ * block_tokens 16, 32 or 64, n_kv_heads <= 65535, n_seqs <= 32767 (else SP_ERR_SHAPE).  The calls
+ * work on the CURRENT device.
  */
 typedef struct {
     void *k, *v;               /* codes [n_blocks, n_kv_heads, block_tokens, head_dim] */

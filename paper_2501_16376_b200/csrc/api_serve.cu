@@ -70,7 +70,7 @@ static sp_status check_cache(const sp_cache *c) {
     if (c->n_blocks < 0 || c->n_seqs < 0 || c->table_cols < 0 || c->n_kv_heads < 1) return SP_ERR_INVALID_ARG;
     if (c->head_dim != 64 && c->head_dim != 128) return SP_ERR_SHAPE;
     if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64) return SP_ERR_SHAPE;
-    if (c->ld_table < c->table_cols || c->n_kv_heads > 65535 || c->n_seqs > 65535) return SP_ERR_SHAPE;
+    if (c->ld_table < c->table_cols || c->n_kv_heads > 65535 || c->n_seqs > 32767) return SP_ERR_SHAPE;
     if (c->table_cols > kMaxCacheTokens / c->block_tokens) return SP_ERR_SHAPE;
     if (c->n_seqs > 0 && c->table_cols > 0 && c->table == nullptr) return SP_ERR_INVALID_ARG;
     if (c->n_blocks > 0 && (c->k == nullptr || c->v == nullptr || c->k_scale == nullptr || c->v_scale == nullptr))

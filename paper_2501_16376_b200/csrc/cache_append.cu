@@ -15,48 +15,53 @@ struct AppendArgs {
     sp_cache cache;
     const uint16_t *x[2];  // K, V
     sp_strides stride[2];
-    int64_t n_new;
+    int n_new;
     const int32_t *start, *count;
-    int64_t touched;  // cache blocks a sequence's new tokens can touch
 };
 
 }  // namespace
 
-// CHUNKS 16-byte pieces of the new values a thread: block_tokens * head_dim / 8 / 128
-template <bool BF16, int CHUNKS, bool VEC>
+template <bool BF16, int D, int T, bool VEC>
 __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
+    constexpr int kRowChunks = D / 8;               // 16-byte pieces of a token's new values
+    constexpr int kChunks = T * kRowChunks / 128;   // of the tile, for a thread
     __shared__ uint32_t warp_amax[4];
     const sp_cache &c = a.cache;
-    const int which = blockIdx.z, head = blockIdx.y;
-    const int64_t seq = blockIdx.x / a.touched;
-    const int D = c.head_dim, T = c.block_tokens, row_chunks = D / 8;
+    const int which = blockIdx.z & 1, head = blockIdx.y;
+    const int64_t seq = blockIdx.z >> 1;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t begin = a.start[seq];
-    const int64_t n = a.count != nullptr ? min(int64_t(a.count[seq]), a.n_new) : a.n_new;
+    const int begin = a.start[seq];
+    const int n = a.count != nullptr ? min(a.count[seq], a.n_new) : a.n_new;
     if (begin < 0 || n <= 0) return;
-    const int64_t place = begin / T + blockIdx.x % a.touched;
-    if (place * T >= begin + n) return;
+    const int64_t place = begin / T + int(blockIdx.x);
+    const int64_t first = place * T - begin;        // the tile's first token among the new ones
+    if (first >= n) return;
+
+    // the new values are on their way before the table is looked up
+    const uint16_t *x = a.x[which] + seq * a.stride[which].seq + head * a.stride[which].head;
+    const int64_t pitch = a.stride[which].token;
+    const int d = threadIdx.x % kRowChunks * 8, row = threadIdx.x / kRowChunks;
+    constexpr int kRowStep = 128 / kRowChunks;
+    uint32_t p[kChunks][4];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int64_t token = first + row + i * kRowStep;
+        if (token >= 0 && token < n) load8<VEC, true>(x + token * pitch, d, D, p[i]);
+        else p[i][0] = p[i][1] = p[i][2] = p[i][3] = 0u;
+    }
     const int64_t block = cache_block(c, seq, place);
     if (block < 0) return;
-
-    const uint16_t *x = a.x[which] + seq * a.stride[which].seq + head * a.stride[which].head;
-    uint8_t *codes = static_cast<uint8_t *>(which == 0 ? c.k : c.v) + (block * c.n_kv_heads + head) * T * D;
+    uint8_t *codes = static_cast<uint8_t *>(which == 0 ? c.k : c.v) + (block * c.n_kv_heads + head) * (T * D);
     float *scale = (which == 0 ? c.k_scale : c.v_scale) + block * c.n_kv_heads + head;
-    const bool has_old = begin > place * T;
-    const int e_old = has_old ? exponent_of(*scale) : kMinCacheExponent;
+    const int e_old = first < 0 ? exponent_of(*scale) : kMinCacheExponent;
 
-    uint32_t p[CHUNKS][4], amax = 0;
+    uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-        const int at = threadIdx.x + i * 128;
-        const int64_t token = place * T + at / row_chunks - begin;
-        if (token >= 0 && token < n) {
-            load8<VEC, true>(x + token * a.stride[which].token, at % row_chunks * 8, D, p[i]);
-            float v[8];
-            unpack8<BF16>(p[i], v);
-            amax = max(amax, finite_amax8(v));
-        }
+    for (int i = 0; i < kChunks; ++i) {
+        float v[8];
+        unpack8<BF16>(p[i], v);
+        amax = max(amax, finite_amax8(v));
     }
     amax = __reduce_max_sync(kFullWarp, amax);
     if ((threadIdx.x & 31) == 0) warp_amax[threadIdx.x >> 5] = amax;
@@ -65,10 +70,9 @@ __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
     const int e = max(cache_exponent(amax), e_old);
     const float inv = pow2(-e);
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-        const int at = threadIdx.x + i * 128;
-        const int64_t token = place * T + at / row_chunks - begin;
-        uint2 *out = reinterpret_cast<uint2 *>(codes) + at;
+    for (int i = 0; i < kChunks; ++i) {
+        const int64_t token = first + row + i * kRowStep;
+        uint2 *out = reinterpret_cast<uint2 *>(codes) + threadIdx.x + i * 128;
         float v[8];
         if (token >= 0 && token < n) {
             unpack8<BF16>(p[i], v);
@@ -95,29 +99,31 @@ sp_status launch_cache_append(const sp_cache &cache, const void *K, const sp_str
     a.x[1] = static_cast<const uint16_t *>(V);
     a.stride[0] = ks;
     a.stride[1] = vs;
-    a.n_new = n_new;
+    a.n_new = static_cast<int>(n_new);
     a.start = start;
     a.count = count;
-    a.touched = (n_new + cache.block_tokens - 2) / cache.block_tokens + 1;
-    if (a.touched > 0x7fffffff / cache.n_seqs) return SP_ERR_SHAPE;
     bool vec = aligned16(K) && aligned16(V);
     for (const sp_strides &s : a.stride) vec = vec && s.seq % 8 == 0 && s.token % 8 == 0 && s.head % 8 == 0;
-    PdlConfig pdl(dim3(static_cast<unsigned>(a.touched * cache.n_seqs), cache.n_kv_heads, 2), dim3(128), stream);
-    const int chunks = cache.block_tokens * cache.head_dim / 1024;
+    // x: the cache blocks that a sequence's new tokens can touch
+    const int64_t touched = (n_new + cache.block_tokens - 2) / cache.block_tokens + 1;
+    PdlConfig pdl(dim3(static_cast<unsigned>(touched), cache.n_kv_heads, static_cast<unsigned>(cache.n_seqs * 2)), dim3(128),
+                  stream);
     cudaError_t e = cudaErrorInvalidValue;
-#define SP_LAUNCH(C)                                                                          \
-    if (chunks == C) {                                                                        \
-        if (dtype == SP_BF16)                                                                 \
-            e = vec ? cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<true, C, true>, a)     \
-                    : cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<true, C, false>, a);   \
-        else                                                                                  \
-            e = vec ? cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<false, C, true>, a)    \
-                    : cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<false, C, false>, a);  \
+#define SP_LAUNCH(D, T)                                                                          \
+    if (cache.head_dim == D && cache.block_tokens == T) {                                        \
+        if (dtype == SP_BF16)                                                                    \
+            e = vec ? cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<true, D, T, true>, a)     \
+                    : cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<true, D, T, false>, a);   \
+        else                                                                                     \
+            e = vec ? cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<false, D, T, true>, a)    \
+                    : cudaLaunchKernelEx(&pdl.cfg, cache_append_kernel<false, D, T, false>, a);  \
     }
-    SP_LAUNCH(1)
-    SP_LAUNCH(2)
-    SP_LAUNCH(4)
-    SP_LAUNCH(8)
+    SP_LAUNCH(64, 16)
+    SP_LAUNCH(64, 32)
+    SP_LAUNCH(64, 64)
+    SP_LAUNCH(128, 16)
+    SP_LAUNCH(128, 32)
+    SP_LAUNCH(128, 64)
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();

@@ -151,59 +151,70 @@ __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const Sele
     if (a.lens_out != nullptr && row % a.n_kv_heads == 0 && tid == 0) a.lens_out[seq] = static_cast<int32_t>(m);
 }
 
-// CHUNKS pieces of 8 codes a thread: block_tokens * head_dim / 8 / 128
-template <int CHUNKS>
+template <int D, int T>
 __global__ void __launch_bounds__(128)
-cache_gather_kernel(const sp_cache src, const sp_cache dst, const int32_t *__restrict__ kept, int64_t budget,
-                    int64_t places) {
+cache_gather_kernel(const sp_cache src, const sp_cache dst, const int32_t *__restrict__ kept, int budget) {
+    constexpr int kRowChunks = D / 8;               // pieces of 8 codes of a token
+    constexpr int kChunks = T * kRowChunks / 128;   // of the tile, for a thread
+    constexpr int kRowStep = 128 / kRowChunks;
     __shared__ uint32_t warp_amax[4];
-    const int which = blockIdx.z, head = blockIdx.y, H = src.n_kv_heads;
-    const int64_t seq = blockIdx.x / places, place = blockIdx.x % places;
-    const int D = src.head_dim, T = src.block_tokens, row_chunks = D / 8;
+    const int which = blockIdx.z & 1, head = blockIdx.y, H = src.n_kv_heads;
+    const int64_t seq = blockIdx.z >> 1;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t to = cache_block(dst, seq, place);
+    const int d = threadIdx.x % kRowChunks, row = threadIdx.x / kRowChunks;
+    const int32_t *k = kept + (seq * H + head) * budget;
+    int j[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int64_t slot = int64_t(blockIdx.x) * T + row + i * kRowStep;
+        j[i] = slot < budget ? k[slot] : -1;
+    }
+    const int64_t to = cache_block(dst, seq, blockIdx.x);
     if (to < 0) return;
     const uint8_t *from = static_cast<const uint8_t *>(which == 0 ? src.k : src.v);
     const float *from_scale = which == 0 ? src.k_scale : src.v_scale;
-    uint2 w[CHUNKS];
-    float scale[CHUNKS];
-    uint32_t amax = 0;
+    uint2 w[kChunks];
+    float scale[kChunks];
+    int64_t at[kChunks];
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-        const int at = threadIdx.x + i * 128;
-        const int64_t slot = place * T + at / row_chunks;
-        const int64_t j = slot < budget ? kept[(seq * H + head) * budget + slot] : -1;
-        const int64_t block = j >= 0 ? cache_block(src, seq, j / T) : -1;
+    for (int i = 0; i < kChunks; ++i) at[i] = j[i] >= 0 ? cache_block(src, seq, unsigned(j[i]) / T) * H + head : -1;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
         w[i] = make_uint2(0u, 0u);
         scale[i] = 0.0f;
-        if (block >= 0) {
-            w[i] = __ldg(reinterpret_cast<const uint2 *>(from + ((block * H + head) * T + j % T) * D) + at % row_chunks);
-            scale[i] = from_scale[block * H + head];
+        if (at[i] >= 0) {
+            w[i] = __ldg(reinterpret_cast<const uint2 *>(from + (at[i] * T + unsigned(j[i]) % T) * D) + d);
+            scale[i] = from_scale[at[i]];
         }
     }
+    // the largest finite code of a piece, times its token's scale
+    uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
+    for (int i = 0; i < kChunks; ++i) {
         float v[8];
         e4m3_unpack8(w[i], v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= scale[i];
-        amax = max(amax, finite_amax8(v));
+        amax = max(amax, __float_as_uint(__uint_as_float(finite_amax8(v)) * scale[i]));
     }
     amax = __reduce_max_sync(kFullWarp, amax);
     if ((threadIdx.x & 31) == 0) warp_amax[threadIdx.x >> 5] = amax;
     __syncthreads();
     amax = max(max(warp_amax[0], warp_amax[1]), max(warp_amax[2], warp_amax[3]));
     const int e = cache_exponent(amax);
-    uint2 *out = reinterpret_cast<uint2 *>(static_cast<uint8_t *>(which == 0 ? dst.k : dst.v) + (to * H + head) * T * D);
+    const float inv = pow2(-e);
+    uint2 *out = reinterpret_cast<uint2 *>(static_cast<uint8_t *>(which == 0 ? dst.k : dst.v) + (to * H + head) * (T * D));
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-        float v[8];
-        e4m3_unpack8(w[i], v);
-        const float f = scale[i] * pow2(-e);
+    for (int i = 0; i < kChunks; ++i) {
+        const float f = scale[i] * inv;
+        uint2 y = w[i];
+        if (f != 1.0f) {  // most tokens keep their scale, and so their codes
+            float v[8];
+            e4m3_unpack8(w[i], v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= f;
-        out[threadIdx.x + i * 128] = e4m3_pack8(v);
+            for (int q = 0; q < 8; ++q) v[q] *= f;
+            y = e4m3_pack8(v);
+        }
+        out[threadIdx.x + i * 128] = y;
     }
     if (threadIdx.x == 0) (which == 0 ? dst.k_scale : dst.v_scale)[to * H + head] = pow2(e);
 }
@@ -213,7 +224,7 @@ sp_status launch_cache_evict(const sp_cache &src, const int32_t *lens, int64_t m
                              int64_t ld_acc_out, int32_t *lens_out, cudaStream_t stream) {
     const int64_t rows = src.n_seqs * src.n_kv_heads;
     const int64_t places = (budget + src.block_tokens - 1) / src.block_tokens;
-    if (rows > 0x7fffffff || places > 0x7fffffff / src.n_seqs) return SP_ERR_SHAPE;
+    if (rows > 0x7fffffff) return SP_ERR_SHAPE;
     SelectArgs a = {};
     a.lens = lens;
     a.acc = acc;
@@ -232,13 +243,19 @@ sp_status launch_cache_evict(const sp_cache &src, const int32_t *lens, int64_t m
     sp_status st = check_launch();
     if (st != SP_OK) return st;
     if (places == 0) return SP_OK;
-    PdlConfig pdl(dim3(static_cast<unsigned>(places * src.n_seqs), src.n_kv_heads, 2), dim3(128), stream);
-    switch (src.block_tokens * src.head_dim / 1024) {
-        case 1: e = cudaLaunchKernelEx(&pdl.cfg, cache_gather_kernel<1>, src, dst, kept, budget, places); break;
-        case 2: e = cudaLaunchKernelEx(&pdl.cfg, cache_gather_kernel<2>, src, dst, kept, budget, places); break;
-        case 4: e = cudaLaunchKernelEx(&pdl.cfg, cache_gather_kernel<4>, src, dst, kept, budget, places); break;
-        default: e = cudaLaunchKernelEx(&pdl.cfg, cache_gather_kernel<8>, src, dst, kept, budget, places); break;
-    }
+    PdlConfig pdl(dim3(static_cast<unsigned>(places), src.n_kv_heads, static_cast<unsigned>(src.n_seqs * 2)), dim3(128), stream);
+    const int kept_budget = static_cast<int>(budget);
+    e = cudaErrorInvalidValue;
+#define SP_LAUNCH(D, T)                                      \
+    if (src.head_dim == D && src.block_tokens == T)          \
+        e = cudaLaunchKernelEx(&pdl.cfg, cache_gather_kernel<D, T>, src, dst, kept, kept_budget);
+    SP_LAUNCH(64, 16)
+    SP_LAUNCH(64, 32)
+    SP_LAUNCH(64, 64)
+    SP_LAUNCH(128, 16)
+    SP_LAUNCH(128, 32)
+    SP_LAUNCH(128, 64)
+#undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }
