@@ -56,17 +56,33 @@ __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
     float *scale = (which == 0 ? c.k_scale : c.v_scale) + block * c.n_kv_heads + head;
     const int e_old = first < 0 ? exponent_of(*scale) : kMinCacheExponent;
 
+    // bit patterns of magnitudes order like the magnitudes; only a tile that holds something not
+    // finite looks again
+    auto reduce = [&](uint32_t m) {
+        m = __reduce_max_sync(kFullWarp, m);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) warp_amax[threadIdx.x >> 5] = m;
+        __syncthreads();
+        return max(max(warp_amax[0], warp_amax[1]), max(warp_amax[2], warp_amax[3]));
+    };
     uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        float v[8];
-        unpack8<BF16>(p[i], v);
-        amax = max(amax, finite_amax8(v));
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) amax = __vmaxu2(amax, p[i][k] & 0x7fff7fffu);
+    amax = max(amax & 0xffffu, amax >> 16);
+    amax = reduce(__float_as_uint(unpack2<BF16>(amax).x));
+    const bool finite = amax < 0x7f800000u;
+    if (!finite) {
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            float v[8];
+            unpack8<BF16>(p[i], v);
+            amax = max(amax, finite_amax8(v));
+        }
+        amax = reduce(amax);
     }
-    amax = __reduce_max_sync(kFullWarp, amax);
-    if ((threadIdx.x & 31) == 0) warp_amax[threadIdx.x >> 5] = amax;
-    __syncthreads();
-    amax = max(max(warp_amax[0], warp_amax[1]), max(warp_amax[2], warp_amax[3]));
     const int e = max(cache_exponent(amax), e_old);
     const float inv = pow2(-e);
 #pragma unroll
@@ -78,7 +94,7 @@ __global__ void __launch_bounds__(128) cache_append_kernel(const AppendArgs a) {
             unpack8<BF16>(p[i], v);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= inv;
-            *out = e4m3_pack8(v);
+            *out = finite ? e4m3_pack8_finite(v) : e4m3_pack8(v);
         } else if (token < 0 && e != e_old) {
             e4m3_unpack8(*out, v);
             const float f = pow2(e_old - e);

@@ -41,18 +41,26 @@ __device__ __forceinline__ void e4m3_unpack8(uint2 w, float (&v)[8]) {
         v[2 * i + 1] = f.y;
     }
 }
-// Eight binary32 values (at most 448 in magnitude, or not finite: stored as NaN) -> codes.
+// Eight binary32 values, at most 448 in magnitude -> codes; NaN stays NaN.
+__device__ __forceinline__ uint2 e4m3_pack8_finite(const float (&v)[8]) {
+    uint2 w;
+    asm("{\n\t.reg .b16 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 a, %3, %2;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 b, %5, %4;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 c, %7, %6;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 d, %9, %8;\n\t"
+        "mov.b32 %0, {a, b};\n\t"
+        "mov.b32 %1, {c, d};\n\t}"
+        : "=r"(w.x), "=r"(w.y)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return w;
+}
+// The same where infinities may occur: they are stored as NaN.
 __device__ __forceinline__ uint2 e4m3_pack8(const float (&v)[8]) {
-    uint32_t q[4];
+    float u[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint16_t h;
-        const float a = isfinite(v[2 * i]) ? v[2 * i] : __uint_as_float(0x7fc00000u);
-        const float b = isfinite(v[2 * i + 1]) ? v[2 * i + 1] : __uint_as_float(0x7fc00000u);
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(b), "f"(a));
-        q[i] = h;
-    }
-    return make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
+    for (int i = 0; i < 8; ++i) u[i] = isfinite(v[i]) ? v[i] : __uint_as_float(0x7fc00000u);
+    return e4m3_pack8_finite(u);
 }
 // Largest finite magnitude, as bits.
 __device__ __forceinline__ uint32_t finite_amax8(const float (&v)[8]) {
