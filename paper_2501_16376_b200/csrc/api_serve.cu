@@ -29,15 +29,17 @@ static PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
 }
 
 static cudaError_t encode_tiles(CUtensorMap *map, CUtensorMapDataType type, int element_bytes, const void *base,
-                                int64_t rows, int64_t row_elements, int64_t pitch_bytes, int box_rows) {
+                                int64_t rows, int64_t row_elements, int64_t pitch_bytes, int box_rows,
+                                int box_bytes = 128) {
     const auto encode = tensor_map_encoder();
     if (encode == nullptr) return cudaErrorNotSupported;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(row_elements), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch_bytes)};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / element_bytes), static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes / element_bytes), static_cast<cuuint32_t>(box_rows)};
     const cuuint32_t step[2] = {1, 1};
     const CUresult r = encode(map, type, 2, const_cast<void *>(base), dims, strides, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -46,6 +48,9 @@ cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, 
     return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, row_bytes, pitch, box_rows);
 }
 
+cudaError_t encode_byte_rows(CUtensorMap *map, const void *base, int64_t rows, int row_bytes, int box_rows) {
+    return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, row_bytes, row_bytes, box_rows, row_bytes);
+}
 cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
     return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, rows, cols, ld * 2, box_rows);
 }

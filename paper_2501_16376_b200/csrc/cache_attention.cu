@@ -9,26 +9,30 @@
 // Bound by memory: 2 * head_dim bytes per token and kv head.  The heads of a group and the query
 // tokens form the rows that share a pass, 8 (or 16) at a time.  Tokens are the long side of both
 // tensor-core products (m16n8k16 on binary16, to which e4m3 converts exactly), so that 8 rows
-// cost no padding to 16 and no operand passes through shared memory:
-//   S^T [16 tokens x 8 rows] = K [16 x D] Q^T: a lane loads D/4 consecutive bytes of two tokens'
+// cost no padding to 16 and no operand is rearranged:
+//   S^T [16 tokens x 8 rows] = K [16 x D] Q^T: a lane takes D/4 consecutive bytes of two tokens'
 //     keys - the order of the inner dimension is free as long as Q agrees - and uses them as they lie;
-//   O^T [D x 8 rows] += V^T [D x 16] P^T: a lane loads D/8 consecutive bytes of four tokens'
+//   O^T [D x 8 rows] += V^T [D x 16] P^T: a lane takes D/8 consecutive bytes of four tokens'
 //     values and interleaves pairs of tokens bytewise before converting; P^T is S^T transposed
 //     8x8 by movmatrix.
 // The block scale of K goes onto the scores and that of V onto the 16-token partial product, in
-// binary32.  P is rounded to binary16 for the product; for binary16 outputs the remainder follows
+// binary32.  Every warp has a ring of its own in shared memory, filled by TMA two steps of 16 tokens
+// ahead (128 KB in flight on an SM, no registers, no barrier but the copy's own; the swizzle keeps
+// both access patterns free of bank conflicts).  P is rounded to binary16 for the product; for binary16 outputs the remainder follows
 // as a second operand (2^-22 in all), since one rounding of P alone would be as large as that of
 // the output.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
 // the reductions of nearly all steps and leaves P at most 256.
 #include <algorithm>
 
 #include "cache_common.cuh"
+#include "sp_tma.cuh"
 
 namespace sp {
 
 namespace {
 
 constexpr int kAttnWarps = 4;
+constexpr int kRing = 3;           // steps of 16 tokens in a warp's ring
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;  // how far (in powers of two) a score may exceed the running maximum
 
@@ -38,7 +42,7 @@ struct AttnArgs {
     sp_strides q, o;
     int64_t n_q, max_len;
     int n_heads, group, rows;  // rows = n_q * group
-    int row_tiles, splits;
+    int row_tiles, splits, block_shift;  // block_tokens = 1 << block_shift
     const int32_t *lens;
     float scale_log2;
     uint16_t *O;
@@ -64,19 +68,18 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t u) { return unpack2<false>(u); }
 
-// N consecutive words of read-once cache data
+__device__ __forceinline__ float exp2_fast(float x) {  // what is below 2^-126 counts as 0
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 template <int N>
-__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N]) {
-    if constexpr (N == 2) {
-        const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(p));
-        w[0] = v.x; w[1] = v.y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(p + i * 4));
-            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
-        }
-    }
+__device__ __forceinline__ void read_piece(uint32_t src, uint32_t *w) {
+    if constexpr (N == 4)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src));
+    else
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(src));
 }
 
 // Place of a row's query token in its sequence, at most the last cached token; < 0: sees nothing.
@@ -89,26 +92,74 @@ __device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row
 
 // NT: tiles of 8 rows
 template <bool BF16, int D, int NT>
-__global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attention_kernel(const __grid_constant__ CUtensorMap k_map,
+                                                                                               const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
     constexpr int VW = D / 32;  // words of values a lane holds of one token
     constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
-    __shared__ float sh_o[kAttnWarps][NT * 8][D];
+    constexpr int kStage = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
+    extern __shared__ __align__(1024) uint8_t ring[];  // [warp][kRing][kStage]; afterwards the warps' sums
+    float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
     __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
+    __shared__ uint64_t full[kAttnWarps][kRing];
+    __shared__ uint32_t failed;
     __shared__ int nan_from[D];  // first token among the call's own whose value is NaN, by column
     const sp_cache &c = a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t seq = blockIdx.z;
     const int head = blockIdx.y / a.row_tiles, row0 = blockIdx.y % a.row_tiles * NT * 8;
-    const int H = c.n_kv_heads, T = c.block_tokens;
+    const int H = c.n_kv_heads, shift = a.block_shift;
     pdl_launch_dependents();
     for (int d = threadIdx.x; d < D; d += kAttnWarps * 32) nan_from[d] = 0x7fffffff;
+    if (threadIdx.x == 0) {
+        if (c.n_blocks > 0) {
+            tma_prefetch_map(&k_map);
+            tma_prefetch_map(&v_map);
+        }
+        for (int i = 0; i < kAttnWarps * kRing; ++i) mbar_init(smem_addr(&full[0][0] + i), 1);
+        failed = 0u;
+        mbar_fence_init();
+    }
+    __syncthreads();
     pdl_wait();
-    const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols * T)));
+    const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
     const int steps = (len + 15) / 16;
     const int first = static_cast<int>(int64_t(steps) * blockIdx.x / a.splits);
     const int last = static_cast<int>(int64_t(steps) * (blockIdx.x + 1) / a.splits);
+
+    // this warp's steps: first + warp, + kAttnWarps, ...; a step's block is looked up a round before
+    // its copy, its scales travel in registers
+    const int32_t *table = c.table + seq * c.ld_table;
+    const uint32_t my_ring = smem_addr(ring) + warp * (kRing * kStage);
+    auto block_of = [&](int step) {  // -1: none
+        if (step >= last) return -1;
+        const int id = table[step >> (shift - 4)];
+        return id >= 0 && id < c.n_blocks ? id : -1;
+    };
+    int blocks[kRing];  // of the steps in the ring, then of the one to be copied next
+    float2 scales[kRing];
+    auto copy_step = [&](int step, int block, int slot) {
+        float2 s = make_float2(0.0f, 0.0f);
+        if (block >= 0) {
+            const int64_t tile = int64_t(block) * H + head;
+            if (lane == 0) {
+                const uint32_t bar = smem_addr(&full[warp][slot]), to = my_ring + slot * kStage;
+                const int row = static_cast<int>((tile << shift) + ((step << 4) & ((1 << shift) - 1)));
+                mbar_expect_tx(bar, kStage);
+                tma_load_2d(to, &k_map, 0, row, bar);
+                tma_load_2d(to + kStage / 2, &v_map, 0, row, bar);
+            }
+            s = make_float2(c.k_scale[tile], c.v_scale[tile]);
+        }
+        return s;
+    };
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) blocks[i] = block_of(first + warp + i * kAttnWarps);
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) scales[i] = copy_step(first + warp + i * kAttnWarps, blocks[i], i);
+    RingPlace<kRing> place;
+    uint32_t parities = 0;  // bit: parity of the slot's next completion (a slot without a block has none)
 
     // queries: operand registers, and the factor that undoes their scaling
     uint32_t qf[NT][KW][2];
@@ -124,8 +175,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
             uint32_t raw[KW][2];
 #pragma unroll
             for (int s = 0; s < KW; ++s) {
-                raw[s][0] = q[4 * s] | (uint32_t(q[4 * s + 1]) << 16);
-                raw[s][1] = q[4 * s + 2] | (uint32_t(q[4 * s + 3]) << 16);
+                const uint16_t *at = q + s * 4;  // as the lane's words of K lie
+                raw[s][0] = at[0] | (uint32_t(at[1]) << 16);
+                raw[s][1] = at[2] | (uint32_t(at[3]) << 16);
             }
             if constexpr (BF16) {
                 // binary16 holds a row scaled by a power of two: its largest magnitude comes to
@@ -177,9 +229,22 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
     }
     __syncthreads();
 
+    // of token g, row 2t of this tile; 8-byte aligned where rows is even
+    float *const scores = a.scores + ((seq * H + head) * a.max_len + g) * a.rows + row0 + 2 * t;
     for (int step = first + warp; step < last; step += kAttnWarps) {
         const int j0 = step * 16;
-        const int64_t block = cache_block(c, seq, j0 / T);
+        const int block = blocks[0], slot = place.slot;
+        const int free_slot = slot == 0 ? kRing - 1 : slot - 1;
+        __syncwarp();  // every lane has read what the last step left there
+        scales[kRing - 1] = copy_step(step + (kRing - 1) * kAttnWarps, blocks[kRing - 1], free_slot);
+        const float k_scale = scales[0].x, v_scale = scales[0].y;
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) {
+            blocks[i] = blocks[i + 1];
+            scales[i] = scales[i + 1];
+        }
+        blocks[kRing - 1] = block_of(step + kRing * kAttnWarps);
+        place.next();
         if (block < 0) {
             if (a.scores != nullptr)
 #pragma unroll
@@ -192,16 +257,25 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
                     }
             continue;
         }
-        const int64_t at = ((block * H + head) * T + j0 % T) * D;
-        const uint8_t *kp = static_cast<const uint8_t *>(c.k) + at, *vp = static_cast<const uint8_t *>(c.v) + at;
+        if (!__all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&full[warp][slot]), (parities >> slot) & 1u, &failed))) break;
+        parities ^= 1u << slot;
         uint32_t kw[2][KW], vw[4][VW];
-        load_words(kp + g * D + t * (D / 4), kw[0]);
-        load_words(kp + (g + 8) * D + t * (D / 4), kw[1]);
-        load_words(vp + (2 * t) * D + g * (D / 8), vw[0]);
-        load_words(vp + (2 * t + 1) * D + g * (D / 8), vw[1]);
-        load_words(vp + (2 * t + 8) * D + g * (D / 8), vw[2]);
-        load_words(vp + (2 * t + 9) * D + g * (D / 8), vw[3]);
-        const float k_scale = c.k_scale[block * H + head], v_scale = c.v_scale[block * H + head];
+        {
+            // 16-byte chunk x of row r lies at x ^ (r & 7) (128-byte rows) or x ^ (r / 2 & 3)
+            const uint32_t k_at = my_ring + slot * kStage, v_at = k_at + kStage / 2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = g + 8 * i, swap = D == 128 ? r & 7 : (r >> 1) & 3;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) read_piece<4>(k_at + r * D + (((t * (D / 64) + x) ^ swap) << 4), &kw[i][x * 4]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 2 * t + (i & 1) + (i >> 1) * 8, swap = D == 128 ? r & 7 : (r >> 1) & 3;
+                if constexpr (D == 128) read_piece<4>(v_at + r * D + ((g ^ swap) << 4), vw[i]);
+                else read_piece<2>(v_at + r * D + (((g >> 1) ^ swap) << 4) + (g & 1) * 8, vw[i]);
+            }
+        }
 
         // scores
         float s[NT][4];
@@ -230,13 +304,22 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
                     raise |= s[n][i] > m[n][i & 1] + kRaise;
                 }
             if (a.scores != nullptr) {
+                // rows 2t, 2t + 1 of tokens g and g + 8
+                float *to = scores + int64_t(j0) * a.rows;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = j0 + g + (i >> 1) * 8, row = row0 + n * 8 + 2 * t + (i & 1);
-                        if (j < len && row < a.rows)
-                            a.scores[((seq * H + head) * a.max_len + j) * a.rows + row] = s[n][i];
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = row0 + n * 8 + 2 * t;
+                        if (j0 + g + h * 8 < len && row < a.rows) {
+                            float *at = to + (h * 8) * a.rows + n * 8;
+                            if ((a.rows & 1) == 0) {
+                                *reinterpret_cast<float2 *>(at) = make_float2(s[n][2 * h], s[n][2 * h + 1]);
+                            } else {
+                                at[0] = s[n][2 * h];
+                                if (row + 1 < a.rows) at[1] = s[n][2 * h + 1];
+                            }
+                        }
                     }
             }
             if (__any_sync(kFullWarp, raise)) {
@@ -249,7 +332,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 16));
                         top = fmaxf(top, m[n][i]);
-                        const float f = top == m[n][i] ? 1.0f : exp2f(m[n][i] - top);
+                        const float f = top == m[n][i] ? 1.0f : exp2_fast(m[n][i] - top);
                         m[n][i] = top;
                         l[n][i] *= f;
 #pragma unroll
@@ -268,7 +351,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = j0 + g + (i >> 1) * 8;
-                p[i] = j <= limit[n][i & 1] ? exp2f(s[n][i] - m[n][i & 1]) : 0.0f;
+                p[i] = j <= limit[n][i & 1] ? exp2_fast(s[n][i] - m[n][i & 1]) : 0.0f;
                 l[n][i & 1] += p[i];
             }
 #pragma unroll
@@ -322,7 +405,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
         }
     }
 
-    // the warps' parts meet in shared memory
+    // a warp that gave up still has copies in flight
+    if (failed != 0u && lane == 0)
+        for (int i = 0; i < kRing; ++i) mbar_wait(smem_addr(&full[warp][i]), (parities >> i) & 1u);
+    // the warps' parts meet in shared memory (the ring's: every copy has been waited for)
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -375,56 +462,92 @@ __global__ void __launch_bounds__(kAttnWarps * 32) cache_attention_kernel(const 
 }
 
 // Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)
-// takes the rows x, x + gridDim.x, ... of the output and the x-th stretch of the tokens.
-template <bool BF16>
-__global__ void __launch_bounds__(256)
-cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t ld_acc, int64_t stretch) {
+// takes the rows x, x + gridDim.x, ... of the output and the x-th stretch of kJoinTokens tokens.
+// ROWS: rows where they are 1, 2, 4 or 8 (a token's scores are one load), else 0.
+constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinTokens = kJoinThreads * kJoinEach;
+
+template <bool BF16, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads)
+cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t ld_acc) {
     extern __shared__ float row_lse[];  // log2 of the sum of 2^s, +inf where a row sees nothing
     const sp_cache &c = a.cache;
     const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y;
     const int64_t seq = blockIdx.z, pair = seq * H + head;
+    const int rows = ROWS != 0 ? ROWS : a.rows;
     pdl_launch_dependents();
     pdl_wait();
-    const float2 *ml = a.part_ml + pair * a.splits * a.rows;
-    const float *part = a.part_o + pair * a.splits * a.rows * D;
-    if (acc_out != nullptr) {
-        for (int row = threadIdx.x; row < a.rows; row += blockDim.x) {
-            float top = -INFINITY, sum = 0.0f;
-            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * a.rows + row].x);
-            for (int s = 0; s < a.splits; ++s) {
-                const float2 v = ml[s * a.rows + row];
-                sum = fmaf(v.x == top ? 1.0f : exp2f(v.x - top), v.y, sum);
+    const float2 *ml = a.part_ml + pair * a.splits * rows;
+    const float *part = a.part_o + pair * a.splits * rows * D;
+    const int j0 = blockIdx.x * kJoinTokens + threadIdx.x;
+    if (acc_out != nullptr && int64_t(blockIdx.x) * kJoinTokens < a.max_len) {
+        const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols * c.block_tokens)));
+        const int own = static_cast<int>(max(int64_t(-1), min(a.lens[seq] - a.n_q, a.max_len)));
+        // the scores and the old sums are on their way before the rows' sums are joined
+        float s[kJoinEach][ROWS != 0 ? ROWS : 1], sum[kJoinEach];
+        const float *scores = a.scores + (pair * a.max_len + j0) * rows;
+#pragma unroll
+        for (int i = 0; i < kJoinEach; ++i) {
+            const int j = j0 + i * kJoinThreads;
+            sum[i] = acc_in != nullptr && j < own ? acc_in[pair * ld_acc + j] : 0.0f;
+            if constexpr (ROWS != 0) {
+                const float *at = scores + int64_t(i) * kJoinThreads * ROWS;
+                if (j >= len) {
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) s[i][r] = -INFINITY;
+                } else if constexpr (ROWS == 1) {
+                    s[i][0] = __ldcs(at);
+                } else if constexpr (ROWS == 2) {
+                    const float2 v = __ldcs(reinterpret_cast<const float2 *>(at));
+                    s[i][0] = v.x; s[i][1] = v.y;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < ROWS; r += 4) {
+                        const float4 v = __ldcs(reinterpret_cast<const float4 *>(at + r));
+                        s[i][r] = v.x; s[i][r + 1] = v.y; s[i][r + 2] = v.z; s[i][r + 3] = v.w;
+                    }
+                }
             }
-            row_lse[row] = top == -INFINITY && sum == 0.0f ? INFINITY : top + log2f(sum);
+        }
+        for (int row = threadIdx.x; row < rows; row += kJoinThreads) {
+            float top = -INFINITY, total = 0.0f;
+            for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ml[k * rows + row].x);
+            for (int k = 0; k < a.splits; ++k) {
+                const float2 v = ml[k * rows + row];
+                total = fmaf(v.x == top ? 1.0f : exp2_fast(v.x - top), v.y, total);
+            }
+            row_lse[row] = top == -INFINITY && total == 0.0f ? INFINITY : top + log2f(total);
         }
         __syncthreads();
-        const int64_t len = max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols * c.block_tokens));
-        const int64_t own = a.lens[seq] - a.n_q;
-        const int64_t end = min((blockIdx.x + 1) * stretch, a.max_len);
-        for (int64_t j = blockIdx.x * stretch + threadIdx.x; j < end; j += blockDim.x) {
-            float sum = 0.0f;
-            if (j < len) {
-                const float *s = a.scores + (pair * a.max_len + j) * a.rows;
-                for (int row = 0; row < a.rows; ++row) {
-                    const float x = s[row], z = row_lse[row];
-                    sum += x == -INFINITY ? 0.0f : exp2f(x - z);
+#pragma unroll
+        for (int i = 0; i < kJoinEach; ++i) {
+            const int j = j0 + i * kJoinThreads;
+            if (j >= a.max_len) break;
+            float add = 0.0f;
+            if constexpr (ROWS != 0) {
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) add += s[i][r] == -INFINITY ? 0.0f : exp2_fast(s[i][r] - row_lse[r]);
+            } else if (j < len) {
+                const float *at = scores + int64_t(i) * kJoinThreads * rows;
+                for (int r = 0; r < rows; ++r) {
+                    const float x = __ldcs(at + r);
+                    add += x == -INFINITY ? 0.0f : exp2_fast(x - row_lse[r]);
                 }
-                if (acc_in != nullptr && j < own) sum += acc_in[pair * ld_acc + j];
             }
-            acc_out[pair * ld_acc + j] = sum;
+            acc_out[pair * ld_acc + j] = j < len ? sum[i] + add : 0.0f;
         }
     }
-    for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
         const int i = row / a.group, hq = head * a.group + row % a.group;
         float top = -INFINITY;
-        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * a.rows + row].x);
-        for (int d = threadIdx.x; d < D; d += blockDim.x) {
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * rows + row].x);
+        for (int d = threadIdx.x; d < D; d += kJoinThreads) {
             float sum = 0.0f, out = 0.0f;
+#pragma unroll 4
             for (int s = 0; s < a.splits; ++s) {
-                const float2 v = ml[s * a.rows + row];
-                const float f = v.x == top ? 1.0f : exp2f(v.x - top);
+                const float2 v = ml[s * rows + row];
+                const float f = v.x == top ? 1.0f : exp2_fast(v.x - top);
                 sum = fmaf(f, v.y, sum);
-                out = fmaf(f, part[(s * a.rows + row) * int64_t(D) + d], out);
+                out = fmaf(f, part[(s * rows + row) * int64_t(D) + d], out);
             }
             const float y = top == -INFINITY && sum == 0.0f ? 0.0f : out / sum;
             uint16_t bits;
@@ -451,7 +574,7 @@ int64_t cache_attention_workspace(const sp_cache &c, int64_t n_q, int n_heads, i
     const int splits = attention_splits(c, attention_row_tiles(rows), max_len, want_acc);
     if (pairs == 0 || rows == 0 || (splits == 1 && !want_acc)) return 0;
     int64_t bytes = pairs * splits * rows * (c.head_dim * 4 + 8);
-    if (want_acc) bytes += pairs * max_len * rows * 4;
+    if (want_acc) bytes += (pairs * max_len * rows + 3) / 4 * 16;
     return bytes;
 }
 
@@ -470,6 +593,7 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     a.group = n_heads / c.n_kv_heads;
     a.rows = static_cast<int>(n_q * a.group);
     a.row_tiles = attention_row_tiles(a.rows);
+    a.block_shift = c.block_tokens == 16 ? 4 : c.block_tokens == 32 ? 5 : 6;
     a.splits = attention_splits(c, a.row_tiles, max_len, acc_out != nullptr);
     a.lens = lens;
     a.scale_log2 = scale * kLog2e;
@@ -478,13 +602,32 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     const int64_t pairs = c.n_seqs * c.n_kv_heads;
     const bool join = a.splits > 1 || acc_out != nullptr;
     if (join) {
-        a.part_ml = static_cast<float2 *>(workspace);
-        a.part_o = reinterpret_cast<float *>(a.part_ml + pairs * a.splits * a.rows);
-        if (acc_out != nullptr) a.scores = a.part_o + pairs * a.splits * a.rows * c.head_dim;
+        // scores first: their loads want 16-byte boundaries
+        float *at = static_cast<float *>(workspace);
+        if (acc_out != nullptr) {
+            a.scores = at;
+            at += (pairs * max_len * a.rows + 3) / 4 * 4;
+        }
+        a.part_o = at;
+        a.part_ml = reinterpret_cast<float2 *>(at + pairs * a.splits * a.rows * c.head_dim);
     }
     PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
-    cudaError_t e;
-#define SP_LAUNCH(B, DD, N) e = cudaLaunchKernelEx(&pdl.cfg, cache_attention_kernel<B, DD, N>, a)
+    CUtensorMap k_map = {}, v_map = {};
+    cudaError_t e = cudaSuccess;
+    if (c.n_blocks > 0) {
+        const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
+        if (c.n_blocks > 0x7fffffff || pool_rows > 0x7fffffff) return SP_ERR_SHAPE;
+        e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
+        if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, 16);
+    }
+    if (e != cudaSuccess) return cuda_fail(e);
+    pdl.cfg.dynamicSmemBytes = kAttnWarps * kRing * c.head_dim * 32;
+#define SP_LAUNCH(B, DD, N)                                                                              \
+    do {                                                                                                 \
+        static DynamicSmem limit;                                                                        \
+        e = limit.allow(reinterpret_cast<const void *>(cache_attention_kernel<B, DD, N>));               \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, cache_attention_kernel<B, DD, N>, k_map, v_map, a); \
+    } while (0)
 #define SP_PICK(B)                                                                                     \
     if (c.head_dim == 64) { if (a.rows <= 8) SP_LAUNCH(B, 64, 1); else SP_LAUNCH(B, 64, 2); }          \
     else { if (a.rows <= 8) SP_LAUNCH(B, 128, 1); else SP_LAUNCH(B, 128, 2); }
@@ -494,12 +637,20 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     if (e != cudaSuccess) return cuda_fail(e);
     sp_status st = check_launch();
     if (st != SP_OK || !join) return st;
-    const int64_t stretch = 1024;
-    const int64_t blocks = std::max(acc_out != nullptr ? (max_len + stretch - 1) / stretch : 1, std::min(int64_t(a.rows), int64_t(8)));
-    PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(256), stream);
+    const int64_t blocks = std::max(acc_out != nullptr ? (max_len + kJoinTokens - 1) / kJoinTokens : 1, std::min(int64_t(a.rows), int64_t(8)));
+    PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(kJoinThreads), stream);
     second.cfg.dynamicSmemBytes = a.rows * sizeof(float);
-    if (dtype == SP_BF16) e = cudaLaunchKernelEx(&second.cfg, cache_join_kernel<true>, a, acc_in, acc_out, ld_acc, stretch);
-    else e = cudaLaunchKernelEx(&second.cfg, cache_join_kernel<false>, a, acc_in, acc_out, ld_acc, stretch);
+#define SP_LAUNCH(R)                                                                                                 \
+    e = dtype == SP_BF16 ? cudaLaunchKernelEx(&second.cfg, cache_join_kernel<true, R>, a, acc_in, acc_out, ld_acc)   \
+                         : cudaLaunchKernelEx(&second.cfg, cache_join_kernel<false, R>, a, acc_in, acc_out, ld_acc)
+    switch (a.rows) {
+        case 1: SP_LAUNCH(1); break;
+        case 2: SP_LAUNCH(2); break;
+        case 4: SP_LAUNCH(4); break;
+        case 8: SP_LAUNCH(8); break;
+        default: SP_LAUNCH(0); break;
+    }
+#undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }

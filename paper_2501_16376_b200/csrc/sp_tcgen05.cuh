@@ -18,19 +18,6 @@ __device__ __forceinline__ bool elect_one() {
 // The warp's index, known to the compiler to be the same in all lanes.
 __device__ __forceinline__ int uniform_warp() { return __shfl_sync(kFullWarp, static_cast<int>(threadIdx.x >> 5), 0); }
 
-// Place in a ring of stages: the slot, and the parity of the barrier phase that its current use completes.
-template <int SLOTS>
-struct RingPlace {
-    int slot = 0;
-    uint32_t parity = 0;
-    __device__ __forceinline__ void next() {
-        if (++slot == SLOTS) {
-            slot = 0;
-            parity ^= 1u;
-        }
-    }
-};
-
 // ---- tensor memory (512 columns of 128 lanes x 32 bits on an SM)
 
 // One warp allocates; the base address lands in shared memory.  columns: a power of two >= 32.

@@ -58,6 +58,19 @@ __device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity,
     return false;
 }
 
+// Place in a ring of stages: the slot, and the parity of the barrier phase that its current use completes.
+template <int SLOTS>
+struct RingPlace {
+    int slot = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == SLOTS) {
+            slot = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -83,7 +96,10 @@ __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.w
 // Elements are bytes.  api_serve.cu holds the driver entry point.
 cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t row_bytes,
                               int64_t pitch, int box_rows);
-// The same for 16-bit elements (an inner extent that is not a multiple of 16 bytes is clipped
+// The same for rows of 64 or 128 bytes that follow one another, as whole rows (swizzled over 64 or
+// 128 bytes: with 64, chunk c of row r lands at c ^ (r / 2 & 3)).
+cudaError_t encode_byte_rows(CUtensorMap *map, const void *base, int64_t rows, int row_bytes, int box_rows);
+// As encode_byte_tiles for 16-bit elements (an inner extent that is not a multiple of 16 bytes is clipped
 // exactly): boxes of 64 elements x box_rows.
 cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld,
                               int box_rows);
