@@ -16,9 +16,8 @@
 //     values and interleaves pairs of tokens bytewise before converting; P^T is S^T transposed
 //     8x8 by movmatrix.
 // The block scale of K goes onto the scores and that of V onto the 16-token partial product, in
-// binary32.  Every warp has a ring of its own in shared memory, filled by TMA two steps of 16 tokens
-// ahead (128 KB in flight on an SM, no registers, no barrier but the copy's own; the swizzle keeps
-// both access patterns free of bank conflicts).  P is rounded to binary16 for the product; for binary16 outputs the remainder follows
+// binary32.  The cache arrives by TMA, two stages of 64 tokens ahead (128 KB in flight on an SM; the
+// swizzle keeps both access patterns free of bank conflicts).  P is rounded to binary16 for the product; for binary16 outputs the remainder follows
 // as a second operand (2^-22 in all), since one rounding of P alone would be as large as that of
 // the output.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
 // the reductions of nearly all steps and leaves P at most 256.
@@ -32,8 +31,9 @@ namespace sp {
 namespace {
 
 constexpr int kAttnWarps = 4;
-constexpr int kRing = 3;           // steps of 16 tokens in a warp's ring
+constexpr int kRing = 3;           // stages of 16 tokens for every warp
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -1e30f;  // running maximum before any score
 constexpr float kRaise = 8.0f;  // how far (in powers of two) a score may exceed the running maximum
 
 struct AttnArgs {
@@ -57,6 +57,11 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -74,6 +79,9 @@ __device__ __forceinline__ float exp2_fast(float x) {  // what is below 2^-126 c
     return y;
 }
 
+__device__ __forceinline__ void copy_scale(uint32_t dst, const float *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void read_piece(uint32_t src, uint32_t *w) {
     if constexpr (N == 4)
@@ -97,11 +105,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
     constexpr int VW = D / 32;  // words of values a lane holds of one token
     constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
-    constexpr int kStage = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
-    extern __shared__ __align__(1024) uint8_t ring[];  // [warp][kRing][kStage]; afterwards the warps' sums
+    constexpr int kStep = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
+    extern __shared__ __align__(1024) uint8_t ring[];  // [kRing][warp][kStep]; afterwards the warps' sums
     float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
     __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
-    __shared__ uint64_t full[kAttnWarps][kRing];
+    __shared__ uint64_t full[kRing], empty[kRing];
+    __shared__ float2 scales[kRing][kAttnWarps];  // of K and V
+    __shared__ uint32_t present[kRing][kAttnWarps];  // whether the table names a block there
     __shared__ uint32_t failed;
     __shared__ int nan_from[D];  // first token among the call's own whose value is NaN, by column
     const sp_cache &c = a.cache;
@@ -116,7 +126,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             tma_prefetch_map(&k_map);
             tma_prefetch_map(&v_map);
         }
-        for (int i = 0; i < kAttnWarps * kRing; ++i) mbar_init(smem_addr(&full[0][0] + i), 1);
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(smem_addr(&full[i]), 2 * kAttnWarps);  // a step's copies: the two of TMA, and the scales
+            mbar_init(smem_addr(&empty[i]), kAttnWarps);
+        }
         failed = 0u;
         mbar_fence_init();
     }
@@ -124,42 +137,53 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     pdl_wait();
     const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
+    // the tokens before this one are seen by every query
+    const int all_see = static_cast<int>(max(int64_t(0), min(int64_t(len), a.lens[seq] - a.n_q + 1)));
     const int steps = (len + 15) / 16;
     const int first = static_cast<int>(int64_t(steps) * blockIdx.x / a.splits);
     const int last = static_cast<int>(int64_t(steps) * (blockIdx.x + 1) / a.splits);
 
-    // this warp's steps: first + warp, + kAttnWarps, ...; a step's block is looked up a round before
-    // its copy, its scales travel in registers
+    // A stage holds a step of 16 tokens for every warp.  The warps take turns in filling stages, two
+    // ahead: four lanes copy a step each, scales included (4-byte copies on the same barrier).  The
+    // blocks are looked up a turn before they are wanted.
     const int32_t *table = c.table + seq * c.ld_table;
-    const uint32_t my_ring = smem_addr(ring) + warp * (kRing * kStage);
-    auto block_of = [&](int step) {  // -1: none
-        if (step >= last) return -1;
-        const int id = table[step >> (shift - 4)];
-        return id >= 0 && id < c.n_blocks ? id : -1;
+    const uint32_t n_blocks = static_cast<uint32_t>(c.n_blocks), ring_at = smem_addr(ring);
+    const int stages = (last - first + kAttnWarps - 1) / kAttnWarps;
+    const uint64_t policy = l2_evict_first();  // leaves the L2 to the scores, which the joining kernel reads
+    auto block_of = [&](int stage) {
+        const int step = first + stage * kAttnWarps + lane;
+        return lane < kAttnWarps && step < last ? table[step >> (shift - 4)] : -1;
     };
-    int blocks[kRing];  // of the steps in the ring, then of the one to be copied next
-    float2 scales[kRing];
-    auto copy_step = [&](int step, int block, int slot) {
-        float2 s = make_float2(0.0f, 0.0f);
-        if (block >= 0) {
-            const int64_t tile = int64_t(block) * H + head;
-            if (lane == 0) {
-                const uint32_t bar = smem_addr(&full[warp][slot]), to = my_ring + slot * kStage;
-                const int row = static_cast<int>((tile << shift) + ((step << 4) & ((1 << shift) - 1)));
-                mbar_expect_tx(bar, kStage);
-                tma_load_2d(to, &k_map, 0, row, bar);
-                tma_load_2d(to + kStage / 2, &v_map, 0, row, bar);
+    auto fill = [&](int stage, int slot, int block) {
+        if (lane < kAttnWarps) {
+            const int step = first + stage * kAttnWarps + lane;
+            const uint32_t bar = smem_addr(&full[slot]);
+            const bool here = uint32_t(block) < n_blocks;
+            present[slot][lane] = here;
+            if (here) {
+                const int tile = block * H + head;
+                const uint32_t to = ring_at + (slot * kAttnWarps + lane) * kStep;
+                const int row = (tile << shift) + ((step << 4) & ((1 << shift) - 1));
+                mbar_expect_tx(bar, kStep);
+                tma_load_2d(to, &k_map, 0, row, bar, policy);
+                tma_load_2d(to + kStep / 2, &v_map, 0, row, bar, policy);
+                copy_scale(smem_addr(&scales[slot][lane].x), c.k_scale + tile);
+                copy_scale(smem_addr(&scales[slot][lane].y), c.v_scale + tile);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            } else {
+                mbar_arrive(bar);
+                mbar_arrive(bar);
             }
-            s = make_float2(c.k_scale[tile], c.v_scale[tile]);
         }
-        return s;
+        __syncwarp();
     };
-#pragma unroll
-    for (int i = 0; i < kRing; ++i) blocks[i] = block_of(first + warp + i * kAttnWarps);
-#pragma unroll
-    for (int i = 0; i < kRing - 1; ++i) scales[i] = copy_step(first + warp + i * kAttnWarps, blocks[i], i);
+    int next_block = block_of(warp);  // of the stage this warp fills next
+    static_assert(kRing - 1 <= kAttnWarps, "the first stages are filled by different warps");
+    if (warp < kRing - 1) {
+        if (warp < stages) fill(warp, warp, next_block);
+        next_block = block_of(warp + kAttnWarps);
+    }
     RingPlace<kRing> place;
-    uint32_t parities = 0;  // bit: parity of the slot's next completion (a slot without a block has none)
 
     // queries: operand registers, and the factor that undoes their scaling
     uint32_t qf[NT][KW][2];
@@ -219,7 +243,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         for (int i = 0; i < 2; ++i) {
             qscale[n][i] = __shfl_sync(kFullWarp, undo, (2 * t + i) * 4);
             limit[n][i] = row_limit(a, seq, row0 + n * 8 + 2 * t + i, len);
-            m[n][i] = -INFINITY;
+            m[n][i] = kLowest;
             l[n][i] = 0.0f;
         }
 #pragma unroll
@@ -231,21 +255,23 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
 
     // of token g, row 2t of this tile; 8-byte aligned where rows is even
     float *const scores = a.scores + ((seq * H + head) * a.max_len + g) * a.rows + row0 + 2 * t;
-    for (int step = first + warp; step < last; step += kAttnWarps) {
-        const int j0 = step * 16;
-        const int block = blocks[0], slot = place.slot;
-        const int free_slot = slot == 0 ? kRing - 1 : slot - 1;
-        __syncwarp();  // every lane has read what the last step left there
-        scales[kRing - 1] = copy_step(step + (kRing - 1) * kAttnWarps, blocks[kRing - 1], free_slot);
-        const float k_scale = scales[0].x, v_scale = scales[0].y;
-#pragma unroll
-        for (int i = 0; i < kRing - 1; ++i) {
-            blocks[i] = blocks[i + 1];
-            scales[i] = scales[i + 1];
+    int stage = 0;
+    for (; stage < stages; ++stage, place.next()) {
+        const int step = first + stage * kAttnWarps + warp, j0 = step * 16, slot = place.slot;
+        const int ahead = stage + kRing - 1;
+        bool ok = true;
+        if ((ahead & (kAttnWarps - 1)) == warp && ahead < stages) {
+            // the slot was last used by the stage before this one
+            const int free_slot = slot == 0 ? kRing - 1 : slot - 1;
+            if (ahead >= kRing) ok = mbar_wait_or_fail(smem_addr(&empty[free_slot]), slot == 0 ? place.parity ^ 1u : place.parity, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
+            fill(ahead, free_slot, next_block);
+            next_block = block_of(ahead + kAttnWarps);
         }
-        blocks[kRing - 1] = block_of(step + kRing * kAttnWarps);
-        place.next();
-        if (block < 0) {
+        ok = mbar_wait_or_fail(smem_addr(&full[slot]), place.parity, &failed);
+        if (!__all_sync(kFullWarp, ok)) break;
+        if (step >= last) break;  // only in the last stage
+        if (!present[slot][warp]) {
             if (a.scores != nullptr)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -255,14 +281,15 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                         if (j < len && row < a.rows)
                             a.scores[((seq * H + head) * a.max_len + j) * a.rows + row] = -INFINITY;
                     }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
             continue;
         }
-        if (!__all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&full[warp][slot]), (parities >> slot) & 1u, &failed))) break;
-        parities ^= 1u << slot;
+        const float k_scale = scales[slot][warp].x, v_scale = scales[slot][warp].y;
         uint32_t kw[2][KW], vw[4][VW];
         {
             // 16-byte chunk x of row r lies at x ^ (r & 7) (128-byte rows) or x ^ (r / 2 & 3)
-            const uint32_t k_at = my_ring + slot * kStage, v_at = k_at + kStage / 2;
+            const uint32_t k_at = ring_at + (slot * kAttnWarps + warp) * kStep, v_at = k_at + kStep / 2;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = g + 8 * i, swap = D == 128 ? r & 7 : (r >> 1) & 3;
@@ -276,33 +303,40 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 else read_piece<2>(v_at + r * D + (((g >> 1) ^ swap) << 4) + (g & 1) * 8, vw[i]);
             }
         }
+        __syncwarp();  // the step is in registers
+        if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
 
         // scores
         float s[NT][4];
         {
             float s2[NT][2][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s2[n][0][i] = s2[n][1][i] = 0.0f;
-#pragma unroll
             for (int k = 0; k < KW; ++k) {
                 uint32_t f[4];
                 e4m3_to_f16(kw[0][k], f[0], f[2]);
                 e4m3_to_f16(kw[1][k], f[1], f[3]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma_f16(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
+                for (int n = 0; n < NT; ++n) {
+                    if (k < 2) mma_f16_first(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
+                    else mma_f16(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][i] = (s2[n][0][i] + s2[n][1][i]) * (k_scale * qscale[n][i & 1]);
+            if (j0 + 16 > all_see) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (j0 + g + (i >> 1) * 8 > limit[n][i & 1]) s[n][i] = -INFINITY;
             }
             bool raise = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + g + (i >> 1) * 8;
-                    const float x = (s2[n][0][i] + s2[n][1][i]) * (k_scale * qscale[n][i & 1]);
-                    s[n][i] = j <= limit[n][i & 1] ? x : -INFINITY;
-                    raise |= s[n][i] > m[n][i & 1] + kRaise;
-                }
+                for (int i = 0; i < 2; ++i) raise |= fmaxf(s[n][i], s[n][i + 2]) > m[n][i] + kRaise;
             if (a.scores != nullptr) {
                 // rows 2t, 2t + 1 of tokens g and g + 8
                 float *to = scores + int64_t(j0) * a.rows;
@@ -332,7 +366,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 16));
                         top = fmaxf(top, m[n][i]);
-                        const float f = top == m[n][i] ? 1.0f : exp2_fast(m[n][i] - top);
+                        const float f = exp2_fast(m[n][i] - top);
                         m[n][i] = top;
                         l[n][i] *= f;
 #pragma unroll
@@ -350,8 +384,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             float p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int j = j0 + g + (i >> 1) * 8;
-                p[i] = j <= limit[n][i & 1] ? exp2_fast(s[n][i] - m[n][i & 1]) : 0.0f;
+                p[i] = exp2_fast(s[n][i] - m[n][i & 1]);
                 l[n][i & 1] += p[i];
             }
 #pragma unroll
@@ -395,8 +428,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 e4m3_to_f16(prmt(vw[2][w], vw[3][w], sel), f[2], f[3]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    mma_f16(x, f, ph[n][0], ph[n][1]);
+                    float x[4];
+                    mma_f16_first(x, f, ph[n][0], ph[n][1]);
                     if constexpr (!BF16) mma_f16(x, f, pl[n][0], pl[n][1]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[n][2 * w + half][i] = fmaf(v_scale, x[i], o[n][2 * w + half][i]);
@@ -405,9 +438,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         }
     }
 
-    // a warp that gave up still has copies in flight
-    if (failed != 0u && lane == 0)
-        for (int i = 0; i < kRing; ++i) mbar_wait(smem_addr(&full[warp][i]), (parities >> i) & 1u);
+    // a block that gave up still has copies in flight
+    if (failed != 0u && threadIdx.x == 0)
+        for (int i = 0; i < 2 * kRing; ++i) mbar_wait(smem_addr(&full[i % kRing]), i / kRing);
     // the warps' parts meet in shared memory (the ring's: every copy has been waited for)
     __syncthreads();
 #pragma unroll
@@ -439,7 +472,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         float sum = 0.0f, out = 0.0f;
 #pragma unroll
         for (int w = 0; w < kAttnWarps; ++w) {
-            const float f = sh_m[w][r] == top ? 1.0f : exp2f(sh_m[w][r] - top);
+            const float f = exp2_fast(sh_m[w][r] - top);
             sum = fmaf(f, sh_l[w][r], sum);
             out = fmaf(f, sh_o[w][r][d], out);
         }
@@ -450,7 +483,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             if (d == 0) a.part_ml[p] = make_float2(top, sum);
         } else {
             const int i = row / a.group, hq = head * a.group + row % a.group;
-            const float y = top == -INFINITY && sum == 0.0f ? 0.0f : out / sum;
+            const float y = sum == 0.0f ? 0.0f : out / sum;
             uint16_t bits;
             if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
             else bits = __half_as_ushort(__float2half_rn(y));
@@ -508,14 +541,23 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
                 }
             }
         }
-        for (int row = threadIdx.x; row < rows; row += kJoinThreads) {
+        // a warp joins a row, a lane reads a split
+        const int lane = threadIdx.x & 31;
+        for (int row = threadIdx.x >> 5; row < rows; row += kJoinThreads / 32) {
             float top = -INFINITY, total = 0.0f;
-            for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ml[k * rows + row].x);
-            for (int k = 0; k < a.splits; ++k) {
-                const float2 v = ml[k * rows + row];
-                total = fmaf(v.x == top ? 1.0f : exp2_fast(v.x - top), v.y, total);
+            for (int k0 = 0; k0 < a.splits; k0 += 32) {
+                const float2 v = k0 + lane < a.splits ? ml[(k0 + lane) * rows + row] : make_float2(-INFINITY, 0.0f);
+                float most = v.x;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(kFullWarp, most, o));
+                most = fmaxf(most, top);
+                float part_sum = v.y * exp2_fast(v.x - most);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) part_sum += __shfl_xor_sync(kFullWarp, part_sum, o);
+                total = fmaf(total, exp2_fast(top - most), part_sum);
+                top = most;
             }
-            row_lse[row] = top == -INFINITY && total == 0.0f ? INFINITY : top + log2f(total);
+            if (lane == 0) row_lse[row] = total == 0.0f ? INFINITY : top + log2f(total);
         }
         __syncthreads();
 #pragma unroll
@@ -525,12 +567,12 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
             float add = 0.0f;
             if constexpr (ROWS != 0) {
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) add += s[i][r] == -INFINITY ? 0.0f : exp2_fast(s[i][r] - row_lse[r]);
+                for (int r = 0; r < ROWS; ++r) add += exp2_fast(s[i][r] - row_lse[r]);
             } else if (j < len) {
                 const float *at = scores + int64_t(i) * kJoinThreads * rows;
                 for (int r = 0; r < rows; ++r) {
                     const float x = __ldcs(at + r);
-                    add += x == -INFINITY ? 0.0f : exp2_fast(x - row_lse[r]);
+                    add += exp2_fast(x - row_lse[r]);
                 }
             }
             acc_out[pair * ld_acc + j] = j < len ? sum[i] + add : 0.0f;
@@ -545,11 +587,11 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
 #pragma unroll 4
             for (int s = 0; s < a.splits; ++s) {
                 const float2 v = ml[s * rows + row];
-                const float f = v.x == top ? 1.0f : exp2_fast(v.x - top);
+                const float f = exp2_fast(v.x - top);
                 sum = fmaf(f, v.y, sum);
                 out = fmaf(f, part[(s * rows + row) * int64_t(D) + d], out);
             }
-            const float y = top == -INFINITY && sum == 0.0f ? 0.0f : out / sum;
+            const float y = sum == 0.0f ? 0.0f : out / sum;
             uint16_t bits;
             if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
             else bits = __half_as_ushort(__float2half_rn(y));
