@@ -9,9 +9,11 @@
 // lose bits that are as far below the row's largest products.
 //
 // Bound by the tensor cores.  The weights are the 128 rows of a tile because that side is the one
-// that has to be converted: every weight once for up to 256 tokens, 16 weights a cycle, which
-// eight warps do beside the products.  One thread streams the activations by TMA, one the codes,
-// one issues the products, four warps empty the accumulators (two, alternating: 2 x 256 columns).
+// that has to be converted: every weight once for up to 256 tokens, 16 weights a cycle.  Converting
+// a stage of 64 columns is a chain of waits, loads and stores about four times as long as its
+// products, so three groups of four warps do every third stage each, a thread a row.  One thread
+// streams the activations by TMA, one the codes, one issues the products, four warps empty the
+// accumulators (two, alternating: 2 x 256 columns).
 #include <algorithm>
 
 #include "mx4_common.cuh"
@@ -28,7 +30,7 @@ constexpr int kMostTokens = 256;
 constexpr int kSlotBytes = kWeightBytes + kMostTokens * 128;
 constexpr int kCodeSlotBytes = kMx4TileRows * 128 + 2 * kMx4TileBytes;
 constexpr int kTmemColumns = 512;
-constexpr int kThreads = 512;  // 4 warps of single threads' roles, 4 that empty, 8 that convert
+constexpr int kThreads = 256 + kSlots * 128;  // 4 warps of single roles, 4 that empty, a group of 4 for every slot
 
 struct Gemm16Args {
     const uint8_t *scales;
@@ -77,19 +79,22 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots], acc_full[2], acc_free, drained;
     __shared__ uint32_t tmem_base, failed;
-    __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
+    // largest scale byte of a row, for eight tiles in turn: a group writes a tile's not before the
+    // products of six stages earlier are done, and with them (a stage a tile at worst) the tile of
+    // eight earlier has been emptied
+    __shared__ int row_top[8][kMx4TileRows];
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
         tma_prefetch_map(&w_map);
         for (int s = 0; s < kSlots; ++s) {
-            mbar_init(smem_addr(&full[s]), 9);  // the activations' copy and eight converting warps
+            mbar_init(smem_addr(&full[s]), 5);  // the activations' copy and four converting warps
             mbar_init(smem_addr(&empty[s]), 1);
         }
         for (int s = 0; s < kCodeSlots; ++s) {
             mbar_init(smem_addr(&code_full[s]), 1);
-            mbar_init(smem_addr(&code_empty[s]), 8);
+            mbar_init(smem_addr(&code_empty[s]), 16);  // four warps for each of four stages of 64 columns
         }
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
@@ -180,52 +185,58 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
             if (lane == 0) mbar_wait(smem_addr(&drained), 0);
         }
     } else if (warp >= 8) {
-        // a thread converts one block of 32 columns of a stage: row and half
-        const int row = (threadIdx.x - 256) >> 1, half = threadIdx.x & 1, swap = row & 7;
+        // group `slot` converts every kSlots-th stage, into its own slot; a thread has a row of it
+        const int slot = (warp - 8) >> 2, row = threadIdx.x & 127, swap = row & 7;
         const uint32_t scale_at = (row & 31) * 16 + (row >> 5) * 4;
-        int step = 0, code_step = 0, count = 0;
+        uint8_t *const out = slots + slot * kSlotBytes + row * 128;
+        int step = 0, code0 = 0, count = 0;  // stages before this tile's first; uses of the group's slot
+        uint32_t uses = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count, step += a.steps, code0 += code_steps) {
             int top = 0;
             if constexpr (!BF16) {
                 const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + scale_at;
                 uint32_t most = 0;
-#pragma unroll 4
-                for (int c = half; c < a.tile_cols; c += 2) {
-                    uint32_t w = *reinterpret_cast<const uint32_t *>(s + int64_t(c) * kMx4TileBytes);
+#pragma unroll 16
+                for (int c = 0; c < a.tile_cols; ++c) {
+                    uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(s + int64_t(c) * kMx4TileBytes));
                     w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
                     most = __vmaxu4(most, w);
                 }
                 most = __vmaxu4(most, most >> 16);
-                most = max(most & 0xffu, (most >> 8) & 0xffu);
-                top = static_cast<int>(max(most, __shfl_xor_sync(kFullWarp, most, 1)));
-                if (half == 0) row_top[count & 3][row] = top;
+                top = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
+                if (step % kSlots == slot) row_top[count & 7][row] = top;  // the group that converts the tile's first stage
             }
-            for (int k = 0; ok && k < a.steps; ++k, ++step) {
-                const int slot = step % kSlots, code_slot = code_step % kCodeSlots, sub = k & 3;
-                if (sub == 0) ok = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed));
-                if (ok && step >= kSlots)
-                    ok = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&empty[slot]), (step / kSlots - 1) & 1, &failed));
-                if (!ok) break;
+            // the first stage of this tile that is the group's
+            for (int k = (slot + kSlots - step % kSlots) % kSlots; k < a.steps; k += kSlots, ++uses) {
+                const int sub = k & 3, code_step = code0 + (k >> 2), code_slot = code_step % kCodeSlots;
+                ok = mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed);
+                if (uses > 0) ok = ok && mbar_wait_or_fail(smem_addr(&empty[slot]), (uses - 1) & 1u, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 const uint8_t *in = codes + code_slot * kCodeSlotBytes;
-                const uint32_t byte = in[kMx4TileRows * 128 + (sub >> 1) * kMx4TileBytes + scale_at + (sub & 1) * 2 + half];
-                uint32_t factor;
-                if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
-                else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
-                factor |= factor << 16;
-                const uint4 w = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
-                uint8_t *out = slots + slot * kSlotBytes + row * 128;
-                const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+                const uint32_t bytes = *reinterpret_cast<const uint16_t *>(in + kMx4TileRows * 128 + (sub >> 1) * kMx4TileBytes +
+                                                                           scale_at + (sub & 1) * 2);
+                uint4 w[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<uint4 *>(out + (((half * 4 + i) ^ swap) << 4)) = convert8<BF16>(words[i], factor);
+                for (int half = 0; half < 2; ++half)
+                    w[half] = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
+                __syncwarp();  // the codes are in registers
+                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 4 - sub : 1);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t byte = half == 0 ? bytes & 0xffu : bytes >> 8;
+                    uint32_t factor;
+                    if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
+                    else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
+                    factor |= factor << 16;
+                    const uint32_t words[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint4 *>(out + (((half * 4 + i) ^ swap) << 4)) = convert8<BF16>(words[i], factor);
+                }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_addr(&full[slot]));
-                    if (sub == 3 || k == a.steps - 1) mbar_arrive(smem_addr(&code_empty[code_slot]));
-                }
-                if (sub == 3 || k == a.steps - 1) ++code_step;
+                if (lane == 0) mbar_arrive(smem_addr(&full[slot]));
             }
         }
     } else if (warp >= 4) {
@@ -242,7 +253,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
             const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
             float f0 = 1.0f, f1 = 1.0f;
             if constexpr (!BF16) {
-                const int e = row_top[count & 3][quarter * 32 + lane] - 140;
+                const int e = row_top[count & 7][quarter * 32 + lane] - 140;
                 f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
                 f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
             }
