@@ -2,18 +2,21 @@
 // tokens than the streaming kernel takes in a pass).
 //
 // Mathematics: Y^T [rows, tokens] = V X^T, V = code * 2^(byte - 127) brought to the activations'
-// type in shared memory on the way to the tensor cores.  In bf16 that is exact (4-bit codes and
-// powers of two fit at every scale).  binary16 has not the range, so a row of V is kept relative
-// to its largest scale R: V = code * 2^(byte - R + 13), 49152 at most, and the sums are multiplied
-// by 2^(R - 140) when they leave; blocks whose scale lies more than 2^36 below the row's largest
-// lose bits that are as far below the row's largest products.
+// type on the way to the tensor cores.  In bf16 that is exact (4-bit codes and powers of two fit at
+// every scale).  binary16 has not the range, so a row of V is kept relative to its largest scale R:
+// V = code * 2^(byte - R + 13), 49152 at most, and the sums are multiplied by 2^(R - 140) when they
+// leave; blocks whose scale lies more than 2^36 below the row's largest lose bits that are as far
+// below the row's largest products.
 //
-// Bound by the tensor cores.  The weights are the 128 rows of a tile because that side is the one
-// that has to be converted: every weight once for up to 256 tokens, 16 weights a cycle.  Converting
-// a stage of 64 columns is a chain of waits, loads and stores about four times as long as its
-// products, so three groups of four warps do every third stage each, a thread a row.  One thread
-// streams the activations by TMA, one the codes, one issues the products, four warps empty the
-// accumulators (two, alternating: 2 x 256 columns).
+// Bound by the tensor cores.  The weights are the 128 rows of a tile because that side has to be
+// converted, every weight once for up to 192 tokens, and because that operand may lie in tensor
+// memory: a thread converts 64 columns of its row in registers and stores them there.  (Through
+// shared memory the converted weights were written once and read once at 16 KB a stage, and with
+// the activations that kept shared memory, not the tensor cores, busy: 586 cycles for a stage of
+// 112 tokens against 224 of products.)  Converting a stage of 64 columns is a long chain of waits,
+// loads and stores, so four groups of four warps do every fourth stage each.  One thread streams the
+// activations by TMA, one the codes, one issues the products, four warps empty the accumulators
+// (two, alternating) and find the next tile's R.
 #include <algorithm>
 
 #include "mx4_common.cuh"
@@ -23,14 +26,14 @@ namespace sp {
 
 namespace {
 
-constexpr int kSlots = 3;                        // stages of 64 columns: converted weights and activations
-constexpr int kCodeSlots = 3;                    // stages of 256 columns: codes and scales as stored
-constexpr int kWeightBytes = kMx4TileRows * 128; // 128 rows x 64 columns of 16 bits
-constexpr int kMostTokens = 256;
-constexpr int kSlotBytes = kWeightBytes + kMostTokens * 128;
+constexpr int kSlots = 4;                        // stages of 64 columns
+constexpr int kCodeSlots = 4;                    // stages of 256 columns: codes and scales as stored
+constexpr int kMostTokens = 192;
+constexpr int kSlotBytes = kMostTokens * 128;
 constexpr int kCodeSlotBytes = kMx4TileRows * 128 + 2 * kMx4TileBytes;
-constexpr int kTmemColumns = 512;
-constexpr int kThreads = 256 + kSlots * 128;  // 4 warps of single roles, 4 that empty, a group of 4 for every slot
+constexpr int kTmemColumns = 512;                // two accumulators of 192, four stages of 32 of weights
+constexpr int kWeightColumns = 2 * kMostTokens;
+constexpr int kThreads = 256 + kSlots * 128;     // 4 warps of single roles, 4 that empty, a group of 4 for every slot
 
 struct Gemm16Args {
     const uint8_t *scales;
@@ -49,8 +52,7 @@ __device__ __forceinline__ uint32_t half_pow2(int e) {
 
 // Eight codes -> eight values in the activations' type; `factor` holds the scale in both halves.
 template <bool BF16>
-__device__ __forceinline__ uint4 convert8(uint32_t w, uint32_t factor) {
-    uint32_t h[4];
+__device__ __forceinline__ void convert8(uint32_t w, uint32_t factor, uint32_t (&h)[4]) {
     if constexpr (BF16) {
         // bytes of the bf16 magnitudes by table, signs from bit 3 of the codes
         const uint32_t sel = w & 0x77777777u, up = w << 4;
@@ -68,7 +70,6 @@ __device__ __forceinline__ uint4 convert8(uint32_t w, uint32_t factor) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("mul.f16x2 %0, %0, %1;" : "+r"(h[i]) : "r"(factor));
     }
-    return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
 }  // namespace
@@ -77,12 +78,10 @@ template <bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Gemm16Args a) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots], acc_full[2], acc_free, drained;
+    __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots];
+    __shared__ uint64_t acc_full[2], acc_free, top_full[2], drained;
     __shared__ uint32_t tmem_base, failed;
-    // largest scale byte of a row, for eight tiles in turn: a group writes a tile's not before the
-    // products of six stages earlier are done, and with them (a stage a tile at worst) the tile of
-    // eight earlier has been emptied
-    __shared__ int row_top[8][kMx4TileRows];
+    __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -99,6 +98,8 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
         mbar_init(smem_addr(&acc_free), 128);
+        mbar_init(smem_addr(&top_full[0]), 128);
+        mbar_init(smem_addr(&top_full[1]), 128);
         mbar_init(smem_addr(&drained), 1);
         failed = 0u;
         mbar_fence_init();
@@ -124,7 +125,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 if (elect_one()) {
                     const uint32_t bar = smem_addr(&full[at.slot]);
                     mbar_expect_tx(bar, a.tile_tokens * 128);
-                    tma_load_2d(smem_addr(slots + at.slot * kSlotBytes + kWeightBytes), &x_map, k * 128, n * a.tile_tokens, bar);
+                    tma_load_2d(smem_addr(slots + at.slot * kSlotBytes), &x_map, k * 128, n * a.tile_tokens, bar);
                 }
                 __syncwarp();
             }
@@ -164,15 +165,16 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
             if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
-            const uint32_t acc = tmem + (count & 1) * 256;
+            const uint32_t acc = tmem + (count & 1) * kMostTokens;
             for (int k = 0; k < a.steps; ++k, at.next()) {
                 ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 tcgen05_fence_after();
                 if (elect_one()) {
-                    const uint64_t da = desc0 + static_cast<uint32_t>(at.slot * (kSlotBytes / 16)), db = da + kWeightBytes / 16;
+                    const uint64_t db = desc0 + static_cast<uint32_t>(at.slot * (kSlotBytes / 16));
+                    const uint32_t ta = tmem + kWeightColumns + at.slot * 32;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) mma_16bit(acc, da + p * 2, db + p * 2, instruction, k > 0 || p > 0);
+                    for (int p = 0; p < 4; ++p) mma_16bit(acc, ta + p * 8, db + p * 2, instruction, k > 0 || p > 0);
                     tcgen05_commit(smem_addr(&empty[at.slot]));
                     if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
                 }
@@ -188,53 +190,49 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         // group `slot` converts every kSlots-th stage, into its own slot; a thread has a row of it
         const int slot = (warp - 8) >> 2, row = threadIdx.x & 127, swap = row & 7;
         const uint32_t scale_at = (row & 31) * 16 + (row >> 5) * 4;
-        uint8_t *const out = slots + slot * kSlotBytes + row * 128;
-        int step = 0, code0 = 0, count = 0;  // stages before this tile's first; uses of the group's slot
-        uint32_t uses = 0;
+        const uint32_t to = tmem + kWeightColumns + slot * 32 + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        int step = 0, code0 = 0, count = 0;  // stages before this tile's first
+        uint32_t uses = 0;                   // of the group's slot
         bool ok = true;
         for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count, step += a.steps, code0 += code_steps) {
-            int top = 0;
-            if constexpr (!BF16) {
-                const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + scale_at;
-                uint32_t most = 0;
-#pragma unroll 16
-                for (int c = 0; c < a.tile_cols; ++c) {
-                    uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(s + int64_t(c) * kMx4TileBytes));
-                    w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
-                    most = __vmaxu4(most, w);
-                }
-                most = __vmaxu4(most, most >> 16);
-                top = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
-                if (step % kSlots == slot) row_top[count & 7][row] = top;  // the group that converts the tile's first stage
-            }
             // the first stage of this tile that is the group's
-            for (int k = (slot + kSlots - step % kSlots) % kSlots; k < a.steps; k += kSlots, ++uses) {
+            int k = (slot + kSlots - step % kSlots) % kSlots, top = 0;
+            if constexpr (!BF16) {
+                if (k < a.steps) {
+                    ok = mbar_wait_or_fail(smem_addr(&top_full[count & 1]), (count >> 1) & 1, &failed);
+                    if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                    top = row_top[count & 3][row];
+                }
+            }
+            for (; k < a.steps; k += kSlots, ++uses) {
                 const int sub = k & 3, code_step = code0 + (k >> 2), code_slot = code_step % kCodeSlots;
                 ok = mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed);
-                if (uses > 0) ok = ok && mbar_wait_or_fail(smem_addr(&empty[slot]), (uses - 1) & 1u, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 const uint8_t *in = codes + code_slot * kCodeSlotBytes;
                 const uint32_t bytes = *reinterpret_cast<const uint16_t *>(in + kMx4TileRows * 128 + (sub >> 1) * kMx4TileBytes +
                                                                            scale_at + (sub & 1) * 2);
-                uint4 w[2];
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    w[half] = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
-                __syncwarp();  // the codes are in registers
-                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 4 - sub : 1);
+                uint32_t v[32];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
                     const uint32_t byte = half == 0 ? bytes & 0xffu : bytes >> 8;
                     uint32_t factor;
                     if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
                     else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
                     factor |= factor << 16;
-                    const uint32_t words[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint4 *>(out + (((half * 4 + i) ^ swap) << 4)) = convert8<BF16>(words[i], factor);
+                        convert8<BF16>(words[i], factor, *reinterpret_cast<uint32_t(*)[4]>(&v[half * 16 + i * 4]));
                 }
-                fence_async_smem();
+                __syncwarp();  // the codes are in registers
+                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 4 - sub : 1);
+                if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&empty[slot]), (uses - 1) & 1u, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                tcgen05_fence_after();
+                tmem_store32(to, v);
+                tmem_store_wait();
+                tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&full[slot]));
             }
@@ -242,18 +240,34 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     } else if (warp >= 4) {
         const int quarter = warp & 3;
         int count = 0;
+        // the largest scale byte of this thread's row in a tile
+        auto find_top = [&](int tile, int c) {
+            const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + lane * 16 + quarter * 4;
+            uint32_t most = 0;
+#pragma unroll 16
+            for (int i = 0; i < a.tile_cols; ++i) {
+                uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(s + int64_t(i) * kMx4TileBytes));
+                w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
+                most = __vmaxu4(most, w);
+            }
+            most = __vmaxu4(most, most >> 16);
+            row_top[c & 3][quarter * 32 + lane] = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
+            mbar_arrive(smem_addr(&top_full[c & 1]));
+        };
+        if (!BF16 && blockIdx.x < a.tiles) find_top(blockIdx.x, 0);
         for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++count) {
             const int m = tile % a.row_tiles, n = tile / a.row_tiles;
+            if (!BF16 && tile + int(gridDim.x) < a.tiles) find_top(tile + gridDim.x, count + 1);
             const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
             tcgen05_fence_before();
             mbar_arrive(smem_addr(&acc_free));  // the other accumulator was emptied before
-            const uint32_t acc = tmem + (count & 1) * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
+            const uint32_t acc = tmem + (count & 1) * kMostTokens + (static_cast<uint32_t>(quarter * 32) << 16);
             const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
             float f0 = 1.0f, f1 = 1.0f;
             if constexpr (!BF16) {
-                const int e = row_top[count & 7][quarter * 32 + lane] - 140;
+                const int e = row_top[count & 3][quarter * 32 + lane] - 140;
                 f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
                 f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
             }
@@ -304,7 +318,7 @@ static int tile_tokens(int64_t n_tokens, int64_t row_tiles, int sms) {
     for (int64_t parts = first; parts <= first + 8; ++parts) {
         const int64_t n = ((n_tokens + parts - 1) / parts + 15) / 16 * 16;
         const int64_t tiles = row_tiles * ((n_tokens + n - 1) / n);
-        const int64_t cost = (tiles + sms - 1) / sms * std::max(n, int64_t(112));
+        const int64_t cost = (tiles + sms - 1) / sms * std::max(n, int64_t(64));
         if (cost < least) {
             least = cost;
             best = static_cast<int>(n);
