@@ -9,12 +9,13 @@
 // below the row's largest products.
 //
 // Bound by the tensor cores.  The weights are the 128 rows of a tile because that side has to be
-// converted, every weight once for up to 192 tokens, and because that operand may lie in tensor
-// memory: a thread converts 64 columns of its row in registers and stores them there.  (Through
-// shared memory the converted weights were written once and read once at 16 KB a stage, and with
-// the activations that kept shared memory, not the tensor cores, busy: 586 cycles for a stage of
-// 112 tokens against 224 of products.)  Converting a stage of 64 columns is a long chain of waits,
-// loads and stores, so four groups of four warps do every fourth stage each.  One thread streams the
+// converted, every weight once for up to 160 tokens, and because that operand may lie in tensor
+// memory: a thread converts 128 columns of its row in registers and stores them there.  (Through
+// shared memory the converted weights were written once and read once at 16 KB for 64 columns, and
+// with the activations that kept shared memory, not the tensor cores, busy.)  A stage costs the
+// issuing warp some 500 cycles of waiting and signalling whatever it holds, so it holds 128 columns;
+// converting it is a longer chain still, so three groups of four warps do every third stage each,
+// a thread a row.  One thread streams the
 // activations by TMA, one the codes, one issues the products, four warps empty the accumulators
 // (two, alternating) and find the next tile's R.
 #include <algorithm>
@@ -26,12 +27,13 @@ namespace sp {
 
 namespace {
 
-constexpr int kSlots = 4;                        // stages of 64 columns
+constexpr int kSlots = 3;                        // stages of 128 columns
 constexpr int kCodeSlots = 4;                    // stages of 256 columns: codes and scales as stored
-constexpr int kMostTokens = 192;
-constexpr int kSlotBytes = kMostTokens * 128;
+constexpr int kMostTokens = 160;
+constexpr int kHalfBytes = kMostTokens * 128;    // 64 columns of activations
+constexpr int kSlotBytes = 2 * kHalfBytes;
 constexpr int kCodeSlotBytes = kMx4TileRows * 128 + 2 * kMx4TileBytes;
-constexpr int kTmemColumns = 512;                // two accumulators of 192, four stages of 32 of weights
+constexpr int kTmemColumns = 512;                // two accumulators of 160, three stages of 64 of weights
 constexpr int kWeightColumns = 2 * kMostTokens;
 constexpr int kThreads = 256 + kSlots * 128;     // 4 warps of single roles, 4 that empty, a group of 4 for every slot
 
@@ -40,7 +42,7 @@ struct Gemm16Args {
     uint16_t *Y;
     int64_t n_tokens, n_rows, ldy;
     int tile_cols;    // scale tiles along the columns
-    int steps;        // 64-column stages
+    int steps;        // 128-column stages
     int tile_tokens;  // tokens of a tile, a multiple of 16
     int row_tiles, tiles;
 };
@@ -93,7 +95,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         }
         for (int s = 0; s < kCodeSlots; ++s) {
             mbar_init(smem_addr(&code_full[s]), 1);
-            mbar_init(smem_addr(&code_empty[s]), 16);  // four warps for each of four stages of 64 columns
+            mbar_init(smem_addr(&code_empty[s]), 8);  // four warps for each of two stages of 128 columns
         }
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
@@ -111,7 +113,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     const uint32_t tmem = tmem_base;
     pdl_launch_dependents();
     pdl_wait();
-    const int code_steps = (a.steps + 3) / 4;
+    const int code_steps = (a.steps + 1) / 2;
 
     if (warp == 0) {
         RingPlace<kSlots> at;
@@ -124,8 +126,10 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 if (elect_one()) {
                     const uint32_t bar = smem_addr(&full[at.slot]);
-                    mbar_expect_tx(bar, a.tile_tokens * 128);
-                    tma_load_2d(smem_addr(slots + at.slot * kSlotBytes), &x_map, k * 128, n * a.tile_tokens, bar);
+                    const uint32_t to = smem_addr(slots + at.slot * kSlotBytes);
+                    mbar_expect_tx(bar, a.tile_tokens * 256);
+                    tma_load_2d(to, &x_map, k * 256, n * a.tile_tokens, bar);
+                    tma_load_2d(to + kHalfBytes, &x_map, k * 256 + 128, n * a.tile_tokens, bar);
                 }
                 __syncwarp();
             }
@@ -172,9 +176,10 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 tcgen05_fence_after();
                 if (elect_one()) {
                     const uint64_t db = desc0 + static_cast<uint32_t>(at.slot * (kSlotBytes / 16));
-                    const uint32_t ta = tmem + kWeightColumns + at.slot * 32;
+                    const uint32_t ta = tmem + kWeightColumns + at.slot * 64;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) mma_16bit(acc, ta + p * 8, db + p * 2, instruction, k > 0 || p > 0);
+                    for (int p = 0; p < 8; ++p)
+                        mma_16bit(acc, ta + p * 8, db + (p >> 2) * (kHalfBytes / 16) + (p & 3) * 2, instruction, k > 0 || p > 0);
                     tcgen05_commit(smem_addr(&empty[at.slot]));
                     if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
                 }
@@ -190,7 +195,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         // group `slot` converts every kSlots-th stage, into its own slot; a thread has a row of it
         const int slot = (warp - 8) >> 2, row = threadIdx.x & 127, swap = row & 7;
         const uint32_t scale_at = (row & 31) * 16 + (row >> 5) * 4;
-        const uint32_t to = tmem + kWeightColumns + slot * 32 + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const uint32_t to = tmem + kWeightColumns + slot * 64 + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         int step = 0, code0 = 0, count = 0;  // stages before this tile's first
         uint32_t uses = 0;                   // of the group's slot
         bool ok = true;
@@ -205,32 +210,40 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 }
             }
             for (; k < a.steps; k += kSlots, ++uses) {
-                const int sub = k & 3, code_step = code0 + (k >> 2), code_slot = code_step % kCodeSlots;
+                const int sub = k & 1, code_step = code0 + (k >> 1), code_slot = code_step % kCodeSlots;
                 ok = mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 const uint8_t *in = codes + code_slot * kCodeSlotBytes;
-                const uint32_t bytes = *reinterpret_cast<const uint16_t *>(in + kMx4TileRows * 128 + (sub >> 1) * kMx4TileBytes +
-                                                                           scale_at + (sub & 1) * 2);
-                uint32_t v[32];
+                const uint32_t bytes = *reinterpret_cast<const uint32_t *>(in + kMx4TileRows * 128 + sub * kMx4TileBytes + scale_at);
+                uint4 w[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 4 + b) ^ swap) << 4));
+                __syncwarp();  // the codes are in registers
+                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 2 - sub : 1);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 2 + half) ^ swap) << 4));
-                    const uint32_t byte = half == 0 ? bytes & 0xffu : bytes >> 8;
-                    uint32_t factor;
-                    if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
-                    else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
-                    factor |= factor << 16;
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+                    uint32_t v[32];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        convert8<BF16>(words[i], factor, *reinterpret_cast<uint32_t(*)[4]>(&v[half * 16 + i * 4]));
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t byte = (bytes >> (8 * (half * 2 + b))) & 0xffu;
+                        uint32_t factor;
+                        if constexpr (BF16) factor = byte == 255u ? 0x7fc0u : max(byte << 7, 0x0040u);
+                        else factor = byte == 255u ? 0x7e00u : half_pow2(static_cast<int>(byte) - top + 13);
+                        factor |= factor << 16;
+                        const uint4 c = w[half * 2 + b];
+                        const uint32_t words[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            convert8<BF16>(words[i], factor, *reinterpret_cast<uint32_t(*)[4]>(&v[b * 16 + i * 4]));
+                    }
+                    if (half == 0) {
+                        if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&empty[slot]), (uses - 1) & 1u, &failed);
+                        if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                        tcgen05_fence_after();
+                    }
+                    tmem_store32(to + half * 32, v);
                 }
-                __syncwarp();  // the codes are in registers
-                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 4 - sub : 1);
-                if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&empty[slot]), (uses - 1) & 1u, &failed);
-                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
-                tcgen05_fence_after();
-                tmem_store32(to, v);
+                if (!ok) break;
                 tmem_store_wait();
                 tcgen05_fence_before();
                 __syncwarp();
@@ -355,7 +368,7 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     a.n_rows = p.n_rows;
     a.ldy = p.ldy;
     a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
-    a.steps = static_cast<int>((p.n_cols + 63) / 64);
+    a.steps = a.tile_cols;
     const int64_t row_tiles = mx4_tile_rows(p.n_rows);
     a.tile_tokens = tile_tokens(p.n_tokens, row_tiles, sms);
     const int64_t tiles = row_tiles * ((p.n_tokens + a.tile_tokens - 1) / a.tile_tokens);
