@@ -22,7 +22,7 @@ constexpr int kTileTokens = 128;
 constexpr int kStageBytesA = kTileTokens * 128;
 constexpr int kOutBytes = 32 * 128;   // a warp's piece of the output, 32 tokens x 64 rows, on its way out
 constexpr int kTmemColumns = 512;
-constexpr int kScaleColumns = 448;  // two buffers of 24 columns: A 2 tiles x 4, B 2 x 8
+constexpr int kScaleBuffer = 24;      // columns of a stage's scales: A 2 tiles x 4, B 2 x 8
 
 struct GemmArgs {
     const uint8_t *scale_x, *scale_w;
@@ -46,6 +46,9 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     constexpr int kScaleBytes = 2 * kMx4TileBytes * (1 + kScaleTilesB);
     constexpr int kSecond = N == 256 ? 192 : N;             // column of the second accumulator
     constexpr int kShared = N == 256 ? 64 : 0;              // its first columns that the first one shares
+    constexpr int kScaleColumns = N == 256 ? 448 : 2 * N;   // scales follow
+    // scale columns for every stage, where there is room; else two sets in turn
+    constexpr bool kScalesPerStage = kScaleColumns + STAGES * kScaleBuffer <= kTmemColumns;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free, drained;
     __shared__ uint32_t tmem_base, failed;
@@ -116,15 +119,16 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             const uint32_t skip = (n * N % kMx4TileRows) / 32;
             for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
                 ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
-                // the scale columns written now were last read two stages ago
-                if (step >= 2) {
+                // the scale columns written now were last read two stages ago (or, a set a stage, by
+                // the products whose end let this stage be filled again)
+                if (!kScalesPerStage && step >= 2) {
                     ok = ok && mbar_wait_or_fail(smem_addr(&empty[before.slot]), before.parity, &failed);
                     before.next();
                 }
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 tcgen05_fence_after();
                 if (elect_one()) {
-                    const uint32_t sfa = tmem + kScaleColumns + (step & 1) * 24, sfb = sfa + 8;
+                    const uint32_t sfa = tmem + kScaleColumns + (kScalesPerStage ? at.slot : step & 1) * kScaleBuffer, sfb = sfa + 8;
                     const uint64_t da = desc0 + static_cast<uint32_t>(at.slot * (kOperandBytes / 16)), db = da + kStageBytesA / 16;
                     const uint64_t sc = scale0 + static_cast<uint32_t>(at.slot * (kScaleBytes / 16));
 #pragma unroll
