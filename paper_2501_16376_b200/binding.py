@@ -8,6 +8,7 @@ fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -536,25 +537,50 @@ def sp_calib_stats_noalloc(X: torch.Tensor, colsq_out: torch.Tensor | None = Non
 
 # ---------------------------------------------------------------- microscaled 4-bit weights
 
-def _on_current_device(t: torch.Tensor, what: str):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+# These calls sit in decoding loops whose kernels take microseconds, so their checks are kept to
+# a few hundred nanoseconds each: the current device is asked for once a call, and what depends on
+# sizes alone is remembered.
+
+def _on_device(t: torch.Tensor, what: str, device: int):
+    if t.get_device() != device:
         raise SpError(SP_ERR_INVALID_ARG, "%s must be a CUDA tensor of the current device" % what)
 
 
-def _codes(codes: torch.Tensor, scales: torch.Tensor, n_cols: int):
+def _rows(t: torch.Tensor, what: str, device: int):
+    """_matrix for a tensor of the current device."""
+    if t.get_device() != device:
+        raise SpError(SP_ERR_INVALID_ARG, "%s must be a CUDA tensor of the current device" % what)
+    shape = t.shape
+    if len(shape) != 2:
+        raise SpError(SP_ERR_SHAPE, "%s must be 2-D with unit stride along its rows" % what)
+    R, n = shape
+    ld, inner = t.stride()
+    if n > 1 and inner != 1:
+        raise SpError(SP_ERR_SHAPE, "%s must be 2-D with unit stride along its rows" % what)
+    return t.data_ptr(), R, n, ld if R > 1 else max(ld, n)
+
+
+_current_device = torch.cuda.current_device
+
+
+def _raw_stream(stream, device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+
+
+def _codes(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, device: int):
     if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
         raise SpError(SP_ERR_DTYPE, "codes and scales are uint8 tensors")
-    _on_current_device(codes, "codes")
-    _on_current_device(scales, "scales")
-    ptr, R, width, ldc = _matrix(codes, "codes")
+    ptr, R, width, ldc = _rows(codes, "codes", device)
+    _on_device(scales, "scales", device)
     if width < (n_cols + 31) // 32 * 16:
         raise SpError(SP_ERR_SHAPE, "codes have %d bytes a row, %d columns need %d"
                       % (width, n_cols, (n_cols + 31) // 32 * 16))
-    if scales.numel() < lib.sp_mx4_scale_bytes(R, n_cols) or not scales.is_contiguous():
+    if scales.numel() < sp_mx4_scale_bytes(R, n_cols) or not scales.is_contiguous():
         raise SpError(SP_ERR_SHAPE, "scales must be contiguous with sp_mx4_scale_bytes entries")
     return ptr, R, ldc, scales.data_ptr()
 
 
+@functools.lru_cache(maxsize=4096)
 def sp_mx4_scale_bytes(n_rows: int, n_cols: int) -> int:
     return int(lib.sp_mx4_scale_bytes(int(n_rows), int(n_cols)))
 
@@ -564,37 +590,37 @@ def sp_mx4_quantize(W: torch.Tensor, mask: torch.Tensor | None = None, codes=Non
     """Microscaled 4-bit form of W (with the keep mask of a selection applied on the way).
     Returns (codes uint8 [rows, 16 * ceil(cols / 32)], scales uint8 in tiles; layout in the C
     header)."""
-    _on_current_device(W, "W")
-    ptr, R, n, ld = _matrix(W, "W")
+    device = _current_device()
+    ptr, R, n, ld = _rows(W, "W", device)
     if mask is not None:
-        _on_current_device(mask, "mask")
+        _on_device(mask, "mask", device)
         if (mask.dtype != torch.int32 or tuple(mask.shape) != (R, (n + 31) // 32)
                 or not mask.is_contiguous()):
             raise SpError(SP_ERR_SHAPE, "mask must be contiguous int32 [rows, ceil(cols/32)]")
     if codes is None:
         codes = torch.empty(R, (n + 31) // 32 * 16, dtype=torch.uint8, device=W.device)
     if scales is None:
-        scales = torch.empty(lib.sp_mx4_scale_bytes(R, n), dtype=torch.uint8, device=W.device)
-    cptr, rows, ldc, sptr = _codes(codes, scales, n)
+        scales = torch.empty(sp_mx4_scale_bytes(R, n), dtype=torch.uint8, device=W.device)
+    cptr, rows, ldc, sptr = _codes(codes, scales, n, device)
     if rows != R:
         raise SpError(SP_ERR_SHAPE, "codes have %d rows, W has %d" % (rows, R))
     _check(lib.sp_mx4_quantize(ptr, _dtype_of(W), R, n, ld, _ptr(mask), cptr, ldc, sptr,
-                               _stream(stream)))
+                               _raw_stream(stream, device)))
     return codes, scales
 
 
 def sp_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, dtype=None,
                       W_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The values of a 4-bit matrix as a 16-bit one [rows, n_cols] (of W_out's type, or dtype)."""
-    cptr, R, ldc, sptr = _codes(codes, scales, n_cols)
+    device = _current_device()
+    cptr, R, ldc, sptr = _codes(codes, scales, n_cols, device)
     if W_out is None:
         W_out = torch.empty(R, n_cols, dtype=dtype or torch.bfloat16, device=codes.device)
-    _on_current_device(W_out, "W_out")
-    optr, rows, n, ldo = _matrix(W_out, "W_out")
+    optr, rows, n, ldo = _rows(W_out, "W_out", device)
     if (rows, n) != (R, n_cols):
         raise SpError(SP_ERR_SHAPE, "W_out must be [%d, %d]" % (R, n_cols))
     _check(lib.sp_mx4_dequantize(cptr, ldc, sptr, R, n_cols, _dtype_of(W_out), optr, ldo,
-                                 _stream(stream)))
+                                 _raw_stream(stream, device)))
     return W_out
 
 
@@ -616,6 +642,7 @@ def _hold(keep, workspace, stream):
                            else torch.cuda.ExternalStream(int(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def sp_mx4_linear_workspace(n_tokens: int, n_rows: int, n_cols: int, mode: int = SP_MX4_A16) -> int:
     need = ctypes.c_int64()
     _check(lib.sp_mx4_linear_workspace(int(n_tokens), int(n_rows), int(n_cols), int(mode),
@@ -628,52 +655,57 @@ def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Y [tokens, rows] = X [tokens, cols] times the transposed 4-bit matrix.  SP_MX4_A16 takes
     X as it is, SP_MX4_A4 quantises it like the weights first."""
-    _on_current_device(X, "X")
-    ptr, T, n, ldx = _matrix(X, "X")
-    cptr, R, ldc, sptr = _codes(codes, scales, n)
+    device = _current_device()
+    ptr, T, n, ldx = _rows(X, "X", device)
+    cptr, R, ldc, sptr = _codes(codes, scales, n, device)
     if Y is None:
         Y = torch.empty(T, R, dtype=X.dtype, device=X.device)
-    _on_current_device(Y, "Y")
-    yptr, rows, cols, ldy = _matrix(Y, "Y")
+    yptr, rows, cols, ldy = _rows(Y, "Y", device)
     if (rows, cols) != (T, R):
         raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
     if Y.dtype != X.dtype:
         raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
     wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X.device)
-    _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, int(mode), yptr,
-                             ldy, wptr, wbytes, _stream(stream)))
+    _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, mode, yptr, ldy,
+                             wptr, wbytes, _raw_stream(stream, device)))
     _hold(keep, workspace, stream)
     return Y
 
 
 # ---------------------------------------------------------------- 8-bit key/value cache
 
-def _heads(t: torch.Tensor, what: str, n_seqs: int, head_dim: int) -> Strides:
-    if t.dim() != 4 or t.shape[0] != n_seqs or t.shape[3] != head_dim or t.stride(3) != 1:
+@functools.lru_cache(maxsize=4096)
+def _strides(seq: int, token: int, head: int) -> Strides:
+    return Strides(seq, token, head)
+
+
+def _heads(t: torch.Tensor, what: str, n_seqs: int, head_dim: int, device: int) -> Strides:
+    shape, s = t.shape, t.stride()
+    if len(shape) != 4 or shape[0] != n_seqs or shape[3] != head_dim or s[3] != 1:
         raise SpError(SP_ERR_SHAPE, "%s must be [%d, tokens, heads, %d] with consecutive values"
                       % (what, n_seqs, head_dim))
-    _on_current_device(t, what)
-    s = t.stride()
-    return Strides(s[0], s[1], s[2])
+    _on_device(t, what, device)
+    return _strides(s[0], s[1], s[2])
 
 
-def _int32(t, what, shape):
+def _int32(t, what, shape, device: int):
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous int32 %s" % (what, list(shape)))
-    _on_current_device(t, what)
+    _on_device(t, what, device)
     return t.data_ptr()
 
 
-def _acc(t, what, n_seqs, n_heads, length):
+def _acc(t, what, n_seqs, n_heads, length, device: int):
     """Pointer and leading dimension of a float [n_seqs, kv heads, >= length] tensor."""
-    if (t.dtype != torch.float32 or t.dim() != 3 or t.shape[0] != n_seqs or t.shape[1] != n_heads
-            or t.shape[2] < length or not t.is_contiguous()):
+    shape = t.shape
+    if (t.dtype != torch.float32 or len(shape) != 3 or shape[0] != n_seqs or shape[1] != n_heads
+            or shape[2] < length or not t.is_contiguous()):
         raise SpError(SP_ERR_SHAPE, "%s must be contiguous float32 [%d, %d, >= %d]"
                       % (what, n_seqs, n_heads, length))
-    _on_current_device(t, what)
-    return t.data_ptr(), t.shape[2]
+    _on_device(t, what, device)
+    return t.data_ptr(), shape[2]
 
 
 class KvCache:
@@ -682,26 +714,28 @@ class KvCache:
     and V, and an int32 table [n_seqs, blocks of a sequence]."""
 
     def __init__(self, k, v, k_scale, v_scale, table):
+        device = _current_device()
         for t, what in ((k, "k"), (v, "v")):
             if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous():
                 raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous uint8 [n_blocks, heads, "
                                                   "block tokens, head size]" % what)
-            _on_current_device(t, what)
+            _on_device(t, what, device)
         if k.shape != v.shape:
             raise SpError(SP_ERR_SHAPE, "k and v must have the same shape")
         for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             if t.dtype != torch.float32 or t.shape != k.shape[:2] or not t.is_contiguous():
                 raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous float32 [n_blocks, heads]" % what)
-            _on_current_device(t, what)
+            _on_device(t, what, device)
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise SpError(SP_ERR_INVALID_ARG, "table must be int32 [n_seqs, blocks]")
-        _on_current_device(table, "table")
+        _on_device(table, "table", device)
         self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
         self.n_seqs, (_, self.n_kv_heads, self.block_tokens, self.head_dim) = table.shape[0], k.shape
         ld = table.stride(0) if self.n_seqs > 1 else max(table.stride(0), table.shape[1])
         self._c = CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                               table.data_ptr(), k.shape[0], self.n_seqs, table.shape[1], ld,
                               self.n_kv_heads, self.head_dim, self.block_tokens)
+        self._workspaces = {}
 
     @classmethod
     def empty(cls, n_seqs: int, max_tokens: int, n_kv_heads: int, head_dim: int,
@@ -718,21 +752,30 @@ class KvCache:
     def sp_cache_append(self, K, V, start, count=None, stream=None):
         """Writes K, V [n_seqs, new, kv heads, head size] at the places start[b] and following
         (start, count: int32 [n_seqs]; count defaults to all the new tokens)."""
-        ks, vs = (_heads(t, w, self.n_seqs, self.head_dim) for t, w in ((K, "K"), (V, "V")))
+        device = _current_device()
+        ks = _heads(K, "K", self.n_seqs, self.head_dim, device)
+        vs = _heads(V, "V", self.n_seqs, self.head_dim, device)
         if K.shape != V.shape or K.shape[2] != self.n_kv_heads:
             raise SpError(SP_ERR_SHAPE, "K and V must have the same shape and %d heads" % self.n_kv_heads)
         if K.dtype != V.dtype:
             raise SpError(SP_ERR_DTYPE, "K and V must have the same dtype")
         shape = (self.n_seqs,)
         _check(lib.sp_cache_append(self._c, K.data_ptr(), ks, V.data_ptr(), vs, _dtype_of(K),
-                                   K.shape[1], _int32(start, "start", shape),
-                                   _int32(count, "count", shape), _stream(stream)))
+                                   K.shape[1], _int32(start, "start", shape, device),
+                                   _int32(count, "count", shape, device),
+                                   _raw_stream(stream, device)))
 
     def sp_cache_attention_workspace(self, n_q: int, n_heads: int, max_len: int, want_acc: bool) -> int:
-        need = ctypes.c_int64()
-        _check(lib.sp_cache_attention_workspace(self._c, n_q, n_heads, max_len, int(want_acc),
-                                                ctypes.byref(need)))
-        return need.value
+        key = (n_q, n_heads, max_len, want_acc)
+        found = self._workspaces.get(key)
+        if found is None:
+            need = ctypes.c_int64()
+            _check(lib.sp_cache_attention_workspace(self._c, n_q, n_heads, max_len, int(want_acc),
+                                                    ctypes.byref(need)))
+            if len(self._workspaces) > 4096:
+                self._workspaces.clear()
+            found = self._workspaces[key] = need.value
+        return found
 
     def sp_cache_attention(self, Q, lens, max_len: int, scale: float | None = None, O=None,
                            lse=None, acc_in=None, acc_out=None, workspace=None, stream=None):
@@ -740,33 +783,35 @@ class KvCache:
         [n_seqs]) count the call's own n_q tokens; max_len bounds them.  scale defaults to
         1 / sqrt(head size).  acc_out (float32 [n_seqs, kv heads, >= max_len]) accumulates the
         attention every token received on top of acc_in.  Returns O."""
-        qs = _heads(Q, "Q", self.n_seqs, self.head_dim)
+        device = _current_device()
+        qs = _heads(Q, "Q", self.n_seqs, self.head_dim, device)
         if O is None:
             O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-        os_ = _heads(O, "O", self.n_seqs, self.head_dim)
+        os_ = _heads(O, "O", self.n_seqs, self.head_dim, device)
         if O.shape != Q.shape:
             raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
         if O.dtype != Q.dtype:
             raise SpError(SP_ERR_DTYPE, "Q and O must have the same dtype")
         n_q, n_heads = Q.shape[1], Q.shape[2]
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
-                                or tuple(lse.shape) != tuple(Q.shape[:3])):
-            raise SpError(SP_ERR_SHAPE, "lse must be contiguous float32 [n_seqs, n_q, heads]")
+        if lse is not None:
+            if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != Q.shape[:3]:
+                raise SpError(SP_ERR_SHAPE, "lse must be contiguous float32 [n_seqs, n_q, heads]")
+            _on_device(lse, "lse", device)
         ai = ao = None
         ld = max_len
         if acc_out is not None:
-            ao, ld = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, max_len)
+            ao, ld = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, max_len, device)
             if acc_in is not None:
-                ai, ld_in = _acc(acc_in, "acc_in", self.n_seqs, self.n_kv_heads, max_len)
+                ai, ld_in = _acc(acc_in, "acc_in", self.n_seqs, self.n_kv_heads, max_len, device)
                 if ld_in != ld:
                     raise SpError(SP_ERR_SHAPE, "acc_in and acc_out must have the same shape")
         need = self.sp_cache_attention_workspace(n_q, n_heads, max_len, ao is not None)
         wptr, wbytes, keep = _workspace(need, workspace, Q.device)
         _check(lib.sp_cache_attention(self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads,
-                                      _int32(lens, "lens", (self.n_seqs,)), max_len,
+                                      _int32(lens, "lens", (self.n_seqs,), device), max_len,
                                       self.head_dim ** -0.5 if scale is None else scale,
                                       O.data_ptr(), os_, _ptr(lse), ai, ao, ld, wptr, wbytes,
-                                      _stream(stream)))
+                                      _raw_stream(stream, device)))
         _hold(keep, workspace, stream)
         return O
 
@@ -774,7 +819,8 @@ class KvCache:
                        acc_out=None, kept_out=None, lens_out=None, stream=None):
         """Keeps budget tokens of every (sequence, kv head): the last `recent` and those with the
         largest acc; lays them into dst's blocks.  Returns (kept_out, acc_out, lens_out)."""
-        a, ld = _acc(acc, "acc", self.n_seqs, self.n_kv_heads, max_len)
+        device = _current_device()
+        a, ld = _acc(acc, "acc", self.n_seqs, self.n_kv_heads, max_len, device)
         if dst.n_seqs != self.n_seqs:
             raise SpError(SP_ERR_SHAPE, "dst must have the same sequences")
         shape = (self.n_seqs, self.n_kv_heads, budget)
@@ -784,11 +830,13 @@ class KvCache:
             acc_out = torch.empty(shape, dtype=torch.float32, device=acc.device)
         if lens_out is None:
             lens_out = torch.empty(self.n_seqs, dtype=torch.int32, device=acc.device)
-        ao, ld_out = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, budget)
-        _check(lib.sp_cache_evict(self._c, _int32(lens, "lens", (self.n_seqs,)), max_len, a, ld,
-                                  budget, recent, dst._c, _int32(kept_out, "kept_out", shape), ao,
-                                  ld_out, _int32(lens_out, "lens_out", (self.n_seqs,)),
-                                  _stream(stream)))
+        ao, ld_out = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, budget, device)
+        lens_shape = (self.n_seqs,)
+        _check(lib.sp_cache_evict(self._c, _int32(lens, "lens", lens_shape, device), max_len, a, ld,
+                                  budget, recent, dst._c,
+                                  _int32(kept_out, "kept_out", shape, device), ao, ld_out,
+                                  _int32(lens_out, "lens_out", lens_shape, device),
+                                  _raw_stream(stream, device)))
         return kept_out, acc_out, lens_out
 
 
