@@ -3,8 +3,10 @@
 // Mathematics: s_j = scale * q . k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) with the
 // running maximum m of an online softmax, in one pass over the cache; the splits of a long cache
 // are joined afterwards by the same rule.  Accumulated weights need the final maximum and sum, so
-// the pass leaves the scores (4 bytes a row and token, against 2 * head_dim of cache) and the
-// joining kernel turns them into weights.
+// the pass leaves the scores (4 bytes a row and token, against 2 * head_dim of cache) and they are
+// turned into weights at the end.  Up to 8 splits are a cluster and finish in the kernel, through
+// distributed shared memory, each block with the scores it left itself; more splits (few sequences,
+// long caches), or weights summed over several tiles of rows, take a second kernel.
 //
 // Bound by memory: 2 * head_dim bytes per token and kv head.  The heads of a group and the query
 // tokens form the rows that share a pass, 8 (or 16) at a time.  Tokens are the long side of both
@@ -50,6 +52,9 @@ struct AttnArgs {
     float *part_o;   // [seq, kv head, split, row, D] unnormalised, relative to part_m
     float2 *part_ml; // [seq, kv head, split, row] maximum (log2) and sum
     float *scores;   // [seq, kv head, max_len, rows], log2; nullable
+    const float *acc_in;  // accumulated weights; acc_out is null where a second kernel joins the splits
+    float *acc_out;
+    int64_t ld_acc;
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -90,6 +95,18 @@ __device__ __forceinline__ void read_piece(uint32_t src, uint32_t *w) {
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(src));
 }
 
+// A peer block's value.
+__device__ __forceinline__ float load_remote(const float *p, int rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_address(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 load_remote(const float2 *p, int rank) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(remote_address(p, rank)) : "memory");
+    return v;
+}
+
 // Place of a row's query token in its sequence, at most the last cached token; < 0: sees nothing.
 __device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row, int64_t len) {
     if (row >= a.rows) return -1;
@@ -108,7 +125,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     constexpr int kStep = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
     extern __shared__ __align__(1024) uint8_t ring[];  // [kRing][warp][kStep]; afterwards the warps' sums
     float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
-    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
+    float(*block_o)[D] = sh_o[kAttnWarps];             // the block's sum of them
+    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8], row_lse[NT * 8];
+    __shared__ float2 block_ml[NT * 8];
     __shared__ uint64_t full[kRing], empty[kRing];
     __shared__ float2 scales[kRing][kAttnWarps];  // of K and V
     __shared__ uint32_t present[kRing][kAttnWarps];  // whether the table names a block there
@@ -482,16 +501,70 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             a.part_o[p * D + d] = out;
             if (d == 0) a.part_ml[p] = make_float2(top, sum);
         } else {
-            const int i = row / a.group, hq = head * a.group + row % a.group;
-            const float y = sum == 0.0f ? 0.0f : out / sum;
-            uint16_t bits;
-            if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-            else bits = __half_as_ushort(__float2half_rn(y));
-            a.O[seq * a.o.seq + i * a.o.token + hq * a.o.head + d] = bits;
-            if (d == 0 && a.lse != nullptr)
-                a.lse[(seq * a.n_q + i) * a.n_heads + hq] = (top + log2f(sum)) * 0.6931471805599453f;
+            block_o[r][d] = out;
+            if (d == 0) block_ml[r] = make_float2(top, sum);
         }
     }
+    if (a.part_o != nullptr) return;
+
+    // the cluster's blocks share the output's elements
+    const int ranks = a.splits, rank = blockIdx.x;
+    if (ranks > 1) cluster_sync();
+    else __syncthreads();
+    const int share = NT * 8 * D / ranks;
+    for (int at = rank * share + threadIdx.x; at < (rank + 1) * share; at += kAttnWarps * 32) {
+        const int r = at / D, d = at % D, row = row0 + r;
+        if (row >= a.rows) break;
+        float top = kLowest, sum = 0.0f, out = 0.0f;
+        for (int k = 0; k < ranks; ++k) {
+            const float2 ml = load_remote(&block_ml[r], k);
+            const float v = load_remote(&block_o[r][d], k), most = fmaxf(top, ml.x);
+            const float f = exp2_fast(top - most), h = exp2_fast(ml.x - most);
+            sum = fmaf(sum, f, ml.y * h);
+            out = fmaf(out, f, v * h);
+            top = most;
+        }
+        const int i = row / a.group, hq = head * a.group + row % a.group;
+        const float y = sum == 0.0f ? 0.0f : out / sum;
+        uint16_t bits;
+        if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+        else bits = __half_as_ushort(__float2half_rn(y));
+        a.O[seq * a.o.seq + i * a.o.token + hq * a.o.head + d] = bits;
+        if (d == 0 && a.lse != nullptr) a.lse[(seq * a.n_q + i) * a.n_heads + hq] = (top + log2f(sum)) * 0.6931471805599453f;
+    }
+    if (a.acc_out != nullptr) {
+        if (threadIdx.x < NT * 8) {
+            float top = kLowest, sum = 0.0f;
+            for (int k = 0; k < ranks; ++k) {
+                const float2 ml = load_remote(&block_ml[threadIdx.x], k);
+                const float most = fmaxf(top, ml.x);
+                sum = fmaf(sum, exp2_fast(top - most), ml.y * exp2_fast(ml.x - most));
+                top = most;
+            }
+            row_lse[threadIdx.x] = sum == 0.0f ? INFINITY : top + log2f(sum);
+        }
+        __syncthreads();
+        const int64_t pair = seq * H + head;
+        const int own = static_cast<int>(max(int64_t(-1), min(a.lens[seq] - a.n_q, a.max_len)));
+        const int end = min(last * 16, len);
+        for (int j = first * 16 + threadIdx.x; j < end; j += kAttnWarps * 32) {
+            const float *x = a.scores + (pair * a.max_len + j) * a.rows;
+            float sum = a.acc_in != nullptr && j < own ? a.acc_in[pair * a.ld_acc + j] : 0.0f, add = 0.0f;
+            if ((a.rows & 3) == 0) {
+                for (int r = 0; r < a.rows; r += 4) {
+                    const float4 v = *reinterpret_cast<const float4 *>(x + r);
+                    add += exp2_fast(v.x - row_lse[r]) + exp2_fast(v.y - row_lse[r + 1]) + exp2_fast(v.z - row_lse[r + 2]) +
+                           exp2_fast(v.w - row_lse[r + 3]);
+                }
+            } else {
+                for (int r = 0; r < a.rows; ++r) add += exp2_fast(x[r] - row_lse[r]);
+            }
+            a.acc_out[pair * a.ld_acc + j] = sum + add;
+        }
+        for (int64_t j = len + rank * (kAttnWarps * 32) + threadIdx.x; j < a.max_len; j += ranks * kAttnWarps * 32)
+            a.acc_out[pair * a.ld_acc + j] = 0.0f;
+    }
+    if (ranks > 1) cluster_sync();  // no block leaves while its sums are read
 }
 
 // Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)
@@ -602,21 +675,39 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
     }
 }
 
-// How many blocks share a (sequence, kv head, row tile): enough for about 8 blocks an SM, none
-// with less than 64 tokens.
-static int attention_splits(const sp_cache &c, int row_tiles, int64_t max_len, bool want_acc) {
-    const int64_t units = c.n_seqs * c.n_kv_heads * row_tiles;
+// How many blocks share a (sequence, kv head, row tile), none with less than 64 tokens, and whether
+// they finish together.  Where that gives a few blocks (short caches, few heads), a cluster of up
+// to 8 spares the second kernel: 517 tokens of 16 heads take 6.7 us against 7.6.  Otherwise all
+// blocks run at once, 4 an SM, and the second kernel has the device to itself: 32 x 8191 tokens of
+// 8 heads with weights take 102 us, in clusters 115 to 117 (blocks of a cluster start and end
+// together).
+struct AttentionPlan {
+    int row_tiles, splits;
+    bool join;  // a second kernel joins the splits
+};
+static AttentionPlan attention_plan(const sp_cache &c, int64_t rows, int64_t max_len, bool want_acc) {
+    AttentionPlan p;
+    p.row_tiles = static_cast<int>(rows <= 8 ? 1 : (rows + 15) / 16);
+    const int64_t units = std::max(int64_t(1), c.n_seqs * c.n_kv_heads * p.row_tiles);
     const int64_t most = std::max(int64_t(1), (max_len + 63) / 64);
-    return static_cast<int>(std::max(int64_t(1), std::min(std::min(most, int64_t(256)), 148 * 8 / units)));
+    const int64_t want = std::max(int64_t(1), std::min(std::min(most, int64_t(256)), 148 * 4 / units));
+    p.splits = static_cast<int>(want);
+    if (want <= 15 && units * 8 <= 148 * 2 && (!want_acc || p.row_tiles == 1)) {
+        p.splits = 1;
+        while (p.splits < 8 && p.splits * 2 <= want) p.splits *= 2;
+        p.join = false;
+    } else {
+        p.join = p.splits > 1 || want_acc;
+    }
+    return p;
 }
-static int attention_row_tiles(int64_t rows) { return static_cast<int>(rows <= 8 ? 1 : (rows + 15) / 16); }
 
 int64_t cache_attention_workspace(const sp_cache &c, int64_t n_q, int n_heads, int64_t max_len, bool want_acc) {
     const int64_t rows = n_q * (n_heads / c.n_kv_heads), pairs = c.n_seqs * c.n_kv_heads;
-    const int splits = attention_splits(c, attention_row_tiles(rows), max_len, want_acc);
-    if (pairs == 0 || rows == 0 || (splits == 1 && !want_acc)) return 0;
-    int64_t bytes = pairs * splits * rows * (c.head_dim * 4 + 8);
-    if (want_acc) bytes += (pairs * max_len * rows + 3) / 4 * 16;
+    if (pairs == 0 || rows == 0) return 0;
+    const AttentionPlan plan = attention_plan(c, rows, max_len, want_acc);
+    int64_t bytes = want_acc ? (pairs * max_len * rows + 3) / 4 * 16 : 0;
+    if (plan.join) bytes += pairs * plan.splits * rows * (c.head_dim * 4 + 8);
     return bytes;
 }
 
@@ -634,26 +725,30 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     a.n_heads = n_heads;
     a.group = n_heads / c.n_kv_heads;
     a.rows = static_cast<int>(n_q * a.group);
-    a.row_tiles = attention_row_tiles(a.rows);
+    const AttentionPlan plan = attention_plan(c, a.rows, max_len, acc_out != nullptr);
+    a.row_tiles = plan.row_tiles;
+    a.splits = plan.splits;
     a.block_shift = c.block_tokens == 16 ? 4 : c.block_tokens == 32 ? 5 : 6;
-    a.splits = attention_splits(c, a.row_tiles, max_len, acc_out != nullptr);
     a.lens = lens;
     a.scale_log2 = scale * kLog2e;
     a.O = static_cast<uint16_t *>(O);
     a.lse = lse;
     const int64_t pairs = c.n_seqs * c.n_kv_heads;
-    const bool join = a.splits > 1 || acc_out != nullptr;
-    if (join) {
-        // scores first: their loads want 16-byte boundaries
-        float *at = static_cast<float *>(workspace);
-        if (acc_out != nullptr) {
-            a.scores = at;
-            at += (pairs * max_len * a.rows + 3) / 4 * 4;
-        }
+    // scores first: their loads want 16-byte boundaries
+    float *at = static_cast<float *>(workspace);
+    if (acc_out != nullptr) {
+        a.scores = at;
+        at += (pairs * max_len * a.rows + 3) / 4 * 4;
+    }
+    if (!plan.join) {
+        a.acc_in = acc_in;
+        a.acc_out = acc_out;
+        a.ld_acc = ld_acc;
+    } else {
         a.part_o = at;
         a.part_ml = reinterpret_cast<float2 *>(at + pairs * a.splits * a.rows * c.head_dim);
     }
-    PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
+    ClusterPdlConfig pdl(plan.join ? 1 : a.splits, dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
     CUtensorMap k_map = {}, v_map = {};
     cudaError_t e = cudaSuccess;
     if (c.n_blocks > 0) {
@@ -678,7 +773,7 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     sp_status st = check_launch();
-    if (st != SP_OK || !join) return st;
+    if (st != SP_OK || !plan.join) return st;
     const int64_t blocks = std::max(acc_out != nullptr ? (max_len + kJoinTokens - 1) / kJoinTokens : 1, std::min(int64_t(a.rows), int64_t(8)));
     PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(kJoinThreads), stream);
     second.cfg.dynamicSmemBytes = a.rows * sizeof(float);

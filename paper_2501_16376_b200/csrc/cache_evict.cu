@@ -39,14 +39,6 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t remote_address(const void *p, int rank) {
-    uint32_t remote;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr(p)), "r"(rank));
-    return remote;
-}
 __device__ __forceinline__ uint32_t load_remote(const uint32_t *p, int rank) {
     uint32_t v;
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote_address(p, rank)) : "memory");
@@ -271,20 +263,9 @@ __global__ void __launch_bounds__(THREADS, 2) cache_select_kernel(const SelectAr
 
 template <int THREADS, int KEYS, bool HELD>
 static cudaError_t launch_select(const SelectArgs &a, int64_t rows, int ranks, cudaStream_t stream) {
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = ranks;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ranks, static_cast<unsigned>(a.n_kv_heads), static_cast<unsigned>(rows / a.n_kv_heads));
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = ranks > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, cache_select_kernel<THREADS, KEYS, HELD>, a);
+    ClusterPdlConfig pdl(ranks, dim3(ranks, static_cast<unsigned>(a.n_kv_heads), static_cast<unsigned>(rows / a.n_kv_heads)),
+                         dim3(THREADS), stream);
+    return cudaLaunchKernelEx(&pdl.cfg, cache_select_kernel<THREADS, KEYS, HELD>, a);
 }
 
 static cudaError_t launch_select(const SelectArgs &a, int64_t rows, cudaStream_t stream) {

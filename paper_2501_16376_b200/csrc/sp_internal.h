@@ -195,6 +195,25 @@ struct PdlConfig {
     }
 };
 
+// The same for clusters of `blocks` neighbours along x.
+struct ClusterPdlConfig {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    ClusterPdlConfig(int blocks, dim3 grid, dim3 block, cudaStream_t stream) : cfg{}, attr{} {
+        cfg.gridDim = grid;
+        cfg.blockDim = block;
+        cfg.stream = stream;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = static_cast<unsigned>(blocks);
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = blocks > 1 ? 2 : 1;
+    }
+};
+
 // Allows a kernel all the dynamic shared memory of an SM, once for each device.
 class DynamicSmem {
    public:
