@@ -39,7 +39,9 @@ static cudaError_t encode_tiles(CUtensorMap *map, CUtensorMapDataType type, int 
     const cuuint32_t step[2] = {1, 1};
     const CUresult r = encode(map, type, 2, const_cast<void *>(base), dims, strides, box, step,
                               CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              box_bytes == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                              : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                : CU_TENSOR_MAP_SWIZZLE_NONE,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -50,6 +52,9 @@ cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 
 cudaError_t encode_byte_rows(CUtensorMap *map, const void *base, int64_t rows, int row_bytes, int box_rows) {
     return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, row_bytes, row_bytes, box_rows, row_bytes);
+}
+cudaError_t encode_scale_tiles(CUtensorMap *map, const void *base, int64_t rows, int box_rows) {
+    return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, base, rows, 128, 512, box_rows, 512);
 }
 cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
     return encode_tiles(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, rows, cols, ld * 2, box_rows);

@@ -73,15 +73,6 @@ __device__ __forceinline__ uint32_t finite_amax8(const float (&v)[8]) {
     return m;
 }
 
-// Thread-block clusters: a barrier over the cluster, and the address of a peer block's shared memory.
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t remote_address(const void *p, int rank) {
-    uint32_t remote;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_addr(p)), "r"(rank));
-    return remote;
-}
 // Block that holds the tokens from place * block_tokens of a sequence; -1 if the table names none.
 __device__ __forceinline__ int64_t cache_block(const sp_cache &c, int64_t seq, int64_t place) {
     if (place >= c.table_cols) return -1;

@@ -2,8 +2,11 @@
 // activations are quantised first (mx4_quantize.cu, into the workspace), then
 //     Y [tokens, rows] = Xq Wq^T,   both operands as they are stored, scales included.
 //
-// Bound by the tensor cores at many tokens, by the weights' bytes at few.  A tile is 128 tokens x
-// N rows of the weights (N = 64 .. 256, see tile_rows), summed over the columns 256 at a time:
+// Bound by the weights' bytes at few tokens; at many, by what flows into an SM (64 bytes a cycle: a
+// stage of 128 x 256 rows of 128 bytes takes 800 cycles, its products 512) unless two blocks share a
+// tile.  A tile is 128 tokens x N rows of the weights (N = 64 .. 256, see choose_tile), or, for a
+// pair of blocks, 256 tokens, each block with 128 of them and half of the weights' rows, of which
+// the tensor cores of both read.  It is summed over the columns 256 at a time:
 // one thread keeps kStages of both operands and their scale tiles in flight by TMA, one issues
 // the products (64 columns each; scale tiles go to tensor memory by a copy just before), four
 // warps empty the accumulators.  Two accumulators alternate so that emptying one overlaps
@@ -36,11 +39,13 @@ struct GemmArgs {
 
 }  // namespace
 
-template <bool BF16, int N, int STAGES>
+template <bool BF16, int N, int STAGES, bool PAIR>
 __global__ void __launch_bounds__(256, 1)
 mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
-                const __grid_constant__ CUtensorMap y_map, const GemmArgs a) {
-    constexpr int kStageBytesB = N * 128;
+                const __grid_constant__ CUtensorMap y_map, const __grid_constant__ CUtensorMap x_scale_map,
+                const __grid_constant__ CUtensorMap w_scale_map, const GemmArgs a) {
+    constexpr int kBlocks = PAIR ? 2 : 1, kRowsB = N / kBlocks;  // rows of the weights that a block holds
+    constexpr int kStageBytesB = kRowsB * 128;
     constexpr int kOperandBytes = kStageBytesA + kStageBytesB;
     constexpr int kScaleTilesB = N > 128 ? 2 : 1;           // row tiles of scales under a tile of N rows
     constexpr int kScaleBytes = 2 * kMx4TileBytes * (1 + kScaleTilesB);
@@ -54,23 +59,25 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     __shared__ uint32_t tmem_base, failed;
     uint8_t *const operands = smem, *const out_stage = smem + STAGES * kOperandBytes, *const scales = out_stage + 4 * kOutBytes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
+    const int rank = PAIR ? blockIdx.x & 1 : 0, unit = blockIdx.x / kBlocks, units = gridDim.x / kBlocks;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
         tma_prefetch_map(&w_map);
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(smem_addr(&full[s]), 1);
+            mbar_init(smem_addr(&full[s]), kBlocks);  // of a pair: the first block's counts, for both
             mbar_init(smem_addr(&empty[s]), 1);
         }
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
-        mbar_init(smem_addr(&acc_free), 128);
+        mbar_init(smem_addr(&acc_free), 128 * kBlocks);
         mbar_init(smem_addr(&drained), 1);
         failed = 0u;
         mbar_fence_init();
     }
-    if (warp == 2) tmem_alloc(&tmem_base, kTmemColumns);
+    if (warp == 2) tmem_alloc<PAIR>(&tmem_base, kTmemColumns);
     tcgen05_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();  // the peer's barriers are ready
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     pdl_launch_dependents();
@@ -80,8 +87,8 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         RingPlace<STAGES> at;
         int step = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
-            const int m = tile % a.token_tiles, n = tile / a.token_tiles;
+        for (int tile = unit; ok && tile < a.tiles; tile += units) {
+            const int m = tile % a.token_tiles * kBlocks + rank, n = tile / a.token_tiles;
             const int64_t wt = int64_t(n) * N / kMx4TileRows;
             const int w_tiles = static_cast<int>(min(int64_t(kScaleTilesB), mx4_tile_rows(a.n_rows) - wt));
             const uint8_t *sx = a.scale_x + int64_t(m) * a.tile_cols * kMx4TileBytes;
@@ -90,27 +97,39 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                 if (step >= STAGES) ok = mbar_wait_or_fail(smem_addr(&empty[at.slot]), at.parity ^ 1u, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 if (elect_one()) {
-                    const uint32_t bar = smem_addr(&full[at.slot]);
-                    const int bytes = min(2, a.tile_cols - 2 * k) * kMx4TileBytes;
                     const uint32_t to = smem_addr(operands + at.slot * kOperandBytes), sc = smem_addr(scales + at.slot * kScaleBytes);
-                    mbar_expect_tx(bar, kOperandBytes + bytes * (1 + w_tiles));
-                    tma_load_2d(to, &x_map, k * 128, m * kTileTokens, bar);
-                    tma_load_2d(to + kStageBytesA, &w_map, k * 128, n * N, bar);
-                    bulk_load(sc, sx + k * (2 * kMx4TileBytes), bytes, bar);
-                    for (int i = 0; i < w_tiles; ++i)
-                        bulk_load(sc + (1 + i) * 2 * kMx4TileBytes, sw + (int64_t(i) * a.tile_cols + 2 * k) * kMx4TileBytes, bytes, bar);
+                    if constexpr (PAIR) {
+                        const uint32_t bar = remote_address(&full[at.slot], 0);
+                        mbar_expect_tx_cluster(bar, kOperandBytes + kScaleBytes);
+                        tma_load_2d_pair(to, &x_map, k * 128, m * kTileTokens, bar);
+                        tma_load_2d_pair(to + kStageBytesA, &w_map, k * 128, n * N + rank * kRowsB, bar);
+                        // two tiles each; of an odd last one the second is not used
+                        tma_load_2d_pair(sc, &x_scale_map, 0, m * a.tile_cols + 2 * k, bar);
+#pragma unroll
+                        for (int i = 0; i < kScaleTilesB; ++i)
+                            tma_load_2d_pair(sc + (1 + i) * 2 * kMx4TileBytes, &w_scale_map, 0, static_cast<int>(wt + i) * a.tile_cols + 2 * k, bar);
+                    } else {
+                        const uint32_t bar = smem_addr(&full[at.slot]);
+                        const int bytes = min(2, a.tile_cols - 2 * k) * kMx4TileBytes;
+                        mbar_expect_tx(bar, kOperandBytes + bytes * (1 + w_tiles));
+                        tma_load_2d(to, &x_map, k * 128, m * kTileTokens, bar);
+                        tma_load_2d(to + kStageBytesA, &w_map, k * 128, n * N, bar);
+                        bulk_load(sc, sx + k * (2 * kMx4TileBytes), bytes, bar);
+                        for (int i = 0; i < w_tiles; ++i)
+                            bulk_load(sc + (1 + i) * 2 * kMx4TileBytes, sw + (int64_t(i) * a.tile_cols + 2 * k) * kMx4TileBytes, bytes, bar);
+                    }
                 }
                 __syncwarp();
             }
         }
         if (failed != 0u && lane == 0)
             for (int s = max(0, step - STAGES); s < step; ++s) mbar_wait(smem_addr(&full[s % STAGES]), (s / STAGES) & 1);
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         RingPlace<STAGES> at, before;  // `before` follows two stages behind
         int step = 0, count = 0;
         bool ok = true;
         const uint64_t desc0 = desc_rows128(smem_addr(operands)), scale0 = desc_scales(smem_addr(scales));
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count) {
             const int n = tile / a.token_tiles;
             if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
@@ -134,33 +153,37 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (2 * k + c >= a.tile_cols) break;
-                        tmem_copy_scales(sfa + c * 4, sc + c * (kMx4TileBytes / 16));
+                        tmem_copy_scales<PAIR>(sfa + c * 4, sc + c * (kMx4TileBytes / 16));
 #pragma unroll
                         for (int i = 0; i < kScaleTilesB; ++i)
-                            tmem_copy_scales(sfb + c * 8 + i * 4, sc + ((1 + i) * 2 + c) * (kMx4TileBytes / 16));
+                            tmem_copy_scales<PAIR>(sfb + c * 8 + i * 4, sc + ((1 + i) * 2 + c) * (kMx4TileBytes / 16));
                     }
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
                         if (2 * k + (p >> 1) >= a.tile_cols) break;
-                        mma_mxf4(acc, da + p * 2, db + p * 2, mxf4_instruction(N, p & 1), sfa + (p >> 1) * 4,
+                        mma_mxf4<PAIR>(acc, da + p * 2, db + p * 2, mxf4_instruction<PAIR>(N, p & 1), sfa + (p >> 1) * 4,
                                  sfb + (p >> 1) * 8 + skip, k > 0 || p > 0);
                     }
-                    tcgen05_commit(smem_addr(&empty[at.slot]));
-                    if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+                    tcgen05_commit<PAIR>(smem_addr(&empty[at.slot]));
+                    if (k == a.steps - 1) tcgen05_commit<PAIR>(smem_addr(&acc_full[count & 1]));
                 }
                 __syncwarp();
             }
         }
         if (failed != 0u) {
-            if (elect_one()) tcgen05_commit(smem_addr(&drained));
+            if (elect_one()) tcgen05_commit<PAIR>(smem_addr(&drained));
             __syncwarp();
             if (lane == 0) mbar_wait(smem_addr(&drained), 0);
         }
     } else if (warp >= 4) {
         const int quarter = warp & 3;
         int count = 0;
-        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++count) {
-            const int m = tile % a.token_tiles, n = tile / a.token_tiles;
+        auto free_accumulator = [&] {
+            if constexpr (PAIR) mbar_arrive_cluster(remote_address(&acc_free, 0));
+            else mbar_arrive(smem_addr(&acc_free));
+        };
+        for (int tile = unit; tile < a.tiles; tile += units, ++count) {
+            const int m = tile % a.token_tiles * kBlocks + rank, n = tile / a.token_tiles;
             const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
@@ -168,7 +191,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             const int64_t token0 = int64_t(m) * kTileTokens + quarter * 32, token = token0 + lane;
             if (kShared == 0) {
                 tcgen05_fence_before();
-                mbar_arrive(smem_addr(&acc_free));
+                free_accumulator();
             }
 #pragma unroll 1
             for (int i = 0; i < N / 64; ++i) {
@@ -180,7 +203,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                 tmem_load_wait();
                 if (kShared != 0 && i == 0) {
                     tcgen05_fence_before();
-                    mbar_arrive(smem_addr(&acc_free));
+                    free_accumulator();
                 }
                 const int64_t row = int64_t(n) * N + piece * 64;
                 uint32_t h[32];
@@ -219,37 +242,52 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         tcgen05_fence_before();
     }
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();
     if (warp == 2) {
         tcgen05_fence_after();
-        tmem_free(tmem, kTmemColumns);
+        tmem_free<PAIR>(tmem, kTmemColumns);
     }
 }
 
-// Rows of the weights in a tile: the size that needs the least time in whole rounds over the SMs
-// (a round costs N and something like 32 for filling and emptying).
-static int tile_rows(int64_t token_tiles, int64_t n_rows, int sms) {
-    int best = 256;
+// Tile of a launch: the one that needs the least time in whole rounds over the SMs.  A stage's time
+// is that of its bytes, 64 a cycle into an SM: 128 tokens and the block's rows of 128 bytes, and
+// the scales.
+struct GemmTile {
+    int rows;
+    bool pair;
+};
+static GemmTile choose_tile(int64_t token_tiles, int64_t n_rows, int sms) {
+    GemmTile best = {256, false};
     int64_t least = INT64_MAX;
-    for (int n = 256; n >= 64; n -= 64) {
-        const int64_t tiles = token_tiles * ((n_rows + n - 1) / n);
-        const int64_t cost = (tiles + sms - 1) / sms * (n + 32);
-        if (cost < least) {
-            least = cost;
-            best = n;
+    for (int pair = 1; pair >= 0; --pair) {
+        if (pair && token_tiles < 2) continue;
+        for (int n = 256; n >= (pair ? 128 : 64); n -= 64) {
+            const int64_t tiles = (token_tiles + pair) / (1 + pair) * ((n_rows + n - 1) / n);
+            const int64_t units = sms / (1 + pair);
+            const int64_t cost = (tiles + units - 1) / units * ((128 + n / (1 + pair)) * 2 + 16 * (n > 128 ? 3 : 2));
+            if (cost < least) {
+                least = cost;
+                best = {n, pair != 0};
+            }
         }
     }
     return best;
 }
 
-template <bool BF16, int N, int STAGES>
-static sp_status launch_gemm(const CUtensorMap &x_map, const CUtensorMap &w_map, const CUtensorMap &y_map, GemmArgs a, int sms, cudaStream_t stream) {
-    auto *kernel = mx4_gemm_kernel<BF16, N, STAGES>;
+struct GemmMaps {
+    CUtensorMap x, w, y, x_scale, w_scale;
+};
+
+template <bool BF16, int N, int STAGES, bool PAIR>
+static sp_status launch_gemm(const GemmMaps &maps, GemmArgs a, int sms, cudaStream_t stream) {
+    auto *kernel = mx4_gemm_kernel<BF16, N, STAGES, PAIR>;
     static DynamicSmem limit;
     cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
     if (e != cudaSuccess) return cuda_fail(e);
-    PdlConfig pdl(dim3(static_cast<unsigned>(std::min(a.tiles, sms))), dim3(256), stream);
-    pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2)) + 4 * kOutBytes;
-    e = cudaLaunchKernelEx(&pdl.cfg, kernel, x_map, w_map, y_map, a);
+    constexpr int kBlocks = PAIR ? 2 : 1;
+    ClusterPdlConfig pdl(kBlocks, dim3(static_cast<unsigned>(std::min(a.tiles, sms / kBlocks) * kBlocks)), dim3(256), stream);
+    pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N / kBlocks * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2)) + 4 * kOutBytes;
+    e = cudaLaunchKernelEx(&pdl.cfg, kernel, maps.x, maps.w, maps.y, maps.x_scale, maps.w_scale, a);
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }
@@ -279,24 +317,38 @@ sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t str
     a.steps = (a.tile_cols + 1) / 2;
     a.tma_y = aligned16(p.Y) && p.ldy % 8 == 0;
     const int64_t token_tiles = (p.n_tokens + kTileTokens - 1) / kTileTokens;
-    const int n = tile_rows(token_tiles, p.n_rows, sms);
-    const int64_t tiles = token_tiles * ((p.n_rows + n - 1) / n);
+    const GemmTile tile = choose_tile(token_tiles, p.n_rows, sms);
+    const int blocks = tile.pair ? 2 : 1;
+    const int64_t tiles = (token_tiles + blocks - 1) / blocks * ((p.n_rows + tile.rows - 1) / tile.rows);
     if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
-    a.token_tiles = static_cast<int>(token_tiles);
+    a.token_tiles = static_cast<int>((token_tiles + blocks - 1) / blocks);
     a.tiles = static_cast<int>(tiles);
-    CUtensorMap x_map, w_map, y_map = {};
-    e = encode_byte_tiles(&x_map, codes, p.n_tokens, pitch, pitch, kTileTokens);
-    if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, pitch, p.ldc, n);
-    if (e == cudaSuccess && a.tma_y) e = encode_half_tiles(&y_map, p.Y, p.n_tokens, p.n_rows, p.ldy, 32);
+    GemmMaps maps = {};
+    e = encode_byte_tiles(&maps.x, codes, p.n_tokens, pitch, pitch, kTileTokens);
+    if (e == cudaSuccess) e = encode_byte_tiles(&maps.w, p.codes, p.n_rows, pitch, p.ldc, tile.rows / blocks);
+    if (e == cudaSuccess && a.tma_y) e = encode_half_tiles(&maps.y, p.Y, p.n_tokens, p.n_rows, p.ldy, 32);
+    if (tile.pair) {
+        const int64_t w_tiles = mx4_tile_rows(p.n_rows) * a.tile_cols, x_tiles = token_tiles * a.tile_cols;
+        if (w_tiles > 0x7fffffff || x_tiles > 0x7fffffff) return SP_ERR_SHAPE;
+        if (e == cudaSuccess) e = encode_scale_tiles(&maps.x_scale, scales, x_tiles, 2);
+        if (e == cudaSuccess) e = encode_scale_tiles(&maps.w_scale, p.scales, w_tiles, 2);
+    }
     if (e != cudaSuccess) return cuda_fail(e);
-#define SP_LAUNCH(NN, S)                                                                        \
-    return p.dtype == SP_BF16 ? launch_gemm<true, NN, S>(x_map, w_map, y_map, a, sms, stream)          \
-                              : launch_gemm<false, NN, S>(x_map, w_map, y_map, a, sms, stream)
-    switch (n) {
-        case 64: SP_LAUNCH(64, 8);
-        case 128: SP_LAUNCH(128, 6);
-        case 192: SP_LAUNCH(192, 4);
-        default: SP_LAUNCH(256, 4);
+#define SP_LAUNCH(N, S, P)                                                             \
+    return p.dtype == SP_BF16 ? launch_gemm<true, N, S, P>(maps, a, sms, stream)       \
+                              : launch_gemm<false, N, S, P>(maps, a, sms, stream)
+    if (tile.pair) {
+        switch (tile.rows) {
+            case 128: SP_LAUNCH(128, 7, true);
+            case 192: SP_LAUNCH(192, 5, true);
+            default: SP_LAUNCH(256, 5, true);
+        }
+    }
+    switch (tile.rows) {
+        case 64: SP_LAUNCH(64, 8, false);
+        case 128: SP_LAUNCH(128, 6, false);
+        case 192: SP_LAUNCH(192, 4, false);
+        default: SP_LAUNCH(256, 4, false);
     }
 #undef SP_LAUNCH
 }

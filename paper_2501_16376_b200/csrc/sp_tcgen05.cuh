@@ -21,18 +21,33 @@ __device__ __forceinline__ int uniform_warp() { return __shfl_sync(kFullWarp, st
 // ---- tensor memory (512 columns of 128 lanes x 32 bits on an SM)
 
 // One warp allocates; the base address lands in shared memory.  columns: a power of two >= 32.
+// PAIR: for products of a pair of blocks; a warp of each block allocates and frees.
+template <bool PAIR = false>
 __device__ __forceinline__ void tmem_alloc(uint32_t *dst, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
 }
+template <bool PAIR = false>
 __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
 }
 __device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// Arrives on the barrier when all tensor-core work this thread issued before has completed.
+// Arrives on the barrier (PAIR: of both blocks) when all tensor-core work this thread issued before
+// has completed.
+template <bool PAIR = false>
 __device__ __forceinline__ void tcgen05_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // 32 columns of this warp's 32 lanes (lanes 32 * (warp % 4) and following).
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
@@ -78,9 +93,11 @@ __device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
 // ---- instructions
 
 // A tile of scales (32 rows x 16 bytes) -> four columns of tensor memory, the same for each
-// quarter of the lanes.
+// quarter of the lanes.  PAIR: in both blocks, each from its own shared memory.
+template <bool PAIR = false>
 __device__ __forceinline__ void tmem_copy_scales(uint32_t dst, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(desc) : "memory");
 }
 
 // D [128 x n] (+)= A [128 x 16] B [n x 16]^T of 16-bit floats, binary32 sums.
@@ -95,16 +112,24 @@ __device__ __forceinline__ void mma_16bit(uint32_t d, uint32_t a, uint64_t b, ui
 }
 
 // D [128 x n] (+)= A [128 x 64] B [n x 64]^T of 4-bit floats with a scale for every 32.
-// `half`: which two of a tile's four blocks the 64 columns are.
+// `half`: which two of a tile's four blocks the 64 columns are.  PAIR: 256 rows of A, half of them
+// and half of B's rows in each block; every block has the scales of its rows of A and of all of B.
+template <bool PAIR = false>
 __device__ __forceinline__ uint32_t mxf4_instruction(int n, int half) {
     const uint32_t id = half ? 2u : 0u;
-    return (id << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (8u << 24) | (id << 29);
+    return (id << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | ((PAIR ? 16u : 8u) << 24) | (id << 29);
 }
+template <bool PAIR = false>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scale_a,
                                          uint32_t scale_b, bool accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"(accumulate ? 1u : 0u) : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"(accumulate ? 1u : 0u) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"(accumulate ? 1u : 0u) : "memory");
 }
 
 }  // namespace sp

@@ -93,6 +93,17 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
                  "[%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
 }
+// Pairs of blocks: the barrier may be the other block's (its address in the cluster's window).
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // Shared memory written by ordinary stores becomes visible to the asynchronous copies.
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Shared memory -> box of a 2-D tensor at (x, y), both inside it; what lies outside is not written.
@@ -114,6 +125,8 @@ cudaError_t encode_byte_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 // The same for rows of 64 or 128 bytes that follow one another, as whole rows (swizzled over 64 or
 // 128 bytes: with 64, chunk c of row r lands at c ^ (r / 2 & 3)).
 cudaError_t encode_byte_rows(CUtensorMap *map, const void *base, int64_t rows, int row_bytes, int box_rows);
+// Rows of 512 bytes that follow one another (tiles of scale bytes), unswizzled: boxes of box_rows rows.
+cudaError_t encode_scale_tiles(CUtensorMap *map, const void *base, int64_t rows, int box_rows);
 // As encode_byte_tiles for 16-bit elements (an inner extent that is not a multiple of 16 bytes is clipped
 // exactly): boxes of 64 elements x box_rows.
 cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld,
