@@ -87,9 +87,22 @@ __device__ __forceinline__ uint32_t mx4_quantize_quad(const uint32_t (&p)[4], ui
     const uint32_t byte = mx4_scale_byte(a);
     const float inv = mx4_inverse_scale(min(byte, 254u));
     float v[8];
-    unpack8<BF16>(p, v);
+    if constexpr (BF16) {
+        // one mixed-precision multiply-add an element (the factor is a power of two that bf16 has);
+        // adding -0 keeps the sign of a zero
+        const unsigned short f = static_cast<unsigned short>(__float_as_uint(inv) >> 16);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= inv;
+        for (int i = 0; i < 4; ++i) {
+            unsigned short lo, hi;
+            asm("mov.b32 {%0, %1}, %2;" : "=h"(lo), "=h"(hi) : "r"(p[i]));
+            asm("fma.rn.f32.bf16 %0, %1, %2, %3;" : "=f"(v[2 * i]) : "h"(lo), "h"(f), "f"(-0.0f));
+            asm("fma.rn.f32.bf16 %0, %1, %2, %3;" : "=f"(v[2 * i + 1]) : "h"(hi), "h"(f), "f"(-0.0f));
+        }
+    } else {
+        unpack8<BF16>(p, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= inv;
+    }
     codes = byte == 255u ? 0u : mx4_pack8(v);
     return byte;
 }

@@ -25,13 +25,15 @@ mx4_quantize_kernel(const uint16_t *__restrict__ W, int64_t n_rows, int64_t n_co
         // this warp's rows: row0, row0 + 32, + 64, + 96 of a tile of 128
         const int in_tile = (group & 3) * 8 + warp;
         const int64_t row0 = int64_t(group >> 2) * kMx4TileRows + in_tile;
+        const int here = static_cast<int>(min(int64_t(4), (n_rows - row0 + 31) / 32));  // of its four rows
         const uint16_t *w = W + row0 * ldw;
         uint8_t *c = codes + row0 * ldc + (col >> 1);
         uint32_t p[4][4], keep[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (row0 + 32 * i < n_rows) {
-                load8<VEC, true>(w + 32 * i * ldw, col, n_cols, p[i]);
+            if (i < here) {
+                load8<VEC, true>(w, col, n_cols, p[i]);
+                w += 32 * ldw;
                 if constexpr (MASK)
                     keep[i] = col < n_cols ? mask[(row0 + 32 * i) * ((n_cols + 31) / 32) + (col >> 5)] >> (col & 31) : 0u;
             } else {
@@ -45,7 +47,8 @@ mx4_quantize_kernel(const uint16_t *__restrict__ W, int64_t n_rows, int64_t n_co
             if constexpr (MASK) zero_pruned(p[i], keep[i]);
             uint32_t word;
             const uint32_t byte = mx4_quantize_quad<BF16>(p[i], word);
-            if (row0 + 32 * i < n_rows && has_codes) *reinterpret_cast<uint32_t *>(c + 32 * i * ldc) = word;
+            if (i < here && has_codes) *reinterpret_cast<uint32_t *>(c) = word;
+            c += 32 * ldc;
             uint32_t t = byte << (8 * ((lane >> 2) & 3));
             t |= __shfl_xor_sync(kFullWarp, t, 4);
             t |= __shfl_xor_sync(kFullWarp, t, 8);
