@@ -7,8 +7,10 @@
 // sum by one multiply-add per output instead of to every weight.
 //
 // Bound by memory: 17/32 byte per weight.  A block of threads owns 128 rows and a slice of the
-// columns; a producer thread keeps kStages x (128 rows x 256 columns) in flight by TMA; eight
-// warps (4 groups of 32 rows x 2 halves of the columns of a stage) convert and multiply.  The
+// columns; a producer thread keeps kStages x (128 rows x 512 columns) in flight by TMA; 16 warps (4
+// groups of 32 rows x 4 quarters of the columns of a stage; 8 with halves for more than 16 tokens)
+// convert and multiply.  (With stages of 256 columns a warp's overhead for a stage was a third of
+// its instructions, and issuing them is what the kernel waits for besides memory.)  The
 // column order inside a 32-column block is free as long as weights and activations agree on it:
 // a lane takes 8 consecutive columns, so a weight operand is one 4-byte word of codes (four
 // conversions) and an activation operand is one 16-byte load.  With few rows the columns are cut
@@ -26,10 +28,11 @@ namespace sp {
 
 namespace {
 
-constexpr int kStages = 4;
-constexpr int kCodeBytes = kMx4TileRows * 128;  // codes of a stage: 128 rows x 256 columns
+constexpr int kStages = 3;
+constexpr int kStageTiles = 4;                    // scale tiles of a stage: 512 columns
+constexpr int kBoxBytes = kMx4TileRows * 128;    // codes of 128 rows x 256 columns
+constexpr int kCodeBytes = 2 * kBoxBytes;
 constexpr int kPartPitch = 132;                 // floats between columns of a block's partial sums
-constexpr int kWarps = 8;
 
 struct StreamArgs {
     const uint16_t *X;
@@ -38,7 +41,7 @@ struct StreamArgs {
     uint16_t *Y;
     int64_t ldy;
     int tile_cols;     // scale tiles along a row
-    int stages;        // 256-column stages of a row
+    int stages;        // 512-column stages of a row
     int chunk_stages;  // stages whose activations are in shared memory at a time
     int quantize_x;
     int vec_x;
@@ -59,18 +62,14 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <int WARPS>
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
 
 // One (token, 256 columns) of the activations -> binary16 in shared memory and its scale;
 // returns whether a remainder is left (bf16).  pass 1 stores the remainders.
 template <bool BF16>
-__device__ __forceinline__ bool convert_x(const StreamArgs &a, int64_t token, int64_t col, int lane,
-                                          int pass, __half *dst, float *scale_out) {
-    uint32_t p[4] = {0u, 0u, 0u, 0u};
-    if (token < a.n_tokens) {
-        if (a.vec_x) load8<true, false>(a.X + token * a.ldx, col, a.n_cols, p);
-        else load8<false, false>(a.X + token * a.ldx, col, a.n_cols, p);
-    }
+__device__ __forceinline__ bool convert_x(const StreamArgs &a, const uint32_t (&p)[4], int lane, int pass,
+                                          __half *dst, float *scale_out) {
     float v[8];
     if (a.quantize_x) {
         uint32_t word, h[4];
@@ -124,18 +123,22 @@ __device__ __forceinline__ bool convert_x(const StreamArgs &a, int64_t token, in
 }  // namespace
 
 template <bool BF16, int NT>
-__global__ void __launch_bounds__(kWarps * 32 + 32)
+constexpr int stream_warps() { return NT <= 2 ? 16 : 8; }
+
+template <bool BF16, int NT>
+__global__ void __launch_bounds__(stream_warps<BF16, NT>() * 32 + 32)
 mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kStages], empty[kStages];
     __shared__ uint32_t failed, has_rest;
-    constexpr int kTokens = NT * 8;
+    constexpr int kTokens = NT * 8, kWarps = stream_warps<BF16, NT>();
+    constexpr int kParts = kWarps / 4, kTiles = kStageTiles / kParts;  // of a stage's columns; scale tiles in each
     uint8_t *const code_smem = smem;
     uint8_t *const scale_smem = smem + kStages * kCodeBytes;
-    const int x_pitch = a.chunk_stages * 512 + 64;              // bytes; 64 mod 128: no conflicts
-    uint8_t *const x_smem = scale_smem + kStages * 2 * kMx4TileBytes;
+    const int x_pitch = a.chunk_stages * 1024 + 64;              // bytes; 64 mod 128: no conflicts
+    uint8_t *const x_smem = scale_smem + kStages * kStageTiles * kMx4TileBytes;
     float *const xs_smem = reinterpret_cast<float *>(x_smem + kTokens * x_pitch);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const int slices = gridDim.y, slice = blockIdx.y;
     const int64_t row0 = int64_t(blockIdx.x) * kMx4TileRows;
     const int first = static_cast<int>(int64_t(a.stages) * slice / slices);
@@ -150,6 +153,11 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
         failed = has_rest = 0u;
         mbar_fence_init();
     }
+    // tokens that do not exist: zeros
+    for (int at = static_cast<int>(a.n_tokens) * x_pitch + threadIdx.x * 16; at < kTokens * x_pitch; at += (kWarps * 32 + 32) * 16)
+        *reinterpret_cast<uint4 *>(x_smem + at) = make_uint4(0u, 0u, 0u, 0u);
+    for (int at = threadIdx.x; at < a.chunk_stages * 2 * kTokens; at += kWarps * 32 + 32)
+        if (at % kTokens >= a.n_tokens) xs_smem[at] = 0.0f;
     __syncthreads();
     pdl_launch_dependents();
     pdl_wait();
@@ -167,41 +175,62 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
     int step = 0;  // stages issued (producer) or taken (consumers), over both passes
     for (int pass = 0; pass < 2; ++pass) {
         if (warp == kWarps) {
-            if (lane == 0) {
-                for (int s = first; s < last; ++s, ++step) {
-                    const int slot = step % kStages;
-                    if (step >= kStages && !mbar_wait_or_fail(smem_addr(&empty[slot]), ((step / kStages) - 1) & 1, &failed)) break;
-                    const int tiles = min(2, a.tile_cols - 2 * s);
-                    const uint32_t bar = smem_addr(&full[slot]);
-                    mbar_expect_tx(bar, kCodeBytes + tiles * kMx4TileBytes);
-                    tma_load_2d(smem_addr(code_smem + slot * kCodeBytes), &codes_map, s * 128,
-                                static_cast<int>(row0), bar);
-                    bulk_load(smem_addr(scale_smem + slot * 2 * kMx4TileBytes),
-                              a.scales + (int64_t(blockIdx.x) * a.tile_cols + 2 * s) * kMx4TileBytes,
+            for (int s = first; s < last; ++s, ++step) {
+                const int slot = step % kStages;
+                bool ok = true;
+                if (step >= kStages) ok = mbar_wait_or_fail(smem_addr(&empty[slot]), ((step / kStages) - 1) & 1, &failed);
+                if (!__all_sync(kFullWarp, ok)) break;
+                if (elect_one()) {
+                    const int tiles = min(kStageTiles, a.tile_cols - kStageTiles * s);
+                    const uint32_t bar = smem_addr(&full[slot]), to = smem_addr(code_smem + slot * kCodeBytes);
+                    mbar_expect_tx(bar, (tiles > 2 ? kCodeBytes : kBoxBytes) + tiles * kMx4TileBytes);
+                    tma_load_2d(to, &codes_map, s * 256, static_cast<int>(row0), bar);
+                    if (tiles > 2) tma_load_2d(to + kBoxBytes, &codes_map, s * 256 + 128, static_cast<int>(row0), bar);
+                    bulk_load(smem_addr(scale_smem + slot * kStageTiles * kMx4TileBytes),
+                              a.scales + (int64_t(blockIdx.x) * a.tile_cols + kStageTiles * s) * kMx4TileBytes,
                               tiles * kMx4TileBytes, bar);
                 }
+                __syncwarp();
             }
-            __syncwarp();
         } else {
             for (int c0 = first; c0 < last; c0 += a.chunk_stages) {
                 const int c1 = min(c0 + a.chunk_stages, last);
-                if (c0 != first || pass != 0) consumer_sync();  // everyone is done with the last chunk
+                if (c0 != first || pass != 0) consumer_sync<kWarps>();  // everyone is done with the last chunk
+                // (token, 256 columns) pairs over the warps, four loads on their way at a time
+                const int cs = 2 * (c1 - c0), pairs = cs * static_cast<int>(a.n_tokens);
                 bool rest = false;
-                for (int u = warp; u < (c1 - c0) * kTokens; u += kWarps) {
-                    const int s = u / kTokens, token = u % kTokens;
-                    rest |= convert_x<BF16>(a, token, int64_t(c0 + s) * 256 + lane * 8, lane, pass,
-                                            reinterpret_cast<__half *>(x_smem + token * x_pitch + s * 512),
-                                            xs_smem + u);
+                for (int u0 = warp; u0 < pairs; u0 += 4 * kWarps) {
+                    uint32_t p[4][4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = u0 + i * kWarps, token = u / cs, s = u - token * cs;
+                        if (u < pairs) {
+                            const uint16_t *x = a.X + token * a.ldx;
+                            const int64_t col = int64_t(2 * c0 + s) * 256 + lane * 8;
+                            if (a.vec_x) load8<true, false>(x, col, a.n_cols, p[i]);
+                            else load8<false, false>(x, col, a.n_cols, p[i]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = u0 + i * kWarps, token = u / cs, s = u - token * cs;
+                        if (u < pairs)
+                            rest |= convert_x<BF16>(a, p[i], lane, pass, reinterpret_cast<__half *>(x_smem + token * x_pitch + s * 512),
+                                                    xs_smem + s * kTokens + token);
+                    }
                 }
                 if (rest) has_rest = 1u;
-                consumer_sync();
+                consumer_sync<kWarps>();
                 for (int s = c0; s < c1; ++s, ++step) {
                     const int slot = step % kStages;
                     mbar_wait_or_fail(smem_addr(&full[slot]), (step / kStages) & 1, &failed);
-                    if (2 * s + wk < a.tile_cols) {
-                        const uint32_t codes = smem_addr(code_smem + slot * kCodeBytes) + (wr * 32 + g) * 128 + t * 4;
-                        const uint32_t sc = smem_addr(scale_smem + (slot * 2 + wk) * kMx4TileBytes) + g * 16 + wr * 4;
-                        const uint32_t xa = smem_addr(x_smem) + g * x_pitch + (s - c0) * 512 + wk * 256 + t * 16;
+#pragma unroll
+                    for (int part = 0; part < kTiles; ++part) {
+                        const int tile = wk * kTiles + part;  // of the stage
+                        if (kStageTiles * s + tile >= a.tile_cols) break;
+                        const uint32_t codes = smem_addr(code_smem + slot * kCodeBytes + (tile >> 1) * kBoxBytes) + (wr * 32 + g) * 128 + t * 4;
+                        const uint32_t sc = smem_addr(scale_smem + (slot * kStageTiles + tile) * kMx4TileBytes) + g * 16 + wr * 4;
+                        const uint32_t xa = smem_addr(x_smem) + g * x_pitch + (s - c0) * 1024 + tile * 256 + t * 16;
                         uint32_t scale_word[4];  // rows g, g+8, g+16, g+24 of the warp's 32
 #pragma unroll
                         for (int j = 0; j < 4; ++j) scale_word[j] = lds32(sc + j * 128);
@@ -211,8 +240,8 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                             uint4 x[NT];
 #pragma unroll
                             for (int n = 0; n < NT; ++n) x[n] = lds128(xa + n * 8 * x_pitch + b * 64);
-                            // chunk of row r in the swizzled stage: block ^ (r & 7); all rows here have r & 7 == g
-                            const uint32_t at = codes + (((wk * 4 + b) ^ g) << 4);
+                            // chunk of row r in the swizzled box: block ^ (r & 7); all rows here have r & 7 == g
+                            const uint32_t at = codes + ((((tile & 1) * 4 + b) ^ g) << 4);
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
                                 uint32_t lo[4], hi[4];
@@ -237,7 +266,8 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                         }
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const float2 xs = *reinterpret_cast<const float2 *>(xs_smem + (s - c0) * kTokens + n * 8 + 2 * t);
+                            const float2 xs = *reinterpret_cast<const float2 *>(
+                                xs_smem + (2 * (s - c0) + (tile >> 1)) * kTokens + n * 8 + 2 * t);
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
                                 acc[m][n][0] = fmaf(xs.x, st[m][n][0], acc[m][n][0]);
@@ -260,11 +290,12 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
             for (int s = max(0, step - kStages); s < step; ++s) mbar_wait(smem_addr(&full[s % kStages]), (s / kStages) & 1);
     }
 
-    // the two column halves meet in shared memory (the stages are free: all copies have arrived)
+    // the column parts meet in shared memory (the stages are free: all copies have arrived)
     float *const part = reinterpret_cast<float *>(smem);
-    float *const mine = part + (2 * t) * kPartPitch + wr * 32 + g;
+    constexpr int kPartFloats = kTokens * kPartPitch;
     if (failed != 0u) __syncthreads();
-    if (warp < kWarps && wk == 1) {
+    if (warp < kWarps) {
+        float *const mine = part + wk * kPartFloats + (2 * t) * kPartPitch + wr * 32 + g;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -274,36 +305,34 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                     mine[(n * 8 + (i & 1)) * kPartPitch + m * 16 + (i >> 1) * 8] = acc[m][n][i];
     }
     __syncthreads();
-    if (warp < kWarps && wk == 0) {
+    for (int at = threadIdx.x; at < static_cast<int>(a.n_tokens) * 128; at += kWarps * 32 + 32) {
+        float *p = part + (at >> 7) * kPartPitch + (at & 127);
+        float sum = p[0];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    mine[(n * 8 + (i & 1)) * kPartPitch + m * 16 + (i >> 1) * 8] += acc[m][n][i];
+        for (int k = 1; k < kParts; ++k) sum += p[k * kPartFloats];
+        p[0] = sum;
     }
     if (slices > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        cluster_sync();
     } else {
         __syncthreads();
     }
     // (token, row) pairs over the threads of the cluster's blocks; ranks are summed in order
     const int row = threadIdx.x & 127;
     if (warp < kWarps && row0 + row < a.n_rows) {
-        for (int token = slice * 2 + (threadIdx.x >> 7); token < min(int64_t(kTokens), a.n_tokens); token += 2 * slices) {
-            const uint32_t at = smem_addr(part + token * kPartPitch + row);
+        for (int token = slice * kParts + (threadIdx.x >> 7); token < a.n_tokens; token += kParts * slices) {
             float sum = 0.0f;
-            for (int r = 0; r < slices; ++r) {
-                float v;
-                if (slices > 1) {
-                    uint32_t remote;
-                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(r));
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
-                } else {
-                    v = part[token * kPartPitch + row];
-                }
-                sum += v;
+            if (slices > 1) {
+                float v[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)  // all on their way before the first is used
+                    if (r < slices)
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(remote_address(part + token * kPartPitch + row, r)));
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < slices) sum += v[r];
+            } else {
+                sum = part[token * kPartPitch + row];
             }
             uint16_t bits;
             if constexpr (BF16) bits = __bfloat16_as_ushort(__float2bfloat16_rn(sum));
@@ -311,20 +340,19 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
             a.Y[token * a.ldy + row0 + row] = bits;
         }
     }
-    if (slices > 1)
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (slices > 1) cluster_sync();  // no block leaves while its sums are read
 }
 
 template <bool BF16, int NT>
 static sp_status launch_tile(const CUtensorMap &map, StreamArgs a, cudaStream_t stream) {
     const int row_tiles = static_cast<int>(mx4_tile_rows(a.n_rows));
-    // enough blocks for every SM; a slice has two stages at least
+    // blocks for the SMs in one round
     int slices = 1;
-    while (slices < 8 && row_tiles * slices < 128 && a.stages >= 4 * slices) slices *= 2;
+    while (slices < 8 && row_tiles * slices <= 74 && a.stages >= 2 * slices) slices *= 2;
     const int per_slice = (a.stages + slices - 1) / slices;
-    a.chunk_stages = min(per_slice, 16 / NT);
-    const size_t smem = kStages * (kCodeBytes + 2 * kMx4TileBytes) +
-                        NT * 8 * (a.chunk_stages * 512 + 64 + a.chunk_stages * 4);
+    a.chunk_stages = min(per_slice, 8 / NT);
+    const size_t smem = kStages * (kCodeBytes + kStageTiles * kMx4TileBytes) +
+                        NT * 8 * (a.chunk_stages * 1024 + 64 + a.chunk_stages * 8);
     auto *kernel = mx4_stream_kernel<BF16, NT>;
     static DynamicSmem limit;
     cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
@@ -338,7 +366,7 @@ static sp_status launch_tile(const CUtensorMap &map, StreamArgs a, cudaStream_t 
     attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(row_tiles, slices);
-    cfg.blockDim = dim3(kWarps * 32 + 32);
+    cfg.blockDim = dim3(stream_warps<BF16, NT>() * 32 + 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
@@ -359,7 +387,7 @@ sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
     a.scales = p.scales;
     a.ldy = p.ldy;
     a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
-    a.stages = (a.tile_cols + 1) / 2;
+    a.stages = (a.tile_cols + kStageTiles - 1) / kStageTiles;
     a.quantize_x = p.quantize_x;
     a.vec_x = aligned16(p.X) && p.ldx % 8 == 0 && p.n_cols % 8 == 0;
     for (int64_t t0 = 0; t0 < p.n_tokens; t0 += 32) {

@@ -6,18 +6,6 @@
 
 namespace sp {
 
-// The tensor cores are driven by one thread, but the warp walks the loop together and elects it
-// only for the instructions themselves: operands then stay in uniform registers.  Driven from a
-// branch on the lane index, a stage took 1400 cycles of one thread's latencies against 512 of
-// products (128 x 256 x 256 columns in 4 bits).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one != 0u;
-}
-// The warp's index, known to the compiler to be the same in all lanes.
-__device__ __forceinline__ int uniform_warp() { return __shfl_sync(kFullWarp, static_cast<int>(threadIdx.x >> 5), 0); }
-
 // ---- tensor memory (512 columns of 128 lanes x 32 bits on an SM)
 
 // One warp allocates; the base address lands in shared memory.  columns: a power of two >= 32.

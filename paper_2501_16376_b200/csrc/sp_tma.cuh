@@ -61,6 +61,18 @@ __device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity,
     return false;
 }
 
+// Asynchronous copies and the tensor cores are driven by one thread, but the warp walks the loop
+// together and elects it only for the instructions themselves: operands then stay in uniform
+// registers.  Driven from a branch on the lane index, a stage of products took 1400 cycles of one
+// thread's latencies against 512 of products (128 x 256 x 256 columns in 4 bits).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0u;
+}
+// The warp's index, known to the compiler to be the same in all lanes.
+__device__ __forceinline__ int uniform_warp() { return __shfl_sync(kFullWarp, static_cast<int>(threadIdx.x >> 5), 0); }
+
 // Place in a ring of stages: the slot, and the parity of the barrier phase that its current use completes.
 template <int SLOTS>
 struct RingPlace {
