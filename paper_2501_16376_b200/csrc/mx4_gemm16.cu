@@ -45,6 +45,7 @@ struct Gemm16Args {
     int steps;        // 128-column stages
     int tile_tokens;  // tokens of a tile, a multiple of 16
     int row_tiles, tiles;
+    int slices;       // blocks of a cluster that share a tile, each with a part of the columns
 };
 
 // 2^e as binary16 bits, 0 below its range.
@@ -85,6 +86,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     __shared__ uint32_t tmem_base, failed;
     __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
+    float *const part = reinterpret_cast<float *>(smem);  // of a shared tile, [token][row], when the slots are done with
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
@@ -113,23 +115,27 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     const uint32_t tmem = tmem_base;
     pdl_launch_dependents();
     pdl_wait();
-    const int code_steps = (a.steps + 1) / 2;
+    // With few tiles a cluster shares each: its blocks take a part of the columns and add their sums
+    // up at the end.
+    const int slices = a.slices, rank = blockIdx.x % slices, unit = blockIdx.x / slices, units = gridDim.x / slices;
+    const int code_begin = (a.steps + 1) / 2 * rank / slices, code_steps = (a.steps + 1) / 2 * (rank + 1) / slices - code_begin;
+    const int first_step = 2 * code_begin, steps = min(2 * code_steps, a.steps - first_step);
 
     if (warp == 0) {
         RingPlace<kSlots> at;
         int step = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
+        for (int tile = unit; ok && tile < a.tiles; tile += units) {
             const int n = tile / a.row_tiles;
-            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+            for (int k = 0; k < steps; ++k, ++step, at.next()) {
                 if (step >= kSlots) ok = mbar_wait_or_fail(smem_addr(&empty[at.slot]), at.parity ^ 1u, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 if (elect_one()) {
                     const uint32_t bar = smem_addr(&full[at.slot]);
                     const uint32_t to = smem_addr(slots + at.slot * kSlotBytes);
                     mbar_expect_tx(bar, a.tile_tokens * 256);
-                    tma_load_2d(to, &x_map, k * 256, n * a.tile_tokens, bar);
-                    tma_load_2d(to + kHalfBytes, &x_map, k * 256 + 128, n * a.tile_tokens, bar);
+                    tma_load_2d(to, &x_map, (first_step + k) * 256, n * a.tile_tokens, bar);
+                    tma_load_2d(to + kHalfBytes, &x_map, (first_step + k) * 256 + 128, n * a.tile_tokens, bar);
                 }
                 __syncwarp();
             }
@@ -142,10 +148,10 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         RingPlace<kCodeSlots> at;
         int step = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
+        for (int tile = unit; ok && tile < a.tiles; tile += units) {
             const int m = tile % a.row_tiles;
             const uint8_t *sw = a.scales + int64_t(m) * a.tile_cols * kMx4TileBytes;
-            for (int k = 0; k < code_steps; ++k, ++step, at.next()) {
+            for (int k = code_begin; k < code_begin + code_steps; ++k, ++step, at.next()) {
                 if (step >= kCodeSlots) ok = mbar_wait_or_fail(smem_addr(&code_empty[at.slot]), at.parity ^ 1u, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 if (elect_one()) {
@@ -166,11 +172,11 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         RingPlace<kSlots> at;
         int count = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count) {
+        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count) {
             if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             const uint32_t acc = tmem + (count & 1) * kMostTokens;
-            for (int k = 0; k < a.steps; ++k, at.next()) {
+            for (int k = 0; k < steps; ++k, at.next()) {
                 ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 tcgen05_fence_after();
@@ -181,7 +187,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                     for (int p = 0; p < 8; ++p)
                         mma_16bit(acc, ta + p * 8, db + (p >> 2) * (kHalfBytes / 16) + (p & 3) * 2, instruction, k > 0 || p > 0);
                     tcgen05_commit(smem_addr(&empty[at.slot]));
-                    if (k == a.steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+                    if (k == steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
                 }
                 __syncwarp();
             }
@@ -199,17 +205,17 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         int step = 0, code0 = 0, count = 0;  // stages before this tile's first
         uint32_t uses = 0;                   // of the group's slot
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++count, step += a.steps, code0 += code_steps) {
+        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count, step += steps, code0 += code_steps) {
             // the first stage of this tile that is the group's
             int k = (slot + kSlots - step % kSlots) % kSlots, top = 0;
             if constexpr (!BF16) {
-                if (k < a.steps) {
+                if (k < steps) {
                     ok = mbar_wait_or_fail(smem_addr(&top_full[count & 1]), (count >> 1) & 1, &failed);
                     if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                     top = row_top[count & 3][row];
                 }
             }
-            for (; k < a.steps; k += kSlots, ++uses) {
+            for (; k < steps; k += kSlots, ++uses) {
                 const int sub = k & 1, code_step = code0 + (k >> 1), code_slot = code_step % kCodeSlots;
                 ok = mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
@@ -219,7 +225,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
 #pragma unroll
                 for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 4 + b) ^ swap) << 4));
                 __syncwarp();  // the codes are in registers
-                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == a.steps - 1 ? 2 - sub : 1);
+                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == steps - 1 ? 2 - sub : 1);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t v[32];
@@ -267,10 +273,10 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
             row_top[c & 3][quarter * 32 + lane] = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
             mbar_arrive(smem_addr(&top_full[c & 1]));
         };
-        if (!BF16 && blockIdx.x < a.tiles) find_top(blockIdx.x, 0);
-        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++count) {
+        if (!BF16 && unit < a.tiles) find_top(unit, 0);
+        for (int tile = unit; tile < a.tiles; tile += units, ++count) {
             const int m = tile % a.row_tiles, n = tile / a.row_tiles;
-            if (!BF16 && tile + int(gridDim.x) < a.tiles) find_top(tile + gridDim.x, count + 1);
+            if (!BF16 && tile + units < a.tiles) find_top(tile + units, count + 1);
             const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
@@ -291,7 +297,11 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 uint32_t v[32];
                 tmem_load32(acc + c, v);
                 tmem_load_wait();
-                if (row < a.n_rows) {
+                if (slices > 1) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (c + j < tokens) part[(c + j) * kMx4TileRows + quarter * 32 + lane] = __uint_as_float(v[j]);
+                } else if (row < a.n_rows) {
                     uint16_t *y = a.Y + (token0 + c) * a.ldy + row;
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
@@ -310,6 +320,35 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     if (warp == 2) {
         tcgen05_fence_after();
         tmem_free(tmem, kTmemColumns);
+    }
+    if (slices > 1) {
+        cluster_sync();
+        const int r = threadIdx.x & 127;
+        const int64_t row = int64_t(unit % a.row_tiles) * kMx4TileRows + r, token0 = int64_t(unit / a.row_tiles) * a.tile_tokens;
+        const int tokens = static_cast<int>(min(int64_t(a.tile_tokens), a.n_tokens - token0));
+        float f0 = 1.0f, f1 = 1.0f;
+        if constexpr (!BF16) {
+            const int e = row_top[0][r] - 140;
+            f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
+            f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
+        }
+        if (row < a.n_rows) {
+            constexpr int kGroups = kThreads / 128;
+            for (int c = rank * kGroups + (threadIdx.x >> 7); c < tokens; c += slices * kGroups) {
+                float v[8], sum = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)  // all on their way before the first is used; added in rank order
+                    if (k < slices)
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[k]) : "r"(remote_address(part + c * kMx4TileRows + r, k)));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < slices) sum += v[k];
+                const float x = sum * f0 * f1;
+                if constexpr (BF16) a.Y[(token0 + c) * a.ldy + row] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+                else a.Y[(token0 + c) * a.ldy + row] = __half_as_ushort(__float2half_rn(x));
+            }
+        }
+        cluster_sync();  // no block leaves while its sums are read
     }
 }
 
@@ -379,7 +418,10 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     e = encode_byte_tiles(&x_map, X, p.n_tokens, p.n_cols * 2, ldx * 2, a.tile_tokens);
     if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
     if (e != cudaSuccess) return cuda_fail(e);
-    PdlConfig pdl(dim3(static_cast<unsigned>(std::min(a.tiles, sms))), dim3(kThreads), stream);
+    a.slices = 1;
+    while (a.slices < 8 && a.tiles * a.slices * 2 <= sms && a.steps >= 8 * a.slices) a.slices *= 2;
+    ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(a.slices > 1 ? a.tiles * a.slices : std::min(a.tiles, sms))),
+                         dim3(kThreads), stream);
     pdl.cfg.dynamicSmemBytes = kSlots * kSlotBytes + kCodeSlots * kCodeSlotBytes;
     if (p.dtype == SP_BF16) {
         static DynamicSmem limit;
