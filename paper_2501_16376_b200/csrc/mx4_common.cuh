@@ -20,6 +20,13 @@ __host__ __device__ inline int64_t mx4_blocks(int64_t n_cols) { return (n_cols +
 __host__ __device__ inline int64_t mx4_tile_cols(int64_t n_cols) { return (n_cols + 127) / 128; }
 __host__ __device__ inline int64_t mx4_tile_rows(int64_t n_rows) { return (n_rows + 127) / 128; }
 
+// Whether `tiles` clusters of `slices` blocks, an SM each, run in one round.  Clusters lie within a
+// group of SMs (16 to 18 of them here), so that 8 blocks leave room unused: 16 clusters of 8 took
+// two rounds.
+inline bool cluster_slices_fit(int64_t tiles, int slices, int sms) {
+    return tiles * slices <= (slices > 4 ? 64 : sms);
+}
+
 // Scale byte of a block whose largest magnitude is `amax` (the bits of a non-negative binary32
 // number): the exponent of amax less 2, the exponent of the largest code, so that amax / scale
 // lies in [4, 8); at least 0 (the smallest scale), 255 for a block that is not finite.

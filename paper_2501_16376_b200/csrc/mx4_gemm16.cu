@@ -82,9 +82,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Gemm16Args a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots];
-    __shared__ uint64_t acc_full[2], acc_free, top_full[2], drained;
+    __shared__ uint64_t acc_full[2], acc_free, top_full[8], drained;
     __shared__ uint32_t tmem_base, failed;
-    __shared__ int row_top[4][kMx4TileRows];  // largest scale byte of a row, for four tiles in turn
+    // Largest scale byte of a row, for eight tiles in turn.  A group may have no stage of a tile and
+    // then does not look at it; it has one within three tiles, and the tile after the next is the last
+    // that is published before it is converted, so no barrier is two phases ahead of a group.
+    __shared__ int row_top[8][kMx4TileRows];
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
     float *const part = reinterpret_cast<float *>(smem);  // of a shared tile, [token][row], when the slots are done with
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
@@ -97,13 +100,12 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         }
         for (int s = 0; s < kCodeSlots; ++s) {
             mbar_init(smem_addr(&code_full[s]), 1);
-            mbar_init(smem_addr(&code_empty[s]), 8);  // four warps for each of two stages of 128 columns
+            mbar_init(smem_addr(&code_empty[s]), 4 * kSlots);  // every converting warp
         }
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
         mbar_init(smem_addr(&acc_free), 128);
-        mbar_init(smem_addr(&top_full[0]), 128);
-        mbar_init(smem_addr(&top_full[1]), 128);
+        for (int i = 0; i < 8; ++i) mbar_init(smem_addr(&top_full[i]), 128);
         mbar_init(smem_addr(&drained), 1);
         failed = 0u;
         mbar_fence_init();
@@ -202,30 +204,36 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         const int slot = (warp - 8) >> 2, row = threadIdx.x & 127, swap = row & 7;
         const uint32_t scale_at = (row & 31) * 16 + (row >> 5) * 4;
         const uint32_t to = tmem + kWeightColumns + slot * 64 + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        int step = 0, code0 = 0, count = 0;  // stages before this tile's first
+        RingPlace<kCodeSlots> code_at;
+        int turn = slot, count = 0;          // stages until the group's next
         uint32_t uses = 0;                   // of the group's slot
         bool ok = true;
-        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count, step += steps, code0 += code_steps) {
-            // the first stage of this tile that is the group's
-            int k = (slot + kSlots - step % kSlots) % kSlots, top = 0;
-            if constexpr (!BF16) {
-                if (k < steps) {
-                    ok = mbar_wait_or_fail(smem_addr(&top_full[count & 1]), (count >> 1) & 1, &failed);
-                    if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
-                    top = row_top[count & 3][row];
-                }
-            }
-            for (; k < steps; k += kSlots, ++uses) {
-                const int sub = k & 1, code_step = code0 + (k >> 1), code_slot = code_step % kCodeSlots;
-                ok = mbar_wait_or_fail(smem_addr(&code_full[code_slot]), (code_step / kCodeSlots) & 1, &failed);
+        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count) {
+            int top = 0;
+            if (!BF16 && turn < steps) {
+                ok = mbar_wait_or_fail(smem_addr(&top_full[count & 7]), (count >> 3) & 1, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
-                const uint8_t *in = codes + code_slot * kCodeSlotBytes;
+                top = row_top[count & 7][row];
+            }
+            // every group follows every stage of codes (a barrier that it passed over might be taken
+            // for a later phase), and converts at most one half of it
+            for (int c = 0; c < code_steps; ++c, code_at.next()) {
+                ok = mbar_wait_or_fail(smem_addr(&code_full[code_at.slot]), code_at.parity, &failed);
+                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
+                const int here = min(2, steps - 2 * c), sub = turn;
+                if (sub >= here) {
+                    turn -= here;
+                    if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_at.slot]));
+                    continue;
+                }
+                turn += kSlots - here;
+                const uint8_t *in = codes + code_at.slot * kCodeSlotBytes;
                 const uint32_t bytes = *reinterpret_cast<const uint32_t *>(in + kMx4TileRows * 128 + sub * kMx4TileBytes + scale_at);
                 uint4 w[4];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint4 *>(in + row * 128 + (((sub * 4 + b) ^ swap) << 4));
                 __syncwarp();  // the codes are in registers
-                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_slot]), k == steps - 1 ? 2 - sub : 1);
+                if (lane == 0) mbar_arrive(smem_addr(&code_empty[code_at.slot]));
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t v[32];
@@ -254,6 +262,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&full[slot]));
+                ++uses;
             }
         }
     } else if (warp >= 4) {
@@ -270,8 +279,8 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 most = __vmaxu4(most, w);
             }
             most = __vmaxu4(most, most >> 16);
-            row_top[c & 3][quarter * 32 + lane] = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
-            mbar_arrive(smem_addr(&top_full[c & 1]));
+            row_top[c & 7][quarter * 32 + lane] = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
+            mbar_arrive(smem_addr(&top_full[c & 7]));
         };
         if (!BF16 && unit < a.tiles) find_top(unit, 0);
         for (int tile = unit; tile < a.tiles; tile += units, ++count) {
@@ -286,7 +295,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
             const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
             float f0 = 1.0f, f1 = 1.0f;
             if constexpr (!BF16) {
-                const int e = row_top[count & 3][quarter * 32 + lane] - 140;
+                const int e = row_top[count & 7][quarter * 32 + lane] - 140;
                 f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
                 f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
             }
@@ -419,7 +428,7 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
     if (e != cudaSuccess) return cuda_fail(e);
     a.slices = 1;
-    while (a.slices < 8 && a.tiles * a.slices * 2 <= sms && a.steps >= 8 * a.slices) a.slices *= 2;
+    while (a.slices < 8 && cluster_slices_fit(a.tiles, a.slices * 2, sms) && a.steps >= 8 * a.slices) a.slices *= 2;
     ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(a.slices > 1 ? a.tiles * a.slices : std::min(a.tiles, sms))),
                          dim3(kThreads), stream);
     pdl.cfg.dynamicSmemBytes = kSlots * kSlotBytes + kCodeSlots * kCodeSlotBytes;

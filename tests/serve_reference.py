@@ -44,9 +44,8 @@ def mx4_pack(code, byte):
     codes = (pairs[..., 0] | (pairs[..., 1] << 4)).astype(np.uint8)
     kt = (nb + 3) // 4
     scales = np.zeros((rows + 127) // 128 * kt * 512, dtype=np.uint8)
-    for r in range(rows):
-        for b in range(nb):
-            scales[(r // 128 * kt + b // 4) * 512 + r % 32 * 16 + r // 32 % 4 * 4 + b % 4] = byte[r, b]
+    r, b = np.arange(rows)[:, None], np.arange(nb)[None]
+    scales[(r // 128 * kt + b // 4) * 512 + r % 32 * 16 + r // 32 % 4 * 4 + b % 4] = byte
     return codes, scales
 
 

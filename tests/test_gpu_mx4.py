@@ -127,6 +127,16 @@ def test_product_of_odd_sizes(sp, rows, cols, T, dtype, mode):
 
 
 @pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("rows,cols,T", [(10000, 130, 140), (15000, 96, 150), (20000, 96, 20), (25000, 96, 20), (30000, 96, 9),
+                                         (40000, 130, 20), (40000, 96, 140), (40000, 96, 400), (20000, 1100, 40), (19000, 1100, 260)])
+def test_product_of_many_rows(sp, rows, cols, T, mode):
+    # tiles of every height, several of them for a block, in both tile kernels
+    codes, scales, V = ref.mx4_random(rows, cols, rows + cols)
+    X = torch.randn(T, cols, generator=torch.Generator().manual_seed(T)).to(torch.bfloat16 if T % 20 else torch.float16)
+    _check_product(sp, X, codes, scales, V, mode)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
 @pytest.mark.parametrize("T", [1, 12, 150])
 def test_product_of_strided_tensors_on_another_stream(sp, T, mode):
     rows, cols, dtype = 200, 520, torch.bfloat16
