@@ -62,9 +62,11 @@ cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 
 constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens of a 4-bit product
 
-// Whether a product takes the kernels that tile over tokens: from 33 tokens on, where streaming
-// the weights past registers would take a second pass.
-static bool takes_tiles(int64_t n_tokens) { return n_tokens > 32; }
+// Whether a product takes the kernels that tile over tokens: from 9 tokens on, the columns of one
+// mma of the streaming kernel.  (At 8 tokens it is ahead, bf16 activations: 7.2 us against 9.5 for
+// 4096 x 4096, 14.8 against 18.1 for 4096 x 14336; with two such columns, at 16 tokens, it took 9.3
+// against 9.6 and 22.8 against 18.3.)
+static bool takes_tiles(int64_t n_tokens) { return n_tokens > 8; }
 
 static sp_status check_codes(const void *codes, int64_t ldc, const void *scales, int64_t n_cols) {
     if (codes == nullptr || scales == nullptr) return SP_ERR_INVALID_ARG;

@@ -34,6 +34,7 @@ struct GemmArgs {
     int tile_cols;  // scale tiles along the columns
     int steps;      // 256-column stages
     int token_tiles, tiles;
+    int slices;     // blocks of a cluster that share a tile, each with a part of the columns (not pairs)
     int tma_y;
 };
 
@@ -57,9 +58,14 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_free, drained;
     __shared__ uint32_t tmem_base, failed;
+    constexpr int kPartPitch = N + 4;  // floats; rows 16 bytes apart in the banks
+    float *const part = reinterpret_cast<float *>(smem);  // of a shared tile, [token][row], when the operands are done with
     uint8_t *const operands = smem, *const out_stage = smem + STAGES * kOperandBytes, *const scales = out_stage + 4 * kOutBytes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
-    const int rank = PAIR ? blockIdx.x & 1 : 0, unit = blockIdx.x / kBlocks, units = gridDim.x / kBlocks;
+    const int slices = PAIR ? 1 : a.slices, slice = blockIdx.x % slices;
+    const int rank = PAIR ? blockIdx.x & 1 : 0, unit = blockIdx.x / (kBlocks * slices), units = gridDim.x / (kBlocks * slices);
+    const int first_step = static_cast<int>(int64_t(a.steps) * slice / slices);
+    const int steps = static_cast<int>(int64_t(a.steps) * (slice + 1) / slices) - first_step;
     if (threadIdx.x == 0) {
         tma_prefetch_map(&x_map);
         tma_prefetch_map(&w_map);
@@ -93,7 +99,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             const int w_tiles = static_cast<int>(min(int64_t(kScaleTilesB), mx4_tile_rows(a.n_rows) - wt));
             const uint8_t *sx = a.scale_x + int64_t(m) * a.tile_cols * kMx4TileBytes;
             const uint8_t *sw = a.scale_w + wt * a.tile_cols * kMx4TileBytes;
-            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+            for (int k = first_step; k < first_step + steps; ++k, ++step, at.next()) {
                 if (step >= STAGES) ok = mbar_wait_or_fail(smem_addr(&empty[at.slot]), at.parity ^ 1u, &failed);
                 if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
                 if (elect_one()) {
@@ -136,7 +142,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             const uint32_t acc = tmem + (count & 1) * kSecond;
             // a tile of 64 or 192 rows may begin in the middle of a tile of scales
             const uint32_t skip = (n * N % kMx4TileRows) / 32;
-            for (int k = 0; k < a.steps; ++k, ++step, at.next()) {
+            for (int k = first_step; k < first_step + steps; ++k, ++step, at.next()) {
                 ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
                 // the scale columns written now were last read two stages ago (or, a set a stage, by
                 // the products whose end let this stage be filled again)
@@ -162,10 +168,10 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     for (int p = 0; p < 4; ++p) {
                         if (2 * k + (p >> 1) >= a.tile_cols) break;
                         mma_mxf4<PAIR>(acc, da + p * 2, db + p * 2, mxf4_instruction<PAIR>(N, p & 1), sfa + (p >> 1) * 4,
-                                 sfb + (p >> 1) * 8 + skip, k > 0 || p > 0);
+                                 sfb + (p >> 1) * 8 + skip, k > first_step || p > 0);
                     }
                     tcgen05_commit<PAIR>(smem_addr(&empty[at.slot]));
-                    if (k == a.steps - 1) tcgen05_commit<PAIR>(smem_addr(&acc_full[count & 1]));
+                    if (k == first_step + steps - 1) tcgen05_commit<PAIR>(smem_addr(&acc_full[count & 1]));
                 }
                 __syncwarp();
             }
@@ -206,6 +212,13 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     free_accumulator();
                 }
                 const int64_t row = int64_t(n) * N + piece * 64;
+                if (slices > 1) {
+                    float *const mine = part + (quarter * 32 + lane) * kPartPitch + piece * 64;
+#pragma unroll
+                    for (int j = 0; j < 64; j += 4)
+                        *reinterpret_cast<uint4 *>(mine + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    continue;
+                }
                 uint32_t h[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
@@ -247,27 +260,78 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         tcgen05_fence_after();
         tmem_free<PAIR>(tmem, kTmemColumns);
     }
+    if (slices > 1) {
+        cluster_sync();
+        const int64_t token0 = int64_t(unit % a.token_tiles) * kTileTokens, row0 = int64_t(unit / a.token_tiles) * N;
+        const int tokens = static_cast<int>(min(int64_t(kTileTokens), a.n_tokens - token0));
+        constexpr int kQuads = N / 4;
+        for (int at = slice * 256 + threadIdx.x; at < tokens * kQuads; at += slices * 256) {
+            const int token = at / kQuads, r = at % kQuads * 4;
+            if (row0 + r >= a.n_rows) continue;
+            float4 v[8], sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)  // all on their way before the first is used; added in rank order
+                if (k < slices)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(v[k].x), "=f"(v[k].y), "=f"(v[k].z), "=f"(v[k].w)
+                                 : "r"(remote_address(part + token * kPartPitch + r, k)));
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < slices) {
+                    sum.x += v[k].x;
+                    sum.y += v[k].y;
+                    sum.z += v[k].z;
+                    sum.w += v[k].w;
+                }
+            uint32_t h[2];
+            if constexpr (BF16) {
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
+                h[0] = *reinterpret_cast<const uint32_t *>(&lo);
+                h[1] = *reinterpret_cast<const uint32_t *>(&hi);
+            } else {
+                const __half2 lo = __floats2half2_rn(sum.x, sum.y), hi = __floats2half2_rn(sum.z, sum.w);
+                h[0] = *reinterpret_cast<const uint32_t *>(&lo);
+                h[1] = *reinterpret_cast<const uint32_t *>(&hi);
+            }
+            uint16_t *y = a.Y + (token0 + token) * a.ldy + row0 + r;
+            if (a.tma_y && row0 + r + 4 <= a.n_rows) {
+                *reinterpret_cast<uint2 *>(y) = make_uint2(h[0], h[1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (row0 + r + j < a.n_rows) y[j] = static_cast<uint16_t>(j & 1 ? h[j >> 1] >> 16 : h[j >> 1]);
+            }
+        }
+        cluster_sync();  // no block leaves while its sums are read
+    }
 }
 
 // Tile of a launch: the one that needs the least time in whole rounds over the SMs.  A stage's time
 // is that of its bytes, 64 a cycle into an SM: 128 tokens and the block's rows of 128 bytes, and
-// the scales.
+// the scales.  Where the tiles are few, several blocks share one along the columns, at some 4500
+// cycles for adding up (64 tokens x 14336 x 4096: 20 us without, 13.2 us with 4 blocks for each of
+// 32 tiles).
 struct GemmTile {
     int rows;
     bool pair;
+    int slices;
 };
-static GemmTile choose_tile(int64_t token_tiles, int64_t n_rows, int sms) {
-    GemmTile best = {256, false};
+static GemmTile choose_tile(int64_t token_tiles, int64_t n_rows, int steps, int sms) {
+    GemmTile best = {256, false, 1};
     int64_t least = INT64_MAX;
     for (int pair = 1; pair >= 0; --pair) {
         if (pair && token_tiles < 2) continue;
         for (int n = 256; n >= (pair ? 128 : 64); n -= 64) {
             const int64_t tiles = (token_tiles + pair) / (1 + pair) * ((n_rows + n - 1) / n);
             const int64_t units = sms / (1 + pair);
-            const int64_t cost = (tiles + units - 1) / units * ((128 + n / (1 + pair)) * 2 + 16 * (n > 128 ? 3 : 2));
-            if (cost < least) {
-                least = cost;
-                best = {n, pair != 0};
+            const int64_t stage = (128 + n / (1 + pair)) * 2 + 16 * (n > 128 ? 3 : 2);
+            for (int slices = 1; slices <= (!pair && n <= 128 ? 8 : 1); slices *= 2) {
+                if (slices > 1 && (!cluster_slices_fit(tiles, slices, sms) || steps < 2 * slices)) break;
+                const int64_t cost = (tiles * slices + units - 1) / units * ((steps + slices - 1) / slices) * stage + (slices > 1 ? 4500 : 0);
+                if (cost < least) {
+                    least = cost;
+                    best = {n, pair != 0, slices};
+                }
             }
         }
     }
@@ -285,7 +349,9 @@ static sp_status launch_gemm(const GemmMaps &maps, GemmArgs a, int sms, cudaStre
     cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
     if (e != cudaSuccess) return cuda_fail(e);
     constexpr int kBlocks = PAIR ? 2 : 1;
-    ClusterPdlConfig pdl(kBlocks, dim3(static_cast<unsigned>(std::min(a.tiles, sms / kBlocks) * kBlocks)), dim3(256), stream);
+    const int cluster = kBlocks * a.slices;
+    ClusterPdlConfig pdl(cluster, dim3(static_cast<unsigned>((a.slices > 1 ? a.tiles : std::min(a.tiles, sms / kBlocks)) * cluster)),
+                         dim3(256), stream);
     pdl.cfg.dynamicSmemBytes = STAGES * (kStageBytesA + N / kBlocks * 128 + 2 * kMx4TileBytes * (N > 128 ? 3 : 2)) + 4 * kOutBytes;
     e = cudaLaunchKernelEx(&pdl.cfg, kernel, maps.x, maps.w, maps.y, maps.x_scale, maps.w_scale, a);
     if (e != cudaSuccess) return cuda_fail(e);
@@ -317,12 +383,13 @@ sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t str
     a.steps = (a.tile_cols + 1) / 2;
     a.tma_y = aligned16(p.Y) && p.ldy % 8 == 0;
     const int64_t token_tiles = (p.n_tokens + kTileTokens - 1) / kTileTokens;
-    const GemmTile tile = choose_tile(token_tiles, p.n_rows, sms);
+    const GemmTile tile = choose_tile(token_tiles, p.n_rows, a.steps, sms);
     const int blocks = tile.pair ? 2 : 1;
     const int64_t tiles = (token_tiles + blocks - 1) / blocks * ((p.n_rows + tile.rows - 1) / tile.rows);
     if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
     a.token_tiles = static_cast<int>((token_tiles + blocks - 1) / blocks);
     a.tiles = static_cast<int>(tiles);
+    a.slices = tile.slices;
     GemmMaps maps = {};
     e = encode_byte_tiles(&maps.x, codes, p.n_tokens, pitch, pitch, kTileTokens);
     if (e == cudaSuccess) e = encode_byte_tiles(&maps.w, p.codes, p.n_rows, pitch, p.ldc, tile.rows / blocks);

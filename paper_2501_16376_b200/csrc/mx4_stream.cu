@@ -8,14 +8,15 @@
 //
 // Bound by memory: 17/32 byte per weight.  A block of threads owns 128 rows and a slice of the
 // columns; a producer thread keeps kStages x (128 rows x 512 columns) in flight by TMA; 16 warps (4
-// groups of 32 rows x 4 quarters of the columns of a stage; 8 with halves for more than 16 tokens)
-// convert and multiply.  (With stages of 256 columns a warp's overhead for a stage was a third of
-// its instructions, and issuing them is what the kernel waits for besides memory.)  The
-// column order inside a 32-column block is free as long as weights and activations agree on it:
-// a lane takes 8 consecutive columns, so a weight operand is one 4-byte word of codes (four
-// conversions) and an activation operand is one 16-byte load.  With few rows the columns are cut
-// over a cluster of up to 8 blocks whose partial sums meet through distributed shared memory, in
-// rank order (results do not depend on scheduling).
+// groups of 32 rows x 4 quarters of a stage's columns) convert and multiply.  (With stages of 256
+// columns a warp's overhead for a stage was a third of its instructions, and issuing them is what
+// the kernel waits for besides memory.)  The column order inside a 32-column block is free as long
+// as weights and activations agree on it: a lane takes 8 consecutive columns, so a weight operand
+// is one 4-byte word of codes (four conversions) and an activation operand is one 16-byte load.
+// With few rows the columns are cut over a cluster of up to 8 blocks whose partial sums meet
+// through distributed shared memory, in rank order (results do not depend on scheduling).
+// Measured: 1 token x 4096 x 4096 5.6 us, x 4096 x 14336 10.7 us (2.9 TB/s: 112 blocks of one wave,
+// each 8 stages and some 3 us of start and end).
 //
 // bf16 activations become binary16 here: every (token, 256 columns) is scaled by a power of two
 // so that its largest magnitude lies in [2^14, 2^15).  What binary16 cannot hold - an element
@@ -32,6 +33,8 @@ constexpr int kStages = 3;
 constexpr int kStageTiles = 4;                    // scale tiles of a stage: 512 columns
 constexpr int kBoxBytes = kMx4TileRows * 128;    // codes of 128 rows x 256 columns
 constexpr int kCodeBytes = 2 * kBoxBytes;
+constexpr int kWarps = 16;                        // 4 groups of 32 rows x 4 scale tiles of columns
+constexpr int kTokens = 8;                        // columns of an mma
 constexpr int kPartPitch = 132;                 // floats between columns of a block's partial sums
 
 struct StreamArgs {
@@ -42,6 +45,7 @@ struct StreamArgs {
     int64_t ldy;
     int tile_cols;     // scale tiles along a row
     int stages;        // 512-column stages of a row
+    int slices;        // blocks of a cluster that share the rows
     int chunk_stages;  // stages whose activations are in shared memory at a time
     int quantize_x;
     int vec_x;
@@ -62,8 +66,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
     return v;
 }
-template <int WARPS>
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
 
 // One (token, 256 columns) of the activations -> binary16 in shared memory and its scale;
 // returns whether a remainder is left (bf16).  pass 1 stores the remainders.
@@ -122,25 +125,20 @@ __device__ __forceinline__ bool convert_x(const StreamArgs &a, const uint32_t (&
 
 }  // namespace
 
-template <bool BF16, int NT>
-constexpr int stream_warps() { return NT <= 2 ? 16 : 8; }
-
-template <bool BF16, int NT>
-__global__ void __launch_bounds__(stream_warps<BF16, NT>() * 32 + 32)
+template <bool BF16>
+__global__ void __launch_bounds__(kWarps * 32 + 32)
 mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kStages], empty[kStages];
     __shared__ uint32_t failed, has_rest;
-    constexpr int kTokens = NT * 8, kWarps = stream_warps<BF16, NT>();
-    constexpr int kParts = kWarps / 4, kTiles = kStageTiles / kParts;  // of a stage's columns; scale tiles in each
     uint8_t *const code_smem = smem;
     uint8_t *const scale_smem = smem + kStages * kCodeBytes;
     const int x_pitch = a.chunk_stages * 1024 + 64;              // bytes; 64 mod 128: no conflicts
     uint8_t *const x_smem = scale_smem + kStages * kStageTiles * kMx4TileBytes;
     float *const xs_smem = reinterpret_cast<float *>(x_smem + kTokens * x_pitch);
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
-    const int slices = gridDim.y, slice = blockIdx.y;
-    const int64_t row0 = int64_t(blockIdx.x) * kMx4TileRows;
+    const int slices = a.slices, slice = blockIdx.x % slices, row_tile = blockIdx.x / slices;
+    const int64_t row0 = int64_t(row_tile) * kMx4TileRows;
     const int first = static_cast<int>(int64_t(a.stages) * slice / slices);
     const int last = static_cast<int>(int64_t(a.stages) * (slice + 1) / slices);
 
@@ -162,13 +160,11 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
     pdl_launch_dependents();
     pdl_wait();
 
-    float acc[2][NT][4];
+    float acc[2][4];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) acc[m][i] = 0.0f;
 
     const int g = lane >> 2, t = lane & 3;
     const int wr = warp & 3, wk = warp >> 2;
@@ -187,7 +183,7 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                     tma_load_2d(to, &codes_map, s * 256, static_cast<int>(row0), bar);
                     if (tiles > 2) tma_load_2d(to + kBoxBytes, &codes_map, s * 256 + 128, static_cast<int>(row0), bar);
                     bulk_load(smem_addr(scale_smem + slot * kStageTiles * kMx4TileBytes),
-                              a.scales + (int64_t(blockIdx.x) * a.tile_cols + kStageTiles * s) * kMx4TileBytes,
+                              a.scales + (int64_t(row_tile) * a.tile_cols + kStageTiles * s) * kMx4TileBytes,
                               tiles * kMx4TileBytes, bar);
                 }
                 __syncwarp();
@@ -195,7 +191,7 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
         } else {
             for (int c0 = first; c0 < last; c0 += a.chunk_stages) {
                 const int c1 = min(c0 + a.chunk_stages, last);
-                if (c0 != first || pass != 0) consumer_sync<kWarps>();  // everyone is done with the last chunk
+                if (c0 != first || pass != 0) consumer_sync();  // everyone is done with the last chunk
                 // (token, 256 columns) pairs over the warps, four loads on their way at a time
                 const int cs = 2 * (c1 - c0), pairs = cs * static_cast<int>(a.n_tokens);
                 bool rest = false;
@@ -220,28 +216,23 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                     }
                 }
                 if (rest) has_rest = 1u;
-                consumer_sync<kWarps>();
+                consumer_sync();
                 for (int s = c0; s < c1; ++s, ++step) {
                     const int slot = step % kStages;
                     mbar_wait_or_fail(smem_addr(&full[slot]), (step / kStages) & 1, &failed);
-#pragma unroll
-                    for (int part = 0; part < kTiles; ++part) {
-                        const int tile = wk * kTiles + part;  // of the stage
-                        if (kStageTiles * s + tile >= a.tile_cols) break;
-                        const uint32_t codes = smem_addr(code_smem + slot * kCodeBytes + (tile >> 1) * kBoxBytes) + (wr * 32 + g) * 128 + t * 4;
-                        const uint32_t sc = smem_addr(scale_smem + (slot * kStageTiles + tile) * kMx4TileBytes) + g * 16 + wr * 4;
-                        const uint32_t xa = smem_addr(x_smem) + g * x_pitch + (s - c0) * 1024 + tile * 256 + t * 16;
+                    if (kStageTiles * s + wk < a.tile_cols) {
+                        const uint32_t codes = smem_addr(code_smem + slot * kCodeBytes + (wk >> 1) * kBoxBytes) + (wr * 32 + g) * 128 + t * 4;
+                        const uint32_t sc = smem_addr(scale_smem + (slot * kStageTiles + wk) * kMx4TileBytes) + g * 16 + wr * 4;
+                        const uint32_t xa = smem_addr(x_smem) + g * x_pitch + (s - c0) * 1024 + wk * 256 + t * 16;
                         uint32_t scale_word[4];  // rows g, g+8, g+16, g+24 of the warp's 32
 #pragma unroll
                         for (int j = 0; j < 4; ++j) scale_word[j] = lds32(sc + j * 128);
-                        float st[2][NT][4];
+                        float st[2][4];
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
-                            uint4 x[NT];
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) x[n] = lds128(xa + n * 8 * x_pitch + b * 64);
+                            const uint4 x = lds128(xa + b * 64);
                             // chunk of row r in the swizzled box: block ^ (r & 7); all rows here have r & 7 == g
-                            const uint32_t at = codes + ((((tile & 1) * 4 + b) ^ g) << 4);
+                            const uint32_t at = codes + ((((wk & 1) * 4 + b) ^ g) << 4);
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
                                 uint32_t lo[4], hi[4];
@@ -251,31 +242,21 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
                                 const uint32_t a1[4] = {lo[2], hi[2], lo[3], hi[3]};
                                 const float s0 = mx4_scale((scale_word[2 * m] >> (8 * b)) & 0xffu);
                                 const float s1 = mx4_scale((scale_word[2 * m + 1] >> (8 * b)) & 0xffu);
+                                float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                mma_f16(c, a0, x.x, x.y);
+                                mma_f16(c, a1, x.z, x.w);
 #pragma unroll
-                                for (int n = 0; n < NT; ++n) {
-                                    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                                    mma_f16(c, a0, x[n].x, x[n].y);
-                                    mma_f16(c, a1, x[n].z, x[n].w);
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const float sc_i = i < 2 ? s0 : s1;
-                                        st[m][n][i] = b == 0 ? sc_i * c[i] : fmaf(sc_i, c[i], st[m][n][i]);
-                                    }
+                                for (int i = 0; i < 4; ++i) {
+                                    const float sc_i = i < 2 ? s0 : s1;
+                                    st[m][i] = b == 0 ? sc_i * c[i] : fmaf(sc_i, c[i], st[m][i]);
                                 }
                             }
                         }
+                        const float2 xs = *reinterpret_cast<const float2 *>(xs_smem + (2 * (s - c0) + (wk >> 1)) * kTokens + 2 * t);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const float2 xs = *reinterpret_cast<const float2 *>(
-                                xs_smem + (2 * (s - c0) + (tile >> 1)) * kTokens + n * 8 + 2 * t);
+                        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                            for (int m = 0; m < 2; ++m) {
-                                acc[m][n][0] = fmaf(xs.x, st[m][n][0], acc[m][n][0]);
-                                acc[m][n][1] = fmaf(xs.y, st[m][n][1], acc[m][n][1]);
-                                acc[m][n][2] = fmaf(xs.x, st[m][n][2], acc[m][n][2]);
-                                acc[m][n][3] = fmaf(xs.y, st[m][n][3], acc[m][n][3]);
-                            }
-                        }
+                            for (int i = 0; i < 4; ++i) acc[m][i] = fmaf(i & 1 ? xs.y : xs.x, st[m][i], acc[m][i]);
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
@@ -299,17 +280,14 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    mine[(n * 8 + (i & 1)) * kPartPitch + m * 16 + (i >> 1) * 8] = acc[m][n][i];
+            for (int i = 0; i < 4; ++i) mine[(i & 1) * kPartPitch + m * 16 + (i >> 1) * 8] = acc[m][i];
     }
     __syncthreads();
     for (int at = threadIdx.x; at < static_cast<int>(a.n_tokens) * 128; at += kWarps * 32 + 32) {
         float *p = part + (at >> 7) * kPartPitch + (at & 127);
         float sum = p[0];
 #pragma unroll
-        for (int k = 1; k < kParts; ++k) sum += p[k * kPartFloats];
+        for (int k = 1; k < kStageTiles; ++k) sum += p[k * kPartFloats];
         p[0] = sum;
     }
     if (slices > 1) {
@@ -320,7 +298,7 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
     // (token, row) pairs over the threads of the cluster's blocks; ranks are summed in order
     const int row = threadIdx.x & 127;
     if (warp < kWarps && row0 + row < a.n_rows) {
-        for (int token = slice * kParts + (threadIdx.x >> 7); token < a.n_tokens; token += kParts * slices) {
+        for (int token = slice * (kWarps / 4) + (threadIdx.x >> 7); token < a.n_tokens; token += kWarps / 4 * slices) {
             float sum = 0.0f;
             if (slices > 1) {
                 float v[8];
@@ -343,42 +321,13 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
     if (slices > 1) cluster_sync();  // no block leaves while its sums are read
 }
 
-template <bool BF16, int NT>
-static sp_status launch_tile(const CUtensorMap &map, StreamArgs a, cudaStream_t stream) {
-    const int row_tiles = static_cast<int>(mx4_tile_rows(a.n_rows));
-    // blocks for the SMs in one round
-    int slices = 1;
-    while (slices < 8 && row_tiles * slices <= 74 && a.stages >= 2 * slices) slices *= 2;
-    const int per_slice = (a.stages + slices - 1) / slices;
-    a.chunk_stages = min(per_slice, 8 / NT);
-    const size_t smem = kStages * (kCodeBytes + kStageTiles * kMx4TileBytes) +
-                        NT * 8 * (a.chunk_stages * 1024 + 64 + a.chunk_stages * 8);
-    auto *kernel = mx4_stream_kernel<BF16, NT>;
-    static DynamicSmem limit;
-    cudaError_t e = limit.allow(reinterpret_cast<const void *>(kernel));
-    if (e != cudaSuccess) return cuda_fail(e);
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 1;
-    attr[1].val.clusterDim.y = slices;
-    attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(row_tiles, slices);
-    cfg.blockDim = dim3(stream_warps<BF16, NT>() * 32 + 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = slices > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, map, a);
-    if (e != cudaSuccess) return cuda_fail(e);
-    return check_launch();
-}
-
 sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
     CUtensorMap map;
     cudaError_t e = encode_byte_tiles(&map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
+    if (e != cudaSuccess) return cuda_fail(e);
+    int device = 0, sms = 0;
+    e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return cuda_fail(e);
     StreamArgs a = {};
     a.ldx = p.ldx;
@@ -390,19 +339,25 @@ sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
     a.stages = (a.tile_cols + kStageTiles - 1) / kStageTiles;
     a.quantize_x = p.quantize_x;
     a.vec_x = aligned16(p.X) && p.ldx % 8 == 0 && p.n_cols % 8 == 0;
-    for (int64_t t0 = 0; t0 < p.n_tokens; t0 += 32) {
+    // blocks for the SMs in one round
+    const int row_tiles = static_cast<int>(mx4_tile_rows(p.n_rows));
+    a.slices = 1;
+    while (a.slices < 8 && cluster_slices_fit(row_tiles, a.slices * 2, sms) && a.stages >= 2 * a.slices) a.slices *= 2;
+    a.chunk_stages = min((a.stages + a.slices - 1) / a.slices, 8);
+    auto *kernel = p.dtype == SP_BF16 ? mx4_stream_kernel<true> : mx4_stream_kernel<false>;
+    static DynamicSmem limit[2];
+    e = limit[p.dtype == SP_BF16].allow(reinterpret_cast<const void *>(kernel));
+    if (e != cudaSuccess) return cuda_fail(e);
+    ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(row_tiles * a.slices)), dim3(kWarps * 32 + 32), stream);
+    pdl.cfg.dynamicSmemBytes = kStages * (kCodeBytes + kStageTiles * kMx4TileBytes) +
+                               kTokens * (a.chunk_stages * 1024 + 64 + a.chunk_stages * 8);
+    for (int64_t t0 = 0; t0 < p.n_tokens; t0 += kTokens) {
         a.X = static_cast<const uint16_t *>(p.X) + t0 * p.ldx;
         a.Y = static_cast<uint16_t *>(p.Y) + t0 * p.ldy;
-        a.n_tokens = min(int64_t(32), p.n_tokens - t0);
-        sp_status st;
-        if (p.dtype == SP_BF16)
-            st = a.n_tokens <= 8 ? launch_tile<true, 1>(map, a, stream)
-                                 : a.n_tokens <= 16 ? launch_tile<true, 2>(map, a, stream)
-                                                    : launch_tile<true, 4>(map, a, stream);
-        else
-            st = a.n_tokens <= 8 ? launch_tile<false, 1>(map, a, stream)
-                                 : a.n_tokens <= 16 ? launch_tile<false, 2>(map, a, stream)
-                                                    : launch_tile<false, 4>(map, a, stream);
+        a.n_tokens = min(int64_t(kTokens), p.n_tokens - t0);
+        e = cudaLaunchKernelEx(&pdl.cfg, kernel, map, a);
+        if (e != cudaSuccess) return cuda_fail(e);
+        sp_status st = check_launch();
         if (st != SP_OK) return st;
     }
     return SP_OK;
