@@ -8,16 +8,19 @@
 // leave; blocks whose scale lies more than 2^36 below the row's largest lose bits that are as far
 // below the row's largest products.
 //
-// Bound by the tensor cores.  The weights are the 128 rows of a tile because that side has to be
-// converted, every weight once for up to 160 tokens, and because that operand may lie in tensor
-// memory: a thread converts 128 columns of its row in registers and stores them there.  (Through
-// shared memory the converted weights were written once and read once at 16 KB for 64 columns, and
-// with the activations that kept shared memory, not the tensor cores, busy.)  A stage costs the
-// issuing warp some 500 cycles of waiting and signalling whatever it holds, so it holds 128 columns;
-// converting it is a longer chain still, so three groups of four warps do every third stage each,
-// a thread a row.  One thread streams the
-// activations by TMA, one the codes, one issues the products, four warps empty the accumulators
-// (two, alternating) and find the next tile's R.
+// The weights are the 128 rows of a tile because that side has to be converted, every weight once for
+// up to 160 tokens, and because that operand may lie in tensor memory: a thread converts 128 columns
+// of its row in registers and stores them there.  (Through shared memory the converted weights were
+// written once and read once at 16 KB for 64 columns, and with the activations that kept shared
+// memory busy: 333 tokens x 4096 x 11008 took 50.8 us against 41.1.)  Converting a stage of 128
+// columns is a long chain, so four (three) groups of four warps do every fourth stage each, a thread
+// a row.  One thread streams the activations by TMA, one the codes, one issues the products, four
+// warps empty the accumulators (two, alternating) and find the next tile's R; the last tile of a
+// block is emptied by the converting warps too.
+//
+// Bound by the thread that issues the products: 128 tokens take 520 cycles of tensor core a stage,
+// and its wait, even for what is there already, 140 more.  Measured (f16): 333 x 4096 x 11008
+// 28.2 us (1063 TFLOP/s; two rounds of tiles, the second three quarters full).
 #include <algorithm>
 
 #include "mx4_common.cuh"
@@ -27,15 +30,22 @@ namespace sp {
 
 namespace {
 
-constexpr int kSlots = 3;                        // stages of 128 columns
 constexpr int kCodeSlots = 4;                    // stages of 256 columns: codes and scales as stored
-constexpr int kMostTokens = 160;
-constexpr int kHalfBytes = kMostTokens * 128;    // 64 columns of activations
-constexpr int kSlotBytes = 2 * kHalfBytes;
 constexpr int kCodeSlotBytes = kMx4TileRows * 128 + 2 * kMx4TileBytes;
-constexpr int kTmemColumns = 512;                // two accumulators of 160, three stages of 64 of weights
-constexpr int kWeightColumns = 2 * kMostTokens;
-constexpr int kThreads = 256 + kSlots * 128;     // 4 warps of single roles, 4 that empty, a group of 4 for every slot
+constexpr int kTmemColumns = 512;
+
+// Tiles of up to 128 tokens leave tensor memory for four stages of converted weights (of 64 columns
+// of it), up to 160 for three.
+template <bool WIDE>
+struct Gemm16Tile {
+    static constexpr int kMostTokens = WIDE ? 160 : 128;
+    static constexpr int kSlots = WIDE ? 3 : 4;             // stages of 128 columns
+    static constexpr int kHalfBytes = kMostTokens * 128;    // 64 columns of activations
+    static constexpr int kSlotBytes = 2 * kHalfBytes;
+    static constexpr int kWeightColumns = 2 * kMostTokens;  // behind two accumulators
+    static constexpr int kThreads = 256 + kSlots * 128;     // 4 warps of single roles, 4 that empty, a group of 4 for every slot
+    static constexpr int kSmemBytes = kSlots * kSlotBytes + kCodeSlots * kCodeSlotBytes;
+};
 
 struct Gemm16Args {
     const uint8_t *scales;
@@ -77,15 +87,18 @@ __device__ __forceinline__ void convert8(uint32_t w, uint32_t factor, uint32_t (
 
 }  // namespace
 
-template <bool BF16>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool BF16, bool WIDE>
+__global__ void __launch_bounds__(Gemm16Tile<WIDE>::kThreads, 1)
 mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Gemm16Args a) {
+    using Tile = Gemm16Tile<WIDE>;
+    constexpr int kMostTokens = Tile::kMostTokens, kSlots = Tile::kSlots, kHalfBytes = Tile::kHalfBytes;
+    constexpr int kSlotBytes = Tile::kSlotBytes, kWeightColumns = Tile::kWeightColumns, kThreads = Tile::kThreads;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots];
-    __shared__ uint64_t acc_full[2], acc_free, top_full[8], drained;
+    __shared__ uint64_t acc_full[2], acc_free, last_full, top_full[8], drained;
     __shared__ uint32_t tmem_base, failed;
     // Largest scale byte of a row, for eight tiles in turn.  A group may have no stage of a tile and
-    // then does not look at it; it has one within three tiles, and the tile after the next is the last
+    // then does not look at it; it has one within four tiles, and the tile after the next is the last
     // that is published before it is converted, so no barrier is two phases ahead of a group.
     __shared__ int row_top[8][kMx4TileRows];
     uint8_t *const slots = smem, *const codes = smem + kSlots * kSlotBytes;
@@ -105,6 +118,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         mbar_init(smem_addr(&acc_full[0]), 1);
         mbar_init(smem_addr(&acc_full[1]), 1);
         mbar_init(smem_addr(&acc_free), 128);
+        mbar_init(smem_addr(&last_full), 1);
         for (int i = 0; i < 8; ++i) mbar_init(smem_addr(&top_full[i]), 128);
         mbar_init(smem_addr(&drained), 1);
         failed = 0u;
@@ -122,6 +136,43 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     const int slices = a.slices, rank = blockIdx.x % slices, unit = blockIdx.x / slices, units = gridDim.x / slices;
     const int code_begin = (a.steps + 1) / 2 * rank / slices, code_steps = (a.steps + 1) / 2 * (rank + 1) / slices - code_begin;
     const int first_step = 2 * code_begin, steps = min(2 * code_steps, a.steps - first_step);
+
+    // Accumulator -> output (or the block's part of the sums), every step-th 32 tokens from the
+    // first-th on; a warp has the rows that its quarter of tensor memory holds.
+    auto empty_tile = [&](int tile, int count, int quarter, int first, int step) {
+        const int m = tile % a.row_tiles, n = tile / a.row_tiles;
+        const uint32_t acc = tmem + (count & 1) * kMostTokens + (static_cast<uint32_t>(quarter * 32) << 16);
+        const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
+        float f0 = 1.0f, f1 = 1.0f;
+        if constexpr (!BF16) {
+            const int e = row_top[count & 7][quarter * 32 + lane] - 140;
+            f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
+            f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
+        }
+        const int64_t token0 = int64_t(n) * a.tile_tokens;
+        const int tokens = static_cast<int>(min(int64_t(a.tile_tokens), a.n_tokens - token0));
+#pragma unroll 1
+        for (int c = first * 32; c < tokens; c += step * 32) {
+            uint32_t v[32];
+            tmem_load32(acc + c, v);
+            tmem_load_wait();
+            if (slices > 1) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j < tokens) part[(c + j) * kMx4TileRows + quarter * 32 + lane] = __uint_as_float(v[j]);
+            } else if (row < a.n_rows) {
+                uint16_t *y = a.Y + (token0 + c) * a.ldy + row;
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j < tokens) {
+                        const float x = __uint_as_float(v[j]) * f0 * f1;
+                        if constexpr (BF16) y[j * a.ldy] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+                        else y[j * a.ldy] = __half_as_ushort(__float2half_rn(x));
+                    }
+            }
+            __syncwarp();
+        }
+    };
 
     if (warp == 0) {
         RingPlace<kSlots> at;
@@ -171,29 +222,29 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     } else if (warp == 1) {
         const uint32_t instruction = f16_instruction(a.tile_tokens, BF16);
         const uint64_t desc0 = desc_rows128(smem_addr(slots));
-        RingPlace<kSlots> at;
-        int count = 0;
-        bool ok = true;
-        for (int tile = unit; ok && tile < a.tiles; tile += units, ++count) {
-            if (count > 0) ok = mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed);
-            if (!__all_sync(kFullWarp, ok)) break;
-            const uint32_t acc = tmem + (count & 1) * kMostTokens;
-            for (int k = 0; k < steps; ++k, at.next()) {
-                ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
-                if (!__all_sync(kFullWarp, ok)) { ok = false; break; }
-                tcgen05_fence_after();
-                if (elect_one()) {
+        if (elect_one()) {  // once: electing a thread for every stage took 85 cycles each time
+            RingPlace<kSlots> at;
+            int count = 0;
+            bool ok = true;
+            for (int tile = unit; ok && tile < a.tiles; tile += units, ++count) {
+                if (count > 0 && !mbar_wait_or_fail(smem_addr(&acc_free), (count - 1) & 1, &failed)) break;
+                const uint32_t acc = tmem + (count & 1) * kMostTokens;
+                for (int k = 0; k < steps; ++k, at.next()) {
+                    ok = mbar_wait_or_fail(smem_addr(&full[at.slot]), at.parity, &failed);
+                    if (!ok) break;
+                    tcgen05_fence_after();
                     const uint64_t db = desc0 + static_cast<uint32_t>(at.slot * (kSlotBytes / 16));
                     const uint32_t ta = tmem + kWeightColumns + at.slot * 64;
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
                         mma_16bit(acc, ta + p * 8, db + (p >> 2) * (kHalfBytes / 16) + (p & 3) * 2, instruction, k > 0 || p > 0);
                     tcgen05_commit(smem_addr(&empty[at.slot]));
-                    if (k == steps - 1) tcgen05_commit(smem_addr(&acc_full[count & 1]));
                 }
-                __syncwarp();
+                if (ok) tcgen05_commit(smem_addr(&acc_full[count & 1]));
+                if (ok && tile + units >= a.tiles) tcgen05_commit(smem_addr(&last_full));
             }
         }
+        __syncwarp();
         if (failed != 0u) {
             if (elect_one()) tcgen05_commit(smem_addr(&drained));
             __syncwarp();
@@ -265,6 +316,12 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
                 ++uses;
             }
         }
+        ok = ok && mbar_wait_or_fail(smem_addr(&last_full), 0, &failed);
+        if (__all_sync(kFullWarp, ok)) {
+            tcgen05_fence_after();
+            empty_tile(unit + (count - 1) * units, count - 1, warp & 3, 1 + slot, 1 + kSlots);
+        }
+        tcgen05_fence_before();
     } else if (warp >= 4) {
         const int quarter = warp & 3;
         int count = 0;
@@ -272,7 +329,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         auto find_top = [&](int tile, int c) {
             const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + lane * 16 + quarter * 4;
             uint32_t most = 0;
-#pragma unroll 16
+#pragma unroll 32
             for (int i = 0; i < a.tile_cols; ++i) {
                 uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(s + int64_t(i) * kMx4TileBytes));
                 w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
@@ -284,44 +341,14 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         };
         if (!BF16 && unit < a.tiles) find_top(unit, 0);
         for (int tile = unit; tile < a.tiles; tile += units, ++count) {
-            const int m = tile % a.row_tiles, n = tile / a.row_tiles;
             if (!BF16 && tile + units < a.tiles) find_top(tile + units, count + 1);
             const bool ok = mbar_wait_or_fail(smem_addr(&acc_full[count & 1]), (count >> 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
             tcgen05_fence_before();
             mbar_arrive(smem_addr(&acc_free));  // the other accumulator was emptied before
-            const uint32_t acc = tmem + (count & 1) * kMostTokens + (static_cast<uint32_t>(quarter * 32) << 16);
-            const int64_t row = int64_t(m) * kMx4TileRows + quarter * 32 + lane;
-            float f0 = 1.0f, f1 = 1.0f;
-            if constexpr (!BF16) {
-                const int e = row_top[count & 7][quarter * 32 + lane] - 140;
-                f0 = __uint_as_float(static_cast<uint32_t>(e / 2 + 127) << 23);
-                f1 = __uint_as_float(static_cast<uint32_t>(e - e / 2 + 127) << 23);
-            }
-            const int64_t token0 = int64_t(n) * a.tile_tokens;
-            const int tokens = static_cast<int>(min(int64_t(a.tile_tokens), a.n_tokens - token0));
-#pragma unroll 1
-            for (int c = 0; c < tokens; c += 32) {
-                uint32_t v[32];
-                tmem_load32(acc + c, v);
-                tmem_load_wait();
-                if (slices > 1) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c + j < tokens) part[(c + j) * kMx4TileRows + quarter * 32 + lane] = __uint_as_float(v[j]);
-                } else if (row < a.n_rows) {
-                    uint16_t *y = a.Y + (token0 + c) * a.ldy + row;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c + j < tokens) {
-                            const float x = __uint_as_float(v[j]) * f0 * f1;
-                            if constexpr (BF16) y[j * a.ldy] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
-                            else y[j * a.ldy] = __half_as_ushort(__float2half_rn(x));
-                        }
-                }
-                __syncwarp();
-            }
+            // the last tile is emptied by all warps but the first four
+            empty_tile(tile, count, quarter, 0, tile + units < a.tiles ? 1 : 1 + kSlots);
         }
         tcgen05_fence_before();
     }
@@ -370,22 +397,45 @@ mx4_align_rows_kernel(const uint16_t *__restrict__ X, int64_t ldx, int64_t n_col
     for (int64_t c = threadIdx.x; c < n_cols; c += blockDim.x) out[row * pitch + c] = X[row * ldx + c];
 }
 
-// Tokens of a tile: as few rounds over the SMs as possible, each as short as possible (a round
-// of less than 112 tokens is bound by the conversion).
-static int tile_tokens(int64_t n_tokens, int64_t row_tiles, int sms) {
-    int best = 16;
+// Tokens of a tile, and blocks that share it along the columns where the tiles are few: the least
+// time in whole rounds over the SMs.  A stage of 128 columns takes the time of 320 tokens, for waits
+// and conversion, and that of its own; with more than 128 tokens, one slot less, of 432 (8192
+// columns, a tile on every SM, f16: 16 tokens 26.8 us, 128 34.0, 160 43.4; 160 as two of 80: 51.7).
+// Adding up a shared tile takes about that of 3000 (64 tokens x 14336 x 4096: 19.3 us, without 49.9).
+struct Gemm16Shape {
+    int tokens, slices;
+};
+static Gemm16Shape choose_shape(int64_t n_tokens, int64_t row_tiles, int steps, int sms) {
+    constexpr int kMostTokens = Gemm16Tile<true>::kMostTokens;
+    Gemm16Shape best = {16, 1};
     int64_t least = INT64_MAX;
     const int64_t first = (n_tokens + kMostTokens - 1) / kMostTokens;
     for (int64_t parts = first; parts <= first + 8; ++parts) {
         const int64_t n = ((n_tokens + parts - 1) / parts + 15) / 16 * 16;
         const int64_t tiles = row_tiles * ((n_tokens + n - 1) / n);
-        const int64_t cost = (tiles + sms - 1) / sms * std::max(n, int64_t(64));
-        if (cost < least) {
-            least = cost;
-            best = static_cast<int>(n);
+        const int64_t stage = n + (n > Gemm16Tile<false>::kMostTokens ? 432 : 320);
+        for (int slices = 1; slices <= 8; slices *= 2) {
+            if (slices > 1 && (!cluster_slices_fit(tiles, slices, sms) || steps < 4 * slices)) break;
+            const int64_t cost = (tiles * slices + sms - 1) / sms * ((steps + slices - 1) / slices) * stage + (slices > 1 ? 3000 : 0);
+            if (cost < least) {
+                least = cost;
+                best = {static_cast<int>(n), slices};
+            }
         }
     }
     return best;
+}
+
+template <bool BF16, bool WIDE>
+static cudaError_t launch_gemm16(const CUtensorMap &x_map, const CUtensorMap &w_map, const Gemm16Args &a, int sms, cudaStream_t stream) {
+    using Tile = Gemm16Tile<WIDE>;
+    static DynamicSmem limit;
+    cudaError_t e = limit.allow(reinterpret_cast<const void *>(mx4_gemm16_kernel<BF16, WIDE>));
+    if (e != cudaSuccess) return e;
+    ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(a.slices > 1 ? a.tiles * a.slices : std::min(a.tiles, sms))),
+                         dim3(Tile::kThreads), stream);
+    pdl.cfg.dynamicSmemBytes = Tile::kSmemBytes;
+    return cudaLaunchKernelEx(&pdl.cfg, mx4_gemm16_kernel<BF16, WIDE>, x_map, w_map, a);
 }
 
 int64_t mx4_gemm16_workspace(int64_t n_tokens, int64_t n_cols) { return n_tokens * ((n_cols + 7) / 8 * 8) * 2; }
@@ -418,7 +468,9 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     a.tile_cols = static_cast<int>(mx4_tile_cols(p.n_cols));
     a.steps = a.tile_cols;
     const int64_t row_tiles = mx4_tile_rows(p.n_rows);
-    a.tile_tokens = tile_tokens(p.n_tokens, row_tiles, sms);
+    const Gemm16Shape shape = choose_shape(p.n_tokens, row_tiles, a.steps, sms);
+    a.tile_tokens = shape.tokens;
+    a.slices = shape.slices;
     const int64_t tiles = row_tiles * ((p.n_tokens + a.tile_tokens - 1) / a.tile_tokens);
     if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
     a.row_tiles = static_cast<int>(row_tiles);
@@ -427,20 +479,9 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     e = encode_byte_tiles(&x_map, X, p.n_tokens, p.n_cols * 2, ldx * 2, a.tile_tokens);
     if (e == cudaSuccess) e = encode_byte_tiles(&w_map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
     if (e != cudaSuccess) return cuda_fail(e);
-    a.slices = 1;
-    while (a.slices < 8 && cluster_slices_fit(a.tiles, a.slices * 2, sms) && a.steps >= 8 * a.slices) a.slices *= 2;
-    ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(a.slices > 1 ? a.tiles * a.slices : std::min(a.tiles, sms))),
-                         dim3(kThreads), stream);
-    pdl.cfg.dynamicSmemBytes = kSlots * kSlotBytes + kCodeSlots * kCodeSlotBytes;
-    if (p.dtype == SP_BF16) {
-        static DynamicSmem limit;
-        e = limit.allow(reinterpret_cast<const void *>(mx4_gemm16_kernel<true>));
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, mx4_gemm16_kernel<true>, x_map, w_map, a);
-    } else {
-        static DynamicSmem limit;
-        e = limit.allow(reinterpret_cast<const void *>(mx4_gemm16_kernel<false>));
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, mx4_gemm16_kernel<false>, x_map, w_map, a);
-    }
+    const bool wide = a.tile_tokens > Gemm16Tile<false>::kMostTokens;
+    if (p.dtype == SP_BF16) e = (wide ? launch_gemm16<true, true> : launch_gemm16<true, false>)(x_map, w_map, a, sms, stream);
+    else e = (wide ? launch_gemm16<false, true> : launch_gemm16<false, false>)(x_map, w_map, a, sms, stream);
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }
