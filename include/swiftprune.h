@@ -504,7 +504,8 @@ sp_status sp_cache_append(const sp_cache *cache /* host struct */, const void *K
  * that every token received, for sp_cache_evict:
  *     acc_out[b, g, j] = acc_in[b, g, j] + sum of p[j] over the queries and the heads of group g
  * for j < lens[b], 0 up to max_len; acc_in (nullable: zeros; may be acc_out) counts as 0 for the
- * call's own n_q tokens.  workspace as in sp_mx4_linear.
+ * call's own n_q tokens.  workspace as in sp_mx4_linear.  The pool may have at most 2^31 - 1
+ * rows n_blocks * n_kv_heads * block_tokens here (else SP_ERR_SHAPE).
  */
 sp_status sp_cache_attention_workspace(const sp_cache *cache, int64_t n_q, int n_heads,
                                        int64_t max_len, int want_acc, int64_t *bytes /* host */);

@@ -18,9 +18,9 @@
 // warps empty the accumulators (two, alternating) and find the next tile's R; the last tile of a
 // block is emptied by the converting warps too.
 //
-// Bound by the thread that issues the products: 128 tokens take 520 cycles of tensor core a stage,
+// Bound by the tensor core and the thread that feeds it: 128 tokens take 520 cycles of products a stage,
 // and its wait, even for what is there already, 140 more.  Measured (f16): 333 x 4096 x 11008
-// 28.2 us (1063 TFLOP/s; two rounds of tiles, the second three quarters full).
+// 28.3 us (1060 TFLOP/s; two rounds of tiles, the second three quarters full).
 #include <algorithm>
 
 #include "mx4_common.cuh"
