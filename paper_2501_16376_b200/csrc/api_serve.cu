@@ -65,7 +65,7 @@ constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens o
 // Whether a product takes the kernels that tile over tokens: from 9 tokens on, the columns of one
 // mma of the streaming kernel.  (At 8 tokens it is ahead, bf16 activations: 7.2 us against 9.5 for
 // 4096 x 4096, 14.8 against 18.1 for 4096 x 14336; with two such columns, at 16 tokens, it took 9.3
-// against 9.6 and 22.8 against 18.3.)
+// against 9.9 and 22.8 against 18.6.)
 static bool takes_tiles(int64_t n_tokens) { return n_tokens > 8; }
 
 static sp_status check_codes(const void *codes, int64_t ldc, const void *scales, int64_t n_cols) {
