@@ -19,9 +19,9 @@
 //     8x8 by movmatrix.
 // The block scale of K goes onto the scores and that of V onto the 16-token partial product, in
 // binary32.  The cache arrives by TMA, two stages of 64 tokens ahead (128 KB in flight on an SM; the
-// swizzle keeps both access patterns free of bank conflicts).  P is rounded to binary16 for the
-// product; for binary16 outputs the remainder follows as a second operand (2^-22 in all), since one rounding of P alone would be as large as that of
-// the output.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
+// swizzle keeps both access patterns free of bank conflicts).  P goes
+// into the product in two binary16 parts (2^-22 in all): with one, a weight is off by up to 2^-12 of
+// itself, which outputs far smaller than their values show in either type.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
 // the reductions of nearly all steps and leaves P at most 256.
 #include <algorithm>
 
@@ -410,10 +410,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             for (int h = 0; h < 2; ++h) {
                 const uint32_t hi = pack_f16(p[2 * h], p[2 * h + 1]);
                 ph[n][h] = transpose8x8(hi);
-                if constexpr (!BF16) {
-                    const float2 r = unpack_f16(hi);
-                    pl[n][h] = transpose8x8(pack_f16(p[2 * h] - r.x, p[2 * h + 1] - r.y));
-                }
+                const float2 r = unpack_f16(hi);
+                pl[n][h] = transpose8x8(pack_f16(p[2 * h] - r.x, p[2 * h + 1] - r.y));
             }
         }
         // values past the end, and NaN of the call's own tokens, which some rows do not see
@@ -449,7 +447,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 for (int n = 0; n < NT; ++n) {
                     float x[4];
                     mma_f16_first(x, f, ph[n][0], ph[n][1]);
-                    if constexpr (!BF16) mma_f16(x, f, pl[n][0], pl[n][1]);
+                    mma_f16(x, f, pl[n][0], pl[n][1]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[n][2 * w + half][i] = fmaf(v_scale, x[i], o[n][2 * w + half][i]);
                 }
