@@ -19,10 +19,16 @@
 //     8x8 by movmatrix.
 // The block scale of K goes onto the scores and that of V onto the 16-token partial product, in
 // binary32.  The cache arrives by TMA, two stages of 64 tokens ahead (128 KB in flight on an SM; the
-// swizzle keeps both access patterns free of bank conflicts).  P goes
-// into the product in two binary16 parts (2^-22 in all): with one, a weight is off by up to 2^-12 of
-// itself, which outputs far smaller than their values show in either type.  The maximum is raised only when a score exceeds it by more than 2^8, which saves
-// the reductions of nearly all steps and leaves P at most 256.
+// swizzle keeps both access patterns free of bank conflicts).  P goes into the product in two
+// binary16 parts: with one, a weight is off by up to 2^-12 of itself, which outputs far smaller than
+// their values show in either type.  The maximum is raised only when a score exceeds it by more than
+// 2^8, which saves the reductions of nearly all steps.  P is kept relative to 2^-7 of the maximum, so
+// that it reaches 2^15 and uses binary16's range, and its second part is multiplied by 2^12: together
+// they hold a weight to 2^-22 of itself down to 2^-22 of the largest, and to 2^-44 of the largest
+// below.  (A token with most of the attention and a value near 0 leaves an output that is made of
+// small weights.)  Against one part for bf16 outputs, and two parts within 2^-32 of the largest for
+// f16, this costs nothing up to 4 rows, and more above: 32 x 8191 tokens of 8 heads without weights
+// take 85 us with 4 rows, 98 with 8 (93), 164 with 16 (139 and 157).
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -36,7 +42,9 @@ constexpr int kAttnWarps = 4;
 constexpr int kRing = 3;           // stages of 16 tokens for every warp
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;  // running maximum before any score
-constexpr float kRaise = 8.0f;  // how far (in powers of two) a score may exceed the running maximum
+constexpr float kLift = 7.0f;   // the reference lies this far (in powers of two) below the running maximum
+constexpr float kRaise = 8.0f;  // how far a score may exceed the running maximum
+constexpr float kRest = 4096.0f;  // factor of a weight's second part
 
 struct AttnArgs {
     sp_cache cache;
@@ -66,6 +74,14 @@ __device__ __forceinline__ void mma_f16_first(float (&d)[4], const uint32_t (&a)
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+// (d0, d1) += a * (b0, b1), two multiply-adds in one instruction.
+__device__ __forceinline__ void add_scaled2(float &d0, float &d1, float a, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %2};\n\tmov.b64 b, {%3, %4};\n\tmov.b64 d, {%0, %1};\n\t"
+        "fma.rn.f32x2 d, a, b, d;\n\t"
+        "mov.b64 {%0, %1}, d;\n\t}"
+        : "+f"(d0), "+f"(d1) : "f"(a), "f"(b0), "f"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t r;
@@ -115,8 +131,9 @@ __device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row
 
 }  // namespace
 
-// NT: tiles of 8 rows
-template <bool BF16, int D, int NT>
+// NT: tiles of 8 rows.  TWICE (at most 4 rows): the rows stand twice in their tile, and the second
+// time take their weights' second parts, so that one product serves both parts.
+template <bool BF16, int D, int NT, bool TWICE>
 __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attention_kernel(const __grid_constant__ CUtensorMap k_map,
                                                                                                const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
@@ -210,7 +227,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     int limit[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = row0 + n * 8 + g;
+        const int row = row0 + n * 8 + (TWICE ? g & 3 : g);
         float undo = a.scale_log2;
         if (row < a.rows) {
             const uint16_t *q = a.Q + seq * a.q.seq + (row / a.group) * a.q.token +
@@ -261,7 +278,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             qscale[n][i] = __shfl_sync(kFullWarp, undo, (2 * t + i) * 4);
-            limit[n][i] = row_limit(a, seq, row0 + n * 8 + 2 * t + i, len);
+            limit[n][i] = row_limit(a, seq, row0 + n * 8 + (TWICE ? (2 * t + i) & 3 : 2 * t + i), len);
             m[n][i] = kLowest;
             l[n][i] = 0.0f;
         }
@@ -304,7 +321,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
             continue;
         }
-        const float k_scale = scales[slot][warp].x, v_scale = scales[slot][warp].y;
+        const float k_scale = scales[slot][warp].x;
+        const float v_scale = scales[slot][warp].y * (TWICE && t >= 2 ? 1.0f / kRest : 1.0f);
         uint32_t kw[2][KW], vw[4][VW];
         {
             // 16-byte chunk x of row r lies at x ^ (r & 7) (128-byte rows) or x ^ (r / 2 & 3)
@@ -355,7 +373,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) raise |= fmaxf(s[n][i], s[n][i + 2]) > m[n][i] + kRaise;
+                for (int i = 0; i < 2; ++i) raise |= fmaxf(s[n][i], s[n][i + 2]) > m[n][i] + (kLift + kRaise);
             if (a.scores != nullptr) {
                 // rows 2t, 2t + 1 of tokens g and g + 8
                 float *to = scores + int64_t(j0) * a.rows;
@@ -384,7 +402,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, 16));
-                        top = fmaxf(top, m[n][i]);
+                        top = fmaxf(top - kLift, m[n][i]);
                         const float f = exp2_fast(m[n][i] - top);
                         m[n][i] = top;
                         l[n][i] *= f;
@@ -409,9 +427,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t hi = pack_f16(p[2 * h], p[2 * h + 1]);
-                ph[n][h] = transpose8x8(hi);
                 const float2 r = unpack_f16(hi);
-                pl[n][h] = transpose8x8(pack_f16(p[2 * h] - r.x, p[2 * h + 1] - r.y));
+                const uint32_t rest = pack_f16((p[2 * h] - r.x) * kRest, (p[2 * h + 1] - r.y) * kRest);
+                ph[n][h] = transpose8x8(TWICE && t >= 2 ? rest : hi);
+                if constexpr (!TWICE) pl[n][h] = transpose8x8(rest);
             }
         }
         // values past the end, and NaN of the call's own tokens, which some rows do not see
@@ -447,9 +466,15 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 for (int n = 0; n < NT; ++n) {
                     float x[4];
                     mma_f16_first(x, f, ph[n][0], ph[n][1]);
-                    mma_f16(x, f, pl[n][0], pl[n][1]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[n][2 * w + half][i] = fmaf(v_scale, x[i], o[n][2 * w + half][i]);
+                    if constexpr (!TWICE) {
+                        float rest[4];
+                        mma_f16_first(rest, f, pl[n][0], pl[n][1]);
+                        add_scaled2(x[0], x[1], 1.0f / kRest, rest[0], rest[1]);
+                        add_scaled2(x[2], x[3], 1.0f / kRest, rest[2], rest[3]);
+                    }
+                    float(&to)[4] = o[n][2 * w + half];
+                    add_scaled2(to[0], to[1], v_scale, x[0], x[1]);
+                    add_scaled2(to[2], to[3], v_scale, x[2], x[3]);
                 }
             }
         }
@@ -491,7 +516,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         for (int w = 0; w < kAttnWarps; ++w) {
             const float f = exp2_fast(sh_m[w][r] - top);
             sum = fmaf(f, sh_l[w][r], sum);
-            out = fmaf(f, sh_o[w][r][d], out);
+            out = fmaf(f, TWICE ? sh_o[w][r][d] + sh_o[w][r + 4][d] : sh_o[w][r][d], out);
         }
         if (nan_from[d] <= row_limit(a, seq, row, len)) out = __uint_as_float(0x7fc00000u);
         if (a.part_o != nullptr) {
@@ -677,7 +702,7 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
 // they finish together.  Where that gives a few blocks (short caches, few heads), a cluster of up
 // to 8 spares the second kernel: 517 tokens of 16 heads take 6.7 us against 7.6.  Otherwise all
 // blocks run at once, 4 an SM, and the second kernel has the device to itself: 32 x 8191 tokens of
-// 8 heads with weights take 103 us (5.0 TB/s), in clusters 115 to 117 (blocks of a cluster start and end
+// 8 heads with weights take 102 us (5.0 TB/s), in clusters 115 to 117 (blocks of a cluster start and end
 // together).
 struct AttentionPlan {
     int row_tiles, splits;
@@ -757,17 +782,24 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     }
     if (e != cudaSuccess) return cuda_fail(e);
     pdl.cfg.dynamicSmemBytes = kAttnWarps * kRing * c.head_dim * 32;
-#define SP_LAUNCH(B, DD, N)                                                                              \
+#define SP_LAUNCH(B, DD, N, TWICE)                                                                       \
     do {                                                                                                 \
         static DynamicSmem limit;                                                                        \
-        e = limit.allow(reinterpret_cast<const void *>(cache_attention_kernel<B, DD, N>));               \
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, cache_attention_kernel<B, DD, N>, k_map, v_map, a); \
+        auto *kernel = cache_attention_kernel<B, DD, N, TWICE>;                                          \
+        e = limit.allow(reinterpret_cast<const void *>(kernel));                                         \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, kernel, k_map, v_map, a);                 \
     } while (0)
-#define SP_PICK(B)                                                                                     \
-    if (c.head_dim == 64) { if (a.rows <= 8) SP_LAUNCH(B, 64, 1); else SP_LAUNCH(B, 64, 2); }          \
-    else { if (a.rows <= 8) SP_LAUNCH(B, 128, 1); else SP_LAUNCH(B, 128, 2); }
+#define SP_ROWS(B, DD)                                    \
+    do {                                                  \
+        if (a.rows <= 4) SP_LAUNCH(B, DD, 1, true);       \
+        else if (a.rows <= 8) SP_LAUNCH(B, DD, 1, false); \
+        else SP_LAUNCH(B, DD, 2, false);                  \
+    } while (0)
+#define SP_PICK(B) \
+    if (c.head_dim == 64) SP_ROWS(B, 64); else SP_ROWS(B, 128);
     if (dtype == SP_BF16) { SP_PICK(true) } else { SP_PICK(false) }
 #undef SP_PICK
+#undef SP_ROWS
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     sp_status st = check_launch();

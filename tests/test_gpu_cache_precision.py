@@ -47,3 +47,30 @@ def test_values_that_cancel(sp, heads, group, D, dtype):
     got, want, mag = _attention(sp, K.to(dtype), V.to(dtype), Q.to(dtype))
     err = np.abs(got - want)
     assert (err <= UNIT[dtype] * np.abs(want) + 2.0 ** -19 * mag + TINY[dtype]).all(), (err - UNIT[dtype] * np.abs(want)).max()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("L,heads,D", [(200, 4, 64), (3000, 1, 128), (20000, 2, 64)])
+@pytest.mark.parametrize("below", [18.0, 24.0, 26.0])
+def test_outputs_that_lie_in_many_small_weights(sp, L, heads, D, below, dtype):
+    """One token takes nearly all the attention and has the value 0 (a sink), so that the output is
+    made of weights 2^-26, 2^-34.6 and 2^-37.5 of the largest.  A score is one exact product of at most
+    26, times log2(e) in binary32: its exponent is off by 2^-18 at most (38 * 2^-24, and the
+    exponential's own 2^-22), a weight by as much of itself; the two parts end 2^-37 below weights
+    of at least 2^7, 2^-44 relative to the largest, and the sums in binary32 lose 2^-24 for each of
+    a lane's additions, L / 16 at most."""
+    g = torch.Generator().manual_seed(L)
+    K = torch.zeros(1, L, heads, D)
+    K[..., 0] = -below
+    top = 448.0 * (64 if dtype == torch.float16 else 1)
+    V = (torch.rand(1, L, heads, D, generator=g) * 0.9 + 0.1) * top
+    at = L // 3
+    K[:, at, :, 0], V[:, at] = 0.0, 0.0
+    Q = torch.zeros(1, 2, heads * 2, D)
+    Q[..., 0] = 1.0
+    got, want, mag = _attention(sp, K.to(dtype), V.to(dtype), Q.to(dtype))
+    assert (want > 1e-9).all()
+    err = np.abs(got - want)
+    allowed = (UNIT[dtype] * want + (2.0 ** -17 + L / 16 * 2.0 ** -24) * mag
+               + L * 2.0 ** -44 * top + TINY[dtype])
+    assert (err <= allowed).all(), (err / allowed).max()
