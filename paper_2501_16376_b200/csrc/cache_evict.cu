@@ -355,11 +355,11 @@ cache_gather_kernel(const sp_cache src, const sp_cache dst, const int32_t *__res
     for (int which = 0; which < 2; ++which) {
         const uint32_t *m = warp_amax[which];
         const int e = cache_exponent(max(max(m[0], m[1]), max(m[2], m[3])));
-        const float inv = pow2(-e);
         uint4 *out = static_cast<uint4 *>(which == 0 ? dst.k : dst.v) + (to * H + head) * (T * kRowPieces);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const float f = scale[which][i] * inv;
+            // between scales further apart than binary32 reaches, a code is 0 or NaN: any factor serves
+            const float f = pow2(min(exponent_of(scale[which][i]) - e, 127));
             uint4 y = w[which][i];
             if (f != 1.0f) {  // most tokens keep their scale, and so their codes
                 float v[8];

@@ -1,0 +1,52 @@
+"""The 8-bit key/value cache at its edges: zeros from blocks of large values, lengths of zero."""
+import numpy as np
+import pytest
+import torch
+
+from .test_gpu_cache import _check_evict, _i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sp():
+    from paper_2501_16376_b200 import binding
+    yield binding
+    assert binding.sp_wait_status() == 0
+
+
+@pytest.mark.parametrize("dim,block", [(64, 16), (128, 32), (128, 64)])
+@pytest.mark.parametrize("kept", [1, 16, 40])
+def test_evicted_zeros_stay_zeros(sp, dim, block, kept):
+    """Zero tokens of blocks whose scale is large (their largest value is left behind) are kept alone,
+    beside NaN, and beside tiny values: results are equal to the definition's, bit for bit."""
+    L, heads = 200, 3
+    g = torch.Generator().manual_seed(kept)
+    K, V = torch.zeros(2, 1, L, heads, dim)
+    K[0, ::8, 0], V[0, ::8, 0] = 2000.0, -3e4                       # scales of 8 and 128
+    K[0, ::8, 1], V[0, ::8, 1] = torch.randn(dim, generator=g) * 1e3, 6e4
+    V[0, 1::4, 1, ::5] = float("nan")
+    K[0, ::8, 2], V[0, 2::4, 2] = 1.0, 2.0 ** -24
+    V[0, ::8, 2] = 448.0
+    cache = sp.KvCache.empty(1, L, heads, dim, block)
+    cache.sp_cache_append(K.half().cuda(), V.half().cuda(), _i32(0))
+    acc = torch.rand(1, heads, L, generator=g)
+    acc[..., ::8] = 0.0                                             # the large ones go
+    _check_evict(sp, cache, [L], L, acc, kept, 0)
+    # bf16 holds values large enough that the factor between two scales passes binary32's range
+    K[0, ::8], V[0, ::8] = 1e38, -3e38
+    V[0, 3::4, 0, 7] = 1e-38
+    cache = sp.KvCache.empty(1, L, heads, dim, block)
+    cache.sp_cache_append(K.bfloat16().cuda(), V.bfloat16().cuda(), _i32(0))
+    _check_evict(sp, cache, [L], L, acc, kept, 0)
+
+
+def test_attention_after_the_eviction_of_zeros(sp):
+    K, V = torch.zeros(2, 1, 16, 1, 64)
+    K[0, 0], V[0, 0] = 1e4, 1e4
+    cache, dst = sp.KvCache.empty(1, 32, 1, 64, 16), sp.KvCache.empty(1, 8, 1, 64, 16)
+    cache.sp_cache_append(K.half().cuda(), V.half().cuda(), _i32(0))
+    kept, _, lens = cache.sp_cache_evict(_i32(16), 16, torch.zeros(1, 1, 16, device="cuda"), 8, 8, dst)
+    assert kept.flatten().tolist() == list(range(8, 16))
+    O = dst.sp_cache_attention(torch.ones(1, 1, 1, 64, dtype=torch.float16, device="cuda"), lens, 8)
+    assert np.array_equal(O.cpu().numpy(), np.zeros((1, 1, 1, 64)))
