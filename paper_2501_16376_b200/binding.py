@@ -4,6 +4,9 @@ Every step of the pruning pass runs in the library's CUDA kernels.  PyTorch tens
 for device memory and streams; this module reads their ``data_ptr()``, shape and stride and
 passes them through.  If the compiled library is missing the import fails: there is no
 fallback path.
+
+A call works on the current stream, or on ``stream``.  What it makes itself (results that were not
+given, scratch memory) is then that stream's memory; inputs are ordered by the caller.
 """
 from __future__ import annotations
 
@@ -184,6 +187,32 @@ def _stream(stream) -> int:
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _torch_stream(stream):
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+
+
+def _scratch(stream, make, *args, **kw):
+    """make(*args, **kw): a tensor that only the work of a call on `stream` (None: the current one)
+    uses.  It comes from that stream's memory.  A block that the allocator hands out again on the
+    current stream may still be in use by what is pending there, and a launch on another stream
+    does not wait for that."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(_torch_stream(stream)):
+        return make(*args, **kw)
+
+
+def _result(stream, make, *args, **kw):
+    """The same for a tensor that is returned: the caller's stream counts as using it, so that it is
+    not handed out again while work there reads it."""
+    t = _scratch(stream, make, *args, **kw)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream())
+    return t
 
 
 def _ptr(t):
@@ -598,9 +627,9 @@ def sp_mx4_quantize(W: torch.Tensor, mask: torch.Tensor | None = None, codes=Non
                 or not mask.is_contiguous()):
             raise SpError(SP_ERR_SHAPE, "mask must be contiguous int32 [rows, ceil(cols/32)]")
     if codes is None:
-        codes = torch.empty(R, (n + 31) // 32 * 16, dtype=torch.uint8, device=W.device)
+        codes = _result(stream, torch.empty, R, (n + 31) // 32 * 16, dtype=torch.uint8, device=W.device)
     if scales is None:
-        scales = torch.empty(sp_mx4_scale_bytes(R, n), dtype=torch.uint8, device=W.device)
+        scales = _result(stream, torch.empty, sp_mx4_scale_bytes(R, n), dtype=torch.uint8, device=W.device)
     cptr, rows, ldc, sptr = _codes(codes, scales, n, device)
     if rows != R:
         raise SpError(SP_ERR_SHAPE, "codes have %d rows, W has %d" % (rows, R))
@@ -615,7 +644,7 @@ def sp_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, dt
     device = _current_device()
     cptr, R, ldc, sptr = _codes(codes, scales, n_cols, device)
     if W_out is None:
-        W_out = torch.empty(R, n_cols, dtype=dtype or torch.bfloat16, device=codes.device)
+        W_out = _result(stream, torch.empty, R, n_cols, dtype=dtype or torch.bfloat16, device=codes.device)
     optr, rows, n, ldo = _rows(W_out, "W_out", device)
     if (rows, n) != (R, n_cols):
         raise SpError(SP_ERR_SHAPE, "W_out must be [%d, %d]" % (R, n_cols))
@@ -624,22 +653,15 @@ def sp_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, dt
     return W_out
 
 
-def _workspace(need: int, workspace, device):
+def _workspace(need: int, workspace, device, stream):
     """(pointer, bytes, tensor that keeps it alive) of a call's scratch memory."""
     if need == 0:
         return None, 0, None
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _scratch(stream, torch.empty, need, dtype=torch.uint8, device=device)
     elif workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
         raise SpError(SP_ERR_INVALID_ARG, "the workspace needs %d contiguous bytes" % need)
     return workspace.data_ptr(), need, workspace
-
-
-def _hold(keep, workspace, stream):
-    """Scratch memory made here is not reused before the work on another stream is done."""
-    if keep is not None and workspace is None and stream is not None:
-        keep.record_stream(stream if hasattr(stream, "cuda_stream")
-                           else torch.cuda.ExternalStream(int(stream)))
 
 
 @functools.lru_cache(maxsize=4096)
@@ -659,16 +681,15 @@ def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     ptr, T, n, ldx = _rows(X, "X", device)
     cptr, R, ldc, sptr = _codes(codes, scales, n, device)
     if Y is None:
-        Y = torch.empty(T, R, dtype=X.dtype, device=X.device)
+        Y = _result(stream, torch.empty, T, R, dtype=X.dtype, device=X.device)
     yptr, rows, cols, ldy = _rows(Y, "Y", device)
     if (rows, cols) != (T, R):
         raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
     if Y.dtype != X.dtype:
         raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
-    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X.device)
+    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X.device, stream)
     _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, mode, yptr, ldy,
                              wptr, wbytes, _raw_stream(stream, device)))
-    _hold(keep, workspace, stream)
     return Y
 
 
@@ -786,7 +807,7 @@ class KvCache:
         device = _current_device()
         qs = _heads(Q, "Q", self.n_seqs, self.head_dim, device)
         if O is None:
-            O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            O = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
         os_ = _heads(O, "O", self.n_seqs, self.head_dim, device)
         if O.shape != Q.shape:
             raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
@@ -806,13 +827,12 @@ class KvCache:
                 if ld_in != ld:
                     raise SpError(SP_ERR_SHAPE, "acc_in and acc_out must have the same shape")
         need = self.sp_cache_attention_workspace(n_q, n_heads, max_len, ao is not None)
-        wptr, wbytes, keep = _workspace(need, workspace, Q.device)
+        wptr, wbytes, keep = _workspace(need, workspace, Q.device, stream)
         _check(lib.sp_cache_attention(self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads,
                                       _int32(lens, "lens", (self.n_seqs,), device), max_len,
                                       self.head_dim ** -0.5 if scale is None else scale,
                                       O.data_ptr(), os_, _ptr(lse), ai, ao, ld, wptr, wbytes,
                                       _raw_stream(stream, device)))
-        _hold(keep, workspace, stream)
         return O
 
     def sp_cache_evict(self, lens, max_len: int, acc, budget: int, recent: int, dst: "KvCache",
@@ -825,11 +845,11 @@ class KvCache:
             raise SpError(SP_ERR_SHAPE, "dst must have the same sequences")
         shape = (self.n_seqs, self.n_kv_heads, budget)
         if kept_out is None:
-            kept_out = torch.empty(shape, dtype=torch.int32, device=acc.device)
+            kept_out = _result(stream, torch.empty, shape, dtype=torch.int32, device=acc.device)
         if acc_out is None:
-            acc_out = torch.empty(shape, dtype=torch.float32, device=acc.device)
+            acc_out = _result(stream, torch.empty, shape, dtype=torch.float32, device=acc.device)
         if lens_out is None:
-            lens_out = torch.empty(self.n_seqs, dtype=torch.int32, device=acc.device)
+            lens_out = _result(stream, torch.empty, self.n_seqs, dtype=torch.int32, device=acc.device)
         ao, ld_out = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, budget, device)
         lens_shape = (self.n_seqs,)
         _check(lib.sp_cache_evict(self._c, _int32(lens, "lens", lens_shape, device), max_len, a, ld,

@@ -307,7 +307,7 @@ cache_gather_kernel(const sp_cache src, const sp_cache dst, const int32_t *__res
     }
     int block[kPieces];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) block[i] = j[i] >= 0 ? table[unsigned(j[i]) / T] : -1;  // a kept place is in the table
+    for (int i = 0; i < kPieces; ++i) block[i] = j[i] >= 0 && unsigned(j[i]) / T < src.table_cols ? table[unsigned(j[i]) / T] : -1;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         w[0][i] = w[1][i] = make_uint4(0u, 0u, 0u, 0u);
