@@ -308,7 +308,7 @@ class Context:
             return None
         ptr, R, n, ld = _matrix(W, "W")
         self._check_width(n)
-        scores = torch.empty(R, n, dtype=torch.float32, device=W.device)
+        scores = _result(stream, torch.empty, R, n, dtype=torch.float32, device=W.device)
         _check(lib.sp_score(self._h, ptr, _dtype_of(W), R, ld, scores.data_ptr(), _stream(stream)))
         return scores
 
@@ -318,9 +318,9 @@ class Context:
         ptr, R, n, ld = _matrix(W, "W")
         self._check_width(n)
         if values is None:
-            values = torch.empty(R, n // 2, dtype=W.dtype, device=W.device)
+            values = _result(stream, torch.empty, R, n // 2, dtype=W.dtype, device=W.device)
         if meta is None:
-            meta = torch.zeros(R, (n + 31) // 32, dtype=torch.int32, device=W.device)
+            meta = _result(stream, torch.zeros, R, (n + 31) // 32, dtype=torch.int32, device=W.device)
         vptr, _, _, ldv = _matrix(values, "values")
         _check(lib.sp_select_24_compressed(self._h, ptr, _dtype_of(W), R, ld, vptr, ldv,
                                            meta.data_ptr(), _stream(stream)))
@@ -330,14 +330,14 @@ class Context:
         if n != self.d_in:
             raise SpError(SP_ERR_SHAPE, "W has %d columns, context has %d" % (n, self.d_in))
 
-    def _outputs(self, W, mask, W_out, want_mask, inplace):
+    def _outputs(self, W, mask, W_out, want_mask, inplace, stream):
         R, n = W.shape
         if mask is None and want_mask:
-            mask = torch.empty(R, (n + 31) // 32, dtype=torch.int32, device=W.device)
+            mask = _result(stream, torch.empty, R, (n + 31) // 32, dtype=torch.int32, device=W.device)
         if inplace:
             W_out = W
         elif W_out is None:
-            W_out = torch.empty_like(W)
+            W_out = _result(stream, torch.empty_like, W)
         return mask, W_out
 
     # -- selection -----------------------------------------------------------
@@ -347,7 +347,7 @@ class Context:
         """Algorithm 1 on every row of W.  Returns (mask int32 [R, ceil(n/32)], W_out)."""
         ptr, R, n, ld = _matrix(W, "W")
         self._check_width(n)
-        mask, W_out = self._outputs(W, mask, W_out, want_mask, inplace)
+        mask, W_out = self._outputs(W, mask, W_out, want_mask, inplace, stream)
         optr, _, _, ldo = _matrix(W_out, "W_out")
         if params is not None:
             _check(lib.sp_select_unstructured_ex(self._h, ptr, _dtype_of(W), R, ld,
@@ -364,7 +364,7 @@ class Context:
         tensors [R, d_in].  Sequential diagnostic, meant for a few rows."""
         ptr, R, n, ld = _matrix(W, "W")
         self._check_width(n)
-        est, dev, L = (torch.empty(R, n, dtype=torch.float32, device=W.device) for _ in range(3))
+        est, dev, L = (_result(stream, torch.empty, R, n, dtype=torch.float32, device=W.device) for _ in range(3))
         _check(lib.sp_ewma_trace(self._h, ptr, _dtype_of(W), R, ld, ctypes.byref(params),
                                  est.data_ptr(), dev.data_ptr(), L.data_ptr(), _stream(stream)))
         return est, dev, L
@@ -386,7 +386,7 @@ class Context:
         """N:M selection (keep N of every M).  Returns (mask, W_out)."""
         ptr, R, n, ld = _matrix(W, "W")
         self._check_width(n)
-        mask, W_out = self._outputs(W, mask, W_out, want_mask, inplace)
+        mask, W_out = self._outputs(W, mask, W_out, want_mask, inplace, stream)
         optr, _, _, ldo = _matrix(W_out, "W_out")
         _check(lib.sp_select_nm(self._h, ptr, _dtype_of(W), R, ld, int(N), int(M), _ptr(mask),
                                 optr, ldo, _stream(stream)))
@@ -398,7 +398,7 @@ class Context:
                                      counters=None, stream=None):
         """Algorithm 1 on several matrices that read this context's input, in one call.
         Returns (masks, W_outs)."""
-        arr, k, dtype, masks, W_outs = _group(self, Ws, masks, W_outs, want_mask, inplace)
+        arr, k, dtype, masks, W_outs = _group(self, Ws, masks, W_outs, want_mask, inplace, stream)
         if params is not None:
             _check(lib.sp_select_unstructured_group_ex(self._h, arr, k, dtype, ctypes.byref(params),
                                                        _ptr(counters), _stream(stream)))
@@ -411,7 +411,7 @@ class Context:
                            want_mask=True, stream=None):
         """N:M selection of several matrices that read this context's input, in one call.
         Returns (masks, W_outs)."""
-        arr, k, dtype, masks, W_outs = _group(self, Ws, masks, W_outs, want_mask, inplace)
+        arr, k, dtype, masks, W_outs = _group(self, Ws, masks, W_outs, want_mask, inplace, stream)
         _check(lib.sp_select_nm_group(self._h, arr, k, dtype, int(N), int(M), _stream(stream)))
         return masks, W_outs
 
@@ -440,7 +440,7 @@ class Context:
                                                _ptr(mask), optr, ldo, _stream(stream)))
 
 
-def _group(ctx, Ws, masks, W_outs, want_mask, inplace):
+def _group(ctx, Ws, masks, W_outs, want_mask, inplace, stream):
     """Marshals a list of weight tensors (and optional outputs) into an sp_matrix array."""
     k = len(Ws)
     masks = list(masks) if masks is not None else [None] * k
@@ -452,7 +452,7 @@ def _group(ctx, Ws, masks, W_outs, want_mask, inplace):
         ctx._check_width(n)
         if _dtype_of(W) != dtype:
             raise SpError(SP_ERR_DTYPE, "all matrices of a group must have the same dtype")
-        masks[i], W_outs[i] = ctx._outputs(W, masks[i], W_outs[i], want_mask, inplace)
+        masks[i], W_outs[i] = ctx._outputs(W, masks[i], W_outs[i], want_mask, inplace, stream)
         optr, _, _, ldo = _matrix(W_outs[i], "W_out")
         arr[i] = Matrix(ptr, R, ld, _ptr(masks[i]), optr, ldo)
     return arr, k, dtype, masks, W_outs
@@ -486,7 +486,7 @@ def sp_finalize_multi(ctxs, stream=None):
     _check(lib.sp_finalize_multi(handles, len(ctxs), _stream(stream)))
 
 
-def _multi(ctxs, Ws, masks, W_outs, want_mask, inplace):
+def _multi(ctxs, Ws, masks, W_outs, want_mask, inplace, stream):
     """Marshals matrices with a context each into an sp_matrix array and a handle array."""
     k = len(Ws)
     if k != len(ctxs) or k < 1:
@@ -501,7 +501,7 @@ def _multi(ctxs, Ws, masks, W_outs, want_mask, inplace):
         ctx._check_width(n)
         if _dtype_of(W) != dtype:
             raise SpError(SP_ERR_DTYPE, "all matrices of a call must have the same dtype")
-        masks[i], W_outs[i] = ctx._outputs(W, masks[i], W_outs[i], want_mask, inplace)
+        masks[i], W_outs[i] = ctx._outputs(W, masks[i], W_outs[i], want_mask, inplace, stream)
         optr, _, _, ldo = _matrix(W_outs[i], "W_out")
         arr[i] = Matrix(ptr, R, ld, _ptr(masks[i]), optr, ldo)
         handles[i] = ctx._h
@@ -513,7 +513,7 @@ def sp_select_unstructured_multi(ctxs, Ws, sparsity=None, *, params: EwmaParams 
                                  counters=None, stream=None):
     """Algorithm 1 on matrices that read different layer inputs, in one call: Ws[i] is pruned
     with the statistics of ctxs[i] (contexts may repeat).  Returns (masks, W_outs)."""
-    handles, arr, k, dtype, masks, W_outs = _multi(ctxs, Ws, masks, W_outs, want_mask, inplace)
+    handles, arr, k, dtype, masks, W_outs = _multi(ctxs, Ws, masks, W_outs, want_mask, inplace, stream)
     if params is not None:
         _check(lib.sp_select_unstructured_multi_ex(handles, arr, k, dtype, ctypes.byref(params),
                                                    _ptr(counters), _stream(stream)))
@@ -527,7 +527,7 @@ def sp_select_nm_multi(ctxs, Ws, N: int, M: int, *, masks=None, W_outs=None, inp
                        want_mask=True, stream=None):
     """N:M selection of matrices that read different layer inputs, in one call: Ws[i] is pruned
     with the statistics of ctxs[i].  Returns (masks, W_outs)."""
-    handles, arr, k, dtype, masks, W_outs = _multi(ctxs, Ws, masks, W_outs, want_mask, inplace)
+    handles, arr, k, dtype, masks, W_outs = _multi(ctxs, Ws, masks, W_outs, want_mask, inplace, stream)
     _check(lib.sp_select_nm_multi(handles, arr, k, dtype, int(N), int(M), _stream(stream)))
     return masks, W_outs
 
@@ -536,7 +536,7 @@ def sp_apply_mask(W: torch.Tensor, mask: torch.Tensor, W_out: torch.Tensor | Non
                   stream=None) -> torch.Tensor:
     ptr, R, n, ld = _matrix(W, "W")
     if W_out is None:
-        W_out = torch.empty_like(W)
+        W_out = _result(stream, torch.empty_like, W)
     optr, _, _, ldo = _matrix(W_out, "W_out")
     if mask.dim() != 2 or tuple(mask.shape) != (R, (n + 31) // 32) or not mask.is_contiguous():
         raise SpError(SP_ERR_SHAPE, "mask must be contiguous [rows, ceil(cols/32)]")

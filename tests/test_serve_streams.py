@@ -123,3 +123,32 @@ def test_serving_calls_allocate_on_the_stream_they_work_on(sp, call, stream):
 def test_the_default_stream_may_be_named_by_its_handle(sp, call):
     call(sp, 0)
     assert sp.log.made and all(s is CURRENT for _, s in sp.log.made)
+
+
+def _context(sp):
+    ctx = sp.Context.__new__(sp.Context)
+    ctx.d_in, ctx._h = 64, None
+    return ctx
+
+
+def _W():
+    return torch.ones(16, 64, dtype=torch.float16)
+
+
+PRUNING = [
+    lambda sp, s: [_context(sp).sp_score(_W(), stream=s)],
+    lambda sp, s: _context(sp).sp_select_24_compressed(_W(), stream=s),
+    lambda sp, s: _context(sp).sp_select_unstructured(_W(), 0.5, stream=s),
+    lambda sp, s: _context(sp).sp_select_nm(_W(), 2, 4, stream=s),
+    lambda sp, s: _context(sp).sp_ewma_trace(_W(), sp.EwmaParams(0.1, 0.1, 1.0, 0), stream=s),
+    lambda sp, s: sum(_context(sp).sp_select_unstructured_group([_W(), _W()], 0.5, stream=s), []),
+    lambda sp, s: sum(_context(sp).sp_select_nm_group([_W(), _W()], 2, 4, stream=s), []),
+    lambda sp, s: sum(sp.sp_select_unstructured_multi([_context(sp)], [_W()], 0.5, stream=s), []),
+    lambda sp, s: sum(sp.sp_select_nm_multi([_context(sp)], [_W()], 2, 4, stream=s), []),
+    lambda sp, s: [sp.sp_apply_mask(_W(), torch.ones(16, 2, dtype=torch.int32), stream=s)],
+]
+
+
+@pytest.mark.parametrize("call", PRUNING)
+def test_pruning_calls_allocate_on_the_stream_they_work_on(sp, call):
+    _check(sp, call, SIDE)
