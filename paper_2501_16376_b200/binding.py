@@ -653,14 +653,16 @@ def sp_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, n_cols: int, dt
     return W_out
 
 
-def _workspace(need: int, workspace, device, stream):
+def _workspace(need: int, workspace, like, device: int, stream):
     """(pointer, bytes, tensor that keeps it alive) of a call's scratch memory."""
     if need == 0:
         return None, 0, None
     if workspace is None:
-        workspace = _scratch(stream, torch.empty, need, dtype=torch.uint8, device=device)
+        workspace = _scratch(stream, torch.empty, need, dtype=torch.uint8, device=like.device)
     elif workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
         raise SpError(SP_ERR_INVALID_ARG, "the workspace needs %d contiguous bytes" % need)
+    else:
+        _on_device(workspace, "the workspace", device)
     return workspace.data_ptr(), need, workspace
 
 
@@ -687,7 +689,7 @@ def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
         raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
     if Y.dtype != X.dtype:
         raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
-    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X.device, stream)
+    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X, device, stream)
     _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, mode, yptr, ldy,
                              wptr, wbytes, _raw_stream(stream, device)))
     return Y
@@ -750,6 +752,7 @@ class KvCache:
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise SpError(SP_ERR_INVALID_ARG, "table must be int32 [n_seqs, blocks]")
         _on_device(table, "table", device)
+        self.device = device
         self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
         self.n_seqs, (_, self.n_kv_heads, self.block_tokens, self.head_dim) = table.shape[0], k.shape
         ld = table.stride(0) if self.n_seqs > 1 else max(table.stride(0), table.shape[1])
@@ -757,6 +760,14 @@ class KvCache:
                               table.data_ptr(), k.shape[0], self.n_seqs, table.shape[1], ld,
                               self.n_kv_heads, self.head_dim, self.block_tokens)
         self._workspaces = {}
+
+    def _here(self, what: str = "the cache") -> int:
+        """The current device, which must be the cache's."""
+        device = _current_device()
+        if self.device != device:
+            raise SpError(SP_ERR_INVALID_ARG, "%s lies on device %d, the current one is %d"
+                          % (what, self.device, device))
+        return device
 
     @classmethod
     def empty(cls, n_seqs: int, max_tokens: int, n_kv_heads: int, head_dim: int,
@@ -773,7 +784,7 @@ class KvCache:
     def sp_cache_append(self, K, V, start, count=None, stream=None):
         """Writes K, V [n_seqs, new, kv heads, head size] at the places start[b] and following
         (start, count: int32 [n_seqs]; count defaults to all the new tokens)."""
-        device = _current_device()
+        device = self._here()
         ks = _heads(K, "K", self.n_seqs, self.head_dim, device)
         vs = _heads(V, "V", self.n_seqs, self.head_dim, device)
         if K.shape != V.shape or K.shape[2] != self.n_kv_heads:
@@ -804,7 +815,7 @@ class KvCache:
         [n_seqs]) count the call's own n_q tokens; max_len bounds them.  scale defaults to
         1 / sqrt(head size).  acc_out (float32 [n_seqs, kv heads, >= max_len]) accumulates the
         attention every token received on top of acc_in.  Returns O."""
-        device = _current_device()
+        device = self._here()
         qs = _heads(Q, "Q", self.n_seqs, self.head_dim, device)
         if O is None:
             O = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
@@ -827,7 +838,7 @@ class KvCache:
                 if ld_in != ld:
                     raise SpError(SP_ERR_SHAPE, "acc_in and acc_out must have the same shape")
         need = self.sp_cache_attention_workspace(n_q, n_heads, max_len, ao is not None)
-        wptr, wbytes, keep = _workspace(need, workspace, Q.device, stream)
+        wptr, wbytes, keep = _workspace(need, workspace, Q, device, stream)
         _check(lib.sp_cache_attention(self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads,
                                       _int32(lens, "lens", (self.n_seqs,), device), max_len,
                                       self.head_dim ** -0.5 if scale is None else scale,
@@ -839,8 +850,9 @@ class KvCache:
                        acc_out=None, kept_out=None, lens_out=None, stream=None):
         """Keeps budget tokens of every (sequence, kv head): the last `recent` and those with the
         largest acc; lays them into dst's blocks.  Returns (kept_out, acc_out, lens_out)."""
-        device = _current_device()
+        device = self._here()
         a, ld = _acc(acc, "acc", self.n_seqs, self.n_kv_heads, max_len, device)
+        dst._here("dst")
         if dst.n_seqs != self.n_seqs:
             raise SpError(SP_ERR_SHAPE, "dst must have the same sequences")
         shape = (self.n_seqs, self.n_kv_heads, budget)
