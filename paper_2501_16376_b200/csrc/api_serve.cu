@@ -198,8 +198,8 @@ sp_status sp_cache_attention(const sp_cache *cache, const void *Q, const sp_stri
     if (!valid_dtype(dtype)) return SP_ERR_DTYPE;
     if (q_strides == nullptr || o_strides == nullptr || !std::isfinite(scale)) return SP_ERR_INVALID_ARG;
     if (acc_out != nullptr && ld_acc < max_len) return SP_ERR_SHAPE;
-    if (n_q == 0 || cache->n_seqs == 0) return SP_OK;
-    if (Q == nullptr || O == nullptr || lens == nullptr) return SP_ERR_INVALID_ARG;
+    if (cache->n_seqs == 0 || (n_q == 0 && acc_out == nullptr)) return SP_OK;
+    if ((n_q > 0 && (Q == nullptr || O == nullptr)) || lens == nullptr) return SP_ERR_INVALID_ARG;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
     return launch_cache_attention(*cache, Q, *q_strides, dtype, n_q, n_heads, lens, max_len, scale, O, *o_strides, lse,
                                   acc_in, acc_out, ld_acc, workspace, static_cast<cudaStream_t>(stream));

@@ -756,6 +756,7 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     a.scale_log2 = scale * kLog2e;
     a.O = static_cast<uint16_t *>(O);
     a.lse = lse;
+    const bool no_rows = a.rows == 0;  // the second kernel moves the accumulated weights alone
     const int64_t pairs = c.n_seqs * c.n_kv_heads;
     // scores first: their loads want 16-byte boundaries
     float *at = static_cast<float *>(workspace);
@@ -774,7 +775,7 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     ClusterPdlConfig pdl(plan.join ? 1 : a.splits, dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
     CUtensorMap k_map = {}, v_map = {};
     cudaError_t e = cudaSuccess;
-    if (c.n_blocks > 0) {
+    if (c.n_blocks > 0 && !no_rows) {
         const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
         if (c.n_blocks > 0x7fffffff || pool_rows > 0x7fffffff) return SP_ERR_SHAPE;
         e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
@@ -797,14 +798,19 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     } while (0)
 #define SP_PICK(B) \
     if (c.head_dim == 64) SP_ROWS(B, 64); else SP_ROWS(B, 128);
-    if (dtype == SP_BF16) { SP_PICK(true) } else { SP_PICK(false) }
+    if (no_rows) {}
+    else if (dtype == SP_BF16) { SP_PICK(true) }
+    else { SP_PICK(false) }
 #undef SP_PICK
 #undef SP_ROWS
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
-    sp_status st = check_launch();
-    if (st != SP_OK || !plan.join) return st;
+    if (!no_rows) {
+        sp_status st = check_launch();
+        if (st != SP_OK || !plan.join) return st;
+    }
     const int64_t blocks = std::max(acc_out != nullptr ? (max_len + kJoinTokens - 1) / kJoinTokens : 1, std::min(int64_t(a.rows), int64_t(8)));
+    if (blocks == 0) return SP_OK;
     PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(kJoinThreads), stream);
     second.cfg.dynamicSmemBytes = a.rows * sizeof(float);
 #define SP_LAUNCH(R)                                                                                                 \

@@ -50,3 +50,23 @@ def test_attention_after_the_eviction_of_zeros(sp):
     assert kept.flatten().tolist() == list(range(8, 16))
     O = dst.sp_cache_attention(torch.ones(1, 1, 1, 64, dtype=torch.float16, device="cuda"), lens, 8)
     assert np.array_equal(O.cpu().numpy(), np.zeros((1, 1, 1, 64)))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_no_query_leaves_the_accumulated_weights(sp, in_place):
+    """What the definition gives for n_q = 0: acc_in up to the length, 0 past it."""
+    lens, L = [1500, 0, 70, 2000, -3], 1600
+    cache = sp.KvCache.empty(5, 1600, 2, 64, 16)
+    acc = torch.rand(5, 2, L, generator=torch.Generator().manual_seed(0))
+    want = acc.clone()
+    for b, n in enumerate(lens):
+        want[b, :, max(n, 0):] = 0
+    Q = torch.zeros(5, 0, 4, 64, dtype=torch.float16, device="cuda")
+    acc_in = acc.cuda()
+    acc_out = acc_in if in_place else torch.full_like(acc_in, 7.0)
+    O = cache.sp_cache_attention(Q, _i32(*lens), L, acc_in=acc_in, acc_out=acc_out)
+    assert O.shape == Q.shape and torch.equal(acc_out.cpu(), want)
+    cache.sp_cache_attention(Q, _i32(*lens), L, acc_out=acc_out)
+    assert (acc_out == 0).all()
+    cache.sp_cache_attention(Q, _i32(*lens), 0, acc_out=acc_out)
+    cache.sp_cache_attention(Q, _i32(*lens), L)
