@@ -100,6 +100,13 @@ __device__ __forceinline__ float exp2_fast(float x) {  // what is below 2^-126 c
     return y;
 }
 
+// A row's weights are 2^(s - reference) / sum: (reference, 1 / sum), 0 where a row sees nothing.
+// (Their logarithm in one number would lose the sum's bits beside a large reference.)
+__device__ __forceinline__ float2 norm_of(float reference, float sum) {
+    return make_float2(reference, sum == 0.0f ? 0.0f : 1.0f / sum);
+}
+__device__ __forceinline__ float weight(float s, float2 norm) { return exp2_fast(s - norm.x) * norm.y; }
+
 __device__ __forceinline__ void copy_scale(uint32_t dst, const float *src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -143,8 +150,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     extern __shared__ __align__(1024) uint8_t ring[];  // [kRing][warp][kStep]; afterwards the warps' sums
     float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
     float(*block_o)[D] = sh_o[kAttnWarps];             // the block's sum of them
-    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8], row_lse[NT * 8];
-    __shared__ float2 block_ml[NT * 8];
+    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
+    __shared__ float2 block_ml[NT * 8], row_norm[NT * 8];
     __shared__ uint64_t full[kRing], empty[kRing];
     __shared__ float2 scales[kRing][kAttnWarps];  // of K and V
     __shared__ uint32_t present[kRing][kAttnWarps];  // whether the table names a block there
@@ -564,7 +571,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 sum = fmaf(sum, exp2_fast(top - most), ml.y * exp2_fast(ml.x - most));
                 top = most;
             }
-            row_lse[threadIdx.x] = sum == 0.0f ? INFINITY : top + log2f(sum);
+            row_norm[threadIdx.x] = norm_of(top, sum);
         }
         __syncthreads();
         const int64_t pair = seq * H + head;
@@ -576,11 +583,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             if ((a.rows & 3) == 0) {
                 for (int r = 0; r < a.rows; r += 4) {
                     const float4 v = *reinterpret_cast<const float4 *>(x + r);
-                    add += exp2_fast(v.x - row_lse[r]) + exp2_fast(v.y - row_lse[r + 1]) + exp2_fast(v.z - row_lse[r + 2]) +
-                           exp2_fast(v.w - row_lse[r + 3]);
+                    add += weight(v.x, row_norm[r]) + weight(v.y, row_norm[r + 1]) + weight(v.z, row_norm[r + 2]) +
+                           weight(v.w, row_norm[r + 3]);
                 }
             } else {
-                for (int r = 0; r < a.rows; ++r) add += exp2_fast(x[r] - row_lse[r]);
+                for (int r = 0; r < a.rows; ++r) add += weight(x[r], row_norm[r]);
             }
             a.acc_out[pair * a.ld_acc + j] = sum + add;
         }
@@ -598,7 +605,7 @@ constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinTokens = kJoinThreads * kJ
 template <bool BF16, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads)
 cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t ld_acc) {
-    extern __shared__ float row_lse[];  // log2 of the sum of 2^s, +inf where a row sees nothing
+    extern __shared__ float2 join_norm[];
     const sp_cache &c = a.cache;
     const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y;
     const int64_t seq = blockIdx.z, pair = seq * H + head;
@@ -653,7 +660,7 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
                 total = fmaf(total, exp2_fast(top - most), part_sum);
                 top = most;
             }
-            if (lane == 0) row_lse[row] = total == 0.0f ? INFINITY : top + log2f(total);
+            if (lane == 0) join_norm[row] = norm_of(top, total);
         }
         __syncthreads();
 #pragma unroll
@@ -663,12 +670,12 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
             float add = 0.0f;
             if constexpr (ROWS != 0) {
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) add += exp2_fast(s[i][r] - row_lse[r]);
+                for (int r = 0; r < ROWS; ++r) add += weight(s[i][r], join_norm[r]);
             } else if (j < len) {
                 const float *at = scores + int64_t(i) * kJoinThreads * rows;
                 for (int r = 0; r < rows; ++r) {
                     const float x = __ldcs(at + r);
-                    add += exp2_fast(x - row_lse[r]);
+                    add += weight(x, join_norm[r]);
                 }
             }
             acc_out[pair * ld_acc + j] = j < len ? sum[i] + add : 0.0f;
@@ -812,10 +819,15 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     const int64_t blocks = std::max(acc_out != nullptr ? (max_len + kJoinTokens - 1) / kJoinTokens : 1, std::min(int64_t(a.rows), int64_t(8)));
     if (blocks == 0) return SP_OK;
     PdlConfig second(dim3(static_cast<unsigned>(blocks), c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(kJoinThreads), stream);
-    second.cfg.dynamicSmemBytes = a.rows * sizeof(float);
+    second.cfg.dynamicSmemBytes = a.rows * sizeof(float2);
 #define SP_LAUNCH(R)                                                                                                 \
-    e = dtype == SP_BF16 ? cudaLaunchKernelEx(&second.cfg, cache_join_kernel<true, R>, a, acc_in, acc_out, ld_acc)   \
-                         : cudaLaunchKernelEx(&second.cfg, cache_join_kernel<false, R>, a, acc_in, acc_out, ld_acc)
+    do {                                                                                                             \
+        auto *kernel = dtype == SP_BF16 ? cache_join_kernel<true, R> : cache_join_kernel<false, R>;                  \
+        static DynamicSmem limit[2];                                                                                 \
+        if (second.cfg.dynamicSmemBytes > 48 * 1024)                                                                 \
+            e = limit[dtype == SP_BF16].allow(reinterpret_cast<const void *>(kernel));                               \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&second.cfg, kernel, a, acc_in, acc_out, ld_acc);               \
+    } while (0)
     switch (a.rows) {
         case 1: SP_LAUNCH(1); break;
         case 2: SP_LAUNCH(2); break;

@@ -1,9 +1,10 @@
-"""The 8-bit key/value cache at its edges: zeros from blocks of large values, lengths of zero."""
+"""The 8-bit key/value cache at its edges: zeros from blocks of large values, no queries, huge scores."""
 import numpy as np
 import pytest
 import torch
 
-from .test_gpu_cache import _check_evict, _i32
+from . import serve_reference as ref
+from .test_gpu_cache import _check_attention, _check_evict, _filled, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,35 @@ def test_no_query_leaves_the_accumulated_weights(sp, in_place):
     assert (acc_out == 0).all()
     cache.sp_cache_attention(Q, _i32(*lens), 0, acc_out=acc_out)
     cache.sp_cache_attention(Q, _i32(*lens), L)
+
+
+@pytest.mark.parametrize("group,n_q", [(1, 1), (2, 1), (3, 1), (4, 1), (8, 1), (4, 4)])
+@pytest.mark.parametrize("L", [40, 3000])
+@pytest.mark.parametrize("score", [300.0, -2.0 ** 16, 2.0 ** 24])
+def test_accumulated_weights_of_large_scores(sp, L, score, group, n_q):
+    """Equal scores of any size give every token its share, whatever the size: the scores are one exact
+    product, equal for all tokens, so a weight is off by the roundings of its exponential and of the
+    sum of up to 3000 equal terms (below 2^-14 of itself; few are added one by one in binary32)."""
+    K = torch.zeros(2, L, 2, 64)
+    K[..., 9] = 2.0
+    Q = torch.zeros(2, n_q, 2 * group, 64)
+    Q[..., 9] = score / 2
+    cache = sp.KvCache.empty(2, L, 2, 64, 16)
+    cache.sp_cache_append(K.bfloat16().cuda(), K.bfloat16().cuda(), _i32(0, 0))
+    acc = torch.zeros(2, 2, L, device="cuda")
+    cache.sp_cache_attention(Q.bfloat16().cuda(), _i32(L, L), L, scale=1.0, acc_out=acc)
+    want = np.zeros(L)
+    for i in range(n_q):
+        end = L - n_q + i + 1
+        want[:end] += group / end
+    assert (np.abs(acc.cpu().double().numpy() / want - 1) <= 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("heads,group,n_q,lens", [(2, 4, 34, [200, 33, 5]), (1, 1, 129, [129, 300]), (1, 5, 103, [400]),
+                                                  (1, 1, 8192, [700])])
+def test_many_query_rows(sp, heads, group, n_q, lens, dtype):
+    cache = _filled(sp, lens, heads, 64, 16)
+    Q = torch.randn(len(lens), n_q, heads * group, 64, generator=torch.Generator().manual_seed(n_q)).to(dtype)
+    acc_in = torch.rand(len(lens), heads, max(lens), generator=torch.Generator().manual_seed(1)).cuda()
+    _check_attention(sp, cache, Q, lens, max(lens), acc_in=acc_in)
