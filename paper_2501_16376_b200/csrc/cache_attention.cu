@@ -41,7 +41,7 @@ namespace {
 constexpr int kAttnWarps = 4;
 constexpr int kRing = 3;           // stages of 16 tokens for every warp
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLowest = -1e30f;  // running maximum before any score
+constexpr float kLowest = -3.4028234663852886e38f;  // running maximum before any score: no finite score lies below
 constexpr float kLift = 7.0f;   // the reference lies this far (in powers of two) below the running maximum
 constexpr float kRaise = 8.0f;  // how far a score may exceed the running maximum
 constexpr float kRest = 4096.0f;  // factor of a weight's second part

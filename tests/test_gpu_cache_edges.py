@@ -103,3 +103,29 @@ def test_many_query_rows(sp, heads, group, n_q, lens, dtype):
     Q = torch.randn(len(lens), n_q, heads * group, 64, generator=torch.Generator().manual_seed(n_q)).to(dtype)
     acc_in = torch.rand(len(lens), heads, max(lens), generator=torch.Generator().manual_seed(1)).cuda()
     _check_attention(sp, cache, Q, lens, max(lens), acc_in=acc_in)
+
+
+@pytest.mark.parametrize("L", [1, 20, 3000])
+@pytest.mark.parametrize("size", [1e15, 1e18])
+def test_scores_of_any_finite_size_are_scores(sp, L, size):
+    """Queries and keys whose products are far below any ordinary score (-1e30, -1e36, equal for all
+    tokens): the weights are 1 / L all the same, and lse is the score."""
+    g = torch.Generator().manual_seed(L)
+    K, V = torch.zeros(1, L, 2, 64), torch.randn(1, L, 2, 64, generator=g)
+    K[..., 3] = -size
+    Q = torch.zeros(1, 1, 4, 64)
+    Q[..., 3] = size
+    K, V, Q = K.bfloat16(), V.bfloat16(), Q.bfloat16()
+    cache = sp.KvCache.empty(1, L, 2, 64, 32)
+    cache.sp_cache_append(K.cuda(), V.cuda(), _i32(0))
+    stored = ref.PlainCache(cache)
+    score = stored.dense("k", 0, 0, 1)[0][0, 3] * float(Q[0, 0, 0, 3])
+    lse, acc = torch.zeros(1, 1, 4, device="cuda"), torch.zeros(1, 2, L, device="cuda")
+    for out in (acc, None):
+        O = cache.sp_cache_attention(Q.cuda(), _i32(L), L, scale=1.0, lse=lse, acc_out=out).cpu().double()
+        # weights 1/L, sums in binary32 and one rounding to bf16
+        want = np.stack([stored.dense("v", 0, h // 2, L)[0].mean(0) for h in range(4)])
+        mag = np.stack([np.abs(stored.dense("v", 0, h // 2, L)[0]).mean(0) for h in range(4)])
+        assert (np.abs(O.numpy()[0, 0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -17 * mag).all()
+        assert np.abs(lse.cpu().double().numpy() / score - 1).max() <= 2.0 ** -20
+    assert (acc.cpu() * L / 2 - 1).abs().max() <= 2.0 ** -17
