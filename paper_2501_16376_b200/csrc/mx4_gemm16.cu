@@ -5,8 +5,9 @@
 // type on the way to the tensor cores.  In bf16 that is exact (4-bit codes and powers of two fit at
 // every scale).  binary16 has not the range, so a row of V is kept relative to its largest scale R:
 // V = code * 2^(byte - R + 13), 49152 at most, and the sums are multiplied by 2^(R - 140) when they
-// leave; blocks whose scale lies more than 2^36 below the row's largest lose bits that are as far
-// below the row's largest products.
+// leave.  That is exact for scales down to 2^36 below the largest.  Rows whose scales lie further
+// apart (their small weights count where the activations of the large ones are 0) are summed again
+// at the end of the block, in binary32 from the codes; a block without such a row only looks at a flag.
 //
 // The weights are the 128 rows of a tile because that side has to be converted, every weight once for
 // up to 160 tokens, and because that operand may lie in tensor memory: a thread converts 128 columns
@@ -20,7 +21,8 @@
 //
 // Bound by the tensor core and the thread that feeds it: 128 tokens take 520 cycles of products a stage,
 // and its wait, even for what is there already, 140 more.  Measured (f16): 333 x 4096 x 11008
-// 28.3 us (1060 TFLOP/s; two rounds of tiles, the second three quarters full).
+// 28.8 us (1040 TFLOP/s; two rounds of tiles, the second three quarters full; 28.4 without the span of
+// the scales); 73 us with one row that is summed again, 4.5 ms with all.
 #include <algorithm>
 
 #include "mx4_common.cuh"
@@ -48,7 +50,10 @@ struct Gemm16Tile {
 };
 
 struct Gemm16Args {
-    const uint8_t *scales;
+    const uint16_t *X;
+    int64_t ldx, n_cols;
+    const uint8_t *codes, *scales;
+    int64_t ldc;
     uint16_t *Y;
     int64_t n_tokens, n_rows, ldy;
     int tile_cols;    // scale tiles along the columns
@@ -56,6 +61,25 @@ struct Gemm16Args {
     int tile_tokens;  // tokens of a tile, a multiple of 16
     int row_tiles, tiles;
     int slices;       // blocks of a cluster that share a tile, each with a part of the columns
+};
+
+constexpr int kMostSpan = 36;  // binary orders between a row's scales that binary16 holds exactly
+
+// Largest and least scale byte of a row, from words of four blocks.  A block of NaN (byte 255) has no
+// say in the largest: one more, modulo 256, makes it 0; a byte 0, the scale of a block of zeros (and
+// of values too small for binary16 products), has none in the least: one less makes it 255.
+struct ScaleSpan {
+    uint32_t most = 0, least = 0xffffffffu;
+    __device__ __forceinline__ void add(uint32_t w) {
+        most = __vmaxu4(most, ((w & 0x7f7f7f7fu) + 0x01010101u) ^ (w & 0x80808080u));
+        least = __vminu4(least, ((w | 0x80808080u) - 0x01010101u) ^ (~w & 0x80808080u));
+    }
+    static __device__ __forceinline__ int largest(uint32_t w) {
+        w = __vmaxu4(w, w >> 16);
+        return static_cast<int>(max(w & 0xffu, (w >> 8) & 0xffu));
+    }
+    __device__ __forceinline__ int top() const { return max(largest(most) - 1, 0); }
+    __device__ __forceinline__ int bottom() const { return 256 - largest(~least); }
 };
 
 // 2^e as binary16 bits, 0 below its range.
@@ -96,7 +120,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[kSlots], empty[kSlots], code_full[kCodeSlots], code_empty[kCodeSlots];
     __shared__ uint64_t acc_full[2], acc_free, last_full, top_full[8], drained;
-    __shared__ uint32_t tmem_base, failed;
+    __shared__ uint32_t tmem_base, failed, wide_rows, wide_mask[4];
     // Largest scale byte of a row, for eight tiles in turn.  A group may have no stage of a tile and
     // then does not look at it; it has one within four tiles, and the tile after the next is the last
     // that is published before it is converted, so no barrier is two phases ahead of a group.
@@ -121,7 +145,7 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         mbar_init(smem_addr(&last_full), 1);
         for (int i = 0; i < 8; ++i) mbar_init(smem_addr(&top_full[i]), 128);
         mbar_init(smem_addr(&drained), 1);
-        failed = 0u;
+        failed = wide_rows = 0u;
         mbar_fence_init();
     }
     if (warp == 2) tmem_alloc(&tmem_base, kTmemColumns);
@@ -328,15 +352,11 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
         // the largest scale byte of this thread's row in a tile
         auto find_top = [&](int tile, int c) {
             const uint8_t *s = a.scales + int64_t(tile % a.row_tiles) * a.tile_cols * kMx4TileBytes + lane * 16 + quarter * 4;
-            uint32_t most = 0;
+            ScaleSpan span;
 #pragma unroll 32
-            for (int i = 0; i < a.tile_cols; ++i) {
-                uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(s + int64_t(i) * kMx4TileBytes));
-                w &= ~__vcmpeq4(w, 0xffffffffu);  // a block of NaN has no say
-                most = __vmaxu4(most, w);
-            }
-            most = __vmaxu4(most, most >> 16);
-            row_top[c & 7][quarter * 32 + lane] = static_cast<int>(max(most & 0xffu, (most >> 8) & 0xffu));
+            for (int i = 0; i < a.tile_cols; ++i) span.add(__ldg(reinterpret_cast<const uint32_t *>(s + int64_t(i) * kMx4TileBytes)));
+            row_top[c & 7][quarter * 32 + lane] = span.top();
+            if (span.top() - span.bottom() > kMostSpan) wide_rows = 1u;
             mbar_arrive(smem_addr(&top_full[c & 7]));
         };
         if (!BF16 && unit < a.tiles) find_top(unit, 0);
@@ -385,6 +405,64 @@ mx4_gemm16_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_consta
             }
         }
         cluster_sync();  // no block leaves while its sums are read
+    }
+    // rows whose scales lie further apart than binary16 holds: the warps of the blocks that share a tile
+    // take a (row, token) each
+    if constexpr (!BF16) {
+        if (wide_rows == 0u) return;
+        constexpr int kWarps = kThreads / 32;
+        for (int tile = unit; tile < a.tiles; tile += units) {
+            const int64_t m = tile % a.row_tiles, row0 = m * kMx4TileRows, token0 = int64_t(tile / a.row_tiles) * a.tile_tokens;
+            const int tokens = static_cast<int>(min(int64_t(a.tile_tokens), a.n_tokens - token0));
+            const uint8_t *const tile_scales = a.scales + m * a.tile_cols * kMx4TileBytes;
+            auto row_scales = [&](int r) { return tile_scales + (r & 31) * 16 + (r >> 5) * 4; };
+            if (threadIdx.x < 4) wide_mask[threadIdx.x] = 0u;
+            __syncthreads();
+            for (int r = warp; r < kMx4TileRows && row0 + r < a.n_rows; r += kWarps) {
+                ScaleSpan span;
+                for (int i = lane; i < a.tile_cols; i += 32)
+                    span.add(*reinterpret_cast<const uint32_t *>(row_scales(r) + int64_t(i) * kMx4TileBytes));
+                const int orders = __reduce_max_sync(kFullWarp, span.top()) - __reduce_min_sync(kFullWarp, span.bottom());
+                if (orders > kMostSpan && lane == 0) atomicOr(&wide_mask[r >> 5], 1u << (r & 31));
+            }
+            __syncthreads();
+            for (int r = 0; r < kMx4TileRows; ++r) {
+                if (((wide_mask[r >> 5] >> (r & 31)) & 1u) == 0u) continue;
+                const uint8_t *const codes_of = a.codes + (row0 + r) * a.ldc, *const scales_of = row_scales(r);
+                constexpr int kEach = 4;  // tokens a warp takes together
+                for (int t = (rank * kWarps + warp) * kEach; t < tokens; t += slices * kWarps * kEach) {
+                    float sum[kEach] = {};
+                    for (int64_t c = lane * 8; c < a.n_cols; c += 256) {
+                        uint32_t h[4], p[kEach][4];
+#pragma unroll
+                        for (int k = 0; k < kEach; ++k) {
+                            const uint16_t *const x = a.X + (token0 + min(t + k, tokens - 1)) * a.ldx;  // on 16-byte boundaries
+                            if (c + 8 <= a.n_cols) load8<true, false>(x, c, a.n_cols, p[k]);
+                            else load8<false, false>(x, c, a.n_cols, p[k]);
+                        }
+                        mx4_unpack8(*reinterpret_cast<const uint32_t *>(codes_of + (c >> 1)), h);
+                        const float scale = mx4_scale(scales_of[(c >> 7) * kMx4TileBytes + ((c >> 5) & 3)]);
+#pragma unroll
+                        for (int k = 0; k < kEach; ++k) {
+                            float part = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float2 v = unpack2<false>(h[i]), u = unpack2<false>(p[k][i]);
+                                part = fmaf(v.y, u.y, fmaf(v.x, u.x, part));
+                            }
+                            sum[k] = fmaf(scale, part, sum[k]);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) {
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) sum[k] += __shfl_xor_sync(kFullWarp, sum[k], o);
+                        if (lane == 0 && t + k < tokens) a.Y[(token0 + t + k) * a.ldy + row0 + r] = __half_as_ushort(__float2half_rn(sum[k]));
+                    }
+                }
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -460,6 +538,11 @@ sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t s
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return cuda_fail(e);
     Gemm16Args a = {};
+    a.X = static_cast<const uint16_t *>(X);
+    a.ldx = ldx;
+    a.n_cols = p.n_cols;
+    a.codes = p.codes;
+    a.ldc = p.ldc;
     a.scales = p.scales;
     a.Y = static_cast<uint16_t *>(p.Y);
     a.n_tokens = p.n_tokens;
