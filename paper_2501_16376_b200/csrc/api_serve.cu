@@ -62,11 +62,11 @@ cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 
 constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens of a 4-bit product
 
-// Whether a product takes the kernels that tile over tokens: from 9 tokens on, the columns of one
-// mma of the streaming kernel.  (At 8 tokens it is ahead, bf16 activations: 7.2 us against 9.5 for
-// 4096 x 4096, 14.8 against 18.1 for 4096 x 14336; with two such columns, at 16 tokens, it took 9.3
-// against 9.9 and 22.8 against 18.6.)
-static bool takes_tiles(int64_t n_tokens) { return n_tokens > 8; }
+// Whether a product takes the kernels that tile over tokens: when they are more than the columns of
+// one mma of the streaming kernel.  (At 8 tokens that one is ahead, 16-bit activations in bf16: 7.2 us
+// against 9.5 for 4096 x 4096, 14.8 against 18.1 for 4096 x 14336; with two such columns, at 16
+// tokens, it took 9.3 against 9.9 and 22.8 against 18.6, and is not kept for the small difference.)
+static bool takes_tiles(int64_t n_tokens) { return n_tokens > kMx4StreamTokens; }
 
 static sp_status check_codes(const void *codes, int64_t ldc, const void *scales, int64_t n_cols) {
     if (codes == nullptr || scales == nullptr) return SP_ERR_INVALID_ARG;

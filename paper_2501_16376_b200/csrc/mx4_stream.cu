@@ -322,6 +322,7 @@ mx4_stream_kernel(const __grid_constant__ CUtensorMap codes_map, const StreamArg
 }
 
 sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
+    static_assert(kMx4StreamTokens == kTokens, "the entry point sends up to a product's columns here");
     CUtensorMap map;
     cudaError_t e = encode_byte_tiles(&map, p.codes, p.n_rows, mx4_blocks(p.n_cols) * 16, p.ldc, kMx4TileRows);
     if (e != cudaSuccess) return cuda_fail(e);
@@ -330,6 +331,9 @@ sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return cuda_fail(e);
     StreamArgs a = {};
+    a.X = static_cast<const uint16_t *>(p.X);
+    a.Y = static_cast<uint16_t *>(p.Y);
+    a.n_tokens = p.n_tokens;
     a.ldx = p.ldx;
     a.n_cols = p.n_cols;
     a.n_rows = p.n_rows;
@@ -351,16 +355,9 @@ sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream) {
     ClusterPdlConfig pdl(a.slices, dim3(static_cast<unsigned>(row_tiles * a.slices)), dim3(kWarps * 32 + 32), stream);
     pdl.cfg.dynamicSmemBytes = kStages * (kCodeBytes + kStageTiles * kMx4TileBytes) +
                                kTokens * (a.chunk_stages * 1024 + 64 + a.chunk_stages * 8);
-    for (int64_t t0 = 0; t0 < p.n_tokens; t0 += kTokens) {
-        a.X = static_cast<const uint16_t *>(p.X) + t0 * p.ldx;
-        a.Y = static_cast<uint16_t *>(p.Y) + t0 * p.ldy;
-        a.n_tokens = min(int64_t(kTokens), p.n_tokens - t0);
-        e = cudaLaunchKernelEx(&pdl.cfg, kernel, map, a);
-        if (e != cudaSuccess) return cuda_fail(e);
-        sp_status st = check_launch();
-        if (st != SP_OK) return st;
-    }
-    return SP_OK;
+    e = cudaLaunchKernelEx(&pdl.cfg, kernel, map, a);
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
 }
 
 }  // namespace sp

@@ -262,7 +262,8 @@ struct Mx4Product {
     sp_dtype dtype;
     bool quantize_x;  // SP_MX4_A4
 };
-// mx4_stream.cu: few tokens, the weights stream by once for every 8
+// mx4_stream.cu: up to 8 tokens, the weights stream by once
+constexpr int kMx4StreamTokens = 8;
 sp_status launch_mx4_stream(const Mx4Product &p, cudaStream_t stream);
 // mx4_gemm.cu: both operands in 4 bits (quantises X into the workspace first)
 int64_t mx4_gemm_workspace(int64_t n_tokens, int64_t n_cols);
