@@ -129,3 +129,33 @@ def test_scores_of_any_finite_size_are_scores(sp, L, size):
         assert (np.abs(O.numpy()[0, 0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -17 * mag).all()
         assert np.abs(lse.cpu().double().numpy() / score - 1).max() <= 2.0 ** -20
     assert (acc.cpu() * L / 2 - 1).abs().max() <= 2.0 ** -17
+
+
+def test_captured_cache_calls_leave_the_same_bits(sp):
+    """A decoding step of append, attention and eviction in one graph: lengths are read on the device."""
+    B, L, H, D = 2, 600, 2, 128
+    g = torch.Generator().manual_seed(0)
+    K, V = (torch.randn(B, L, H, D, generator=g).half().cuda() for _ in range(2))
+    k, v, q = (torch.randn(B, 1, n, D, generator=g).half().cuda() for n in (H, H, 4 * H))
+    start, lens = _i32(500, 30), _i32(501, 31)
+
+    def fresh():
+        cache = sp.KvCache.empty(B, 640, H, D, 32)
+        cache.sp_cache_append(K, V, _i32(0, 0))
+        return cache, sp.KvCache.empty(B, 64, H, D, 32), torch.zeros(B, H, 640, device="cuda")
+
+    def step(cache, dst, acc):
+        cache.sp_cache_append(k, v, start)
+        O = cache.sp_cache_attention(q, lens, 640, acc_in=acc, acc_out=acc)
+        return (O, *cache.sp_cache_evict(lens, 640, acc, 64, 4, dst), dst.k, dst.v, dst.k_scale, dst.v_scale)
+    a, b = fresh(), fresh()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(*b)
+    for _ in range(3):
+        want = [t.clone() for t in step(*a)]
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(want, outs))
+        start += 1
+        lens += 1
