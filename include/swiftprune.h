@@ -438,7 +438,8 @@ sp_status sp_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *sc
  *   SP_MX4_A4    X quantised like the weights first, 32 channels at a time (what long prompts
  *                use: both operands then go to the 4-bit tensor cores as they are).
  * workspace: sp_mx4_linear_workspace bytes of device memory, 16-byte aligned, contents arbitrary
- * before and after (NULL where that is 0).  n_cols >= 1.  Y must not overlap X or the workspace.
+ * before and after (NULL where that is 0, and with SP_MX4_A16 where X is 16-byte aligned and ldx a
+ * multiple of 8: only other rows are copied there).  n_cols >= 1.  Y must not overlap X or the workspace.
  */
 typedef enum { SP_MX4_A16 = 0, SP_MX4_A4 = 1 } sp_mx4_mode;
 sp_status sp_mx4_linear_workspace(int64_t n_tokens, int64_t n_rows, int64_t n_cols, int mode,

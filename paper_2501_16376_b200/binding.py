@@ -689,7 +689,10 @@ def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
         raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
     if Y.dtype != X.dtype:
         raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
-    wptr, wbytes, keep = _workspace(sp_mx4_linear_workspace(T, R, n, mode), workspace, X, device, stream)
+    need = sp_mx4_linear_workspace(T, R, n, mode)
+    if mode == SP_MX4_A16 and ptr % 16 == 0 and ldx % 8 == 0:
+        need = 0
+    wptr, wbytes, keep = _workspace(need, workspace, X, device, stream)
     _check(lib.sp_mx4_linear(ptr, _dtype_of(X), T, ldx, cptr, ldc, sptr, R, n, mode, yptr, ldy,
                              wptr, wbytes, _raw_stream(stream, device)))
     return Y

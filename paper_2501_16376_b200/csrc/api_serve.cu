@@ -151,6 +151,7 @@ sp_status sp_mx4_linear(const void *X, sp_dtype dtype, int64_t n_tokens, int64_t
     if (X == nullptr || Y == nullptr) return SP_ERR_INVALID_ARG;
     st = check_codes(codes, ldc, scales, n_cols);
     if (st != SP_OK) return st;
+    if (mode == SP_MX4_A16 && mx4_gemm16_reads(X, ldx)) need = 0;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
     const Mx4Product p{X, n_tokens, ldx, codes, ldc, scales, n_rows, n_cols, Y, ldy, dtype, mode == SP_MX4_A4};
     if (takes_tiles(n_tokens))

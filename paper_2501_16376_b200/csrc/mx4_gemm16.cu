@@ -518,11 +518,13 @@ static cudaError_t launch_gemm16(const CUtensorMap &x_map, const CUtensorMap &w_
 
 int64_t mx4_gemm16_workspace(int64_t n_tokens, int64_t n_cols) { return n_tokens * ((n_cols + 7) / 8 * 8) * 2; }
 
+bool mx4_gemm16_reads(const void *X, int64_t ldx) { return aligned16(X) && ldx % 8 == 0; }
+
 sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t stream) {
     const void *X = p.X;
     int64_t ldx = p.ldx;
     cudaError_t e;
-    if (!aligned16(X) || ldx % 8 != 0) {
+    if (!mx4_gemm16_reads(X, ldx)) {
         ldx = (p.n_cols + 7) / 8 * 8;
         if (p.n_tokens > 0x7fffffff) return SP_ERR_SHAPE;
         PdlConfig copy(dim3(static_cast<unsigned>(p.n_tokens)), dim3(256), stream);

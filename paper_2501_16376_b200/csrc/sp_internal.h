@@ -270,6 +270,7 @@ int64_t mx4_gemm_workspace(int64_t n_tokens, int64_t n_cols);
 sp_status launch_mx4_gemm(const Mx4Product &p, void *workspace, cudaStream_t stream);
 // mx4_gemm16.cu: 16-bit activations (the workspace takes rows that TMA cannot read)
 int64_t mx4_gemm16_workspace(int64_t n_tokens, int64_t n_cols);
+bool mx4_gemm16_reads(const void *X, int64_t ldx);  // whether TMA reads the rows as they are
 sp_status launch_mx4_gemm16(const Mx4Product &p, void *workspace, cudaStream_t stream);
 
 // cache_append.cu, cache_attention.cu, cache_evict.cu: the 8-bit key/value cache
