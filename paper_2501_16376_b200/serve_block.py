@@ -23,7 +23,7 @@ import torch
 from . import binding as sp
 from . import synth
 
-#: head size and kv heads by (model width, width of its k projection)
+#: head size by model width (64 for any other)
 HEAD_DIM = {1024: 64, 4096: 128, 5120: 128}
 
 
@@ -80,6 +80,9 @@ class ServedBlock:
         """Evicts down to the budget if n more tokens do not fit."""
         if self.length + n <= self.capacity:
             return
+        if min(self.length, self.budget) + n > self.capacity:
+            raise ValueError("%d tokens do not fit beside the %d kept of a cache of %d"
+                             % (n, min(self.length, self.budget), self.capacity))
         lens = torch.full((self.n_seqs,), self.length, dtype=torch.int32, device="cuda")
         _, _, kept = self.cache.sp_cache_evict(lens, self.length, self.acc[0], self.budget, self.recent,
                                                self.spare, acc_out=self.acc[1])
@@ -111,6 +114,8 @@ class ServedBlock:
 def run(w: synth.Workload, n_seqs: int, prompt: int, steps: int, budget: int, chunk: int = 32,
         recent: int = 16, sparsity: float = 0.5):
     """Takes a prompt, generates steps tokens; returns (block, outputs of the steps, report)."""
+    if min(n_seqs, prompt, steps, chunk) < 1 or budget < 0:
+        raise ValueError("sequences, prompt, steps and chunk are at least 1, the budget at least 0")
     capacity = max(prompt, budget + chunk)
     block = ServedBlock(w, n_seqs, capacity, budget, min(recent, budget), sparsity=sparsity)
     g = torch.Generator(device="cuda").manual_seed(synth.tensor_seed(w.seed, w.name, "serve"))
