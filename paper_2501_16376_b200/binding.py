@@ -689,6 +689,8 @@ def sp_mx4_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
         raise SpError(SP_ERR_SHAPE, "Y must be [%d, %d]" % (T, R))
     if Y.dtype != X.dtype:
         raise SpError(SP_ERR_DTYPE, "X and Y must have the same dtype")
+    if yptr == ptr and ptr:
+        raise SpError(SP_ERR_INVALID_ARG, "Y is memory apart from X")
     need = sp_mx4_linear_workspace(T, R, n, mode)
     if mode == SP_MX4_A16 and ptr % 16 == 0 and ldx % 8 == 0:
         need = 0
@@ -866,11 +868,12 @@ class KvCache:
         if lens_out is None:
             lens_out = _result(stream, torch.empty, self.n_seqs, dtype=torch.int32, device=acc.device)
         ao, ld_out = _acc(acc_out, "acc_out", self.n_seqs, self.n_kv_heads, budget, device)
-        lens_shape = (self.n_seqs,)
-        _check(lib.sp_cache_evict(self._c, _int32(lens, "lens", lens_shape, device), max_len, a, ld,
-                                  budget, recent, dst._c,
-                                  _int32(kept_out, "kept_out", shape, device), ao, ld_out,
-                                  _int32(lens_out, "lens_out", lens_shape, device),
+        n = _int32(lens, "lens", (self.n_seqs,), device)
+        no = _int32(lens_out, "lens_out", (self.n_seqs,), device)
+        if (n == no and n) or (a == ao and a):
+            raise SpError(SP_ERR_INVALID_ARG, "lens_out and acc_out are memory apart from lens and acc")
+        _check(lib.sp_cache_evict(self._c, n, max_len, a, ld, budget, recent, dst._c,
+                                  _int32(kept_out, "kept_out", shape, device), ao, ld_out, no,
                                   _raw_stream(stream, device)))
         return kept_out, acc_out, lens_out
 

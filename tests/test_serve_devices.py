@@ -83,3 +83,20 @@ def test_a_workspace_of_another_device(sp):
     with pytest.raises(sp.SpError):
         attend(On1)
     assert sp.calls == ["sp_mx4_linear", "sp_cache_attention"]
+
+
+def test_outputs_that_the_kernels_read_beside_writing_them(sp):
+    """Kernels of one call read lens, acc and X in some blocks while others write the outputs."""
+    src, dst = _cache(sp, On0, 0), _cache(sp, On0, 0)
+    lens, acc = _t(On0, 2, dtype=torch.int32), _t(On0, 2, 2, 32, dtype=torch.float32)
+    evict = lambda **kw: src.sp_cache_evict(lens, 32, acc, 32, 4, dst, **{
+        **dict(kept_out=_t(On0, 2, 2, 32, dtype=torch.int32), acc_out=_t(On0, 2, 2, 32, dtype=torch.float32),
+               lens_out=_t(On0, 2, dtype=torch.int32)), **kw})
+    evict()
+    for kw in (dict(lens_out=lens), dict(acc_out=acc)):
+        with pytest.raises(sp.SpError):
+            evict(**kw)
+    X, codes, scales = _t(On0, 64, 64), _t(On0, 64, 32, dtype=torch.uint8), _t(On0, 512, dtype=torch.uint8)
+    with pytest.raises(sp.SpError):
+        sp.sp_mx4_linear(X, codes, scales, Y=X)
+    assert sp.calls == ["sp_cache_evict"]
