@@ -487,11 +487,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         }
     }
 
-    // a block that gave up still has copies in flight
-    if (failed != 0u && threadIdx.x == 0)
-        for (int i = 0; i < 2 * kRing; ++i) mbar_wait(smem_addr(&full[i % kRing]), i / kRing);
     // the warps' parts meet in shared memory (the ring's: every copy has been waited for)
     __syncthreads();
+    if (failed != 0u) {  // a block that gave up still has copies in flight; no warp starts any more
+        if (threadIdx.x == 0)
+            for (int i = 0; i < 2 * kRing; ++i) mbar_wait(smem_addr(&full[i % kRing]), i / kRing);
+        __syncthreads();
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
