@@ -500,7 +500,8 @@ sp_status sp_cache_append(const sp_cache *cache /* host struct */, const void *K
  * consecutive heads share a kv head.  A query that sees no token gives 0 and lse -inf.  What lies
  * in the cache past a query's place takes no part, whatever it is.  max_len >= every lens[b]
  * (tokens past it are ignored).  lse (nullable): [n_seqs, n_q, n_heads], log of the sum of
- * exp(scale * q . k).
+ * exp(scale * q . k).  Scores and sums are binary32; the weights enter their product to 2^-22 of
+ * themselves and 2^-44 of the row's largest.
  * acc_out (nullable) [n_seqs, n_kv_heads, ld_acc], ld_acc >= max_len, accumulates the attention
  * that every token received, for sp_cache_evict:
  *     acc_out[b, g, j] = acc_in[b, g, j] + sum of p[j] over the queries and the heads of group g

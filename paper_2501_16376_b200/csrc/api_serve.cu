@@ -63,9 +63,11 @@ cudaError_t encode_half_tiles(CUtensorMap *map, const void *base, int64_t rows, 
 constexpr int64_t kMaxMx4Side = int64_t(1) << 30;  // rows, columns and tokens of a 4-bit product
 
 // Whether a product takes the kernels that tile over tokens: when they are more than the columns of
-// one mma of the streaming kernel.  (At 8 tokens that one is ahead, 16-bit activations in bf16: 7.2 us
-// against 9.5 for 4096 x 4096, 14.8 against 18.1 for 4096 x 14336; with two such columns, at 16
-// tokens, it took 9.3 against 9.9 and 22.8 against 18.6, and is not kept for the small difference.)
+// one mma of the streaming kernel.  bf16, 4096 columns: 8 tokens there against 9 in tiles take 6.9 and
+// 9.1 us for 4096 rows, 14.4 and 18.0 for 14336.  With 4-bit activations they take 7.2 and 9.0, but
+// 15.5 and 12.8: the rule does not tell the two modes apart, and large matrices lose by it there.
+// (With two such columns, at 16 tokens, the streaming kernel took 9.3 against 9.9 and 22.8 against
+// 18.6, and is not kept for the small difference.)
 static bool takes_tiles(int64_t n_tokens) { return n_tokens > kMx4StreamTokens; }
 
 static sp_status check_codes(const void *codes, int64_t ldc, const void *scales, int64_t n_cols) {

@@ -26,8 +26,8 @@
 // that it reaches 2^15 and uses binary16's range, and its second part is multiplied by 2^12: together
 // they hold a weight to 2^-22 of itself down to 2^-22 of the largest, and to 2^-44 of the largest
 // below.  (A token with most of the attention and a value near 0 leaves an output that is made of
-// small weights.)  Against one part for bf16 outputs, and two parts within 2^-32 of the largest for
-// f16, this costs nothing up to 4 rows, and more above: 32 x 8191 tokens of 8 heads without weights
+// small weights.)  Against one part for bf16 outputs, and two parts that ended at 2^-25 of the
+// largest for f16, this costs nothing up to 4 rows, and more above: 32 x 8191 tokens of 8 heads without weights
 // take 85 us with 4 rows, 98 with 8 (93), 164 with 16 (139 and 157).
 #include <algorithm>
 
@@ -713,6 +713,7 @@ cache_join_kernel(const AttnArgs a, const float *acc_in, float *acc_out, int64_t
 // blocks run at once, 4 an SM, and the second kernel has the device to itself: 32 x 8191 tokens of
 // 8 heads with weights take 102 us (5.0 TB/s), in clusters 115 to 117 (blocks of a cluster start and end
 // together).
+// The counts are those of a B200's 148 SMs: the workspace is asked for without a device.
 struct AttentionPlan {
     int row_tiles, splits;
     bool join;  // a second kernel joins the splits

@@ -10,7 +10,7 @@
 // passes.  Gathering: a block of threads lays block_tokens kept tokens of one head into a new
 // cache block, K and V, the scales found from the codes it already holds in registers.  Bound by
 // memory: 4 bytes read per token, and 2 * head_dim read and written per kept one.  Measured: 8 x 32768
-// tokens of 8 heads to 4096 46.5 us, of which some 20 are the selection's chain of barriers and
+// tokens of 8 heads to 4096 47.0 us, of which some 20 are the selection's chain of barriers and
 // remote counts (several copies of the first digit's counts did not shorten it).
 #include <algorithm>
 
