@@ -45,6 +45,7 @@ constexpr float kLowest = -3.4028234663852886e38f;  // running maximum before an
 constexpr float kLift = 7.0f;   // the reference lies this far (in powers of two) below the running maximum
 constexpr float kRaise = 8.0f;  // how far a score may exceed the running maximum
 constexpr float kRest = 4096.0f;  // factor of a weight's second part
+constexpr float kQueryRest = 1099511627776.0f;  // 2^40, of a query's
 
 struct AttnArgs {
     sp_cache cache;
@@ -138,46 +139,82 @@ __device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row
 
 }  // namespace
 
-// NT: tiles of 8 rows.  TWICE (at most 4 rows): the rows stand twice in their tile, and the second
-// time take their weights' second parts, so that one product serves both parts.
+// What a block keeps in shared memory beside the ring, for the two functions that work on it.  (Single
+// variables: as members of one object they cost the loop registers, and the long decoding case 2 %.)
+template <int D, int NT>
+struct AttnShared {
+    float (&m)[kAttnWarps][NT * 8], (&l)[kAttnWarps][NT * 8];  // of the warps
+    float2 (&block_ml)[NT * 8], (&row_norm)[NT * 8];
+    uint64_t (&full)[kRing], (&empty)[kRing];
+    float2 (&scales)[kRing][kAttnWarps];                       // of K and V
+    uint32_t (&present)[kRing][kAttnWarps];                    // whether the table names a block there
+    uint32_t &failed, &queries_rest;
+    int (&nan_from)[D];                                        // first token among the call's own whose value is NaN, by column
+    uint2 (&query_rest)[NT][D / 16][32];                       // the queries' second parts, as the operand registers lie
+};
+template <int D, int NT>
+__device__ __forceinline__ AttnShared<D, NT> attention_shared() {
+    __shared__ float m[kAttnWarps][NT * 8], l[kAttnWarps][NT * 8];
+    __shared__ float2 block_ml[NT * 8], row_norm[NT * 8];
+    __shared__ uint64_t full[kRing], empty[kRing];
+    __shared__ float2 scales[kRing][kAttnWarps];
+    __shared__ uint32_t present[kRing][kAttnWarps];
+    __shared__ uint32_t failed, queries_rest;
+    __shared__ int nan_from[D];
+    __shared__ uint2 query_rest[NT][D / 16][32];
+    return {m, l, block_ml, row_norm, full, empty, scales, present, failed, queries_rest, nan_from, query_rest};
+}
+
 template <bool BF16, int D, int NT, bool TWICE>
-__global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attention_kernel(const __grid_constant__ CUtensorMap k_map,
-                                                                                               const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
+__device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
+                                                  int next_block);
+
+// NT: tiles of 8 rows.  TWICE (at most 4 rows): the rows stand twice in their tile, and the second
+// time take their weights' second parts, so that one product serves both parts.  REST: the queries
+// have second parts as well; a block that finds so once it has started goes on in a function of its
+// own, so that the ordinary loop keeps the registers (inlined, that cost it 2 %).
+template <bool BF16, int D, int NT, bool TWICE, bool REST>
+__device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
+                                                int next_block) {
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
     constexpr int VW = D / 32;  // words of values a lane holds of one token
     constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
     constexpr int kStep = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
     extern __shared__ __align__(1024) uint8_t ring[];  // [kRing][warp][kStep]; afterwards the warps' sums
+    const AttnShared<D, NT> sh = attention_shared<D, NT>();
     float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
     float(*block_o)[D] = sh_o[kAttnWarps];             // the block's sum of them
-    __shared__ float sh_m[kAttnWarps][NT * 8], sh_l[kAttnWarps][NT * 8];
-    __shared__ float2 block_ml[NT * 8], row_norm[NT * 8];
-    __shared__ uint64_t full[kRing], empty[kRing];
-    __shared__ float2 scales[kRing][kAttnWarps];  // of K and V
-    __shared__ uint32_t present[kRing][kAttnWarps];  // whether the table names a block there
-    __shared__ uint32_t failed;
-    __shared__ int nan_from[D];  // first token among the call's own whose value is NaN, by column
+    auto &sh_m = sh.m, &sh_l = sh.l;
+    auto &block_ml = sh.block_ml, &row_norm = sh.row_norm;
+    auto &full = sh.full, &empty = sh.empty;
+    auto &scales = sh.scales;
+    auto &present = sh.present;
+    auto &nan_from = sh.nan_from;
+    auto &query_rest = sh.query_rest;
+    uint32_t &failed = sh.failed, &queries_rest = sh.queries_rest;
     const sp_cache &c = a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t seq = blockIdx.z;
     const int head = blockIdx.y / a.row_tiles, row0 = blockIdx.y % a.row_tiles * NT * 8;
     const int H = c.n_kv_heads, shift = a.block_shift;
-    pdl_launch_dependents();
-    for (int d = threadIdx.x; d < D; d += kAttnWarps * 32) nan_from[d] = 0x7fffffff;
-    if (threadIdx.x == 0) {
-        if (c.n_blocks > 0) {
-            tma_prefetch_map(&k_map);
-            tma_prefetch_map(&v_map);
+    if constexpr (!REST) {
+        pdl_launch_dependents();
+        for (int d = threadIdx.x; d < D; d += kAttnWarps * 32) nan_from[d] = 0x7fffffff;
+        if (threadIdx.x == 0) {
+            if (c.n_blocks > 0) {
+                tma_prefetch_map(&k_map);
+                tma_prefetch_map(&v_map);
+            }
+            for (int i = 0; i < kRing; ++i) {
+                mbar_init(smem_addr(&full[i]), 2 * kAttnWarps);  // a step's copies: the two of TMA, and the scales
+                mbar_init(smem_addr(&empty[i]), kAttnWarps);
+            }
+            failed = queries_rest = 0u;
+            mbar_fence_init();
         }
-        for (int i = 0; i < kRing; ++i) {
-            mbar_init(smem_addr(&full[i]), 2 * kAttnWarps);  // a step's copies: the two of TMA, and the scales
-            mbar_init(smem_addr(&empty[i]), kAttnWarps);
-        }
-        failed = 0u;
-        mbar_fence_init();
+        __syncthreads();
+        pdl_wait();
     }
-    __syncthreads();
-    pdl_wait();
     const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
     // the tokens before this one are seen by every query
@@ -220,11 +257,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         }
         __syncwarp();
     };
-    int next_block = block_of(warp);  // of the stage this warp fills next
+    // next_block: of the stage this warp fills next
     static_assert(kRing - 1 <= kAttnWarps, "the first stages are filled by different warps");
-    if (warp < kRing - 1) {
-        if (warp < stages) fill(warp, warp, next_block);
-        next_block = block_of(warp + kAttnWarps);
+    if constexpr (!REST) {
+        next_block = block_of(warp);
+        if (warp < kRing - 1) {
+            if (warp < stages) fill(warp, warp, next_block);
+            next_block = block_of(warp + kAttnWarps);
+        }
     }
     RingPlace<kRing> place;
 
@@ -236,6 +276,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
     for (int n = 0; n < NT; ++n) {
         const int row = row0 + n * 8 + (TWICE ? g & 3 : g);
         float undo = a.scale_log2;
+        [[maybe_unused]] uint32_t rest[KW][2] = {}, any_rest = 0u;
         if (row < a.rows) {
             const uint16_t *q = a.Q + seq * a.q.seq + (row / a.group) * a.q.token +
                                 (head * a.group + row % a.group) * a.q.head + t * (D / 4);
@@ -248,7 +289,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             }
             if constexpr (BF16) {
                 // binary16 holds a row scaled by a power of two: its largest magnitude comes to
-                // [2^14, 2^15), and what is lost lies 2^39 below that
+                // [2^14, 2^15).  What lies more than 2^30 below that loses bits; what is lost, 2^40
+                // times, is a second operand, which a block takes only if it has one (down to 2^70
+                // below the largest)
                 uint32_t top = 0;
 #pragma unroll
                 for (int s = 0; s < KW; ++s)
@@ -270,6 +313,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                     for (int i = 0; i < 2; ++i) {
                         const float2 v = unpack2<true>(raw[s][i]);
                         raw[s][i] = pack_f16(v.x * f, v.y * f);
+                        const float2 h = unpack_f16(raw[s][i]);
+                        // 0 for what is not finite
+                        const float lo = fabsf(h.x) <= 65504.0f ? v.x * f - h.x : 0.0f, hi = fabsf(h.y) <= 65504.0f ? v.y * f - h.y : 0.0f;
+                        if constexpr (REST) rest[s][i] = pack_f16(lo * kQueryRest, hi * kQueryRest);
+                        else any_rest |= __float_as_uint(lo) | __float_as_uint(hi);
                     }
             }
 #pragma unroll
@@ -280,6 +328,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         } else {
 #pragma unroll
             for (int s = 0; s < KW; ++s) qf[n][s][0] = qf[n][s][1] = 0u;
+        }
+        if constexpr (REST) {
+            if (warp == 0)
+#pragma unroll
+                for (int s = 0; s < KW; ++s) query_rest[n][s][lane] = make_uint2(rest[s][0], rest[s][1]);
+        } else if (any_rest != 0u) {
+            queries_rest = 1u;
         }
         // the scores' columns are rows 2t and 2t + 1
 #pragma unroll
@@ -295,11 +350,16 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             for (int i = 0; i < 4; ++i) o[n][k][i] = 0.0f;
     }
     __syncthreads();
+    if constexpr (BF16 && !REST) {
+        if (queries_rest != 0u) {
+            attention_block_rest<BF16, D, NT, TWICE>(k_map, v_map, a, next_block);
+            return;
+        }
+    }
 
     // of token g, row 2t of this tile; 8-byte aligned where rows is even
     float *const scores = a.scores + ((seq * H + head) * a.max_len + g) * a.rows + row0 + 2 * t;
-    int stage = 0;
-    for (; stage < stages; ++stage, place.next()) {
+    for (int stage = 0; stage < stages; ++stage, place.next()) {
         const int step = first + stage * kAttnWarps + warp, j0 = step * 16, slot = place.slot;
         const int ahead = stage + kRing - 1;
         bool ok = true;
@@ -354,6 +414,24 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
         float s[NT][4];
         {
             float s2[NT][2][4];
+            if constexpr (REST) {
+#pragma unroll
+                for (int k = 0; k < KW; ++k) {
+                    uint32_t f[4];
+                    e4m3_to_f16(kw[0][k], f[0], f[2]);
+                    e4m3_to_f16(kw[1][k], f[1], f[3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint2 b = query_rest[n][k][lane];
+                        if (k == 0) mma_f16_first(s2[n][0], f, b.x, b.y);
+                        else mma_f16(s2[n][0], f, b.x, b.y);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s2[n][0][i] *= 1.0f / kQueryRest;
+            }
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
                 uint32_t f[4];
@@ -361,7 +439,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
                 e4m3_to_f16(kw[1][k], f[1], f[3]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    if (k < 2) mma_f16_first(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
+                    if (k < 2 && !(REST && k == 0)) mma_f16_first(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
                     else mma_f16(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
                 }
             }
@@ -597,6 +675,19 @@ __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2) cache_attent
             a.acc_out[pair * a.ld_acc + j] = 0.0f;
     }
     if (ranks > 1) cluster_sync();  // no block leaves while its sums are read
+}
+
+template <bool BF16, int D, int NT, bool TWICE>
+__device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
+                                                  int next_block) {
+    attention_block<BF16, D, NT, TWICE, true>(k_map, v_map, a, next_block);
+}
+
+template <bool BF16, int D, int NT, bool TWICE>
+__global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2)
+cache_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                       const __grid_constant__ AttnArgs a) {
+    attention_block<BF16, D, NT, TWICE, false>(k_map, v_map, a, 0);
 }
 
 // Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)

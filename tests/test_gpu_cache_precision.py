@@ -1,9 +1,10 @@
-"""Attention over the 8-bit cache where the roundings of its weights show in the output."""
+"""Attention over the 8-bit cache where the roundings of its weights and queries show in the output."""
 import numpy as np
 import pytest
 import torch
 
 from . import serve_reference as ref
+from .test_gpu_cache import _check_attention, _filled
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +75,46 @@ def test_outputs_that_lie_in_many_small_weights(sp, L, heads, D, below, dtype):
     allowed = (UNIT[dtype] * want + (2.0 ** -17 + L / 16 * 2.0 ** -24) * mag
                + L * 2.0 ** -44 * top + TINY[dtype])
     assert (err <= allowed).all(), (err / allowed).max()
+
+
+@pytest.mark.parametrize("heads,group,n_q,D", [(2, 1, 1, 64), (1, 4, 1, 128), (1, 8, 1, 128), (2, 4, 3, 64)])
+@pytest.mark.parametrize("far", [20, 34, 45, 60])
+def test_queries_with_a_channel_far_above_the_others(sp, heads, group, n_q, D, far):
+    """bf16 queries, one channel of which is 2^far times the others and meets keys of 0: the others alone
+    make the scores.  They are held to 2^-20 of themselves at least (eight bits of bf16, exact, or two
+    binary16 parts), so a score of D / 16 sums is off as in any other row: (D / 16 + 4) * 2^-22 of its terms'
+    magnitudes, and a weight by twice that."""
+    B, L = 2, 150
+    g = torch.Generator().manual_seed(far)
+    K, V = torch.randn(2, B, L, heads, D, generator=g)
+    Q = torch.randn(B, n_q, heads * group, D, generator=g) * 0.3
+    K[..., 11] = 0
+    Q[..., 11] = 2.0 ** far
+    Q[0, 0, 0] = torch.randn(D, generator=g)                   # one ordinary row
+    K, V, Q = K.bfloat16(), V.bfloat16(), Q.bfloat16()
+    cache = sp.KvCache.empty(B, L, heads, D, 32)
+    cache.sp_cache_append(K.cuda(), V.cuda(), torch.zeros(B, dtype=torch.int32, device="cuda"))
+    lens = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(B, n_q, heads * group, device="cuda")
+    got = cache.sp_cache_attention(Q.cuda(), lens, L, scale=1.0, lse=lse).cpu().double().numpy()
+    want, want_lse, _, mag, terms = ref.PlainCache(cache).attention(Q, [L] * B, L, 1.0)
+    d = (D / 16 + 4) * 2.0 ** -22 * terms + 2.0 ** -21
+    assert d.max() < 0.001
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + (4 * d[..., None] + 2.0 ** -20) * mag).all()
+    assert (np.abs(lse.cpu().double().numpy() - want_lse) <= 2 * d + 2.0 ** -20 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("lens,heads,group,n_q,D", [([3000, 700], 2, 4, 1, 128), ([40, 16, 0, 2], 1, 2, 4, 128),
+                                                    ([900, 20], 1, 8, 3, 64), ([5000], 1, 1, 1, 64)])
+def test_such_queries_in_every_way_a_call_ends(sp, lens, heads, group, n_q, D):
+    """Clusters and joined splits, accumulated weights, and NaN among the call's own tokens."""
+    cache = _filled(sp, lens, heads, D, 16, dtype=torch.bfloat16)
+    at = torch.arange(cache.k.numel(), device="cuda").view_as(cache.k) % D == 7
+    cache.k[at] = 0
+    for b, n in enumerate(lens):
+        if n_q > 1 and n > 2:
+            cache.v[int(cache.table[b, (n - 1) // 16]), 0, (n - 1) % 16, 5] = 0x7f
+    Q = torch.randn(len(lens), n_q, heads * group, D, generator=torch.Generator().manual_seed(1))
+    Q[:, :, ::2, 7] = 2.0 ** 50
+    acc_in = torch.rand(len(lens), heads, max(lens), generator=torch.Generator().manual_seed(1)).cuda()
+    _check_attention(sp, cache, Q.bfloat16(), lens, max(lens), acc_in=acc_in)
