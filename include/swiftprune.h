@@ -534,6 +534,96 @@ sp_status sp_cache_evict(const sp_cache *src, const int32_t *lens, int64_t max_l
                          const sp_cache *dst, int32_t *kept_out, float *acc_out,
                          int64_t ld_acc_out, int32_t *lens_out, sp_stream stream);
 
+/* ------------------------------------------------------------------ several answers of one prompt */
+
+/*
+ * Positions: for every head of every query and key, optionally its norm, then its rotation:
+ *     y = x * w / sqrt(mean(x^2) + eps)       (where the weight [head_dim] of dtype is given)
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = (start[b] + i) * freq[k]
+ * for token i of sequence b (start: device int32) and the pairs k < rotary / 2 of the first `rotary`
+ * values of a head: (2k, 2k + 1) if pairs != 0, else (k, k + rotary / 2).  What follows them is
+ * normalised alone.  freq: device, binary32 [rotary / 2].  Angles are worked out in binary64, all
+ * else in binary32, rounded once.  Tensors are [sequence, token, head, head_dim] with strides as for
+ * sp_cache_append; an output may be its input's memory with the same strides, and overlaps no other.
+ * head_dim is even, 2 to 256; 0 <= rotary <= head_dim, even; n_heads + n_kv_heads <= 65535 and
+ * n_seqs * n_tokens <= 2^31 - 1 (else SP_ERR_SHAPE).  Either head count may be 0.
+ */
+sp_status sp_qk_norm_rotary(const void *Q, const sp_strides *q_strides, int n_heads, const void *K,
+                            const sp_strides *k_strides, int n_kv_heads, sp_dtype dtype,
+                            int64_t n_seqs, int64_t n_tokens, int head_dim, const void *q_weight,
+                            const void *k_weight, float eps, const int32_t *start,
+                            const float *freq, int rotary, int pairs, void *Q_out,
+                            const sp_strides *q_out_strides, void *K_out,
+                            const sp_strides *k_out_strides, sp_stream stream);
+
+/*
+ * Shared blocks.  Rows of a cache's table may name the same block; refs (device int32 [n_blocks])
+ * counts the table entries that name each, and a block with refs 0 is free.  The calls keep the
+ * table (written here although sp_cache declares it const) and refs in agreement, and need no
+ * answer from the host: results are the same whatever runs at the same time inside them.  A pool
+ * has at most 2^31 - 1 blocks.  Workspaces as in sp_mx4_linear.
+ *
+ * sp_cache_fork: row dst[i] of the table becomes a copy of row src[i], or empty (-1) where src is
+ * NULL or src[i] names no row: so answers start from one prompt, beams change places, and finished
+ * sequences give their blocks back.  All rows are read before any is written; of several i with one
+ * dst[i] the last counts; a dst[i] that names no row is passed over.  dst, src: device int32 [n],
+ * n <= 2^24.
+ */
+sp_status sp_cache_fork_workspace(const sp_cache *cache, int64_t n, int64_t *bytes /* host */);
+sp_status sp_cache_fork(const sp_cache *cache, int32_t *refs, const int32_t *dst,
+                        const int32_t *src, int64_t n, void *workspace, int64_t workspace_bytes,
+                        sp_stream stream);
+
+/*
+ * sp_cache_reserve: makes the places start[b] .. start[b] + count[b] - 1 of every sequence ready for
+ * sp_cache_append (start, count as there; a negative start asks for nothing).  A place without a
+ * block gets a free one; a place in a block that other entries name too gets a block of its own,
+ * with a copy of the tokens that lie in it before start[b].  A block that everything that names it
+ * asks for stays with the first of them.  Requests are served in the order of sequences and places
+ * with the free blocks in ascending order, all or none: status (device int32 [2]) receives how many
+ * blocks were missing (0: all served; else nothing has changed) and how many are free afterwards.
+ * n_seqs times the blocks that n_new tokens may touch is at most 2^30.
+ */
+sp_status sp_cache_reserve_workspace(const sp_cache *cache, int64_t n_new, int64_t *bytes /* host */);
+sp_status sp_cache_reserve(const sp_cache *cache, int32_t *refs, const int32_t *start,
+                           const int32_t *count, int64_t n_new, int32_t *status, void *workspace,
+                           int64_t workspace_bytes, sp_stream stream);
+
+/*
+ * sp_cache_compact: the live blocks (refs > 0), n of them, come to lie in the blocks 0 .. n - 1, so
+ * that the rest of the pool can be given back.  Those numbered below n stay; the others go, in
+ * ascending order, to the free ones below n.  table_out [n_seqs, ld_table_out] and refs_out
+ * [n_blocks] receive the table and the counts that go with it (they may be cache->table, with the
+ * same leading dimension, and refs; otherwise they overlap neither); an entry that names a free
+ * block becomes -1.  live (device int32 [1]) receives n.  Blocks from n on keep their contents.
+ */
+sp_status sp_cache_compact_workspace(const sp_cache *cache, int64_t *bytes /* host */);
+sp_status sp_cache_compact(const sp_cache *cache, const int32_t *refs, int32_t *table_out,
+                           int64_t ld_table_out, int32_t *refs_out, int32_t *live, void *workspace,
+                           int64_t workspace_bytes, sp_stream stream);
+
+/*
+ * sp_cache_attention for sequences that share prefixes: a prefix is read once for all queries of a
+ * group.  Group g is the sequences group_start[g] .. group_start[g + 1] - 1 (device int32
+ * [n_groups + 1], ascending, 0 to n_seqs; sequences of no group share nothing); the whole blocks
+ * among its first prefix[g] tokens (device int32) are those of the table's row group_start[g] for all
+ * of them, whatever their own rows name there.  All else is as in sp_cache_attention, without the
+ * accumulated weights: queries see the tokens up to their own place, in the prefix too.  max_prefix
+ * >= every prefix[g] and max_group >= the sequences of every group (tokens of a prefix past
+ * max_prefix, and sequences past the first max_group of a group, are read through the sequences' own
+ * rows).
+ */
+sp_status sp_cache_attention_shared_workspace(const sp_cache *cache, int64_t n_q, int n_heads,
+                                              int64_t max_len, int64_t n_groups, int64_t max_prefix,
+                                              int64_t max_group, int64_t *bytes /* host */);
+sp_status sp_cache_attention_shared(const sp_cache *cache, const void *Q,
+                                    const sp_strides *q_strides, sp_dtype dtype, int64_t n_q,
+                                    int n_heads, const int32_t *lens, int64_t max_len,
+                                    const int32_t *group_start, int64_t n_groups,
+                                    const int32_t *prefix, int64_t max_prefix, int64_t max_group,
+                                    float scale, void *O, const sp_strides *o_strides, float *lse,
+                                    void *workspace, int64_t workspace_bytes, sp_stream stream);
+
 /*
  * Waits of the kernels above on their own copies and tensor-core work are bounded; *expired
  * receives how many ran out on the current device since the last clear (0 unless the device or

@@ -39,7 +39,10 @@ EXPORTS = (
     "sp_select_unstructured_group_ex", "sp_select_nm_group", "sp_select_unstructured_multi",
     "sp_select_unstructured_multi_ex", "sp_select_nm_multi", "sp_mx4_scale_bytes", "sp_mx4_quantize",
     "sp_mx4_dequantize", "sp_mx4_linear_workspace", "sp_mx4_linear", "sp_cache_append",
-    "sp_cache_attention_workspace", "sp_cache_attention", "sp_cache_evict", "sp_wait_status",
+    "sp_cache_attention_workspace", "sp_cache_attention", "sp_cache_evict", "sp_qk_norm_rotary",
+    "sp_cache_fork_workspace", "sp_cache_fork", "sp_cache_reserve_workspace", "sp_cache_reserve",
+    "sp_cache_compact_workspace", "sp_cache_compact", "sp_cache_attention_shared_workspace",
+    "sp_cache_attention_shared", "sp_wait_status",
     "sp_debug_status", "sp_status_string",
     "sp_last_cuda_error", "sp_launch_count",
 )
@@ -140,6 +143,17 @@ def _load() -> ctypes.CDLL:
     lib.sp_cache_attention.argtypes = [pc, vp, ps, ci, i64, ci, vp, i64, f32, vp, ps, vp, vp, vp,
                                        i64, vp, i64, vp]
     lib.sp_cache_evict.argtypes = [pc, vp, i64, vp, i64, i64, i64, pc, vp, vp, i64, vp, vp]
+    lib.sp_qk_norm_rotary.argtypes = [vp, ps, ci, vp, ps, ci, ci, i64, i64, ci, vp, vp, f32, vp, vp,
+                                      ci, ci, vp, ps, vp, ps, vp]
+    lib.sp_cache_fork_workspace.argtypes = [pc, i64, pi64]
+    lib.sp_cache_fork.argtypes = [pc, vp, vp, vp, i64, vp, i64, vp]
+    lib.sp_cache_reserve_workspace.argtypes = [pc, i64, pi64]
+    lib.sp_cache_reserve.argtypes = [pc, vp, vp, vp, i64, vp, vp, i64, vp]
+    lib.sp_cache_compact_workspace.argtypes = [pc, pi64]
+    lib.sp_cache_compact.argtypes = [pc, vp, vp, i64, vp, vp, vp, i64, vp]
+    lib.sp_cache_attention_shared_workspace.argtypes = [pc, i64, ci, i64, i64, i64, i64, pi64]
+    lib.sp_cache_attention_shared.argtypes = [pc, vp, ps, ci, i64, ci, vp, i64, vp, i64, vp, i64, i64,
+                                              f32, vp, ps, vp, vp, i64, vp]
     lib.sp_wait_status.argtypes = [ctypes.POINTER(ci), ci]
     lib.sp_debug_status.argtypes = [ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(i64),
                                     ctypes.POINTER(i64), ci]
@@ -739,9 +753,10 @@ def _acc(t, what, n_seqs, n_heads, length, device: int):
 class KvCache:
     """An 8-bit key/value cache over tensors that the caller owns (``sp_cache``): codes uint8
     [n_blocks, kv heads, block tokens, head size] and float32 scales [n_blocks, kv heads] for K
-    and V, and an int32 table [n_seqs, blocks of a sequence]."""
+    and V, and an int32 table [n_seqs, blocks of a sequence].  refs (int32 [n_blocks]) counts the
+    table entries that name each block, for the calls that share and hand out blocks."""
 
-    def __init__(self, k, v, k_scale, v_scale, table):
+    def __init__(self, k, v, k_scale, v_scale, table, refs=None):
         device = _current_device()
         for t, what in ((k, "k"), (v, "v")):
             if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous():
@@ -757,7 +772,8 @@ class KvCache:
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise SpError(SP_ERR_INVALID_ARG, "table must be int32 [n_seqs, blocks]")
         _on_device(table, "table", device)
-        self.device = device
+        _int32(refs, "refs", k.shape[:1], device)
+        self.device, self.refs = device, refs
         self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
         self.n_seqs, (_, self.n_kv_heads, self.block_tokens, self.head_dim) = table.shape[0], k.shape
         ld = table.stride(0) if self.n_seqs > 1 else max(table.stride(0), table.shape[1])
@@ -785,6 +801,19 @@ class KvCache:
         ks, vs = (torch.ones(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
         table = torch.arange(n_seqs * per, dtype=torch.int32, device=device).view(n_seqs, per)
         return cls(k, v, ks, vs, table)
+
+    @classmethod
+    def pool(cls, n_seqs: int, max_tokens: int, n_blocks: int, n_kv_heads: int, head_dim: int,
+             block_tokens: int = 32, device=None) -> "KvCache":
+        """A cache of n_blocks blocks that are all free (``sp_cache_reserve`` hands them out), with
+        a table for max_tokens tokens of each sequence."""
+        device = device or torch.device("cuda", torch.cuda.current_device())
+        shape = (n_blocks, n_kv_heads, block_tokens, head_dim)
+        k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        ks, vs = (torch.ones(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
+        per = (max_tokens + block_tokens - 1) // block_tokens
+        table = torch.full((n_seqs, per), -1, dtype=torch.int32, device=device)
+        return cls(k, v, ks, vs, table, torch.zeros(n_blocks, dtype=torch.int32, device=device))
 
     def sp_cache_append(self, K, V, start, count=None, stream=None):
         """Writes K, V [n_seqs, new, kv heads, head size] at the places start[b] and following
@@ -876,6 +905,154 @@ class KvCache:
                                   _int32(kept_out, "kept_out", shape, device), ao, ld_out, no,
                                   _raw_stream(stream, device)))
         return kept_out, acc_out, lens_out
+
+
+    # ------------------------------------------------ several answers of one prompt
+
+    def _counted(self) -> int:
+        """The current device, for calls that need the counts."""
+        device = self._here()
+        if self.refs is None:
+            raise SpError(SP_ERR_INVALID_ARG, "the cache has no refs")
+        return device
+
+    def _need(self, call: str, *sizes) -> int:
+        """A call's workspace, remembered by its sizes."""
+        key = (call,) + sizes
+        found = self._workspaces.get(key)
+        if found is None:
+            need = ctypes.c_int64()
+            _check(getattr(lib, call)(self._c, *sizes, ctypes.byref(need)))
+            if len(self._workspaces) > 4096:
+                self._workspaces.clear()
+            found = self._workspaces[key] = need.value
+        return found
+
+    def sp_cache_fork(self, dst, src=None, workspace=None, stream=None):
+        """Rows dst of the table (int32 [n]) become copies of the rows src, or empty where src is
+        None or -1; refs follow."""
+        device = self._counted()
+        if dst.dim() != 1:
+            raise SpError(SP_ERR_SHAPE, "dst must be one-dimensional")
+        n = dst.shape[0]
+        need = self._need("sp_cache_fork_workspace", n)
+        wptr, wbytes, keep = _workspace(need, workspace, self.table, device, stream)
+        _check(lib.sp_cache_fork(self._c, self.refs.data_ptr(), _int32(dst, "dst", (n,), device),
+                                 _int32(src, "src", (n,), device), n, wptr, wbytes,
+                                 _raw_stream(stream, device)))
+
+    def sp_cache_reserve(self, start, n_new: int, count=None, status=None, workspace=None, stream=None):
+        """Makes the places start[b] and following, n_new (or count[b]) of them, ready for
+        sp_cache_append: free blocks, and own copies of shared ones.  Returns status (int32 [2]):
+        how many blocks were missing (then nothing has changed), how many are free."""
+        device = self._counted()
+        if status is None:
+            status = _result(stream, torch.empty, 2, dtype=torch.int32, device=self.table.device)
+        shape = (self.n_seqs,)
+        need = self._need("sp_cache_reserve_workspace", n_new)
+        wptr, wbytes, keep = _workspace(need, workspace, self.table, device, stream)
+        _check(lib.sp_cache_reserve(self._c, self.refs.data_ptr(), _int32(start, "start", shape, device),
+                                    _int32(count, "count", shape, device), n_new,
+                                    _int32(status, "status", (2,), device), wptr, wbytes,
+                                    _raw_stream(stream, device)))
+        return status
+
+    def sp_cache_compact(self, live=None, table_out=None, refs_out=None, workspace=None, stream=None):
+        """Moves the live blocks, n of them, into the blocks 0 .. n - 1.  The table and the refs
+        that go with it replace the cache's own unless table_out and refs_out (int32, of their
+        shapes) are given.  Returns live (int32 [1]), which holds n."""
+        device = self._counted()
+        if live is None:
+            live = _result(stream, torch.empty, 1, dtype=torch.int32, device=self.table.device)
+        table_out = self.table if table_out is None else table_out
+        refs_out = self.refs if refs_out is None else refs_out
+        shape = self.table.shape
+        if (table_out.dtype != torch.int32 or table_out.shape != shape
+                or (shape[1] > 1 and table_out.stride(1) != 1)):
+            raise SpError(SP_ERR_INVALID_ARG, "table_out must be int32 %s" % list(shape))
+        _on_device(table_out, "table_out", device)
+        ld = table_out.stride(0) if shape[0] > 1 else max(table_out.stride(0), shape[1])
+        need = self._need("sp_cache_compact_workspace")
+        wptr, wbytes, keep = _workspace(need, workspace, self.table, device, stream)
+        _check(lib.sp_cache_compact(self._c, self.refs.data_ptr(), table_out.data_ptr(), ld,
+                                    _int32(refs_out, "refs_out", self.refs.shape, device),
+                                    _int32(live, "live", (1,), device), wptr, wbytes,
+                                    _raw_stream(stream, device)))
+        return live
+
+    def sp_cache_attention_shared(self, Q, lens, max_len: int, group_start, prefix, max_prefix: int,
+                                  max_group: int, scale: float | None = None, O=None, lse=None,
+                                  workspace=None, stream=None):
+        """sp_cache_attention where the sequences group_start[g] .. group_start[g + 1] - 1 (int32
+        [groups + 1]) share the whole blocks among their first prefix[g] tokens (int32 [groups]),
+        which are read once, through the group's first row of the table.  max_prefix and max_group
+        bound the prefixes and the sequences of a group.  Returns O."""
+        device = self._here()
+        qs = _heads(Q, "Q", self.n_seqs, self.head_dim, device)
+        if O is None:
+            O = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
+        os_ = _heads(O, "O", self.n_seqs, self.head_dim, device)
+        if O.shape != Q.shape:
+            raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
+        if O.dtype != Q.dtype:
+            raise SpError(SP_ERR_DTYPE, "Q and O must have the same dtype")
+        n_q, n_heads, optr = Q.shape[1], Q.shape[2], O.data_ptr()
+        if optr == Q.data_ptr() and optr:
+            raise SpError(SP_ERR_INVALID_ARG, "O is memory apart from Q")
+        if lse is not None:
+            if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != Q.shape[:3]:
+                raise SpError(SP_ERR_SHAPE, "lse must be contiguous float32 [n_seqs, n_q, heads]")
+            _on_device(lse, "lse", device)
+        if prefix.dim() != 1:
+            raise SpError(SP_ERR_SHAPE, "prefix must be one-dimensional")
+        groups = prefix.shape[0]
+        need = self._need("sp_cache_attention_shared_workspace", n_q, n_heads, max_len, groups, max_prefix, max_group)
+        wptr, wbytes, keep = _workspace(need, workspace, Q, device, stream)
+        _check(lib.sp_cache_attention_shared(
+            self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads, _int32(lens, "lens", (self.n_seqs,), device),
+            max_len, _int32(group_start, "group_start", (groups + 1,), device), groups,
+            _int32(prefix, "prefix", (groups,), device), max_prefix, max_group,
+            self.head_dim ** -0.5 if scale is None else scale, optr, os_, _ptr(lse), wptr, wbytes,
+            _raw_stream(stream, device)))
+        return O
+
+
+def sp_qk_norm_rotary(Q, K, start, freq, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      pairs: bool = False, Q_out=None, K_out=None, stream=None):
+    """Norms the heads of Q and K [n_seqs, tokens, heads, head size] (where a weight [head size] is
+    given) and turns their first 2 * len(freq) values by (start[b] + i) * freq: neighbours together
+    if pairs, else the two halves.  Q_out and K_out may be Q and K.  Returns (Q_out, K_out)."""
+    device = _current_device()
+    n_seqs, dim = Q.shape[0], Q.shape[-1]
+    qs, ks = _heads(Q, "Q", n_seqs, dim, device), _heads(K, "K", n_seqs, dim, device)
+    if Q.shape[1] != K.shape[1]:
+        raise SpError(SP_ERR_SHAPE, "Q and K must have the same tokens")
+    if Q_out is None:
+        Q_out = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
+    if K_out is None:
+        K_out = _result(stream, torch.empty, K.shape, dtype=K.dtype, device=K.device)
+    qo, ko = _heads(Q_out, "Q_out", n_seqs, dim, device), _heads(K_out, "K_out", n_seqs, dim, device)
+    if Q_out.shape != Q.shape or K_out.shape != K.shape:
+        raise SpError(SP_ERR_SHAPE, "Q_out and K_out must have the shapes of Q and K")
+    if not Q.dtype == K.dtype == Q_out.dtype == K_out.dtype:
+        raise SpError(SP_ERR_DTYPE, "Q, K and their outputs must have the same dtype")
+    for x, out, same in ((Q, Q_out, qs is qo), (K, K_out, ks is ko)):
+        if out.data_ptr() == x.data_ptr() and x.numel() and not same and out.stride() != x.stride():
+            raise SpError(SP_ERR_INVALID_ARG, "an output in its input's place has its strides")
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            if w.dtype != Q.dtype or w.shape != (dim,) or not w.is_contiguous():
+                raise SpError(SP_ERR_SHAPE, "%s must be contiguous [%d] of the type of Q" % (what, dim))
+            _on_device(w, what, device)
+    if freq.dtype != torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
+        raise SpError(SP_ERR_INVALID_ARG, "freq must be contiguous float32 [rotary / 2]")
+    _on_device(freq, "freq", device)
+    _check(lib.sp_qk_norm_rotary(Q.data_ptr(), qs, Q.shape[2], K.data_ptr(), ks, K.shape[2], _dtype_of(Q),
+                                 n_seqs, Q.shape[1], dim, _ptr(q_weight), _ptr(k_weight), eps,
+                                 _int32(start, "start", (n_seqs,), device), freq.data_ptr(),
+                                 2 * freq.shape[0], 1 if pairs else 0, Q_out.data_ptr(), qo,
+                                 K_out.data_ptr(), ko, _raw_stream(stream, device)))
+    return Q_out, K_out
 
 
 def sp_wait_status(clear: bool = False) -> int:

@@ -228,6 +228,141 @@ sp_status sp_cache_evict(const sp_cache *src, const int32_t *lens, int64_t max_l
                               lens_out, static_cast<cudaStream_t>(stream));
 }
 
+sp_status sp_qk_norm_rotary(const void *Q, const sp_strides *q_strides, int n_heads, const void *K,
+                            const sp_strides *k_strides, int n_kv_heads, sp_dtype dtype, int64_t n_seqs, int64_t n_tokens,
+                            int head_dim, const void *q_weight, const void *k_weight, float eps, const int32_t *start,
+                            const float *freq, int rotary, int pairs, void *Q_out, const sp_strides *q_out_strides,
+                            void *K_out, const sp_strides *k_out_strides, sp_stream stream) {
+    SP_CALL_RANGE();
+    if (!valid_dtype(dtype)) return SP_ERR_DTYPE;
+    if (n_heads < 0 || n_kv_heads < 0 || n_seqs < 0 || n_tokens < 0) return SP_ERR_INVALID_ARG;
+    if (head_dim < 2 || head_dim > 256 || head_dim % 2 != 0 || rotary < 0 || rotary > head_dim || rotary % 2 != 0)
+        return SP_ERR_SHAPE;
+    if (n_heads > 65535 - n_kv_heads || (n_seqs > 0 && n_tokens > 0x7fffffff / n_seqs)) return SP_ERR_SHAPE;
+    if (!std::isfinite(eps) || eps < 0.0f) return SP_ERR_INVALID_ARG;
+    if (n_heads + n_kv_heads == 0 || n_seqs == 0 || n_tokens == 0) return SP_OK;
+    if (n_heads > 0 && (Q == nullptr || Q_out == nullptr || q_strides == nullptr || q_out_strides == nullptr)) return SP_ERR_INVALID_ARG;
+    if (n_kv_heads > 0 && (K == nullptr || K_out == nullptr || k_strides == nullptr || k_out_strides == nullptr)) return SP_ERR_INVALID_ARG;
+    if (rotary > 0 && (start == nullptr || freq == nullptr)) return SP_ERR_INVALID_ARG;
+    const sp_strides none = {};
+    const QkRotary r{Q, K, q_weight, k_weight, Q_out, K_out, n_heads > 0 ? *q_strides : none, n_kv_heads > 0 ? *k_strides : none,
+                     n_heads > 0 ? *q_out_strides : none, n_kv_heads > 0 ? *k_out_strides : none, dtype, n_seqs, n_tokens,
+                     n_heads, n_kv_heads, head_dim, rotary, start, freq, eps, pairs != 0};
+    return launch_qk_rotary(r, static_cast<cudaStream_t>(stream));
+}
+
+static sp_status check_pages(const sp_cache *c) {
+    sp_status st = check_cache(c);
+    if (st == SP_OK && c->n_blocks > 0x7fffffff) st = SP_ERR_SHAPE;
+    return st;
+}
+
+sp_status sp_cache_fork_workspace(const sp_cache *cache, int64_t n, int64_t *bytes) {
+    sp_status st = check_pages(cache);
+    if (st != SP_OK) return st;
+    if (bytes == nullptr || n < 0) return SP_ERR_INVALID_ARG;
+    if (n > (1 << 24)) return SP_ERR_SHAPE;
+    *bytes = cache_fork_workspace(*cache, n);
+    return SP_OK;
+}
+
+sp_status sp_cache_fork(const sp_cache *cache, int32_t *refs, const int32_t *dst, const int32_t *src, int64_t n,
+                        void *workspace, int64_t workspace_bytes, sp_stream stream) {
+    SP_CALL_RANGE();
+    int64_t need = 0;
+    sp_status st = sp_cache_fork_workspace(cache, n, &need);
+    if (st != SP_OK) return st;
+    if (n == 0 || cache->n_seqs == 0 || cache->table_cols == 0) return SP_OK;
+    if (dst == nullptr || (refs == nullptr && cache->n_blocks > 0)) return SP_ERR_INVALID_ARG;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
+    return launch_cache_fork(*cache, refs, dst, src, n, workspace, static_cast<cudaStream_t>(stream));
+}
+
+sp_status sp_cache_reserve_workspace(const sp_cache *cache, int64_t n_new, int64_t *bytes) {
+    sp_status st = check_pages(cache);
+    if (st != SP_OK) return st;
+    if (bytes == nullptr || n_new < 0) return SP_ERR_INVALID_ARG;
+    if (n_new > kMaxCacheTokens) return SP_ERR_SHAPE;
+    const int64_t touched = std::min(cache->table_cols, n_new / cache->block_tokens + 2);
+    if (cache->n_seqs > 0 && touched > (int64_t(1) << 30) / cache->n_seqs) return SP_ERR_SHAPE;
+    *bytes = cache_reserve_workspace(*cache, n_new);
+    return SP_OK;
+}
+
+sp_status sp_cache_reserve(const sp_cache *cache, int32_t *refs, const int32_t *start, const int32_t *count, int64_t n_new,
+                           int32_t *status, void *workspace, int64_t workspace_bytes, sp_stream stream) {
+    SP_CALL_RANGE();
+    int64_t need = 0;
+    sp_status st = sp_cache_reserve_workspace(cache, n_new, &need);
+    if (st != SP_OK) return st;
+    if (status == nullptr || (refs == nullptr && cache->n_blocks > 0) || (start == nullptr && cache->n_seqs > 0)) return SP_ERR_INVALID_ARG;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
+    return launch_cache_reserve(*cache, refs, start, count, n_new, status, workspace, static_cast<cudaStream_t>(stream));
+}
+
+sp_status sp_cache_compact_workspace(const sp_cache *cache, int64_t *bytes) {
+    sp_status st = check_pages(cache);
+    if (st != SP_OK) return st;
+    if (bytes == nullptr) return SP_ERR_INVALID_ARG;
+    *bytes = cache_compact_workspace(*cache);
+    return SP_OK;
+}
+
+sp_status sp_cache_compact(const sp_cache *cache, const int32_t *refs, int32_t *table_out, int64_t ld_table_out,
+                           int32_t *refs_out, int32_t *live, void *workspace, int64_t workspace_bytes, sp_stream stream) {
+    SP_CALL_RANGE();
+    int64_t need = 0;
+    sp_status st = sp_cache_compact_workspace(cache, &need);
+    if (st != SP_OK) return st;
+    if (ld_table_out < cache->table_cols) return SP_ERR_SHAPE;
+    if (table_out == cache->table && table_out != nullptr && ld_table_out != cache->ld_table) return SP_ERR_SHAPE;
+    if (live == nullptr || (cache->n_blocks > 0 && (refs == nullptr || refs_out == nullptr))) return SP_ERR_INVALID_ARG;
+    if (cache->n_seqs > 0 && cache->table_cols > 0 && table_out == nullptr) return SP_ERR_INVALID_ARG;
+    if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)) return SP_ERR_INVALID_ARG;
+    return launch_cache_compact(*cache, refs, table_out, ld_table_out, refs_out, live, workspace,
+                                static_cast<cudaStream_t>(stream));
+}
+
+sp_status sp_cache_attention_shared_workspace(const sp_cache *cache, int64_t n_q, int n_heads, int64_t max_len,
+                                              int64_t n_groups, int64_t max_prefix, int64_t max_group, int64_t *bytes) {
+    int64_t alone = 0;
+    sp_status st = sp_cache_attention_workspace(cache, n_q, n_heads, max_len, 0, &alone);
+    if (st != SP_OK) return st;
+    if (bytes == nullptr || n_groups < 0 || max_prefix < 0 || max_group < 0) return SP_ERR_INVALID_ARG;
+    if (n_groups > 32767 || max_prefix > kMaxCacheTokens || max_group > 32767) return SP_ERR_SHAPE;
+    SharedAttention s = {};
+    s.n_q = n_q;
+    s.n_heads = n_heads;
+    s.max_len = max_len;
+    s.n_groups = n_groups;
+    s.max_prefix = max_prefix;
+    s.max_group = max_group;
+    *bytes = cache_shared_workspace(*cache, s);
+    return SP_OK;
+}
+
+sp_status sp_cache_attention_shared(const sp_cache *cache, const void *Q, const sp_strides *q_strides, sp_dtype dtype,
+                                    int64_t n_q, int n_heads, const int32_t *lens, int64_t max_len,
+                                    const int32_t *group_start, int64_t n_groups, const int32_t *prefix,
+                                    int64_t max_prefix, int64_t max_group, float scale, void *O,
+                                    const sp_strides *o_strides, float *lse, void *workspace, int64_t workspace_bytes,
+                                    sp_stream stream) {
+    SP_CALL_RANGE();
+    int64_t need = 0;
+    sp_status st = sp_cache_attention_shared_workspace(cache, n_q, n_heads, max_len, n_groups, max_prefix, max_group, &need);
+    if (st != SP_OK) return st;
+    if (!valid_dtype(dtype)) return SP_ERR_DTYPE;
+    if (q_strides == nullptr || o_strides == nullptr || !std::isfinite(scale)) return SP_ERR_INVALID_ARG;
+    if (cache->n_blocks > 0x7fffffff / (int64_t(cache->n_kv_heads) * cache->block_tokens)) return SP_ERR_SHAPE;
+    if (cache->n_seqs == 0 || n_q == 0) return SP_OK;
+    if (Q == nullptr || O == nullptr || lens == nullptr) return SP_ERR_INVALID_ARG;
+    if (n_groups > 0 && (group_start == nullptr || prefix == nullptr)) return SP_ERR_INVALID_ARG;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return SP_ERR_INVALID_ARG;
+    const SharedAttention s{Q, *q_strides, *o_strides, dtype, n_q, max_len, n_groups, max_prefix, max_group, n_heads,
+                            lens, group_start, prefix, scale, O, lse};
+    return launch_cache_shared(*cache, s, workspace, static_cast<cudaStream_t>(stream));
+}
+
 sp_status sp_wait_status(int *expired, int clear) {
     SP_CALL_RANGE();
     if (expired == nullptr) return SP_ERR_INVALID_ARG;

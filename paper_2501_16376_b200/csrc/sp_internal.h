@@ -286,6 +286,47 @@ sp_status launch_cache_evict(const sp_cache &src, const int32_t *lens, int64_t m
                              int64_t budget, int64_t recent, const sp_cache &dst, int32_t *kept, float *acc_out,
                              int64_t ld_acc_out, int32_t *lens_out, cudaStream_t stream);
 
+// qk_rotary.cu: norms of queries and keys and the rotation by position
+struct QkRotary {
+    const void *Q, *K, *q_weight, *k_weight;
+    void *Q_out, *K_out;
+    sp_strides q, k, q_out, k_out;
+    sp_dtype dtype;
+    int64_t n_seqs, n_tokens;
+    int n_heads, n_kv_heads, head_dim, rotary;
+    const int32_t *start;
+    const float *freq;
+    float eps;
+    bool pairs;
+};
+sp_status launch_qk_rotary(const QkRotary &r, cudaStream_t stream);
+
+// cache_pages.cu: shared blocks of the 8-bit cache
+int64_t cache_fork_workspace(const sp_cache &c, int64_t n);
+sp_status launch_cache_fork(const sp_cache &c, int32_t *refs, const int32_t *dst, const int32_t *src,
+                            int64_t n, void *workspace, cudaStream_t stream);
+int64_t cache_reserve_workspace(const sp_cache &c, int64_t n_new);
+sp_status launch_cache_reserve(const sp_cache &c, int32_t *refs, const int32_t *start,
+                               const int32_t *count, int64_t n_new, int32_t *status, void *workspace, cudaStream_t stream);
+int64_t cache_compact_workspace(const sp_cache &c);
+sp_status launch_cache_compact(const sp_cache &c, const int32_t *refs, int32_t *table_out, int64_t ld_table_out,
+                               int32_t *refs_out, int32_t *live, void *workspace, cudaStream_t stream);
+
+// cache_shared.cu: attention over a prefix that a group of sequences shares
+struct SharedAttention {
+    const void *Q;
+    sp_strides q, o;
+    sp_dtype dtype;
+    int64_t n_q, max_len, n_groups, max_prefix, max_group;
+    int n_heads;
+    const int32_t *lens, *group_start, *prefix;
+    float scale;
+    void *O;
+    float *lse;
+};
+int64_t cache_shared_workspace(const sp_cache &c, const SharedAttention &s);
+sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void *workspace, cudaStream_t stream);
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace sp
