@@ -64,6 +64,8 @@ struct AttnArgs {
     const float *acc_in;  // accumulated weights; acc_out is null where a second kernel joins the splits
     float *acc_out;
     int64_t ld_acc;
+    SharedGroups groups;  // SHARED: the tokens that a sequence's group shares are left out
+    int all_splits, first_split;  // SHARED: parts of a (sequence, kv head), and the first of this kernel's
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -71,10 +73,25 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+template <bool BF16>
+__device__ __forceinline__ void mma_16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else mma_f16(c, a, b0, b1);
+}
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+template <bool BF16>
+__device__ __forceinline__ void mma_16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (BF16) {
+        d[0] = d[1] = d[2] = d[3] = 0.0f;
+        mma_16<true>(d, a, b0, b1);
+    } else mma_f16_first(d, a, b0, b1);
 }
 // (d0, d1) += a * (b0, b1), two multiply-adds in one instruction.
 __device__ __forceinline__ void add_scaled2(float &d0, float &d1, float a, float b0, float b1) {
@@ -172,10 +189,13 @@ __device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, cons
 // NT: tiles of 8 rows.  TWICE (at most 4 rows): the rows stand twice in their tile, and the second
 // time take their weights' second parts, so that one product serves both parts.  REST: the queries
 // have second parts as well; a block that finds so once it has started goes on in a function of its
-// own, so that the ordinary loop keeps the registers (inlined, that cost it 2 %).
-template <bool BF16, int D, int NT, bool TWICE, bool REST>
+// own, so that the ordinary loop keeps the registers (inlined, that cost it 2 %).  SHARED: the first
+// tokens of a sequence are its group's and another kernel's; keys become bf16 for bf16 queries, which
+// then need no second parts.
+template <bool BF16, int D, int NT, bool TWICE, bool SHARED, bool REST>
 __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
                                                 int next_block) {
+    int from = 0;
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
     constexpr int VW = D / 32;  // words of values a lane holds of one token
     constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
@@ -213,15 +233,18 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             mbar_fence_init();
         }
         __syncthreads();
-        pdl_wait();
+        // the kernel over the prefix has waited before it let this one start; its results are not
+        // read here
+        if constexpr (SHARED) from = static_cast<int>(shared_blocks(a.groups, c, seq) << (shift - 4));
+        else pdl_wait();
     }
     const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
     // the tokens before this one are seen by every query
     const int all_see = static_cast<int>(max(int64_t(0), min(int64_t(len), a.lens[seq] - a.n_q + 1)));
-    const int steps = (len + 15) / 16;
-    const int first = static_cast<int>(int64_t(steps) * blockIdx.x / a.splits);
-    const int last = static_cast<int>(int64_t(steps) * (blockIdx.x + 1) / a.splits);
+    const int steps = SHARED ? max((len + 15) / 16 - from, 0) : (len + 15) / 16;
+    const int first = (SHARED ? from : 0) + static_cast<int>(int64_t(steps) * blockIdx.x / a.splits);
+    const int last = (SHARED ? from : 0) + static_cast<int>(int64_t(steps) * (blockIdx.x + 1) / a.splits);
 
     // A stage holds a step of 16 tokens for every warp.  The warps take turns in filling stages, two
     // ahead: four lanes copy a step each, scales included (4-byte copies on the same barrier).  The
@@ -287,7 +310,31 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                 raw[s][0] = at[0] | (uint32_t(at[1]) << 16);
                 raw[s][1] = at[2] | (uint32_t(at[3]) << 16);
             }
-            if constexpr (BF16) {
+            if constexpr (BF16 && SHARED) {
+                // keys become bf16: a row is taken as it is, 2^64 times smaller where sums of its
+                // products with codes might leave binary32's range
+                uint32_t top = 0;
+#pragma unroll
+                for (int s = 0; s < KW; ++s)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t lo = (raw[s][i] << 16) & 0x7fffffffu, hi = raw[s][i] & 0x7fff0000u;
+                        top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+                    }
+                const unsigned quad = 0xfu << (lane & 28);
+                top = max(top, __shfl_xor_sync(quad, top, 1));
+                top = max(top, __shfl_xor_sync(quad, top, 2));
+                if (top > kLargeQuery) {
+                    undo *= pow2(64);
+#pragma unroll
+                    for (int s = 0; s < KW; ++s)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 v = unpack2<true>(raw[s][i]);
+                            raw[s][i] = pack_bf16(v.x * pow2(-64), v.y * pow2(-64));
+                        }
+                }
+            } else if constexpr (BF16) {
                 // binary16 holds a row scaled by a power of two: its largest magnitude comes to
                 // [2^14, 2^15).  What lies more than 2^30 below that loses bits; what is lost, 2^40
                 // times, is a second operand, which a block takes only if it has one (down to 2^70
@@ -350,7 +397,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             for (int i = 0; i < 4; ++i) o[n][k][i] = 0.0f;
     }
     __syncthreads();
-    if constexpr (BF16 && !REST) {
+    if constexpr (BF16 && !REST && !SHARED) {
         if (queries_rest != 0u) {
             attention_block_rest<BF16, D, NT, TWICE>(k_map, v_map, a, next_block);
             return;
@@ -437,10 +484,14 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                 uint32_t f[4];
                 e4m3_to_f16(kw[0][k], f[0], f[2]);
                 e4m3_to_f16(kw[1][k], f[1], f[3]);
+                if constexpr (BF16 && SHARED) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = f16_to_bf16(f[i]);
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    if (k < 2 && !(REST && k == 0)) mma_f16_first(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
-                    else mma_f16(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
+                    if (k < 2 && !(REST && k == 0)) mma_16_first<BF16 && SHARED>(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
+                    else mma_16<BF16 && SHARED>(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
                 }
             }
 #pragma unroll
@@ -607,7 +658,8 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         }
         if (nan_from[d] <= row_limit(a, seq, row, len)) out = __uint_as_float(0x7fc00000u);
         if (a.part_o != nullptr) {
-            const int64_t p = ((seq * H + head) * a.splits + blockIdx.x) * a.rows + row;
+            const int64_t split = SHARED ? (seq * H + head) * a.all_splits + a.first_split + blockIdx.x : (seq * H + head) * a.splits + blockIdx.x;
+            const int64_t p = split * a.rows + row;
             a.part_o[p * D + d] = out;
             if (d == 0) a.part_ml[p] = make_float2(top, sum);
         } else {
@@ -615,7 +667,8 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             if (d == 0) block_ml[r] = make_float2(top, sum);
         }
     }
-    if (a.part_o != nullptr) return;
+    if constexpr (SHARED) pdl_wait();  // this kernel's end is the prefix kernel's too
+    if (SHARED || a.part_o != nullptr) return;
 
     // the cluster's blocks share the output's elements
     const int ranks = a.splits, rank = blockIdx.x;
@@ -680,14 +733,14 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
 template <bool BF16, int D, int NT, bool TWICE>
 __device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
                                                   int next_block) {
-    attention_block<BF16, D, NT, TWICE, true>(k_map, v_map, a, next_block);
+    attention_block<BF16, D, NT, TWICE, false, true>(k_map, v_map, a, next_block);
 }
 
-template <bool BF16, int D, int NT, bool TWICE>
+template <bool BF16, int D, int NT, bool TWICE, bool SHARED>
 __global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2)
 cache_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                        const __grid_constant__ AttnArgs a) {
-    attention_block<BF16, D, NT, TWICE, false>(k_map, v_map, a, 0);
+    attention_block<BF16, D, NT, TWICE, SHARED, false>(k_map, v_map, a, 0);
 }
 
 // Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)
@@ -887,7 +940,7 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
 #define SP_LAUNCH(B, DD, N, TWICE)                                                                       \
     do {                                                                                                 \
         static DynamicSmem limit;                                                                        \
-        auto *kernel = cache_attention_kernel<B, DD, N, TWICE>;                                          \
+        auto *kernel = cache_attention_kernel<B, DD, N, TWICE, false>;                                   \
         e = limit.allow(reinterpret_cast<const void *>(kernel));                                         \
         if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, kernel, k_map, v_map, a);                 \
     } while (0)
@@ -930,6 +983,120 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
         default: SP_LAUNCH(0); break;
     }
 #undef SP_LAUNCH
+    if (e != cudaSuccess) return cuda_fail(e);
+    return check_launch();
+}
+
+// ------------------------------------------------------------------ beside a shared prefix
+
+// How many blocks share the tail of a (sequence, kv head, row tile): `tail` estimates its tokens.
+int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail) {
+    return attention_plan(c, rows, tail, true).splits;
+}
+
+// A block joins a (sequence, kv head): a warp a row, four columns a lane at a time.
+constexpr int kSharedJoinThreads = 128;
+template <bool BF16>
+__global__ void __launch_bounds__(kSharedJoinThreads)
+cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SharedParts parts) {
+    const sp_cache &c = a.cache;
+    const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t seq = blockIdx.z, pair = seq * H + head;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // the prefix's parts do not exist
+    for (int row = blockIdx.x * (kSharedJoinThreads / 32) + warp; row < a.rows; row += gridDim.x * (kSharedJoinThreads / 32)) {
+        const int64_t p0 = pair * parts.splits * a.rows + row;
+        float top = kLowest;
+        for (int s = skip + lane; s < parts.splits; s += 32) top = fmaxf(top, parts.ml[p0 + int64_t(s) * a.rows].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, o));
+        float sum = 0.0f, out[4] = {};
+#pragma unroll 4
+        for (int s = skip; s < parts.splits; ++s) {
+            const int64_t p = p0 + int64_t(s) * a.rows;
+            const float2 v = parts.ml[p];
+            const float f = exp2_fast(v.x - top), total = f * v.y;
+            sum += total;
+            if (total == 0.0f || lane * 4 >= D) continue;  // a part that saw nothing has no output
+            const float4 x = *reinterpret_cast<const float4 *>(parts.o + p * D + lane * 4);
+            const float by = s < parts.prefix_splits ? total : f;
+            out[0] = fmaf(by, x.x, out[0]);
+            out[1] = fmaf(by, x.y, out[1]);
+            out[2] = fmaf(by, x.z, out[2]);
+            out[3] = fmaf(by, x.w, out[3]);
+        }
+        const int i = row / a.group, hq = head * a.group + row % a.group;
+        if (lane * 4 < D) {
+            uint16_t *to = a.O + seq * a.o.seq + i * a.o.token + hq * a.o.head + lane * 4;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const float y = sum == 0.0f ? 0.0f : out[d] / sum;
+                if constexpr (BF16) to[d] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+                else to[d] = __half_as_ushort(__float2half_rn(y));
+            }
+        }
+        if (lane == 0 && a.lse != nullptr) a.lse[(seq * a.n_q + i) * a.n_heads + hq] = (top + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, cudaStream_t stream) {
+    AttnArgs a = {};
+    a.cache = c;
+    a.Q = static_cast<const uint16_t *>(s.Q);
+    a.q = s.q;
+    a.o = s.o;
+    a.n_q = s.n_q;
+    a.max_len = s.max_len;
+    a.n_heads = s.n_heads;
+    a.group = s.n_heads / c.n_kv_heads;
+    a.rows = static_cast<int>(s.n_q * a.group);
+    a.row_tiles = a.rows <= 8 ? 1 : (a.rows + 15) / 16;
+    a.splits = parts.splits - parts.prefix_splits;
+    a.all_splits = parts.splits;
+    a.first_split = parts.prefix_splits;
+    a.block_shift = c.block_tokens == 16 ? 4 : c.block_tokens == 32 ? 5 : 6;
+    a.lens = s.lens;
+    a.scale_log2 = s.scale * kLog2e;
+    a.O = static_cast<uint16_t *>(s.O);
+    a.lse = s.lse;
+    a.part_o = parts.o;
+    a.part_ml = parts.ml;
+    a.groups = SharedGroups{s.group_start, s.prefix, s.n_groups, s.max_prefix, s.max_group};
+    PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
+    CUtensorMap k_map = {}, v_map = {};
+    const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
+    cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
+    if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, 16);
+    if (e != cudaSuccess) return cuda_fail(e);
+    pdl.cfg.dynamicSmemBytes = kAttnWarps * kRing * c.head_dim * 32;
+    const bool bf16 = s.dtype == SP_BF16;
+#define SP_LAUNCH(B, DD, N, TWICE)                                                       \
+    do {                                                                                 \
+        static DynamicSmem limit;                                                        \
+        auto *kernel = cache_attention_kernel<B, DD, N, TWICE, true>;                    \
+        e = limit.allow(reinterpret_cast<const void *>(kernel));                         \
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&pdl.cfg, kernel, k_map, v_map, a); \
+    } while (0)
+#define SP_ROWS(B, DD)                                    \
+    do {                                                  \
+        if (a.rows <= 4) SP_LAUNCH(B, DD, 1, true);       \
+        else if (a.rows <= 8) SP_LAUNCH(B, DD, 1, false); \
+        else SP_LAUNCH(B, DD, 2, false);                  \
+    } while (0)
+    if (bf16 && c.head_dim == 64) SP_ROWS(true, 64);
+    else if (bf16) SP_ROWS(true, 128);
+    else if (c.head_dim == 64) SP_ROWS(false, 64);
+    else SP_ROWS(false, 128);
+#undef SP_ROWS
+#undef SP_LAUNCH
+    if (e != cudaSuccess) return cuda_fail(e);
+    sp_status st = check_launch();
+    if (st != SP_OK) return st;
+    const int blocks = std::min((a.rows + kSharedJoinThreads / 32 - 1) / (kSharedJoinThreads / 32), 64);
+    PdlConfig second(dim3(blocks, c.n_kv_heads, static_cast<unsigned>(c.n_seqs)), dim3(kSharedJoinThreads), stream);
+    e = bf16 ? cudaLaunchKernelEx(&second.cfg, cache_shared_join_kernel<true>, a, parts)
+             : cudaLaunchKernelEx(&second.cfg, cache_shared_join_kernel<false>, a, parts);
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
 }

@@ -30,6 +30,16 @@ __device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t &lo, uint32_t &
         "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
         : "=r"(lo), "=r"(hi) : "r"(w));
 }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// Two packed binary16 values -> bf16 (exact for what e4m3 holds).
+__device__ __forceinline__ uint32_t f16_to_bf16(uint32_t h) {
+    const float2 f = unpack2<false>(h);
+    return pack_bf16(f.x, f.y);
+}
+constexpr uint32_t kLargeQuery = 0x5f800000u;  // 2^64: larger bf16 queries are scaled down by that
 __device__ __forceinline__ void e4m3_unpack8(uint2 w, float (&v)[8]) {
     uint32_t h[4];
     e4m3_to_f16(w.x, h[0], h[1]);
@@ -79,5 +89,52 @@ __device__ __forceinline__ int64_t cache_block(const sp_cache &c, int64_t seq, i
     const int64_t id = c.table[seq * c.ld_table + place];
     return id >= 0 && id < c.n_blocks ? id : -1;
 }
+
+// Groups of sequences that share the first blocks of their first row.
+struct SharedGroups {
+    const int32_t *start, *prefix;  // [n_groups + 1], [n_groups]
+    int64_t n_groups, max_prefix, max_group;
+};
+// Sequences [begin, end) of a group share the first `blocks` blocks of row begin.
+struct SharedGroup {
+    int64_t begin, end, blocks;
+};
+__device__ __forceinline__ SharedGroup shared_group(const SharedGroups &g, const sp_cache &c, int64_t i) {
+    SharedGroup r;
+    r.begin = max(g.start[i], 0);
+    r.end = min(min(int64_t(g.start[i + 1]), r.begin + g.max_group), c.n_seqs);
+    r.blocks = min(max(int64_t(0), min(int64_t(g.prefix[i]), g.max_prefix)) / c.block_tokens, c.table_cols);
+    return r;
+}
+// Blocks that a sequence shares, 0 if it is in no group; the whole warp asks.  The last group that
+// does not begin behind the sequence is found 32 candidates at a time.
+__device__ __forceinline__ int64_t shared_blocks(const SharedGroups &g, const sp_cache &c, int64_t seq) {
+    const int lane = threadIdx.x & 31;
+    int64_t at = 0, n = g.n_groups;
+    while (n > 0) {
+        const int64_t stride = (n + 31) / 32, i = at + lane * stride;
+        const unsigned vote = __ballot_sync(kFullWarp, lane * stride < n && g.start[i] <= seq);
+        if (vote == 0u) return 0;
+        const int64_t skip = (31 - __clz(vote)) * stride;
+        at += skip;
+        if (stride == 1) break;
+        n = min(stride, n - skip);
+    }
+    if (n == 0) return 0;
+    const SharedGroup r = shared_group(g, c, at);
+    return seq >= r.begin && seq < r.end ? r.blocks : 0;
+}
+
+// What the two kernels over prefix and tails leave for the one that joins them: for a sequence and kv
+// head `splits` parts, those of the prefix first.
+struct SharedParts {
+    float *o;    // [seq, kv head, part, row, D]: of the prefix divided by its sum, of the tails not
+    float2 *ml;  // [seq, kv head, part, row]: maximum (log2) and sum
+    int splits, prefix_splits;
+};
+
+// cache_attention.cu: the tokens behind the prefixes, and the join.
+int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail);
+sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, cudaStream_t stream);
 
 }  // namespace sp

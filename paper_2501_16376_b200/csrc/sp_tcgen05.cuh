@@ -73,6 +73,11 @@ constexpr uint64_t kDescVersion = uint64_t(1) << 46;
 __device__ __forceinline__ uint64_t desc_rows128(uint32_t addr) {
     return ((addr & 0x3ffffu) >> 4) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | kDescVersion | (uint64_t(2) << 61);
 }
+// The same memory read the other way: 64 columns to a row of 128 bytes, rows along the inner dimension,
+// which advances by rows * 128 bytes; the next 64 columns are `next` bytes further.
+__device__ __forceinline__ uint64_t desc_columns128(uint32_t addr, uint32_t next) {
+    return ((addr & 0x3ffffu) >> 4) | (uint64_t(next >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | kDescVersion | (uint64_t(2) << 61);
+}
 // A 512-byte tile of scales, 32 rows of 16 bytes without swizzle: groups of 8 rows are 128 bytes apart.
 __device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
     return ((addr & 0x3ffffu) >> 4) | (uint64_t(128 >> 4) << 16) | (uint64_t(128 >> 4) << 32) | kDescVersion;
@@ -92,6 +97,7 @@ __device__ __forceinline__ void tmem_copy_scales(uint32_t dst, uint64_t desc) {
 __device__ __forceinline__ uint32_t f16_instruction(int n, bool bf16) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
+constexpr uint32_t kColumnsB = 1u << 16;  // B is described by desc_columns128
 // A in tensor memory: a lane a row, 8 columns of two elements each.
 __device__ __forceinline__ void mma_16bit(uint32_t d, uint32_t a, uint64_t b, uint32_t instruction, bool accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
