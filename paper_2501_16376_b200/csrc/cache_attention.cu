@@ -667,7 +667,9 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             if (d == 0) block_ml[r] = make_float2(top, sum);
         }
     }
-    if constexpr (SHARED) pdl_wait();  // this kernel's end is the prefix kernel's too
+    // this kernel does not end before the one over the prefixes: one block waits for all
+    if constexpr (SHARED)
+        if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) pdl_wait();
     if (SHARED || a.part_o != nullptr) return;
 
     // the cluster's blocks share the output's elements

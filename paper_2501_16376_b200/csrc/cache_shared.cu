@@ -13,7 +13,9 @@
 // reference but in the last exponents.  A thread owns a row: its maximum and sum stay in registers,
 // and nothing crosses lanes.  The maximum is raised only when a score exceeds it by more than 2^8.
 //
-// Warps: four for each 128 rows (softmax), four convert, one issues products, one copies.
+// Two groups of four softmax warps, each with sums of its own, hide one another's latency: with 256
+// rows each has 128 of them, with 128 they take the steps in turn and their sums are joined at the end.
+// Four warps convert, one issues products, one copies.
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -29,21 +31,22 @@ constexpr float kRaise = 8.0f;       // how far (in powers of two) a score may e
 constexpr int kRaiseScale = 40;      // how far a value scale may exceed its reference
 constexpr int kStep = 64;            // tokens
 constexpr int kTmemColumns = 512;
+constexpr int kConverted = 3;        // steps of converted keys, and of values
 
 template <int D, int TILES>
 struct PrefixTile {
-    static constexpr int kSlots = D == 128 ? 6 : 12;           // steps of codes on their way
-    static constexpr int kBuffers = TILES == 1 ? 2 : 1;        // of scores
+    static constexpr int kSlots = D == 128 ? 4 : 10;           // steps of codes on their way
+    static constexpr int kBuffers = TILES == 1 ? 3 : 2;        // of scores
     static constexpr int kRawBytes = 2 * kStep * D;            // keys, then values
     static constexpr int kHalfBytes = kStep * 128;             // 64 converted columns
     static constexpr int kConvBytes = D / 64 * kHalfBytes;     // keys (or values) of a step
-    static constexpr int kSmem = kSlots * kRawBytes + 4 * kConvBytes;
-    static constexpr int kSoftmaxWarps = 4 * TILES;
+    static constexpr int kSmem = kSlots * kRawBytes + 2 * kConverted * kConvBytes;
+    static constexpr int kSoftmaxWarps = 8;
     static constexpr int kWarps = kSoftmaxWarps + 4 + 2;
-    // tensor memory: of a tile
-    static __device__ constexpr uint32_t q(int t) { return t * 256; }
-    static __device__ constexpr uint32_t s(int t, int b) { return t * 256 + 64 + b * 64; }
-    static __device__ constexpr uint32_t o(int t) { return TILES == 1 ? 256 : t * 256 + 128; }
+    // tensor memory: queries of a tile, scores, sums of a stream
+    static __device__ constexpr uint32_t q(int t) { return t * 64; }
+    static __device__ constexpr uint32_t s(int b) { return TILES * 64 + b * 64; }
+    static __device__ constexpr uint32_t o(int g) { return 256 + g * 128; }
 };
 
 struct PrefixArgs {
@@ -76,6 +79,39 @@ __device__ __forceinline__ uint2 convert4(uint32_t w) {
     }
     return h;
 }
+// Pairs of binary32 values in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 c, a, b, c;\n\tmov.b64 {%0, %1}, c;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float max16(const uint32_t *v) {
+    auto f = [&](int i) { return __uint_as_float(v[i]); };
+    const float a = max3(f(0), f(1), f(2)), b = max3(f(3), f(4), f(5)), c = max3(f(6), f(7), f(8));
+    const float d = max3(f(9), f(10), f(11)), e = max3(f(12), f(13), f(14));
+    return max3(max3(a, b, c), fmaxf(d, e), f(15));
+}
 __device__ __forceinline__ uint4 load_shared16(uint32_t at) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -94,9 +130,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     using Tile = PrefixTile<D, TILES>;
     constexpr int kSlots = Tile::kSlots, kBuffers = Tile::kBuffers, kSoftmaxWarps = Tile::kSoftmaxWarps;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ uint64_t raw_full[kSlots], raw_empty[kSlots], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    __shared__ uint64_t s_full[TILES][kBuffers], p_full[TILES][kBuffers], pv_done[TILES], drained;
+    __shared__ uint64_t raw_full[kSlots], raw_empty[kSlots], k_full[kConverted], k_empty[kConverted], v_full[kConverted], v_empty[kConverted];
+    __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], pv_done[2], drained;
     __shared__ uint32_t tmem_base, failed, present[kSlots];
+    __shared__ float4 group_sums[2][128];  // TILES == 1: maximum, sum, 2^reference of a group's rows
     __shared__ int all_see, nan_from[D];
     const sp_cache &c = a.cache;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
@@ -108,19 +145,18 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             mbar_init(smem_addr(&raw_full[i]), 1);
             mbar_init(smem_addr(&raw_empty[i]), 4);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kConverted; ++i) {
             mbar_init(smem_addr(&k_full[i]), 4);
             mbar_init(smem_addr(&v_full[i]), 4);
             mbar_init(smem_addr(&k_empty[i]), 1);
             mbar_init(smem_addr(&v_empty[i]), 1);
         }
-        for (int t = 0; t < TILES; ++t) {
-            for (int b = 0; b < kBuffers; ++b) {
-                mbar_init(smem_addr(&s_full[t][b]), 1);
-                mbar_init(smem_addr(&p_full[t][b]), 4);
-            }
-            mbar_init(smem_addr(&pv_done[t]), 1);
+        for (int b = 0; b < kBuffers; ++b) {
+            mbar_init(smem_addr(&s_full[b]), 1);
+            mbar_init(smem_addr(&p_full[b]), 4);
         }
+        mbar_init(smem_addr(&pv_done[0]), 1);
+        mbar_init(smem_addr(&pv_done[1]), 1);
         mbar_init(smem_addr(&drained), 1);
         failed = 0u;
         all_see = 0x7fffffff;
@@ -146,10 +182,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     };
 
     // the row of this thread: its place, and its queries
-    const int tile = warp >> 2, row = row0 + (warp >> 2) * 128 + (warp & 3) * 32 + lane;
+    const int stream = warp >> 2, tile = TILES == 1 ? 0 : stream, row = row0 + tile * 128 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     int limit = -1;        // the last token that it sees
-    float undo = a.scale_log2;
+    float undo = fabsf(a.scale_log2);  // its sign goes to the queries: factors of scores are positive
     uint4 q[D / 8];
     if (warp < kSoftmaxWarps) {
 #pragma unroll
@@ -191,11 +227,14 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             }
         }
     }
+    if (a.scale_log2 < 0.0f)
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) q[i] = make_uint4(q[i].x ^ 0x80008000u, q[i].y ^ 0x80008000u, q[i].z ^ 0x80008000u, q[i].w ^ 0x80008000u);
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
-    if (warp < kSoftmaxWarps) {
+    if (warp < 4 * TILES) {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) tmem_store32(tmem + lanes + Tile::q(tile) + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&q[i * 8]));
         tmem_store_wait();
@@ -203,32 +242,43 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     }
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t raw = smem_addr(smem), conv = raw + kSlots * Tile::kRawBytes;  // conv: K, K, V, V
+    const uint32_t raw = smem_addr(smem), conv = raw + kSlots * Tile::kRawBytes;  // conv: keys, then values
 
     if (warp == kSoftmaxWarps + 5) {
-        // ---- copies: a lane a block of the cache
-        const int blocks = kStep >> shift;  // of a step: 4, 2 or 1
+        // ---- copies: a lane a block of the cache.  A load of the table takes longer than a step, so the
+        // lanes hold the blocks of several steps, and those of the next ones are on their way
+        const int blocks = kStep >> shift, held = 32 / blocks;  // of a step: 4, 2 or 1
         const uint32_t piece = static_cast<uint32_t>(D) << shift;
         RingPlace<kSlots> at;
         bool ok = true;
-        int id = lane < blocks ? block_at(first * kStep + (lane << shift)) : -1, issued = 0;
+        auto blocks_from = [&](int step) {
+            const int mine = step + lane / blocks;
+            return mine < count ? block_at((first + mine) * kStep + (lane % blocks << shift)) : -1;
+        };
+        int ids = blocks_from(0), next_ids = blocks_from(held), issued = 0;
         for (int step = 0; step < count; ++step, at.next()) {
+            const int turn = step % held;
+            if (step > 0 && turn == 0) {
+                ids = next_ids;
+                next_ids = blocks_from(step + held);
+            }
+            const int id = __shfl_sync(kFullWarp, ids, turn * blocks + lane % blocks);
+            const bool mine = lane < blocks && id >= 0;
             if (step >= kSlots) ok = mbar_wait_or_fail(smem_addr(&raw_empty[at.slot]), at.parity ^ 1u, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
-            const unsigned here = __ballot_sync(kFullWarp, id >= 0);
+            const unsigned here = __ballot_sync(kFullWarp, mine);
             const uint32_t bar = smem_addr(&raw_full[at.slot]), to = raw + at.slot * Tile::kRawBytes + lane * piece;
             if (lane == 0) {
                 present[at.slot] = here;
                 mbar_expect_tx(bar, 2 * piece * __popc(here));
             }
             __syncwarp();
-            if (id >= 0) {
+            if (mine) {
                 const int y = (id * c.n_kv_heads + head) << shift;
                 tma_load_2d(to, &k_map, 0, y, bar);
                 tma_load_2d(to + kStep * D, &v_map, 0, y, bar);
             }
             issued = step + 1;
-            id = lane < blocks && step + 1 < count ? block_at((first + step + 1) * kStep + (lane << shift)) : -1;
             __syncwarp();
         }
         if (failed != 0u && lane == 0)
@@ -237,41 +287,45 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         // ---- products
         if (elect_one()) {
             const uint32_t qk = f16_instruction(kStep, BF16), pv = f16_instruction(D, true) | kColumnsB;
-            auto scores = [&](int t, int step) {
-                const int b = step % kBuffers;
-                const uint64_t k = desc_rows128(conv + (step & 1) * Tile::kConvBytes);
+            // Whichever product has its operands goes next; products run in the order of their issue.  A
+            // step's scores go where the weights of three steps before (of the step before) were.
+            constexpr int kAhead = TILES == 1 ? 3 : 1;
+            int scored[TILES] = {}, weighed[TILES] = {};
+            auto ready = [&](uint64_t *bar, int use) { return mbar_test(smem_addr(bar), use & 1); };
+            for (uint32_t idle = 0; weighed[0] < count || weighed[TILES - 1] < count;) {
+                bool issued = false;
 #pragma unroll
-                for (int p = 0; p < D / 16; ++p)
-                    mma_16bit(tmem + Tile::s(t, b), tmem + Tile::q(t) + p * 8, k + (p >> 2) * (Tile::kHalfBytes / 16) + (p & 3) * 2, qk, p > 0);
-                tcgen05_commit(smem_addr(&s_full[t][b]));
-            };
-            bool ok = true;
-            for (int step = 0; ok && step < min(count, kBuffers); ++step) {
-                ok = mbar_wait_or_fail(smem_addr(&k_full[step & 1]), 0, &failed);
-                if (!ok) break;
-                tcgen05_fence_after();
-                for (int t = 0; t < TILES; ++t) scores(t, step);
-                tcgen05_commit(smem_addr(&k_empty[step & 1]));
-            }
-            for (int step = 0; ok && step < count; ++step) {
-                const int b = step % kBuffers, next = step + kBuffers;
-                ok = mbar_wait_or_fail(smem_addr(&v_full[step & 1]), (step >> 1) & 1, &failed);
-                if (ok && next < count) ok = mbar_wait_or_fail(smem_addr(&k_full[next & 1]), (next >> 1) & 1, &failed);
-                if (!ok) break;
-                const uint64_t v = desc_columns128(conv + (2 + (step & 1)) * Tile::kConvBytes, Tile::kHalfBytes);
                 for (int t = 0; t < TILES; ++t) {
-                    ok = mbar_wait_or_fail(smem_addr(&p_full[t][b]), (step / kBuffers) & 1, &failed);
-                    if (!ok) break;
-                    tcgen05_fence_after();
-                    // two parts of P, 64 tokens each
+                    const int v = weighed[t], v_at = v % kConverted, p_at = TILES == 1 ? v % 3 : t;
+                    if (v < scored[t] && ready(&p_full[p_at], TILES == 1 ? v / 3 : v) && ready(&v_full[v_at], v / kConverted)) {
+                        tcgen05_fence_after();
+                        const int g = TILES == 1 ? v & 1 : t;
+                        const uint64_t values = desc_columns128(conv + (kConverted + v_at) * Tile::kConvBytes, Tile::kHalfBytes);
 #pragma unroll
-                    for (int p = 0; p < 8; ++p)
-                        mma_16bit(tmem + Tile::o(t), tmem + Tile::s(t, b) + p * 8, v + (p & 3) * (16 * 128 / 16), pv, step > 0 || p > 0);
-                    tcgen05_commit(smem_addr(&pv_done[t]));
-                    if (t == TILES - 1) tcgen05_commit(smem_addr(&v_empty[step & 1]));
-                    if (next < count) scores(t, next);
+                        for (int p = 0; p < 8; ++p)  // two parts of P, 64 tokens each
+                            mma_16bit(tmem + Tile::o(g), tmem + Tile::s(p_at) + p * 8, values + (p & 3) * (16 * 128 / 16), pv,
+                                      v >= (TILES == 1 ? 2 : 1) || p > 0);
+                        tcgen05_commit(smem_addr(&pv_done[g]));
+                        ++weighed[t];
+                        if (TILES == 1 || weighed[1 - t] > v) tcgen05_commit(smem_addr(&v_empty[v_at]));
+                        issued = true;
+                    }
+                    const int k = scored[t], k_at = k % kConverted, s_at = TILES == 1 ? k % 3 : t;
+                    if (k < count && k - weighed[t] < kAhead && ready(&k_full[k_at], k / kConverted)) {
+                        tcgen05_fence_after();
+                        const uint64_t keys = desc_rows128(conv + k_at * Tile::kConvBytes);
+#pragma unroll
+                        for (int p = 0; p < D / 16; ++p)
+                            mma_16bit(tmem + Tile::s(s_at), tmem + Tile::q(t) + p * 8, keys + (p >> 2) * (Tile::kHalfBytes / 16) + (p & 3) * 2, qk, p > 0);
+                        tcgen05_commit(smem_addr(&s_full[s_at]));
+                        ++scored[t];
+                        if (TILES == 1 || scored[1 - t] > k) tcgen05_commit(smem_addr(&k_empty[k_at]));
+                        issued = true;
+                    }
                 }
-                if (ok && next < count) tcgen05_commit(smem_addr(&k_empty[next & 1]));
+                idle = issued ? 0 : idle + 1;
+                if (idle > kWaitLimit) mbar_give_up(&failed);
+                if (idle != 0 && *static_cast<volatile uint32_t *>(&failed) != 0u) break;
             }
         }
         __syncwarp();
@@ -288,27 +342,32 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         bool ok = true;
         for (int step = 0; step < count; ++step, at.next()) {
             ok = mbar_wait_or_fail(smem_addr(&raw_full[at.slot]), at.parity, &failed);
-            const int buffer = step & 1;
-            if (ok && step >= 2) ok = mbar_wait_or_fail(smem_addr(&k_empty[buffer]), ((step >> 1) - 1) & 1, &failed);
+            const int buffer = step % kConverted, uses = step / kConverted;
+            if (ok && uses > 0) ok = mbar_wait_or_fail(smem_addr(&k_empty[buffer]), (uses - 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             const uint32_t from = raw + at.slot * Tile::kRawBytes, here = present[at.slot];
             const int token0 = (first + step) * kStep;
             const bool checked = token0 + kStep > all_see;  // some rows do not see all of it
             auto convert = [&](auto is_key) {
                 constexpr bool KEY = decltype(is_key)::value;
-                const uint32_t src = from + (KEY ? 0 : kStep * D), dst = conv + (KEY ? buffer : 2 + buffer) * Tile::kConvBytes;
+                const uint32_t src = from + (KEY ? 0 : kStep * D), dst = conv + (KEY ? buffer : kConverted + buffer) * Tile::kConvBytes;
+                constexpr int kEach = kStep * kChunks / 128;
+                uint4 w[kEach];
+                // eight lanes: a row's chunks (D = 64: of two rows)
 #pragma unroll
-                for (int i = 0; i < kStep * kChunks / 128; ++i) {
-                    const int x = i * 128 + thread;
-                    // eight lanes: a row's chunks (D = 64: of two rows)
-                    const int r = x / kChunks, ch = x % kChunks;
+                for (int i = 0; i < kEach; ++i) {
+                    const int x = i * 128 + thread, r = x / kChunks, ch = x % kChunks;
                     const int swap = D == 128 ? r & 7 : (r >> 1) & 3;
-                    uint4 w = load_shared16(src + r * D + ((ch ^ swap) << 4));
+                    w[i] = load_shared16(src + r * D + ((ch ^ swap) << 4));
+                }
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int x = i * 128 + thread, r = x / kChunks, ch = x % kChunks;
                     if constexpr (!KEY) {
                         if (!((here >> (r >> shift)) & 1u)) {
-                            w = make_uint4(0u, 0u, 0u, 0u);
+                            w[i] = make_uint4(0u, 0u, 0u, 0u);
                         } else if (checked) {
-                            uint32_t *word = reinterpret_cast<uint32_t *>(&w);
+                            uint32_t *word = reinterpret_cast<uint32_t *>(&w[i]);
 #pragma unroll
                             for (int k = 0; k < 16; ++k)
                                 if (((word[k >> 2] >> (8 * (k & 3))) & 0x7fu) == 0x7fu) {
@@ -317,8 +376,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                                 }
                         }
                     }
-                    const uint2 a0 = convert4<KEY ? BF16 : true>(w.x), a1 = convert4<KEY ? BF16 : true>(w.y);
-                    const uint2 a2 = convert4<KEY ? BF16 : true>(w.z), a3 = convert4<KEY ? BF16 : true>(w.w);
+                    const uint2 a0 = convert4<KEY ? BF16 : true>(w[i].x), a1 = convert4<KEY ? BF16 : true>(w[i].y);
+                    const uint2 a2 = convert4<KEY ? BF16 : true>(w[i].z), a3 = convert4<KEY ? BF16 : true>(w[i].w);
                     const uint32_t to = dst + (ch >> 2) * Tile::kHalfBytes + r * 128, c0 = (ch & 3) * 2;
                     store_shared16(to + ((c0 ^ (r & 7)) << 4), a0.x, a0.y, a1.x, a1.y);
                     store_shared16(to + (((c0 + 1) ^ (r & 7)) << 4), a2.x, a2.y, a3.x, a3.y);
@@ -328,7 +387,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&k_full[buffer]));
-            if (step >= 2) ok = mbar_wait_or_fail(smem_addr(&v_empty[buffer]), ((step >> 1) - 1) & 1, &failed);
+            if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&v_empty[buffer]), (uses - 1) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             convert(std::false_type{});
             fence_async_smem();
@@ -339,121 +398,137 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             }
         }
     } else {
-        // ---- softmax: a thread a row
+        // ---- softmax: a thread a row, of the steps stream, stream + kEvery, ...
+        constexpr int kEvery = TILES == 1 ? 2 : 1;
+        const int from = TILES == 1 ? stream : 0, turns = (count - from + kEvery - 1) / kEvery;
         float m = kLowest, l = 0.0f;
         int reference = -200;  // of the value scales, as an exponent
         bool ok = true;
         // scales of a step: lanes 0 .. 3 hold those of its 16-token pieces
         auto piece_block = [&](int step) { return lane < 4 && step < count ? block_at((first + step) * kStep + lane * 16) : -1; };
         auto scale_of = [&](const float *scales, int id) { return id >= 0 ? scales[int64_t(id) * c.n_kv_heads + head] : 0.0f; };
-        int id = piece_block(0), next_id = piece_block(1);
+        int id = piece_block(from), next_id = piece_block(from + kEvery);
         float ks = scale_of(c.k_scale, id), vs = scale_of(c.v_scale, id);
-        for (int step = 0; step < count; ++step) {
-            const int b = step % kBuffers;
+        for (int turn = 0; turn < turns; ++turn) {
+            const int step = from + turn * kEvery, b = TILES == 1 ? step % 3 : stream;
             const unsigned here = __ballot_sync(kFullWarp, id >= 0) & 0xfu;
             const float ks_now = ks, vs_now = vs;
             id = next_id;
             ks = scale_of(c.k_scale, id);
             vs = scale_of(c.v_scale, id);
-            next_id = piece_block(step + 2);
+            next_id = piece_block(step + 2 * kEvery);
             // the largest value scale among the pieces that are there
             int e = lane < 4 && ((here >> lane) & 1u) ? exponent_of(vs_now) : -200;
             e = max(e, __shfl_xor_sync(kFullWarp, e, 1));
             e = max(e, __shfl_xor_sync(kFullWarp, e, 2));
             e = __shfl_sync(kFullWarp, e, 0);
-            float kf[4];
+            float kf[4], vf[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kf[i] = fminf(__shfl_sync(kFullWarp, ks_now, i) * undo, 3.0e38f);
-            ok = mbar_wait_or_fail(smem_addr(&s_full[tile][b]), (step / kBuffers) & 1, &failed);
+            for (int i = 0; i < 4; ++i) {
+                kf[i] = fminf(fmaxf(__shfl_sync(kFullWarp, ks_now, i) * undo, 1.2e-38f), 3.0e38f);
+                vf[i] = __shfl_sync(kFullWarp, vs_now, i);
+            }
+            ok = mbar_wait_or_fail(smem_addr(&s_full[b]), (TILES == 1 ? step / 3 : step) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
-            uint32_t raw_s[2][32];
-            tmem_load32(tmem + lanes + Tile::s(tile, b), raw_s[0]);
-            tmem_load32(tmem + lanes + Tile::s(tile, b) + 32, raw_s[1]);
+            uint32_t s[2][32];
+            tmem_load32(tmem + lanes + Tile::s(b), s[0]);
+            tmem_load32(tmem + lanes + Tile::s(b) + 32, s[1]);
             tmem_load_wait();
-            float s[64];
             const int token0 = (first + step) * kStep;
-#pragma unroll
-            for (int j = 0; j < 64; ++j) s[j] = __uint_as_float(raw_s[j >> 5][j & 31]) * kf[j >> 4];
             if (here != 0xfu || token0 + kStep > all_see) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
-                    if (token0 + j > limit || !((here >> (j >> 4)) & 1u)) s[j] = -INFINITY;
+                    if (token0 + j > limit || !((here >> (j >> 4)) & 1u)) s[j >> 5][j & 31] = 0xff800000u;
             }
-            float top = s[0];
-#pragma unroll
-            for (int j = 1; j < 64; ++j) top = fmaxf(top, s[j]);
+            const float top = fmaxf(max3(max16(s[0]) * kf[0], max16(s[0] + 16) * kf[1], max16(s[1]) * kf[2]), max16(s[1] + 16) * kf[3]);
             if (__any_sync(kFullWarp, top > m + kRaise) || e > reference + kRaiseScale) {
                 const float most = fmaxf(m, top), f = exp2_fast(m - most);
                 const int to = max(reference, e);
                 m = most;
                 l *= f;
-                if (step > 0) {
-                    ok = mbar_wait_or_fail(smem_addr(&pv_done[tile]), (step - 1) & 1, &failed);
+                if (turn > 0) {
+                    ok = mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turn - 1) & 1, &failed);
                     if (!__all_sync(kFullWarp, ok)) break;
                     tcgen05_fence_after();
                     const float by = f * pow2(reference - to);
 #pragma unroll 1
-                    for (int d = 0; d < D; d += 32) {
-                        uint32_t v[32];
-                        tmem_load32(tmem + lanes + Tile::o(tile) + d, v);
+                    for (int d = 0; d < D; d += 16) {
+                        uint32_t v[16];
+                        tmem_load16(tmem + lanes + Tile::o(stream) + d, v);
                         tmem_load_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
-                        tmem_store32(tmem + lanes + Tile::o(tile) + d, v);
+                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
+                        tmem_store16(tmem + lanes + Tile::o(stream) + d, v);
                     }
                 }
                 reference = to;
             }
-            float vf[4];
+            // value scales relative to the reference: at most 2^40
+            const float down = pow2((-reference) / 2), rest = pow2(-reference - (-reference) / 2);
+            float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {  // relative to the reference, at most 2^40
-                const float scale = __shfl_sync(kFullWarp, vs_now, i);
-                const int down = -reference;
-                vf[i] = scale * pow2(down / 2) * pow2(down - down / 2);
-            }
-            uint32_t hi[32], lo[32];
-            float sum0 = 0.0f, sum1 = 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                const float2 factor = make_float2(kf[i], kf[i]), less = make_float2(-m, -m);
+                const float v = vf[i] * down * rest;
+                uint32_t part[2][8];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const float p0 = exp2_fast(s[2 * j] - m), p1 = exp2_fast(s[2 * j + 1] - m);
-                sum0 += p0;
-                sum1 += p1;
-                const float x0 = p0 * vf[j >> 3], x1 = p1 * vf[j >> 3];
-                hi[j] = pack_bf16(x0, x1);
-                lo[j] = pack_bf16(x0 - __uint_as_float(hi[j] << 16), x1 - __uint_as_float(hi[j] & 0xffff0000u));
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t *at = &s[i >> 1][(i & 1) * 16 + 2 * j];
+                    float2 p = fma2(make_float2(__uint_as_float(at[0]), __uint_as_float(at[1])), factor, less);
+                    p.x = exp2_fast(p.x);
+                    p.y = exp2_fast(p.y);
+                    sum = add2(sum, p);
+                    p = mul2(p, make_float2(v, v));
+                    const uint32_t hi = pack_bf16(p.x, p.y);
+                    p = fma2(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), make_float2(-1.0f, -1.0f), p);
+                    part[0][j] = hi;
+                    part[1][j] = pack_bf16(p.x, p.y);
+                }
+                tmem_store8(tmem + lanes + Tile::s(b) + i * 8, part[0]);
+                tmem_store8(tmem + lanes + Tile::s(b) + 32 + i * 8, part[1]);
             }
-            l += sum0 + sum1;
-            tmem_store32(tmem + lanes + Tile::s(tile, b), hi);
-            tmem_store32(tmem + lanes + Tile::s(tile, b) + 32, lo);
+            l += sum.x + sum.y;
             tmem_store_wait();
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&p_full[tile][b]));
+            if (lane == 0) mbar_arrive(smem_addr(&p_full[b]));
         }
-        // the sums
-        if (count > 0) {
-            ok = ok && mbar_wait_or_fail(smem_addr(&pv_done[tile]), (count - 1) & 1, &failed);
-            ok = __all_sync(kFullWarp, ok);
+        // the sums: of both groups, each taking half of the columns, or of this one's rows
+        const int lanes_row = (warp & 3) * 32 + lane;
+        float4 mine = make_float4(m, l, pow2(max(reference, -126)), 0.0f), other = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
+        if (turns > 0) ok = ok && mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turns - 1) & 1, &failed);
+        const int other_turns = TILES == 1 ? (count - (1 - stream) + 1) / 2 : 0;
+        if constexpr (TILES == 1) {
+            if (other_turns > 0) ok = ok && mbar_wait_or_fail(smem_addr(&pv_done[1 - stream]), (other_turns - 1) & 1, &failed);
+            group_sums[stream][lanes_row] = mine;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            other = group_sums[1 - stream][lanes_row];
         }
+        ok = __all_sync(kFullWarp, ok);
         tcgen05_fence_after();
         const int64_t pair = (g.begin + row / a.rows) * c.n_kv_heads + head;
         const int64_t part = (pair * a.parts.splits + blockIdx.x) * a.rows + row % a.rows;
+        const float most = fmaxf(mine.x, other.x), mine_f = exp2_fast(mine.x - most), other_f = exp2_fast(other.x - most);
+        const float total = mine.y * mine_f + other.y * other_f, inverse = total == 0.0f ? 0.0f : 1.0f / total;
         if (count > 0 && ok) {
-            const float inverse = l == 0.0f ? 0.0f : 1.0f / l, back = pow2(max(reference, -126));
+            constexpr int kColumns = TILES == 1 ? D / 2 : D;
+            const int d0 = TILES == 1 ? stream * kColumns : 0;
 #pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
-                uint32_t v[32];
-                tmem_load32(tmem + lanes + Tile::o(tile) + d, v);
+            for (int d = d0; d < d0 + kColumns; d += 16) {
+                uint32_t v[16], w[16];
+                if (turns > 0) tmem_load16(tmem + lanes + Tile::o(stream) + d, v);
+                if (other_turns > 0) tmem_load16(tmem + lanes + Tile::o(1 - stream) + d, w);
                 tmem_load_wait();
                 if (row < rows) {
                     float4 *to = reinterpret_cast<float4 *>(a.parts.o + part * D + d);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < 4; ++j) {
                         float y[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            y[k] = __uint_as_float(v[j * 4 + k]) * inverse * back;
+                            y[k] = turns > 0 ? __uint_as_float(v[j * 4 + k]) * (mine_f * inverse) * mine.z : 0.0f;
+                            if (other_turns > 0) y[k] += __uint_as_float(w[j * 4 + k]) * (other_f * inverse) * other.z;
                             if (nan_from[d + j * 4 + k] <= limit) y[k] = __uint_as_float(0x7fc00000u);
                         }
                         to[j] = make_float4(y[0], y[1], y[2], y[3]);
@@ -462,7 +537,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 __syncwarp();
             }
         }
-        if (row < rows && tokens > 0) a.parts.ml[part] = make_float2(m, l);
+        if (row < rows && tokens > 0 && (TILES == 2 || stream == 0)) a.parts.ml[part] = make_float2(most, total);
         tcgen05_fence_before();
     }
     __syncthreads();

@@ -48,6 +48,20 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0u;
 }
+// The same at once, without waiting a while.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0u;
+}
+// A wait has run out: the block gives up.
+__device__ __forceinline__ void mbar_give_up(volatile uint32_t *failed) {
+    *failed = 1u;
+    atomicAdd(&g_expired_waits, 1u);
+}
 // True once the phase of the given parity has completed; false if the wait ran out or another
 // thread of the block has given up.
 __device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity, volatile uint32_t *failed) {
@@ -56,8 +70,7 @@ __device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity,
         if (mbar_try(bar, parity)) return true;
         if (*failed != 0u) return false;
     }
-    *failed = 1u;
-    atomicAdd(&g_expired_waits, 1u);
+    mbar_give_up(failed);
     return false;
 }
 
