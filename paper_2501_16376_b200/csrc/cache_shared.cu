@@ -11,11 +11,12 @@
 // e4m3 converts exactly to binary16 and bf16, and the queries enter as they are.  P times the value
 // scale enters in two bf16 parts: 2^-18 of itself, with binary32's range, so that no scale needs a
 // reference but in the last exponents.  A thread owns a row: its maximum and sum stay in registers,
-// and nothing crosses lanes.  The maximum is raised only when a score exceeds it by more than 2^8.
+// and nothing crosses lanes.  The maximum is raised only when weights reach 2^14, which spares a pass
+// over the scores.
 //
 // Two groups of four softmax warps, each with sums of its own, hide one another's latency: with 256
 // rows each has 128 of them, with 128 they take the steps in turn and their sums are joined at the end.
-// Four warps convert, one issues products, one copies.
+// Four warps convert keys, four values, one issues products, one copies, one looks scales up.
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -27,7 +28,10 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;
-constexpr float kRaise = 8.0f;       // how far (in powers of two) a score may exceed the maximum
+constexpr float kRaise = 16384.0f;   // weights of 16 tokens whose sum reaches this raise the maximum
+constexpr int kScaleSlots = 8;       // steps of scales
+constexpr float kFarMaximum = 1073741824.0f;  // 2^30: scores are whole multiples of 64 from here on
+constexpr int kFarScale = -40;       // of a value scale below the reference
 constexpr int kRaiseScale = 40;      // how far a value scale may exceed its reference
 constexpr int kStep = 64;            // tokens
 constexpr int kTmemColumns = 512;
@@ -40,9 +44,11 @@ struct PrefixTile {
     static constexpr int kRawBytes = 2 * kStep * D;            // keys, then values
     static constexpr int kHalfBytes = kStep * 128;             // 64 converted columns
     static constexpr int kConvBytes = D / 64 * kHalfBytes;     // keys (or values) of a step
-    static constexpr int kSmem = kSlots * kRawBytes + 2 * kConverted * kConvBytes;
+    static constexpr int kStageBytes = 8 * 4096;               // of queries on their way: the values' place, and more
+    static constexpr int kSmem = kSlots * kRawBytes + kConverted * kConvBytes + std::max(kConverted * kConvBytes, kStageBytes);
     static constexpr int kSoftmaxWarps = 8;
-    static constexpr int kWarps = kSoftmaxWarps + 4 + 2;
+    static constexpr int kConvertWarps = 8;                    // half of them keys, half values
+    static constexpr int kWarps = kSoftmaxWarps + kConvertWarps + 3;
     // tensor memory: queries of a tile, scores, sums of a stream
     static __device__ constexpr uint32_t q(int t) { return t * 64; }
     static __device__ constexpr uint32_t s(int b) { return TILES * 64 + b * 64; }
@@ -61,23 +67,13 @@ struct PrefixArgs {
     int row_tiles, splits;  // blocks along the rows, along the prefix
     int block_shift;
     float scale_log2;
+    bool q_pieces;          // whether queries lie on 16-byte boundaries
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// Four e4m3 codes -> four 16-bit floats (exact).
-template <bool BF16>
-__device__ __forceinline__ uint2 convert4(uint32_t w) {
-    uint2 h;
-    e4m3_to_f16(w, h.x, h.y);
-    if constexpr (BF16) {
-        h.x = f16_to_bf16(h.x);
-        h.y = f16_to_bf16(h.y);
-    }
-    return h;
 }
 // Pairs of binary32 values in one instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -100,6 +96,24 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         "add.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+}
+// a less one half of a pair of bf16 values, in one instruction.
+template <int HALF>
+__device__ __forceinline__ float less_bf16(float a, uint32_t pair) {
+    unsigned short lo, hi;
+    asm("mov.b32 {%0, %1}, %2;" : "=h"(lo), "=h"(hi) : "r"(pair));
+    float d;
+    asm("fma.rn.f32.bf16 %0, %1, %2, %3;" : "=f"(d) : "h"(HALF ? hi : lo), "h"(static_cast<unsigned short>(0xbf80)), "f"(a));
+    return d;
+}
+// 32 values -> two bf16 parts of each.
+__device__ __forceinline__ void split16(float2 (&p)[16], uint32_t (&part)[32]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) part[j] = pack_bf16(p[j].x, p[j].y);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) p[j] = make_float2(less_bf16<0>(p[j].x, part[j]), less_bf16<1>(p[j].y, part[j]));
+#pragma unroll
+    for (int j = 0; j < 16; ++j) part[16 + j] = pack_bf16(p[j].x, p[j].y);
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -134,7 +148,12 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], pv_done[2], drained;
     __shared__ uint32_t tmem_base, failed, present[kSlots];
     __shared__ float4 group_sums[2][128];  // TILES == 1: maximum, sum, 2^reference of a group's rows
-    __shared__ int all_see, nan_from[D];
+    __shared__ uint64_t q_full, scale_full[kScaleSlots], scale_empty[kScaleSlots];
+    __shared__ float4 scale_k[kScaleSlots];  // of 16 tokens each
+    __shared__ int4 scale_v[kScaleSlots];    // as exponents, less the reference
+    __shared__ int2 scale_info[kScaleSlots];                       // which of the four are there; the reference
+    __shared__ int all_see, any_nan, nan_from[D];
+    __shared__ uint32_t row_top[2][128];
     const sp_cache &c = a.cache;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const int head = blockIdx.y / a.row_tiles, row0 = blockIdx.y % a.row_tiles * (128 * TILES);
@@ -143,7 +162,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         tma_prefetch_map(&v_map);
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(smem_addr(&raw_full[i]), 1);
-            mbar_init(smem_addr(&raw_empty[i]), 4);
+            mbar_init(smem_addr(&raw_empty[i]), 8);
         }
         for (int i = 0; i < kConverted; ++i) {
             mbar_init(smem_addr(&k_full[i]), 4);
@@ -158,12 +177,23 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         mbar_init(smem_addr(&pv_done[0]), 1);
         mbar_init(smem_addr(&pv_done[1]), 1);
         mbar_init(smem_addr(&drained), 1);
+        mbar_init(smem_addr(&q_full), kSoftmaxWarps);
+        for (int i = 0; i < kScaleSlots; ++i) {
+            mbar_init(smem_addr(&scale_full[i]), 1);
+            mbar_init(smem_addr(&scale_empty[i]), 4 * TILES);
+        }
         failed = 0u;
         all_see = 0x7fffffff;
+        any_nan = 0;
         mbar_fence_init();
     }
     for (int d = threadIdx.x; d < D; d += Tile::kWarps * 32) nan_from[d] = 0x7fffffff;
-    if (warp == kSoftmaxWarps + 4) tmem_alloc(&tmem_base, kTmemColumns);
+    constexpr int kProducts = kSoftmaxWarps + Tile::kConvertWarps, kCopies = kProducts + 1, kScales = kProducts + 2;
+    if (warp == kProducts) tmem_alloc(&tmem_base, kTmemColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base;
     pdl_wait();
     pdl_launch_dependents();  // the kernel over the tails counts on what came before this one
 
@@ -181,80 +211,57 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         return static_cast<uint32_t>(id) < static_cast<uint32_t>(c.n_blocks) ? id : -1;
     };
 
-    // the row of this thread: its place, and its queries
-    const int stream = warp >> 2, tile = TILES == 1 ? 0 : stream, row = row0 + tile * 128 + (warp & 3) * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    int limit = -1;        // the last token that it sees
-    float undo = fabsf(a.scale_log2);  // its sign goes to the queries: factors of scores are positive
-    uint4 q[D / 8];
-    if (warp < kSoftmaxWarps) {
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (row < rows) {
-            const int64_t seq = g.begin + row / a.rows, i = row % a.rows / a.group;
-            limit = static_cast<int>(max(int64_t(-1), min(min(a.lens[seq] - a.n_q + i, min(int64_t(a.lens[seq]), a.max_len) - 1), int64_t(tokens))));
-            atomicMin(&all_see, limit + 1);
-            const uint16_t *from = a.Q + seq * a.q.seq + i * a.q.token + (head * a.group + row % a.group) * a.q.head;
-            if ((reinterpret_cast<uintptr_t>(from) & 15u) == 0) {
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) q[i] = *reinterpret_cast<const uint4 *>(from + i * 8);
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = from[i * 8 + 2 * k] | uint32_t(from[i * 8 + 2 * k + 1]) << 16;
-                    q[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
-        }
-        if constexpr (BF16) {
-            // sums of products with codes up to 448 stay in binary32's range
-            uint32_t top = 0;
-            uint32_t *w = reinterpret_cast<uint32_t *>(q);
-#pragma unroll
-            for (int i = 0; i < D / 2; ++i) {
-                const uint32_t lo = (w[i] << 16) & 0x7fffffffu, hi = w[i] & 0x7fff0000u;
-                top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-            }
-            if (top > kLargeQuery) {
-                undo *= pow2(64);
-#pragma unroll
-                for (int i = 0; i < D / 2; ++i) {
-                    const float2 v = unpack2<true>(w[i]);
-                    w[i] = pack_bf16(v.x * pow2(-64), v.y * pow2(-64));
-                }
-            }
-        }
-    }
-    if (a.scale_log2 < 0.0f)
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) q[i] = make_uint4(q[i].x ^ 0x80008000u, q[i].y ^ 0x80008000u, q[i].z ^ 0x80008000u, q[i].w ^ 0x80008000u);
-    tcgen05_fence_before();
-    __syncthreads();
-    tcgen05_fence_after();
-    const uint32_t tmem = tmem_base;
-    if (warp < 4 * TILES) {
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) tmem_store32(tmem + lanes + Tile::q(tile) + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&q[i * 8]));
-        tmem_store_wait();
-        tcgen05_fence_before();
-    }
-    __syncthreads();
-    tcgen05_fence_after();
     const uint32_t raw = smem_addr(smem), conv = raw + kSlots * Tile::kRawBytes;  // conv: keys, then values
 
-    if (warp == kSoftmaxWarps + 5) {
-        // ---- copies: a lane a block of the cache.  A load of the table takes longer than a step, so the
-        // lanes hold the blocks of several steps, and those of the next ones are on their way
-        const int blocks = kStep >> shift, held = 32 / blocks;  // of a step: 4, 2 or 1
+    // The lanes of a warp hold the blocks of several steps: a load of the table takes longer than a step.
+    const int blocks = kStep >> shift, held = 32 / blocks;  // of a step: 4, 2 or 1
+    auto blocks_from = [&](int step) {
+        const int mine = step + lane / blocks;
+        return mine < count ? block_at((first + mine) * kStep + (lane % blocks << shift)) : -1;
+    };
+    if (warp == kScales) {
+        // ---- scales: the values' over a power of two that follows the largest by at most 2^40
+        auto scale_of = [&](const float *scales, int id) { return id >= 0 ? scales[int64_t(id) * c.n_kv_heads + head] : 0.0f; };
+        int id = blocks_from(0), next_id = blocks_from(held), after_id = blocks_from(2 * held), reference = -200;
+        float ks = scale_of(c.k_scale, id), vs = scale_of(c.v_scale, id);
+        float next_ks = scale_of(c.k_scale, next_id), next_vs = scale_of(c.v_scale, next_id);
+        RingPlace<kScaleSlots> at;
+        bool ok = true;
+        for (int step = 0; step < count; ++step, at.next()) {
+            const int turn = step % held;
+            if (step > 0 && turn == 0) {
+                id = next_id;
+                ks = next_ks;
+                vs = next_vs;
+                next_id = after_id;
+                next_ks = scale_of(c.k_scale, next_id);
+                next_vs = scale_of(c.v_scale, next_id);
+                after_id = blocks_from(step + 2 * held);
+            }
+            // lanes 0 .. 3 take a piece of 16 tokens
+            const int holder = turn * blocks + ((lane & 3) * 16 >> shift);
+            const int piece_id = __shfl_sync(kFullWarp, id, holder);
+            const float piece_k = __shfl_sync(kFullWarp, ks, holder), piece_v = __shfl_sync(kFullWarp, vs, holder);
+            const unsigned here = __ballot_sync(kFullWarp, piece_id >= 0) & 0xfu;
+            int e = piece_id >= 0 ? exponent_of(piece_v) : -200;
+            e = max(e, __shfl_xor_sync(kFullWarp, e, 1));
+            e = max(e, __shfl_xor_sync(kFullWarp, e, 2));
+            if (e > reference + kRaiseScale) reference = e;
+            if (step >= kScaleSlots) ok = mbar_wait_or_fail(smem_addr(&scale_empty[at.slot]), at.parity ^ 1u, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
+            if (lane < 4) {
+                reinterpret_cast<float *>(&scale_k[at.slot])[lane] = piece_k;
+                reinterpret_cast<int *>(&scale_v[at.slot])[lane] = piece_id >= 0 ? exponent_of(piece_v) - reference : 0;
+            }
+            if (lane == 0) scale_info[at.slot] = make_int2(static_cast<int>(here), reference);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&scale_full[at.slot]));
+        }
+    } else if (warp == kCopies) {
+        // ---- copies: a lane a block of the cache
         const uint32_t piece = static_cast<uint32_t>(D) << shift;
         RingPlace<kSlots> at;
         bool ok = true;
-        auto blocks_from = [&](int step) {
-            const int mine = step + lane / blocks;
-            return mine < count ? block_at((first + mine) * kStep + (lane % blocks << shift)) : -1;
-        };
         int ids = blocks_from(0), next_ids = blocks_from(held), issued = 0;
         for (int step = 0; step < count; ++step, at.next()) {
             const int turn = step % held;
@@ -283,9 +290,11 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
         if (failed != 0u && lane == 0)
             for (int s = max(0, issued - kSlots); s < issued; ++s) mbar_wait(smem_addr(&raw_full[s % kSlots]), (s / kSlots) & 1);
-    } else if (warp == kSoftmaxWarps + 4) {
+    } else if (warp == kProducts) {
         // ---- products
-        if (elect_one()) {
+        const bool begun = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&q_full), 0, &failed));
+        tcgen05_fence_after();
+        if (begun && elect_one()) {
             const uint32_t qk = f16_instruction(kStep, BF16), pv = f16_instruction(D, true) | kColumnsB;
             // Whichever product has its operands goes next; products run in the order of their issue.  A
             // step's scores go where the weights of three steps before (of the step before) were.
@@ -302,8 +311,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                         const int g = TILES == 1 ? v & 1 : t;
                         const uint64_t values = desc_columns128(conv + (kConverted + v_at) * Tile::kConvBytes, Tile::kHalfBytes);
 #pragma unroll
-                        for (int p = 0; p < 8; ++p)  // two parts of P, 64 tokens each
-                            mma_16bit(tmem + Tile::o(g), tmem + Tile::s(p_at) + p * 8, values + (p & 3) * (16 * 128 / 16), pv,
+                        for (int p = 0; p < 8; ++p)  // of 32 tokens both parts, 16 tokens each
+                            mma_16bit(tmem + Tile::o(g), tmem + Tile::s(p_at) + p * 8, values + ((p >> 2) * 2 + (p & 1)) * (16 * 128 / 16), pv,
                                       v >= (TILES == 1 ? 2 : 1) || p > 0);
                         tcgen05_commit(smem_addr(&pv_done[g]));
                         ++weighed[t];
@@ -334,165 +343,323 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             __syncwarp();
             if (lane == 0) mbar_wait(smem_addr(&drained), 0);
         }
-    } else if (warp >= kSoftmaxWarps) {
-        // ---- conversion: a thread 16 codes at a time
-        const int thread = threadIdx.x - kSoftmaxWarps * 32;
-        constexpr int kChunks = D / 16;
+    } else if (warp >= kSoftmaxWarps && warp < kProducts) {
+        // ---- conversion: a thread 16 codes at a time; four warps keys, four values
+        const int thread = threadIdx.x & 127;
+        constexpr int kEach = kStep * D / 16 / 128;
+        // Eight lanes read and write all banks: of the chunks of a row's half and those of the row whose
+        // number differs in bits 0 and 2 (D = 64: of a row and the next).
+        int r[kEach], ch[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int x = i * 128 + thread;
+            r[i] = D == 128 ? (x >> 4 << 1) ^ (x & 4 ? 5 : 0) : x >> 2;
+            ch[i] = D == 128 ? (x >> 1 & 4) | (x & 3) : x & 3;
+        }
         RingPlace<kSlots> at;
-        bool ok = true;
-        for (int step = 0; step < count; ++step, at.next()) {
-            ok = mbar_wait_or_fail(smem_addr(&raw_full[at.slot]), at.parity, &failed);
-            const int buffer = step % kConverted, uses = step / kConverted;
-            if (ok && uses > 0) ok = mbar_wait_or_fail(smem_addr(&k_empty[buffer]), (uses - 1) & 1, &failed);
-            if (!__all_sync(kFullWarp, ok)) break;
-            const uint32_t from = raw + at.slot * Tile::kRawBytes, here = present[at.slot];
-            const int token0 = (first + step) * kStep;
-            const bool checked = token0 + kStep > all_see;  // some rows do not see all of it
-            auto convert = [&](auto is_key) {
-                constexpr bool KEY = decltype(is_key)::value;
-                const uint32_t src = from + (KEY ? 0 : kStep * D), dst = conv + (KEY ? buffer : kConverted + buffer) * Tile::kConvBytes;
-                constexpr int kEach = kStep * kChunks / 128;
+        auto convert_steps = [&](auto is_key) {
+            constexpr bool KEY = decltype(is_key)::value;
+            uint64_t *full = KEY ? k_full : v_full, *empty = KEY ? k_empty : v_empty;
+            // which tokens all rows see is known when the queries are there
+            bool ok = KEY || mbar_wait_or_fail(smem_addr(&q_full), 0, &failed);
+            int buffer = 0, uses = 0;
+            for (int step = 0; step < count; ++step, at.next()) {
+                ok = ok && mbar_wait_or_fail(smem_addr(&raw_full[at.slot]), at.parity, &failed);
+                if (!__all_sync(kFullWarp, ok)) break;
+                const uint32_t from = raw + at.slot * Tile::kRawBytes + (KEY ? 0 : kStep * D), here = present[at.slot];
+                const uint32_t to = conv + (KEY ? buffer : kConverted + buffer) * Tile::kConvBytes;
                 uint4 w[kEach];
-                // eight lanes: a row's chunks (D = 64: of two rows)
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
-                    const int x = i * 128 + thread, r = x / kChunks, ch = x % kChunks;
-                    const int swap = D == 128 ? r & 7 : (r >> 1) & 3;
-                    w[i] = load_shared16(src + r * D + ((ch ^ swap) << 4));
+                    const int swap = D == 128 ? r[i] & 7 : (r[i] >> 1) & 3;
+                    w[i] = load_shared16(from + r[i] * D + ((ch[i] ^ swap) << 4));
                 }
+                if constexpr (!KEY) {
+                    const int token0 = (first + step) * kStep;
+                    if (token0 + kStep > all_see) {
+                        // NaN that some rows do not see: 0 here, and noted for those who do
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int x = i * 128 + thread, r = x / kChunks, ch = x % kChunks;
-                    if constexpr (!KEY) {
-                        if (!((here >> (r >> shift)) & 1u)) {
-                            w[i] = make_uint4(0u, 0u, 0u, 0u);
-                        } else if (checked) {
+                        for (int i = 0; i < kEach; ++i) {
+                            if (!((here >> (r[i] >> shift)) & 1u)) continue;
                             uint32_t *word = reinterpret_cast<uint32_t *>(&w[i]);
 #pragma unroll
                             for (int k = 0; k < 16; ++k)
                                 if (((word[k >> 2] >> (8 * (k & 3))) & 0x7fu) == 0x7fu) {
-                                    atomicMin(&nan_from[ch * 16 + k], token0 + r);
+                                    atomicMin(&nan_from[ch[i] * 16 + k], token0 + r[i]);
+                                    any_nan = 1;
                                     word[k >> 2] &= ~(0xffu << (8 * (k & 3)));
                                 }
                         }
                     }
-                    const uint2 a0 = convert4<KEY ? BF16 : true>(w[i].x), a1 = convert4<KEY ? BF16 : true>(w[i].y);
-                    const uint2 a2 = convert4<KEY ? BF16 : true>(w[i].z), a3 = convert4<KEY ? BF16 : true>(w[i].w);
-                    const uint32_t to = dst + (ch >> 2) * Tile::kHalfBytes + r * 128, c0 = (ch & 3) * 2;
-                    store_shared16(to + ((c0 ^ (r & 7)) << 4), a0.x, a0.y, a1.x, a1.y);
-                    store_shared16(to + (((c0 + 1) ^ (r & 7)) << 4), a2.x, a2.y, a3.x, a3.y);
+                    if (here != (kStep >> shift == 4 ? 0xfu : kStep >> shift == 2 ? 3u : 1u)) {
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i)
+                            if (!((here >> (r[i] >> shift)) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                    }
                 }
-            };
-            convert(std::true_type{});
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&k_full[buffer]));
-            if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&v_empty[buffer]), (uses - 1) & 1, &failed);
-            if (!__all_sync(kFullWarp, ok)) break;
-            convert(std::false_type{});
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_addr(&v_full[buffer]));
-                mbar_arrive(smem_addr(&raw_empty[at.slot]));
+                if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&empty[buffer]), (uses - 1) & 1, &failed);
+                if (!__all_sync(kFullWarp, ok)) break;
+                if (lane == 0) mbar_arrive(smem_addr(&raw_empty[at.slot]));
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    uint32_t h[8];
+                    const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) e4m3_to_f16(words[k], h[2 * k], h[2 * k + 1]);
+                    if constexpr (!KEY || BF16) {
+                        float2 f[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] = unpack2<false>(h[k]);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) h[k] = pack_bf16(f[k].x, f[k].y);
+                    }
+                    const uint32_t row_at = to + (ch[i] >> 2) * Tile::kHalfBytes + r[i] * 128, c0 = (ch[i] & 3) * 2;
+                    store_shared16(row_at + ((c0 ^ (r[i] & 7)) << 4), h[0], h[1], h[2], h[3]);
+                    store_shared16(row_at + (((c0 + 1) ^ (r[i] & 7)) << 4), h[4], h[5], h[6], h[7]);
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&full[buffer]));
+                if (++buffer == kConverted) {
+                    buffer = 0;
+                    ++uses;
+                }
             }
-        }
-    } else {
+        };
+        if (warp < kSoftmaxWarps + 4) convert_steps(std::true_type{});
+        else convert_steps(std::false_type{});
+    } else if (warp < kSoftmaxWarps) {
         // ---- softmax: a thread a row, of the steps stream, stream + kEvery, ...
+        const int stream = warp >> 2, tile = TILES == 1 ? 0 : stream, row = row0 + tile * 128 + (warp & 3) * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        int limit = 0x7ffffffe;            // the last token that the row sees
+        float undo = fabsf(a.scale_log2);  // its sign goes to the queries: factors of scores are positive
+        {
+            // A warp brings 64 columns of its rows at a time (with 128 rows, the groups take one each where
+            // a head has 128): read along the rows, and turned in shared memory, the values' own from here
+            // on only, so that a thread gets its row's.
+            constexpr int kHalves = TILES == 1 ? 1 : D / 64;
+            const bool loads = TILES == 2 || stream < D / 64;
+            const int half0 = TILES == 1 ? stream : 0;
+            const uint32_t stage = conv + kConverted * Tile::kConvBytes + warp * 4096;
+            const bool valid = row < rows;
+            const int64_t seq = g.begin + row / a.rows, i = row % a.rows / a.group;
+            const int64_t at = seq * a.q.seq + i * a.q.token + (head * a.group + row % a.group) * a.q.head;
+            const unsigned all_valid = __ballot_sync(kFullWarp, valid);
+            uint32_t q[kHalves][32];
+            if (loads && a.q_pieces) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    uint4 w[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = k * 4 + (lane >> 3);
+                        const int64_t from = __shfl_sync(kFullWarp, at, r) + (half0 + h) * 64 + (lane & 7) * 8;
+                        w[k] = (all_valid >> r) & 1u ? *reinterpret_cast<const uint4 *>(a.Q + from) : make_uint4(0u, 0u, 0u, 0u);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = k * 4 + (lane >> 3);
+                        store_shared16(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4), w[k].x, w[k].y, w[k].z, w[k].w);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *reinterpret_cast<uint4 *>(&q[h][k * 4]) = load_shared16(stage + lane * 128 + ((k ^ (lane & 7)) << 4));
+                    __syncwarp();
+                }
+            } else if (loads) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const uint16_t *from = a.Q + at + (half0 + h) * 64 + 2 * k;
+                        q[h][k] = valid ? from[0] | uint32_t(from[1]) << 16 : 0u;
+                    }
+            }
+            if (valid) {
+                const int64_t len = a.lens[seq];
+                limit = static_cast<int>(max(int64_t(-1), min(min(len - a.n_q + i, min(len, a.max_len) - 1), int64_t(tokens))));
+            }
+            const int least = __reduce_min_sync(kFullWarp, limit);
+            if (lane == 0) atomicMin(&all_see, least + 1);
+            if constexpr (BF16) {
+                // sums of products with codes up to 448 stay in binary32's range
+                uint32_t top = 0;
+                if (loads)
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) top = __vmaxu2(top, q[h][k] & 0x7fff7fffu);
+                top = max(top & 0xffffu, top >> 16);
+                if constexpr (TILES == 1) {
+                    row_top[stream][row - row0] = top;
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    top = max(top, row_top[1 - stream][row - row0]);
+                }
+                if (top > kLargeQuery >> 16) {
+                    undo *= pow2(64);
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const float2 v = unpack2<true>(q[h][k]);
+                            q[h][k] = pack_bf16(v.x * pow2(-64), v.y * pow2(-64));
+                        }
+                }
+            }
+            const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+            __syncwarp();
+            if (loads) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) q[h][k] ^= sign;
+                    tmem_store32(tmem + lanes + Tile::q(tile) + (half0 + h) * 32, q[h]);
+                }
+                tmem_store_wait();
+                tcgen05_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&q_full));
+        }
         constexpr int kEvery = TILES == 1 ? 2 : 1;
         const int from = TILES == 1 ? stream : 0, turns = (count - from + kEvery - 1) / kEvery;
         float m = kLowest, l = 0.0f;
         int reference = -200;  // of the value scales, as an exponent
-        bool ok = true;
-        // scales of a step: lanes 0 .. 3 hold those of its 16-token pieces
-        auto piece_block = [&](int step) { return lane < 4 && step < count ? block_at((first + step) * kStep + lane * 16) : -1; };
-        auto scale_of = [&](const float *scales, int id) { return id >= 0 ? scales[int64_t(id) * c.n_kv_heads + head] : 0.0f; };
-        int id = piece_block(from), next_id = piece_block(from + kEvery);
-        float ks = scale_of(c.k_scale, id), vs = scale_of(c.v_scale, id);
+        bool ok = mbar_wait_or_fail(smem_addr(&q_full), 0, &failed);  // all_see is final
+        RingPlace<kScaleSlots> scale_at;
+        if (from == 1) scale_at.next();
+        bool far_maximum = false;  // of a row of the warp
+        // sums of the steps before, by a row's own factor
+        auto scale_sums = [&](int turn, float by) {
+            if (turn == 0) return true;
+            const bool ok = mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turn - 1) & 1, &failed);
+            if (!__all_sync(kFullWarp, ok)) return false;
+            tcgen05_fence_after();
+#pragma unroll 1
+            for (int d = 0; d < D; d += 16) {
+                uint32_t v[16];
+                tmem_load16(tmem + lanes + Tile::o(stream) + d, v);
+                tmem_load_wait(v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
+                tmem_store16(tmem + lanes + Tile::o(stream) + d, v);
+            }
+            return true;
+        };
         for (int turn = 0; turn < turns; ++turn) {
             const int step = from + turn * kEvery, b = TILES == 1 ? step % 3 : stream;
-            const unsigned here = __ballot_sync(kFullWarp, id >= 0) & 0xfu;
-            const float ks_now = ks, vs_now = vs;
-            id = next_id;
-            ks = scale_of(c.k_scale, id);
-            vs = scale_of(c.v_scale, id);
-            next_id = piece_block(step + 2 * kEvery);
-            // the largest value scale among the pieces that are there
-            int e = lane < 4 && ((here >> lane) & 1u) ? exponent_of(vs_now) : -200;
-            e = max(e, __shfl_xor_sync(kFullWarp, e, 1));
-            e = max(e, __shfl_xor_sync(kFullWarp, e, 2));
-            e = __shfl_sync(kFullWarp, e, 0);
-            float kf[4], vf[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                kf[i] = fminf(fmaxf(__shfl_sync(kFullWarp, ks_now, i) * undo, 1.2e-38f), 3.0e38f);
-                vf[i] = __shfl_sync(kFullWarp, vs_now, i);
+            ok = ok && mbar_wait_or_fail(smem_addr(&scale_full[scale_at.slot]), scale_at.parity, &failed);
+            if (!__all_sync(kFullWarp, ok)) break;
+            const int2 info = scale_info[scale_at.slot];
+            const float *ks = reinterpret_cast<const float *>(&scale_k[scale_at.slot]);
+            const int *vs = reinterpret_cast<const int *>(&scale_v[scale_at.slot]);
+            if (info.y != reference) {
+                ok = scale_sums(turn, pow2(reference - info.y));
+                if (!ok) break;
+                reference = info.y;
             }
             ok = mbar_wait_or_fail(smem_addr(&s_full[b]), (TILES == 1 ? step / 3 : step) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             tcgen05_fence_after();
-            uint32_t s[2][32];
-            tmem_load32(tmem + lanes + Tile::s(b), s[0]);
-            tmem_load32(tmem + lanes + Tile::s(b) + 32, s[1]);
-            tmem_load_wait();
+            // 32 tokens at a time; the weights lie where their scores were, first parts and second ones
+            const uint32_t scores = tmem + lanes + Tile::s(b);
             const int token0 = (first + step) * kStep;
-            if (here != 0xfu || token0 + kStep > all_see) {
-#pragma unroll
-                for (int j = 0; j < 64; ++j)
-                    if (token0 + j > limit || !((here >> (j >> 4)) & 1u)) s[j >> 5][j & 31] = 0xff800000u;
-            }
-            const float top = fmaxf(max3(max16(s[0]) * kf[0], max16(s[0] + 16) * kf[1], max16(s[1]) * kf[2]), max16(s[1] + 16) * kf[3]);
-            if (__any_sync(kFullWarp, top > m + kRaise) || e > reference + kRaiseScale) {
-                const float most = fmaxf(m, top), f = exp2_fast(m - most);
-                const int to = max(reference, e);
-                m = most;
-                l *= f;
-                if (turn > 0) {
-                    ok = mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turn - 1) & 1, &failed);
-                    if (!__all_sync(kFullWarp, ok)) break;
-                    tcgen05_fence_after();
-                    const float by = f * pow2(reference - to);
+            const bool masked = info.x != 0xf || token0 + kStep > all_see;
+            float step_sum = 0.0f;
 #pragma unroll 1
-                    for (int d = 0; d < D; d += 16) {
-                        uint32_t v[16];
-                        tmem_load16(tmem + lanes + Tile::o(stream) + d, v);
-                        tmem_load_wait();
+            for (int i = 0; i < 2; ++i) {
+                const float k[2] = {fminf(fmaxf(ks[2 * i] * undo, 1.2e-38f), 3.0e38f), fminf(fmaxf(ks[2 * i + 1] * undo, 1.2e-38f), 3.0e38f)};
+                const int e[2] = {vs[2 * i], vs[2 * i + 1]};
+                float sum;
+                uint32_t part[32];
+                auto load_scores = [&](uint32_t (&now)[32]) {
+                    tmem_load32(scores + i * 32, now);
+                    tmem_load_wait(now);
+                    if (masked) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
-                        tmem_store16(tmem + lanes + Tile::o(stream) + d, v);
+                        for (int j = 0; j < 32; ++j)
+                            if (token0 + i * 32 + j > limit || !((info.x >> (2 * i + (j >> 4))) & 1)) now[j] = 0xff800000u;
+                    }
+                };
+                for (;;) {
+                    // the value scale goes into the exponent, and out of the sum again; step by step for all
+                    // 32, since a warp waits for each of its instructions' operands in turn
+                    float2 p[16];
+                    const bool near = !far_maximum && min(e[0], e[1]) >= kFarScale;
+                    {
+                        uint32_t now[32];
+                        load_scores(now);
+                        if (near) {
+                            const float less[2] = {static_cast<float>(e[0]) - m, static_cast<float>(e[1]) - m};
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                p[j] = fma2(make_float2(__uint_as_float(now[2 * j]), __uint_as_float(now[2 * j + 1])),
+                                            make_float2(k[j >> 3], k[j >> 3]), make_float2(less[j >> 3], less[j >> 3]));
+                        } else {
+                            // scores so large that a product differs from the maximum, itself rounded, by
+                            // powers of two; value scales that would take the weights out of the sum
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                p[j] = add2(mul2(make_float2(__uint_as_float(now[2 * j]), __uint_as_float(now[2 * j + 1])), make_float2(k[j >> 3], k[j >> 3])),
+                                            make_float2(-m, -m));
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) p[j] = make_float2(exp2_fast(p[j].x), exp2_fast(p[j].y));
+                    float sums[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float2 *x = p + 8 * h;
+                        const float2 t = add2(add2(add2(x[0], x[1]), add2(x[2], x[3])), add2(add2(x[4], x[5]), add2(x[6], x[7])));
+                        sums[h] = t.x + t.y;
+                    }
+                    if (near) {
+                        sum = sums[0] * pow2(-e[0]) + sums[1] * pow2(-e[1]);
+                    } else {
+                        sum = sums[0] + sums[1];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) p[j] = mul2(p[j], make_float2(pow2(e[j >> 3]), pow2(e[j >> 3])));
+                    }
+                    split16(p, part);
+                    if (!__any_sync(kFullWarp, sum > kRaise)) break;
+                    // the maximum rises: the sums before, and this step's weights before, follow
+                    uint32_t v[32];
+                    load_scores(v);
+                    const float most = fmaxf(m, fmaxf(max16(v) * k[0], max16(v + 16) * k[1])), f = exp2_fast(m - most);
+                    m = most;
+                    far_maximum = __any_sync(kFullWarp, fabsf(m) > kFarMaximum && m != kLowest);
+                    l *= f;
+                    step_sum *= f;
+                    ok = scale_sums(turn, f);
+                    if (!ok) break;
+                    if (i > 0) {
+                        tmem_store_wait();
+                        tmem_load32(scores, v);
+                        tmem_load_wait(v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            p[j] = mul2(add2(make_float2(__uint_as_float(v[j] << 16), __uint_as_float(v[j] & 0xffff0000u)),
+                                             make_float2(__uint_as_float(v[16 + j] << 16), __uint_as_float(v[16 + j] & 0xffff0000u))), make_float2(f, f));
+                        split16(p, v);
+                        tmem_store32(scores, v);
                     }
                 }
-                reference = to;
+                if (!ok) break;
+                step_sum += sum;
+                tmem_store32(scores + i * 32, part);
             }
-            // value scales relative to the reference: at most 2^40
-            const float down = pow2((-reference) / 2), rest = pow2(-reference - (-reference) / 2);
-            float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 factor = make_float2(kf[i], kf[i]), less = make_float2(-m, -m);
-                const float v = vf[i] * down * rest;
-                uint32_t part[2][8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t *at = &s[i >> 1][(i & 1) * 16 + 2 * j];
-                    float2 p = fma2(make_float2(__uint_as_float(at[0]), __uint_as_float(at[1])), factor, less);
-                    p.x = exp2_fast(p.x);
-                    p.y = exp2_fast(p.y);
-                    sum = add2(sum, p);
-                    p = mul2(p, make_float2(v, v));
-                    const uint32_t hi = pack_bf16(p.x, p.y);
-                    p = fma2(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), make_float2(-1.0f, -1.0f), p);
-                    part[0][j] = hi;
-                    part[1][j] = pack_bf16(p.x, p.y);
-                }
-                tmem_store8(tmem + lanes + Tile::s(b) + i * 8, part[0]);
-                tmem_store8(tmem + lanes + Tile::s(b) + 32 + i * 8, part[1]);
-            }
-            l += sum.x + sum.y;
+            if (!ok) break;
+            l += step_sum;
             tmem_store_wait();
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&p_full[b]));
+            if (lane == 0) {
+                mbar_arrive(smem_addr(&p_full[b]));
+                mbar_arrive(smem_addr(&scale_empty[scale_at.slot]));
+            }
+            for (int i = 0; i < kEvery; ++i) scale_at.next();
         }
         // the sums: of both groups, each taking half of the columns, or of this one's rows
         const int lanes_row = (warp & 3) * 32 + lane;
@@ -512,27 +679,41 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         const float most = fmaxf(mine.x, other.x), mine_f = exp2_fast(mine.x - most), other_f = exp2_fast(other.x - most);
         const float total = mine.y * mine_f + other.y * other_f, inverse = total == 0.0f ? 0.0f : 1.0f / total;
         if (count > 0 && ok) {
+            // 32 columns at a time, turned in shared memory (the codes', which have all been converted)
             constexpr int kColumns = TILES == 1 ? D / 2 : D;
             const int d0 = TILES == 1 ? stream * kColumns : 0;
+            const uint32_t stage = raw + warp * 4096;
+            const unsigned all_valid = __ballot_sync(kFullWarp, row < rows);
 #pragma unroll 1
-            for (int d = d0; d < d0 + kColumns; d += 16) {
-                uint32_t v[16], w[16];
-                if (turns > 0) tmem_load16(tmem + lanes + Tile::o(stream) + d, v);
-                if (other_turns > 0) tmem_load16(tmem + lanes + Tile::o(1 - stream) + d, w);
-                tmem_load_wait();
-                if (row < rows) {
-                    float4 *to = reinterpret_cast<float4 *>(a.parts.o + part * D + d);
+            for (int d = d0; d < d0 + kColumns; d += 32) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float y[4];
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t v[16] = {}, w[16] = {};
+                    if (turns > 0) tmem_load16(tmem + lanes + Tile::o(stream) + d + h * 16, v);
+                    if (other_turns > 0) tmem_load16(tmem + lanes + Tile::o(1 - stream) + d + h * 16, w);
+                    tmem_load_wait(v);
+                    tmem_load_wait(w);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            y[k] = turns > 0 ? __uint_as_float(v[j * 4 + k]) * (mine_f * inverse) * mine.z : 0.0f;
-                            if (other_turns > 0) y[k] += __uint_as_float(w[j * 4 + k]) * (other_f * inverse) * other.z;
-                            if (nan_from[d + j * 4 + k] <= limit) y[k] = __uint_as_float(0x7fc00000u);
-                        }
-                        to[j] = make_float4(y[0], y[1], y[2], y[3]);
+                    for (int j = 0; j < 16; ++j) {
+                        float y = turns > 0 ? __uint_as_float(v[j]) * (mine_f * inverse) * mine.z : 0.0f;
+                        if (other_turns > 0) y += __uint_as_float(w[j]) * (other_f * inverse) * other.z;
+                        v[j] = __float_as_uint(y);
                     }
+                    if (any_nan != 0)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (nan_from[d + h * 16 + j] <= limit) v[j] = 0x7fc00000u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        store_shared16(stage + lane * 128 + (((h * 4 + j) ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int r = k * 4 + (lane >> 3);
+                    const int64_t to = __shfl_sync(kFullWarp, part, r) * D + d + (lane & 7) * 4;
+                    const uint4 y = load_shared16(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                    if ((all_valid >> r) & 1u) *reinterpret_cast<uint4 *>(a.parts.o + to) = y;
                 }
                 __syncwarp();
             }
@@ -541,7 +722,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         tcgen05_fence_before();
     }
     __syncthreads();
-    if (warp == kSoftmaxWarps + 4) {
+    if (warp == kProducts) {
         tcgen05_fence_after();
         tmem_free(tmem, kTmemColumns);
     }
@@ -609,6 +790,7 @@ sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void 
     a.splits = plan.splits;
     a.block_shift = c.block_tokens == 16 ? 4 : c.block_tokens == 32 ? 5 : 6;
     a.scale_log2 = s.scale * kLog2e;
+    a.q_pieces = aligned16(s.Q) && s.q.seq % 8 == 0 && s.q.token % 8 == 0 && s.q.head % 8 == 0;
     CUtensorMap k_map = {}, v_map = {};
     const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
     cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, c.block_tokens);
