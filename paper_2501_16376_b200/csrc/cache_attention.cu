@@ -158,52 +158,54 @@ __device__ __forceinline__ int row_limit(const AttnArgs &a, int64_t seq, int row
 
 // What a block keeps in shared memory beside the ring, for the two functions that work on it.  (Single
 // variables: as members of one object they cost the loop registers, and the long decoding case 2 %.)
-template <int D, int NT>
+// (SECOND: whether queries may have second parts.)
+template <int D, int NT, int WARPS, bool SECOND>
 struct AttnShared {
-    float (&m)[kAttnWarps][NT * 8], (&l)[kAttnWarps][NT * 8];  // of the warps
+    float (&m)[WARPS][NT * 8], (&l)[WARPS][NT * 8];  // of the warps
     float2 (&block_ml)[NT * 8], (&row_norm)[NT * 8];
     uint64_t (&full)[kRing], (&empty)[kRing];
-    float2 (&scales)[kRing][kAttnWarps];                       // of K and V
-    uint32_t (&present)[kRing][kAttnWarps];                    // whether the table names a block there
+    float2 (&scales)[kRing][WARPS];                       // of K and V
+    uint32_t (&present)[kRing][WARPS];                    // whether the table names a block there
     uint32_t &failed, &queries_rest;
     int (&nan_from)[D];                                        // first token among the call's own whose value is NaN, by column
-    uint2 (&query_rest)[NT][D / 16][32];                       // the queries' second parts, as the operand registers lie
+    uint2 (&query_rest)[SECOND ? NT : 1][SECOND ? D / 16 : 1][SECOND ? 32 : 1];  // the queries' second parts, as the operand registers lie
 };
-template <int D, int NT>
-__device__ __forceinline__ AttnShared<D, NT> attention_shared() {
-    __shared__ float m[kAttnWarps][NT * 8], l[kAttnWarps][NT * 8];
+template <int D, int NT, int WARPS, bool SECOND>
+__device__ __forceinline__ AttnShared<D, NT, WARPS, SECOND> attention_shared() {
+    __shared__ float m[WARPS][NT * 8], l[WARPS][NT * 8];
     __shared__ float2 block_ml[NT * 8], row_norm[NT * 8];
     __shared__ uint64_t full[kRing], empty[kRing];
-    __shared__ float2 scales[kRing][kAttnWarps];
-    __shared__ uint32_t present[kRing][kAttnWarps];
+    __shared__ float2 scales[kRing][WARPS];
+    __shared__ uint32_t present[kRing][WARPS];
     __shared__ uint32_t failed, queries_rest;
     __shared__ int nan_from[D];
-    __shared__ uint2 query_rest[NT][D / 16][32];
+    __shared__ uint2 query_rest[SECOND ? NT : 1][SECOND ? D / 16 : 1][SECOND ? 32 : 1];
     return {m, l, block_ml, row_norm, full, empty, scales, present, failed, queries_rest, nan_from, query_rest};
 }
 
-template <bool BF16, int D, int NT, bool TWICE>
+template <bool BF16, int D, int NT, bool TWICE, bool SHARED>
 __device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
-                                                  int next_block);
+                                                  int next_block, int from);
 
 // NT: tiles of 8 rows.  TWICE (at most 4 rows): the rows stand twice in their tile, and the second
 // time take their weights' second parts, so that one product serves both parts.  REST: the queries
 // have second parts as well; a block that finds so once it has started goes on in a function of its
 // own, so that the ordinary loop keeps the registers (inlined, that cost it 2 %).  SHARED: the first
-// tokens of a sequence are its group's and another kernel's; keys become bf16 for bf16 queries, which
-// then need no second parts.
+// tokens of a sequence are its group's and another kernel's (`from` steps of 16 are left out); a block is
+// one warp, since such tails are many and short; queries that binary16 does not hold are taken as they
+// are instead, with keys in bf16.
 template <bool BF16, int D, int NT, bool TWICE, bool SHARED, bool REST>
 __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
-                                                int next_block) {
-    int from = 0;
+                                                int next_block, int from) {
     constexpr int KW = D / 16;  // words of keys a lane holds of one token, inner steps of the score product
     constexpr int VW = D / 32;  // words of values a lane holds of one token
     constexpr int MT = D / 16;  // 16-wide pieces of the head in the output product
     constexpr int kStep = 2 * 16 * D;  // bytes: 16 tokens' keys, 16 tokens' values
     extern __shared__ __align__(1024) uint8_t ring[];  // [kRing][warp][kStep]; afterwards the warps' sums
-    const AttnShared<D, NT> sh = attention_shared<D, NT>();
+    constexpr int WARPS = SHARED ? 1 : kAttnWarps;
+    const AttnShared<D, NT, WARPS, !SHARED> sh = attention_shared<D, NT, WARPS, !SHARED>();
     float(*sh_o)[NT * 8][D] = reinterpret_cast<float(*)[NT * 8][D]>(ring);
-    float(*block_o)[D] = sh_o[kAttnWarps];             // the block's sum of them
+    float(*block_o)[D] = sh_o[WARPS];             // the block's sum of them
     auto &sh_m = sh.m, &sh_l = sh.l;
     auto &block_ml = sh.block_ml, &row_norm = sh.row_norm;
     auto &full = sh.full, &empty = sh.empty;
@@ -219,15 +221,15 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
     const int H = c.n_kv_heads, shift = a.block_shift;
     if constexpr (!REST) {
         pdl_launch_dependents();
-        for (int d = threadIdx.x; d < D; d += kAttnWarps * 32) nan_from[d] = 0x7fffffff;
+        for (int d = threadIdx.x; d < D; d += WARPS * 32) nan_from[d] = 0x7fffffff;
         if (threadIdx.x == 0) {
             if (c.n_blocks > 0) {
                 tma_prefetch_map(&k_map);
                 tma_prefetch_map(&v_map);
             }
             for (int i = 0; i < kRing; ++i) {
-                mbar_init(smem_addr(&full[i]), 2 * kAttnWarps);  // a step's copies: the two of TMA, and the scales
-                mbar_init(smem_addr(&empty[i]), kAttnWarps);
+                mbar_init(smem_addr(&full[i]), 2 * WARPS);  // a step's copies: the two of TMA, and the scales
+                mbar_init(smem_addr(&empty[i]), WARPS);
             }
             failed = queries_rest = 0u;
             mbar_fence_init();
@@ -251,21 +253,21 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
     // blocks are looked up a turn before they are wanted.
     const int32_t *table = c.table + seq * c.ld_table;
     const uint32_t n_blocks = static_cast<uint32_t>(c.n_blocks), ring_at = smem_addr(ring);
-    const int stages = (last - first + kAttnWarps - 1) / kAttnWarps;
+    const int stages = (last - first + WARPS - 1) / WARPS;
     const uint64_t policy = l2_evict_first();  // leaves the L2 to the scores, which the joining kernel reads
     auto block_of = [&](int stage) {
-        const int step = first + stage * kAttnWarps + lane;
-        return lane < kAttnWarps && step < last ? table[step >> (shift - 4)] : -1;
+        const int step = first + stage * WARPS + lane;
+        return lane < WARPS && step < last ? table[step >> (shift - 4)] : -1;
     };
     auto fill = [&](int stage, int slot, int block) {
-        if (lane < kAttnWarps) {
-            const int step = first + stage * kAttnWarps + lane;
+        if (lane < WARPS) {
+            const int step = first + stage * WARPS + lane;
             const uint32_t bar = smem_addr(&full[slot]);
             const bool here = uint32_t(block) < n_blocks;
             present[slot][lane] = here;
             if (here) {
                 const int tile = block * H + head;
-                const uint32_t to = ring_at + (slot * kAttnWarps + lane) * kStep;
+                const uint32_t to = ring_at + (slot * WARPS + lane) * kStep;
                 const int row = (tile << shift) + ((step << 4) & ((1 << shift) - 1));
                 mbar_expect_tx(bar, kStep);
                 tma_load_2d(to, &k_map, 0, row, bar, policy);
@@ -281,12 +283,18 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         __syncwarp();
     };
     // next_block: of the stage this warp fills next
-    static_assert(kRing - 1 <= kAttnWarps, "the first stages are filled by different warps");
-    if constexpr (!REST) {
+    static_assert(kRing - 1 <= WARPS || WARPS == 1, "the first stages are filled by different warps, or by one");
+    if constexpr (!REST && WARPS == 1) {
+        for (int stage = 0; stage < kRing - 1; ++stage) {
+            next_block = block_of(stage);
+            if (stage < stages) fill(stage, stage, next_block);
+        }
+        next_block = block_of(kRing - 1);
+    } else if constexpr (!REST) {
         next_block = block_of(warp);
         if (warp < kRing - 1) {
             if (warp < stages) fill(warp, warp, next_block);
-            next_block = block_of(warp + kAttnWarps);
+            next_block = block_of(warp + WARPS);
         }
     }
     RingPlace<kRing> place;
@@ -310,7 +318,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                 raw[s][0] = at[0] | (uint32_t(at[1]) << 16);
                 raw[s][1] = at[2] | (uint32_t(at[3]) << 16);
             }
-            if constexpr (BF16 && SHARED) {
+            if constexpr (BF16 && SHARED && REST) {
                 // keys become bf16: a row is taken as it is, 2^64 times smaller where sums of its
                 // products with codes might leave binary32's range
                 uint32_t top = 0;
@@ -376,11 +384,11 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
 #pragma unroll
             for (int s = 0; s < KW; ++s) qf[n][s][0] = qf[n][s][1] = 0u;
         }
-        if constexpr (REST) {
+        if constexpr (REST && !SHARED) {
             if (warp == 0)
 #pragma unroll
                 for (int s = 0; s < KW; ++s) query_rest[n][s][lane] = make_uint2(rest[s][0], rest[s][1]);
-        } else if (any_rest != 0u) {
+        } else if (!REST && any_rest != 0u) {
             queries_rest = 1u;
         }
         // the scores' columns are rows 2t and 2t + 1
@@ -397,9 +405,9 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             for (int i = 0; i < 4; ++i) o[n][k][i] = 0.0f;
     }
     __syncthreads();
-    if constexpr (BF16 && !REST && !SHARED) {
+    if constexpr (BF16 && !REST) {
         if (queries_rest != 0u) {
-            attention_block_rest<BF16, D, NT, TWICE>(k_map, v_map, a, next_block);
+            attention_block_rest<BF16, D, NT, TWICE, SHARED>(k_map, v_map, a, next_block, from);
             return;
         }
     }
@@ -407,16 +415,16 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
     // of token g, row 2t of this tile; 8-byte aligned where rows is even
     float *const scores = a.scores + ((seq * H + head) * a.max_len + g) * a.rows + row0 + 2 * t;
     for (int stage = 0; stage < stages; ++stage, place.next()) {
-        const int step = first + stage * kAttnWarps + warp, j0 = step * 16, slot = place.slot;
+        const int step = first + stage * WARPS + warp, j0 = step * 16, slot = place.slot;
         const int ahead = stage + kRing - 1;
         bool ok = true;
-        if ((ahead & (kAttnWarps - 1)) == warp && ahead < stages) {
+        if ((ahead & (WARPS - 1)) == warp && ahead < stages) {
             // the slot was last used by the stage before this one
             const int free_slot = slot == 0 ? kRing - 1 : slot - 1;
             if (ahead >= kRing) ok = mbar_wait_or_fail(smem_addr(&empty[free_slot]), slot == 0 ? place.parity ^ 1u : place.parity, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             fill(ahead, free_slot, next_block);
-            next_block = block_of(ahead + kAttnWarps);
+            next_block = block_of(ahead + WARPS);
         }
         ok = mbar_wait_or_fail(smem_addr(&full[slot]), place.parity, &failed);
         if (!__all_sync(kFullWarp, ok)) break;
@@ -440,7 +448,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         uint32_t kw[2][KW], vw[4][VW];
         {
             // 16-byte chunk x of row r lies at x ^ (r & 7) (128-byte rows) or x ^ (r / 2 & 3)
-            const uint32_t k_at = ring_at + (slot * kAttnWarps + warp) * kStep, v_at = k_at + kStep / 2;
+            const uint32_t k_at = ring_at + (slot * WARPS + warp) * kStep, v_at = k_at + kStep / 2;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = g + 8 * i, swap = D == 128 ? r & 7 : (r >> 1) & 3;
@@ -461,7 +469,8 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         float s[NT][4];
         {
             float s2[NT][2][4];
-            if constexpr (REST) {
+            constexpr bool kSecond = REST && !SHARED, kKeys16 = BF16 && SHARED && REST;
+            if constexpr (kSecond) {
 #pragma unroll
                 for (int k = 0; k < KW; ++k) {
                     uint32_t f[4];
@@ -484,14 +493,14 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                 uint32_t f[4];
                 e4m3_to_f16(kw[0][k], f[0], f[2]);
                 e4m3_to_f16(kw[1][k], f[1], f[3]);
-                if constexpr (BF16 && SHARED) {
+                if constexpr (kKeys16) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) f[i] = f16_to_bf16(f[i]);
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    if (k < 2 && !(REST && k == 0)) mma_16_first<BF16 && SHARED>(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
-                    else mma_16<BF16 && SHARED>(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
+                    if (k < 2 && !(kSecond && k == 0)) mma_16_first<kKeys16>(s2[n][k], f, qf[n][k][0], qf[n][k][1]);
+                    else mma_16<kKeys16>(s2[n][k & 1], f, qf[n][k][0], qf[n][k][1]);
                 }
             }
 #pragma unroll
@@ -643,15 +652,15 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             }
         }
     __syncthreads();
-    for (int at = threadIdx.x; at < NT * 8 * D; at += kAttnWarps * 32) {
+    for (int at = threadIdx.x; at < NT * 8 * D; at += WARPS * 32) {
         const int r = at / D, d = at % D, row = row0 + r;
         if (row >= a.rows) break;
         float top = sh_m[0][r];
 #pragma unroll
-        for (int w = 1; w < kAttnWarps; ++w) top = fmaxf(top, sh_m[w][r]);
+        for (int w = 1; w < WARPS; ++w) top = fmaxf(top, sh_m[w][r]);
         float sum = 0.0f, out = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kAttnWarps; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
             const float f = exp2_fast(sh_m[w][r] - top);
             sum = fmaf(f, sh_l[w][r], sum);
             out = fmaf(f, TWICE ? sh_o[w][r][d] + sh_o[w][r + 4][d] : sh_o[w][r][d], out);
@@ -677,7 +686,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
     if (ranks > 1) cluster_sync();
     else __syncthreads();
     const int share = NT * 8 * D / ranks;
-    for (int at = rank * share + threadIdx.x; at < (rank + 1) * share; at += kAttnWarps * 32) {
+    for (int at = rank * share + threadIdx.x; at < (rank + 1) * share; at += WARPS * 32) {
         const int r = at / D, d = at % D, row = row0 + r;
         if (row >= a.rows) break;
         float top = kLowest, sum = 0.0f, out = 0.0f;
@@ -712,7 +721,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         const int64_t pair = seq * H + head;
         const int own = static_cast<int>(max(int64_t(-1), min(a.lens[seq] - a.n_q, a.max_len)));
         const int end = min(last * 16, len);
-        for (int j = first * 16 + threadIdx.x; j < end; j += kAttnWarps * 32) {
+        for (int j = first * 16 + threadIdx.x; j < end; j += WARPS * 32) {
             const float *x = a.scores + (pair * a.max_len + j) * a.rows;
             float sum = a.acc_in != nullptr && j < own ? a.acc_in[pair * a.ld_acc + j] : 0.0f, add = 0.0f;
             if ((a.rows & 3) == 0) {
@@ -726,23 +735,23 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             }
             a.acc_out[pair * a.ld_acc + j] = sum + add;
         }
-        for (int64_t j = len + rank * (kAttnWarps * 32) + threadIdx.x; j < a.max_len; j += ranks * kAttnWarps * 32)
+        for (int64_t j = len + rank * (WARPS * 32) + threadIdx.x; j < a.max_len; j += ranks * WARPS * 32)
             a.acc_out[pair * a.ld_acc + j] = 0.0f;
     }
     if (ranks > 1) cluster_sync();  // no block leaves while its sums are read
 }
 
-template <bool BF16, int D, int NT, bool TWICE>
+template <bool BF16, int D, int NT, bool TWICE, bool SHARED>
 __device__ __noinline__ void attention_block_rest(const CUtensorMap &k_map, const CUtensorMap &v_map, const AttnArgs &a,
-                                                  int next_block) {
-    attention_block<BF16, D, NT, TWICE, false, true>(k_map, v_map, a, next_block);
+                                                  int next_block, int from) {
+    attention_block<BF16, D, NT, TWICE, SHARED, true>(k_map, v_map, a, next_block, from);
 }
 
 template <bool BF16, int D, int NT, bool TWICE, bool SHARED>
-__global__ void __launch_bounds__(kAttnWarps * 32, NT == 1 ? 4 : 2)
+__global__ void __launch_bounds__(SHARED ? 32 : kAttnWarps * 32, SHARED ? (NT == 1 ? 16 : 8) : NT == 1 ? 4 : 2)
 cache_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                        const __grid_constant__ AttnArgs a) {
-    attention_block<BF16, D, NT, TWICE, SHARED, false>(k_map, v_map, a, 0);
+    attention_block<BF16, D, NT, TWICE, SHARED, false>(k_map, v_map, a, 0, 0);
 }
 
 // Joins the splits; turns the scores into accumulated weights.  Block x of a (sequence, kv head)
@@ -991,9 +1000,11 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
 
 // ------------------------------------------------------------------ beside a shared prefix
 
-// How many blocks share the tail of a (sequence, kv head, row tile): `tail` estimates its tokens.
+// How many blocks, of a warp each, share the tail of a (sequence, kv head, row tile): `tail` estimates
+// its tokens.  16 fit on an SM; none has less than 64 tokens.
 int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail) {
-    return attention_plan(c, rows, tail, true).splits;
+    const int64_t units = std::max(int64_t(1), c.n_seqs * c.n_kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16));
+    return static_cast<int>(std::max(int64_t(1), std::min({(tail + 63) / 64, int64_t(256), 148 * 16 / units})));
 }
 
 // A block joins a (sequence, kv head): a warp a row, four columns a lane at a time.
@@ -1005,28 +1016,39 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t seq = blockIdx.z, pair = seq * H + head;
     pdl_launch_dependents();
+    // what groups there are was known before the tails began
+    const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // else there are no parts of the prefix
     pdl_wait();
-    const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // the prefix's parts do not exist
     for (int row = blockIdx.x * (kSharedJoinThreads / 32) + warp; row < a.rows; row += gridDim.x * (kSharedJoinThreads / 32)) {
         const int64_t p0 = pair * parts.splits * a.rows + row;
-        float top = kLowest;
-        for (int s = skip + lane; s < parts.splits; s += 32) top = fmaxf(top, parts.ml[p0 + int64_t(s) * a.rows].x);
+        const float *o = parts.o + p0 * D + lane * 4;
+        float top = kLowest, sum = 0.0f, out[4] = {};
+        for (int s0 = skip; s0 < parts.splits; s0 += 32) {  // a lane a part
+            const int n = min(32, parts.splits - s0);
+            const float2 v = lane < n ? parts.ml[p0 + int64_t(s0 + lane) * a.rows] : make_float2(kLowest, 0.0f);
+            float most = fmaxf(v.x, top);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullWarp, top, o));
-        float sum = 0.0f, out[4] = {};
-#pragma unroll 4
-        for (int s = skip; s < parts.splits; ++s) {
-            const int64_t p = p0 + int64_t(s) * a.rows;
-            const float2 v = parts.ml[p];
-            const float f = exp2_fast(v.x - top), total = f * v.y;
-            sum += total;
-            if (total == 0.0f || lane * 4 >= D) continue;  // a part that saw nothing has no output
-            const float4 x = *reinterpret_cast<const float4 *>(parts.o + p * D + lane * 4);
-            const float by = s < parts.prefix_splits ? total : f;
-            out[0] = fmaf(by, x.x, out[0]);
-            out[1] = fmaf(by, x.y, out[1]);
-            out[2] = fmaf(by, x.z, out[2]);
-            out[3] = fmaf(by, x.w, out[3]);
+            for (int w = 16; w > 0; w >>= 1) most = fmaxf(most, __shfl_xor_sync(kFullWarp, most, w));
+            const float old = exp2_fast(top - most), f = exp2_fast(v.x - most);
+            float total = f * v.y;
+            // the prefix's parts have been divided by their sums; one that saw nothing has no output
+            const float by = total == 0.0f ? 0.0f : s0 + lane < parts.prefix_splits ? total : f;
+#pragma unroll
+            for (int w = 16; w > 0; w >>= 1) total += __shfl_xor_sync(kFullWarp, total, w);
+            sum = sum * old + total;
+            top = most;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) out[d] *= old;
+#pragma unroll 8
+            for (int s = 0; s < n; ++s) {
+                const float g = __shfl_sync(kFullWarp, by, s);
+                float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (g != 0.0f && lane * 4 < D) x = *reinterpret_cast<const float4 *>(o + int64_t(s0 + s) * a.rows * D);
+                out[0] = fmaf(g, x.x, out[0]);
+                out[1] = fmaf(g, x.y, out[1]);
+                out[2] = fmaf(g, x.z, out[2]);
+                out[3] = fmaf(g, x.w, out[3]);
+            }
         }
         const int i = row / a.group, hq = head * a.group + row % a.group;
         if (lane * 4 < D) {
@@ -1065,13 +1087,13 @@ sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const 
     a.part_o = parts.o;
     a.part_ml = parts.ml;
     a.groups = SharedGroups{s.group_start, s.prefix, s.n_groups, s.max_prefix, s.max_group};
-    PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(kAttnWarps * 32), stream);
+    PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(32), stream);
     CUtensorMap k_map = {}, v_map = {};
     const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
     cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
     if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, 16);
     if (e != cudaSuccess) return cuda_fail(e);
-    pdl.cfg.dynamicSmemBytes = kAttnWarps * kRing * c.head_dim * 32;
+    pdl.cfg.dynamicSmemBytes = kRing * c.head_dim * 32;
     const bool bf16 = s.dtype == SP_BF16;
 #define SP_LAUNCH(B, DD, N, TWICE)                                                       \
     do {                                                                                 \

@@ -30,7 +30,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kRaise = 16384.0f;   // weights of 16 tokens whose sum reaches this raise the maximum
 constexpr int kScaleSlots = 8;       // steps of scales
-constexpr float kFarMaximum = 1073741824.0f;  // 2^30: scores are whole multiples of 64 from here on
+constexpr float kFarMaximum = 16777216.0f;  // 2^24: the maximum's own rounding is off by 1 from here on
 constexpr int kFarScale = -40;       // of a value scale below the reference
 constexpr int kRaiseScale = 40;      // how far a value scale may exceed its reference
 constexpr int kStep = 64;            // tokens
@@ -583,7 +583,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                             if (token0 + i * 32 + j > limit || !((info.x >> (2 * i + (j >> 4))) & 1)) now[j] = 0xff800000u;
                     }
                 };
-                for (;;) {
+                for (int attempt = 0;; ++attempt) {
                     // the value scale goes into the exponent, and out of the sum again; step by step for all
                     // 32, since a warp waits for each of its instructions' operands in turn
                     float2 p[16];
@@ -623,7 +623,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                         for (int j = 0; j < 16; ++j) p[j] = mul2(p[j], make_float2(pow2(e[j >> 3]), pow2(e[j >> 3])));
                     }
                     split16(p, part);
-                    if (!__any_sync(kFullWarp, sum > kRaise)) break;
+                    if (attempt == 1 || !__any_sync(kFullWarp, sum > kRaise)) break;  // once raised, a weight is at most 2
                     // the maximum rises: the sums before, and this step's weights before, follow
                     uint32_t v[32];
                     load_scores(v);
@@ -728,8 +728,9 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     }
 }
 
-// A block for every SM: as many stretches of a prefix as that gives, each of four steps at least.
-// (The device's 148 SMs: the workspace is asked for without a device.)
+// A block for every SM, as many stretches of a prefix as that gives; the tails' blocks, 15 to an SM, run
+// beside them on SMs of their own where they are few.  (The device's 148 SMs: the workspace is asked for
+// without a device.)
 struct PrefixPlan {
     int tiles, row_tiles, splits, tail_splits;
 };
@@ -741,8 +742,10 @@ static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     if (s.n_groups == 0 || all == 0 || blocks == 0) return p;
     p.tiles = all <= 128 ? 1 : 2;
     p.row_tiles = static_cast<int>((all + 128 * p.tiles - 1) / (128 * p.tiles));
-    const int64_t units = s.n_groups * c.n_kv_heads * p.row_tiles, most = std::max(int64_t(1), tokens / (4 * kStep));
-    p.splits = static_cast<int>(std::max(int64_t(1), std::min(most, 148 / units)));
+    const int64_t units = s.n_groups * c.n_kv_heads * p.row_tiles, steps = (tokens + kStep - 1) / kStep;
+    const int64_t tails = (c.n_seqs * c.n_kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16) * p.tail_splits + 14) / 15;
+    const int64_t sms = tails <= 48 ? 148 - tails : 148;
+    p.splits = static_cast<int>(std::max(int64_t(1), std::min((steps + 1) / 2, sms / units)));
     return p;
 }
 
