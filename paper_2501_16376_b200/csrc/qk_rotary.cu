@@ -36,6 +36,11 @@ struct RotaryArgs {
     bool pairs;
 };
 
+// Where a token's heads begin.
+struct Offsets {
+    int64_t q, k, q_out, k_out;
+};
+
 // cos and sin of place * freq.
 __device__ __forceinline__ float2 turn(int64_t place, float freq) {
     double t = static_cast<double>(place) * static_cast<double>(freq) * 0.15915494309189535;  // turns
@@ -70,96 +75,135 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 
 // Heads of D values whose pieces are 16-byte aligned; PAIRS, or halves with rotary a multiple of 16.
 template <bool BF16, int D, bool PAIRS>
-__global__ void __launch_bounds__(kRotaryThreads)
+__global__ void __launch_bounds__(kRotaryThreads, 4)
 qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     constexpr int kLanes = D / 16, kRows = kRotaryThreads / kLanes;
-    __shared__ float2 angle[kMostTokens][D / 2];
+    __shared__ __align__(16) float cosine[kMostTokens][D / 2], sine[kMostTokens][D / 2];
+    __shared__ __align__(16) uint16_t weight[2][D];
+    __shared__ Offsets offset[kMostTokens];
     pdl_launch_dependents();
     pdl_wait();
     const int64_t token0 = int64_t(blockIdx.x) * a.tokens;
     const int tokens = static_cast<int>(min(int64_t(a.tokens), a.total - token0));
     const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
     const int head0 = blockIdx.y * a.head_share, heads = min(a.head_share, a.heads + a.kv_heads - head0);
-    const int items = tokens * heads;
-    // where the lane's two pieces of 8 lie in a head
+    // Where the lane's two pieces of 8 lie in a head: neighbouring lanes' pieces are neighbours (with both
+    // pieces of a lane side by side, 32768 tokens of 40 heads took 150 us).
     const int half = a.rotary / 2, units = PAIRS ? 0 : half / 8;
     const bool halves = !PAIRS && lane < units;
-    const int at0 = halves ? lane * 8 : lane * 16, at1 = halves ? at0 + half : at0 + 8;
-    uint4 x0, x1;
-    auto load = [&](int item) {
-        const int t = item / heads, h = head0 + item % heads;
-        const int64_t token = token0 + t, seq = token / a.n_tokens, i = token % a.n_tokens;
-        const uint16_t *p = h < a.heads ? a.Q + seq * a.q.seq + i * a.q.token + h * a.q.head
-                                        : a.K + seq * a.k.seq + i * a.k.token + (h - a.heads) * a.k.head;
-        x0 = *reinterpret_cast<const uint4 *>(p + at0);
-        x1 = *reinterpret_cast<const uint4 *>(p + at1);
+    const int at0 = PAIRS || halves ? lane * 8 : a.rotary + (lane - units) * 8;
+    const int at1 = PAIRS ? D / 2 + at0 : halves ? at0 + half : at0 + (kLanes - units) * 8;
+    // (all tokens together are fewer than 2^31)
+    auto place = [&](int t, uint32_t &seq) {
+        const uint32_t token = static_cast<uint32_t>(token0) + t, n = static_cast<uint32_t>(a.n_tokens);
+        seq = token / n;
+        return token - seq * n;
     };
-    if (row < items) load(row);
-    for (int at = threadIdx.x; at < tokens * (D / 2); at += kRotaryThreads) {
-        const int t = at / (D / 2), k = at % (D / 2);
-        const int64_t token = token0 + t, seq = token / a.n_tokens;
-        if (k < half) angle[t][k] = turn(a.start[seq] + token % a.n_tokens, a.freq[k]);
+    // a head of a token at a time; the first one's values are on their way before anything else
+    int t = 0, h = row;
+    auto settle = [&] {
+        while (h >= heads) {
+            h -= heads;
+            ++t;
+        }
+    };
+    uint4 x0, x1;
+    auto load = [&](int64_t q_at, int64_t k_at) {
+        const int at = head0 + h;
+        const uint16_t *p = at < a.heads ? a.Q + q_at + at * a.q.head : a.K + k_at + (at - a.heads) * a.k.head;
+        x0 = __ldcs(reinterpret_cast<const uint4 *>(p + at0));
+        x1 = __ldcs(reinterpret_cast<const uint4 *>(p + at1));
+    };
+    settle();
+    if (t < tokens) {
+        uint32_t seq;
+        const int64_t i = place(t, seq);
+        load(seq * a.q.seq + i * a.q.token, seq * a.k.seq + i * a.k.token);
+    }
+    for (int n = threadIdx.x; n < tokens; n += kRotaryThreads) {
+        uint32_t seq;
+        const int64_t i = place(n, seq);
+        offset[n] = Offsets{seq * a.q.seq + i * a.q.token, seq * a.k.seq + i * a.k.token,
+                            seq * a.q_out.seq + i * a.q_out.token, seq * a.k_out.seq + i * a.k_out.token};
+    }
+    for (int at = threadIdx.x; at < tokens * half; at += kRotaryThreads) {
+        uint32_t seq;
+        const int64_t i = place(at / half, seq);
+        const float2 cs = turn(a.start[seq] + i, a.freq[at % half]);
+        cosine[at / half][at % half] = cs.x;
+        sine[at / half][at % half] = cs.y;
+    }
+    for (int d = threadIdx.x; d < D; d += kRotaryThreads) {
+        if (a.q_weight != nullptr) weight[0][d] = a.q_weight[d];
+        if (a.k_weight != nullptr) weight[1][d] = a.k_weight[d];
     }
     __syncthreads();
-    for (int item = row; item < items; item += kRows) {
-        const int t = item / heads, h = head0 + item % heads;
+    while (t < tokens) {
+        const int at = head0 + h;
+        const bool is_q = at < a.heads;
         const uint32_t p0[4] = {x0.x, x0.y, x0.z, x0.w}, p1[4] = {x1.x, x1.y, x1.z, x1.w};
-        if (item + kRows < items) load(item + kRows);
-        float u[8], v[8];
-        unpack8<BF16>(p0, u);
-        unpack8<BF16>(p1, v);
-        const uint16_t *w = h < a.heads ? a.q_weight : a.k_weight;
-        if (w != nullptr) {
-            float sum = 0.0f;
+        uint16_t *out = is_q ? a.Q_out + offset[t].q_out + at * a.q_out.head : a.K_out + offset[t].k_out + (at - a.heads) * a.k_out.head;
+        const float *cos = cosine[t], *sin = sine[t];
+        h += kRows;
+        settle();
+        if (t < tokens) load(offset[t].q, offset[t].k);
+        float2 u[4], v[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(u[i], u[i], fmaf(v[i], v[i], sum));
-            const unsigned mask = kLanes == 32 ? kFullWarp : ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
+        for (int i = 0; i < 4; ++i) {
+            u[i] = unpack2<BF16>(p0[i]);
+            v[i] = unpack2<BF16>(p1[i]);
+        }
+        if ((is_q ? a.q_weight : a.k_weight) != nullptr) {
+            float2 sums = mul2(u[0], u[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) sums = fma2(u[i], u[i], sums);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums = fma2(v[i], v[i], sums);
+            float sum = sums.x + sums.y;
+            const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
             const float f = rsqrtf(sum * (1.0f / D) + a.eps);
-            const uint4 w0 = *reinterpret_cast<const uint4 *>(w + at0), w1 = *reinterpret_cast<const uint4 *>(w + at1);
+            const uint4 w0 = *reinterpret_cast<const uint4 *>(&weight[is_q ? 0 : 1][at0]), w1 = *reinterpret_cast<const uint4 *>(&weight[is_q ? 0 : 1][at1]);
             const uint32_t q0[4] = {w0.x, w0.y, w0.z, w0.w}, q1[4] = {w1.x, w1.y, w1.z, w1.w};
-            float g0[8], g1[8];
-            unpack8<BF16>(q0, g0);
-            unpack8<BF16>(q1, g1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[i] *= f * g0[i];
-                v[i] *= f * g1[i];
+            for (int i = 0; i < 4; ++i) {
+                u[i] = mul2(u[i], mul2(unpack2<BF16>(q0[i]), make_float2(f, f)));
+                v[i] = mul2(v[i], mul2(unpack2<BF16>(q1[i]), make_float2(f, f)));
             }
         }
         // what is not turned stays as it is: a product with 0 would let an infinity through
-        const float4 *cs = reinterpret_cast<const float4 *>(&angle[t][lane * 8]);
-        auto rotate = [](float &a, float &b, float cos, float sin) {
-            const float y = a * cos - b * sin;
-            b = b * cos + a * sin;
+        auto rotate2 = [](float2 &a, float2 &b, float2 c, float2 s) {  // two pairs
+            const float2 y = fma2(a, c, mul2(b, make_float2(-s.x, -s.y)));
+            b = fma2(b, c, mul2(a, s));
             a = y;
         };
-        if (PAIRS ? lane * 8 < half : lane < units) {
+        if constexpr (PAIRS) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float4 c = cs[i];  // of pairs 2i and 2i + 1
-                if constexpr (PAIRS) {
-                    float *s = i < 2 ? u + 4 * i : v + 4 * (i - 2);
-                    if (lane * 8 + 2 * i < half) rotate(s[0], s[1], c.x, c.y);
-                    if (lane * 8 + 2 * i + 1 < half) rotate(s[2], s[3], c.z, c.w);
-                } else {
-                    rotate(u[2 * i], v[2 * i], c.x, c.y);
-                    rotate(u[2 * i + 1], v[2 * i + 1], c.z, c.w);
+                float2 *s = i < 2 ? u + 2 * i : v + 2 * (i - 2);
+                const int pair = (i < 2 ? 0 : D / 4) + lane * 4 + (i & 1) * 2;
+                if (pair < half) {
+                    const float2 c = *reinterpret_cast<const float2 *>(cos + pair), sn = *reinterpret_cast<const float2 *>(sin + pair);
+                    float2 first = make_float2(s[0].x, s[1].x), second = make_float2(s[0].y, s[1].y);
+                    rotate2(first, second, c, sn);
+                    s[0] = make_float2(first.x, second.x);
+                    if (pair + 1 < half) s[1] = make_float2(first.y, second.y);
                 }
             }
+        } else if (lane < units) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                rotate2(u[i], v[i], *reinterpret_cast<const float2 *>(cos + lane * 8 + 2 * i), *reinterpret_cast<const float2 *>(sin + lane * 8 + 2 * i));
         }
         uint32_t y0[4], y1[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            y0[i] = pack2<BF16>(u[2 * i], u[2 * i + 1]);
-            y1[i] = pack2<BF16>(v[2 * i], v[2 * i + 1]);
+            y0[i] = pack2<BF16>(u[i].x, u[i].y);
+            y1[i] = pack2<BF16>(v[i].x, v[i].y);
         }
-        const int64_t token = token0 + t, seq = token / a.n_tokens, i = token % a.n_tokens;
-        uint16_t *out = h < a.heads ? a.Q_out + seq * a.q_out.seq + i * a.q_out.token + h * a.q_out.head
-                                    : a.K_out + seq * a.k_out.seq + i * a.k_out.token + (h - a.heads) * a.k_out.head;
-        *reinterpret_cast<uint4 *>(out + at0) = make_uint4(y0[0], y0[1], y0[2], y0[3]);
-        *reinterpret_cast<uint4 *>(out + at1) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
+        __stcs(reinterpret_cast<uint4 *>(out + at0), make_uint4(y0[0], y0[1], y0[2], y0[3]));
+        __stcs(reinterpret_cast<uint4 *>(out + at1), make_uint4(y1[0], y1[1], y1[2], y1[3]));
     }
 }
 
