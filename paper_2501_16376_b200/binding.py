@@ -733,9 +733,10 @@ def _heads(t: torch.Tensor, what: str, n_seqs: int, head_dim: int, device: int) 
 def _int32(t, what, shape, device: int):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise SpError(SP_ERR_INVALID_ARG, "%s must be contiguous int32 %s" % (what, list(shape)))
-    _on_device(t, what, device)
+    if t.get_device() != device:
+        _on_device(t, what, device)
     return t.data_ptr()
 
 
@@ -1017,42 +1018,60 @@ class KvCache:
         return O
 
 
+@functools.lru_cache(maxsize=4096)
+def _rotary_layout(q, qs, k, ks, qo, qos, ko, kos):
+    """What a call's shapes and strides come to, checked once: sizes and the four sp_strides."""
+    for shape, stride, what in ((q, qs, "Q"), (k, ks, "K"), (qo, qos, "Q_out"), (ko, kos, "K_out")):
+        if len(shape) != 4 or shape[0] != q[0] or shape[3] != q[3] or stride[3] != 1:
+            raise SpError(SP_ERR_SHAPE, "%s must be [n_seqs, tokens, heads, head size] with consecutive "
+                                        "values, of the sequences and the head size of Q" % what)
+    if q[1] != k[1]:
+        raise SpError(SP_ERR_SHAPE, "Q and K must have the same tokens")
+    if qo != q or ko != k:
+        raise SpError(SP_ERR_SHAPE, "Q_out and K_out must have the shapes of Q and K")
+    return q[0], q[1], q[2], k[2], q[3], _strides(*qs[:3]), _strides(*ks[:3]), _strides(*qos[:3]), _strides(*kos[:3])
+
+
 def sp_qk_norm_rotary(Q, K, start, freq, q_weight=None, k_weight=None, eps: float = 1e-6,
                       pairs: bool = False, Q_out=None, K_out=None, stream=None):
     """Norms the heads of Q and K [n_seqs, tokens, heads, head size] (where a weight [head size] is
     given) and turns their first 2 * len(freq) values by (start[b] + i) * freq: neighbours together
     if pairs, else the two halves.  Q_out and K_out may be Q and K.  Returns (Q_out, K_out)."""
     device = _current_device()
-    n_seqs, dim = Q.shape[0], Q.shape[-1]
-    qs, ks = _heads(Q, "Q", n_seqs, dim, device), _heads(K, "K", n_seqs, dim, device)
-    if Q.shape[1] != K.shape[1]:
-        raise SpError(SP_ERR_SHAPE, "Q and K must have the same tokens")
     if Q_out is None:
         Q_out = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
     if K_out is None:
         K_out = _result(stream, torch.empty, K.shape, dtype=K.dtype, device=K.device)
-    qo, ko = _heads(Q_out, "Q_out", n_seqs, dim, device), _heads(K_out, "K_out", n_seqs, dim, device)
-    if Q_out.shape != Q.shape or K_out.shape != K.shape:
-        raise SpError(SP_ERR_SHAPE, "Q_out and K_out must have the shapes of Q and K")
-    if not Q.dtype == K.dtype == Q_out.dtype == K_out.dtype:
+    q_strides, k_strides = Q.stride(), K.stride()
+    qo_strides, ko_strides = Q_out.stride(), K_out.stride()
+    n_seqs, tokens, heads, kv_heads, dim, qs, ks, qo, ko = _rotary_layout(
+        Q.shape, q_strides, K.shape, k_strides, Q_out.shape, qo_strides, K_out.shape, ko_strides)
+    dtype = Q.dtype
+    if not (K.dtype is dtype and Q_out.dtype is dtype and K_out.dtype is dtype):
         raise SpError(SP_ERR_DTYPE, "Q, K and their outputs must have the same dtype")
-    for x, out, same in ((Q, Q_out, qs is qo), (K, K_out, ks is ko)):
-        if out.data_ptr() == x.data_ptr() and x.numel() and not same and out.stride() != x.stride():
-            raise SpError(SP_ERR_INVALID_ARG, "an output in its input's place has its strides")
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            if w.dtype != Q.dtype or w.shape != (dim,) or not w.is_contiguous():
-                raise SpError(SP_ERR_SHAPE, "%s must be contiguous [%d] of the type of Q" % (what, dim))
-            _on_device(w, what, device)
-    if freq.dtype != torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
+    if not device == Q.get_device() == K.get_device() == Q_out.get_device() == K_out.get_device() == freq.get_device():
+        raise SpError(SP_ERR_INVALID_ARG, "Q, K, their outputs and freq must be CUDA tensors of the current device")
+    qp, kp, qop, kop = Q.data_ptr(), K.data_ptr(), Q_out.data_ptr(), K_out.data_ptr()
+    if (qp == qop and q_strides != qo_strides and qp) or (kp == kop and k_strides != ko_strides and kp):
+        raise SpError(SP_ERR_INVALID_ARG, "an output in its input's place has its strides")
+    wq = wk = None
+    if q_weight is not None:
+        wq = _head_weight(q_weight, "q_weight", dtype, dim, device)
+    if k_weight is not None:
+        wk = _head_weight(k_weight, "k_weight", dtype, dim, device)
+    if freq.dtype is not torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
         raise SpError(SP_ERR_INVALID_ARG, "freq must be contiguous float32 [rotary / 2]")
-    _on_device(freq, "freq", device)
-    _check(lib.sp_qk_norm_rotary(Q.data_ptr(), qs, Q.shape[2], K.data_ptr(), ks, K.shape[2], _dtype_of(Q),
-                                 n_seqs, Q.shape[1], dim, _ptr(q_weight), _ptr(k_weight), eps,
-                                 _int32(start, "start", (n_seqs,), device), freq.data_ptr(),
-                                 2 * freq.shape[0], 1 if pairs else 0, Q_out.data_ptr(), qo,
-                                 K_out.data_ptr(), ko, _raw_stream(stream, device)))
+    _check(lib.sp_qk_norm_rotary(qp, qs, heads, kp, ks, kv_heads, _dtype_of(Q), n_seqs, tokens, dim, wq, wk,
+                                 eps, _int32(start, "start", (n_seqs,), device), freq.data_ptr(),
+                                 2 * freq.shape[0], 1 if pairs else 0, qop, qo, kop, ko,
+                                 _raw_stream(stream, device)))
     return Q_out, K_out
+
+
+def _head_weight(w, what, dtype, dim, device) -> int:
+    if w.dtype is not dtype or w.shape != (dim,) or not w.is_contiguous() or w.get_device() != device:
+        raise SpError(SP_ERR_SHAPE, "%s must be contiguous [%d] of the type and device of Q" % (what, dim))
+    return w.data_ptr()
 
 
 def sp_wait_status(clear: bool = False) -> int:

@@ -66,6 +66,7 @@ struct AttnArgs {
     int64_t ld_acc;
     SharedGroups groups;  // SHARED: the tokens that a sequence's group shares are left out
     int all_splits, first_split;  // SHARED: parts of a (sequence, kv head), and the first of this kernel's
+    bool q_pieces;                // SHARED: whether queries lie on 8-byte boundaries
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -312,11 +313,20 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             const uint16_t *q = a.Q + seq * a.q.seq + (row / a.group) * a.q.token +
                                 (head * a.group + row % a.group) * a.q.head + t * (D / 4);
             uint32_t raw[KW][2];
+            if (SHARED && a.q_pieces) {
 #pragma unroll
-            for (int s = 0; s < KW; ++s) {
-                const uint16_t *at = q + s * 4;  // as the lane's words of K lie
-                raw[s][0] = at[0] | (uint32_t(at[1]) << 16);
-                raw[s][1] = at[2] | (uint32_t(at[3]) << 16);
+                for (int s = 0; s < KW; ++s) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(q + s * 4);
+                    raw[s][0] = w.x;
+                    raw[s][1] = w.y;
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < KW; ++s) {
+                    const uint16_t *at = q + s * 4;  // as the lane's words of K lie
+                    raw[s][0] = at[0] | (uint32_t(at[1]) << 16);
+                    raw[s][1] = at[2] | (uint32_t(at[3]) << 16);
+                }
             }
             if constexpr (BF16 && SHARED && REST) {
                 // keys become bf16: a row is taken as it is, 2^64 times smaller where sums of its
@@ -632,6 +642,36 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             for (int i = 0; i < 2 * kRing; ++i) mbar_wait(smem_addr(&full[i % kRing]), i / kRing);
         __syncthreads();
     }
+    if constexpr (SHARED) {
+        // one warp: its sums are the block's, and go out as the lanes hold them
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = row0 + n * 8 + 2 * t + i;
+                float sum = l[n][i];
+                sum += __shfl_xor_sync(kFullWarp, sum, 4);
+                sum += __shfl_xor_sync(kFullWarp, sum, 8);
+                sum += __shfl_xor_sync(kFullWarp, sum, 16);
+                const bool here = row < a.rows && (!TWICE || t < 2);
+                const int64_t p = ((seq * H + head) * a.all_splits + a.first_split + blockIdx.x) * a.rows + row;
+                const int see = here ? row_limit(a, seq, row, len) : -1;
+#pragma unroll
+                for (int k = 0; k < MT; k += 2) {
+                    float y[4] = {o[n][k][i], o[n][k][i + 2], o[n][k + 1][i], o[n][k + 1][i + 2]};
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        if constexpr (TWICE) y[d] += __shfl_xor_sync(kFullWarp, y[d], 2);
+                        if (own_from < len && nan_from[g * (D / 8) + 2 * k + d] <= see) y[d] = __uint_as_float(0x7fc00000u);
+                    }
+                    if (here) *reinterpret_cast<float4 *>(a.part_o + p * D + g * (D / 8) + 2 * k) = make_float4(y[0], y[1], y[2], y[3]);
+                }
+                if (here && g == 0) a.part_ml[p] = make_float2(m[n][i], sum);
+            }
+        // this kernel does not end before the one over the prefixes: one block waits for all
+        if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) pdl_wait();
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -667,8 +707,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         }
         if (nan_from[d] <= row_limit(a, seq, row, len)) out = __uint_as_float(0x7fc00000u);
         if (a.part_o != nullptr) {
-            const int64_t split = SHARED ? (seq * H + head) * a.all_splits + a.first_split + blockIdx.x : (seq * H + head) * a.splits + blockIdx.x;
-            const int64_t p = split * a.rows + row;
+            const int64_t p = ((seq * H + head) * a.splits + blockIdx.x) * a.rows + row;
             a.part_o[p * D + d] = out;
             if (d == 0) a.part_ml[p] = make_float2(top, sum);
         } else {
@@ -676,10 +715,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             if (d == 0) block_ml[r] = make_float2(top, sum);
         }
     }
-    // this kernel does not end before the one over the prefixes: one block waits for all
-    if constexpr (SHARED)
-        if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) pdl_wait();
-    if (SHARED || a.part_o != nullptr) return;
+    if (a.part_o != nullptr) return;
 
     // the cluster's blocks share the output's elements
     const int ranks = a.splits, rank = blockIdx.x;
@@ -1084,6 +1120,7 @@ sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const 
     a.scale_log2 = s.scale * kLog2e;
     a.O = static_cast<uint16_t *>(s.O);
     a.lse = s.lse;
+    a.q_pieces = (reinterpret_cast<uintptr_t>(s.Q) & 7u) == 0 && s.q.seq % 4 == 0 && s.q.token % 4 == 0 && s.q.head % 4 == 0;
     a.part_o = parts.o;
     a.part_ml = parts.ml;
     a.groups = SharedGroups{s.group_start, s.prefix, s.n_groups, s.max_prefix, s.max_group};
