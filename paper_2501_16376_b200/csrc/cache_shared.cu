@@ -579,9 +579,9 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                             // scores so large that a product differs from the maximum, itself rounded, by
                             // powers of two; value scales that would take the weights out of the sum
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                p[j] = add2(mul2(make_float2(__uint_as_float(now[2 * j]), __uint_as_float(now[2 * j + 1])), make_float2(k[j >> 3], k[j >> 3])),
-                                            make_float2(-m, -m));
+                            for (int j = 0; j < 16; ++j)  // (of pairs, a product and a sum would be made one)
+                                p[j] = make_float2(__fadd_rn(__fmul_rn(__uint_as_float(now[2 * j]), k[j >> 3]), -m),
+                                                   __fadd_rn(__fmul_rn(__uint_as_float(now[2 * j + 1]), k[j >> 3]), -m));
                         }
                     }
 #pragma unroll
@@ -605,7 +605,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                     // the maximum rises: the sums before, and this step's weights before, follow
                     uint32_t v[32];
                     load_scores(v);
-                    const float most = fmaxf(m, fmaxf(max16(v) * k[0], max16(v + 16) * k[1])), f = exp2_fast(m - most);
+                    const float most = fmaxf(m, fmaxf(__fmul_rn(max16(v), k[0]), __fmul_rn(max16(v + 16), k[1]))), f = exp2_fast(m - most);
                     m = most;
                     far_maximum = __any_sync(kFullWarp, fabsf(m) > kFarMaximum && m != kLowest);
                     l *= f;

@@ -246,3 +246,45 @@ def test_captured_replays_and_streams(sp):
 
 def test_waits_have_not_run_out(sp):
     assert sp.sp_wait_status() == 0
+
+
+@pytest.mark.parametrize("log2", [10, 23, 25, 27, 29, 31, 40, 60])
+def test_one_token_far_above_the_others(sp, log2):
+    """Scores of 2^log2 at one or two tokens and 0, or small ones, at the others: the output is their
+    values' mean whatever the maximum's own rounding comes to."""
+    for dtype in DTYPES:
+        cache = _cache(sp, 3, 14, 1, 64, 16, seed=20, spread=0)
+        row = cache.table[0].long()
+        one = torch.tensor(1.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        cache.k[:] = 0
+        cache.k_scale[:] = 1.0
+        cache.k[row[3], 0, 5, 0] = cache.k[row[9], 0, 1, 0] = one
+        cache.k[row[4], 0, 2, 0] = one | 0x80                              # as far below
+        cache.k[:, :, :, 1] = one                                          # a term that all have
+        Q = torch.zeros(3, 1, 4, 64)
+        Q[..., 0], Q[..., 1] = 1.5, 0.25
+        O = cache.sp_cache_attention_shared(Q.to(dtype).cuda(), _i32([224, 200, 193]), 224, _i32([0, 3]), _i32([192]), 192, 3,
+                                            scale=2.0 ** log2).double().cpu()
+        v = cache.v.view(torch.float8_e4m3fn).double() * cache.v_scale.double()[..., None, None]
+        want = ((v[row[3], 0, 5] + v[row[9], 0, 1]) / 2).cpu()
+        assert ((O - want).abs() <= torch.finfo(dtype).eps / 2 * want.abs() + 2.0 ** -17 * v.abs().max().cpu()).all()
+        far = cache.sp_cache_attention_shared(-Q.to(dtype).cuda(), _i32([224, 200, 193]), 224, _i32([0, 3]), _i32([192]), 192, 3,
+                                              scale=-2.0 ** log2).double().cpu()
+        assert torch.equal(far, O)                                         # a negative scale
+
+
+def test_scores_that_rise_by_a_little_and_by_much(sp):
+    """The maximum is raised within a step and between steps, by less and by more than a weight may exceed it."""
+    for dtype in DTYPES:
+        for rise in (0.05, 0.3, 1.0, 4.0):
+            cache = _cache(sp, 2, 20, 1, 64, 16, seed=21, spread=0)
+            cache.k[:] = 0
+            cache.k_scale[:] = 2.0 ** -4
+            place = torch.arange(320).view(20, 16)
+            row = cache.table[0].long().cpu()
+            codes = (place.float() * rise).clamp(max=448).to(torch.float8_e4m3fn).view(torch.uint8)
+            for i in range(20):
+                cache.k[row[i], 0, :, 3] = codes[i].cuda()
+            Q = torch.zeros(2, 1, 3, 64)
+            Q[..., 3] = 8.0
+            _check(sp, cache, Q.to(dtype), [320, 311], 320, [0, 2], [304], scale=1.0)
