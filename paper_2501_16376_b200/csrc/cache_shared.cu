@@ -35,7 +35,7 @@ constexpr int kFarScale = -40;       // of a value scale below the reference
 constexpr int kRaiseScale = 40;      // how far a value scale may exceed its reference
 constexpr int kStep = 64;            // tokens
 constexpr int kTmemColumns = 512;
-constexpr int kConverted = 3;        // steps of converted keys, and of values
+constexpr int kConverted = 3;        // steps of converted keys, and of values; of scores too, with 128 rows
 
 template <int D, int TILES>
 struct PrefixTile {
@@ -65,6 +65,7 @@ struct PrefixArgs {
     int64_t n_q, max_len;
     int group, rows;        // heads of a kv head; rows of a sequence (n_q * group)
     int row_tiles, splits;  // blocks along the rows, along the prefix
+    int copies;             // of the rows in a tile, each with a share of a step's tokens
     int block_shift;
     float scale_log2;
     bool q_pieces;          // whether queries lie on 16-byte boundaries
@@ -123,7 +124,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     constexpr int kSlots = Tile::kSlots, kBuffers = Tile::kBuffers, kSoftmaxWarps = Tile::kSoftmaxWarps;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t raw_full[kSlots], raw_empty[kSlots], k_full[kConverted], k_empty[kConverted], v_full[kConverted], v_empty[kConverted];
-    __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], pv_done[2], drained;
+    __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], drained;
     __shared__ uint32_t tmem_base, failed, present[kSlots];
     __shared__ float4 group_sums[2][128];  // TILES == 1: maximum, sum, 2^reference of a group's rows
     __shared__ uint64_t q_full, scale_full[kScaleSlots], scale_empty[kScaleSlots];
@@ -152,8 +153,6 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             mbar_init(smem_addr(&s_full[b]), 1);
             mbar_init(smem_addr(&p_full[b]), 4);
         }
-        mbar_init(smem_addr(&pv_done[0]), 1);
-        mbar_init(smem_addr(&pv_done[1]), 1);
         mbar_init(smem_addr(&drained), 1);
         mbar_init(smem_addr(&q_full), kSoftmaxWarps);
         for (int i = 0; i < kScaleSlots; ++i) {
@@ -269,50 +268,86 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         if (failed != 0u && lane == 0)
             for (int s = max(0, issued - kSlots); s < issued; ++s) mbar_wait(smem_addr(&raw_full[s % kSlots]), (s / kSlots) & 1);
     } else if (warp == kProducts) {
-        // ---- products
-        const bool begun = __all_sync(kFullWarp, mbar_wait_or_fail(smem_addr(&q_full), 0, &failed));
-        tcgen05_fence_after();
-        if (begun && elect_one()) {
-            const uint32_t qk = f16_instruction(kStep, BF16), pv = f16_instruction(D, true) | kColumnsB;
-            // Whichever product has its operands goes next; products run in the order of their issue.  A
-            // step's scores go where the weights of three steps before (of the step before) were.
-            constexpr int kAhead = TILES == 1 ? 3 : 1;
-            int scored[TILES] = {}, weighed[TILES] = {};
-            auto ready = [&](uint64_t *bar, int use) { return mbar_test(smem_addr(bar), use & 1); };
-            for (uint32_t idle = 0; weighed[0] < count || weighed[TILES - 1] < count;) {
-                bool issued = false;
+        // ---- products.  The warp walks the loop together and elects a thread for the instructions alone:
+        // operands then stay in uniform registers.  They run in the order of their issue: a step's scores
+        // go where the weights of three steps before (with 256 rows: of the step before) were, right behind
+        // the product that reads those.
+        const uint32_t qk = f16_instruction(kStep, BF16), pv = f16_instruction(D, true) | kColumnsB;
+        const uint32_t base = __shfl_sync(kFullWarp, tmem, 0);
+        const int steps_here = __shfl_sync(kFullWarp, count, 0);
+        auto all = [&](bool ok) {
+            ok = __all_sync(kFullWarp, ok);
+            tcgen05_fence_after();
+            return ok;
+        };
+        auto scores = [&](int t, int step) {  // of one thread
+            const int s_at = TILES == 1 ? step % 3 : t;
+            const uint64_t keys = desc_rows128(conv + step % kConverted * Tile::kConvBytes);
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    const int v = weighed[t], v_at = v % kConverted, p_at = TILES == 1 ? v % 3 : t;
-                    if (v < scored[t] && ready(&p_full[p_at], TILES == 1 ? v / 3 : v) && ready(&v_full[v_at], v / kConverted)) {
-                        tcgen05_fence_after();
-                        const int g = TILES == 1 ? v & 1 : t;
-                        const uint64_t values = desc_columns128(conv + (kConverted + v_at) * Tile::kConvBytes, Tile::kHalfBytes);
+            for (int p = 0; p < D / 16; ++p)
+                mma_16bit(base + Tile::s(s_at), base + Tile::q(t) + p * 8, keys + (p >> 2) * (Tile::kHalfBytes / 16) + (p & 3) * 2, qk, p > 0);
+            tcgen05_commit(smem_addr(&s_full[s_at]));
+            if (t == 1) tcgen05_commit(smem_addr(&k_empty[step % kConverted]));
+        };
+        auto values = [&](int t, int step) {
+            const int p_at = TILES == 1 ? step % 3 : t, g = TILES == 1 ? step & 1 : t;
+            const uint64_t v = desc_columns128(conv + (kConverted + step % kConverted) * Tile::kConvBytes, Tile::kHalfBytes);
 #pragma unroll
-                        for (int p = 0; p < 8; ++p)  // of 32 tokens both parts, 16 tokens each
-                            mma_16bit(tmem + Tile::o(g), tmem + Tile::s(p_at) + p * 8, values + ((p >> 2) * 2 + (p & 1)) * (16 * 128 / 16), pv,
-                                      v >= (TILES == 1 ? 2 : 1) || p > 0);
-                        tcgen05_commit(smem_addr(&pv_done[g]));
-                        ++weighed[t];
-                        if (TILES == 1 || weighed[1 - t] > v) tcgen05_commit(smem_addr(&v_empty[v_at]));
-                        issued = true;
-                    }
-                    const int k = scored[t], k_at = k % kConverted, s_at = TILES == 1 ? k % 3 : t;
-                    if (k < count && k - weighed[t] < kAhead && ready(&k_full[k_at], k / kConverted)) {
-                        tcgen05_fence_after();
-                        const uint64_t keys = desc_rows128(conv + k_at * Tile::kConvBytes);
-#pragma unroll
-                        for (int p = 0; p < D / 16; ++p)
-                            mma_16bit(tmem + Tile::s(s_at), tmem + Tile::q(t) + p * 8, keys + (p >> 2) * (Tile::kHalfBytes / 16) + (p & 3) * 2, qk, p > 0);
-                        tcgen05_commit(smem_addr(&s_full[s_at]));
-                        ++scored[t];
-                        if (TILES == 1 || scored[1 - t] > k) tcgen05_commit(smem_addr(&k_empty[k_at]));
-                        issued = true;
-                    }
+            for (int p = 0; p < 8; ++p)  // of 32 tokens both parts, 16 tokens each
+                mma_16bit(base + Tile::o(g), base + Tile::s(p_at) + p * 8, v + ((p >> 2) * 2 + (p & 1)) * (16 * 128 / 16), pv,
+                          step >= (TILES == 1 ? 2 : 1) || p > 0);
+            if (TILES == 1 || t == 1) tcgen05_commit(smem_addr(&v_empty[step % kConverted]));
+        };
+        bool ok = all(mbar_wait_or_fail(smem_addr(&q_full), 0, &failed));
+        if constexpr (TILES == 1) {
+            // Whichever product has its operands goes next (in a fixed order, 16 rows took 0.86 us a step
+            // for 0.77; the looks at the barriers overlap).
+            int scored = 0, weighed = 0;
+            for (uint32_t idle = 0; ok && weighed < steps_here;) {
+                const bool p_ready = mbar_test(smem_addr(&p_full[weighed % 3]), weighed / 3 & 1);
+                const bool v_ready = mbar_test(smem_addr(&v_full[weighed % 3]), weighed / 3 & 1);
+                const bool k_ready = mbar_test(smem_addr(&k_full[scored % 3]), scored / 3 & 1);
+                const bool weigh = __all_sync(kFullWarp, p_ready && v_ready) && weighed < scored;
+                const bool score = __all_sync(kFullWarp, k_ready) && scored < steps_here && scored - weighed - (weigh ? 1 : 0) < 3;
+                if (!weigh && !score) {
+                    if (++idle > kWaitLimit) mbar_give_up(&failed);
+                    ok = __all_sync(kFullWarp, *static_cast<volatile uint32_t *>(&failed) == 0u);
+                    continue;
                 }
-                idle = issued ? 0 : idle + 1;
-                if (idle > kWaitLimit) mbar_give_up(&failed);
-                if (idle != 0 && *static_cast<volatile uint32_t *>(&failed) != 0u) break;
+                idle = 0;
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    if (weigh) values(0, weighed);
+                    if (score) scores(0, scored);
+                }
+                __syncwarp();
+                weighed += weigh;
+                scored += score;
+            }
+        } else {
+            // two tiles in turn: a step's scores right behind the step before (as above, 12 % more)
+            if (ok && steps_here > 0 && (ok = all(mbar_wait_or_fail(smem_addr(&k_full[0]), 0, &failed)))) {
+                if (elect_one()) {
+                    scores(0, 0);
+                    scores(1, 0);
+                }
+                __syncwarp();
+            }
+            for (int step = 0; ok && step < steps_here; ++step) {
+                const int next = step + 1;
+                const uint32_t v_bar = smem_addr(&v_full[step % kConverted]), v_use = step / kConverted & 1;
+                const uint32_t k_bar = next < steps_here ? smem_addr(&k_full[next % kConverted]) : v_bar, k_use = next < steps_here ? next / kConverted & 1 : v_use;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (t == 0) ok = all(mbar_wait3_or_fail(v_bar, v_use, k_bar, k_use, smem_addr(&p_full[0]), step & 1, &failed));
+                    else ok = ok && all(mbar_wait_or_fail(smem_addr(&p_full[1]), step & 1, &failed));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        values(t, step);
+                        if (next < steps_here) scores(t, next);
+                    }
+                    __syncwarp();
+                }
             }
         }
         __syncwarp();
@@ -328,30 +363,32 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         // Eight lanes read and write all banks: of the chunks of a row's half and those of the row whose
         // number differs in bits 0 and 2 (D = 64: of a row and the next).
         int r[kEach], ch[kEach];
+        uint32_t in[kEach], out[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int x = i * 128 + thread;
             r[i] = D == 128 ? (x >> 4 << 1) ^ (x & 4 ? 5 : 0) : x >> 2;
             ch[i] = D == 128 ? (x >> 1 & 4) | (x & 3) : x & 3;
+            in[i] = r[i] * D + ((ch[i] ^ (D == 128 ? r[i] & 7 : (r[i] >> 1) & 3)) << 4);
+            out[i] = (ch[i] >> 2) * Tile::kHalfBytes + r[i] * 128 + ((((ch[i] & 3) * 2) ^ (r[i] & 7)) << 4);
         }
         RingPlace<kSlots> at;
         auto convert_steps = [&](auto is_key) {
             constexpr bool KEY = decltype(is_key)::value;
-            uint64_t *full = KEY ? k_full : v_full, *empty = KEY ? k_empty : v_empty;
+            // (the product with the keys in a buffer fills the scores of the same number)
+            uint64_t *full = KEY ? k_full : v_full, *empty = !KEY ? v_empty : TILES == 1 ? s_full : k_empty;
             // which tokens all rows see is known when the queries are there
             bool ok = KEY || mbar_wait_or_fail(smem_addr(&q_full), 0, &failed);
             int buffer = 0, uses = 0;
             for (int step = 0; step < count; ++step, at.next()) {
-                ok = ok && mbar_wait_or_fail(smem_addr(&raw_full[at.slot]), at.parity, &failed);
+                if (uses > 0) ok = ok && mbar_wait2_or_fail(smem_addr(&raw_full[at.slot]), at.parity, smem_addr(&empty[buffer]), (uses - 1) & 1, &failed);
+                else ok = ok && mbar_wait_or_fail(smem_addr(&raw_full[at.slot]), at.parity, &failed);
                 if (!__all_sync(kFullWarp, ok)) break;
                 const uint32_t from = raw + at.slot * Tile::kRawBytes + (KEY ? 0 : kStep * D), here = present[at.slot];
                 const uint32_t to = conv + (KEY ? buffer : kConverted + buffer) * Tile::kConvBytes;
                 uint4 w[kEach];
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int swap = D == 128 ? r[i] & 7 : (r[i] >> 1) & 3;
-                    w[i] = load_shared16(from + r[i] * D + ((ch[i] ^ swap) << 4));
-                }
+                for (int i = 0; i < kEach; ++i) w[i] = load_shared16(from + in[i]);
                 if constexpr (!KEY) {
                     const int token0 = (first + step) * kStep;
                     if (token0 + kStep > all_see) {
@@ -375,8 +412,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                             if (!((here >> (r[i] >> shift)) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
-                if (uses > 0) ok = mbar_wait_or_fail(smem_addr(&empty[buffer]), (uses - 1) & 1, &failed);
-                if (!__all_sync(kFullWarp, ok)) break;
+                __syncwarp();  // the codes are in registers
                 if (lane == 0) mbar_arrive(smem_addr(&raw_empty[at.slot]));
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
@@ -391,9 +427,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
 #pragma unroll
                         for (int k = 0; k < 8; ++k) h[k] = pack_bf16(f[k].x, f[k].y);
                     }
-                    const uint32_t row_at = to + (ch[i] >> 2) * Tile::kHalfBytes + r[i] * 128, c0 = (ch[i] & 3) * 2;
-                    store_shared16(row_at + ((c0 ^ (r[i] & 7)) << 4), h[0], h[1], h[2], h[3]);
-                    store_shared16(row_at + (((c0 + 1) ^ (r[i] & 7)) << 4), h[4], h[5], h[6], h[7]);
+                    store_shared16(to + out[i], h[0], h[1], h[2], h[3]);
+                    store_shared16(to + (out[i] ^ 16u), h[4], h[5], h[6], h[7]);
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -408,7 +443,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         else convert_steps(std::false_type{});
     } else if (warp < kSoftmaxWarps) {
         // ---- softmax: a thread a row, of the steps stream, stream + kEvery, ...
-        const int stream = warp >> 2, tile = TILES == 1 ? 0 : stream, row = row0 + tile * 128 + (warp & 3) * 32 + lane;
+        const int stream = warp >> 2, tile = TILES == 1 ? 0 : stream;
+        // Up to 64 rows stand twice in their tile, and each copy takes half of a step's tokens.
+        const int copy = TILES == 1 && a.copies == 2 ? (warp & 3) >> 1 : -1;
+        const int row = row0 + tile * 128 + (copy >= 0 ? warp & 1 : warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         int limit = 0x7ffffffe;            // the last token that the row sees
         float undo = fabsf(a.scale_log2);  // its sign goes to the queries: factors of scores are positive
@@ -471,9 +509,9 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                         for (int k = 0; k < 32; ++k) top = __vmaxu2(top, q[h][k] & 0x7fff7fffu);
                 top = max(top & 0xffffu, top >> 16);
                 if constexpr (TILES == 1) {
-                    row_top[stream][row - row0] = top;
+                    row_top[stream][(warp & 3) * 32 + lane] = top;
                     asm volatile("bar.sync 1, 256;" ::: "memory");
-                    top = max(top, row_top[1 - stream][row - row0]);
+                    top = max(top, row_top[1 - stream][(warp & 3) * 32 + lane]);
                 }
                 if (top > kLargeQuery >> 16) {
                     undo *= pow2(64);
@@ -512,7 +550,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         // sums of the steps before, by a row's own factor
         auto scale_sums = [&](int turn, float by) {
             if (turn == 0) return true;
-            const bool ok = mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turn - 1) & 1, &failed);
+            const int before = from + (turn - 1) * kEvery;  // no later product with values is issued without this step's weights
+            const bool ok = mbar_wait_or_fail(smem_addr(&v_empty[before % kConverted]), (before / kConverted) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) return false;
             tcgen05_fence_after();
 #pragma unroll 1
@@ -528,8 +567,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         };
         for (int turn = 0; turn < turns; ++turn) {
             const int step = from + turn * kEvery, b = TILES == 1 ? step % 3 : stream;
-            ok = ok && mbar_wait_or_fail(smem_addr(&scale_full[scale_at.slot]), scale_at.parity, &failed);
+            ok = ok && mbar_wait2_or_fail(smem_addr(&scale_full[scale_at.slot]), scale_at.parity, smem_addr(&s_full[b]),
+                                          (TILES == 1 ? step / 3 : step) & 1, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
+            tcgen05_fence_after();
             const int2 info = scale_info[scale_at.slot];
             const float *ks = reinterpret_cast<const float *>(&scale_k[scale_at.slot]);
             const int *vs = reinterpret_cast<const int *>(&scale_v[scale_at.slot]);
@@ -538,9 +579,6 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 if (!ok) break;
                 reference = info.y;
             }
-            ok = mbar_wait_or_fail(smem_addr(&s_full[b]), (TILES == 1 ? step / 3 : step) & 1, &failed);
-            if (!__all_sync(kFullWarp, ok)) break;
-            tcgen05_fence_after();
             // 32 tokens at a time; the weights lie where their scores were, first parts and second ones
             const uint32_t scores = tmem + lanes + Tile::s(b);
             const int token0 = (first + step) * kStep;
@@ -548,10 +586,16 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             float step_sum = 0.0f;
 #pragma unroll 1
             for (int i = 0; i < 2; ++i) {
+                uint32_t part[32];
+                if (copy == 1 - i) {  // the other copy's tokens
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[j] = 0u;
+                    tmem_store32(scores + i * 32, part);
+                    continue;
+                }
                 const float k[2] = {fminf(fmaxf(ks[2 * i] * undo, 1.2e-38f), 3.0e38f), fminf(fmaxf(ks[2 * i + 1] * undo, 1.2e-38f), 3.0e38f)};
                 const int e[2] = {vs[2 * i], vs[2 * i + 1]};
                 float sum;
-                uint32_t part[32];
                 auto load_scores = [&](uint32_t (&now)[32]) {
                     tmem_load32(scores + i * 32, now);
                     tmem_load_wait(now);
@@ -642,10 +686,9 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         // the sums: of both groups, each taking half of the columns, or of this one's rows
         const int lanes_row = (warp & 3) * 32 + lane;
         float4 mine = make_float4(m, l, pow2(max(reference, -126)), 0.0f), other = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
-        if (turns > 0) ok = ok && mbar_wait_or_fail(smem_addr(&pv_done[stream]), (turns - 1) & 1, &failed);
+        if (count > 0) ok = ok && mbar_wait_or_fail(smem_addr(&v_empty[(count - 1) % kConverted]), ((count - 1) / kConverted) & 1, &failed);
         const int other_turns = TILES == 1 ? (count - (1 - stream) + 1) / 2 : 0;
         if constexpr (TILES == 1) {
-            if (other_turns > 0) ok = ok && mbar_wait_or_fail(smem_addr(&pv_done[1 - stream]), (other_turns - 1) & 1, &failed);
             group_sums[stream][lanes_row] = mine;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             other = group_sums[1 - stream][lanes_row];
@@ -653,7 +696,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         ok = __all_sync(kFullWarp, ok);
         tcgen05_fence_after();
         const int64_t pair = (g.begin + row / a.rows) * c.n_kv_heads + head;
-        const int64_t part = (pair * a.parts.splits + blockIdx.x) * a.rows + row % a.rows;
+        const int64_t part = (pair * a.parts.splits + (copy >= 0 ? blockIdx.x * 2 + copy : blockIdx.x)) * a.rows + row % a.rows;
         const float most = fmaxf(mine.x, other.x), mine_f = exp2_fast(mine.x - most), other_f = exp2_fast(other.x - most);
         const float total = mine.y * mine_f + other.y * other_f, inverse = total == 0.0f ? 0.0f : 1.0f / total;
         if (count > 0 && ok) {
@@ -710,7 +753,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
 // beside them on SMs of their own where they are few.  (The device's 148 SMs: the workspace is asked for
 // without a device.)
 struct PrefixPlan {
-    int tiles, row_tiles, splits, tail_splits;
+    int tiles, row_tiles, splits, copies, tail_splits;
 };
 static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     PrefixPlan p = {};
@@ -719,6 +762,7 @@ static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     p.tail_splits = shared_tail_splits(c, rows, std::max(int64_t(1), s.max_len - tokens + c.block_tokens));
     if (s.n_groups == 0 || all == 0 || blocks == 0) return p;
     p.tiles = all <= 128 ? 1 : 2;
+    p.copies = all <= 64 ? 2 : 1;
     p.row_tiles = static_cast<int>((all + 128 * p.tiles - 1) / (128 * p.tiles));
     const int64_t units = s.n_groups * c.n_kv_heads * p.row_tiles, steps = (tokens + kStep - 1) / kStep;
     const int64_t tails = (c.n_seqs * c.n_kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16) * p.tail_splits + 14) / 15;
@@ -732,7 +776,7 @@ int64_t cache_shared_workspace(const sp_cache &c, const SharedAttention &s) {
     if (rows == 0 || pairs == 0) return 0;
     const PrefixPlan plan = prefix_plan(c, s);
     if (plan.splits == 0) return cache_attention_workspace(c, s.n_q, s.n_heads, s.max_len, false);
-    return pairs * (plan.splits + plan.tail_splits) * rows * (c.head_dim * 4 + 8);
+    return pairs * (plan.splits * plan.copies + plan.tail_splits) * rows * (c.head_dim * 4 + 8);
 }
 
 template <bool BF16, int D, int TILES>
@@ -758,8 +802,9 @@ sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void 
     a.groups = SharedGroups{s.group_start, s.prefix, s.n_groups, s.max_prefix, s.max_group};
     a.group = s.n_heads / c.n_kv_heads;
     a.rows = static_cast<int>(s.n_q * a.group);
-    a.parts.splits = plan.splits + plan.tail_splits;
-    a.parts.prefix_splits = plan.splits;
+    a.parts.prefix_splits = plan.splits * plan.copies;
+    a.parts.splits = a.parts.prefix_splits + plan.tail_splits;
+    a.copies = plan.copies;
     a.parts.o = static_cast<float *>(workspace);
     a.parts.ml = reinterpret_cast<float2 *>(a.parts.o + c.n_seqs * c.n_kv_heads * a.parts.splits * a.rows * c.head_dim);
     a.Q = static_cast<const uint16_t *>(s.Q);

@@ -74,6 +74,20 @@ __device__ __forceinline__ bool mbar_wait_or_fail(uint32_t bar, uint32_t parity,
     return false;
 }
 
+// Both phases: their first looks at the barriers overlap.
+__device__ __forceinline__ bool mbar_wait2_or_fail(uint32_t bar, uint32_t parity, uint32_t other, uint32_t other_parity,
+                                                   volatile uint32_t *failed) {
+    const bool one = mbar_test(bar, parity), two = mbar_test(other, other_parity);
+    return (one || mbar_wait_or_fail(bar, parity, failed)) && (two || mbar_wait_or_fail(other, other_parity, failed));
+}
+
+__device__ __forceinline__ bool mbar_wait3_or_fail(uint32_t a, uint32_t a_parity, uint32_t b, uint32_t b_parity, uint32_t c,
+                                                   uint32_t c_parity, volatile uint32_t *failed) {
+    const bool one = mbar_test(a, a_parity), two = mbar_test(b, b_parity), three = mbar_test(c, c_parity);
+    return (one || mbar_wait_or_fail(a, a_parity, failed)) && (two || mbar_wait_or_fail(b, b_parity, failed)) &&
+           (three || mbar_wait_or_fail(c, c_parity, failed));
+}
+
 // Asynchronous copies and the tensor cores are driven by one thread, but the warp walks the loop
 // together and elects it only for the instructions themselves: operands then stay in uniform
 // registers.  Driven from a branch on the lane index, a stage of products took 1400 cycles of one
