@@ -285,12 +285,17 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
     };
     // next_block: of the stage this warp fills next
     static_assert(kRing - 1 <= WARPS || WARPS == 1, "the first stages are filled by different warps, or by one");
-    if constexpr (!REST && WARPS == 1) {
-        for (int stage = 0; stage < kRing - 1; ++stage) {
-            next_block = block_of(stage);
-            if (stage < stages) fill(stage, stage, next_block);
-        }
-        next_block = block_of(kRing - 1);
+    // SHARED: the lanes hold the blocks of 32 stages, and those of the next 32 are on their way
+    [[maybe_unused]] int held = -1, held_next = -1;
+    [[maybe_unused]] auto blocks_from = [&](int stage) {
+        const int step = first + stage + lane;
+        return step < last ? table[step >> (shift - 4)] : -1;
+    };
+    if constexpr (SHARED) {
+        held = blocks_from(0);
+        held_next = blocks_from(32);
+        if constexpr (!REST)
+            for (int stage = 0; stage < min(stages, kRing - 1); ++stage) fill(stage, stage, __shfl_sync(kFullWarp, held, stage));
     } else if constexpr (!REST) {
         next_block = block_of(warp);
         if (warp < kRing - 1) {
@@ -431,10 +436,18 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         if ((ahead & (WARPS - 1)) == warp && ahead < stages) {
             // the slot was last used by the stage before this one
             const int free_slot = slot == 0 ? kRing - 1 : slot - 1;
-            if (ahead >= kRing) ok = mbar_wait_or_fail(smem_addr(&empty[free_slot]), slot == 0 ? place.parity ^ 1u : place.parity, &failed);
-            if (!__all_sync(kFullWarp, ok)) break;
-            fill(ahead, free_slot, next_block);
-            next_block = block_of(ahead + WARPS);
+            if constexpr (SHARED) {  // by this warp itself, which has used what it read
+                fill(ahead, free_slot, __shfl_sync(kFullWarp, held, ahead & 31));
+                if ((ahead & 31) == 31) {
+                    held = held_next;
+                    held_next = blocks_from(ahead + 33);
+                }
+            } else {
+                if (ahead >= kRing) ok = mbar_wait_or_fail(smem_addr(&empty[free_slot]), slot == 0 ? place.parity ^ 1u : place.parity, &failed);
+                if (!__all_sync(kFullWarp, ok)) break;
+                fill(ahead, free_slot, next_block);
+                next_block = block_of(ahead + WARPS);
+            }
         }
         ok = mbar_wait_or_fail(smem_addr(&full[slot]), place.parity, &failed);
         if (!__all_sync(kFullWarp, ok)) break;
@@ -450,7 +463,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                             a.scores[((seq * H + head) * a.max_len + j) * a.rows + row] = -INFINITY;
                     }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
+            if (!SHARED && lane == 0) mbar_arrive(smem_addr(&empty[slot]));
             continue;
         }
         const float k_scale = scales[slot][warp].x;
@@ -473,7 +486,7 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             }
         }
         __syncwarp();  // the step is in registers
-        if (lane == 0) mbar_arrive(smem_addr(&empty[slot]));
+        if (!SHARED && lane == 0) mbar_arrive(smem_addr(&empty[slot]));
 
         // scores
         float s[NT][4];
