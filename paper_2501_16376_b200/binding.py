@@ -730,6 +730,19 @@ def _heads(t: torch.Tensor, what: str, n_seqs: int, head_dim: int, device: int) 
     return _strides(s[0], s[1], s[2])
 
 
+@functools.lru_cache(maxsize=4096)
+def _query_layout(q, qs, o, os_, n_seqs: int, head_dim: int):
+    """Queries, heads and strides of a [n_seqs, n_q, heads, head size] tensor and an output like it,
+    checked once for their shapes and strides."""
+    for shape, stride, what in ((q, qs, "Q"), (o, os_, "O")):
+        if len(shape) != 4 or shape[0] != n_seqs or shape[3] != head_dim or stride[3] != 1:
+            raise SpError(SP_ERR_SHAPE, "%s must be [%d, tokens, heads, %d] with consecutive values"
+                          % (what, n_seqs, head_dim))
+    if o != q:
+        raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
+    return q[1], q[2], _strides(*qs[:3]), _strides(*os_[:3])
+
+
 def _int32(t, what, shape, device: int):
     if t is None:
         return None
@@ -989,16 +1002,15 @@ class KvCache:
         which are read once, through the group's first row of the table.  max_prefix and max_group
         bound the prefixes and the sequences of a group.  Returns O."""
         device = self._here()
-        qs = _heads(Q, "Q", self.n_seqs, self.head_dim, device)
         if O is None:
             O = _result(stream, torch.empty, Q.shape, dtype=Q.dtype, device=Q.device)
-        os_ = _heads(O, "O", self.n_seqs, self.head_dim, device)
-        if O.shape != Q.shape:
-            raise SpError(SP_ERR_SHAPE, "O must have the shape of Q")
-        if O.dtype != Q.dtype:
+        n_q, n_heads, qs, os_ = _query_layout(Q.shape, Q.stride(), O.shape, O.stride(), self.n_seqs, self.head_dim)
+        if O.dtype is not Q.dtype:
             raise SpError(SP_ERR_DTYPE, "Q and O must have the same dtype")
-        n_q, n_heads, optr = Q.shape[1], Q.shape[2], O.data_ptr()
-        if optr == Q.data_ptr() and optr:
+        if not device == Q.get_device() == O.get_device():
+            raise SpError(SP_ERR_INVALID_ARG, "Q and O must be CUDA tensors of the current device")
+        qptr, optr = Q.data_ptr(), O.data_ptr()
+        if optr == qptr and optr:
             raise SpError(SP_ERR_INVALID_ARG, "O is memory apart from Q")
         if lse is not None:
             if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != Q.shape[:3]:
@@ -1010,7 +1022,7 @@ class KvCache:
         need = self._need("sp_cache_attention_shared_workspace", n_q, n_heads, max_len, groups, max_prefix, max_group)
         wptr, wbytes, keep = _workspace(need, workspace, Q, device, stream)
         _check(lib.sp_cache_attention_shared(
-            self._c, Q.data_ptr(), qs, _dtype_of(Q), n_q, n_heads, _int32(lens, "lens", (self.n_seqs,), device),
+            self._c, qptr, qs, _dtype_of(Q), n_q, n_heads, _int32(lens, "lens", (self.n_seqs,), device),
             max_len, _int32(group_start, "group_start", (groups + 1,), device), groups,
             _int32(prefix, "prefix", (groups,), device), max_prefix, max_group,
             self.head_dim ** -0.5 if scale is None else scale, optr, os_, _ptr(lse), wptr, wbytes,

@@ -1113,7 +1113,8 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     }
 }
 
-sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, cudaStream_t stream) {
+sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, const CUtensorMap &k_map,
+                             const CUtensorMap &v_map, cudaStream_t stream) {
     AttnArgs a = {};
     a.cache = c;
     a.Q = static_cast<const uint16_t *>(s.Q);
@@ -1138,11 +1139,7 @@ sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const 
     a.part_ml = parts.ml;
     a.groups = SharedGroups{s.group_start, s.prefix, s.n_groups, s.max_prefix, s.max_group};
     PdlConfig pdl(dim3(a.splits, c.n_kv_heads * a.row_tiles, static_cast<unsigned>(c.n_seqs)), dim3(32), stream);
-    CUtensorMap k_map = {}, v_map = {};
-    const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
-    cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
-    if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, 16);
-    if (e != cudaSuccess) return cuda_fail(e);
+    cudaError_t e = cudaSuccess;
     pdl.cfg.dynamicSmemBytes = kRing * c.head_dim * 32;
     const bool bf16 = s.dtype == SP_BF16;
 #define SP_LAUNCH(B, DD, N, TWICE)                                                       \

@@ -2,6 +2,8 @@
 // scale that the block_tokens x head_dim codes of a (block, head) have in common.
 #pragma once
 
+#include <cuda.h>
+
 #include "sp_device.cuh"
 #include "sp_internal.h"
 
@@ -135,6 +137,7 @@ struct SharedParts {
 
 // cache_attention.cu: the tokens behind the prefixes, and the join.
 int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail);
-sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, cudaStream_t stream);
+sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const SharedParts &parts, const CUtensorMap &k_map,
+                             const CUtensorMap &v_map, cudaStream_t stream);
 
 }  // namespace sp

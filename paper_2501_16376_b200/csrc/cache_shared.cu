@@ -190,22 +190,20 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
 
     const uint32_t raw = smem_addr(smem), conv = raw + kSlots * Tile::kRawBytes;  // conv: keys, then values
 
-    // The lanes of a warp hold the blocks of several steps: a load of the table takes longer than a step.
-    const int blocks = kStep >> shift, held = 32 / blocks;  // of a step: 4, 2 or 1
-    auto blocks_from = [&](int step) {
-        const int mine = step + lane / blocks;
-        return mine < count ? block_at((first + mine) * kStep + (lane % blocks << shift)) : -1;
-    };
+    // The lanes of a warp hold the blocks of eight steps, one for every 16 tokens: a load of the table takes
+    // longer than a step.
+    constexpr int kHeld = 8;
+    auto blocks_from = [&](int step) { return step + (lane >> 2) < count ? block_at((first + step) * kStep + lane * 16) : -1; };
     if (warp == kScales) {
         // ---- scales: the values' over a power of two that follows the largest by at most 2^40
         auto scale_of = [&](const float *scales, int id) { return id >= 0 ? scales[int64_t(id) * c.n_kv_heads + head] : 0.0f; };
-        int id = blocks_from(0), next_id = blocks_from(held), after_id = blocks_from(2 * held), reference = -200;
+        int id = blocks_from(0), next_id = blocks_from(kHeld), after_id = blocks_from(2 * kHeld), reference = -200;
         float ks = scale_of(c.k_scale, id), vs = scale_of(c.v_scale, id);
         float next_ks = scale_of(c.k_scale, next_id), next_vs = scale_of(c.v_scale, next_id);
         RingPlace<kScaleSlots> at;
         bool ok = true;
         for (int step = 0; step < count; ++step, at.next()) {
-            const int turn = step % held;
+            const int turn = step % kHeld;
             if (step > 0 && turn == 0) {
                 id = next_id;
                 ks = next_ks;
@@ -213,10 +211,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 next_id = after_id;
                 next_ks = scale_of(c.k_scale, next_id);
                 next_vs = scale_of(c.v_scale, next_id);
-                after_id = blocks_from(step + 2 * held);
+                after_id = blocks_from(step + 2 * kHeld);
             }
             // lanes 0 .. 3 take a piece of 16 tokens
-            const int holder = turn * blocks + ((lane & 3) * 16 >> shift);
+            const int holder = turn * 4 + (lane & 3);
             const int piece_id = __shfl_sync(kFullWarp, id, holder);
             const float piece_k = __shfl_sync(kFullWarp, ks, holder), piece_v = __shfl_sync(kFullWarp, vs, holder);
             const unsigned here = __ballot_sync(kFullWarp, piece_id >= 0) & 0xfu;
@@ -235,30 +233,30 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             if (lane == 0) mbar_arrive(smem_addr(&scale_full[at.slot]));
         }
     } else if (warp == kCopies) {
-        // ---- copies: a lane a block of the cache
-        const uint32_t piece = static_cast<uint32_t>(D) << shift;
+        // ---- copies: a lane 16 tokens
+        constexpr uint32_t kPiece = 16 * D;
         RingPlace<kSlots> at;
         bool ok = true;
-        int ids = blocks_from(0), next_ids = blocks_from(held), issued = 0;
+        int ids = blocks_from(0), next_ids = blocks_from(kHeld), issued = 0;
         for (int step = 0; step < count; ++step, at.next()) {
-            const int turn = step % held;
+            const int turn = step % kHeld;
             if (step > 0 && turn == 0) {
                 ids = next_ids;
-                next_ids = blocks_from(step + held);
+                next_ids = blocks_from(step + kHeld);
             }
-            const int id = __shfl_sync(kFullWarp, ids, turn * blocks + lane % blocks);
-            const bool mine = lane < blocks && id >= 0;
+            const int id = __shfl_sync(kFullWarp, ids, turn * 4 + (lane & 3));
+            const bool mine = lane < 4 && id >= 0;
             if (step >= kSlots) ok = mbar_wait_or_fail(smem_addr(&raw_empty[at.slot]), at.parity ^ 1u, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             const unsigned here = __ballot_sync(kFullWarp, mine);
-            const uint32_t bar = smem_addr(&raw_full[at.slot]), to = raw + at.slot * Tile::kRawBytes + lane * piece;
+            const uint32_t bar = smem_addr(&raw_full[at.slot]), to = raw + at.slot * Tile::kRawBytes + lane * kPiece;
             if (lane == 0) {
                 present[at.slot] = here;
-                mbar_expect_tx(bar, 2 * piece * __popc(here));
+                mbar_expect_tx(bar, 2 * kPiece * __popc(here));
             }
             __syncwarp();
             if (mine) {
-                const int y = (id * c.n_kv_heads + head) << shift;
+                const int y = ((id * c.n_kv_heads + head) << shift) + (((first + step) * kStep + lane * 16) & ((1 << shift) - 1));
                 tma_load_2d(to, &k_map, 0, y, bar);
                 tma_load_2d(to + kStep * D, &v_map, 0, y, bar);
             }
@@ -395,7 +393,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                         // NaN that some rows do not see: 0 here, and noted for those who do
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) {
-                            if (!((here >> (r[i] >> shift)) & 1u)) continue;
+                            if (!((here >> (r[i] >> 4)) & 1u)) continue;
                             uint32_t *word = reinterpret_cast<uint32_t *>(&w[i]);
 #pragma unroll
                             for (int k = 0; k < 16; ++k)
@@ -406,10 +404,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                                 }
                         }
                     }
-                    if (here != (kStep >> shift == 4 ? 0xfu : kStep >> shift == 2 ? 3u : 1u)) {
+                    if (here != 0xfu) {
 #pragma unroll
                         for (int i = 0; i < kEach; ++i)
-                            if (!((here >> (r[i] >> shift)) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                            if (!((here >> (r[i] >> 4)) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
                 __syncwarp();  // the codes are in registers
@@ -819,8 +817,8 @@ sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void 
     a.q_pieces = aligned16(s.Q) && s.q.seq % 8 == 0 && s.q.token % 8 == 0 && s.q.head % 8 == 0;
     CUtensorMap k_map = {}, v_map = {};
     const int64_t pool_rows = c.n_blocks * c.n_kv_heads * c.block_tokens;
-    cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, c.block_tokens);
-    if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, c.block_tokens);
+    cudaError_t e = encode_byte_rows(&k_map, c.k, pool_rows, c.head_dim, 16);
+    if (e == cudaSuccess) e = encode_byte_rows(&v_map, c.v, pool_rows, c.head_dim, 16);
     if (e != cudaSuccess) return cuda_fail(e);
     const bool bf16 = s.dtype == SP_BF16, two = plan.tiles == 2;
 #define SP_LAUNCH(B, DD) \
@@ -832,7 +830,7 @@ sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void 
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     sp_status st = check_launch();
-    return st == SP_OK ? launch_cache_tails(c, s, a.parts, stream) : st;
+    return st == SP_OK ? launch_cache_tails(c, s, a.parts, k_map, v_map, stream) : st;
 }
 
 }  // namespace sp

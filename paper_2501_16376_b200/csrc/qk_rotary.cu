@@ -12,6 +12,7 @@
 // partners of one another (halves) or neighbours (pairs), so that no value changes lanes but in the
 // sum of squares.
 #include <algorithm>
+#include <type_traits>
 
 #include "sp_device.cuh"
 #include "sp_internal.h"
@@ -73,11 +74,13 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 
 }  // namespace
 
-// Heads of D values whose pieces are 16-byte aligned; PAIRS, or halves with rotary a multiple of 16.
-template <bool BF16, int D, bool PAIRS>
+// Heads of D values in pieces of P, aligned as such; PAIRS (8), or halves with rotary a multiple of 2 P.
+template <bool BF16, int D, bool PAIRS, int P>
 __global__ void __launch_bounds__(kRotaryThreads, 4)
 qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
-    constexpr int kLanes = D / 16, kRows = kRotaryThreads / kLanes;
+    static_assert(P == 8 || (P == 4 && !PAIRS), "pairs are turned in pieces of 8");
+    using Piece = typename std::conditional<P == 8, uint4, uint2>::type;
+    constexpr int kLanes = D / (2 * P), kRows = kRotaryThreads / kLanes, W = P / 2;
     __shared__ __align__(16) float cosine[kMostTokens][D / 2], sine[kMostTokens][D / 2];
     __shared__ __align__(16) uint16_t weight[2][D];
     __shared__ Offsets offset[kMostTokens];
@@ -87,12 +90,12 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     const int tokens = static_cast<int>(min(int64_t(a.tokens), a.total - token0));
     const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
     const int head0 = blockIdx.y * a.head_share, heads = min(a.head_share, a.heads + a.kv_heads - head0);
-    // Where the lane's two pieces of 8 lie in a head: neighbouring lanes' pieces are neighbours (with both
+    // Where the lane's two pieces lie in a head: neighbouring lanes' pieces are neighbours (with both
     // pieces of a lane side by side, 32768 tokens of 40 heads took 150 us).
-    const int half = a.rotary / 2, units = PAIRS ? 0 : half / 8;
+    const int half = a.rotary / 2, units = PAIRS ? 0 : half / P;
     const bool halves = !PAIRS && lane < units;
-    const int at0 = PAIRS || halves ? lane * 8 : a.rotary + (lane - units) * 8;
-    const int at1 = PAIRS ? D / 2 + at0 : halves ? at0 + half : at0 + (kLanes - units) * 8;
+    const int at0 = PAIRS || halves ? lane * P : a.rotary + (lane - units) * P;
+    const int at1 = PAIRS ? D / 2 + at0 : halves ? at0 + half : at0 + (kLanes - units) * P;
     // (all tokens together are fewer than 2^31)
     auto place = [&](int t, uint32_t &seq) {
         const uint32_t token = static_cast<uint32_t>(token0) + t, n = static_cast<uint32_t>(a.n_tokens);
@@ -107,12 +110,12 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
             ++t;
         }
     };
-    uint4 x0, x1;
+    Piece x0, x1;
     auto load = [&](int64_t q_at, int64_t k_at) {
         const int at = head0 + h;
         const uint16_t *p = at < a.heads ? a.Q + q_at + at * a.q.head : a.K + k_at + (at - a.heads) * a.k.head;
-        x0 = __ldcs(reinterpret_cast<const uint4 *>(p + at0));
-        x1 = __ldcs(reinterpret_cast<const uint4 *>(p + at1));
+        x0 = __ldcs(reinterpret_cast<const Piece *>(p + at0));
+        x1 = __ldcs(reinterpret_cast<const Piece *>(p + at1));
     };
     settle();
     if (t < tokens) {
@@ -141,33 +144,34 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     while (t < tokens) {
         const int at = head0 + h;
         const bool is_q = at < a.heads;
-        const uint32_t p0[4] = {x0.x, x0.y, x0.z, x0.w}, p1[4] = {x1.x, x1.y, x1.z, x1.w};
+        const Piece now0 = x0, now1 = x1;
+        const uint32_t *p0 = reinterpret_cast<const uint32_t *>(&now0), *p1 = reinterpret_cast<const uint32_t *>(&now1);
         uint16_t *out = is_q ? a.Q_out + offset[t].q_out + at * a.q_out.head : a.K_out + offset[t].k_out + (at - a.heads) * a.k_out.head;
         const float *cos = cosine[t], *sin = sine[t];
         h += kRows;
         settle();
         if (t < tokens) load(offset[t].q, offset[t].k);
-        float2 u[4], v[4];
+        float2 u[W], v[W];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < W; ++i) {
             u[i] = unpack2<BF16>(p0[i]);
             v[i] = unpack2<BF16>(p1[i]);
         }
         if ((is_q ? a.q_weight : a.k_weight) != nullptr) {
             float2 sums = mul2(u[0], u[0]);
 #pragma unroll
-            for (int i = 1; i < 4; ++i) sums = fma2(u[i], u[i], sums);
+            for (int i = 1; i < W; ++i) sums = fma2(u[i], u[i], sums);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums = fma2(v[i], v[i], sums);
+            for (int i = 0; i < W; ++i) sums = fma2(v[i], v[i], sums);
             float sum = sums.x + sums.y;
             const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
             const float f = rsqrtf(sum * (1.0f / D) + a.eps);
-            const uint4 w0 = *reinterpret_cast<const uint4 *>(&weight[is_q ? 0 : 1][at0]), w1 = *reinterpret_cast<const uint4 *>(&weight[is_q ? 0 : 1][at1]);
-            const uint32_t q0[4] = {w0.x, w0.y, w0.z, w0.w}, q1[4] = {w1.x, w1.y, w1.z, w1.w};
+            const Piece w0 = *reinterpret_cast<const Piece *>(&weight[is_q ? 0 : 1][at0]), w1 = *reinterpret_cast<const Piece *>(&weight[is_q ? 0 : 1][at1]);
+            const uint32_t *q0 = reinterpret_cast<const uint32_t *>(&w0), *q1 = reinterpret_cast<const uint32_t *>(&w1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < W; ++i) {
                 u[i] = mul2(u[i], mul2(unpack2<BF16>(q0[i]), make_float2(f, f)));
                 v[i] = mul2(v[i], mul2(unpack2<BF16>(q1[i]), make_float2(f, f)));
             }
@@ -193,17 +197,17 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
             }
         } else if (lane < units) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                rotate2(u[i], v[i], *reinterpret_cast<const float2 *>(cos + lane * 8 + 2 * i), *reinterpret_cast<const float2 *>(sin + lane * 8 + 2 * i));
+            for (int i = 0; i < W; ++i)
+                rotate2(u[i], v[i], *reinterpret_cast<const float2 *>(cos + lane * P + 2 * i), *reinterpret_cast<const float2 *>(sin + lane * P + 2 * i));
         }
-        uint32_t y0[4], y1[4];
+        Piece y0, y1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y0[i] = pack2<BF16>(u[i].x, u[i].y);
-            y1[i] = pack2<BF16>(v[i].x, v[i].y);
+        for (int i = 0; i < W; ++i) {
+            reinterpret_cast<uint32_t *>(&y0)[i] = pack2<BF16>(u[i].x, u[i].y);
+            reinterpret_cast<uint32_t *>(&y1)[i] = pack2<BF16>(v[i].x, v[i].y);
         }
-        __stcs(reinterpret_cast<uint4 *>(out + at0), make_uint4(y0[0], y0[1], y0[2], y0[3]));
-        __stcs(reinterpret_cast<uint4 *>(out + at1), make_uint4(y1[0], y1[1], y1[2], y1[3]));
+        __stcs(reinterpret_cast<Piece *>(out + at0), y0);
+        __stcs(reinterpret_cast<Piece *>(out + at1), y1);
     }
 }
 
@@ -260,8 +264,9 @@ qk_rotary_any_kernel(const __grid_constant__ RotaryArgs a) {
     }
 }
 
-static bool pieces16(const void *p, const sp_strides &s) {
-    return aligned16(p) && s.seq % 8 == 0 && s.token % 8 == 0 && s.head % 8 == 0;
+// Whether every head begins on a boundary of n values (2 n bytes).
+static bool pieces(const void *p, const sp_strides &s, int n) {
+    return reinterpret_cast<uintptr_t>(p) % (2 * n) == 0 && s.seq % n == 0 && s.token % n == 0 && s.head % n == 0;
 }
 
 sp_status launch_qk_rotary(const QkRotary &r, cudaStream_t stream) {
@@ -286,12 +291,15 @@ sp_status launch_qk_rotary(const QkRotary &r, cudaStream_t stream) {
     a.rotary = r.rotary;
     a.eps = r.eps;
     a.pairs = r.pairs;
-    const bool fast = (r.head_dim == 64 || r.head_dim == 128) && (r.pairs || r.rotary % 16 == 0) &&
-                      pieces16(r.Q, r.q) && pieces16(r.K, r.k) && pieces16(r.Q_out, r.q_out) && pieces16(r.K_out, r.k_out) &&
-                      aligned16(r.q_weight) && aligned16(r.k_weight);
+    const bool whole = r.head_dim == 64 || r.head_dim == 128;
+    auto in_pieces = [&](int n) {
+        return whole && pieces(r.Q, r.q, n) && pieces(r.K, r.k, n) && pieces(r.Q_out, r.q_out, n) && pieces(r.K_out, r.k_out, n);
+    };
+    // Values a piece: 8 where the layout and the halves allow it, else 4; else one by one.
+    const int piece = in_pieces(8) && (r.pairs || r.rotary % 16 == 0) ? 8 : in_pieces(4) && !r.pairs && r.rotary % 8 == 0 ? 4 : 0;
     // Whole tokens, several to a block once the device is full of blocks; few tokens are shared out by
     // heads instead, each block working the angles out for itself.
-    const int heads = a.heads + a.kv_heads, rows = fast ? kRotaryThreads / (r.head_dim / 16) : kRotaryThreads / 32;
+    const int heads = a.heads + a.kv_heads, rows = piece > 0 ? kRotaryThreads / (r.head_dim / (2 * piece)) : kRotaryThreads / 32;
     a.tokens = static_cast<int>(std::max(int64_t(1), std::min(int64_t(kMostTokens), a.total / (148 * 8))));
     a.head_share = heads;
     while (a.head_share > rows && a.total * ((heads + a.head_share - 1) / a.head_share) < 148) a.head_share = (a.head_share + 1) / 2;
@@ -299,13 +307,15 @@ sp_status launch_qk_rotary(const QkRotary &r, cudaStream_t stream) {
     PdlConfig pdl(dim3(static_cast<unsigned>(blocks), (heads + a.head_share - 1) / a.head_share), dim3(kRotaryThreads), stream);
     const bool bf16 = r.dtype == SP_BF16;
     cudaError_t e;
-#define SP_LAUNCH(D, P) \
-    e = bf16 ? cudaLaunchKernelEx(&pdl.cfg, qk_rotary_kernel<true, D, P>, a) : cudaLaunchKernelEx(&pdl.cfg, qk_rotary_kernel<false, D, P>, a)
-    if (!fast) e = bf16 ? cudaLaunchKernelEx(&pdl.cfg, qk_rotary_any_kernel<true>, a) : cudaLaunchKernelEx(&pdl.cfg, qk_rotary_any_kernel<false>, a);
-    else if (r.head_dim == 64 && r.pairs) SP_LAUNCH(64, true);
-    else if (r.head_dim == 64) SP_LAUNCH(64, false);
-    else if (r.pairs) SP_LAUNCH(128, true);
-    else SP_LAUNCH(128, false);
+#define SP_LAUNCH(D, PAIRS, P) \
+    e = bf16 ? cudaLaunchKernelEx(&pdl.cfg, qk_rotary_kernel<true, D, PAIRS, P>, a) : cudaLaunchKernelEx(&pdl.cfg, qk_rotary_kernel<false, D, PAIRS, P>, a)
+    if (piece == 0) e = bf16 ? cudaLaunchKernelEx(&pdl.cfg, qk_rotary_any_kernel<true>, a) : cudaLaunchKernelEx(&pdl.cfg, qk_rotary_any_kernel<false>, a);
+    else if (r.head_dim == 64 && r.pairs) SP_LAUNCH(64, true, 8);
+    else if (r.pairs) SP_LAUNCH(128, true, 8);
+    else if (r.head_dim == 64 && piece == 8) SP_LAUNCH(64, false, 8);
+    else if (r.head_dim == 64) SP_LAUNCH(64, false, 4);
+    else if (piece == 8) SP_LAUNCH(128, false, 8);
+    else SP_LAUNCH(128, false, 4);
 #undef SP_LAUNCH
     if (e != cudaSuccess) return cuda_fail(e);
     return check_launch();
