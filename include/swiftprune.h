@@ -561,7 +561,8 @@ sp_status sp_qk_norm_rotary(const void *Q, const sp_strides *q_strides, int n_he
  * counts the table entries that name each, and a block with refs 0 is free.  The calls keep the
  * table (written here although sp_cache declares it const) and refs in agreement, and need no
  * answer from the host: results are the same whatever runs at the same time inside them.  A pool
- * has at most 2^31 - 1 blocks.  Workspaces as in sp_mx4_linear.
+ * has at most 2^30 blocks.  Workspaces as in sp_mx4_linear.  sp_cache_append writes where the table
+ * says: a block that others name too is first reserved; sp_cache_evict's dst has blocks of its own.
  *
  * sp_cache_fork: row dst[i] of the table becomes a copy of row src[i], or empty (-1) where src is
  * NULL or src[i] names no row: so answers start from one prompt, beams change places, and finished
@@ -611,7 +612,11 @@ sp_status sp_cache_compact(const sp_cache *cache, const int32_t *refs, int32_t *
  * accumulated weights: queries see the tokens up to their own place, in the prefix too.  max_prefix
  * >= every prefix[g] and max_group >= the sequences of every group (tokens of a prefix past
  * max_prefix, and sequences past the first max_group of a group, are read through the sequences' own
- * rows).
+ * rows).  Weights of the prefix, times their values' scale, enter their product to 2^-17 of themselves
+ * (those of a sequence's own tokens as in sp_cache_attention); bf16 queries enter as they are.
+ * Limits as in sp_cache_attention, and n_groups and max_group at most 32767, n_kv_heads times the
+ * group's rows (max_group * n_q * n_heads / n_kv_heads) over 256, rounded up, at most 65535 (else
+ * SP_ERR_SHAPE).  O must not overlap Q or the workspace.
  */
 sp_status sp_cache_attention_shared_workspace(const sp_cache *cache, int64_t n_q, int n_heads,
                                               int64_t max_len, int64_t n_groups, int64_t max_prefix,

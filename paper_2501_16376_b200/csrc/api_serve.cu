@@ -253,7 +253,7 @@ sp_status sp_qk_norm_rotary(const void *Q, const sp_strides *q_strides, int n_he
 
 static sp_status check_pages(const sp_cache *c) {
     sp_status st = check_cache(c);
-    if (st == SP_OK && c->n_blocks > 0x7fffffff) st = SP_ERR_SHAPE;
+    if (st == SP_OK && c->n_blocks > (1 << 30)) st = SP_ERR_SHAPE;
     return st;
 }
 
@@ -337,6 +337,7 @@ sp_status sp_cache_attention_shared_workspace(const sp_cache *cache, int64_t n_q
     s.n_groups = n_groups;
     s.max_prefix = max_prefix;
     s.max_group = max_group;
+    if (!cache_shared_fits(*cache, s)) return SP_ERR_SHAPE;
     *bytes = cache_shared_workspace(*cache, s);
     return SP_OK;
 }

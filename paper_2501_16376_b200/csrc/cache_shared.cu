@@ -769,11 +769,15 @@ static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     return p;
 }
 
+bool cache_shared_fits(const sp_cache &c, const SharedAttention &s) {
+    return int64_t(prefix_plan(c, s).row_tiles) * c.n_kv_heads <= 65535;
+}
+
 int64_t cache_shared_workspace(const sp_cache &c, const SharedAttention &s) {
     const int64_t rows = s.n_q * (s.n_heads / c.n_kv_heads), pairs = c.n_seqs * c.n_kv_heads;
     if (rows == 0 || pairs == 0) return 0;
     const PrefixPlan plan = prefix_plan(c, s);
-    if (plan.splits == 0) return cache_attention_workspace(c, s.n_q, s.n_heads, s.max_len, false);
+    if (plan.splits == 0 || c.n_blocks == 0) return cache_attention_workspace(c, s.n_q, s.n_heads, s.max_len, false);
     return pairs * (plan.splits * plan.copies + plan.tail_splits) * rows * (c.head_dim * 4 + 8);
 }
 

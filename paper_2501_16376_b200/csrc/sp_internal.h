@@ -324,6 +324,7 @@ struct SharedAttention {
     void *O;
     float *lse;
 };
+bool cache_shared_fits(const sp_cache &c, const SharedAttention &s);  // whether the queries' rows fit in a launch
 int64_t cache_shared_workspace(const sp_cache &c, const SharedAttention &s);
 sp_status launch_cache_shared(const sp_cache &c, const SharedAttention &s, void *workspace, cudaStream_t stream);
 

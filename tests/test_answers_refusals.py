@@ -65,6 +65,8 @@ def test_shared_attention(b):
     for kw in (dict(heads=0), dict(n_q=-1), dict(max_len=-1), dict(groups=-1), dict(max_prefix=-1), dict(max_group=-1), dict(scale=float("inf")),
                dict(Q=None), dict(O=None), dict(lens=None), dict(starts=None), dict(prefix=None)):
         assert call(**kw) == b.SP_ERR_INVALID_ARG, kw
+    many = _cache(b, n_seqs=32767, n_kv_heads=512, head_dim=128)
+    assert call(c=many, n_q=1, heads=4096, max_group=32767) == b.SP_ERR_SHAPE      # 1024 tiles of rows for 512 heads
     assert b.lib.sp_cache_attention_shared_workspace(c, 1, 4, 64, 1, 32, 2, ctypes.byref(n)) == b.SP_OK
     if n.value:
         assert call(ws=None) == b.SP_ERR_INVALID_ARG and call(size=n.value - 1) == b.SP_ERR_INVALID_ARG

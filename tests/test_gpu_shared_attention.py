@@ -288,3 +288,46 @@ def test_scores_that_rise_by_a_little_and_by_much(sp):
             Q = torch.zeros(2, 1, 3, 64)
             Q[..., 3] = 8.0
             _check(sp, cache, Q.to(dtype), [320, 311], 320, [0, 2], [304], scale=1.0)
+
+
+def test_more_rows_than_a_block_takes(sp):
+    """2400 query rows of one prefix, the sequences of a group past 256 rows and 128."""
+    cache = _cache(sp, 300, 6, 1, 64, 16, seed=22)
+    lens = [64 + 1 + (5 * b) % 32 for b in range(300)]
+    _check(sp, cache, _queries(300, 1, 8, 64, torch.bfloat16, 22), lens, 96, [0, 300], [64])
+
+
+def test_pools_and_batches_of_nothing(sp):
+    cache = sp.KvCache.pool(3, 64, 0, 2, 64, 16)
+    Q = _queries(3, 1, 4, 64, torch.float16, 23).cuda()
+    lse = torch.zeros(3, 1, 4, device="cuda")
+    O = cache.sp_cache_attention_shared(Q, _i32([5, 64, 0]), 64, _i32([0, 3]), _i32([48]), 48, 3, lse=lse)
+    assert not O.any() and torch.isneginf(lse).all()
+    cache = sp.KvCache.pool(0, 64, 4, 2, 64, 16)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert cache.sp_cache_attention_shared(Q[:0], none, 64, _i32([0]), none, 48, 3).shape == (0, 1, 4, 64)
+    cache.sp_cache_fork(none)
+    assert cache.sp_cache_reserve(none, 5).tolist() == [0, 4] and cache.sp_cache_compact().item() == 0
+
+
+def test_calls_on_two_streams_at_once(sp):
+    """Two caches of other sizes and types on two streams, each as it is alone, again and again."""
+    jobs = []
+    for seed, (heads, dim, block, dtype, size) in enumerate(((2, 64, 16, torch.float16, 20), (4, 128, 32, torch.bfloat16, 40))):
+        cache = _cache(sp, size, 20, heads, dim, block, seed=30 + seed)
+        Q = _queries(size, 1, heads * 4, dim, dtype, seed).cuda()
+        n = 16 * block
+        lens = _i32([n + 1 + b % (3 * block) for b in range(size)])
+        call = lambda cache=cache, Q=Q, lens=lens, n=n, size=size, block=block: cache.sp_cache_attention_shared(
+            Q, lens, 20 * block, _i32([0, size]), _i32([n]), n, size)
+        jobs.append((call, call()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    outs = [[], []]
+    for _ in range(30):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(jobs[i][0]())
+    torch.cuda.synchronize()
+    for (_, want), got in zip(jobs, outs):
+        assert all(torch.equal(want, o) for o in got)
