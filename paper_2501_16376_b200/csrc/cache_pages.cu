@@ -48,22 +48,22 @@ cache_fork_kernel(const ForkArgs a) {
     __syncthreads();
     for (int i = threadIdx.x; i < a.n; i += kForkThreads)
         if (names(a.dst[i], a.n_seqs)) atomicMax(&winner[a.dst[i]], i);
+    __syncthreads();
 #pragma unroll 4
     for (int i = warp; i < a.n; i += kForkWarps) {
-        const int s = a.src != nullptr ? a.src[i] : -1;
-        staged[i * 32 + lane] = here && names(s, a.n_seqs) ? a.table[s * a.ld_table + col] : -1;
+        const int d = a.dst[i], s = a.src != nullptr ? a.src[i] : -1;
+        if (!here || !names(d, a.n_seqs) || winner[d] != i) continue;
+        const int now = names(s, a.n_seqs) ? a.table[s * a.ld_table + col] : -1, was = a.table[d * a.ld_table + col];
+        staged[int64_t(i) * 32 + lane] = now;
+        if (was == now) continue;
+        if (names(was, a.n_blocks)) atomicSub(&a.refs[was], 1);
+        if (names(now, a.n_blocks)) atomicAdd(&a.refs[now], 1);
     }
     __syncthreads();
 #pragma unroll 4
     for (int i = warp; i < a.n; i += kForkWarps) {
         const int d = a.dst[i];
-        if (!here || !names(d, a.n_seqs) || winner[d] != i) continue;
-        int32_t *at = a.table + d * a.ld_table + col;
-        const int was = *at, now = staged[i * 32 + lane];
-        if (was == now) continue;
-        *at = now;
-        if (names(was, a.n_blocks)) atomicSub(&a.refs[was], 1);
-        if (names(now, a.n_blocks)) atomicAdd(&a.refs[now], 1);
+        if (here && names(d, a.n_seqs) && winner[d] == i) a.table[d * a.ld_table + col] = staged[int64_t(i) * 32 + lane];
     }
 }
 
@@ -101,14 +101,24 @@ struct Stretch {
         end = min(n_blocks, begin + each);
     }
 };
-__device__ __forceinline__ int count_live(const int32_t *refs, const Stretch &s) {
+// `flags` keeps what a lane saw in its first 32 looks (pools up to 32768 blocks), for is_live.
+__device__ __forceinline__ int count_live(const int32_t *refs, const Stretch &s, uint32_t &flags) {
     const int lane = threadIdx.x & 31;
     int live = 0;
+    flags = 0u;
 #pragma unroll 8
-    for (int i = s.begin; i < s.end; i += 32) live += i + lane < s.end && refs[i + lane] > 0;
+    for (int i = s.begin, look = 0; i < s.end; i += 32, ++look) {
+        const uint32_t one = i + lane < s.end && refs[i + lane] > 0;
+        live += one;
+        if (look < 32) flags |= one << look;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) live += __shfl_xor_sync(kFullWarp, live, o);
     return live;
+}
+__device__ __forceinline__ bool is_live(const int32_t *refs, const Stretch &s, uint32_t flags, int i) {
+    const int look = (i - s.begin) >> 5, at = i + (threadIdx.x & 31);
+    return look < 32 ? (flags >> look) & 1u : at < s.end && refs[at] > 0;
 }
 
 // ------------------------------------------------------------------ reserve
@@ -124,26 +134,27 @@ struct ReserveArgs {
     int2 *copies;            // [n_seqs]: (from, to), from < 0 where nothing is copied
     int64_t n_new;
     int per;                 // requests of a sequence
-    int64_t requests;
+    int requests, block_shift;
 };
 
 struct Request {
-    int64_t row, entry;   // of the table
+    int row;
+    int64_t entry;        // of the table
     int id;               // the block named there, or < 0
     bool asked, partial;  // whether it is asked for; whether tokens before the new ones lie in it
 };
-__device__ __forceinline__ Request request(const ReserveArgs &a, int64_t r) {
+__device__ __forceinline__ Request request(const ReserveArgs &a, int r) {
     const sp_cache &c = a.cache;
     Request q = {};
     q.id = -1;
     if (r >= a.requests) return q;
     q.row = r / a.per;
-    const int64_t start = a.start[q.row], T = c.block_tokens;
+    const int start = a.start[q.row];
     const int64_t n = a.count != nullptr ? min(int64_t(a.count[q.row]), a.n_new) : a.n_new;
-    const int64_t place = start / T + r % a.per;
-    if (start < 0 || n <= 0 || place * T >= start + n || place >= c.table_cols) return q;
+    const int64_t place = (start >> a.block_shift) + (r - q.row * a.per), first = place << a.block_shift;
+    if (start < 0 || n <= 0 || first >= start + n || place >= c.table_cols) return q;
     q.asked = true;
-    q.partial = place * T < start;
+    q.partial = first < start;
     q.entry = q.row * c.ld_table + place;
     const int id = a.table[q.entry];
     q.id = names(id, static_cast<int>(c.n_blocks)) ? id : -1;
@@ -160,7 +171,7 @@ cache_reserve_kernel(const __grid_constant__ ReserveArgs a) {
     const int n_blocks = static_cast<int>(c.n_blocks), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_launch_dependents();
     pdl_wait();
-    for (int64_t r = threadIdx.x; r < a.requests; r += kBookThreads) {
+    for (int r = threadIdx.x; r < a.requests; r += kBookThreads) {
         const Request q = request(a, r);
         if (q.id >= 0) {
             a.asked[q.id] = 0;
@@ -169,14 +180,15 @@ cache_reserve_kernel(const __grid_constant__ ReserveArgs a) {
         if (r % a.per == 0) a.copies[r / a.per] = make_int2(-1, -1);
     }
     const Stretch mine(n_blocks);
-    const int live = count_live(a.refs, mine);
+    uint32_t flags;
+    const int live = count_live(a.refs, mine, flags);
     if (lane == 0) live_before[warp] = live;
     __syncthreads();
-    for (int64_t r = threadIdx.x; r < a.requests; r += kBookThreads) {
+    for (int r = threadIdx.x; r < a.requests; r += kBookThreads) {
         const Request q = request(a, r);
         if (q.id >= 0) {
             atomicAdd(&a.asked[q.id], 1);
-            atomicMin(&a.first[q.id], static_cast<int>(r));
+            atomicMin(&a.first[q.id], r);
         }
     }
     if (warp == 0) {  // live blocks before each warp's stretch
@@ -193,13 +205,13 @@ cache_reserve_kernel(const __grid_constant__ ReserveArgs a) {
     __syncthreads();
     const int n_free = n_blocks - live_before[kBookWarps];
     int need = 0;
-    for (int64_t r0 = 0; r0 < a.requests; r0 += kBookThreads) {
-        const int64_t r = r0 + threadIdx.x;
+    for (int r0 = 0; r0 < a.requests; r0 += kBookThreads) {
+        const int r = r0 + static_cast<int>(threadIdx.x);
         const Request q = request(a, r);
         bool wants = q.asked;
         if (q.id >= 0) {
             const int refs = a.refs[q.id];
-            if (refs <= 1 || (a.asked[q.id] >= refs && a.first[q.id] == static_cast<int>(r))) wants = false;
+            if (refs <= 1 || (a.asked[q.id] >= refs && a.first[q.id] == r)) wants = false;
         }
         int total;
         const int at = block_scan(wants, warp_sums, total);
@@ -215,14 +227,14 @@ cache_reserve_kernel(const __grid_constant__ ReserveArgs a) {
     // the free blocks that are handed out
     int before = mine.begin - live_before[warp];
     for (int i = mine.begin; i < mine.end && before < need; i += 32) {
-        const bool is_free = i + lane < mine.end && a.refs[i + lane] <= 0;
+        const bool is_free = i + lane < mine.end && !is_live(a.refs, mine, flags, i);
         const unsigned vote = __ballot_sync(kFullWarp, is_free);
         const int at = before + __popc(vote & ((1u << lane) - 1u));
         if (is_free && at < need) a.free[at] = i + lane;
         before += __popc(vote);
     }
     __syncthreads();
-    for (int64_t r = threadIdx.x; r < a.requests; r += kBookThreads) {
+    for (int r = threadIdx.x; r < a.requests; r += kBookThreads) {
         const int at = a.rank[r];
         if (at < 0) continue;
         const Request q = request(a, r);
@@ -301,7 +313,8 @@ cache_compact_kernel(const __grid_constant__ CompactArgs a) {
     pdl_launch_dependents();
     pdl_wait();
     const Stretch mine(n_blocks);
-    const int live = count_live(a.refs, mine);
+    uint32_t flags;
+    const int live = count_live(a.refs, mine, flags);
     if (lane == 0) live_before[warp] = live;
     if (threadIdx.x == 0) low_live = 0;
     __syncthreads();
@@ -321,7 +334,7 @@ cache_compact_kernel(const __grid_constant__ CompactArgs a) {
     // live blocks among the first n_live numbers: each warp's share of them
     {
         int low = 0;
-        for (int i = mine.begin; i < min(mine.end, n_live); i += 32) low += i + lane < min(mine.end, n_live) && a.refs[i + lane] > 0;
+        for (int i = mine.begin; i < min(mine.end, n_live); i += 32) low += i + lane < n_live && is_live(a.refs, mine, flags, i);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) low += __shfl_xor_sync(kFullWarp, low, o);
         if (lane == 0 && low != 0) atomicAdd(&low_live, low);
@@ -335,13 +348,13 @@ cache_compact_kernel(const __grid_constant__ CompactArgs a) {
     int before = live_before[warp];
     for (int i = mine.begin; i < mine.end; i += 32) {
         const int id = i + lane;
-        const bool in = id < mine.end, is_live = in && a.refs[id] > 0;
-        const unsigned vote = __ballot_sync(kFullWarp, is_live);
+        const bool in = id < mine.end, alive = is_live(a.refs, mine, flags, i);
+        const unsigned vote = __ballot_sync(kFullWarp, alive);
         const int at = before + __popc(vote & ((1u << lane) - 1u));  // live blocks before this one
         if (in) {
-            if (is_live && id >= n_live) a.movers[at - stay] = id;
-            else a.remap[id] = is_live ? id : -1;
-            if (!is_live && id < n_live) a.holes[id - at] = id;
+            if (alive && id >= n_live) a.movers[at - stay] = id;
+            else a.remap[id] = alive ? id : -1;
+            if (!alive && id < n_live) a.holes[id - at] = id;
         }
         before += __popc(vote);
     }
@@ -431,7 +444,8 @@ sp_status launch_cache_reserve(const sp_cache &c, int32_t *refs, const int32_t *
     a.status = status;
     a.n_new = n_new;
     a.per = static_cast<int>(requests_of_a_sequence(c, n_new));
-    a.requests = c.n_seqs * a.per;
+    a.requests = static_cast<int>(c.n_seqs * a.per);
+    a.block_shift = c.block_tokens == 16 ? 4 : c.block_tokens == 32 ? 5 : 6;
     a.copies = static_cast<int2 *>(workspace);
     a.asked = reinterpret_cast<int32_t *>(a.copies + c.n_seqs);
     a.first = a.asked + c.n_blocks;
