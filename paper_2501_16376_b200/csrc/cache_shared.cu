@@ -544,7 +544,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         bool ok = mbar_wait_or_fail(smem_addr(&q_full), 0, &failed);  // all_see is final
         RingPlace<kScaleSlots> scale_at;
         if (from == 1) scale_at.next();
-        bool far_maximum = false;  // of a row of the warp
+        bool far_maximum = false, fresh = true;  // of a row of the warp; before the first scores
         // sums of the steps before, by a row's own factor
         auto scale_sums = [&](int turn, float by) {
             if (turn == 0) return true;
@@ -603,47 +603,51 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                             if (token0 + i * 32 + j > limit || !((info.x >> (2 * i + (j >> 4))) & 1)) now[j] = 0xff800000u;
                     }
                 };
+                float2 p[16];
                 for (int attempt = 0;; ++attempt) {
-                    // the value scale goes into the exponent, and out of the sum again; step by step for all
-                    // 32, since a warp waits for each of its instructions' operands in turn
-                    float2 p[16];
-                    const bool near = !far_maximum && min(e[0], e[1]) >= kFarScale;
-                    {
-                        uint32_t now[32];
-                        load_scores(now);
-                        if (near) {
-                            const float less[2] = {static_cast<float>(e[0]) - m, static_cast<float>(e[1]) - m};
+                    // (the first scores have no maximum to be taken from: it is found first)
+                    if (attempt > 0 || !fresh) {
+                        // the value scale goes into the exponent, and out of the sum again; step by step for all
+                        // 32, since a warp waits for each of its instructions' operands in turn
+                        const bool near = !far_maximum && min(e[0], e[1]) >= kFarScale;
+                        {
+                            uint32_t now[32];
+                            load_scores(now);
+                            if (near) {
+                                const float less[2] = {static_cast<float>(e[0]) - m, static_cast<float>(e[1]) - m};
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                p[j] = fma2(make_float2(__uint_as_float(now[2 * j]), __uint_as_float(now[2 * j + 1])),
-                                            make_float2(k[j >> 3], k[j >> 3]), make_float2(less[j >> 3], less[j >> 3]));
-                        } else {
-                            // scores so large that a product differs from the maximum, itself rounded, by
-                            // powers of two; value scales that would take the weights out of the sum
+                                for (int j = 0; j < 16; ++j)
+                                    p[j] = fma2(make_float2(__uint_as_float(now[2 * j]), __uint_as_float(now[2 * j + 1])),
+                                                make_float2(k[j >> 3], k[j >> 3]), make_float2(less[j >> 3], less[j >> 3]));
+                            } else {
+                                // scores so large that a product differs from the maximum, itself rounded, by
+                                // powers of two; value scales that would take the weights out of the sum
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)  // (of pairs, a product and a sum would be made one)
-                                p[j] = make_float2(__fadd_rn(__fmul_rn(__uint_as_float(now[2 * j]), k[j >> 3]), -m),
-                                                   __fadd_rn(__fmul_rn(__uint_as_float(now[2 * j + 1]), k[j >> 3]), -m));
+                                for (int j = 0; j < 16; ++j)  // (of pairs, a product and a sum would be made one)
+                                    p[j] = make_float2(__fadd_rn(__fmul_rn(__uint_as_float(now[2 * j]), k[j >> 3]), -m),
+                                                       __fadd_rn(__fmul_rn(__uint_as_float(now[2 * j + 1]), k[j >> 3]), -m));
+                            }
                         }
-                    }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) p[j] = make_float2(exp2_fast(p[j].x), exp2_fast(p[j].y));
-                    float sums[2];
+                        for (int j = 0; j < 16; ++j) p[j] = make_float2(exp2_fast(p[j].x), exp2_fast(p[j].y));
+                        float sums[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float2 *x = p + 8 * h;
-                        const float2 t = add2(add2(add2(x[0], x[1]), add2(x[2], x[3])), add2(add2(x[4], x[5]), add2(x[6], x[7])));
-                        sums[h] = t.x + t.y;
-                    }
-                    if (near) {
-                        sum = sums[0] * pow2(-e[0]) + sums[1] * pow2(-e[1]);
-                    } else {
-                        sum = sums[0] + sums[1];
+                        for (int h = 0; h < 2; ++h) {
+                            const float2 *x = p + 8 * h;
+                            const float2 t = add2(add2(add2(x[0], x[1]), add2(x[2], x[3])), add2(add2(x[4], x[5]), add2(x[6], x[7])));
+                            sums[h] = t.x + t.y;
+                        }
+                        if (near) {
+                            sum = sums[0] * pow2(-e[0]) + sums[1] * pow2(-e[1]);
+                        } else {
+                            sum = sums[0] + sums[1];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) p[j] = mul2(p[j], make_float2(pow2(e[j >> 3]), pow2(e[j >> 3])));
+                            for (int j = 0; j < 16; ++j) p[j] = mul2(p[j], make_float2(pow2(e[j >> 3]), pow2(e[j >> 3])));
+                        }
+                        split16(p, part);
+                        if (attempt == 1 || !__any_sync(kFullWarp, sum > kRaise)) break;  // once raised, a weight is at most 2
                     }
-                    split16(p, part);
-                    if (attempt == 1 || !__any_sync(kFullWarp, sum > kRaise)) break;  // once raised, a weight is at most 2
+                    fresh = false;
                     // the maximum rises: the sums before, and this step's weights before, follow
                     uint32_t v[32];
                     load_scores(v);
