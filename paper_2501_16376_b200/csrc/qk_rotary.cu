@@ -76,13 +76,13 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 
 // Heads of D values in pieces of P, aligned as such; PAIRS (8), or halves with rotary a multiple of 2 P.
 template <bool BF16, int D, bool PAIRS, int P>
-__global__ void __launch_bounds__(kRotaryThreads, 4)
+__global__ void __launch_bounds__(kRotaryThreads, 5)
 qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     static_assert(P == 8 || (P == 4 && !PAIRS), "pairs are turned in pieces of 8");
     using Piece = typename std::conditional<P == 8, uint4, uint2>::type;
     constexpr int kLanes = D / (2 * P), kRows = kRotaryThreads / kLanes, W = P / 2;
     __shared__ __align__(16) float cosine[kMostTokens][D / 2], sine[kMostTokens][D / 2];
-    __shared__ __align__(16) uint16_t weight[2][D];
+    __shared__ __align__(16) float weight[2][D];
     __shared__ Offsets offset[kMostTokens];
     pdl_launch_dependents();
     pdl_wait();
@@ -137,8 +137,8 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
         sine[at / half][at % half] = cs.y;
     }
     for (int d = threadIdx.x; d < D; d += kRotaryThreads) {
-        if (a.q_weight != nullptr) weight[0][d] = a.q_weight[d];
-        if (a.k_weight != nullptr) weight[1][d] = a.k_weight[d];
+        if (a.q_weight != nullptr) weight[0][d] = widen<BF16>(a.q_weight[d]);
+        if (a.k_weight != nullptr) weight[1][d] = widen<BF16>(a.k_weight[d]);
     }
     __syncthreads();
     while (t < tokens) {
@@ -168,12 +168,15 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
             const float f = rsqrtf(sum * (1.0f / D) + a.eps);
-            const Piece w0 = *reinterpret_cast<const Piece *>(&weight[is_q ? 0 : 1][at0]), w1 = *reinterpret_cast<const Piece *>(&weight[is_q ? 0 : 1][at1]);
-            const uint32_t *q0 = reinterpret_cast<const uint32_t *>(&w0), *q1 = reinterpret_cast<const uint32_t *>(&w1);
+            const float4 *w0 = reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][at0]), *w1 = reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][at1]);
+            const float2 f2 = make_float2(f, f);
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                u[i] = mul2(u[i], mul2(unpack2<BF16>(q0[i]), make_float2(f, f)));
-                v[i] = mul2(v[i], mul2(unpack2<BF16>(q1[i]), make_float2(f, f)));
+            for (int i = 0; i < W; i += 2) {
+                const float4 g0 = w0[i / 2], g1 = w1[i / 2];
+                u[i] = mul2(u[i], mul2(make_float2(g0.x, g0.y), f2));
+                u[i + 1] = mul2(u[i + 1], mul2(make_float2(g0.z, g0.w), f2));
+                v[i] = mul2(v[i], mul2(make_float2(g1.x, g1.y), f2));
+                v[i + 1] = mul2(v[i + 1], mul2(make_float2(g1.z, g1.w), f2));
             }
         }
         // what is not turned stays as it is: a product with 0 would let an infinity through
