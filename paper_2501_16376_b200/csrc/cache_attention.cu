@@ -1048,6 +1048,11 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
 }
 
 // ------------------------------------------------------------------ beside a shared prefix
+//
+// The tokens behind a prefix are many short caches, with few rows each: blocks of one warp, 13 to 15 of
+// which an SM holds, without a barrier between warps.  256 sequences of 150 to 330 own tokens, 8 heads: 30 us of
+// the whole device, bound by the issue and the fixed latencies of some 700 cycles a step of 16 tokens (blocks of four
+// warps: 35 us, and 8 us where a tail is one step).  They run beside the prefix on SMs of their own.
 
 // How many blocks, of a warp each, share the tail of a (sequence, kv head, row tile): `tail` estimates
 // its tokens.  16 fit on an SM; none has less than 64 tokens.
