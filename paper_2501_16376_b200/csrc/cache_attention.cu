@@ -237,9 +237,12 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
         }
         __syncthreads();
         // the kernel over the prefix has waited before it let this one start; its results are not
-        // read here
-        if constexpr (SHARED) from = static_cast<int>(shared_blocks(a.groups, c, seq) << (shift - 4));
-        else pdl_wait();
+        // read here.  What came before it is in the L2 cache by now: the fence drops what the L1 holds
+        // of older calls.
+        if constexpr (SHARED) {
+            __threadfence();
+            from = static_cast<int>(shared_blocks(a.groups, c, seq) << (shift - 4));
+        } else pdl_wait();
     }
     const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
@@ -1070,7 +1073,8 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t seq = blockIdx.z, pair = seq * H + head;
     pdl_launch_dependents();
-    // what groups there are was known before the tails began
+    // what groups there are was known before the tails began (the fence as there)
+    __threadfence();
     const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // else there are no parts of the prefix
     pdl_wait();
     for (int row = blockIdx.x * (kSharedJoinThreads / 32) + warp; row < a.rows; row += gridDim.x * (kSharedJoinThreads / 32)) {

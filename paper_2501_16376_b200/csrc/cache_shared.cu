@@ -185,6 +185,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     pdl_wait();
+    __threadfence();
     pdl_launch_dependents();  // the kernel over the tails counts on what came before this one
 
     const SharedGroup g = shared_group(a.groups, c, blockIdx.z);

@@ -331,3 +331,39 @@ def test_calls_on_two_streams_at_once(sp):
     torch.cuda.synchronize()
     for (_, want), got in zip(jobs, outs):
         assert all(torch.equal(want, o) for o in got)
+
+
+def test_buffers_that_change_between_calls(sp):
+    """Queries, lengths, groups, table and scales of other values in the same memory from call to call,
+    with nothing waited for between them: each call as it is with its own alone."""
+    size, heads, dim, block, cols = 40, 2, 64, 16, 24
+    base = _cache(sp, size, cols, heads, dim, block, seed=40)
+    freq = torch.ones(dim // 2, device="cuda")
+    cases = []
+    for i in range(3):
+        g = torch.Generator().manual_seed(50 + i)
+        cases.append(dict(
+            q=torch.randn(size, 1, heads * 4, dim, generator=g).half().cuda(), k=torch.randn(size, 1, heads, dim, generator=g).half().cuda(),
+            table=torch.randperm(base.k.shape[0], generator=g)[:size * cols].view(size, cols).to(torch.int32).cuda(),
+            place=torch.randint(200, cols * block - 1, (size,), generator=g, dtype=torch.int32).cuda(),
+            starts=_i32([0, 10 + 5 * i, 40]), prefix=_i32([192 - 32 * i, 160 + 16 * i])))
+    def run(into, of, wait):
+        for name in into:
+            into[name].copy_(of[name])
+        for name, t in (("k", cache.k), ("v", cache.v), ("k_scale", cache.k_scale), ("v_scale", cache.v_scale)):
+            t.copy_(getattr(base, name))
+        cache.table.copy_(into["table"])
+        if wait:
+            torch.cuda.synchronize()
+        lens = into["place"] + 1
+        sp.sp_qk_norm_rotary(into["q"], into["k"], into["place"], freq, Q_out=into["q"], K_out=into["k"])
+        cache.sp_cache_append(into["k"], into["k"], into["place"])
+        if wait:
+            torch.cuda.synchronize()
+        return cache.sp_cache_attention_shared(into["q"], lens, cols * block, into["starts"], into["prefix"], 192, 30)
+    cache = sp.KvCache(base.k.clone(), base.v.clone(), base.k_scale.clone(), base.v_scale.clone(), base.table.clone())
+    into = {name: t.clone() for name, t in cases[0].items()}
+    want = [run({name: t.clone() for name, t in c.items()}, c, True) for c in cases]
+    got = [(i % 3, run(into, cases[i % 3], False)) for i in range(60)]
+    for i, o in got:
+        assert torch.equal(o, want[i])
