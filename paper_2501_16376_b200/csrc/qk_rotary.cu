@@ -6,16 +6,19 @@
 // The angle's product and its reduction to a turn are binary64: at place 10^6 a binary32 product is
 // off by up to 2^-5 radians, which an output in 16 bits shows.
 //
-// Bound by memory: 4 bytes a value, read once and written once.  All heads of a token turn by the
-// same angles, so a block takes whole tokens, works their cosines out once into shared memory and
-// uses them for every head; a head is D / 16 lanes of 16 values, whose two 16-byte pieces are the
-// partners of one another (halves) or hold whole pairs, so that no value changes lanes but in the sum
-// of squares.  Pairs of values share an instruction (one by one, with the lane's pieces side by side
-// and 88 registers, the large case below took 150 us: two thirds of the issue slots beside 55 % of the
-// memory rate).  Measured (calls replayed from a graph): 32768 tokens of 40 heads of 128, normed, bf16
-// 112 us (6.0 TB/s, 0.92 of the copy rate); 4 x 2047 tokens of 32 heads of 64, a quarter turned, f16
-// 11 us (6.1 TB/s); 8 tokens 2.5 us, which is the launch.  Halves of 12 (24 values turned) in pieces of
-// four: 140 us for the large case.
+// Bound by memory, 4 bytes a value read once and written once, and next to it by the issue slots, which count
+// double in a long run: the power limit then takes the clock from 1965 to 1710 MHz.  All heads of a
+// token turn by the same angles, so a block takes whole tokens and works their cosines out once into
+// shared memory.  A head is D / 16 lanes of 16 values, whose two 16-byte pieces are the partners of one another
+// (halves) or hold whole pairs, so that no value changes lanes but in the sum of squares; pairs of
+// values share an instruction, and are laid side by side for that as they are widened.  Lanes keep
+// their head from token to token, so that addresses, weights and masks cost next to nothing (heads
+// and tokens as one list of items took 112 us for the first case below, and 128 in a long run).
+// Weights stay in shared memory, in the order of the lanes: in registers they cost a block of the four (111 us).
+// Measured (calls replayed from a graph, inputs beyond the L2 cache): 32768 tokens of 40 heads of 128, pairs, normed,
+// bf16 107 us (6.3 TB/s, 0.96 of the copy rate), 111 in a long run; the same in halves 107 us; 4 x 2047 tokens of 16 and
+// 16 heads of 64, a quarter turned, f16 13 us; 8 tokens 2.6 us, which is the launch.  Halves of 12 (24 values
+// turned) in pieces of four: 131 us for the large case.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,8 +29,9 @@ namespace sp {
 
 namespace {
 
-constexpr int kRotaryThreads = 256;
-constexpr int kMostTokens = 8;  // of a block
+constexpr int kRotaryThreads = 256;  // one by one
+constexpr int kMostThreads = 320, kFewThreads = 160;  // in pieces; what a block has where a token takes fewer
+constexpr int kMostTokens = 8;       // of a block
 
 struct RotaryArgs {
     const uint16_t *Q, *K, *q_weight, *k_weight;
@@ -38,6 +42,7 @@ struct RotaryArgs {
     int64_t n_tokens, total;  // of a sequence, of all
     int heads, kv_heads, head_dim, rotary;
     int tokens, head_share;  // of a block
+    int slots;               // its tokens that are taken at a time
     float eps;
     bool pairs;
 };
@@ -80,89 +85,100 @@ __device__ __forceinline__ uint16_t narrow(float v) {
 }  // namespace
 
 // Heads of D values in pieces of P, aligned as such; PAIRS (8), or halves with rotary a multiple of 2 P.
+// kLanes threads keep one head, and take every a.slots-th of the block's tokens.
 template <bool BF16, int D, bool PAIRS, int P>
-__global__ void __launch_bounds__(kRotaryThreads, 5)
+__global__ void __launch_bounds__(kMostThreads, 4)
 qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     static_assert(P == 8 || (P == 4 && !PAIRS), "pairs are turned in pieces of 8");
     using Piece = typename std::conditional<P == 8, uint4, uint2>::type;
-    constexpr int kLanes = D / (2 * P), kRows = kRotaryThreads / kLanes, W = P / 2;
-    __shared__ __align__(16) float cosine[kMostTokens][D / 2], sine[kMostTokens][D / 2];
-    __shared__ __align__(16) float weight[2][D];
+    constexpr int kLanes = D / (2 * P), W = P / 2;
+    __shared__ __align__(16) float angle[kMostTokens][2][D / 2];  // cosines, sines
+    __shared__ float4 weight[2][2][W / 2][kLanes];  // of queries, keys; of u, v below; four values of a lane
     __shared__ Offsets offset[kMostTokens];
     pdl_launch_dependents();
     pdl_wait();
     const int64_t token0 = int64_t(blockIdx.x) * a.tokens;
     const int tokens = static_cast<int>(min(int64_t(a.tokens), a.total - token0));
-    const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
-    const int head0 = blockIdx.y * a.head_share, heads = min(a.head_share, a.heads + a.kv_heads - head0);
-    // Where the lane's two pieces lie in a head: neighbouring lanes' pieces are neighbours (with both
-    // pieces of a lane side by side, 32768 tokens of 40 heads took 150 us).
+    const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes, slot = row / a.head_share;
+    const int head = blockIdx.y * a.head_share + row - slot * a.head_share;
+    const bool is_q = head < a.heads, here = slot < a.slots && head < a.heads + a.kv_heads;
+    // Where a lane's two pieces lie in a head: neighbouring lanes' pieces are neighbours.
     const int half = a.rotary / 2, units = PAIRS ? 0 : half / P;
     const bool halves = !PAIRS && lane < units;
-    const int at0 = PAIRS || halves ? lane * P : a.rotary + (lane - units) * P;
-    const int at1 = PAIRS ? D / 2 + at0 : halves ? at0 + half : at0 + (kLanes - units) * P;
+    auto piece0 = [&](int l) { return PAIRS || l < units ? l * P : a.rotary + (l - units) * P; };
+    auto apart_of = [&](int l) { return PAIRS ? D / 2 : l < units ? half : (kLanes - units) * P; };
+    const int at0 = piece0(lane), apart = apart_of(lane);
     // (all tokens together are fewer than 2^31)
     auto place = [&](int t, uint32_t &seq) {
         const uint32_t token = static_cast<uint32_t>(token0) + t, n = static_cast<uint32_t>(a.n_tokens);
         seq = token / n;
         return token - seq * n;
     };
-    // a head of a token at a time; the first one's values are on their way before anything else
-    int t = 0, h = row;
-    auto settle = [&] {
-        while (h >= heads) {
-            h -= heads;
-            ++t;
-        }
-    };
+    const uint16_t *in = at0 + (is_q ? a.Q + head * a.q.head : a.K + (head - a.heads) * a.k.head);
     Piece x0, x1;
-    auto load = [&](int64_t q_at, int64_t k_at) {
-        const int at = head0 + h;
-        const uint16_t *p = at < a.heads ? a.Q + q_at + at * a.q.head : a.K + k_at + (at - a.heads) * a.k.head;
-        x0 = __ldcs(reinterpret_cast<const Piece *>(p + at0));
-        x1 = __ldcs(reinterpret_cast<const Piece *>(p + at1));
+    auto load = [&](int64_t at) {
+        x0 = __ldcs(reinterpret_cast<const Piece *>(in + at));
+        x1 = __ldcs(reinterpret_cast<const Piece *>(in + at + apart));
     };
-    settle();
+    // the first token's values are on their way before anything else
+    int t = here ? slot : tokens;
     if (t < tokens) {
         uint32_t seq;
         const int64_t i = place(t, seq);
-        load(seq * a.q.seq + i * a.q.token, seq * a.k.seq + i * a.k.token);
+        load(is_q ? seq * a.q.seq + i * a.q.token : seq * a.k.seq + i * a.k.token);
     }
-    for (int n = threadIdx.x; n < tokens; n += kRotaryThreads) {
+#pragma unroll 1
+    for (int n = threadIdx.x; n < tokens; n += blockDim.x) {
         uint32_t seq;
         const int64_t i = place(n, seq);
         offset[n] = Offsets{seq * a.q.seq + i * a.q.token, seq * a.k.seq + i * a.k.token,
                             seq * a.q_out.seq + i * a.q_out.token, seq * a.k_out.seq + i * a.k_out.token};
     }
-    for (int at = threadIdx.x; at < tokens * half; at += kRotaryThreads) {
-        uint32_t seq;
-        const int64_t i = place(at / half, seq);
-        const float2 cs = turn(a.start[seq] + i, a.freq[at % half]);
-        cosine[at / half][at % half] = cs.x;
-        sine[at / half][at % half] = cs.y;
+    const uint16_t *w = is_q ? a.q_weight : a.k_weight;
+    const bool normed = here && w != nullptr;
+#pragma unroll 1
+    for (int n = threadIdx.x; n < 2 * W * kLanes; n += blockDim.x) {
+        const int l = n % kLanes, i = n / kLanes % (W / 2), second = n / kLanes / (W / 2) & 1, of = n / kLanes / W;
+        const uint16_t *from = of == 0 ? a.q_weight : a.k_weight;
+        if (from == nullptr) continue;
+        from += piece0(l) + (PAIRS ? i * (D / 2) + second : second * apart_of(l) + 4 * i);
+        constexpr int kNext = PAIRS ? 2 : 1;
+        weight[of][second][i][l] = make_float4(widen<BF16>(from[0]), widen<BF16>(from[kNext]), widen<BF16>(from[2 * kNext]), widen<BF16>(from[3 * kNext]));
     }
-    for (int d = threadIdx.x; d < D; d += kRotaryThreads) {
-        if (a.q_weight != nullptr) weight[0][d] = widen<BF16>(a.q_weight[d]);
-        if (a.k_weight != nullptr) weight[1][d] = widen<BF16>(a.k_weight[d]);
+    const float4 *wl = &weight[is_q ? 0 : 1][0][0][lane];
+    // a warp 32 angles of a token; stored so that a lane's lie four at a time, its neighbours' beside them
+#pragma unroll 1
+    for (int n = threadIdx.x >> 5; n < tokens * (half > 32 ? 2 : 1); n += blockDim.x >> 5) {
+        const int of = half > 32 ? n >> 1 : n, pair = (half > 32 ? (n & 1) * 32 : 0) + (threadIdx.x & 31);
+        if (pair < half) {
+            uint32_t seq;
+            const int64_t i = place(of, seq);
+            const float2 cs = turn(a.start[seq] + i, a.freq[pair]);
+            const int at = PAIRS || P == 4 ? pair : (pair >> 2 & 1) * (D / 4) + (pair >> 3) * 4 + (pair & 3);
+            angle[of][0][at] = cs.x;
+            angle[of][1][at] = cs.y;
+        }
     }
     __syncthreads();
+    uint16_t *out = at0 + (is_q ? a.Q_out + head * a.q_out.head : a.K_out + (head - a.heads) * a.k_out.head);
+    const int64_t *offsets = is_q ? &offset[0].q : &offset[0].k;  // and of the output two further on
     while (t < tokens) {
-        const int at = head0 + h;
-        const bool is_q = at < a.heads;
-        const Piece now0 = x0, now1 = x1;
-        const uint32_t *p0 = reinterpret_cast<const uint32_t *>(&now0), *p1 = reinterpret_cast<const uint32_t *>(&now1);
-        uint16_t *out = is_q ? a.Q_out + offset[t].q_out + at * a.q_out.head : a.K_out + offset[t].k_out + (at - a.heads) * a.k_out.head;
-        const float *cos = cosine[t], *sin = sine[t];
-        h += kRows;
-        settle();
-        if (t < tokens) load(offset[t].q, offset[t].k);
-        float2 u[W], v[W];
+        const uint32_t *p0 = reinterpret_cast<const uint32_t *>(&x0), *p1 = reinterpret_cast<const uint32_t *>(&x1);
+        float2 u[W], v[W];  // partners: the halves' values, or the pairs' even and odd ones
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            u[i] = unpack2<BF16>(p0[i]);
-            v[i] = unpack2<BF16>(p1[i]);
+            if constexpr (PAIRS) {
+                const uint32_t *p = i < 2 ? p0 + 2 * i : p1 + 2 * (i - 2);
+                const float2 first = unpack2<BF16>(p[0]), second = unpack2<BF16>(p[1]);
+                u[i] = make_float2(first.x, second.x);
+                v[i] = make_float2(first.y, second.y);
+            } else {
+                u[i] = unpack2<BF16>(p0[i]);
+                v[i] = unpack2<BF16>(p1[i]);
+            }
         }
-        if ((is_q ? a.q_weight : a.k_weight) != nullptr) {
+        if (t + a.slots < tokens) load(offsets[4 * (t + a.slots)]);
+        if (normed) {
             float2 sums = mul2(u[0], u[0]);
 #pragma unroll
             for (int i = 1; i < W; ++i) sums = fma2(u[i], u[i], sums);
@@ -173,49 +189,54 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
             const float f = rsqrtf(sum * (1.0f / D) + a.eps);
-            const float4 *w0 = reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][at0]), *w1 = reinterpret_cast<const float4 *>(&weight[is_q ? 0 : 1][at1]);
             const float2 f2 = make_float2(f, f);
 #pragma unroll
             for (int i = 0; i < W; i += 2) {
-                const float4 g0 = w0[i / 2], g1 = w1[i / 2];
-                u[i] = mul2(u[i], mul2(make_float2(g0.x, g0.y), f2));
-                u[i + 1] = mul2(u[i + 1], mul2(make_float2(g0.z, g0.w), f2));
-                v[i] = mul2(v[i], mul2(make_float2(g1.x, g1.y), f2));
-                v[i + 1] = mul2(v[i + 1], mul2(make_float2(g1.z, g1.w), f2));
+                const float4 gu = wl[i / 2 * kLanes], gv = wl[(W / 2 + i / 2) * kLanes];
+                u[i] = mul2(mul2(u[i], f2), make_float2(gu.x, gu.y));
+                u[i + 1] = mul2(mul2(u[i + 1], f2), make_float2(gu.z, gu.w));
+                v[i] = mul2(mul2(v[i], f2), make_float2(gv.x, gv.y));
+                v[i + 1] = mul2(mul2(v[i + 1], f2), make_float2(gv.z, gv.w));
             }
         }
         // what is not turned stays as it is: a product with 0 would let an infinity through
-        auto rotate2 = [](float2 &a, float2 &b, float2 c, float2 s) {  // two pairs
-            const float2 y = fma2(a, c, mul2(b, make_float2(-s.x, -s.y)));
-            b = fma2(b, c, mul2(a, s));
-            a = y;
-        };
-        if constexpr (PAIRS) {
+        if (PAIRS ? half > 0 : halves) {
+            const float4 *cs = reinterpret_cast<const float4 *>(angle[t][0]) + lane;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float2 *s = i < 2 ? u + 2 * i : v + 2 * (i - 2);
-                const int pair = (i < 2 ? 0 : D / 4) + lane * 4 + (i & 1) * 2;
-                if (pair < half) {
-                    const float2 c = *reinterpret_cast<const float2 *>(cos + pair), sn = *reinterpret_cast<const float2 *>(sin + pair);
-                    float2 first = make_float2(s[0].x, s[1].x), second = make_float2(s[0].y, s[1].y);
-                    rotate2(first, second, c, sn);
-                    s[0] = make_float2(first.x, second.x);
-                    if (pair + 1 < half) s[1] = make_float2(first.y, second.y);
+            for (int i = 0; i < W; i += 2) {
+                const float4 c = cs[i / 2 * (D / 16)], s = cs[D / 8 + i / 2 * (D / 16)];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float2 ck = k == 0 ? make_float2(c.x, c.y) : make_float2(c.z, c.w), sk = k == 0 ? make_float2(s.x, s.y) : make_float2(s.z, s.w);
+                    float2 &x = u[i + k], &y = v[i + k];
+                    const float2 turned = fma2(x, ck, mul2(y, make_float2(-sk.x, -sk.y))), other = fma2(y, ck, mul2(x, sk));
+                    if (!PAIRS || half == D / 2) {
+                        x = turned;
+                        y = other;
+                    } else {
+                        const int pair = (i < 2 ? 0 : D / 4) + lane * 4 + 2 * k;
+                        if (pair < half) x.x = turned.x, y.x = other.x;
+                        if (pair + 1 < half) x.y = turned.y, y.y = other.y;
+                    }
                 }
             }
-        } else if (lane < units) {
-#pragma unroll
-            for (int i = 0; i < W; ++i)
-                rotate2(u[i], v[i], *reinterpret_cast<const float2 *>(cos + lane * P + 2 * i), *reinterpret_cast<const float2 *>(sin + lane * P + 2 * i));
         }
         Piece y0, y1;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            reinterpret_cast<uint32_t *>(&y0)[i] = pack2<BF16>(u[i].x, u[i].y);
-            reinterpret_cast<uint32_t *>(&y1)[i] = pack2<BF16>(v[i].x, v[i].y);
+            if constexpr (PAIRS) {
+                uint32_t *y = reinterpret_cast<uint32_t *>(i < 2 ? &y0 : &y1) + 2 * (i & 1);
+                y[0] = pack2<BF16>(u[i].x, v[i].x);
+                y[1] = pack2<BF16>(u[i].y, v[i].y);
+            } else {
+                reinterpret_cast<uint32_t *>(&y0)[i] = pack2<BF16>(u[i].x, u[i].y);
+                reinterpret_cast<uint32_t *>(&y1)[i] = pack2<BF16>(v[i].x, v[i].y);
+            }
         }
-        __stcs(reinterpret_cast<Piece *>(out + at0), y0);
-        __stcs(reinterpret_cast<Piece *>(out + at1), y1);
+        uint16_t *to = out + offsets[4 * t + 2];
+        t += a.slots;
+        __stcs(reinterpret_cast<Piece *>(to), y0);
+        __stcs(reinterpret_cast<Piece *>(to + apart), y1);
     }
 }
 
@@ -305,14 +326,20 @@ sp_status launch_qk_rotary(const QkRotary &r, cudaStream_t stream) {
     };
     // Values a piece: 8 where the layout and the halves allow it, else 4; else one by one.
     const int piece = in_pieces(8) && (r.pairs || r.rotary % 16 == 0) ? 8 : in_pieces(4) && !r.pairs && r.rotary % 8 == 0 ? 4 : 0;
-    // Whole tokens, several to a block once the device is full of blocks; few tokens are shared out by
-    // heads instead, each block working the angles out for itself.
-    const int heads = a.heads + a.kv_heads, rows = piece > 0 ? kRotaryThreads / (r.head_dim / (2 * piece)) : kRotaryThreads / 32;
-    a.tokens = static_cast<int>(std::max(int64_t(1), std::min(int64_t(kMostTokens), a.total / (148 * 8))));
-    a.head_share = heads;
-    while (a.head_share > rows && a.total * ((heads + a.head_share - 1) / a.head_share) < 148) a.head_share = (a.head_share + 1) / 2;
+    // A block has all of a token's heads where it has threads for them, and several tokens once the device
+    // (1280 threads an SM) is full three times over; few tokens are shared out by heads instead, each block
+    // working the angles out for itself.
+    const int heads = a.heads + a.kv_heads, lanes = piece > 0 ? r.head_dim / (2 * piece) : 32;
+    const int least = piece > 0 ? 64 / lanes : kRotaryThreads / 32;
+    a.head_share = piece > 0 ? (heads + (heads * lanes - 1) / kMostThreads) / ((heads * lanes - 1) / kMostThreads + 1) : heads;
+    while (a.head_share > least && a.total * ((heads + a.head_share - 1) / a.head_share) < 148) a.head_share = (a.head_share + 1) / 2;
+    const int parts = (heads + a.head_share - 1) / a.head_share;
+    const int full = 3 * 148 * std::max(1, 1280 / std::max(kFewThreads, a.head_share * lanes));
+    a.tokens = static_cast<int>(std::min(int64_t(kMostTokens), (a.total * parts + full - 1) / full));
+    a.slots = std::max(1, std::min(a.tokens, kFewThreads / (a.head_share * lanes)));
     const int64_t blocks = (a.total + a.tokens - 1) / a.tokens;
-    PdlConfig pdl(dim3(static_cast<unsigned>(blocks), (heads + a.head_share - 1) / a.head_share), dim3(kRotaryThreads), stream);
+    const int threads = piece > 0 ? (a.slots * a.head_share * lanes + 31) / 32 * 32 : kRotaryThreads;
+    PdlConfig pdl(dim3(static_cast<unsigned>(blocks), (heads + a.head_share - 1) / a.head_share), dim3(threads), stream);
     const bool bf16 = r.dtype == SP_BF16;
     cudaError_t e;
 #define SP_LAUNCH(D, PAIRS, P) \

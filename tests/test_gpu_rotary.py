@@ -134,3 +134,22 @@ def test_captured(sp):
     graph.replay()
     q, k = sp.sp_qk_norm_rotary(Q, K, start, freq)
     assert torch.equal(q, q2) and torch.equal(k, k2)
+
+
+@pytest.mark.parametrize("B,n,H,Hk,dim,rotary,pairs,norm", [
+    (3, 2501, 3, 1, 64, 64, True, "qk"),       # a block: several tokens at a time, and several turns of them
+    (7, 601, 1, 0, 64, 32, False, "q"),
+    (2, 1003, 20, 1, 128, 24, False, "k"),     # more heads than a block has threads for, pieces of four
+    (1, 2222, 43, 2, 128, 128, False, "qk"),   # more heads, pieces of eight
+    (2, 40, 130, 30, 64, 40, True, ""),        # few tokens, heads shared out
+])
+def test_tokens_and_heads_of_a_block(sp, B, n, H, Hk, dim, rotary, pairs, norm):
+    g = torch.Generator().manual_seed(H)
+    Q, K = (torch.randn(B, n, h, dim, generator=g).to(torch.bfloat16) for h in (H, Hk))
+    wq, wk = ((1 + 0.3 * torch.randn(dim, generator=g)).to(torch.bfloat16) if x in norm else None for x in "qk")
+    start, freq = [11 * b for b in range(B)], _freq(rotary)
+    dev = lambda t: None if t is None else t.cuda()
+    q, k = sp.sp_qk_norm_rotary(Q.cuda(), K.cuda(), torch.tensor(start, dtype=torch.int32).cuda(), freq.cuda(), q_weight=dev(wq),
+                                k_weight=dev(wk), pairs=pairs)
+    _check(q, Q, wq, start, freq, pairs, 1e-6)
+    _check(k, K, wk, start, freq, pairs, 1e-6)
