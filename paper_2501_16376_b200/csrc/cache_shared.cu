@@ -28,7 +28,7 @@
 // scores then wait for the weights' product to be done, not issued), P in two binary16 parts (saves a
 // sixth of the instructions, but ends at 2^-36 of the largest weight).
 // Measured (replayed from a graph, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
-// 128, 129 us (270 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 75 us; 16
+// 128, 128 us (271 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 74 us; 16
 // sequences of 4095 tokens, two queries each, 22.5 us; 4 sequences of 517 tokens, 16 heads of 64, 13.6 us.
 #include <algorithm>
 
@@ -129,8 +129,10 @@ __device__ __forceinline__ void store_shared16(uint32_t at, uint32_t a, uint32_t
 
 }  // namespace
 
+// (Binary16 queries and 128 rows: 80 registers are enough, where 88 or 96 would be taken, and leave room for two
+// or three more blocks of the tails beside: 64 sequences below 75.8 -> 74 us.  bf16 queries then spill.)
 template <bool BF16, int D, int TILES>
-__global__ void __launch_bounds__(PrefixTile<D, TILES>::kWarps * 32, 1)
+__global__ void __launch_bounds__(!BF16 && TILES == 1 ? 768 : PrefixTile<D, TILES>::kWarps * 32, 1)
 cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                     const __grid_constant__ PrefixArgs a) {
     using Tile = PrefixTile<D, TILES>;
