@@ -182,3 +182,42 @@ def test_captured_calls_with_new_values(sp):
         want = plain.reserve(values[2], 5)
         assert tuple(status.tolist()) == want and live.item() == plain.compact()
         plain.check(cache)
+
+
+def test_many_rows_of_a_large_pool(sp):
+    """32767 rows and 70000 blocks, against the same done with whole tensors."""
+    n_seqs, n_blocks, g = 32767, 70000, torch.Generator().manual_seed(9)
+    cache = sp.KvCache.pool(n_seqs, 32, n_blocks, 1, 64, 16)
+    cache.k.copy_(torch.randint(0, 256, cache.k.shape, generator=g, dtype=torch.uint8))
+    cache.v.copy_(torch.randint(0, 256, cache.v.shape, generator=g, dtype=torch.uint8))
+    used = torch.randperm(n_blocks, generator=g)[:20000].to(torch.int32)
+    table = torch.full((n_seqs, 2), -1, dtype=torch.int32)
+    table[torch.randperm(n_seqs, generator=g)[:20000], 0] = used
+    count = lambda t: torch.bincount(t[t >= 0].long().flatten(), minlength=n_blocks).to(torch.int32)
+    cache.table.copy_(table)
+    cache.refs.copy_(count(table))
+    # a row without a first block gets a free one, in the order of the rows
+    status = cache.sp_cache_reserve(torch.zeros(n_seqs, dtype=torch.int32, device="cuda"), 16)
+    free = torch.nonzero(count(table) == 0).flatten().to(torch.int32)
+    wants = table[:, 0] < 0
+    table[wants, 0] = free[:int(wants.sum())]
+    assert torch.equal(cache.table.cpu(), table) and torch.equal(cache.refs.cpu(), count(table))
+    assert status.tolist() == [0, n_blocks - n_seqs]
+    # rows change places
+    dst = torch.randperm(n_seqs, generator=g)[:20000].to(torch.int32)
+    src = torch.randint(-1, n_seqs, (20000,), generator=g, dtype=torch.int32)
+    cache.sp_cache_fork(dst.cuda(), src.cuda())
+    rows = torch.cat([table, torch.full((1, 2), -1, dtype=torch.int32)])   # the last one for -1
+    table[dst.long()] = rows[src.long()]
+    assert torch.equal(cache.table.cpu(), table) and torch.equal(cache.refs.cpu(), count(table))
+    # the same contents at the front of the pool
+    old_k, old_v, old = cache.k.cpu(), cache.v.cpu(), count(table)
+    n = cache.sp_cache_compact().item()
+    assert n == int((old > 0).sum())
+    new = cache.table.cpu()
+    named = table >= 0
+    assert torch.equal(new >= 0, named) and int(new.max()) < n and torch.equal(cache.refs.cpu(), count(new))
+    assert torch.equal(cache.k.cpu()[new[named].long()], old_k[table[named].long()])
+    assert torch.equal(cache.v.cpu()[new[named].long()], old_v[table[named].long()])
+    low = named & (table < n)
+    assert torch.equal(new[low], table[low])                                # those numbered below n stay
