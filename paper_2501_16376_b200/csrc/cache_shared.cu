@@ -28,8 +28,8 @@
 // scores then wait for the weights' product to be done, not issued), P in two binary16 parts (saves a
 // sixth of the instructions, but ends at 2^-36 of the largest weight).
 // Measured (replayed from a graph, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
-// 128, 128 us (271 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 74 us; 16
-// sequences of 4095 tokens, two queries each, 22.5 us; 4 sequences of 517 tokens, 16 heads of 64, 13.6 us.
+// 128, 128 us (271 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 72 us; 16
+// sequences of 4095 tokens, two queries each, 21.3 us; 4 sequences of 517 tokens, 16 heads of 64, 12.6 us.
 #include <algorithm>
 
 #include "cache_common.cuh"

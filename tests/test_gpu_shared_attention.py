@@ -367,3 +367,12 @@ def test_buffers_that_change_between_calls(sp):
     got = [(i % 3, run(into, cases[i % 3], False)) for i in range(60)]
     for i, o in got:
         assert torch.equal(o, want[i])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size,prefix,tail,heads,group,n_q", [(1, 9000, 300, 1, 5, 3), (2, 4500, 10, 1, 1, 1), (8, 3000, 200, 2, 8, 4), (1, 40, 2000, 2, 2, 1)])
+def test_few_rows_of_many_parts(sp, dtype, size, prefix, tail, heads, group, n_q):
+    cols = -(-(prefix + tail) // 64)
+    cache = _cache(sp, size, cols, heads, 64, 64, seed=size)
+    lens = [prefix + tail - 7 * b for b in range(size)]
+    _check(sp, cache, _queries(size, n_q, heads * group, 64, dtype, size), lens, cols * 64, [0, size], [prefix])
