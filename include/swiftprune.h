@@ -613,7 +613,8 @@ sp_status sp_cache_compact(const sp_cache *cache, const int32_t *refs, int32_t *
  * >= every prefix[g] and max_group >= the sequences of every group (tokens of a prefix past
  * max_prefix, and sequences past the first max_group of a group, are read through the sequences' own
  * rows).  Weights of the prefix, times their values' scale, enter their product to 2^-17 of themselves
- * (those of a sequence's own tokens as in sp_cache_attention); bf16 queries enter as they are.
+ * (those of a sequence's own tokens, and where max_group is 1, as in sp_cache_attention); bf16 queries enter
+ * as they are.
  * Limits as in sp_cache_attention, and n_groups and max_group at most 32767, n_kv_heads times the
  * group's rows (max_group * n_q * n_heads / n_kv_heads) over 256, rounded up, at most 65535 (else
  * SP_ERR_SHAPE).  O must not overlap Q or the workspace.

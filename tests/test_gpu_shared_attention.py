@@ -370,9 +370,17 @@ def test_buffers_that_change_between_calls(sp):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("size,prefix,tail,heads,group,n_q", [(1, 9000, 300, 1, 5, 3), (2, 4500, 10, 1, 1, 1), (8, 3000, 200, 2, 8, 4), (1, 40, 2000, 2, 2, 1)])
+@pytest.mark.parametrize("size,prefix,tail,heads,group,n_q", [(1, 9000, 300, 1, 5, 3), (2, 4500, 10, 1, 1, 1), (2, 9000, 300, 1, 5, 3), (2, 40, 2000, 2, 2, 1), (8, 3000, 200, 2, 8, 4), (1, 40, 2000, 2, 2, 1)])
 def test_few_rows_of_many_parts(sp, dtype, size, prefix, tail, heads, group, n_q):
     cols = -(-(prefix + tail) // 64)
     cache = _cache(sp, size, cols, heads, 64, 64, seed=size)
     lens = [prefix + tail - 7 * b for b in range(size)]
     _check(sp, cache, _queries(size, n_q, heads * group, 64, dtype, size), lens, cols * 64, [0, size], [prefix])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,group,n_q", [(4, 2, 1), (3, 8, 1), (2, 3, 4)])
+def test_groups_of_one(sp, dtype, heads, group, n_q):
+    """Every sequence alone: with enough kv heads and few rows, and otherwise."""
+    cache = _cache(sp, 4, 40, heads, 64, 32, seed=60 + heads)
+    _check(sp, cache, _queries(4, n_q, heads * group, 64, dtype, heads), [1280, 1100, 5, 700], 1280, [0, 1, 2, 3, 4], [1000, 1090, 64, 33])
