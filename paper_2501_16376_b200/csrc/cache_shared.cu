@@ -577,6 +577,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
                 tmem_store16(tmem + lanes + Tile::o(stream) + d, v);
             }
+            tmem_store_wait();  // a step may come here three times: a reference and two maxima that rise
             return true;
         };
         for (int turn = 0; turn < turns; ++turn) {

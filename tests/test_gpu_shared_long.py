@@ -1,0 +1,128 @@
+"""Attention over shared prefixes where a block takes many steps of 64 tokens, against its definition in
+binary64: rings that are used again and again, maxima and value scales that rise late."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def sp():
+    from paper_2501_16376_b200 import binding
+    binding.sp_wait_status(clear=True)
+    yield binding
+    assert binding.sp_wait_status() == 0                        # of everything in this file
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _cache(sp, n_seqs, cols, heads, dim, block, seed=0, spread=3, groups=None):
+    """Random finite codes and scales over 2^-spread .. 2^spread; rows with blocks of their own, those
+    of a group [(first, one past the last, blocks)] with the same first ones."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    table = torch.arange(n_seqs * cols).view(n_seqs, cols)
+    for first, end, shared in groups or ():
+        table[first:end, :shared] = table[first, :shared]
+    names, table = torch.unique(table, return_inverse=True)
+    n = len(names) + 3
+    order = torch.randperm(n, generator=torch.Generator().manual_seed(seed))
+    shape = (n, heads, block, dim)
+    k, v = ((torch.randn(shape, generator=g, device="cuda") * 100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+            for _ in range(2))
+    ks, vs = (torch.exp2(torch.randint(-spread, spread + 1, shape[:2], generator=g, device="cuda").float() - 7) for _ in range(2))
+    return sp.KvCache(k, v, ks, vs, order[table].to(torch.int32).cuda())
+
+
+def _queries(n_seqs, n_q, heads, dim, dtype, seed):
+    return torch.randn(n_seqs, n_q, heads, dim, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def _exact(cache, Q, lens, max_len, scale):
+    """(O, lse, weighted magnitudes of the values, largest sum of magnitudes behind a score), binary64;
+    every row of the table as it stands."""
+    B, n, Hq, D = Q.shape
+    H, T = cache.n_kv_heads, cache.block_tokens
+    O, mag = (torch.zeros(Q.shape, dtype=torch.float64, device="cuda") for _ in range(2))
+    lse = torch.full(Q.shape[:3], float("-inf"), dtype=torch.float64, device="cuda")
+    terms = torch.zeros_like(lse)
+    for b in range(B):
+        stored = max(0, min(int(lens[b]), max_len, cache.table.shape[1] * T))
+        if stored == 0:
+            continue
+        ids = cache.table[b, :(stored + T - 1) // T].long()
+        here = (ids >= 0) & (ids < cache.k.shape[0])
+        ids = torch.where(here, ids, 0)
+        dense = lambda c, s: (c[ids].view(torch.float8_e4m3fn).double() * s[ids].double()[..., None, None]).transpose(0, 1).reshape(H, -1, D)[:, :stored]
+        K, V = dense(cache.k, cache.k_scale), dense(cache.v, cache.v_scale)
+        q = Q[b].double().view(n, H, Hq // H, D).permute(1, 0, 2, 3)           # [H, n, group, D]
+        S = torch.einsum("hngd,hjd->hngj", q, K) * scale
+        size = torch.einsum("hngd,hjd->hngj", q.abs(), K.abs()) * abs(scale)
+        at = torch.arange(stored, device="cuda")
+        sees = (at <= int(lens[b]) - n + torch.arange(n, device="cuda")[:, None]) & here.repeat_interleave(T)[:stored]
+        sees = sees[None, :, None]
+        S = torch.where(sees, S, float("-inf"))
+        top = S.amax(-1, keepdim=True)
+        P = torch.where(sees, torch.exp(S - torch.where(top.isinf(), 0.0, top)), 0.0)
+        total = P.sum(-1, keepdim=True)
+        P = torch.where(total > 0, P / total, 0.0)
+        back = lambda t: t.permute(1, 0, 2, 3).reshape(n, Hq, -1)
+        O[b], mag[b] = back(torch.einsum("hngj,hjd->hngd", P, V)), back(torch.einsum("hngj,hjd->hngd", P, V.abs()))
+        lse[b] = back(torch.where(total > 0, total.log() + top, float("-inf")))[..., 0]
+        terms[b] = back(torch.where(sees, size, 0.0).amax(-1, keepdim=True))[..., 0]
+    return O, lse, mag, terms
+
+
+def _check(cache, Q, lens, max_len, starts, prefix, steps, scale=None, max_group=None):
+    """Half a step of the output and, from there on, roundings.  A score is a sum of D products, 16 at a
+    time, which the tensor cores cut to 2^-22: off by d = (D / 16 + 4) 2^-22 of its terms' magnitudes.  A
+    weight is then off by 4 d of itself (weight and sum), by 2^-17 where it enters its product in two
+    parts, by 2^-20 for the exponential and the additions.  An output is a sum of 8 products a step of 64
+    tokens, each cut to 2^-22 of what it is added to.  steps: of a block, at most."""
+    D = Q.shape[-1]
+    sc = D ** -0.5 if scale is None else scale
+    max_group = max(b - a for a, b in zip(starts, starts[1:])) if max_group is None else max_group
+    lse = torch.full(Q.shape[:3], 77.0, device="cuda")
+    O = cache.sp_cache_attention_shared(Q, _i32(lens), max_len, _i32(starts), _i32(prefix), max(prefix), max_group, scale=scale, lse=lse).double()
+    want, want_lse, mag, terms = _exact(cache, Q, lens, max_len, sc)
+    d = (D / 16 + 4) * 2.0 ** -22 * terms
+    bound = torch.finfo(Q.dtype).eps / 2 * want.abs() + (4 * d[..., None] + 2.0 ** -17 + 2.0 ** -20 + 8 * steps * 2.0 ** -22) * mag
+    bound += 2.0 ** (-25 if Q.dtype == torch.float16 else -134)
+    far = (O - want).abs() > bound
+    assert not far.any() and O.isfinite().all(), (far.nonzero()[:4], O[far][:4], want[far][:4], bound[far][:4])
+    empty = want_lse.isinf()
+    assert torch.equal(lse.isinf(), empty)
+    error = torch.where(empty, 0.0, lse.double() - torch.where(empty, 0.0, want_lse)).abs()
+    assert (error <= d + 2.0 ** -20 * (1 + want_lse.abs())).all()
+    return O
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size,dim", [(9, 64), (33, 128), (70, 64), (66, 128)])
+def test_maximum_and_value_scale_rise_in_one_step(sp, size, dim, dtype):
+    """40 (group, kv head) pairs each of two groups, so that a block takes all 16 steps of its prefix.  In the
+    twelfth, the maximum rises by 2^16 in its first 32 tokens and by 2^16 again in its second 32, and in
+    one of the runs the value scale by 2^45 as well: a rescaling that is lost leaves the earlier
+    tokens' sums 2^16 times too large, with values that show it."""
+    heads, block, group = 40, 32, 2
+    shared = 32
+    for jump in (0, 45):
+        starts = [0, size, size + 3]
+        cache = _cache(sp, size + 3, shared + 1, heads, dim, block, seed=size, groups=[(0, size, shared), (size, size + 3, shared)])
+        one = torch.ones(1).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        cache.k.zero_()
+        cache.k_scale.fill_(1.0)
+        cache.v_scale.fill_(2.0 ** (4 if jump == 0 else -30))
+        for first in (0, size):
+            row = cache.table[first].long()
+            late = row[22:24]                                   # places 704 .. 767: the twelfth step
+            cache.v_scale[late] = 2.0 ** (-6 if jump == 0 else jump - 30)
+            cache.k[late[0], :, 9, 0] = one                     # 16 above the rest
+            cache.k[late[1], :, 20, :2] = one                   # 32 above
+        Q = torch.zeros(size + 3, 1, heads * group, dim, device="cuda")
+        Q[..., 0] = Q[..., 1] = 16.0
+        lens = [shared * block + 1 + b % 20 for b in range(size + 3)]
+        _check(cache, Q.to(dtype), lens, (shared + 1) * block, starts, [shared * block] * 2, 16, scale=0.6931471805599453)
