@@ -236,13 +236,8 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
             mbar_fence_init();
         }
         __syncthreads();
-        // the kernel over the prefix has waited before it let this one start; its results are not
-        // read here.  What came before it is in the L2 cache by now: the fence drops what the L1 holds
-        // of older calls.
-        if constexpr (SHARED) {
-            __threadfence();
-            from = static_cast<int>(shared_blocks(a.groups, c, seq) << (shift - 4));
-        } else pdl_wait();
+        pdl_wait();
+        if constexpr (SHARED) from = static_cast<int>(shared_blocks(a.groups, c, seq) << (shift - 4));
     }
     const int len = static_cast<int>(max(int64_t(0), min(min(int64_t(a.lens[seq]), a.max_len), c.table_cols << shift)));
     const int own_from = a.n_q > 1 ? static_cast<int>(min(int64_t(len), max(int64_t(0), a.lens[seq] - a.n_q))) : len;
@@ -684,8 +679,6 @@ __device__ __forceinline__ void attention_block(const CUtensorMap &k_map, const 
                 }
                 if (here && g == 0) a.part_ml[p] = make_float2(m[n][i], sum);
             }
-        // this kernel does not end before the one over the prefixes: one block waits for all
-        if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) pdl_wait();
         return;
     }
 #pragma unroll
@@ -1050,15 +1043,16 @@ sp_status launch_cache_attention(const sp_cache &c, const void *Q, const sp_stri
     return check_launch();
 }
 
-// ------------------------------------------------------------------ beside a shared prefix
+// ------------------------------------------------------------------ behind a shared prefix
 //
-// The tokens behind a prefix are many short caches, with few rows each: blocks of one warp, 13 to 15 of
+// The tokens behind a prefix are many short caches, with few rows each: blocks of one warp, 16 of
 // which an SM holds, without a barrier between warps.  256 sequences of 150 to 330 own tokens, 8 heads: 30 us of
 // the whole device, bound by the issue and the fixed latencies of some 700 cycles a step of 16 tokens (blocks of four
-// warps: 35 us, and 8 us where a tail is one step).  They run beside the prefix on SMs of their own.
+// warps: 35 us, and 8 us where a tail is one step).  They start when the prefix is done: nothing lets a kernel
+// read what came before the one that it may overlap, but a wait for that one's end.
 
 // How many blocks, of a warp each, share the tail of a (sequence, kv head, row tile): `tail` estimates
-// its tokens.  16 fit on an SM; none has less than 64 tokens.
+// its tokens.  None has less than 64 tokens.
 int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail) {
     const int64_t units = std::max(int64_t(1), c.n_seqs * c.n_kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16));
     return static_cast<int>(std::max(int64_t(1), std::min({(tail + 63) / 64, int64_t(256), 148 * 16 / units})));
@@ -1078,10 +1072,8 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const int H = c.n_kv_heads, D = c.head_dim, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t seq = blockIdx.z, pair = seq * H + head;
     pdl_launch_dependents();
-    // what groups there are was known before the tails began (the fence as there)
-    __threadfence();
-    const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // else there are no parts of the prefix
     pdl_wait();
+    const int skip = shared_blocks(a.groups, c, seq) > 0 ? 0 : parts.prefix_splits;  // else there are no parts of the prefix
     const int each = (parts.splits - skip + share - 1) / share, begin = skip + warp % share * each, end = min(begin + each, parts.splits);
     const int at_once = (blockDim.x >> 5) / share;  // rows
     for (int row0 = blockIdx.x * at_once; row0 < a.rows; row0 += gridDim.x * at_once) {

@@ -27,9 +27,9 @@
 // pass over the scores for their maximum (1.2 us), two warps for the two products (1.3 us: the next
 // scores then wait for the weights' product to be done, not issued), P in two binary16 parts (saves a
 // sixth of the instructions, but ends at 2^-36 of the largest weight).
-// Measured (replayed from a graph, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
-// 128, 128 us (271 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 72 us; 16
-// sequences of 4095 tokens, two queries each, 21.3 us; 4 sequences of 517 tokens, 16 heads of 64, 12.6 us.
+// Measured (one call after another, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
+// 128, 127 us (274 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 83 us; 16
+// sequences of 4095 tokens, two queries each, 33 us; 4 sequences of 517 tokens, 16 heads of 64, 18.6 us.
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -129,10 +129,8 @@ __device__ __forceinline__ void store_shared16(uint32_t at, uint32_t a, uint32_t
 
 }  // namespace
 
-// (Binary16 queries and 128 rows: 80 registers are enough, where 88 or 96 would be taken, and leave room for two
-// or three more blocks of the tails beside: 64 sequences below 75.8 -> 74 us.  bf16 queries then spill.)
 template <bool BF16, int D, int TILES>
-__global__ void __launch_bounds__(!BF16 && TILES == 1 ? 768 : PrefixTile<D, TILES>::kWarps * 32, 1)
+__global__ void __launch_bounds__(PrefixTile<D, TILES>::kWarps * 32, 1)
 cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                     const __grid_constant__ PrefixArgs a) {
     using Tile = PrefixTile<D, TILES>;
@@ -186,9 +184,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
+    pdl_launch_dependents();
     pdl_wait();
-    __threadfence();
-    pdl_launch_dependents();  // the kernel over the tails counts on what came before this one
 
     const SharedGroup g = shared_group(a.groups, c, blockIdx.z);
     const int rows = static_cast<int>(max(int64_t(0), g.end - g.begin)) * a.rows;  // of the group
@@ -768,9 +765,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     }
 }
 
-// A block for every SM, as many stretches of a prefix as that gives; the tails' blocks, 15 to an SM, run
-// beside them on SMs of their own where they are few.  (The device's 148 SMs: the workspace is asked for
-// without a device.)
+// A block for every SM, as many stretches of a prefix as that gives.  (The device's 148 SMs: the workspace
+// is asked for without a device.)
 struct PrefixPlan {
     int tiles, row_tiles, splits, copies, tail_splits;
 };
@@ -788,9 +784,7 @@ static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     p.copies = all <= 64 ? 2 : 1;
     p.row_tiles = static_cast<int>((all + 128 * p.tiles - 1) / (128 * p.tiles));
     const int64_t units = s.n_groups * c.n_kv_heads * p.row_tiles, steps = (tokens + kStep - 1) / kStep;
-    const int64_t tails = (c.n_seqs * c.n_kv_heads * (rows <= 8 ? 1 : (rows + 15) / 16) * p.tail_splits + 14) / 15;
-    const int64_t sms = tails <= 48 ? 148 - tails : 148;
-    p.splits = static_cast<int>(std::max(int64_t(1), std::min((steps + 1) / 2, sms / units)));
+    p.splits = static_cast<int>(std::max(int64_t(1), std::min((steps + 1) / 2, 148 / units)));
     return p;
 }
 
