@@ -1089,8 +1089,10 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
             for (int w = 16; w > 0; w >>= 1) most = fmaxf(most, __shfl_xor_sync(kFullWarp, most, w));
             const float old = exp2_fast(top - most), f = exp2_fast(v.x - most);
             float total = f * v.y;
-            // the prefix's parts have been divided by their sums; one that saw nothing has no output
-            const float by = total == 0.0f ? 0.0f : s0 + lane < parts.prefix_splits ? total : f;
+            // the prefix's parts have been divided by their sums; one that saw nothing (but not one whose weights
+            // are 0 beside the others': its NaN counts) has no output
+            const float by = s0 + lane < parts.prefix_splits ? total : f;
+            const unsigned saw = __ballot_sync(kFullWarp, v.y != 0.0f);
 #pragma unroll
             for (int w = 16; w > 0; w >>= 1) total += __shfl_xor_sync(kFullWarp, total, w);
             sum = sum * old + total;
@@ -1101,7 +1103,7 @@ cache_shared_join_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
             for (int s = 0; s < n; ++s) {
                 const float g = __shfl_sync(kFullWarp, by, s);
                 float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (g != 0.0f && lane * 4 < D) x = *reinterpret_cast<const float4 *>(o + int64_t(s0 + s) * a.rows * D);
+                if ((saw >> s & 1u) != 0u && lane * 4 < D) x = *reinterpret_cast<const float4 *>(o + int64_t(s0 + s) * a.rows * D);
                 out[0] = fmaf(g, x.x, out[0]);
                 out[1] = fmaf(g, x.y, out[1]);
                 out[2] = fmaf(g, x.z, out[2]);

@@ -201,3 +201,31 @@ def test_the_same_from_call_to_call(sp):
         for _ in range(40):
             again = call()
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,group,n_q", [(2, 4, 1), (40, 1, 1), (2, 4, 4)])
+@pytest.mark.parametrize("low,high", [(100, 500), (500, 100), (100, 655), (655, 100), (655, 640)])
+def test_nan_far_below_the_maximum(sp, heads, group, n_q, low, high, dtype):
+    """A NaN value whose weight lies 2^-200 below the largest, in another stretch of the prefix, in the
+    tail, in the prefix under a maximum of the tail: it reaches its column of every row that sees it, as
+    in sp_cache_attention."""
+    size, block, shared = 5, 16, 40
+    cache = _cache(sp, size, shared + 2, heads, 64, block, seed=7, groups=[(0, size, shared)])
+    cache.k.zero_()
+    cache.k_scale.fill_(1.0)
+    one = torch.ones(1).to(torch.float8_e4m3fn).view(torch.uint8).item()
+    for b in range(size):
+        cache.k[cache.table[b, high // block].long(), :, high % block, 0] = one
+        cache.v[cache.table[b, low // block].long(), :, low % block, 9] = 0x7f
+    Q = torch.zeros(size, n_q, heads * group, 64, device="cuda")
+    Q[..., 0] = 16.0
+    lens = [672, 660, 657, 300, 660]
+    scale = 200 / 16 * 0.6931471805599453
+    call = dict(scale=scale)
+    O = cache.sp_cache_attention_shared(Q.to(dtype), _i32(lens), 672, _i32([0, size]), _i32([shared * block]), shared * block, size, **call)
+    alone = cache.sp_cache_attention(Q.to(dtype), _i32(lens), 672, **call)
+    sees = torch.tensor([[x - n_q + i >= low for i in range(n_q)] for x in lens], device="cuda")
+    want = torch.zeros(O.shape, dtype=torch.bool, device="cuda")
+    want[..., 9] = sees[..., None]
+    assert torch.equal(O.isnan(), want) and torch.equal(alone.isnan(), want)
