@@ -144,7 +144,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     __shared__ float4 scale_k[kScaleSlots];  // of 16 tokens each
     __shared__ int4 scale_v[kScaleSlots];    // as exponents, less the reference
     __shared__ int2 scale_info[kScaleSlots];                       // which of the four are there; the reference
-    __shared__ int all_see, any_nan, nan_from[D];
+    __shared__ int all_see, any_sees, any_nan, nan_from[D];  // tokens before which all rows see, some row sees
     __shared__ uint32_t row_top[2][128];
     const sp_cache &c = a.cache;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
@@ -174,6 +174,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
         failed = 0u;
         all_see = 0x7fffffff;
+        any_sees = 0;
         any_nan = 0;
         mbar_fence_init();
     }
@@ -214,7 +215,8 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         float ks = scale_of(c.k_scale, id), vs = scale_of(c.v_scale, id);
         float next_ks = scale_of(c.k_scale, next_id), next_vs = scale_of(c.v_scale, next_id);
         RingPlace<kScaleSlots> at;
-        bool ok = true;
+        // what lies behind all that the rows see may hold any scale, and must not become the reference
+        bool ok = mbar_wait_or_fail(smem_addr(&q_full), 0, &failed);
         for (int step = 0; step < count; ++step, at.next()) {
             const int turn = step % kHeld;
             if (step > 0 && turn == 0) {
@@ -228,14 +230,15 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             }
             // lanes 0 .. 3 take a piece of 16 tokens
             const int holder = turn * 4 + (lane & 3);
-            const int piece_id = __shfl_sync(kFullWarp, id, holder);
+            const int held_id = __shfl_sync(kFullWarp, id, holder);
+            const int piece_id = (first + step) * kStep + (lane & 3) * 16 < any_sees ? held_id : -1;
             const float piece_k = __shfl_sync(kFullWarp, ks, holder), piece_v = __shfl_sync(kFullWarp, vs, holder);
             const unsigned here = __ballot_sync(kFullWarp, piece_id >= 0) & 0xfu;
             int e = piece_id >= 0 ? exponent_of(piece_v) : -200;
             e = max(e, __shfl_xor_sync(kFullWarp, e, 1));
             e = max(e, __shfl_xor_sync(kFullWarp, e, 2));
             if (e > reference + kRaiseScale) reference = e;
-            if (step >= kScaleSlots) ok = mbar_wait_or_fail(smem_addr(&scale_empty[at.slot]), at.parity ^ 1u, &failed);
+            if (step >= kScaleSlots) ok = ok && mbar_wait_or_fail(smem_addr(&scale_empty[at.slot]), at.parity ^ 1u, &failed);
             if (!__all_sync(kFullWarp, ok)) break;
             if (lane < 4) {
                 reinterpret_cast<float *>(&scale_k[at.slot])[lane] = piece_k;
@@ -508,8 +511,11 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 const int64_t len = a.lens[seq];
                 limit = static_cast<int>(max(int64_t(-1), min(min(len - a.n_q + i, min(len, a.max_len) - 1), int64_t(tokens))));
             }
-            const int least = __reduce_min_sync(kFullWarp, limit);
-            if (lane == 0) atomicMin(&all_see, least + 1);
+            const int least = __reduce_min_sync(kFullWarp, limit), most = __reduce_max_sync(kFullWarp, valid ? limit : -1);
+            if (lane == 0) {
+                atomicMin(&all_see, least + 1);
+                atomicMax(&any_sees, most + 1);
+            }
             if constexpr (BF16) {
                 // sums of products with codes up to 448 stay in binary32's range
                 uint32_t top = 0;

@@ -229,3 +229,19 @@ def test_nan_far_below_the_maximum(sp, heads, group, n_q, low, high, dtype):
     want = torch.zeros(O.shape, dtype=torch.bool, device="cuda")
     want[..., 9] = sees[..., None]
     assert torch.equal(O.isnan(), want) and torch.equal(alone.isnan(), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,size", [(2, 4), (40, 4), (40, 70)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan"), 2.0 ** 127])
+def test_scales_that_no_row_sees(sp, bad, heads, size, dtype):
+    """Blocks of the prefix behind the longest sequence hold whatever memory held: their scales count for
+    nothing, as in sp_cache_attention, which does not read them."""
+    block, shared = 16, 48
+    cache = _cache(sp, size + 2, shared + 2, heads, 64, block, seed=8, groups=[(0, size, shared), (size, size + 2, shared)])
+    for first in (0, size):
+        row = cache.table[first].long()
+        cache.k_scale[row[33:]] = bad
+        cache.v_scale[row[33:]] = bad
+    lens = [33 * block - b % 9 for b in range(size + 1)] + [7]
+    _check(cache, _queries(size + 2, 1, heads, 64, dtype, 8), lens, (shared + 2) * block, [0, size, size + 2], [shared * block] * 2, 12)
