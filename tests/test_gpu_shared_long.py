@@ -245,3 +245,32 @@ def test_scales_that_no_row_sees(sp, bad, heads, size, dtype):
         cache.v_scale[row[33:]] = bad
     lens = [33 * block - b % 9 for b in range(size + 1)] + [7]
     _check(cache, _queries(size + 2, 1, heads, 64, dtype, 8), lens, (shared + 2) * block, [0, size, size + 2], [shared * block] * 2, 12)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [2, 16, 32])
+def test_sums_of_long_prefixes_do_not_shrink(sp, size, dtype):
+    """75 groups (so that the device has a block for every one) of one prefix of 131072 tokens, positive
+    values.  The tensor cores cut what they add to: at most 1024 products (128 steps) in a row take less
+    than 2^-13 off (each less than 2^-23), and 2^-15 on average (a cut is half of that, a sum half of its
+    last value).  With scores of deviation 2.4 some 400 tokens count, outputs of a column differ from row to
+    row by more than the type's steps, and their own roundings have a mean of 0 (six deviations of it
+    are allowed); with an eighth of that they nearly agree and round alike, so their mean says nothing."""
+    groups, heads, T, tokens = 75, 8, 64, 131072
+    g = torch.Generator(device="cuda").manual_seed(size)
+    shape = (tokens // T, 1, T, 64)
+    k = (torch.randn(shape, generator=g, device="cuda") * 40).to(torch.float8_e4m3fn)
+    v = (torch.rand(shape, generator=g, device="cuda") * 200 + 100).to(torch.float8_e4m3fn)
+    one = torch.full(shape[:2], 2.0 ** -7, device="cuda")
+    table = torch.arange(shape[0], dtype=torch.int32, device="cuda").repeat(groups * size, 1)
+    cache = sp.KvCache(k.view(torch.uint8), v.view(torch.uint8), one, one.clone(), table)
+    Q = _queries(groups * size, 1, heads, 64, dtype, size)
+    K, V = (x.view(-1, 64).double() * 2.0 ** -7 for x in (k, v))
+    rows = torch.randperm(groups * size * heads, generator=torch.Generator().manual_seed(1))[:1024].cuda()
+    for scale in (1 / 8, 1.0):
+        O = cache.sp_cache_attention_shared(Q, _i32([tokens] * (groups * size)), tokens, _i32([i * size for i in range(groups + 1)]),
+                                            _i32([tokens] * groups), tokens, size, scale=scale)
+        want = torch.softmax(Q.view(-1, 64)[rows].double() @ K.T * scale, -1) @ V
+        error = (O.view(-1, 64)[rows].double() - want) / want
+        assert error.abs().max() <= torch.finfo(dtype).eps / 2 + 2.0 ** -13
+    assert error.mean().abs() <= 2.0 ** -15 + 6 * torch.finfo(dtype).eps / 2 / error.numel() ** 0.5
