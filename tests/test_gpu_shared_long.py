@@ -26,7 +26,7 @@ def _cache(sp, n_seqs, cols, heads, dim, block, seed=0, spread=3, groups=None):
     g = torch.Generator(device="cuda").manual_seed(seed)
     table = torch.arange(n_seqs * cols).view(n_seqs, cols)
     for first, end, shared in groups or ():
-        table[first:end, :shared] = table[first, :shared]
+        table[first:end, :shared] = table[first, :shared].clone()
     names, table = torch.unique(table, return_inverse=True)
     n = len(names) + 3
     order = torch.randperm(n, generator=torch.Generator().manual_seed(seed))
@@ -274,3 +274,71 @@ def test_sums_of_long_prefixes_do_not_shrink(sp, size, dtype):
         error = (O.view(-1, 64)[rows].double() - want) / want
         assert error.abs().max() <= torch.finfo(dtype).eps / 2 + 2.0 ** -13
     assert error.mean().abs() <= 2.0 ** -15 + 6 * torch.finfo(dtype).eps / 2 / error.numel() ** 0.5
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("size", [10, 25, 50])
+def test_blocks_of_many_steps(sp, size, dim, dtype):
+    """8 groups of 16 kv heads, a block for each with all 24 steps of its prefix: 40, 100 and 200 rows.  Random
+    scores; scores that rise with every step, by less and by more than a weight may exceed the maximum;
+    value scales that rise by 2^45 in the 17th step."""
+    heads, block, group, groups, shared = 16, 32, 4, 8, 47
+    n, tokens = groups * size, 47 * 32
+    starts = [i * size for i in range(groups + 1)]
+    cache = _cache(sp, n, shared + 2, heads, dim, block, seed=size, groups=[(a, a + size, shared) for a in starts[:-1]])
+    Q = _queries(n, 1, heads * group, dim, dtype, size)
+    lens = [tokens + 1 + (7 * b) % 64 if b % 9 else 700 + 11 * (b % 50) for b in range(n)]
+    call = dict(lens=lens, max_len=tokens + 64, starts=starts, prefix=[tokens + 5 * (i % 3) for i in range(groups)], steps=24)
+    _check(cache, Q, **call)
+    begin = cache.v_scale.clone()
+    for first in starts[:-1]:
+        cache.v_scale[cache.table[first, 34:].long()] *= 2.0 ** 45
+    if dtype == torch.float16:
+        cache.v_scale *= 2.0 ** -45
+    _check(cache, Q, **call)
+    cache.v_scale.copy_(begin)
+    place = torch.arange(tokens + 64).view(-1, block)
+    codes = torch.stack([place // 128, place // 64 % 2, place % 64 // 8], -1).float().to(torch.float8_e4m3fn).view(torch.uint8).cuda()
+    for b in range(n):
+        cache.k[cache.table[b].long(), :, :, :3] = codes[:, None]
+    scale = cache.k_scale.fill_(1.0)
+    cache.k[..., 3:] = 0
+    for rise in (4.0, 24.0):
+        Q[..., 0], Q[..., 1], Q[..., 2] = 2 * rise, rise, rise / 8
+        _check(cache, Q, scale=1.0, **call)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n_q,max_group", [(1, 9), (2, 9), (1, 3)])
+def test_a_hundred_groups_of_all_sizes(sp, n_q, max_group, dtype):
+    """Groups of 0 to 9 sequences, prefixes from nothing to all of a sequence, sequences of no group before and
+    behind them, sequences past max_group."""
+    g = torch.Generator().manual_seed(n_q)
+    sizes = [int(x) for x in torch.randint(0, 10, (100,), generator=g)]
+    starts = [3]
+    for s in sizes:
+        starts.append(starts[-1] + s)
+    n, block, cols = starts[-1] + 5, 16, 30
+    prefix = [int(x) for x in torch.randint(0, 29 * block, (100,), generator=g)]
+    cache = _cache(sp, n, cols, 3, 64, block, seed=n_q, groups=[(a, b, p // block) for a, b, p in zip(starts, starts[1:], prefix) if b > a])
+    lens = [int(x) for x in torch.randint(0, cols * block + 1, (n,), generator=g)]
+    _check(cache, _queries(n, n_q, 6, 64, dtype, 1), lens, cols * block, starts, prefix, 8, max_group=max_group)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,group,dim", [(2, 4, 128), (40, 1, 64), (8, 12, 64)])
+def test_long_tails_beside_a_long_prefix(sp, heads, group, dim, dtype):
+    """A sequence of no group and a group with a short prefix beside a group with a long one: their tails are
+    nearly all they have, many steps for one warp.  bf16 queries with channels far below the largest too."""
+    block, cols, size = 64, 126, 12
+    starts, prefix = [0, size, size + 3], [8000, 64]
+    cache = _cache(sp, size + 4, cols, heads, dim, block, seed=heads, groups=[(0, size, 125), (size, size + 3, 1)])
+    lens = [8001 + 3 * b for b in range(size)] + [3000, 3217, 64, 8000]
+    Q = _queries(size + 4, 1, heads * group, dim, dtype, heads)
+    _check(cache, Q, lens, cols * block, starts, prefix, 125)
+    if dtype == torch.bfloat16:
+        cache.k[..., 5] = 0
+        Q[::2, ..., 5] = 2.0 ** 100
+        Q[1::3, ..., :3] *= 2.0 ** -60
+        _check(cache, Q, lens, cols * block, starts, prefix, 125)
