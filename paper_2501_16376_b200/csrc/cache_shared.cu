@@ -11,7 +11,7 @@
 // e4m3 converts exactly to binary16 and bf16, and the queries enter as they are.  P times the value
 // scale enters in two bf16 parts: 2^-18 of itself, with binary32's range, so that no scale needs a
 // reference but in the last exponents.  A thread owns a row: its maximum and sum stay in registers,
-// and nothing crosses lanes.  The maximum is raised only when weights reach 2^14, which spares a pass
+// and nothing crosses lanes.  The maximum is raised only when weights exceed 2^14, which spares a pass
 // over the scores.
 //
 // Two groups of four softmax warps, each with sums of its own, hide one another's latency: with 256
@@ -41,7 +41,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;
-constexpr float kRaise = 16384.0f;   // weights of 16 tokens whose sum reaches this raise the maximum
+constexpr float kRaise = 16384.0f;   // weights of 32 tokens whose sum exceeds this raise the maximum
 constexpr int kScaleSlots = 8;       // steps of scales
 constexpr float kFarMaximum = 16777216.0f;  // 2^24: the maximum's own rounding is off by 1 from here on
 constexpr int kFarScale = -40;       // of a value scale below the reference
