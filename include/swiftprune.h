@@ -612,9 +612,10 @@ sp_status sp_cache_compact(const sp_cache *cache, const int32_t *refs, int32_t *
  * accumulated weights: queries see the tokens up to their own place, in the prefix too.  max_prefix
  * >= every prefix[g] and max_group >= the sequences of every group (tokens of a prefix past
  * max_prefix, and sequences past the first max_group of a group, are read through the sequences' own
- * rows).  Weights of the prefix, times their values' scale, enter their product to 2^-17 of themselves
- * (those of a sequence's own tokens, and where max_group is 1, as in sp_cache_attention); bf16 queries enter
- * as they are.
+ * rows).  Weights, times their values' scale, enter their product to 2^-17 of themselves or better, unless
+ * that scale lies more than 2^100 below the largest in the prefix that a query of the group sees (from 2^126
+ * on they may count as 0); sums over the prefix may fall short of themselves by 2^-15.  bf16 queries enter as
+ * they are or as in sp_cache_attention.
  * Limits as in sp_cache_attention, and n_groups and max_group at most 32767, n_kv_heads times the
  * group's rows (max_group * n_q * n_heads / n_kv_heads) over 256, rounded up, at most 65535 (else
  * SP_ERR_SHAPE).  O must not overlap Q or the workspace.

@@ -342,3 +342,18 @@ def test_long_tails_beside_a_long_prefix(sp, heads, group, dim, dtype):
         Q[::2, ..., 5] = 2.0 ** 100
         Q[1::3, ..., :3] *= 2.0 ** -60
         _check(cache, Q, lens, cols * block, starts, prefix, 125)
+
+
+@pytest.mark.parametrize("size", [6, 40, 70])
+def test_value_scales_that_others_see(sp, size):
+    """bf16: sequences that end before blocks whose value scales lie 2^100 above theirs."""
+    heads, block, shared = 40, 32, 36
+    cache = _cache(sp, size + 2, shared + 1, heads, 64, block, seed=size, groups=[(0, size, shared), (size, size + 2, shared)])
+    for first in (0, size):
+        row = cache.table[first].long()
+        cache.v_scale[row[:20]] *= 2.0 ** -60
+        cache.v_scale[row[20:]] = 2.0 ** 37
+        cache.v_scale[row[:20]] = cache.v_scale[row[:20]].clamp(min=2.0 ** -63)
+    lens = [(20 * block - b % 40) if b % 3 else (shared * block + 1 + b % 20) for b in range(size + 2)]
+    _check(cache, _queries(size + 2, 1, heads * 2, 64, torch.bfloat16, size), lens, (shared + 1) * block, [0, size, size + 2],
+           [shared * block] * 2, 18)
