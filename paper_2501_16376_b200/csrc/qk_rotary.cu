@@ -61,6 +61,12 @@ __device__ __forceinline__ float2 turn(int64_t place, float freq) {
     return cs;
 }
 
+// Whether binary32 holds a row's mean of squares with all its bits (always, of binary16); otherwise the row
+// is taken times row_scale, and eps times its square.
+template <bool BF16>
+__device__ __forceinline__ bool plain_mean(float mean) { return !BF16 || (mean > 0x1p-100f && mean < 0x1p126f); }
+__device__ __forceinline__ float row_scale(float mean) { return mean > 1.0f ? 0x1p-70f : 0x1p80f; }
+
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     if constexpr (BF16) {
@@ -188,7 +194,21 @@ qk_rotary_kernel(const __grid_constant__ RotaryArgs a) {
             const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
-            const float f = rsqrtf(sum * (1.0f / D) + a.eps);
+            const float mean = sum * (1.0f / D) + a.eps;
+            float f = rsqrtf(mean);
+            if (!plain_mean<BF16>(mean)) {
+                const float by = row_scale(mean);
+                sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    u[i] = mul2(u[i], make_float2(by, by));
+                    v[i] = mul2(v[i], make_float2(by, by));
+                    sum = fmaf(u[i].x, u[i].x, fmaf(u[i].y, u[i].y, fmaf(v[i].x, v[i].x, fmaf(v[i].y, v[i].y, sum))));
+                }
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
+                f = rsqrtf(sum * (1.0f / D) + a.eps * by * by);
+            }
             const float2 f2 = make_float2(f, f);
 #pragma unroll
             for (int i = 0; i < W; i += 2) {
@@ -275,8 +295,20 @@ qk_rotary_any_kernel(const __grid_constant__ RotaryArgs a) {
         if (w != nullptr) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFullWarp, sum, o);
-            const float f = rsqrtf(sum / D + a.eps);
-            for (int d = lane; d < D; d += 32) value[warp][d] *= f * widen<BF16>(w[d]);
+            const float mean = sum / D + a.eps;
+            float f = rsqrtf(mean);
+            if (!plain_mean<BF16>(mean)) {
+                const float by = row_scale(mean);
+                sum = 0.0f;
+                for (int d = lane; d < D; d += 32) {
+                    const float v = value[warp][d] *= by;
+                    sum = fmaf(v, v, sum);
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFullWarp, sum, o);
+                f = rsqrtf(sum / D + a.eps * by * by);
+            }
+            for (int d = lane; d < D; d += 32) value[warp][d] = value[warp][d] * f * widen<BF16>(w[d]);
         }
         __syncwarp();
         for (int d = lane; d < D; d += 32) {
