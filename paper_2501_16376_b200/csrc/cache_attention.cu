@@ -1060,8 +1060,7 @@ int shared_tail_splits(const sp_cache &c, int64_t rows, int64_t tail) {
 
 // Blocks join the rows of a (sequence, kv head), four columns a lane at a time.  Rows of many parts have several
 // warps each (`share`), whose sums are joined again at the end: a warp that takes part after part is bound by the
-// latency of its reads (2 rows of 156 parts, a sequence alone with 13726 tokens: 39.5 us for the whole call, 18.5 with
-// eight warps a row).
+// latency of its reads (40 rows of 225 parts: 70 us for the whole call, 32 with eight warps a row).
 constexpr int kSharedJoinWarps = 8;
 template <bool BF16>
 __global__ void __launch_bounds__(kSharedJoinWarps * 32)
@@ -1194,8 +1193,8 @@ sp_status launch_cache_tails(const sp_cache &c, const SharedAttention &s, const 
     if (e != cudaSuccess) return cuda_fail(e);
     sp_status st = check_launch();
     if (st != SP_OK) return st;
-    // (whole calls: 1024 rows of 28 parts 21.3 us with four warps a row, 25 with eight, 23 with one; 40 rows of 151 parts 22,
-    // 18, 43; 2560 rows of 7 parts 75.8, 84, 72.3)
+    // (whole calls: 1024 rows of 23 parts 32.7 us with four warps a row, 35 with eight, 36 with one; 40 rows of 225 parts 38,
+    // 32, 70; 2560 rows of 7 parts 86, 91, 83)
     const int64_t all_rows = c.n_seqs * c.n_kv_heads * a.rows;
     const int share = parts.splits < 8 ? 1 : all_rows <= 148 * 2 ? 8 : 4;
     const int at_once = share > 1 ? 1 : std::min(a.rows, 4), blocks = std::min((a.rows + at_once - 1) / at_once, 64);

@@ -27,9 +27,9 @@
 // pass over the scores for their maximum (1.2 us), two warps for the two products (1.3 us: the next
 // scores then wait for the weights' product to be done, not issued), P in two binary16 parts (saves a
 // sixth of the instructions, but ends at 2^-36 of the largest weight).
-// Measured (one call after another, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
-// 128, 127 us (274 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 83 us; 16
-// sequences of 4095 tokens, two queries each, 33 us; 4 sequences of 517 tokens, 16 heads of 64, 18.6 us.
+// Measured (replayed from a graph, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
+// 128, 124 us (280 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 83 us; 16
+// sequences of 4095 tokens, two queries each, 33 us; 4 sequences of 517 tokens, 16 heads of 64, 17.3 us.
 #include <algorithm>
 
 #include "cache_common.cuh"
