@@ -24,11 +24,10 @@
 // tensor pipe 35 %.  A block starts and ends in 10 us (queries, first scores; sums written).  What did
 // not pay: one group of softmax warps (2.2 us a step), conversion of keys and values by the same warps
 // (a step's values wait for the product two steps before, and the next keys behind them: 2.4 us), a
-// pass over the scores for their maximum (1.2 us), two warps for the two products (1.3 us: the next
-// scores then wait for the weights' product to be done, not issued), P in two binary16 parts (saves a
+// pass over the scores for their maximum (1.2 us), two warps for the two products (1.3 us), P in two binary16 parts (saves a
 // sixth of the instructions, but ends at 2^-36 of the largest weight).
 // Measured (replayed from a graph, tails and join included): 8 x 32 sequences of 8191 tokens, 32 heads over 8 of
-// 128, 124 us (280 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 83 us; 16
+// 128, 126 us (276 TFLOP/s; 15.3 ms with a warp a query); 64 sequences of 8191 tokens, 40 heads, 84 us; 16
 // sequences of 4095 tokens, two queries each, 33 us; 4 sequences of 517 tokens, 16 heads of 64, 17.3 us.
 #include <algorithm>
 
@@ -140,7 +139,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     constexpr int kSlots = Tile::kSlots, kBuffers = Tile::kBuffers, kSoftmaxWarps = Tile::kSoftmaxWarps;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t raw_full[kSlots], raw_empty[kSlots], k_full[kConverted], k_empty[kConverted], v_full[kConverted], v_empty[kConverted];
-    __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], drained;
+    __shared__ uint64_t s_full[kBuffers], p_full[kBuffers], weighed_first, drained;
     __shared__ uint32_t tmem_base, failed, present[kSlots];
     __shared__ float4 group_sums[2][128];  // TILES == 1: maximum, sum, 2^reference of a group's rows
     __shared__ uint64_t q_full, scale_full[kScaleSlots], scale_empty[kScaleSlots];
@@ -170,6 +169,7 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             mbar_init(smem_addr(&p_full[b]), 4);
         }
         mbar_init(smem_addr(&drained), 1);
+        mbar_init(smem_addr(&weighed_first), 1);
         mbar_init(smem_addr(&q_full), kSoftmaxWarps);
         for (int i = 0; i < kScaleSlots; ++i) {
             mbar_init(smem_addr(&scale_full[i]), 1);
@@ -286,9 +286,10 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             for (int s = max(0, issued - kSlots); s < issued; ++s) mbar_wait(smem_addr(&raw_full[s % kSlots]), (s / kSlots) & 1);
     } else if (warp == kProducts) {
         // ---- products.  The warp walks the loop together and elects a thread for the instructions alone:
-        // operands then stay in uniform registers.  They run in the order of their issue: a step's scores
-        // go where the weights of three steps before (with 256 rows: of the step before) were, right behind
-        // the product that reads those.
+        // operands then stay in uniform registers.  A step's scores go where the weights of three steps before
+        // (with 256 rows: of the step before) were, once the product that reads those is done: products are only
+        // promised to run in the order of their issue where accumulator and shape are the same (right behind
+        // it: 1 to 5 % less for a call, 7 % at worst).
         const uint32_t qk = f16_instruction(kStep, BF16), pv = f16_instruction(D, true) | kColumnsB;
         const uint32_t base = __shfl_sync(kFullWarp, tmem, 0);
         const int steps_here = __shfl_sync(kFullWarp, count, 0);
@@ -318,31 +319,42 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         bool ok = all(mbar_wait_or_fail(smem_addr(&q_full), 0, &failed));
         if constexpr (TILES == 1) {
             // Whichever product has its operands goes next (in a fixed order, 16 rows took 0.86 us a step
-            // for 0.77; the looks at the barriers overlap).
+            // for 0.77).  The lanes look at the four barriers at once: weights, values, keys, the scores' place.
             int scored = 0, weighed = 0;
+            const int which = lane & 3;
+            const uint32_t bars = smem_addr(which == 0 ? p_full : which == 1 ? v_full : which == 2 ? k_full : v_empty);
+            RingPlace<3> weigh_at, score_at;
             for (uint32_t idle = 0; ok && weighed < steps_here;) {
-                const bool p_ready = mbar_test(smem_addr(&p_full[weighed % 3]), weighed / 3 & 1);
-                const bool v_ready = mbar_test(smem_addr(&v_full[weighed % 3]), weighed / 3 & 1);
-                const bool k_ready = mbar_test(smem_addr(&k_full[scored % 3]), scored / 3 & 1);
-                const bool weigh = __all_sync(kFullWarp, p_ready && v_ready) && weighed < scored;
-                const bool score = __all_sync(kFullWarp, k_ready) && scored < steps_here && scored - weighed - (weigh ? 1 : 0) < 3;
+                // (a place that has not been used yet counts as free: its phase before)
+                const bool ready = mbar_test(bars + 8 * (which < 2 ? weigh_at.slot : score_at.slot),
+                                             which < 2 ? weigh_at.parity : score_at.parity ^ (which == 3 ? 1u : 0u));
+                const unsigned looks = __ballot_sync(kFullWarp, ready);
+                const bool weigh = (looks & 3u) == 3u && weighed < scored;
+                const bool score = (looks & 12u) == 12u && scored < steps_here && scored - weighed < 3;
                 if (!weigh && !score) {
-                    if (++idle > kWaitLimit) mbar_give_up(&failed);
-                    ok = __all_sync(kFullWarp, *static_cast<volatile uint32_t *>(&failed) == 0u);
+                    if (++idle > kWaitLimit && lane == 0) mbar_give_up(&failed);
+                    if (idle > kWaitLimit || (idle & 15u) == 0u) ok = __all_sync(kFullWarp, *static_cast<volatile uint32_t *>(&failed) == 0u);
                     continue;
                 }
                 idle = 0;
+                __syncwarp();
                 tcgen05_fence_after();
                 if (elect_one()) {
                     if (weigh) values(0, weighed);
                     if (score) scores(0, scored);
                 }
                 __syncwarp();
-                weighed += weigh;
-                scored += score;
+                if (weigh) {
+                    ++weighed;
+                    weigh_at.next();
+                }
+                if (score) {
+                    ++scored;
+                    score_at.next();
+                }
             }
         } else {
-            // two tiles in turn: a step's scores right behind the step before (as above, 12 % more)
+            // two tiles in turn (as above, 12 % more)
             if (ok && steps_here > 0 && (ok = all(mbar_wait_or_fail(smem_addr(&k_full[0]), 0, &failed)))) {
                 if (elect_one()) {
                     scores(0, 0);
@@ -361,8 +373,14 @@ cache_prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                     if (!ok) break;
                     if (elect_one()) {
                         values(t, step);
-                        if (next < steps_here) scores(t, next);
+                        if (t == 0) tcgen05_commit(smem_addr(&weighed_first));
                     }
+                    __syncwarp();
+                    if (next >= steps_here) continue;
+                    ok = all(t == 0 ? mbar_wait_or_fail(smem_addr(&weighed_first), step & 1, &failed)
+                                    : mbar_wait_or_fail(smem_addr(&v_empty[step % kConverted]), v_use, &failed));
+                    if (!ok) break;
+                    if (elect_one()) scores(t, next);
                     __syncwarp();
                 }
             }
