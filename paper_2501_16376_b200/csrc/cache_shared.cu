@@ -805,9 +805,10 @@ static PrefixPlan prefix_plan(const sp_cache &c, const SharedAttention &s) {
     if (s.n_groups == 0 || all == 0 || blocks == 0) return p;
     // A sequence alone in its group shares nothing, and its few rows leave the products' 128 idle: the
     // kernel without groups is faster with up to 8 rows (4 rows, 8000 tokens: 21 us for 28 with one (sequence,
-    // kv head), 22 for 33 with 8, 30 for 86 with 64; 2 rows of 13726 tokens: 27 for 27), and with more once
-    // there are enough of them (16 rows, 8000 tokens: 49 us for 42 with 16, 52 for 57 with 32, 100 for 144 with 128).
-    if (std::min(s.max_group, c.n_seqs) == 1 && (rows <= 8 || c.n_seqs * c.n_kv_heads >= 32)) return p;
+    // kv head), 22 for 33 with 8, 30 for 86 with 64; 2 rows of 13726 tokens: 27 for 27), and with up to 16 once
+    // there are enough of them (8000 tokens: 50 us for 42 with 16, 53 for 60 with 32, 100 for 149 with 128); with 32
+    // rows it takes 69 for 61 with 32, 174 for 163 with 128, and twice that for 64.
+    if (std::min(s.max_group, c.n_seqs) == 1 && (rows <= 8 || (rows <= 16 && c.n_seqs * c.n_kv_heads >= 32))) return p;
     p.tiles = all <= 128 ? 1 : 2;
     p.copies = all <= 64 ? 2 : 1;
     p.row_tiles = static_cast<int>((all + 128 * p.tiles - 1) / (128 * p.tiles));

@@ -357,3 +357,13 @@ def test_value_scales_that_others_see(sp, size):
     lens = [(20 * block - b % 40) if b % 3 else (shared * block + 1 + b % 20) for b in range(size + 2)]
     _check(cache, _queries(size + 2, 1, heads * 2, 64, torch.bfloat16, size), lens, (shared + 1) * block, [0, size, size + 2],
            [shared * block] * 2, 18)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n_q,group", [(2, 4), (4, 4), (5, 4), (40, 4)])
+def test_sequences_alone_of_few_and_many_queries(sp, n_q, group, dtype):
+    """Groups of one on both sides of the rule for them: 8, 16, 20 and 160 rows, 16 and 40 (sequence, kv head)."""
+    for heads, size in ((8, 2), (8, 5)):
+        cache = _cache(sp, size, 40, heads, 64, 32, seed=n_q)
+        lens = [1280 - 7 * b for b in range(size)]
+        _check(cache, _queries(size, n_q, heads * group, 64, dtype, n_q), lens, 1280, list(range(size + 1)), [1200 - 40 * b for b in range(size)], 19)
